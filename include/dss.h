@@ -402,6 +402,107 @@ dss_status dss_frag(int32_t k_h, int32_t k_w, int32_t S_h, int32_t S_w, int32_t 
 dss_status dss_defrag(int32_t k_h, int32_t k_w, int32_t S_h, int32_t S_w, int32_t C, int32_t H,
                       int32_t W, dss_dtype dtype, const void* in, void* out, hipStream_t stream);
 
+/* ---------------------------------------------------------------- gradient norm and clipping */
+
+/* One tensor of a list: `count` elements, contiguous (in any order of the axes),
+ * aligned to their own size.  An empty tensor's data may be NULL. */
+typedef struct dss_tensor {
+    const void* data;       /* device */
+    int64_t count;
+    int32_t dtype;          /* dss_dtype */
+    int32_t reserved;
+} dss_tensor;
+
+/* Bytes of the workspace of dss_grad_norm and dss_clip_grads, for any list. */
+#define DSS_GRAD_NORM_WORKSPACE_BYTES 8192
+
+/* The norm of a gradient over all of its tensors, sqrt(sum of squares), as
+ * dss_backward_dense's weight and bias gradients (and any others) make one up.
+ * The squares are summed in binary64, in an order that only the counts decide.
+ *   grads      host array of n tensors (n >= 0); read during the call only
+ *   norm       device, one binary32: 0 for no elements, infinite or NaN if an
+ *              element is
+ *   workspace  device scratch of DSS_GRAD_NORM_WORKSPACE_BYTES (256-byte aligned)
+ * Errors: DSS_E_INVALID (NULL or misaligned pointers, counts below 0 or above
+ * 2^40), DSS_E_UNSUPPORTED (dtype), DSS_E_SHAPE (workspace too small), DSS_E_HIP. */
+dss_status dss_grad_norm(const dss_tensor* grads, int32_t n, float* norm, void* workspace, int64_t workspace_bytes,
+                         hipStream_t stream);
+
+/* The norm, and the gradient scaled down to at most max_norm:
+ *   out[t][i] = min(1, max_norm / (norm + 1e-6)) * grads[t].data[i],
+ * formed in binary32 and rounded once to the tensor's type.  With an infinite
+ * norm the factor is 0 (an infinite element becomes NaN), with a NaN one it is
+ * NaN.
+ *   out        host array of n device pointers, out[t] for grads[t].count elements
+ *              of its type; out[t] == grads[t].data clips in place, and no other
+ *              overlap is allowed
+ *   max_norm   >= 0; may be infinite (nothing is clipped)
+ * Other arguments and errors as dss_grad_norm. */
+dss_status dss_clip_grads(const dss_tensor* grads, void* const* out, int32_t n, float max_norm, float* norm,
+                          void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------- tokens in 8 bits */
+
+/* Fully connected layers on many inputs at once ("tokens": window positions of a
+ * dense map, or rows of features), with tokens and weights in 8-bit integers.
+ * Every token and every output channel has one binary32 scale:
+ *   scale[m] = max_k |x[m][k]| / 127,   code[m][k] = clamp(rint(x[m][k] / scale[m]), -127, 127)
+ * (scale and quotient are the binary32 ones, rint goes to the nearest integer and
+ * from a tie to the even one), and a layer is
+ *   y[m][n] = act(scale[m] * weight_scale[n] * sum_k code[m][k] * weight[n][k] + bias[n])
+ * with the sum exact in 32-bit integers.  A token of zeros (or one so small that
+ * its scale is 0) has scale 0 and codes 0.  A token with an infinity or a NaN has
+ * scale NaN and codes 0, so that its outputs are NaN and no other token's are. */
+
+/* Codes and scales of M tokens of K channels, x[m * token_stride + k * channel_stride].
+ * Weights are coded by the same call: their tokens are the output channels.
+ *   x        device, binary32 or bfloat16, aligned to its elements.  One of the
+ *            strides has to be 1: channel_stride = 1 for rows, token_stride = 1 for a
+ *            dense map [K][M] (dss_eval_dense's layout); the other one is >= 0
+ *   codes    device, codes[m * codes_stride + k], codes_stride >= K
+ *   scales   device, binary32 [M]
+ * Inputs and outputs must not overlap.  M = 0 does nothing.  Errors: DSS_E_INVALID
+ * (NULL or misaligned pointers, M < 0, K < 1, a negative stride, codes_stride < K),
+ * DSS_E_UNSUPPORTED (dtype, no stride of 1), DSS_E_HIP. */
+dss_status dss_quantize_tokens(const void* x, dss_dtype dtype, int64_t M, int32_t K, int64_t token_stride,
+                               int64_t channel_stride, int8_t* codes, int64_t codes_stride, float* scales,
+                               hipStream_t stream);
+
+/* Workspace bytes of dss_matmul_tokens (from_codes nonzero) or dss_linear_tokens
+ * for M tokens of K channels and N outputs, whatever the strides (host only). */
+dss_status dss_tokens_workspace(int64_t M, int32_t N, int32_t K, int32_t from_codes, int64_t* workspace_bytes);
+
+/* The layer on tokens that are already codes.
+ *   codes          device, codes[m * codes_stride + k], codes_stride >= K
+ *   scales         device, binary32 [M]
+ *   weight         device, weight[n * weight_stride + k], weight_stride >= K
+ *   weight_scales  device, binary32 [N]
+ *   bias           device, binary32 [N], or NULL for zero bias
+ *   act            a NaN stays one through every activation
+ *   out            device, binary32 or bfloat16 (rounded once, to nearest even),
+ *                  out[m * out_token_stride + n * out_channel_stride]; one of the strides
+ *                  has to be 1: out_channel_stride = 1 for rows, out_token_stride = 1 for a
+ *                  dense map [N][M]; the other one is at least the length it steps over
+ *   workspace      device scratch of dss_tokens_workspace bytes (256-byte aligned);
+ *                  may be NULL where these are 0
+ * Inputs and outputs must not overlap.  M = 0 does nothing.  Errors: DSS_E_INVALID
+ * (NULL or misaligned pointers, sizes or strides out of range, unknown act),
+ * DSS_E_UNSUPPORTED (out_dtype, no stride of 1, K > 131071: the sum could leave
+ * 32 bits), DSS_E_SHAPE (workspace too small), DSS_E_HIP. */
+dss_status dss_matmul_tokens(const int8_t* codes, int64_t codes_stride, const float* scales, int64_t M,
+                             const int8_t* weight, int64_t weight_stride, const float* weight_scales, int32_t N,
+                             int32_t K, const float* bias, dss_act act, void* out, dss_dtype out_dtype,
+                             int64_t out_token_stride, int64_t out_channel_stride, void* workspace,
+                             int64_t workspace_bytes, hipStream_t stream);
+
+/* The layer on tokens as they are: dss_quantize_tokens and dss_matmul_tokens in one
+ * call, with the same bits.  Arguments and errors as theirs. */
+dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t M, int64_t token_stride, int64_t channel_stride,
+                             const int8_t* weight, int64_t weight_stride, const float* weight_scales, int32_t N,
+                             int32_t K, const float* bias, dss_act act, void* out, dss_dtype out_dtype,
+                             int64_t out_token_stride, int64_t out_channel_stride, void* workspace,
+                             int64_t workspace_bytes, hipStream_t stream);
+
 /* ---------------------------------------------------------------- telemetry */
 
 /* Per-launch record of an evaluation on a plan with timing enabled. */

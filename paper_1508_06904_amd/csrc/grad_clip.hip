@@ -1,0 +1,274 @@
+// Norm of a gradient over all of its tensors, and clipping by it:
+//   norm = sqrt(sum_t sum_i g_t[i]^2),   out_t[i] = min(1, max_norm / (norm + 1e-6)) g_t[i].
+//
+// Two passes over the values: sums of squares into one partial sum per
+// workgroup, then the partial sums' total (again in every workgroup: 8 KB at
+// most, from L2) and the scaling.  Both are bound by memory.  The squares are
+// summed in binary64: no square of a binary32 value leaves its range, so a norm
+// is finite and right wherever binary32 can hold it, and the conversion and the
+// multiply-add cost less than the loads they wait for.  Each value's place in the
+// sums depends on the tensors' sizes only: the same gradients give the same bits.
+//
+// The tensors travel as a kernel argument, kTable at a time (a launch more for
+// every kTable tensors); a workgroup finds the tensor of its run of values by
+// bisection.  Tensors need no more than their elements' alignment: the 16-byte
+// loads and stores of this GPU take any address.
+#include <algorithm>
+#include <cmath>
+
+#include "dev_common.h"
+#include "dss_internal.h"
+
+namespace dss {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTable = 112;              // 112 * 32 bytes of tensors: the table fits a 4 KB kernel argument
+constexpr int kMaxGroups = 1024;         // workgroups (and partial sums) of a launch
+constexpr int64_t kMinRun = 4096;        // values of the shortest run: four vectors of each thread
+
+struct TensorTable {
+    const void* in[kTable];
+    void* out[kTable];
+    int64_t count[kTable];
+    int32_t first[kTable];               // the tensor's first run
+    int32_t dtype[kTable];
+    int32_t n, runs;
+    int32_t run_shift;                   // a run has 2^run_shift values
+};
+
+static_assert(sizeof(TensorTable) + 64 <= 4096, "the table is a kernel argument");
+
+// Vectors at the elements' own alignment.
+template <typename T>
+struct Vec16 {
+    T v[16 / sizeof(T)];
+};
+template <typename T>
+__device__ __forceinline__ Vec16<T> load16(const T* p) {
+    Vec16<T> r;
+    __builtin_memcpy(&r, p, 16);
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void store16(T* p, const Vec16<T>& r) {
+    __builtin_memcpy(p, &r, 16);
+}
+
+// The sum of v over the workgroup, in every thread; the order of the additions is fixed.
+__device__ double group_sum(double v) {
+    __shared__ double part[kThreads / 64];
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) v += part[w];
+    return v;
+}
+
+// The tensor that run r belongs to: the last one whose first run is not after r.
+__device__ __forceinline__ int find_tensor(const TensorTable& t, int r) {
+    int lo = 0, hi = t.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (t.first[mid] <= r) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+template <typename T>
+__device__ __forceinline__ double sum_squares(const T* p, int64_t n, double s) {
+    constexpr int V = 16 / (int)sizeof(T);
+    constexpr int U = 4;
+    int64_t i = (int64_t)threadIdx.x * V;
+    for (; i + (int64_t)(U - 1) * kThreads * V + V <= n; i += (int64_t)U * kThreads * V) {
+        Vec16<T> x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = load16(p + i + (int64_t)u * kThreads * V);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const double d = to_f32(x[u].v[k]);
+                s = fma(d, d, s);
+            }
+    }
+    for (; i < n; i += (int64_t)kThreads * V)
+        for (int k = 0; k < V && i + k < n; ++k) {
+            const double d = to_f32(p[i + k]);
+            s = fma(d, d, s);
+        }
+    return s;
+}
+
+__global__ __launch_bounds__(kThreads) void norm_partial_kernel(TensorTable t, double* partial, int add) {
+    double s = 0;
+    for (int r = blockIdx.x; r < t.runs; r += gridDim.x) {
+        const int k = find_tensor(t, r);
+        const int64_t at = (int64_t)(r - t.first[k]) << t.run_shift;
+        const int64_t n = min(t.count[k] - at, (int64_t)1 << t.run_shift);
+        if (t.dtype[k] == DSS_BF16) s = sum_squares((const uint16_t*)t.in[k] + at, n, s);
+        else s = sum_squares((const float*)t.in[k] + at, n, s);
+    }
+    s = group_sum(s);
+    if (threadIdx.x == 0) partial[blockIdx.x] = add ? partial[blockIdx.x] + s : s;
+}
+
+__device__ __forceinline__ double norm_of(const double* partial, int groups) {
+    double s = 0;
+    for (int i = threadIdx.x; i < groups; i += kThreads) s += partial[i];
+    return sqrt(group_sum(s));
+}
+
+__global__ __launch_bounds__(kThreads) void norm_total_kernel(const double* partial, int groups, float* norm) {
+    const double v = norm_of(partial, groups);
+    if (threadIdx.x == 0) *norm = (float)v;
+}
+
+// min(1, b / (norm + 1e-6)); a NaN stays one, an infinite norm gives 0.
+__device__ __forceinline__ float coefficient(double norm, float max_norm) {
+    const double c = (double)max_norm / (norm + 1e-6);
+    return c >= 1.0 ? 1.f : (float)c;
+}
+
+template <typename T>
+__device__ __forceinline__ void scale_run(const T* p, T* q, int64_t n, float c) {
+    constexpr int V = 16 / (int)sizeof(T);
+    constexpr int U = 4;
+    int64_t i = (int64_t)threadIdx.x * V;
+    for (; i + (int64_t)(U - 1) * kThreads * V + V <= n; i += (int64_t)U * kThreads * V) {
+        Vec16<T> x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = load16(p + i + (int64_t)u * kThreads * V);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) store_elem(&x[u].v[k], to_f32(x[u].v[k]) * c);
+            store16(q + i + (int64_t)u * kThreads * V, x[u]);
+        }
+    }
+    for (; i < n; i += (int64_t)kThreads * V)
+        for (int k = 0; k < V && i + k < n; ++k) store_elem(&q[i + k], to_f32(p[i + k]) * c);
+}
+
+__global__ __launch_bounds__(kThreads) void clip_kernel(TensorTable t, const double* partial, int groups,
+                                                        float max_norm, float* norm) {
+    const double total = norm_of(partial, groups);
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
+    const float c = coefficient(total, max_norm);
+    for (int r = blockIdx.x; r < t.runs; r += gridDim.x) {
+        const int k = find_tensor(t, r);
+        if (c == 1.f && t.in[k] == t.out[k]) continue;   // in place, nothing to clip
+        const int64_t at = (int64_t)(r - t.first[k]) << t.run_shift;
+        const int64_t n = min(t.count[k] - at, (int64_t)1 << t.run_shift);
+        if (t.dtype[k] == DSS_BF16) scale_run((const uint16_t*)t.in[k] + at, (uint16_t*)t.out[k] + at, n, c);
+        else scale_run((const float*)t.in[k] + at, (float*)t.out[k] + at, n, c);
+    }
+}
+
+// Runs of 2^shift values: about four of them for each workgroup of a full launch, none shorter than kMinRun.
+int pick_shift(int64_t total) {
+    int shift = 12;
+    while (shift < 20 && (total >> shift) > 4 * kMaxGroups) ++shift;
+    return shift;
+}
+static_assert(kMinRun == 1 << 12, "pick_shift starts there");
+
+// The next table of tensors from *at on; whether there was one.  Empty tensors are left out.
+bool next_table(const dss_tensor* g, void* const* out, int32_t n, int shift, int32_t* at, TensorTable* t) {
+    t->n = t->runs = 0;
+    t->run_shift = shift;
+    for (; *at < n && t->n < kTable; ++*at) {
+        const dss_tensor& x = g[*at];
+        if (x.count == 0) continue;
+        const int64_t runs = ceil_div64(x.count, (int64_t)1 << shift);
+        if (t->runs + runs > (1 << 30)) break;
+        t->in[t->n] = x.data;
+        t->out[t->n] = out ? out[*at] : nullptr;
+        t->count[t->n] = x.count;
+        t->first[t->n] = t->runs;
+        t->dtype[t->n] = x.dtype;
+        t->runs += (int32_t)runs;
+        ++t->n;
+    }
+    return t->n > 0;
+}
+
+dss_status grad_common(const dss_tensor* grads, void* const* out, int32_t n, bool clip, float max_norm, float* norm,
+                       void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+    if (n < 0 || (n > 0 && !grads)) return fail(DSS_E_INVALID, "%d tensors, NULL list or not", n);
+    if (!norm) return fail(DSS_E_INVALID, "NULL norm");
+    if (clip && n > 0 && !out) return fail(DSS_E_INVALID, "NULL list of outputs");
+    if (clip && !(max_norm >= 0.f)) return fail(DSS_E_INVALID, "max_norm %g is negative or not a number", max_norm);
+    int64_t total = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        if (grads[i].dtype != DSS_F32 && grads[i].dtype != DSS_BF16)
+            return fail(DSS_E_UNSUPPORTED, "tensor %d: unknown dtype %d", i, grads[i].dtype);
+        if (grads[i].count < 0 || grads[i].count > ((int64_t)1 << 40) || total > ((int64_t)1 << 42))
+            return fail(DSS_E_INVALID, "tensor %d: %lld elements", i, (long long)grads[i].count);
+        if (grads[i].count == 0) continue;
+        const uintptr_t es = grads[i].dtype == DSS_BF16 ? 2 : 4;
+        if (!grads[i].data || (uintptr_t)grads[i].data % es != 0)
+            return fail(DSS_E_INVALID, "tensor %d: NULL or not aligned to its elements", i);
+        if (clip && (!out[i] || (uintptr_t)out[i] % es != 0))
+            return fail(DSS_E_INVALID, "output %d: NULL or not aligned to its elements", i);
+        total += grads[i].count;
+    }
+    if (!workspace || ((uintptr_t)workspace & 255u) != 0)
+        return fail(DSS_E_INVALID, "workspace is NULL or not 256-byte aligned");
+    if (workspace_bytes < DSS_GRAD_NORM_WORKSPACE_BYTES)
+        return fail(DSS_E_SHAPE, "workspace of %lld bytes is smaller than the %lld bytes needed",
+                    (long long)workspace_bytes, (long long)DSS_GRAD_NORM_WORKSPACE_BYTES);
+    static_assert(kMaxGroups * sizeof(double) <= DSS_GRAD_NORM_WORKSPACE_BYTES, "partial sums");
+
+    double* partial = static_cast<double*>(workspace);
+    const int shift = pick_shift(total);
+    TensorTable t;
+    // every launch but the first adds to the first one's partial sums, so that one has a sum for each of them
+    int groups = 1;
+    for (int32_t at = 0; next_table(grads, out, n, shift, &at, &t);) groups = std::max(groups, std::min(t.runs, kMaxGroups));
+    int32_t at = 0;
+    bool more = next_table(grads, out, n, shift, &at, &t);
+    for (int add = 0; more || !add; add = 1) {
+        norm_partial_kernel<<<dim3(add ? std::min(t.runs, kMaxGroups) : groups), kThreads, 0, stream>>>(t, partial, add);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return hip_fail(e, "gradient norm launch");
+        more = next_table(grads, out, n, shift, &at, &t);
+    }
+    if (!clip || total == 0) {
+        norm_total_kernel<<<1, kThreads, 0, stream>>>(partial, groups, norm);
+        hipError_t e = hipGetLastError();
+        return e == hipSuccess ? DSS_OK : hip_fail(e, "gradient norm launch");
+    }
+    at = 0;
+    for (bool first = true; next_table(grads, out, n, shift, &at, &t); first = false) {
+        clip_kernel<<<dim3(std::min(t.runs, kMaxGroups)), kThreads, 0, stream>>>(t, partial, groups, max_norm,
+                                                                                 first ? norm : nullptr);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return hip_fail(e, "gradient clipping launch");
+    }
+    return DSS_OK;
+}
+
+}  // namespace
+
+}  // namespace dss
+
+extern "C" dss_status dss_grad_norm(const dss_tensor* grads, int32_t n, float* norm, void* workspace,
+                                    int64_t workspace_bytes, hipStream_t stream) try {
+    return dss::grad_common(grads, nullptr, n, false, 0.f, norm, workspace, workspace_bytes, stream);
+} catch (...) {
+    return DSS_E_NOMEM;
+}
+
+extern "C" dss_status dss_clip_grads(const dss_tensor* grads, void* const* out, int32_t n, float max_norm, float* norm,
+                                     void* workspace, int64_t workspace_bytes, hipStream_t stream) try {
+    return dss::grad_common(grads, out, n, true, max_norm, norm, workspace, workspace_bytes, stream);
+} catch (...) {
+    return DSS_E_NOMEM;
+}

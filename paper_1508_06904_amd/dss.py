@@ -65,12 +65,20 @@ class LaunchRecord(ctypes.Structure):
                 ("ms", ctypes.c_double), ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
 
 
+class Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("count", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+GRAD_NORM_WORKSPACE_BYTES = 8192
+
 EXPORTS = ("dss_chain_geometry", "dss_chain_layer_geometry", "dss_plan_create", "dss_plan_destroy",
            "dss_plan_geometry", "dss_plan_layer_geometry", "dss_eval_dense", "dss_eval_mixed", "dss_eval_slide",
            "dss_chain_stride_geometry", "dss_plan_stride_geometry", "dss_eval_stride", "dss_chain_dilate_geometry",
            "dss_plan_dilate_geometry", "dss_eval_dilate", "dss_chain_backward_geometry",
            "dss_plan_backward_geometry", "dss_backward_dense", "dss_eval_dense_noalloc", "dss_frag", "dss_defrag",
-           "dss_plan_set_timing", "dss_plan_timings", "dss_status_string", "dss_last_error", "dss_version")
+           "dss_grad_norm", "dss_clip_grads", "dss_quantize_tokens", "dss_tokens_workspace", "dss_matmul_tokens",
+           "dss_linear_tokens", "dss_plan_set_timing", "dss_plan_timings", "dss_status_string", "dss_last_error", "dss_version")
 
 _lib = None
 
@@ -122,6 +130,13 @@ def lib():
         L.dss_eval_dense_noalloc.argtypes = [VP, VP, I32, I32, VP, VP]
         L.dss_frag.argtypes = [I32, I32, I32, I32, I32, I32, I32, I32, VP, VP, VP]
         L.dss_defrag.argtypes = [I32, I32, I32, I32, I32, I32, I32, I32, VP, VP, VP]
+        L.dss_grad_norm.argtypes = [VP, I32, VP, VP, I64, VP]
+        L.dss_clip_grads.argtypes = [VP, VP, I32, ctypes.c_float, VP, VP, I64, VP]
+        L.dss_quantize_tokens.argtypes = [VP, I32, I64, I32, I64, I64, VP, I64, VP, VP]
+        L.dss_tokens_workspace.argtypes = [I64, I32, I32, I32, P(I64)]
+        L.dss_matmul_tokens.argtypes = [VP, I64, VP, I64, VP, I64, VP, I32, I32, VP, I32, VP, I32, I64, I64, VP, I64, VP]
+        L.dss_linear_tokens.argtypes = [VP, I32, I64, I64, I64, VP, I64, VP, I32, I32, VP, I32, VP, I32, I64, I64, VP,
+                                        I64, VP]
         L.dss_plan_set_timing.argtypes = [VP, I32]
         L.dss_plan_timings.argtypes = [VP, P(LaunchRecord), I32, P(I32)]
         L.dss_status_string.argtypes = [I32]
@@ -135,7 +150,9 @@ def lib():
                      "dss_defrag", "dss_plan_set_timing", "dss_plan_timings", "dss_plan_stride_geometry",
                      "dss_chain_stride_geometry", "dss_eval_stride", "dss_chain_dilate_geometry",
                      "dss_plan_dilate_geometry", "dss_eval_dilate", "dss_chain_backward_geometry",
-                     "dss_plan_backward_geometry", "dss_backward_dense", "dss_eval_dense_noalloc"):
+                     "dss_plan_backward_geometry", "dss_backward_dense", "dss_eval_dense_noalloc", "dss_grad_norm",
+                     "dss_clip_grads", "dss_quantize_tokens", "dss_tokens_workspace", "dss_matmul_tokens",
+                     "dss_linear_tokens"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -501,4 +518,255 @@ def defrag(x, k_h, k_w, S_h, S_w, out=None, stream=None):
         out = torch.empty((S_h * S_w, C, H * k_h, W * k_w), dtype=x.dtype, device=x.device)
     _check_buffer(out, "out", x.element_size(), F * C * H * W, device=x.device)
     _check(lib().dss_defrag(k_h, k_w, S_h, S_w, C, H, W, dt, _ptr(x), _ptr(out), _stream(stream)), "dss_defrag")
+    return out
+
+
+# ---------------------------------------------------------------------------- gradient norm and clipping
+
+def _dtype_codes():
+    global _dtype_code
+    if _dtype_code is None:
+        import torch
+        _dtype_code = {torch.float32: DSS_F32, torch.bfloat16: DSS_BF16}
+    return _dtype_code
+
+
+_dtype_code = None
+
+
+def _on_current_device(device, what):
+    import torch
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError("%s must be on the current CUDA device (got %s)" % (what, device))
+
+
+def _allocate_on(stream):
+    """A context in which new tensors belong to `stream` (None: the current one), so that
+    their memory is not given to another stream's work while the call's kernels use it."""
+    import contextlib
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _is_dense(t):
+    """Whether t's elements fill a block of memory in some order of its axes."""
+    if t.is_contiguous():
+        return True
+    n = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
+        if stride != n:
+            return False
+        n *= size
+    return True
+
+
+def _listed(tensors, what):
+    import torch
+    if not isinstance(tensors, torch.Tensor):
+        tensors = list(tensors)
+        if all([isinstance(t, torch.Tensor) for t in tensors]):
+            return tensors
+    raise ValueError("%s must be a list of tensors" % what)
+
+
+def _tensor_list(tensors, what):
+    """The C list of CUDA tensors (dss_tensor[n], as a numpy array) and their device."""
+    codes = _dtype_codes()
+    devices = {t.device for t in tensors}
+    if len(devices) > 1:
+        raise ValueError("%s are on several devices" % what)
+    for d in devices:
+        _on_current_device(d, what)
+    dtypes = [codes.get(t.dtype, -1) for t in tensors]
+    if -1 in dtypes:
+        raise ValueError("%s must be float32 or bfloat16 (got %s)" % (what, tensors[dtypes.index(-1)].dtype))
+    if not all([_is_dense(t) for t in tensors]):
+        raise ValueError("%s must be dense in memory, without gaps or repeated elements" % what)
+    a = np.empty(len(tensors), dtype=_TENSOR)
+    a["data"] = [t.data_ptr() for t in tensors]
+    a["count"] = [t.numel() for t in tensors]
+    a["dtype"] = dtypes
+    return a
+
+
+_TENSOR = np.dtype([("data", "<u8"), ("count", "<i8"), ("dtype", "<i4"), ("reserved", "<i4")])
+
+
+def grad_norm(grads, norm=None, workspace=None, stream=None):
+    """The norm of a gradient over a list of CUDA tensors (float32 and bfloat16, dense in
+    memory, any sizes): sqrt of the sum of all squares, as a float32 tensor of no axes."""
+    a = _tensor_list(_listed(grads, "grads"), "grads")
+    norm, wp, wb, keep = _norm_buffers(norm, workspace, stream)
+    _check(lib().dss_grad_norm(a.ctypes.data, len(a), _ptr(norm), wp, wb, _stream(stream)), "dss_grad_norm")
+    return norm
+
+
+def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
+    """Scales a gradient, given as for grad_norm, by min(1, max_norm / (norm + 1e-6)).
+    Returns (norm, list of scaled tensors).  `out` is the list of tensors to write, of the
+    same shapes, strides and types (`out=grads` clips in place); allocated if None."""
+    import torch
+    in_place = out is grads
+    grads = _listed(grads, "grads")
+    a = _tensor_list(grads, "grads")
+    if in_place:
+        out, b = grads, a
+    else:
+        if out is None:
+            with _allocate_on(stream):
+                out = [torch.empty_like(g) for g in grads]
+        out = _listed(out, "out")
+        b = _tensor_list(out, "out")
+        if len(b) != len(a) or not all([o.shape == g.shape and o.stride() == g.stride() and o.dtype == g.dtype
+                                        for o, g in zip(out, grads)]):
+            raise ValueError("out must be of grads' shapes, strides and types")
+    norm, wp, wb, keep = _norm_buffers(norm, workspace, stream)
+    ptrs = np.ascontiguousarray(b["data"])
+    _check(lib().dss_clip_grads(a.ctypes.data, ptrs.ctypes.data, len(a), float(max_norm), _ptr(norm), wp, wb,
+                                _stream(stream)), "dss_clip_grads")
+    return norm, out
+
+
+def _norm_buffers(norm, workspace, stream):
+    import torch
+    with _allocate_on(stream):
+        if norm is None:
+            norm = torch.empty((), dtype=torch.float32, device="cuda")
+        if workspace is None:
+            workspace = torch.empty(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    _check_buffer(norm, "norm", torch.float32, 1)
+    wp, wb = _workspace_args(workspace, norm.device)
+    return norm, wp, wb, workspace
+
+
+# ---------------------------------------------------------------------------- tokens in 8 bits
+
+def _check_tokens(x, what):
+    import torch
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("%s must be a tensor [tokens][channels]" % what)
+    _on_current_device(x.device, what)
+
+
+def _check_vector(t, what, dtype, n):
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %d elements" % (what, dtype, n))
+    _on_current_device(t.device, what)
+
+
+def _check_codes(t, what, rows, channels):
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int8 or t.dim() != 2 or (rows is not None and
+                                                                                   t.shape[0] != rows) or \
+            (channels is not None and t.shape[1] != channels):
+        raise ValueError("%s must be an int8 tensor [%s][%s]" % (what, "rows" if rows is None else rows,
+                                                                 "channels" if channels is None else channels))
+    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError("%s must have adjacent channels and rows that do not overlap" % what)
+    _on_current_device(t.device, what)
+
+
+def _row_stride(t):
+    """The stride between a matrix's rows; one row alone may have any."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def quantize_tokens(x, codes=None, scales=None, stream=None):
+    """8-bit codes and scales of the tokens (rows) of x, a float32 or bfloat16 CUDA matrix
+    [M][K] whose channels (x.stride(1) == 1) or tokens (x.stride(0) == 1, as for
+    `eval_dense(...).flatten(1).t()`) are adjacent:
+      scale = max|row| / 127,  code = round(row / scale) clamped to -127 .. 127 (ties to even).
+    Returns (codes int8 [M][K], scales float32 [M]).  A weight matrix [N][K] is coded the
+    same way, with a scale for each output channel."""
+    import torch
+    _check_tokens(x, "x")
+    dt = _dtype_codes().get(x.dtype)
+    if dt is None:
+        raise ValueError("x must be float32 or bfloat16 (got %s)" % x.dtype)
+    M, K = x.shape
+    with _allocate_on(stream):
+        if codes is None:
+            codes = torch.empty((M, K), dtype=torch.int8, device=x.device)
+        if scales is None:
+            scales = torch.empty((M,), dtype=torch.float32, device=x.device)
+    _check_codes(codes, "codes", M, K)
+    _check_vector(scales, "scales", torch.float32, M)
+    _check(lib().dss_quantize_tokens(_ptr(x), dt, M, K, x.stride(0), x.stride(1), _ptr(codes), _row_stride(codes),
+                                     _ptr(scales), _stream(stream)), "dss_quantize_tokens")
+    return codes, scales
+
+
+def _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, device, stream):
+    """Checks a layer's weights and output; returns (out [M][N] to write, N, the C arguments around them)."""
+    import torch
+    _check_codes(weight, "weight", None, K)
+    N = weight.shape[0]
+    _check_vector(weight_scales, "weight_scales", torch.float32, N)
+    if bias is not None:
+        _check_vector(bias, "bias", torch.float32, N)
+    if act not in ACTS:
+        raise ValueError("unknown activation %r" % (act,))
+    shape = (N, M) if planar else (M, N)
+    if out is None:
+        if out_dtype not in _dtype_codes():
+            raise ValueError("out_dtype must be float32 or bfloat16 (got %s)" % out_dtype)
+        with _allocate_on(stream):
+            out = torch.empty(shape, dtype=out_dtype, device=device)
+    elif not isinstance(out, torch.Tensor) or out.shape != shape or out.dtype not in _dtype_codes() or \
+            out.device != device:
+        raise ValueError("out must be a float32 or bfloat16 tensor of shape %s on %s" % (shape, device))
+    ts, cs = (out.stride(1), out.stride(0)) if planar else out.stride()
+    pre = (_ptr(weight), _row_stride(weight), _ptr(weight_scales), N, K, None if bias is None else _ptr(bias),
+           ACTS[act], _ptr(out), _dtype_codes()[out.dtype], ts, cs)
+    return out, N, pre
+
+
+def _tokens_room(M, N, K, from_codes, workspace, device, stream):
+    if workspace is None:
+        import torch
+        need = ctypes.c_int64()
+        _check(lib().dss_tokens_workspace(M, N, K, from_codes, ctypes.byref(need)), "dss_tokens_workspace")
+        if need.value == 0:
+            return ctypes.c_void_p(None), 0, None
+        with _allocate_on(stream):
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
+    wp, wb = _workspace_args(workspace, device)
+    return wp, wb, workspace
+
+
+def matmul_i8(codes, scales, weight, weight_scales, bias=None, act="none", out=None, out_dtype=None, planar=False,
+              workspace=None, stream=None):
+    """A fully connected layer on tokens in 8 bits (quantize_tokens' codes [M][K] and scales [M])
+    with weights in 8 bits (codes [N][K], scales [N]):
+      y[m][n] = act(scales[m] * weight_scales[n] * sum_k codes[m][k] * weight[n][k] + bias[n]),
+    the sum exact.  act is "none", "relu" or "tanh".  Returns out, [M][N] or with planar=True the
+    dense map [N][M], of out_dtype (float32 unless given); an `out` of any row stride is taken."""
+    import torch
+    _check_codes(codes, "codes", None, None)
+    M, K = codes.shape
+    _check_vector(scales, "scales", torch.float32, M)
+    out, N, args = _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype or torch.float32, planar,
+                               codes.device, stream)
+    wp, wb, keep = _tokens_room(M, N, K, 1, workspace, codes.device, stream)
+    _check(lib().dss_matmul_tokens(_ptr(codes), _row_stride(codes), _ptr(scales), M, *args, wp, wb, _stream(stream)),
+           "dss_matmul_tokens")
+    return out
+
+
+def linear_i8(x, weight, weight_scales, bias=None, act="none", out=None, out_dtype=None, planar=False,
+              workspace=None, stream=None):
+    """matmul_i8 on float32 or bfloat16 tokens x [M][K], given as for quantize_tokens: codes them
+    and multiplies in one call, with the same bits as the two calls."""
+    import torch
+    _check_tokens(x, "x")
+    dt = _dtype_codes().get(x.dtype)
+    if dt is None:
+        raise ValueError("x must be float32 or bfloat16 (got %s)" % x.dtype)
+    M, K = x.shape
+    out, N, args = _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype or torch.float32, planar,
+                               x.device, stream)
+    wp, wb, keep = _tokens_room(M, N, K, 0, workspace, x.device, stream)
+    _check(lib().dss_linear_tokens(_ptr(x), dt, M, x.stride(0), x.stride(1), *args, wp, wb, _stream(stream)),
+           "dss_linear_tokens")
     return out

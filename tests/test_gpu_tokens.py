@@ -1,0 +1,389 @@
+"""8-bit tokens and their products with 8-bit weights against the oracle's 64-bit forms.
+
+Codes and scales are equal by definition.  A layer's output: the sum is exact, its conversion and
+the two products with the scales round three times (3 * 2^-24 of the product term), the bias's
+addition once (2^-24 of the result), tanh is within 4 * 2^-24 of its value (and no steeper than 1);
+bfloat16 rounds once more to 8 bits (2^-8).  Tests allow 1 % over that."""
+import numpy as np
+import pytest
+
+from oracle import tokens
+from paper_1508_06904_amd import dss
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    dss.lib()
+    yield
+    torch.cuda.synchronize()
+
+
+def _dev(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).to("cuda")
+
+
+def _np(t):
+    return t.float().cpu().numpy()
+
+
+def _x(M, K, layout="rows", dtype="f32", seed=0, pad=0):
+    """Tokens [M][K] as a view: rows (pad elements between them) or a map's columns."""
+    import torch
+    rng = np.random.default_rng([seed, M, K])
+    a = (rng.standard_normal((M, K)) * np.exp(2 * rng.standard_normal((M, 1)))).astype(np.float32)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    t = _dev(a).to(dt)
+    if layout == "map":
+        return t.t().contiguous().t()
+    wide = torch.full((M, K + pad), float("nan"), dtype=dt, device="cuda")
+    wide[:, :K] = t
+    return wide[:, :K]
+
+
+def _weights(N, K, seed=0):
+    rng = np.random.default_rng([seed, N, K, 1])
+    w = rng.integers(-127, 128, (N, K)).astype(np.int8)
+    return w, (rng.random(N) * 0.02).astype(np.float32), rng.standard_normal(N).astype(np.float32)
+
+
+def _check_layer(got, codes, scales, w, ws, bias, act, bf16=False):
+    want, prod = tokens.layer(codes, scales, w, ws, bias, act)
+    got = _np(got).astype(np.float64)
+    assert got.shape == want.shape
+    pre, _ = tokens.layer(codes, scales, w, ws, bias)
+    bound = 1.01 * U * (3 * prod + np.abs(pre) + 4 * np.abs(want)) + 1e-44
+    if bf16:
+        bound = bound + 2.0 ** -8 * (np.abs(want) + bound) + 2.0 ** -134
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    bad = ~(np.abs(got - want) <= bound) & ~np.isnan(want)
+    assert not bad.any(), (np.argwhere(bad)[:5], got[bad][:5], want[bad][:5], bad.mean())
+
+
+WIDTHS = [1, 2, 3, 4, 7, 8, 15, 16, 17, 31, 33, 63, 64, 65, 100, 127, 128, 129, 255, 256, 257, 511, 513, 1000, 1024, 1025,
+          2047, 2049, 4095, 4097, 8191, 8193, 9216, 16385, 33000, 70001]
+
+
+# ---------------------------------------------------------------------------- codes
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout,pad", [("rows", 0), ("rows", 3), ("map", 0)])
+@pytest.mark.parametrize("K", WIDTHS)
+def test_codes_of_every_width(K, layout, pad, dtype):
+    import torch
+    for M in (1, 2, 67) if K > 2000 else (1, 3, 64, 65, 301):
+        x = _x(M, K, layout, dtype, pad=pad)
+        q, s = dss.quantize_tokens(x)
+        wq, wsc = tokens.quantize(_np(x))
+        assert np.array_equal(s.cpu().numpy(), wsc), (M, K)
+        assert np.array_equal(q.cpu().numpy(), wq), (M, K)
+
+
+@pytest.mark.parametrize("layout", ["rows", "map"])
+@pytest.mark.parametrize("K", [16, 200, 515, 5000, 40000])
+def test_tokens_without_a_scale(K, layout):
+    """Tokens of zeros, of numbers too small for a scale, with infinities and NaN at either end,
+    of the largest numbers: their own rows only, and no other token's."""
+    import torch
+    M = 70
+    a = np.random.default_rng(K).standard_normal((M, K)).astype(np.float32)
+    a[3] = 0
+    a[5] = np.float32(1e-45)
+    a[6] = np.float32(2e-43)
+    a[7] *= np.float32(1e-39)
+    a[10, 0], a[11, K - 1], a[12, K // 2], a[13, K // 3] = np.inf, -np.inf, np.nan, -np.nan
+    a[20, K - 1] = np.float32(3.4028235e38)
+    a[69, K - 1] = np.nan
+    x = _dev(a)
+    x = x.t().contiguous().t() if layout == "map" else x
+    q, s = dss.quantize_tokens(x)
+    wq, wsc = tokens.quantize(a)
+    assert np.array_equal(s.cpu().numpy(), wsc, equal_nan=True)
+    assert np.array_equal(q.cpu().numpy(), wq)
+
+
+@pytest.mark.parametrize("layout", ["rows", "map"])
+def test_ties_go_to_the_even_code(layout):
+    a = np.zeros((40, 255), dtype=np.float32)
+    for m in range(40):
+        a[m] = (np.arange(255) - 127) * np.float32(2.0 ** (m - 20))
+        a[m, 127] = np.float32(2.0 ** (m - 20)) * (254 if m % 2 else 127)
+    x = _dev(a)
+    q, _ = dss.quantize_tokens(x.t().contiguous().t() if layout == "map" else x)
+    assert np.array_equal(q.cpu().numpy(), tokens.quantize(a)[0])
+
+
+def test_quotients_near_ties():
+    """Values at and beside (n + 1/2) scale, where a quotient off by one last place shows."""
+    rng = np.random.default_rng(4)
+    top = np.exp(rng.uniform(-20, 20, (2000, 1))).astype(np.float32)
+    s = top / np.float32(127)
+    near = ((rng.integers(-127, 127, (2000, 96)) + 0.5).astype(np.float32) * s).astype(np.float32)
+    near = np.nextafter(near, near + rng.integers(-1, 2, near.shape).astype(np.float32) * 1e30).astype(np.float32)
+    a = np.concatenate([top, near], axis=1)
+    for x in (_dev(a), _dev(a.T).t()):
+        q, sc = dss.quantize_tokens(x)
+        wq, wsc = tokens.quantize(a)
+        assert np.array_equal(sc.cpu().numpy(), wsc) and np.array_equal(q.cpu().numpy(), wq)
+
+
+@pytest.mark.parametrize("layout", ["rows", "map"])
+@pytest.mark.parametrize("K", [5, 64, 333, 2050])
+def test_codes_into_a_wider_buffer(K, layout):
+    """Codes with a row stride of their own; what lies beside them stays."""
+    import torch
+    x = _x(77, K, layout)
+    buf = torch.full((80, K + 9), 55, dtype=torch.int8, device="cuda")
+    sc = torch.full((80,), -5.0, device="cuda")
+    dss.quantize_tokens(x, codes=buf[1:78, 4:4 + K], scales=sc[1:78])
+    got = buf.cpu().numpy()
+    assert np.array_equal(got[1:78, 4:4 + K], tokens.quantize(_np(x))[0])
+    got[1:78, 4:4 + K] = 55
+    assert (got == 55).all() and sc[0] == -5 and bool((sc[78:] == -5).all())
+
+
+def test_offsets_over_32_bits():
+    """Tokens 2^29 elements apart, and channels 2^29 apart, in bfloat16: the last ones are past 2^32 elements."""
+    import torch
+    n, far = 9, 1 << 29
+    buf = torch.empty(n * far, dtype=torch.bfloat16, device="cuda")
+    a = _np(_x(n, 40, dtype="bf16"))
+    rows = buf.as_strided((n, 40), (far, 1))
+    rows.copy_(_dev(a))
+    wq, wsc = tokens.quantize(a)
+    q, s = dss.quantize_tokens(rows)
+    assert np.array_equal(q.cpu().numpy(), wq) and np.array_equal(s.cpu().numpy(), wsc)
+    cols = buf.as_strided((70, n), (1, far))
+    b = _np(_x(70, n, dtype="bf16"))
+    cols.copy_(_dev(b))
+    wq, wsc = tokens.quantize(b)
+    q, s = dss.quantize_tokens(cols)
+    assert np.array_equal(q.cpu().numpy(), wq) and np.array_equal(s.cpu().numpy(), wsc)
+
+
+def test_no_tokens_and_repeated_tokens():
+    import torch
+    q, s = dss.quantize_tokens(torch.empty((0, 12), device="cuda"))
+    assert q.shape == (0, 12) and s.shape == (0,)
+    x = torch.randn((1, 33), device="cuda").expand(5, 33)
+    q, s = dss.quantize_tokens(x)
+    assert np.array_equal(q.cpu().numpy(), tokens.quantize(_np(x))[0])
+
+
+# ---------------------------------------------------------------------------- products
+
+SHAPES = [(1, 1, 1), (1, 16, 16), (1, 512, 9216), (2, 100, 63), (3, 7, 65), (4, 33, 128), (5, 1000, 200), (13, 300, 4096),
+          (15, 17, 1000), (16, 16, 64), (17, 31, 129), (31, 64, 77), (33, 130, 512), (48, 257, 2305), (64, 64, 64),
+          (65, 65, 65), (100, 300, 131), (127, 129, 255), (128, 128, 128), (129, 127, 257), (200, 2, 512),
+          (255, 255, 1000), (256, 256, 256), (257, 513, 384), (300, 1003, 2305), (511, 640, 144), (1000, 4, 512),
+          (777, 1, 100), (2049, 70, 96), (513, 1030, 520), (600, 520, 8200), (4099, 128, 512), (2500, 260, 1040)]
+
+
+@pytest.mark.parametrize("planar", [False, True])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_products_of_codes(M, N, K, planar):
+    import torch
+    rng = np.random.default_rng([M, N, K])
+    codes = rng.integers(-127, 128, (M, K)).astype(np.int8)
+    scales = (rng.random(M) + 0.1).astype(np.float32)
+    w, ws, bias = _weights(N, K)
+    dc, dsc, dw, dws, db = map(_dev, (codes, scales, w, ws, bias))
+    for act, od, b in (("none", torch.float32, None), ("relu", torch.float32, bias), ("tanh", torch.bfloat16, bias)):
+        y = dss.matmul_i8(dc, dsc, dw, dws, bias=None if b is None else db, act=act, out_dtype=od, planar=planar)
+        assert y.dtype == od and y.is_contiguous() and y.shape == ((N, M) if planar else (M, N))
+        _check_layer(y.t() if planar else y, codes, scales, w, ws, b, act, od == torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout,pad", [("rows", 0), ("rows", 5), ("map", 0)])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_layers_of_tokens(M, N, K, layout, pad, dtype):
+    """linear_i8 is quantize_tokens and matmul_i8, to the bit, and right."""
+    import torch
+    x = _x(M, K, layout, dtype, pad=pad)
+    w, ws, bias = _weights(N, K)
+    dw, dws, db = map(_dev, (w, ws, bias))
+    planar = layout == "map"
+    y = dss.linear_i8(x, dw, dws, bias=db, act="relu", planar=planar)
+    q, s = dss.quantize_tokens(x)
+    two = dss.matmul_i8(q, s, dw, dws, bias=db, act="relu", planar=planar)
+    assert torch.equal(y, two)
+    codes, scales = tokens.quantize(_np(x))
+    _check_layer(y.t() if planar else y, codes, scales, w, ws, bias, "relu")
+    y = dss.linear_i8(x, dw, dws, act="tanh", out_dtype=torch.bfloat16, planar=not planar)
+    _check_layer(y if planar else y.t(), codes, scales, w, ws, None, "tanh", True)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 20, 130), (16, 64, 64), (70, 200, 96), (300, 300, 300)])
+def test_extreme_codes_and_sums(M, N, K):
+    """All codes at the ends of their range, -128 among them (a caller's own codes may have it)."""
+    rng = np.random.default_rng(K)
+    codes = rng.choice([-128, 127], (M, K)).astype(np.int8)
+    codes[0] = -128
+    w = rng.choice([-128, 127], (N, K)).astype(np.int8)
+    w[0], w[-1] = -128, 127
+    s, ws = np.ones(M, np.float32), np.ones(N, np.float32)
+    y = dss.matmul_i8(*map(_dev, (codes, s, w, ws)))
+    _check_layer(y, codes, s, w, ws, None, "none")
+
+
+@pytest.mark.parametrize("M", [1, 20, 300])
+def test_longest_sum(M):
+    K = 131071
+    codes = np.full((M, K), -128, dtype=np.int8)
+    w = np.stack([np.full(K, -128), np.full(K, 127)]).astype(np.int8)
+    s, ws = np.ones(M, np.float32), np.ones(2, np.float32)
+    y = dss.matmul_i8(*map(_dev, (codes, s, w, ws)))
+    _check_layer(y, codes, s, w, ws, None, "none")
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 40, 200), (20, 40, 200), (150, 140, 130), (700, 300, 512)])
+@pytest.mark.parametrize("act", ["none", "relu", "tanh"])
+def test_a_token_that_is_no_number_spoils_its_own_outputs_only(M, N, K, act):
+    import torch
+    for layout in ("rows", "map"):
+        x = _x(M, K, layout).clone()
+        x[M // 2, K - 1] = float("nan")
+        x[0, 0] = float("inf")
+        w, ws, bias = _weights(N, K)
+        y = dss.linear_i8(x, *map(_dev, (w, ws)), bias=_dev(bias), act=act)
+        codes, scales = tokens.quantize(_np(x))
+        _check_layer(y, codes, scales, w, ws, bias, act)
+        assert bool(torch.isnan(y[0]).all()) and bool(torch.isnan(y[M // 2]).all())
+        assert int(torch.isnan(y).any(dim=1).sum()) == len({0, M // 2})
+
+
+@pytest.mark.parametrize("planar", [False, True])
+@pytest.mark.parametrize("M,N,K", [(1, 40, 64), (9, 33, 100), (130, 70, 257), (600, 260, 128)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_operands_and_outputs_in_wider_buffers(M, N, K, planar, dtype):
+    """Row strides everywhere; beside the output nothing is written, beside the inputs nothing used."""
+    import torch
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    rng = np.random.default_rng([M, N, K, 7])
+    codes = rng.integers(-127, 128, (M, K)).astype(np.int8)
+    scales = (rng.random(M) + 0.1).astype(np.float32)
+    w, ws, bias = _weights(N, K)
+    cb = torch.full((M + 2, K + 7), 101, dtype=torch.int8, device="cuda")
+    wb = torch.full((N + 2, K + 5), -99, dtype=torch.int8, device="cuda")
+    cb[1:M + 1, 3:3 + K] = _dev(codes)
+    wb[1:N + 1, 2:2 + K] = _dev(w)
+    rows, cols = (N, M) if planar else (M, N)
+    ob = torch.full((rows + 2, cols + 6), -77.0, dtype=dt, device="cuda")
+    out = ob[1:rows + 1, 3:3 + cols]
+    y = dss.matmul_i8(cb[1:M + 1, 3:3 + K], _dev(scales), wb[1:N + 1, 2:2 + K], _dev(ws), bias=_dev(bias), out=out,
+                      planar=planar)
+    assert y is out
+    _check_layer(out.t() if planar else out, codes, scales, w, ws, bias, "none", dtype == "bf16")
+    ob[1:rows + 1, 3:3 + cols] = -77
+    assert bool((ob == -77).all())
+
+
+@pytest.mark.parametrize("planar", [False, True])
+def test_product_offsets_over_32_bits(planar):
+    """Rows of codes, of weights and of outputs 2^29 apart: the last ones are past 2^32 elements."""
+    import torch
+    far, M, N, K = 1 << 29, 9, 9, 70
+    rng = np.random.default_rng(3)
+    codes = rng.integers(-127, 128, (M, K)).astype(np.int8)
+    w, ws, bias = _weights(N, K)
+    scales = np.ones(M, np.float32)
+    cb = torch.empty(9 * far, dtype=torch.int8, device="cuda").as_strided((M, K), (far, 1))
+    wb = torch.empty(9 * far, dtype=torch.int8, device="cuda").as_strided((N, K), (far, 1))
+    ob = torch.empty(9 * far, dtype=torch.bfloat16, device="cuda").as_strided((N, M) if planar else (M, N), (far, 1))
+    cb.copy_(_dev(codes))
+    wb.copy_(_dev(w))
+    dss.matmul_i8(cb, _dev(scales), wb, _dev(ws), bias=_dev(bias), out=ob, planar=planar)
+    _check_layer(ob.t() if planar else ob, codes, scales, w, ws, bias, "none", True)
+
+
+def test_many_tokens_of_a_map():
+    """More outputs than 2^31: a map of 17 million windows, sampled."""
+    import torch
+    M, K, N = 17_000_003, 4, 128
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn((K, M), generator=gen, device="cuda").to(torch.bfloat16)
+    w, ws, bias = _weights(N, K)
+    y = dss.linear_i8(x.t(), *map(_dev, (w, ws)), bias=_dev(bias), out_dtype=torch.bfloat16, planar=True)
+    at = torch.cat([torch.arange(5), torch.randint(0, M, (3000,), generator=torch.Generator().manual_seed(1)),
+                    torch.arange(M - 70, M), torch.arange((1 << 21) - 9, (1 << 21) + 9)]).to("cuda")
+    codes, scales = tokens.quantize(_np(x[:, at].t()))
+    _check_layer(y[:, at].t(), codes, scales, w, ws, bias, "none", True)
+
+
+def test_no_tokens():
+    import torch
+    w, ws, bias = map(_dev, _weights(5, 12))
+    assert dss.linear_i8(torch.empty((0, 12), device="cuda"), w, ws, bias=bias).shape == (0, 5)
+    assert dss.linear_i8(torch.empty((0, 12), device="cuda"), w, ws, planar=True).shape == (5, 0)
+    assert dss.matmul_i8(w[:0], ws[:0], w, ws).shape == (0, 5)
+
+
+def test_other_stream():
+    import torch
+    side = torch.cuda.Stream()
+    x = _x(300, 129)
+    w, ws, bias = map(_dev, _weights(65, 129))
+    ref = dss.linear_i8(x, w, ws, bias=bias)
+    side.wait_stream(torch.cuda.current_stream())
+    got = dss.linear_i8(x, w, ws, bias=bias, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(ref, got)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 512, 1152), (20, 100, 130), (300, 300, 520)])
+def test_graph_replays(M, N, K):
+    import torch
+    x = _x(M, K)
+    w, ws, bias = map(_dev, _weights(N, K))
+    y = torch.empty((M, N), device="cuda")
+    room = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    call = lambda: dss.linear_i8(x, w, ws, bias=bias, act="tanh", out=y, workspace=room)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for n in range(3):
+        x.copy_(_x(M, K, seed=n + 5))
+        y.fill_(-3)
+        room.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, dss.linear_i8(x, w, ws, bias=bias, act="tanh"))
+
+
+def test_binding_refusals():
+    import torch
+    x = _x(6, 8)
+    w, ws, bias = map(_dev, _weights(5, 8))
+    q, s = dss.quantize_tokens(x)
+    bad = [lambda: dss.quantize_tokens(x.half()), lambda: dss.quantize_tokens(x.cpu()),
+           lambda: dss.quantize_tokens(x, codes=q[:5]), lambda: dss.quantize_tokens(x, codes=q.t().contiguous().t()),
+           lambda: dss.quantize_tokens(x, scales=s[:5]), lambda: dss.quantize_tokens(x, scales=s.double()),
+           lambda: dss.linear_i8(x, w[:, :7], ws), lambda: dss.linear_i8(x, w, ws[:4]),
+           lambda: dss.linear_i8(x, w, ws, bias=bias[:4]), lambda: dss.linear_i8(x, w, ws, act="gelu"),
+           lambda: dss.linear_i8(x, w, ws, out=torch.empty(5, 6, device="cuda")),
+           lambda: dss.linear_i8(x, w, ws, out_dtype=torch.float16), lambda: dss.linear_i8(x, w.t(), ws),
+           lambda: dss.linear_i8(x, w.float(), ws), lambda: dss.linear_i8(x, w, ws.cpu()),
+           lambda: dss.matmul_i8(x, s, w, ws), lambda: dss.matmul_i8(q, s[:5], w, ws),
+           lambda: dss.matmul_i8(q, s, w, ws, out=torch.empty(6, 5, device="cuda", dtype=torch.int32))]
+    for n, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            print("accepted", n)
+    with pytest.raises(dss.DssError) as e:
+        dss.quantize_tokens(torch.randn(16, 32, device="cuda")[::2, ::2])
+    assert e.value.status == 3
+    with pytest.raises(dss.DssError) as e:
+        dss.linear_i8(x, w, ws, out=torch.empty(12, 10, device="cuda")[::2, ::2])
+    assert e.value.status == 3
+    with pytest.raises(dss.DssError) as e:
+        dss.linear_i8(x, w, ws, workspace=torch.empty(10, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == 2
