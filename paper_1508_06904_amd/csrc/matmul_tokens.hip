@@ -10,6 +10,7 @@
 // matrix instruction Q's rows are the result's rows, so that a lane holds four
 // adjacent outputs.
 #include <algorithm>
+#include <cmath>
 
 #include "dev_common.h"
 #include "dss_internal.h"
@@ -48,64 +49,306 @@ __device__ __forceinline__ float output_of(int sum, float wscale, float scale, f
     return activate_nan(act, (float)sum * wscale * scale + bias);
 }
 
-// ------------------------------------------------------------------ any sizes and strides
-// 64 x 64 outputs for four waves of 16 (i) x 64 (j); 64 of K at a time through LDS.
-constexpr int kTile = 64;
-constexpr int kPitch = 64 + 16;
+// D's operands and extents.
+struct Sides {
+    const int8_t *P, *Q;
+    int64_t ps, qs, I, J;
+};
+__host__ __device__ __forceinline__ Sides sides_of(const Layer& L) {
+    if (L.map) return {L.weight, L.codes, L.weight_stride, L.codes_stride, L.N, L.M};
+    return {L.codes, L.weight, L.codes_stride, L.weight_stride, L.M, L.N};
+}
 
+// Four adjacent outputs D[i][j .. j+3] of a layer, those from J on left out.
 template <typename Tout>
-__global__ __launch_bounds__(256) void matmul_any_kernel(Layer L, int tiles_j) {
-    __shared__ __align__(16) int8_t lp[kTile * kPitch], lq[kTile * kPitch];
-    const int8_t* P = L.map ? L.weight : L.codes;
-    const int8_t* Q = L.map ? L.codes : L.weight;
-    const int64_t ps = L.map ? L.weight_stride : L.codes_stride, qs = L.map ? L.codes_stride : L.weight_stride;
-    const int64_t I = L.map ? L.N : L.M, J = L.map ? L.M : L.N;
-    const int64_t i0 = (int64_t)(blockIdx.x / tiles_j) * kTile, j0 = (int64_t)(blockIdx.x % tiles_j) * kTile;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    i32x4 acc[4] = {};
-    for (int k0 = 0; k0 < L.K; k0 += 64) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < kTile * 64; e += 256) {
-            const int r = e >> 6, k = e & 63;
-            const bool in = k0 + k < L.K;
-            lp[r * kPitch + k] = in && i0 + r < I ? P[(i0 + r) * ps + k0 + k] : 0;
-            lq[r * kPitch + k] = in && j0 + r < J ? Q[(j0 + r) * qs + k0 + k] : 0;
-        }
-        __syncthreads();
-        const i32x4 p = *reinterpret_cast<const i32x4*>(lp + (wave * 16 + (lane & 15)) * kPitch + (lane >> 4) * 16);
+__device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum) {
+    Tout* p = static_cast<Tout*>(L.out) + i * L.ldo + j;
+    struct Four {
+        Tout v[4];
+    } r;
+    const int n = (int)min(J - j, (int64_t)4);
+    if (L.map) {
+        const float ws = L.weight_scales[i], b = L.bias ? L.bias[i] : 0.f;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const i32x4 q = *reinterpret_cast<const i32x4*>(lq + (t * 16 + (lane & 15)) * kPitch + (lane >> 4) * 16);
-            acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q, p, acc[t], 0, 0, 0);
+        for (int k = 0; k < 4; ++k) store_elem(&r.v[k], output_of(sum[k], ws, k < n ? L.scales[j + k] : 0.f, b, L.act));
+    } else {
+        const float s = L.scales[i];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            store_elem(&r.v[k], output_of(sum[k], k < n ? L.weight_scales[j + k] : 0.f, s,
+                                          L.bias && k < n ? L.bias[j + k] : 0.f, L.act));
+    }
+    if (n == 4) {
+        __builtin_memcpy(p, &r, sizeof r);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            if (k < n) p[k] = r.v[k];
+    }
+}
+
+// ------------------------------------------------------------------ tiles
+// BI x BJ outputs for WI x WJ waves; kStep bytes of K at a time through two LDS
+// buffers, the next step's bytes on their way while this one's are multiplied.  A
+// row of a buffer is 8 units of 16 bytes; row r keeps unit u at place u ^ (r & 7),
+// so that the 8 rows that a matrix operand's read takes at once lie in different
+// banks.
+//
+// DMA: global memory to LDS without a stop in registers; rows have to start at
+// 16-byte units, and K ends at one.  Otherwise through registers, from any address.
+constexpr int kStep = 128;
+constexpr int kUnits = kStep / 16;
+
+// 16 zero bytes: the source of the units past the end of K.
+__device__ __attribute__((aligned(16))) const unsigned int g_zero16[4] = {0u, 0u, 0u, 0u};
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// Bytes k .. k+15 of a row of K bytes, zeros past its end; nothing past the end is read.
+__device__ __forceinline__ i32x4 load_unit(const int8_t* row, int k, int K) {
+    i32x4 v = {};
+    if (k + 16 <= K) {
+        __builtin_memcpy(&v, row + k, 16);
+    } else if (k < K) {
+        if (K >= 16) {
+            unsigned __int128 w;
+            __builtin_memcpy(&w, row + K - 16, 16);
+            w >>= 8 * (k + 16 - K);
+            __builtin_memcpy(&v, &w, 16);
+        } else {
+            for (int b = 0; b < K - k; ++b) v[b >> 2] |= (int)(uint8_t)row[k + b] << (8 * (b & 3));
         }
     }
-    const int64_t i = i0 + wave * 16 + (lane & 15);
-    if (i >= I) return;
+    return v;
+}
+
+// Workgroups are handed to the 8 XCDs in turn: the id of the tile that makes the
+// tiles of one XCD (and of its L2) neighbours.
+__device__ __forceinline__ int64_t xcd_order(int64_t b, int64_t n) {
+    const int64_t x = b & 7, q = n >> 3, r = n & 7;
+    return x * q + min(x, r) + (b >> 3);
+}
+
+template <typename Tout, int BI, int BJ, int WI, int WJ, bool DMA>
+__global__ __launch_bounds__(WI* WJ * 64) void matmul_tile_kernel(Layer L, int tiles_i, int tiles_j) {
+    constexpr int NW = WI * WJ, THREADS = NW * 64;
+    constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
+    constexpr int LP = BI * kUnits / THREADS, LQ = BJ * kUnits / THREADS;   // units of each thread and step
+    static_assert(LP * THREADS == BI * kUnits && LQ * THREADS == BJ * kUnits && THREADS % 64 == 0, "tile");
+    constexpr int BUF = (BI + BJ) * kStep;
+    extern __shared__ __align__(16) char lds[];
+    const Sides S = sides_of(L);
+    // tiles in strips of 8 along i: a strip's tiles share their rows of Q in cache
+    const int64_t id = xcd_order(blockIdx.x, (int64_t)tiles_i * tiles_j);
+    const int64_t strip = id / ((int64_t)8 * tiles_j), in_strip = id - strip * 8 * tiles_j;
+    const int rows = min(8, tiles_i - (int)strip * 8);
+    const int64_t i0 = (strip * 8 + in_strip % rows) * BI, j0 = in_strip / rows * BJ;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int wi = wave / WJ, wj = wave % WJ;
+
+    // the thread's units: rows row0 + n * (THREADS / 8), and one place in each of them
+    const int row0 = tid >> 3, unit = (tid & 7) ^ (row0 & 7);
+    const int8_t *src_p[LP], *src_q[LQ];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int n = 0; n < LP; ++n) src_p[n] = S.P + min(i0 + row0 + n * (THREADS / 8), S.I - 1) * S.ps;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t j = j0 + t * 16 + (lane >> 4) * 4 + r;
-            if (j >= J) continue;
-            const int64_t m = L.map ? j : i;
-            const int n = (int)(L.map ? i : j);
-            const float y = output_of(acc[t][r], L.weight_scales[n], L.scales[m], L.bias ? L.bias[n] : 0.f, L.act);
-            store_elem(static_cast<Tout*>(L.out) + i * L.ldo + j, y);
+    for (int n = 0; n < LQ; ++n) src_q[n] = S.Q + min(j0 + row0 + n * (THREADS / 8), S.J - 1) * S.qs;
+
+    const int K = L.K, steps = (K + kStep - 1) / kStep;
+    i32x4 acc[TI][TJ] = {};
+    i32x4 rp[DMA ? 1 : LP], rq[DMA ? 1 : LQ];
+
+    auto fetch = [&](int s) {
+        const int k = s * kStep + unit * 16;
+        if constexpr (DMA) {
+            char* to = lds + (s & 1) * BUF + wave * 1024;
+            const bool in = k < K;
+#pragma unroll
+            for (int n = 0; n < LP; ++n)
+                __builtin_amdgcn_global_load_lds(in ? (const void*)(src_p[n] + k) : (const void*)g_zero16,
+                                                 (lds_void*)(to + n * THREADS * 16), 16, 0, 0);
+#pragma unroll
+            for (int n = 0; n < LQ; ++n)
+                __builtin_amdgcn_global_load_lds(in ? (const void*)(src_q[n] + k) : (const void*)g_zero16,
+                                                 (lds_void*)(to + BI * kStep + n * THREADS * 16), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int n = 0; n < LP; ++n) rp[n] = load_unit(src_p[n], k, K);
+#pragma unroll
+            for (int n = 0; n < LQ; ++n) rq[n] = load_unit(src_q[n], k, K);
         }
+    };
+    auto put = [&](int s) {
+        if constexpr (!DMA) {
+            char* to = lds + (s & 1) * BUF + tid * 16;
+#pragma unroll
+            for (int n = 0; n < LP; ++n) *reinterpret_cast<i32x4*>(to + n * THREADS * 16) = rp[n];
+#pragma unroll
+            for (int n = 0; n < LQ; ++n) *reinterpret_cast<i32x4*>(to + BI * kStep + n * THREADS * 16) = rq[n];
+        }
+    };
+
+    fetch(0);
+    put(0);
+    __syncthreads();
+    const int l16 = lane & 15, q16 = lane >> 4;
+    for (int s = 0; s < steps; ++s) {
+        if (s + 1 < steps) fetch(s + 1);
+        const char* bp = lds + (s & 1) * BUF + (wi * TI * 16 + l16) * kStep;
+        const char* bq = lds + (s & 1) * BUF + BI * kStep + (wj * TJ * 16 + l16) * kStep;
+#pragma unroll
+        for (int h = 0; h < kStep / 64; ++h) {
+            const int place = ((h * 4 + q16) ^ (l16 & 7)) * 16;
+            i32x4 p[TI], q[TJ];
+#pragma unroll
+            for (int t = 0; t < TJ; ++t) q[t] = *reinterpret_cast<const i32x4*>(bq + t * 16 * kStep + place);
+#pragma unroll
+            for (int t = 0; t < TI; ++t) p[t] = *reinterpret_cast<const i32x4*>(bp + t * 16 * kStep + place);
+#pragma unroll
+            for (int a = 0; a < TI; ++a)
+#pragma unroll
+                for (int b = 0; b < TJ; ++b) acc[a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[b], p[a], acc[a][b], 0, 0, 0);
+        }
+        if (s + 1 < steps) put(s + 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int a = 0; a < TI; ++a) {
+        const int64_t i = i0 + (wi * TI + a) * 16 + l16;
+#pragma unroll
+        for (int b = 0; b < TJ; ++b) {
+            const int64_t j = j0 + (wj * TJ + b) * 16 + q16 * 4;
+            if (i < S.I && j < S.J) store_outputs<Tout>(L, i, j, S.J, acc[a][b]);
+        }
+    }
+}
+
+template <typename Tout, int BI, int BJ, int WI, int WJ, bool DMA>
+hipError_t run_tile(const Layer& L, hipStream_t s) {
+    const Sides S = sides_of(L);
+    const int64_t ti = ceil_div64(S.I, BI), tj = ceil_div64(S.J, BJ);
+    const auto kern = matmul_tile_kernel<Tout, BI, BJ, WI, WJ, DMA>;
+    constexpr size_t lds = 2 * (BI + BJ) * kStep;
+    const hipError_t e = allow_dynamic_lds((const void*)kern, lds);
+    if (e != hipSuccess) return e;
+    kern<<<dim3((unsigned)(ti * tj)), WI * WJ * 64, lds, s>>>(L, (int)ti, (int)tj);
+    return hipGetLastError();
+}
+
+// The tile: the one whose launch keeps the GPU's 256 units busy with the least time
+// lost to part-filled rounds; wider tiles read less of P and Q for an output.
+struct TileChoice {
+    int bi, bj, resident;                // outputs of a tile, workgroups of a unit at once
+    double rate;                         // of the 256 x 256 tile's, with all units busy
+};
+constexpr TileChoice kTiles[] = {{256, 256, 1, 1.0}, {128, 128, 2, 0.8}, {64, 64, 4, 0.4}};
+
+int pick_tile(const Sides& S) {
+    int best = 0;
+    double least = 0;
+    for (int t = 0; t < 3; ++t) {
+        const TileChoice& c = kTiles[t];
+        const double tiles = (double)ceil_div64(S.I, c.bi) * ceil_div64(S.J, c.bj);
+        const double rounds = std::ceil(tiles / (256.0 * c.resident)) * c.resident;
+        const double time = rounds * c.bi * c.bj / c.rate;
+        if (t == 0 || time < least) best = t, least = time;
+    }
+    return best;
+}
+
+template <typename Tout, bool DMA>
+hipError_t run_product(const Layer& L, hipStream_t s) {
+    switch (pick_tile(sides_of(L))) {
+        case 0: return run_tile<Tout, 256, 256, 2, 4, DMA>(L, s);
+        case 1: return run_tile<Tout, 128, 128, 2, 2, DMA>(L, s);
+        default: return run_tile<Tout, 64, 64, 2, 2, DMA>(L, s);
+    }
+}
+
+// ------------------------------------------------------------------ few tokens
+// At most 16 GT tokens: bound by the weights' bytes, which are read once.  A
+// workgroup takes 16 outputs; its waves divide K in turns of kSlab bytes, straight from
+// memory to matrix operands (any address), and add their sums through LDS.
+constexpr int kSlab = 256;
+constexpr int kFewWaves = 8;
+constexpr int kFewTokens = 64;
+
+template <typename Tout, int GT, bool MAP>
+__global__ __launch_bounds__(kFewWaves * 64) void matmul_few_kernel(Layer L) {
+    __shared__ i32x4 part[kFewWaves][GT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q16 = lane >> 4;
+    const int n0 = blockIdx.x * 16;
+    const int8_t* w = L.weight + (int64_t)min(n0 + l16, L.N - 1) * L.weight_stride;
+    const int8_t* t[GT];
+#pragma unroll
+    for (int g = 0; g < GT; ++g) t[g] = L.codes + min((int64_t)(g * 16 + l16), L.M - 1) * L.codes_stride;
+    const int K = L.K;
+    i32x4 acc[GT] = {};
+    for (int k0 = wave * kSlab; k0 < K; k0 += kFewWaves * kSlab) {
+        i32x4 a[kSlab / 64], b[GT][kSlab / 64];
+        if (k0 + kSlab <= K) {
+#pragma unroll
+            for (int h = 0; h < kSlab / 64; ++h) __builtin_memcpy(&a[h], w + k0 + h * 64 + q16 * 16, 16);
+#pragma unroll
+            for (int g = 0; g < GT; ++g)
+#pragma unroll
+                for (int h = 0; h < kSlab / 64; ++h) __builtin_memcpy(&b[g][h], t[g] + k0 + h * 64 + q16 * 16, 16);
+        } else {
+#pragma unroll
+            for (int h = 0; h < kSlab / 64; ++h) a[h] = load_unit(w, k0 + h * 64 + q16 * 16, K);
+#pragma unroll
+            for (int g = 0; g < GT; ++g)
+#pragma unroll
+                for (int h = 0; h < kSlab / 64; ++h) b[g][h] = load_unit(t[g], k0 + h * 64 + q16 * 16, K);
+        }
+#pragma unroll
+        for (int h = 0; h < kSlab / 64; ++h)
+#pragma unroll
+            for (int g = 0; g < GT; ++g)
+                acc[g] = MAP ? __builtin_amdgcn_mfma_i32_16x16x64_i8(b[g][h], a[h], acc[g], 0, 0, 0)
+                             : __builtin_amdgcn_mfma_i32_16x16x64_i8(a[h], b[g][h], acc[g], 0, 0, 0);
+    }
+#pragma unroll
+    for (int g = 0; g < GT; ++g) part[wave][g][lane] = acc[g];
+    __syncthreads();
+    if (wave >= GT) return;
+    i32x4 sum = part[0][wave][lane];
+#pragma unroll
+    for (int v = 1; v < kFewWaves; ++v) sum += part[v][wave][lane];
+    // MAP: the lane has output n0 + l16 of four tokens; rows: four outputs of token l16
+    const int64_t i = MAP ? n0 + l16 : wave * 16 + l16, j = MAP ? wave * 16 + q16 * 4 : n0 + q16 * 4;
+    const int64_t I = MAP ? L.N : L.M, J = MAP ? L.M : L.N;
+    if (i < I && j < J) store_outputs<Tout>(L, i, j, J, sum);
+}
+
+template <typename Tout, int GT>
+hipError_t run_few(const Layer& L, hipStream_t s) {
+    static_assert(GT <= kFewWaves, "a wave adds up one group of tokens");
+    const dim3 grid((unsigned)ceil_div64(L.N, 16));
+    if (L.map) matmul_few_kernel<Tout, GT, true><<<grid, kFewWaves * 64, 0, s>>>(L);
+    else matmul_few_kernel<Tout, GT, false><<<grid, kFewWaves * 64, 0, s>>>(L);
+    return hipGetLastError();
 }
 
 hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, hipStream_t s) {
-    for (int64_t m = 0; m < L.M; m += kSlabTokens) {
+    if (L.M <= 16) return out_dtype == DSS_BF16 ? run_few<uint16_t, 1>(L, s) : run_few<float, 1>(L, s);
+    if (L.M <= 32) return out_dtype == DSS_BF16 ? run_few<uint16_t, 2>(L, s) : run_few<float, 2>(L, s);
+    if (L.M <= kFewTokens) return out_dtype == DSS_BF16 ? run_few<uint16_t, 4>(L, s) : run_few<float, 4>(L, s);
+    auto whole = [](const int8_t* p, int64_t stride, int64_t rows) {
+        return (uintptr_t)p % 16 == 0 && (stride % 16 == 0 || rows == 1);
+    };
+    const bool dma = L.K % 16 == 0 && whole(L.codes, L.codes_stride, L.M) && whole(L.weight, L.weight_stride, L.N);
+    // a launch has fewer than 2^32 threads
+    const int64_t slab = std::max<int64_t>(256, (((int64_t)1 << 34) / L.N) / 256 * 256);
+    for (int64_t m = 0; m < L.M; m += slab) {
         Layer S = L;
-        S.M = std::min(L.M - m, kSlabTokens);
+        S.M = std::min(L.M - m, slab);
         S.codes += m * L.codes_stride;
         S.scales += m;
         S.out = static_cast<char*>(L.out) + m * (L.map ? 1 : L.ldo) * (int64_t)dtype_size(out_dtype);
-        const int64_t ti = ceil_div64(S.map ? S.N : S.M, kTile), tj = ceil_div64(S.map ? S.M : S.N, kTile);
-        const dim3 grid((unsigned)(ti * tj));
-        if (out_dtype == DSS_BF16) matmul_any_kernel<uint16_t><<<grid, 256, 0, s>>>(S, (int)tj);
-        else matmul_any_kernel<float><<<grid, 256, 0, s>>>(S, (int)tj);
-        const hipError_t e = hipGetLastError();
+        hipError_t e;
+        if (out_dtype == DSS_BF16) e = dma ? run_product<uint16_t, true>(S, s) : run_product<uint16_t, false>(S, s);
+        else e = dma ? run_product<float, true>(S, s) : run_product<float, false>(S, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
