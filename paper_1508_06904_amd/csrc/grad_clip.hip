@@ -171,6 +171,106 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(TensorTable t, const dou
     }
 }
 
+// ------------------------------------------------------------------ short lists, in one launch
+// One workgroup of 16 waves: the waves take runs of kShortRun values in turn, sum
+// their squares, meet for the total and scale the same runs, now in cache.
+constexpr int kShortTable = 16;
+constexpr int kShortWaves = 16;
+constexpr int kShortRun = 1024;          // 16 values of each lane
+constexpr int kShortRuns = 2 * kShortWaves;
+
+struct ShortTable {
+    const void* in[kShortTable];
+    void* out[kShortTable];
+    int32_t count[kShortTable];
+    int16_t first[kShortTable];
+    int16_t dtype[kShortTable];
+    int32_t n, runs;
+};
+
+template <typename T>
+__device__ __forceinline__ double short_squares(const T* p, int n, double s) {
+    const int lane = threadIdx.x & 63;
+    float v[kShortRun / 64];
+#pragma unroll
+    for (int k = 0; k < kShortRun / 64; ++k) v[k] = k * 64 + lane < n ? to_f32(p[k * 64 + lane]) : 0.f;
+#pragma unroll
+    for (int k = 0; k < kShortRun / 64; ++k) s = fma((double)v[k], (double)v[k], s);
+    return s;
+}
+
+template <typename T>
+__device__ __forceinline__ void short_scale(const T* p, T* q, int n, float c) {
+    const int lane = threadIdx.x & 63;
+    float v[kShortRun / 64];
+#pragma unroll
+    for (int k = 0; k < kShortRun / 64; ++k) v[k] = k * 64 + lane < n ? to_f32(p[k * 64 + lane]) : 0.f;
+#pragma unroll
+    for (int k = 0; k < kShortRun / 64; ++k)
+        if (k * 64 + lane < n) store_elem(&q[k * 64 + lane], v[k] * c);
+}
+
+__global__ __launch_bounds__(kShortWaves * 64) void clip_short_kernel(ShortTable t, float max_norm, int clip,
+                                                                      float* norm) {
+    __shared__ double part[kShortWaves];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    int at[kShortRuns / kShortWaves], left[kShortRuns / kShortWaves], who[kShortRuns / kShortWaves];
+    double s = 0;
+#pragma unroll
+    for (int u = 0; u < kShortRuns / kShortWaves; ++u) {
+        const int r = wave + u * kShortWaves;
+        left[u] = 0;
+        if (r >= t.runs) continue;
+        int k = 0;
+        for (int i = 1; i < t.n; ++i)
+            if (t.first[i] <= r) k = i;
+        who[u] = k;
+        at[u] = (r - t.first[k]) * kShortRun;
+        left[u] = min(t.count[k] - at[u], kShortRun);
+        if (t.dtype[k] == DSS_BF16) s = short_squares((const uint16_t*)t.in[k] + at[u], left[u], s);
+        else s = short_squares((const float*)t.in[k] + at[u], left[u], s);
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) part[wave] = s;
+    __syncthreads();
+    s = 0;
+#pragma unroll
+    for (int w = 0; w < kShortWaves; ++w) s += part[w];
+    const double total = sqrt(s);
+    if (threadIdx.x == 0) *norm = (float)total;
+    if (!clip) return;
+    const float c = coefficient(total, max_norm);
+#pragma unroll
+    for (int u = 0; u < kShortRuns / kShortWaves; ++u) {
+        if (left[u] == 0) continue;
+        const int k = who[u];
+        if (c == 1.f && t.in[k] == t.out[k]) continue;
+        if (t.dtype[k] == DSS_BF16)
+            short_scale((const uint16_t*)t.in[k] + at[u], (uint16_t*)t.out[k] + at[u], left[u], c);
+        else
+            short_scale((const float*)t.in[k] + at[u], (float*)t.out[k] + at[u], left[u], c);
+    }
+}
+
+// Whether the list is a short one, and its table.
+bool short_table(const dss_tensor* g, void* const* out, int32_t n, ShortTable* t) {
+    t->n = t->runs = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        if (g[i].count == 0) continue;
+        if (t->n == kShortTable || g[i].count > kShortRuns * kShortRun) return false;
+        t->in[t->n] = g[i].data;
+        t->out[t->n] = out ? out[i] : nullptr;
+        t->count[t->n] = (int32_t)g[i].count;
+        t->first[t->n] = (int16_t)t->runs;
+        t->dtype[t->n] = (int16_t)g[i].dtype;
+        t->runs += (int32_t)ceil_div64(g[i].count, kShortRun);
+        if (t->runs > kShortRuns) return false;
+        ++t->n;
+    }
+    return true;
+}
+
 // Runs of 2^shift values: about four of them for each workgroup of a full launch, none shorter than kMinRun.
 int pick_shift(int64_t total) {
     int shift = 12;
@@ -226,6 +326,12 @@ dss_status grad_common(const dss_tensor* grads, void* const* out, int32_t n, boo
                     (long long)workspace_bytes, (long long)DSS_GRAD_NORM_WORKSPACE_BYTES);
     static_assert(kMaxGroups * sizeof(double) <= DSS_GRAD_NORM_WORKSPACE_BYTES, "partial sums");
 
+    ShortTable brief;
+    if (short_table(grads, out, n, &brief)) {
+        clip_short_kernel<<<1, kShortWaves * 64, 0, stream>>>(brief, max_norm, clip, norm);
+        hipError_t e = hipGetLastError();
+        return e == hipSuccess ? DSS_OK : hip_fail(e, "gradient clipping launch");
+    }
     double* partial = static_cast<double*>(workspace);
     const int shift = pick_shift(total);
     TensorTable t;
@@ -233,14 +339,12 @@ dss_status grad_common(const dss_tensor* grads, void* const* out, int32_t n, boo
     int groups = 1;
     for (int32_t at = 0; next_table(grads, out, n, shift, &at, &t);) groups = std::max(groups, std::min(t.runs, kMaxGroups));
     int32_t at = 0;
-    bool more = next_table(grads, out, n, shift, &at, &t);
-    for (int add = 0; more || !add; add = 1) {
+    for (int add = 0; next_table(grads, out, n, shift, &at, &t); add = 1) {
         norm_partial_kernel<<<dim3(add ? std::min(t.runs, kMaxGroups) : groups), kThreads, 0, stream>>>(t, partial, add);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return hip_fail(e, "gradient norm launch");
-        more = next_table(grads, out, n, shift, &at, &t);
     }
-    if (!clip || total == 0) {
+    if (!clip) {
         norm_total_kernel<<<1, kThreads, 0, stream>>>(partial, groups, norm);
         hipError_t e = hipGetLastError();
         return e == hipSuccess ? DSS_OK : hip_fail(e, "gradient norm launch");

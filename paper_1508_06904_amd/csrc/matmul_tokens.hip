@@ -15,6 +15,7 @@
 #include "dev_common.h"
 #include "dss_internal.h"
 #include "tokens.h"
+#include "tokens_device.h"
 
 namespace dss {
 
@@ -273,36 +274,105 @@ constexpr int kSlab = 256;
 constexpr int kFewWaves = 8;
 constexpr int kFewTokens = 64;
 
-template <typename Tout, int GT, bool MAP>
-__global__ __launch_bounds__(kFewWaves * 64) void matmul_few_kernel(Layer L) {
+// Where the tokens come from: codes in memory (Code = int8_t), or values that the
+// workgroup codes itself into LDS (float, uint16_t), which costs every workgroup a
+// reading of all tokens and saves a launch and the codes' way through memory.
+struct FewValues {
+    const void* x;
+    int64_t token_stride, channel_stride;
+};
+constexpr int kFewValues = 16384;        // values that a workgroup codes at most (their tokens as a power of two)
+
+// Codes and scales of the M <= 16 tokens, in LDS: codes[m * pitch + k], zeros from K to the pitch.
+template <typename T>
+__device__ void code_few(const FewValues& V, int M, int K, int pitch, int8_t* codes, float* scales, uint32_t* tops) {
+    constexpr int E = Chunk<T>::E, THREADS = kFewWaves * 64, CH = 2 * kFewValues / THREADS / E;
+    // THREADS / 2^b lanes for each token
+    const int b = M <= 1 ? 0 : 32 - __clz(M - 1);
+    const int lanes = THREADS >> b, m = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    if (threadIdx.x < 16) tops[threadIdx.x] = 0;
+    __syncthreads();
+    Chunk<T> c[CH];
+    uint32_t top = 0;
+    if (m < M) {
+        const T* row = static_cast<const T*>(V.x) + m * V.token_stride;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int at = (i * lanes + lane) * E;
+            if (V.channel_stride == 1) {
+                c[i] = load_chunk(row + at, K - at);
+            } else {
+#pragma unroll
+                for (int k = 0; k < E; ++k) c[i].v[k] = at + k < K ? row[(at + k) * V.channel_stride] : T(0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int k = 0; k < E; ++k) top = max(top, abs_bits(to_f32(c[i].v[k])));
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    if ((threadIdx.x & 31) == 0 && m < M) atomicMax(&tops[m], top);   // (a maximum has no order)
+    __syncthreads();
+    if (m < M) {
+        const float scale = scale_of(tops[m]);
+        if (lane == 0) scales[m] = scale;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int at = (i * lanes + lane) * E;
+            if (at < pitch) store_codes(codes + m * pitch + at, c[i], scale, E);
+        }
+    }
+    __syncthreads();
+}
+
+// The codes' row length in LDS: whole slabs and 16 bytes, so that tokens start in different banks.
+__host__ __device__ constexpr int few_pitch(int K) { return (K + kSlab - 1) / kSlab * kSlab + 16; }
+
+template <typename Code, typename Tout, int GT, bool MAP>
+__global__ __launch_bounds__(kFewWaves * 64) void matmul_few_kernel(Layer L, FewValues V) {
+    constexpr bool kCodes = sizeof(Code) == 1;
     __shared__ i32x4 part[kFewWaves][GT][64];
+    __shared__ float own_scales[16];
+    __shared__ uint32_t tops[16];
+    extern __shared__ __align__(16) int8_t own_codes[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q16 = lane >> 4;
     const int n0 = blockIdx.x * 16;
     const int8_t* w = L.weight + (int64_t)min(n0 + l16, L.N - 1) * L.weight_stride;
     const int8_t* t[GT];
-#pragma unroll
-    for (int g = 0; g < GT; ++g) t[g] = L.codes + min((int64_t)(g * 16 + l16), L.M - 1) * L.codes_stride;
     const int K = L.K;
+    constexpr int H = kSlab / 64;
+    auto fetch = [&](const int8_t* row, int k0, i32x4* to) {
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            if (k0 + kSlab <= K) __builtin_memcpy(&to[h], row + k0 + h * 64 + q16 * 16, 16);
+            else to[h] = load_unit(row, k0 + h * 64 + q16 * 16, K);
+        }
+    };
+    i32x4 a[H], b[GT][H];
+    if constexpr (kCodes) {
+#pragma unroll
+        for (int g = 0; g < GT; ++g) t[g] = L.codes + min((int64_t)(g * 16 + l16), L.M - 1) * L.codes_stride;
+    } else {
+        code_few<Code>(V, (int)L.M, K, few_pitch(K), own_codes, own_scales, tops);
+        t[0] = own_codes + min(l16, (int)L.M - 1) * few_pitch(K);
+        L.scales = own_scales;
+    }
     i32x4 acc[GT] = {};
     for (int k0 = wave * kSlab; k0 < K; k0 += kFewWaves * kSlab) {
-        i32x4 a[kSlab / 64], b[GT][kSlab / 64];
-        if (k0 + kSlab <= K) {
+        fetch(w, k0, a);
 #pragma unroll
-            for (int h = 0; h < kSlab / 64; ++h) __builtin_memcpy(&a[h], w + k0 + h * 64 + q16 * 16, 16);
+        for (int g = 0; g < GT; ++g) {
+            if constexpr (kCodes) {
+                fetch(t[g], k0, b[g]);
+            } else {
 #pragma unroll
-            for (int g = 0; g < GT; ++g)
-#pragma unroll
-                for (int h = 0; h < kSlab / 64; ++h) __builtin_memcpy(&b[g][h], t[g] + k0 + h * 64 + q16 * 16, 16);
-        } else {
-#pragma unroll
-            for (int h = 0; h < kSlab / 64; ++h) a[h] = load_unit(w, k0 + h * 64 + q16 * 16, K);
-#pragma unroll
-            for (int g = 0; g < GT; ++g)
-#pragma unroll
-                for (int h = 0; h < kSlab / 64; ++h) b[g][h] = load_unit(t[g], k0 + h * 64 + q16 * 16, K);
+                for (int h = 0; h < H; ++h) b[g][h] = *reinterpret_cast<const i32x4*>(t[g] + k0 + h * 64 + q16 * 16);
+            }
         }
 #pragma unroll
-        for (int h = 0; h < kSlab / 64; ++h)
+        for (int h = 0; h < H; ++h)
 #pragma unroll
             for (int g = 0; g < GT; ++g)
                 acc[g] = MAP ? __builtin_amdgcn_mfma_i32_16x16x64_i8(b[g][h], a[h], acc[g], 0, 0, 0)
@@ -321,19 +391,38 @@ __global__ __launch_bounds__(kFewWaves * 64) void matmul_few_kernel(Layer L) {
     if (i < I && j < J) store_outputs<Tout>(L, i, j, J, sum);
 }
 
-template <typename Tout, int GT>
-hipError_t run_few(const Layer& L, hipStream_t s) {
+template <typename Code, typename Tout, int GT>
+hipError_t run_few(const Layer& L, const FewValues& V, hipStream_t s) {
     static_assert(GT <= kFewWaves, "a wave adds up one group of tokens");
     const dim3 grid((unsigned)ceil_div64(L.N, 16));
-    if (L.map) matmul_few_kernel<Tout, GT, true><<<grid, kFewWaves * 64, 0, s>>>(L);
-    else matmul_few_kernel<Tout, GT, false><<<grid, kFewWaves * 64, 0, s>>>(L);
+    const size_t lds = sizeof(Code) == 1 ? 0 : (size_t)L.M * few_pitch(L.K);
+    if (L.map) matmul_few_kernel<Code, Tout, GT, true><<<grid, kFewWaves * 64, lds, s>>>(L, V);
+    else matmul_few_kernel<Code, Tout, GT, false><<<grid, kFewWaves * 64, lds, s>>>(L, V);
     return hipGetLastError();
 }
 
+// Whether the few-token kernel codes M tokens of K channels itself.
+bool codes_itself(int64_t M, int K) {
+    if (M > 16) return false;
+    int p = 1;
+    while (p < M) p *= 2;
+    return (int64_t)p * K <= kFewValues;
+}
+
+template <typename Code>
+hipError_t launch_linear_few(const Layer& L, const FewValues& V, dss_dtype out_dtype, hipStream_t s) {
+    return out_dtype == DSS_BF16 ? run_few<Code, uint16_t, 1>(L, V, s) : run_few<Code, float, 1>(L, V, s);
+}
+
+template <typename Tout>
+hipError_t run_few_codes(const Layer& L, hipStream_t s) {
+    if (L.M <= 16) return run_few<int8_t, Tout, 1>(L, FewValues{}, s);
+    if (L.M <= 32) return run_few<int8_t, Tout, 2>(L, FewValues{}, s);
+    return run_few<int8_t, Tout, 4>(L, FewValues{}, s);
+}
+
 hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, hipStream_t s) {
-    if (L.M <= 16) return out_dtype == DSS_BF16 ? run_few<uint16_t, 1>(L, s) : run_few<float, 1>(L, s);
-    if (L.M <= 32) return out_dtype == DSS_BF16 ? run_few<uint16_t, 2>(L, s) : run_few<float, 2>(L, s);
-    if (L.M <= kFewTokens) return out_dtype == DSS_BF16 ? run_few<uint16_t, 4>(L, s) : run_few<float, 4>(L, s);
+    if (L.M <= kFewTokens) return out_dtype == DSS_BF16 ? run_few_codes<uint16_t>(L, s) : run_few_codes<float>(L, s);
     auto whole = [](const int8_t* p, int64_t stride, int64_t rows) {
         return (uintptr_t)p % 16 == 0 && (stride % 16 == 0 || rows == 1);
     };
@@ -389,7 +478,7 @@ dss_status check_layer(int64_t M, const int8_t* weight, int64_t weight_stride, c
 
 int64_t workspace_bytes_of(int64_t M, int32_t N, int32_t K, bool from_codes) {
     (void)N;
-    return from_codes ? 0 : align256(M * 4) + align256(M * padded_k(K));
+    return from_codes || codes_itself(M, K) ? 0 : align256(M * 4) + align256(M * padded_k(K));
 }
 
 dss_status check_room(int64_t need, const void* workspace, int64_t workspace_bytes) {
@@ -462,14 +551,21 @@ extern "C" dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t 
     if (M == 0) return DSS_OK;
     s = check_room(workspace_bytes_of(M, N, K, false), workspace, workspace_bytes);
     if (s != DSS_OK) return s;
+    const bool map = is_map(M, N, out_token_stride, out_channel_stride);
+    const int64_t ldo = map ? out_channel_stride : out_token_stride;
+    if (codes_itself(M, K)) {
+        const Layer L = {nullptr, 0, nullptr, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out, ldo, map};
+        const FewValues V = {x, token_stride, channel_stride};
+        hipError_t e = dtype == DSS_BF16 ? launch_linear_few<uint16_t>(L, V, out_dtype, stream)
+                                         : launch_linear_few<float>(L, V, out_dtype, stream);
+        return e == hipSuccess ? DSS_OK : hip_fail(e, "token product launch");
+    }
     float* scales = static_cast<float*>(workspace);
     int8_t* codes = static_cast<int8_t*>(workspace) + align256(M * 4);
     const int Kp = padded_k(K);
     hipError_t e = launch_quantize_tokens(dtype, x, M, K, token_stride, channel_stride, codes, Kp, Kp, scales, stream);
     if (e != hipSuccess) return hip_fail(e, "quantize launch");
-    const bool map = is_map(M, N, out_token_stride, out_channel_stride);
-    const Layer L = {codes, Kp, scales, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out,
-                     map ? out_channel_stride : out_token_stride, map};
+    const Layer L = {codes, Kp, scales, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out, ldo, map};
     e = launch_matmul(L, out_dtype, stream);
     return e == hipSuccess ? DSS_OK : hip_fail(e, "token product launch");
 } catch (...) {

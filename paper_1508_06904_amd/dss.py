@@ -11,6 +11,7 @@ Layers are the dicts produced by `workloads`:
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 
@@ -522,36 +523,44 @@ def defrag(x, k_h, k_w, S_h, S_w, out=None, stream=None):
 
 
 # ---------------------------------------------------------------------------- gradient norm and clipping
+#
+# These calls and the token calls below run for a few microseconds on small inputs, about what
+# their arguments' checks cost here: each check is made once, with torch's cheapest query for it.
+
+_DTYPE_CODE = None      # torch dtype -> dss_dtype, once torch is there
+
 
 def _dtype_codes():
-    global _dtype_code
-    if _dtype_code is None:
+    global _DTYPE_CODE
+    if _DTYPE_CODE is None:
         import torch
-        _dtype_code = {torch.float32: DSS_F32, torch.bfloat16: DSS_BF16}
-    return _dtype_code
+        _DTYPE_CODE = {torch.float32: DSS_F32, torch.bfloat16: DSS_BF16}
+    return _DTYPE_CODE
 
 
-_dtype_code = None
-
-
-def _on_current_device(device, what):
+def _launch(stream):
+    """(current device's index, stream handle) of a call; None stands for the current stream."""
     import torch
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ValueError("%s must be on the current CUDA device (got %s)" % (what, device))
+    if not torch.cuda.is_initialized():
+        if not torch.cuda.is_available():
+            raise ValueError("the tensors must be on a CUDA device, and there is none")
+        torch.cuda.init()
+    dev = torch._C._cuda_getDevice()
+    return dev, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
-def _allocate_on(stream):
-    """A context in which new tensors belong to `stream` (None: the current one), so that
-    their memory is not given to another stream's work while the call's kernels use it."""
-    import contextlib
+def _empty(shape, dtype, stream):
+    """A new tensor on the current device.  It belongs to `stream` (None: the current one), so that
+    its memory is not given to another stream's work while the call's kernels use it."""
     import torch
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device="cuda")
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device="cuda")
 
 
 def _is_dense(t):
     """Whether t's elements fill a block of memory in some order of its axes."""
-    if t.is_contiguous():
-        return True
     n = 1
     for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
         if stride != n:
@@ -560,44 +569,34 @@ def _is_dense(t):
     return True
 
 
-def _listed(tensors, what):
+def _tensor_list(tensors, what, dev):
+    """The C list of CUDA tensors (dss_tensor[n]: address, count, dtype and a zero, as three 64-bit
+    words each) and the tensors as a list."""
     import torch
-    if not isinstance(tensors, torch.Tensor):
-        tensors = list(tensors)
-        if all([isinstance(t, torch.Tensor) for t in tensors]):
-            return tensors
-    raise ValueError("%s must be a list of tensors" % what)
-
-
-def _tensor_list(tensors, what):
-    """The C list of CUDA tensors (dss_tensor[n], as a numpy array) and their device."""
-    codes = _dtype_codes()
-    devices = {t.device for t in tensors}
-    if len(devices) > 1:
-        raise ValueError("%s are on several devices" % what)
-    for d in devices:
-        _on_current_device(d, what)
-    dtypes = [codes.get(t.dtype, -1) for t in tensors]
-    if -1 in dtypes:
-        raise ValueError("%s must be float32 or bfloat16 (got %s)" % (what, tensors[dtypes.index(-1)].dtype))
-    if not all([_is_dense(t) for t in tensors]):
-        raise ValueError("%s must be dense in memory, without gaps or repeated elements" % what)
-    a = np.empty(len(tensors), dtype=_TENSOR)
-    a["data"] = [t.data_ptr() for t in tensors]
-    a["count"] = [t.numel() for t in tensors]
-    a["dtype"] = dtypes
-    return a
-
-
-_TENSOR = np.dtype([("data", "<u8"), ("count", "<i8"), ("dtype", "<i4"), ("reserved", "<i4")])
+    if isinstance(tensors, torch.Tensor):
+        raise ValueError("%s must be a list of tensors" % what)
+    codes, tensors, words = _dtype_codes(), list(tensors), []
+    for t in tensors:
+        if not isinstance(t, torch.Tensor):
+            raise ValueError("%s must be a list of tensors" % what)
+        code = codes.get(t.dtype)
+        if code is None:
+            raise ValueError("%s must be float32 or bfloat16 (got %s)" % (what, t.dtype))
+        if t.get_device() != dev:
+            raise ValueError("%s must be on the current CUDA device (got %s)" % (what, t.device))
+        if not (t.is_contiguous() or _is_dense(t)):
+            raise ValueError("%s must be dense in memory, without gaps or repeated elements" % what)
+        words += (t.data_ptr(), t.numel(), code)
+    return array.array("q", words), tensors
 
 
 def grad_norm(grads, norm=None, workspace=None, stream=None):
     """The norm of a gradient over a list of CUDA tensors (float32 and bfloat16, dense in
     memory, any sizes): sqrt of the sum of all squares, as a float32 tensor of no axes."""
-    a = _tensor_list(_listed(grads, "grads"), "grads")
-    norm, wp, wb, keep = _norm_buffers(norm, workspace, stream)
-    _check(lib().dss_grad_norm(a.ctypes.data, len(a), _ptr(norm), wp, wb, _stream(stream)), "dss_grad_norm")
+    dev, handle = _launch(stream)
+    a, grads = _tensor_list(grads, "grads", dev)
+    norm, wp, wb, keep = _norm_buffers(norm, workspace, dev, stream)
+    _check(lib().dss_grad_norm(a.buffer_info()[0], len(grads), norm.data_ptr(), wp, wb, handle), "dss_grad_norm")
     return norm
 
 
@@ -606,70 +605,89 @@ def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None
     Returns (norm, list of scaled tensors).  `out` is the list of tensors to write, of the
     same shapes, strides and types (`out=grads` clips in place); allocated if None."""
     import torch
+    dev, handle = _launch(stream)
     in_place = out is grads
-    grads = _listed(grads, "grads")
-    a = _tensor_list(grads, "grads")
+    a, grads = _tensor_list(grads, "grads", dev)
     if in_place:
-        out, b = grads, a
+        b, out = a, grads
     else:
         if out is None:
-            with _allocate_on(stream):
+            if stream is None:
                 out = [torch.empty_like(g) for g in grads]
-        out = _listed(out, "out")
-        b = _tensor_list(out, "out")
-        if len(b) != len(a) or not all([o.shape == g.shape and o.stride() == g.stride() and o.dtype == g.dtype
-                                        for o, g in zip(out, grads)]):
+            else:
+                with torch.cuda.stream(stream):
+                    out = [torch.empty_like(g) for g in grads]
+        b, out = _tensor_list(out, "out", dev)
+        # counts and types at once; shapes and strides one by one
+        if b[1::3] != a[1::3] or b[2::3] != a[2::3] or not all([o.shape == g.shape for o, g in zip(out, grads)]) or \
+                not all([o.stride() == g.stride() for o, g in zip(out, grads) if not g.is_contiguous()
+                         or not o.is_contiguous()]):
             raise ValueError("out must be of grads' shapes, strides and types")
-    norm, wp, wb, keep = _norm_buffers(norm, workspace, stream)
-    ptrs = np.ascontiguousarray(b["data"])
-    _check(lib().dss_clip_grads(a.ctypes.data, ptrs.ctypes.data, len(a), float(max_norm), _ptr(norm), wp, wb,
-                                _stream(stream)), "dss_clip_grads")
+    norm, wp, wb, keep = _norm_buffers(norm, workspace, dev, stream)
+    ptrs = b[0::3]
+    _check(lib().dss_clip_grads(a.buffer_info()[0], ptrs.buffer_info()[0], len(grads), max_norm, norm.data_ptr(), wp, wb,
+                                handle), "dss_clip_grads")
     return norm, out
 
 
-def _norm_buffers(norm, workspace, stream):
+def _norm_buffers(norm, workspace, dev, stream):
     import torch
-    with _allocate_on(stream):
-        if norm is None:
-            norm = torch.empty((), dtype=torch.float32, device="cuda")
-        if workspace is None:
-            workspace = torch.empty(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
-    _check_buffer(norm, "norm", torch.float32, 1)
-    wp, wb = _workspace_args(workspace, norm.device)
-    return norm, wp, wb, workspace
+    if norm is None:
+        norm = _empty((), torch.float32, stream)
+    elif not isinstance(norm, torch.Tensor) or norm.dtype != torch.float32 or norm.numel() != 1 or \
+            norm.get_device() != dev:
+        raise ValueError("norm must be one float32 on the current CUDA device")
+    if workspace is None:
+        workspace = _empty(GRAD_NORM_WORKSPACE_BYTES, torch.uint8, stream)
+        return norm, workspace.data_ptr(), GRAD_NORM_WORKSPACE_BYTES, workspace
+    return (norm,) + _room(workspace, dev) + (workspace,)
+
+
+def _room(workspace, dev):
+    """(address, bytes) of a caller's workspace."""
+    import torch
+    if not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 # ---------------------------------------------------------------------------- tokens in 8 bits
 
-def _check_tokens(x, what):
+def _check_tokens(x, dev):
+    """dss_dtype, M, K of a matrix of tokens."""
     import torch
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
-        raise ValueError("%s must be a tensor [tokens][channels]" % what)
-    _on_current_device(x.device, what)
+        raise ValueError("x must be a tensor [tokens][channels]")
+    dt = _dtype_codes().get(x.dtype)
+    if dt is None:
+        raise ValueError("x must be float32 or bfloat16 (got %s)" % x.dtype)
+    if x.get_device() != dev:
+        raise ValueError("x must be on the current CUDA device (got %s)" % x.device)
+    return dt, x.shape[0], x.shape[1]
 
 
-def _check_vector(t, what, dtype, n):
+def _check_vector(t, what, n, dev):
+    """The address of n float32 values."""
     import torch
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of %d elements" % (what, dtype, n))
-    _on_current_device(t.device, what)
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or \
+            not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError("%s must be a contiguous float32 tensor of %d elements on the current CUDA device" % (what, n))
+    return t.data_ptr()
 
 
-def _check_codes(t, what, rows, channels):
+def _check_codes(t, what, rows, channels, dev):
+    """(address, row stride) of a matrix of codes; one row alone may have any stride."""
     import torch
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.int8 or t.dim() != 2 or (rows is not None and
-                                                                                   t.shape[0] != rows) or \
-            (channels is not None and t.shape[1] != channels):
-        raise ValueError("%s must be an int8 tensor [%s][%s]" % (what, "rows" if rows is None else rows,
-                                                                 "channels" if channels is None else channels))
-    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int8 or t.dim() != 2 or t.get_device() != dev:
+        raise ValueError("%s must be an int8 matrix on the current CUDA device" % what)
+    m, k = t.shape
+    if rows is not None and m != rows or channels is not None and k != channels:
+        raise ValueError("%s must be [%s][%s] (got [%d][%d])" % (what, "any" if rows is None else rows,
+                                                                 "any" if channels is None else channels, m, k))
+    rs, cs = t.stride()
+    if k > 1 and cs != 1 or m > 1 and rs < k:
         raise ValueError("%s must have adjacent channels and rows that do not overlap" % what)
-    _on_current_device(t.device, what)
-
-
-def _row_stride(t):
-    """The stride between a matrix's rows; one row alone may have any."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return t.data_ptr(), rs if m > 1 else max(rs, k)
 
 
 def quantize_tokens(x, codes=None, scales=None, stream=None):
@@ -680,59 +698,52 @@ def quantize_tokens(x, codes=None, scales=None, stream=None):
     Returns (codes int8 [M][K], scales float32 [M]).  A weight matrix [N][K] is coded the
     same way, with a scale for each output channel."""
     import torch
-    _check_tokens(x, "x")
-    dt = _dtype_codes().get(x.dtype)
-    if dt is None:
-        raise ValueError("x must be float32 or bfloat16 (got %s)" % x.dtype)
-    M, K = x.shape
-    with _allocate_on(stream):
-        if codes is None:
-            codes = torch.empty((M, K), dtype=torch.int8, device=x.device)
-        if scales is None:
-            scales = torch.empty((M,), dtype=torch.float32, device=x.device)
-    _check_codes(codes, "codes", M, K)
-    _check_vector(scales, "scales", torch.float32, M)
-    _check(lib().dss_quantize_tokens(_ptr(x), dt, M, K, x.stride(0), x.stride(1), _ptr(codes), _row_stride(codes),
-                                     _ptr(scales), _stream(stream)), "dss_quantize_tokens")
+    dev, handle = _launch(stream)
+    dt, M, K = _check_tokens(x, dev)
+    if codes is None:
+        codes = _empty((M, K), torch.int8, stream)
+    if scales is None:
+        scales = _empty(M, torch.float32, stream)
+    cp, cstride = _check_codes(codes, "codes", M, K, dev)
+    sp = _check_vector(scales, "scales", M, dev)
+    ts, ks = x.stride()
+    _check(lib().dss_quantize_tokens(x.data_ptr(), dt, M, K, ts, ks, cp, cstride, sp, handle), "dss_quantize_tokens")
     return codes, scales
 
 
-def _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, device, stream):
-    """Checks a layer's weights and output; returns (out [M][N] to write, N, the C arguments around them)."""
+def _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, dev, stream):
+    """Checks a layer's weights and output: (out, N, the C arguments from the weight to the output's strides)."""
     import torch
-    _check_codes(weight, "weight", None, K)
+    wp, wstride = _check_codes(weight, "weight", None, K, dev)
     N = weight.shape[0]
-    _check_vector(weight_scales, "weight_scales", torch.float32, N)
-    if bias is not None:
-        _check_vector(bias, "bias", torch.float32, N)
+    sp = _check_vector(weight_scales, "weight_scales", N, dev)
+    bp = None if bias is None else _check_vector(bias, "bias", N, dev)
     if act not in ACTS:
         raise ValueError("unknown activation %r" % (act,))
-    shape = (N, M) if planar else (M, N)
+    codes, shape = _dtype_codes(), (N, M) if planar else (M, N)
     if out is None:
-        if out_dtype not in _dtype_codes():
+        out_dtype = out_dtype or torch.float32
+        if out_dtype not in codes:
             raise ValueError("out_dtype must be float32 or bfloat16 (got %s)" % out_dtype)
-        with _allocate_on(stream):
-            out = torch.empty(shape, dtype=out_dtype, device=device)
-    elif not isinstance(out, torch.Tensor) or out.shape != shape or out.dtype not in _dtype_codes() or \
-            out.device != device:
-        raise ValueError("out must be a float32 or bfloat16 tensor of shape %s on %s" % (shape, device))
-    ts, cs = (out.stride(1), out.stride(0)) if planar else out.stride()
-    pre = (_ptr(weight), _row_stride(weight), _ptr(weight_scales), N, K, None if bias is None else _ptr(bias),
-           ACTS[act], _ptr(out), _dtype_codes()[out.dtype], ts, cs)
-    return out, N, pre
+        out = _empty(shape, out_dtype, stream)
+    elif not isinstance(out, torch.Tensor) or out.shape != shape or out.dtype not in codes or out.get_device() != dev:
+        raise ValueError("out must be a float32 or bfloat16 tensor of shape %s on the current CUDA device" % (shape,))
+    s0, s1 = out.stride()
+    return out, N, (wp, wstride, sp, N, K, bp, ACTS[act], out.data_ptr(), codes[out.dtype]) + \
+        ((s1, s0) if planar else (s0, s1))
 
 
-def _tokens_room(M, N, K, from_codes, workspace, device, stream):
-    if workspace is None:
-        import torch
-        need = ctypes.c_int64()
-        _check(lib().dss_tokens_workspace(M, N, K, from_codes, ctypes.byref(need)), "dss_tokens_workspace")
-        if need.value == 0:
-            return ctypes.c_void_p(None), 0, None
-        with _allocate_on(stream):
-            workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
-    wp, wb = _workspace_args(workspace, device)
-    return wp, wb, workspace
+def _tokens_room(M, N, K, from_codes, workspace, dev, stream):
+    """(address, bytes) of a call's workspace, and what keeps it."""
+    import torch
+    if workspace is not None:
+        return _room(workspace, dev) + (workspace,)
+    need = ctypes.c_int64()
+    _check(lib().dss_tokens_workspace(M, N, K, from_codes, need), "dss_tokens_workspace")
+    if need.value == 0:
+        return None, 0, None
+    workspace = _empty(need.value, torch.uint8, stream)
+    return workspace.data_ptr(), need.value, workspace
 
 
 def matmul_i8(codes, scales, weight, weight_scales, bias=None, act="none", out=None, out_dtype=None, planar=False,
@@ -742,15 +753,13 @@ def matmul_i8(codes, scales, weight, weight_scales, bias=None, act="none", out=N
       y[m][n] = act(scales[m] * weight_scales[n] * sum_k codes[m][k] * weight[n][k] + bias[n]),
     the sum exact.  act is "none", "relu" or "tanh".  Returns out, [M][N] or with planar=True the
     dense map [N][M], of out_dtype (float32 unless given); an `out` of any row stride is taken."""
-    import torch
-    _check_codes(codes, "codes", None, None)
+    dev, handle = _launch(stream)
+    cp, cstride = _check_codes(codes, "codes", None, None, dev)
     M, K = codes.shape
-    _check_vector(scales, "scales", torch.float32, M)
-    out, N, args = _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype or torch.float32, planar,
-                               codes.device, stream)
-    wp, wb, keep = _tokens_room(M, N, K, 1, workspace, codes.device, stream)
-    _check(lib().dss_matmul_tokens(_ptr(codes), _row_stride(codes), _ptr(scales), M, *args, wp, wb, _stream(stream)),
-           "dss_matmul_tokens")
+    sp = _check_vector(scales, "scales", M, dev)
+    out, N, args = _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, dev, stream)
+    room, size, keep = _tokens_room(M, N, K, 1, workspace, dev, stream)
+    _check(lib().dss_matmul_tokens(cp, cstride, sp, M, *args, room, size, handle), "dss_matmul_tokens")
     return out
 
 
@@ -758,15 +767,10 @@ def linear_i8(x, weight, weight_scales, bias=None, act="none", out=None, out_dty
               workspace=None, stream=None):
     """matmul_i8 on float32 or bfloat16 tokens x [M][K], given as for quantize_tokens: codes them
     and multiplies in one call, with the same bits as the two calls."""
-    import torch
-    _check_tokens(x, "x")
-    dt = _dtype_codes().get(x.dtype)
-    if dt is None:
-        raise ValueError("x must be float32 or bfloat16 (got %s)" % x.dtype)
-    M, K = x.shape
-    out, N, args = _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype or torch.float32, planar,
-                               x.device, stream)
-    wp, wb, keep = _tokens_room(M, N, K, 0, workspace, x.device, stream)
-    _check(lib().dss_linear_tokens(_ptr(x), dt, M, x.stride(0), x.stride(1), *args, wp, wb, _stream(stream)),
-           "dss_linear_tokens")
+    dev, handle = _launch(stream)
+    dt, M, K = _check_tokens(x, dev)
+    ts, ks = x.stride()
+    out, N, args = _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, dev, stream)
+    room, size, keep = _tokens_room(M, N, K, 0, workspace, dev, stream)
+    _check(lib().dss_linear_tokens(x.data_ptr(), dt, M, ts, ks, *args, room, size, handle), "dss_linear_tokens")
     return out

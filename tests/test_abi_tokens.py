@@ -14,7 +14,7 @@ VP = ctypes.c_void_p
 
 
 def _list(*items):
-    a = np.zeros(max(1, len(items)), dtype=dss._TENSOR)
+    a = np.zeros(max(1, len(items)), dtype=[("data", "<u8"), ("count", "<i8"), ("dtype", "<i4"), ("reserved", "<i4")])
     for n, (data, count, dtype) in enumerate(items):
         a[n] = (data, count, dtype, 0)
     return a
@@ -101,7 +101,7 @@ def test_matmul_refusals(status, kw):
 @pytest.mark.parametrize("status,kw", SHARED + [
     (INVALID, dict(x=None)), (INVALID, dict(x=PTR + 2)), (UNSUPPORTED, dict(dt=3)), (INVALID, dict(ts=-64)),
     (UNSUPPORTED, dict(ts=128, ks=2)), (UNSUPPORTED, dict(K=131072, ts=131072, ws=131072)),
-    (INVALID, dict(room=None)), (INVALID, dict(room=PTR + 16)), (SHAPE, dict(bytes=100)),
+    (INVALID, dict(M=500, room=None)), (INVALID, dict(M=500, room=PTR + 16)), (SHAPE, dict(M=500, bytes=100)),
 ], ids=str)
 def test_linear_refusals(status, kw):
     assert _linear(**kw) == status
@@ -110,7 +110,7 @@ def test_linear_refusals(status, kw):
 def test_workspace_query():
     need = ctypes.c_int64()
     q = dss.lib().dss_tokens_workspace
-    assert q(4, 8, 64, 0, ctypes.byref(need)) == OK and need.value >= 4 * 64 + 4 * 4
+    assert q(400, 8, 64, 0, ctypes.byref(need)) == OK and need.value >= 400 * 64 + 400 * 4
     assert q(1 << 33, 8, 64, 0, ctypes.byref(need)) == OK and need.value >= (1 << 33) * 68
     assert q(0, 8, 64, 0, ctypes.byref(need)) == OK
     for bad in ((-1, 8, 64), (4, 0, 64), (4, 8, 0)):
