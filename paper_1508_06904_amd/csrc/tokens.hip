@@ -44,19 +44,19 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const T* __rest
     const T* row = x + m * token_stride;
     Chunk<T> c[CH];
     uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < CH; ++i) c[i] = load_chunk(row + (i * LPR + lane) * E, K - (i * LPR + lane) * E);
+    load_row(c, row, lane, LPR, K);
 #pragma unroll
     for (int i = 0; i < CH; ++i)
 #pragma unroll
         for (int k = 0; k < E; ++k) top = max(top, abs_bits(to_f32(c[i].v[k])));
     const float scale = scale_of(row_max<LPR>(top));
     if (lane == 0) scales[m] = scale;
+    const Coder coder(scale);
     int8_t* out = codes + m * codes_stride;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int at = (i * LPR + lane) * E;
-        if (at < Kp) store_codes(out + at, c[i], scale, Kp - at);
+        if (at < Kp) store_codes(out + at, c[i], coder, Kp - at);
     }
 }
 
@@ -77,9 +77,10 @@ __global__ __launch_bounds__(kThreads) void quantize_long_rows_kernel(const T* _
     }
     const float scale = scale_of(row_max<kThreads>(top));
     if (threadIdx.x == 0) scales[m] = scale;
+    const Coder coder(scale);
     int8_t* out = codes + m * codes_stride;
     for (int64_t at = threadIdx.x * E; at < Kp; at += kThreads * E)
-        store_codes(out + at, load_chunk(row + at, (int)(K - at)), scale, (int)(Kp - at));
+        store_codes(out + at, load_chunk(row + at, (int)(K - at)), coder, (int)(Kp - at));
 }
 
 // Maps: a workgroup takes 64 adjacent tokens; a wave reads them of one channel at
@@ -106,11 +107,12 @@ __global__ __launch_bounds__(kThreads) void quantize_map_kernel(const T* __restr
     __syncthreads();
     top = max(max(tops[t], tops[64 + t]), max(tops[128 + t], tops[192 + t]));
     const float scale = scale_of(top);
+    const Coder coder(scale);
     if (in && w == 0) scales[m0 + t] = scale;
     for (int k0 = 0; k0 < Kp; k0 += 64) {
         __syncthreads();
         for (int k = w; k < 64; k += kThreads / 64)
-            tile[t * kMapPitch + k] = in && k0 + k < K ? (int8_t)code_of(to_f32(col[(k0 + k) * channel_stride]), scale) : 0;
+            tile[t * kMapPitch + k] = in && k0 + k < K ? coder.one(to_f32(col[(k0 + k) * channel_stride])) : 0;
         __syncthreads();
         // 4 lanes of 16 bytes for each token
         const int tok = threadIdx.x >> 2, at = (threadIdx.x & 3) * 16;
