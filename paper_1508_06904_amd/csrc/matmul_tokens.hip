@@ -304,14 +304,13 @@ __device__ void code_few(const FewValues& V, int M, int K, int pitch, int8_t* co
 #pragma unroll
                 for (int k = 0; k < E; ++k) {
                     const int at = (i * lanes + lane) * E + k;
-                    c[i].v[k] = at < K ? row[at * V.channel_stride] : T(0);
+                    if (at < K) c[i].set(k, row[at * V.channel_stride]);
                 }
         }
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int k = 0; k < E; ++k) top = max(top, abs_bits(to_f32(c[i].v[k])));
+        for (int i = 0; i < CH; ++i) top = raise(top, c[i]);
     }
+    top = top_bits<T>(top);
 #pragma unroll
     for (int d = 16; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
     if ((threadIdx.x & 31) == 0 && m < M) atomicMax(&tops[m], top);   // (a maximum has no order)

@@ -46,10 +46,8 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(const T* __rest
     uint32_t top = 0;
     load_row(c, row, lane, LPR, K);
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
-#pragma unroll
-        for (int k = 0; k < E; ++k) top = max(top, abs_bits(to_f32(c[i].v[k])));
-    const float scale = scale_of(row_max<LPR>(top));
+    for (int i = 0; i < CH; ++i) top = raise(top, c[i]);
+    const float scale = scale_of(row_max<LPR>(top_bits<T>(top)));
     if (lane == 0) scales[m] = scale;
     const Coder coder(scale);
     int8_t* out = codes + m * codes_stride;
@@ -70,12 +68,8 @@ __global__ __launch_bounds__(kThreads) void quantize_long_rows_kernel(const T* _
     const int64_t m = blockIdx.x;
     const T* row = x + m * token_stride;
     uint32_t top = 0;
-    for (int64_t at = threadIdx.x * E; at < K; at += kThreads * E) {
-        const Chunk<T> c = load_chunk(row + at, (int)(K - at));
-#pragma unroll
-        for (int k = 0; k < E; ++k) top = max(top, abs_bits(to_f32(c.v[k])));
-    }
-    const float scale = scale_of(row_max<kThreads>(top));
+    for (int64_t at = threadIdx.x * E; at < K; at += kThreads * E) top = raise(top, load_chunk(row + at, (int)(K - at)));
+    const float scale = scale_of(row_max<kThreads>(top_bits<T>(top)));
     if (threadIdx.x == 0) scales[m] = scale;
     const Coder coder(scale);
     int8_t* out = codes + m * codes_stride;
@@ -83,50 +77,47 @@ __global__ __launch_bounds__(kThreads) void quantize_long_rows_kernel(const T* _
         store_codes(out + at, load_chunk(row + at, (int)(K - at)), coder, (int)(Kp - at));
 }
 
-// Maps: a workgroup takes 64 adjacent tokens; a wave reads them of one channel at
-// a time.  The second reading, from cache, goes through LDS, which turns 64
-// channels of the 64 tokens round so that a token's codes leave together.
-constexpr int kMapTokens = 64;
-constexpr int kMapPitch = kMapTokens + 4;    // bytes of a token's row in LDS
-
+// Maps: see MapTile.  Of more channels than a workgroup holds the values are read
+// twice, the second time mostly from cache.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void quantize_map_kernel(const T* __restrict__ x, int64_t M, int K,
-                                                                int64_t channel_stride, int8_t* __restrict__ codes,
-                                                                int64_t codes_stride, int Kp,
-                                                                float* __restrict__ scales) {
-    __shared__ uint32_t tops[kThreads];
-    __shared__ __align__(16) int8_t tile[kMapTokens * kMapPitch];
-    const int t = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t m0 = (int64_t)blockIdx.x * kMapTokens;
-    const bool in = m0 + t < M;
-    const T* col = x + m0 + t;
-    uint32_t top = 0;
-    if (in)
-        for (int k = w; k < K; k += kThreads / 64) top = max(top, abs_bits(to_f32(col[k * channel_stride])));
-    tops[threadIdx.x] = top;
-    __syncthreads();
-    top = max(max(tops[t], tops[64 + t]), max(tops[128 + t], tops[192 + t]));
-    const float scale = scale_of(top);
-    const Coder coder(scale);
-    if (in && w == 0) scales[m0 + t] = scale;
-    for (int k0 = 0; k0 < Kp; k0 += 64) {
-        __syncthreads();
-        for (int k = w; k < 64; k += kThreads / 64)
-            tile[t * kMapPitch + k] = in && k0 + k < K ? coder.one(to_f32(col[(k0 + k) * channel_stride])) : 0;
-        __syncthreads();
-        // 4 lanes of 16 bytes for each token
-        const int tok = threadIdx.x >> 2, at = (threadIdx.x & 3) * 16;
-        if (m0 + tok < M && k0 + at < Kp) {
-            int8_t* p = codes + (m0 + tok) * codes_stride + k0 + at;
-            const int8_t* q = tile + tok * kMapPitch + at;
-            const int n = min(16, Kp - k0 - at);
-            if (n == 16) {
-                uint32_t v[4];
+__global__ __launch_bounds__(kMapWaves * 64) void quantize_map_kernel(const T* __restrict__ x, int64_t M, int K,
+                                                                      int64_t channel_stride,
+                                                                      int8_t* __restrict__ codes, int64_t codes_stride,
+                                                                      int Kp, float* __restrict__ scales) {
+    using Tile = MapTile<T>;
+    __shared__ uint32_t tops[kMapWaves * 64];
+    const int64_t m0 = (int64_t)blockIdx.x * Tile::kTokens;
+    const int left = (int)min(M - m0, (int64_t)Tile::kTokens);
+    const int span = (int)(blockDim.x >> 6) * 64;      // channels held at once
+    Tile tile;
+    uint32_t top[4] = {};
+    tile.load(x + m0, channel_stride, left, 0, K);
+    tile.raise_into(top);
+    for (int k0 = span; k0 < K; k0 += span) {
+        tile.load(x + m0, channel_stride, left, k0, K);
+        tile.raise_into(top);
+    }
+    Tile::meet(top, tops);
+    const int t = (threadIdx.x & 15) * Tile::V;
+    const int rounds = (K + span - 1) / span;
+    for (int round = rounds - 1; round >= 0; --round) {
+        // (the last span is still there)
+        if (round != rounds - 1) tile.load(x + m0, channel_stride, left, round * span, K);
+        const int k = round * span + (int)(threadIdx.x >> 4) * 16;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const uint32_t*>(q + 4 * j);
-                __builtin_memcpy(p, v, 16);
+        for (int j = 0; j < Tile::V; ++j) {
+            const Coder coder(scale_of(Tile::bits(top, j)));
+            if (t + j >= left) continue;
+            if (round == 0 && threadIdx.x < 16) scales[m0 + t + j] = coder.scale;
+            uint32_t w[4];
+            tile.codes(j, coder, w);
+            int8_t* p = codes + (m0 + t + j) * codes_stride + k;
+            if (k + 16 <= Kp) {
+                __builtin_memcpy(p, w, 16);
             } else {
-                for (int j = 0; j < n; ++j) p[j] = q[j];
+#pragma unroll
+                for (int b = 0; b < 16; ++b)
+                    if (k + b < Kp) p[b] = (int8_t)(w[b / 4] >> (8 * (b % 4)));
             }
         }
     }
@@ -143,12 +134,14 @@ void run_quantize(const T* x, int64_t M, int K, int64_t ts, int64_t ks, int8_t* 
                   hipStream_t s) {
     constexpr int E = Chunk<T>::E;
     if (ks != 1 && K > 1) {
-        quantize_map_kernel<T><<<dim3((unsigned)ceil_div64(M, kMapTokens)), kThreads, 0, s>>>(x, M, K, ks, codes, cs, Kp,
-                                                                                             scales);
+        const int waves = std::min<int>((K + 63) / 64, kMapWaves);
+        quantize_map_kernel<T><<<dim3((unsigned)ceil_div64(M, MapTile<T>::kTokens)), waves * 64, 0, s>>>(x, M, K, ks, codes,
+                                                                                                      cs, Kp, scales);
         return;
     }
     // as many lanes for a token as leave each of them a few chunks to have in flight
-    if (Kp <= 16 * E) run_rows<T, 16, 1>(x, M, K, ts, codes, cs, Kp, scales, s);
+    if (Kp <= 4 * E) run_rows<T, 4, 1>(x, M, K, ts, codes, cs, Kp, scales, s);
+    else if (Kp <= 16 * E) run_rows<T, 16, 1>(x, M, K, ts, codes, cs, Kp, scales, s);
     else if (Kp <= 64 * E) run_rows<T, 16, 4>(x, M, K, ts, codes, cs, Kp, scales, s);
     else if (Kp <= 256 * E) run_rows<T, 64, 4>(x, M, K, ts, codes, cs, Kp, scales, s);
     else if (Kp <= 1024 * E) run_rows<T, 256, 4>(x, M, K, ts, codes, cs, Kp, scales, s);

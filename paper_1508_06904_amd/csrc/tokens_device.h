@@ -11,10 +11,20 @@ namespace dss {
 
 constexpr uint32_t kInfBits = 0x7f800000u;
 
+// 16 bytes of a row, as words: their values unpack where they are used.
 template <typename T>
-struct Chunk {                            // 16 bytes of a row
+struct Chunk {
     static constexpr int E = 16 / (int)sizeof(T);
-    T v[E];
+    uint32_t w[4] = {};
+
+    __device__ __forceinline__ float value(int k) const {
+        if constexpr (E == 4) return __uint_as_float(w[k]);
+        else return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+    }
+    __device__ __forceinline__ void set(int k, T v) {  // (over a zero)
+        if constexpr (E == 4) w[k] = __builtin_bit_cast(uint32_t, v);
+        else w[k / 2] |= (uint32_t)v << (16 * (k & 1));
+    }
 };
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
@@ -61,6 +71,29 @@ struct Coder {
     __device__ __forceinline__ int8_t one(float x) const { return (int8_t)((tiny ? tiny_bits(x) : bits(x)) & keep); }
 };
 
+// The largest |value| so far of each of a word's values: of one, or of two at a time.
+template <typename T>
+__device__ __forceinline__ uint32_t raise(uint32_t top, uint32_t word) {
+    if constexpr (sizeof(T) == 4) {
+        return max(top, word & 0x7fffffffu);
+    } else {
+        using u16x2 = __attribute__((ext_vector_type(2))) uint16_t;
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top),
+                                                                      __builtin_bit_cast(u16x2, word & 0x7fff7fffu)));
+    }
+}
+template <typename T>
+__device__ __forceinline__ uint32_t raise(uint32_t top, const Chunk<T>& c) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = raise<T>(top, c.w[k]);
+    return top;
+}
+// The bits of the largest of a word's values, as binary32.
+template <typename T>
+__device__ __forceinline__ uint32_t top_bits(uint32_t top) {
+    return sizeof(T) == 4 ? top : max(top << 16, top & 0xffff0000u);
+}
+
 // E consecutive values from p on, those from n on as zeros (n may be negative).
 template <typename T>
 __device__ __forceinline__ Chunk<T> load_chunk(const T* p, int n) {
@@ -69,7 +102,8 @@ __device__ __forceinline__ Chunk<T> load_chunk(const T* p, int n) {
         __builtin_memcpy(&r, p, 16);
     } else {
 #pragma unroll
-        for (int k = 0; k < Chunk<T>::E; ++k) r.v[k] = k < n ? p[k] : T(0);
+        for (int k = 0; k < Chunk<T>::E; ++k)
+            if (k < n) r.set(k, p[k]);
     }
     return r;
 }
@@ -92,7 +126,7 @@ __device__ __forceinline__ void load_row(Chunk<T> (&c)[CH], const T* row, int la
         if (i * lanes + lane == last) {
 #pragma unroll
             for (int k = 0; k < E - 1; ++k)
-                if (last * E + k < K) c[i].v[k] = row[last * E + k];
+                if (last * E + k < K) c[i].set(k, row[last * E + k]);
         }
 }
 
@@ -103,7 +137,7 @@ __device__ __forceinline__ void store_codes(int8_t* p, const Chunk<T>& x, const 
     uint32_t w[E / 4];
 #pragma unroll
     for (int j = 0; j < E / 4; ++j)
-        w[j] = coder.four(to_f32(x.v[4 * j]), to_f32(x.v[4 * j + 1]), to_f32(x.v[4 * j + 2]), to_f32(x.v[4 * j + 3]));
+        w[j] = coder.four(x.value(4 * j), x.value(4 * j + 1), x.value(4 * j + 2), x.value(4 * j + 3));
     if (n >= E) {
         __builtin_memcpy(p, w, E);
     } else {
@@ -112,5 +146,73 @@ __device__ __forceinline__ void store_codes(int8_t* p, const Chunk<T>& x, const 
             if (k < n) p[k] = (int8_t)(w[k / 4] >> (8 * (k % 4)));
     }
 }
+
+// ------------------------------------------------------------------ tiles of a map
+// A workgroup of up to kMapWaves waves holds kLaneTokens * 16 adjacent tokens of up to
+// 64 channels for each wave in registers.  16 lanes read 16 bytes each of one channel, 256 adjacent
+// bytes; a lane keeps 16 adjacent channels of its tokens, so that each token's
+// codes leave it as 16 bytes, with no turning round through LDS.
+constexpr int kMapWaves = 16;
+
+template <typename T>
+struct MapTile {
+    static constexpr int V = 16 / (int)sizeof(T);      // tokens of a lane
+    static constexpr int kTokens = 16 * V;
+    Chunk<T> c[16];                                    // c[r].value(j): channel r of the lane's group, token j
+
+    // The tile's tokens start at x, `left` of them exist; channels k0 + 64 wave + 16 (lane / 16) + r < K.
+    __device__ __forceinline__ void load(const T* x, int64_t channel_stride, int left, int k0, int K) {
+        const int t = (threadIdx.x & 15) * V, k = k0 + (int)(threadIdx.x >> 4) * 16;
+        const T* p = x + t + k * channel_stride;
+        if (left >= kTokens) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                c[r] = Chunk<T>{};
+                if (k + r < K) __builtin_memcpy(&c[r], p + r * channel_stride, 16);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                c[r] = Chunk<T>{};
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (k + r < K && t + j < left) c[r].set(j, p[r * channel_stride + j]);
+            }
+        }
+    }
+    __device__ __forceinline__ void raise_into(uint32_t (&top)[4]) const {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top[j] = raise<T>(top[j], c[r].w[j]);
+    }
+    // Each of the lane's tokens' largest value over all of the workgroup's lanes; tops has 64 words for each wave.
+    static __device__ __forceinline__ void meet(uint32_t (&top)[4], uint32_t* tops) {
+        const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            top[j] = raise<T>(top[j], (uint32_t)__shfl_xor((int)top[j], 16));
+            top[j] = raise<T>(top[j], (uint32_t)__shfl_xor((int)top[j], 32));
+        }
+        if (lane < 16)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) tops[((threadIdx.x >> 6) * 16 + lane) * 4 + j] = top[j];
+        __syncthreads();
+        for (int w = 0; w < waves; ++w)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top[j] = raise<T>(top[j], tops[(w * 16 + (lane & 15)) * 4 + j]);
+    }
+    // Token j's of these.
+    static __device__ __forceinline__ uint32_t bits(const uint32_t (&top)[4], int j) {
+        if constexpr (V == 4) return top[j];
+        else return j & 1 ? top[j / 2] & 0xffff0000u : top[j / 2] << 16;
+    }
+    // The 16 codes of token j's channels.
+    __device__ __forceinline__ void codes(int j, const Coder& coder, uint32_t (&w)[4]) const {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            w[q] = coder.four(c[4 * q].value(j), c[4 * q + 1].value(j), c[4 * q + 2].value(j), c[4 * q + 3].value(j));
+    }
+};
 
 }  // namespace dss
