@@ -21,35 +21,6 @@ namespace dss {
 
 namespace {
 
-using i32x4 = __attribute__((ext_vector_type(4))) int;
-
-struct Layer {
-    const int8_t* codes;
-    int64_t codes_stride;
-    const float* scales;
-    int64_t M;
-    const int8_t* weight;
-    int64_t weight_stride;
-    const float* weight_scales;
-    int N, K;
-    const float* bias;
-    int act;
-    void* out;
-    int64_t ldo;                         // the output's stride that is not 1
-    int map;                             // out is [N][M], not [M][N]
-};
-
-// A NaN stays one (fmaxf would make it 0).
-__device__ __forceinline__ float activate_nan(int act, float v) {
-    if (act == DSS_ACT_RELU) return v < 0.f ? 0.f : v;
-    if (act == DSS_ACT_TANH) return tanhf(v);
-    return v;
-}
-
-__device__ __forceinline__ float output_of(int sum, float wscale, float scale, float bias, int act) {
-    return activate_nan(act, (float)sum * wscale * scale + bias);
-}
-
 // D's operands and extents.
 struct Sides {
     const int8_t *P, *Q;
@@ -58,34 +29,6 @@ struct Sides {
 __host__ __device__ __forceinline__ Sides sides_of(const Layer& L) {
     if (L.map) return {L.weight, L.codes, L.weight_stride, L.codes_stride, L.N, L.M};
     return {L.codes, L.weight, L.codes_stride, L.weight_stride, L.M, L.N};
-}
-
-// Four adjacent outputs D[i][j .. j+3] of a layer, those from J on left out.
-template <typename Tout>
-__device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum) {
-    Tout* p = static_cast<Tout*>(L.out) + i * L.ldo + j;
-    struct Four {
-        Tout v[4];
-    } r;
-    const int n = (int)min(J - j, (int64_t)4);
-    if (L.map) {
-        const float ws = L.weight_scales[i], b = L.bias ? L.bias[i] : 0.f;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) store_elem(&r.v[k], output_of(sum[k], ws, k < n ? L.scales[j + k] : 0.f, b, L.act));
-    } else {
-        const float s = L.scales[i];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            store_elem(&r.v[k], output_of(sum[k], k < n ? L.weight_scales[j + k] : 0.f, s,
-                                          L.bias && k < n ? L.bias[j + k] : 0.f, L.act));
-    }
-    if (n == 4) {
-        __builtin_memcpy(p, &r, sizeof r);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 3; ++k)
-            if (k < n) p[k] = r.v[k];
-    }
 }
 
 // ------------------------------------------------------------------ tiles
@@ -104,24 +47,6 @@ constexpr int kUnits = kStep / 16;
 __device__ __attribute__((aligned(16))) const unsigned int g_zero16[4] = {0u, 0u, 0u, 0u};
 
 typedef __attribute__((address_space(3))) void lds_void;
-
-// Bytes k .. k+15 of a row of K bytes, zeros past its end; nothing past the end is read.
-__device__ __forceinline__ i32x4 load_unit(const int8_t* row, int k, int K) {
-    i32x4 v = {};
-    if (k + 16 <= K) {
-        __builtin_memcpy(&v, row + k, 16);
-    } else if (k < K) {
-        if (K >= 16) {
-            unsigned __int128 w;
-            __builtin_memcpy(&w, row + K - 16, 16);
-            w >>= 8 * (k + 16 - K);
-            __builtin_memcpy(&v, &w, 16);
-        } else {
-            for (int b = 0; b < K - k; ++b) v[b >> 2] |= (int)(uint8_t)row[k + b] << (8 * (b & 3));
-        }
-    }
-    return v;
-}
 
 // Workgroups are handed to the 8 XCDs in turn: the id of the tile that makes the
 // tiles of one XCD (and of its L2) neighbours.
@@ -266,191 +191,8 @@ hipError_t run_product(const Layer& L, hipStream_t s) {
     }
 }
 
-// ------------------------------------------------------------------ few tokens
-// At most 16 GT tokens: bound by the weights' bytes, which are read once.  A
-// workgroup takes 16 outputs; its waves divide K in turns of kSlab bytes, straight from
-// memory to matrix operands (any address), and add their sums through LDS.
-constexpr int kSlab = 256;
-constexpr int kFewWaves = 8;
-constexpr int kFewTokens = 64;
-
-// Where the tokens come from: codes in memory (Code = int8_t), or values that the
-// workgroup codes itself into LDS (float, uint16_t), which costs every workgroup a
-// reading of all tokens and saves a launch and the codes' way through memory.
-struct FewValues {
-    const void* x;
-    int64_t token_stride, channel_stride;
-};
-constexpr int kFewValues = 16384;        // values that a workgroup codes at most (their tokens as a power of two)
-
-// Codes and scales of the M <= 16 tokens, in LDS: codes[m * pitch + k], zeros from K to the pitch.
-template <typename T>
-__device__ void code_few(const FewValues& V, int M, int K, int pitch, int8_t* codes, float* scales, uint32_t* tops) {
-    constexpr int E = Chunk<T>::E, THREADS = kFewWaves * 64, CH = 2 * kFewValues / THREADS / E;
-    // THREADS / 2^b lanes for each token
-    const int b = M <= 1 ? 0 : 32 - __clz(M - 1);
-    const int lanes = THREADS >> b, m = threadIdx.x / lanes, lane = threadIdx.x % lanes;
-    if (threadIdx.x < 16) tops[threadIdx.x] = 0;
-    __syncthreads();
-    Chunk<T> c[CH];
-    uint32_t top = 0;
-    if (m < M) {
-        const T* row = static_cast<const T*>(V.x) + m * V.token_stride;
-        if (V.channel_stride == 1) {
-            load_row(c, row, lane, lanes, K);
-        } else {
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int k = 0; k < E; ++k) {
-                    const int at = (i * lanes + lane) * E + k;
-                    if (at < K) c[i].set(k, row[at * V.channel_stride]);
-                }
-        }
-#pragma unroll
-        for (int i = 0; i < CH; ++i) top = raise(top, c[i]);
-    }
-    top = top_bits<T>(top);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    if ((threadIdx.x & 31) == 0 && m < M) atomicMax(&tops[m], top);   // (a maximum has no order)
-    __syncthreads();
-    if (m < M) {
-        const Coder coder(scale_of(tops[m]));
-        if (lane == 0) scales[m] = coder.scale;
-#pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const int at = (i * lanes + lane) * E;
-            if (at < pitch) store_codes(codes + m * pitch + at, c[i], coder, E);
-        }
-    }
-    __syncthreads();
-}
-
-// The codes' row length in LDS: whole slabs and 16 bytes, so that tokens start in different banks.
-__host__ __device__ constexpr int few_pitch(int K) { return (K + kSlab - 1) / kSlab * kSlab + 16; }
-
-template <typename Code, typename Tout, int GT, bool MAP>
-__global__ __launch_bounds__(kFewWaves * 64) void matmul_few_kernel(Layer L, FewValues V, int R) {
-    constexpr bool kCodes = sizeof(Code) == 1;
-    __shared__ i32x4 part[kFewWaves][GT][64];
-    __shared__ float own_scales[16];
-    __shared__ uint32_t tops[16];
-    extern __shared__ __align__(16) int8_t own_codes[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q16 = lane >> 4;
-    const int8_t* t[GT];
-    const int K = L.K;
-    constexpr int H = kSlab / 64;
-    auto weights = [&](int tile) { return L.weight + (int64_t)min(tile * R + min(l16, R - 1), L.N - 1) * L.weight_stride; };
-    auto fetch = [&](const int8_t* row, int k0, i32x4* to) {
-#pragma unroll
-        for (int h = 0; h < H; ++h) __builtin_memcpy(&to[h], row + k0 + h * 64 + q16 * 16, 16);
-    };
-    auto multiply = [](i32x4 u, i32x4 v, i32x4 c) {
-        return MAP ? __builtin_amdgcn_mfma_i32_16x16x64_i8(v, u, c, 0, 0, 0)
-                   : __builtin_amdgcn_mfma_i32_16x16x64_i8(u, v, c, 0, 0, 0);
-    };
-    i32x4 a[H], b[GT][H];
-    // the first weights are on their way while the tokens are coded
-    const int8_t* w = weights(blockIdx.x);
-    const int k_first = wave * kSlab, k_whole = K / kSlab * kSlab;
-    if (!kCodes && k_first < k_whole) fetch(w, k_first, a);
-    if constexpr (kCodes) {
-#pragma unroll
-        for (int g = 0; g < GT; ++g) t[g] = L.codes + min((int64_t)(g * 16 + l16), L.M - 1) * L.codes_stride;
-    } else {
-        code_few<Code>(V, (int)L.M, K, few_pitch(K), own_codes, own_scales, tops);
-        t[0] = own_codes + min(l16, (int)L.M - 1) * few_pitch(K);
-        L.scales = own_scales;
-    }
-    const int tiles = (L.N + R - 1) / R;
-    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        if (tile != (int)blockIdx.x) {
-            w = weights(tile);
-            __syncthreads();             // the sums of the last tile have been read
-        }
-        i32x4 acc[GT] = {};
-        auto fetch_tokens = [&](int k0) {
-#pragma unroll
-            for (int g = 0; g < GT; ++g) {
-                if constexpr (kCodes) {
-                    fetch(t[g], k0, b[g]);
-                } else {
-#pragma unroll
-                    for (int h = 0; h < H; ++h) b[g][h] = *reinterpret_cast<const i32x4*>(t[g] + k0 + h * 64 + q16 * 16);
-                }
-            }
-        };
-        for (int k0 = k_first; k0 < k_whole; k0 += kFewWaves * kSlab) {
-            if (kCodes || k0 != k_first || tile != (int)blockIdx.x) fetch(w, k0, a);
-            fetch_tokens(k0);
-#pragma unroll
-            for (int h = 0; h < H; ++h)
-#pragma unroll
-                for (int g = 0; g < GT; ++g) acc[g] = multiply(a[h], b[g][h], acc[g]);
-        }
-        // the slab that K ends in, if it ends in one
-        if (k_whole < K && k_whole / kSlab % kFewWaves == wave) {
-#pragma unroll 1
-            for (int k0 = k_whole; k0 < K; k0 += 64) {
-                const int k = k0 + q16 * 16;
-                const i32x4 u = load_unit(w, k, K);
-#pragma unroll
-                for (int g = 0; g < GT; ++g) {
-                    const i32x4 v = kCodes ? load_unit(t[g], k, K) : *reinterpret_cast<const i32x4*>(t[g] + k);
-                    acc[g] = multiply(u, v, acc[g]);
-                }
-            }
-        }
-#pragma unroll
-        for (int g = 0; g < GT; ++g) part[wave][g][lane] = acc[g];
-        __syncthreads();
-        if (wave >= GT) continue;
-        i32x4 sum = part[0][wave][lane];
-#pragma unroll
-        for (int v = 1; v < kFewWaves; ++v) sum += part[v][wave][lane];
-        // MAP: the lane has output n0 + l16 of four tokens; rows: four outputs of token l16
-        const int n0 = tile * R, n_end = min(n0 + R, L.N);
-        const int64_t i = MAP ? n0 + l16 : wave * 16 + l16, j = MAP ? wave * 16 + q16 * 4 : n0 + q16 * 4;
-        const int64_t I = MAP ? n_end : L.M, J = MAP ? L.M : n_end;
-        if (i < I && j < J) store_outputs<Tout>(L, i, j, J, sum);
-    }
-}
-
-template <typename Code, typename Tout, int GT>
-hipError_t run_few(const Layer& L, const FewValues& V, hipStream_t s) {
-    static_assert(GT <= kFewWaves, "a wave adds up one group of tokens");
-    int R = 16;
-    while (R > 2 && ceil_div64(L.N, R) < 256) R /= 2;
-    const dim3 grid((unsigned)std::min<int64_t>(ceil_div64(L.N, R), sizeof(Code) == 1 ? 4096 : 256));
-    const size_t lds = sizeof(Code) == 1 ? 0 : (size_t)L.M * few_pitch(L.K);
-    if (L.map) matmul_few_kernel<Code, Tout, GT, true><<<grid, kFewWaves * 64, lds, s>>>(L, V, R);
-    else matmul_few_kernel<Code, Tout, GT, false><<<grid, kFewWaves * 64, lds, s>>>(L, V, R);
-    return hipGetLastError();
-}
-
-// Whether the few-token kernel codes M tokens of K channels itself.
-bool codes_itself(int64_t M, int K) {
-    if (M > 16) return false;
-    int p = 1;
-    while (p < M) p *= 2;
-    return (int64_t)p * K <= kFewValues;
-}
-
-template <typename Code>
-hipError_t launch_linear_few(const Layer& L, const FewValues& V, dss_dtype out_dtype, hipStream_t s) {
-    return out_dtype == DSS_BF16 ? run_few<Code, uint16_t, 1>(L, V, s) : run_few<Code, float, 1>(L, V, s);
-}
-
-template <typename Tout>
-hipError_t run_few_codes(const Layer& L, hipStream_t s) {
-    if (L.M <= 16) return run_few<int8_t, Tout, 1>(L, FewValues{}, s);
-    if (L.M <= 32) return run_few<int8_t, Tout, 2>(L, FewValues{}, s);
-    return run_few<int8_t, Tout, 4>(L, FewValues{}, s);
-}
-
 hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, hipStream_t s) {
-    if (L.M <= kFewTokens) return out_dtype == DSS_BF16 ? run_few_codes<uint16_t>(L, s) : run_few_codes<float>(L, s);
+    if (L.M <= kFewTokens) return launch_matmul_few(L, out_dtype, s);
     auto whole = [](const int8_t* p, int64_t stride, int64_t rows) {
         return (uintptr_t)p % 16 == 0 && (stride % 16 == 0 || rows == 1);
     };
@@ -505,8 +247,7 @@ dss_status check_layer(int64_t M, const int8_t* weight, int64_t weight_stride, c
 }
 
 int64_t workspace_bytes_of(int64_t M, int32_t N, int32_t K, bool from_codes) {
-    (void)N;
-    return from_codes || codes_itself(M, K) ? 0 : align256(M * 4) + align256(M * padded_k(K));
+    return from_codes || codes_itself(M, K) || linear_in_tiles(M, N, K) ? 0 : align256(M * 4) + align256(M * padded_k(K));
 }
 
 dss_status check_room(int64_t need, const void* workspace, int64_t workspace_bytes) {
@@ -581,11 +322,11 @@ extern "C" dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t 
     if (s != DSS_OK) return s;
     const bool map = is_map(M, N, out_token_stride, out_channel_stride);
     const int64_t ldo = map ? out_channel_stride : out_token_stride;
-    if (codes_itself(M, K)) {
+    if (codes_itself(M, K) || linear_in_tiles(M, N, K)) {
         const Layer L = {nullptr, 0, nullptr, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out, ldo, map};
-        const FewValues V = {x, token_stride, channel_stride};
-        hipError_t e = dtype == DSS_BF16 ? launch_linear_few<uint16_t>(L, V, out_dtype, stream)
-                                         : launch_linear_few<float>(L, V, out_dtype, stream);
+        const Values V = {x, dtype, token_stride, channel_stride};
+        hipError_t e = codes_itself(M, K) ? launch_linear_few(L, V, out_dtype, stream)
+                                          : launch_linear_tiles(L, V, out_dtype, stream);
         return e == hipSuccess ? DSS_OK : hip_fail(e, "token product launch");
     }
     float* scales = static_cast<float*>(workspace);

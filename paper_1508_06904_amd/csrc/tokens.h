@@ -14,6 +14,42 @@ constexpr int64_t kSlabTokens = (int64_t)1 << 21;
 dss_status check_tokens(const void* x, dss_dtype dtype, int64_t M, int32_t K, int64_t token_stride,
                         int64_t channel_stride);
 
+// A fully connected layer on codes (codes and scales unused where the kernel codes the tokens itself).
+struct Layer {
+    const int8_t* codes;
+    int64_t codes_stride;
+    const float* scales;
+    int64_t M;
+    const int8_t* weight;
+    int64_t weight_stride;
+    const float* weight_scales;
+    int N, K;
+    const float* bias;
+    int act;
+    void* out;
+    int64_t ldo;                         // the output's stride that is not 1
+    int map;                             // out is [N][M], not [M][N]
+};
+
+// Tokens that are not codes yet.
+struct Values {
+    const void* x;
+    dss_dtype dtype;
+    int64_t token_stride, channel_stride;
+};
+
+// The layer for at most kFewTokens tokens (matmul_few.hip); codes_itself: whether
+// the kernel codes M tokens of K channels itself, with no workspace.
+constexpr int kFewTokens = 64;
+hipError_t launch_matmul_few(const Layer& L, dss_dtype out_dtype, hipStream_t s);
+bool codes_itself(int64_t M, int K);
+hipError_t launch_linear_few(const Layer& L, const Values& V, dss_dtype out_dtype, hipStream_t s);
+
+// The layer on many tokens of few channels with few outputs, coded and multiplied
+// in one launch (linear_tile.hip), and whether it runs there.
+bool linear_in_tiles(int64_t M, int N, int K);
+hipError_t launch_linear_tiles(const Layer& L, const Values& V, dss_dtype out_dtype, hipStream_t s);
+
 // Codes and scales of M > 0 tokens; codes[m][K .. Kp-1] are written as zeros.
 hipError_t launch_quantize_tokens(dss_dtype dt, const void* x, int64_t M, int K, int64_t token_stride,
                                   int64_t channel_stride, int8_t* codes, int64_t codes_stride, int Kp, float* scales,

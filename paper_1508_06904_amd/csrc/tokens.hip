@@ -91,19 +91,20 @@ __global__ __launch_bounds__(kMapWaves * 64) void quantize_map_kernel(const T* _
     const int span = (int)(blockDim.x >> 6) * 64;      // channels held at once
     Tile tile;
     uint32_t top[4] = {};
-    tile.load(x + m0, channel_stride, left, 0, K);
+    const int own_k = (int)(threadIdx.x >> 4) * 16;
+    tile.load(x + m0, channel_stride, left, own_k, K);
     tile.raise_into(top);
     for (int k0 = span; k0 < K; k0 += span) {
-        tile.load(x + m0, channel_stride, left, k0, K);
+        tile.load(x + m0, channel_stride, left, k0 + own_k, K);
         tile.raise_into(top);
     }
-    Tile::meet(top, tops);
+    Tile::meet(top, tops, 0, blockDim.x >> 6);
     const int t = (threadIdx.x & 15) * Tile::V;
     const int rounds = (K + span - 1) / span;
     for (int round = rounds - 1; round >= 0; --round) {
         // (the last span is still there)
-        if (round != rounds - 1) tile.load(x + m0, channel_stride, left, round * span, K);
-        const int k = round * span + (int)(threadIdx.x >> 4) * 16;
+        const int k = round * span + own_k;
+        if (round != rounds - 1) tile.load(x + m0, channel_stride, left, k, K);
 #pragma unroll
         for (int j = 0; j < Tile::V; ++j) {
             const Coder coder(scale_of(Tile::bits(top, j)));

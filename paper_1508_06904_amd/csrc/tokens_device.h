@@ -1,4 +1,5 @@
-// Device helpers of the 8-bit tokens: a token's scale and its codes.
+// Device helpers of the 8-bit tokens: a token's scale and its codes, and a layer's
+// outputs from the sums of products.
 //
 // The largest absolute value of a token is taken over the bit patterns: without
 // their sign bits these order as the values do, and infinities and NaN come out
@@ -6,6 +7,7 @@
 #pragma once
 
 #include "dev_common.h"
+#include "tokens.h"
 
 namespace dss {
 
@@ -160,9 +162,9 @@ struct MapTile {
     static constexpr int kTokens = 16 * V;
     Chunk<T> c[16];                                    // c[r].value(j): channel r of the lane's group, token j
 
-    // The tile's tokens start at x, `left` of them exist; channels k0 + 64 wave + 16 (lane / 16) + r < K.
-    __device__ __forceinline__ void load(const T* x, int64_t channel_stride, int left, int k0, int K) {
-        const int t = (threadIdx.x & 15) * V, k = k0 + (int)(threadIdx.x >> 4) * 16;
+    // The tile's tokens start at x, `left` of them exist (or none); the lane's channels k .. k+15, those below K.
+    __device__ __forceinline__ void load(const T* x, int64_t channel_stride, int left, int k, int K) {
+        const int t = (threadIdx.x & 15) * V;
         const T* p = x + t + k * channel_stride;
         if (left >= kTokens) {
 #pragma unroll
@@ -186,9 +188,10 @@ struct MapTile {
 #pragma unroll
             for (int j = 0; j < 4; ++j) top[j] = raise<T>(top[j], c[r].w[j]);
     }
-    // Each of the lane's tokens' largest value over all of the workgroup's lanes; tops has 64 words for each wave.
-    static __device__ __forceinline__ void meet(uint32_t (&top)[4], uint32_t* tops) {
-        const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+    // Each of the lane's tokens' largest value over the lanes of the `waves` waves from `first`
+    // on, which share a tile; tops has 64 words for each wave of the workgroup.
+    static __device__ __forceinline__ void meet(uint32_t (&top)[4], uint32_t* tops, int first, int waves) {
+        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             top[j] = raise<T>(top[j], (uint32_t)__shfl_xor((int)top[j], 16));
@@ -198,7 +201,7 @@ struct MapTile {
 #pragma unroll
             for (int j = 0; j < 4; ++j) tops[((threadIdx.x >> 6) * 16 + lane) * 4 + j] = top[j];
         __syncthreads();
-        for (int w = 0; w < waves; ++w)
+        for (int w = first; w < first + waves; ++w)
 #pragma unroll
             for (int j = 0; j < 4; ++j) top[j] = raise<T>(top[j], tops[(w * 16 + (lane & 15)) * 4 + j]);
     }
@@ -214,5 +217,65 @@ struct MapTile {
             w[q] = coder.four(c[4 * q].value(j), c[4 * q + 1].value(j), c[4 * q + 2].value(j), c[4 * q + 3].value(j));
     }
 };
+
+// ------------------------------------------------------------------ outputs of a layer
+using i32x4 = __attribute__((ext_vector_type(4))) int;
+
+// A NaN stays one (fmaxf would make it 0).
+__device__ __forceinline__ float activate_nan(int act, float v) {
+    if (act == DSS_ACT_RELU) return v < 0.f ? 0.f : v;
+    if (act == DSS_ACT_TANH) return tanhf(v);
+    return v;
+}
+
+__device__ __forceinline__ float output_of(int sum, float wscale, float scale, float bias, int act) {
+    return activate_nan(act, (float)sum * wscale * scale + bias);
+}
+
+// Four adjacent outputs D[i][j .. j+3] of a layer, those from J on left out.
+template <typename Tout>
+__device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum) {
+    Tout* p = static_cast<Tout*>(L.out) + i * L.ldo + j;
+    struct Four {
+        Tout v[4];
+    } r;
+    const int n = (int)min(J - j, (int64_t)4);
+    if (L.map) {
+        const float ws = L.weight_scales[i], b = L.bias ? L.bias[i] : 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) store_elem(&r.v[k], output_of(sum[k], ws, k < n ? L.scales[j + k] : 0.f, b, L.act));
+    } else {
+        const float s = L.scales[i];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            store_elem(&r.v[k], output_of(sum[k], k < n ? L.weight_scales[j + k] : 0.f, s,
+                                          L.bias && k < n ? L.bias[j + k] : 0.f, L.act));
+    }
+    if (n == 4) {
+        __builtin_memcpy(p, &r, sizeof r);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            if (k < n) p[k] = r.v[k];
+    }
+}
+
+// Bytes k .. k+15 of a row of K bytes, zeros past its end; nothing past the end is read.
+__device__ __forceinline__ i32x4 load_unit(const int8_t* row, int k, int K) {
+    i32x4 v = {};
+    if (k + 16 <= K) {
+        __builtin_memcpy(&v, row + k, 16);
+    } else if (k < K) {
+        if (K >= 16) {
+            unsigned __int128 w;
+            __builtin_memcpy(&w, row + K - 16, 16);
+            w >>= 8 * (k + 16 - K);
+            __builtin_memcpy(&v, &w, 16);
+        } else {
+            for (int b = 0; b < K - k; ++b) v[b >> 2] |= (int)(uint8_t)row[k + b] << (8 * (b & 3));
+        }
+    }
+    return v;
+}
 
 }  // namespace dss

@@ -80,6 +80,8 @@ def _linear(x=PTR, dt=0, M=4, ts=64, ks=1, w=PTR, ws=64, wsc=PTR, N=8, K=64, bia
                                        ots, ocs, VP(room), bytes, None)
 
 
+WIDE = dict(M=500, K=2500, ts=2500, ws=2500)       # sizes whose codes need a workspace
+
 SHARED = [
     (INVALID, dict(w=None)), (INVALID, dict(wsc=None)), (INVALID, dict(wsc=PTR + 1)), (INVALID, dict(bias=PTR + 2)),
     (INVALID, dict(out=None)), (INVALID, dict(out=PTR + 2)), (INVALID, dict(out=PTR + 1, odt=1)),
@@ -101,7 +103,7 @@ def test_matmul_refusals(status, kw):
 @pytest.mark.parametrize("status,kw", SHARED + [
     (INVALID, dict(x=None)), (INVALID, dict(x=PTR + 2)), (UNSUPPORTED, dict(dt=3)), (INVALID, dict(ts=-64)),
     (UNSUPPORTED, dict(ts=128, ks=2)), (UNSUPPORTED, dict(K=131072, ts=131072, ws=131072)),
-    (INVALID, dict(M=500, room=None)), (INVALID, dict(M=500, room=PTR + 16)), (SHAPE, dict(M=500, bytes=100)),
+    (INVALID, dict(WIDE, room=None)), (INVALID, dict(WIDE, room=PTR + 16)), (SHAPE, dict(WIDE, bytes=100)),
 ], ids=str)
 def test_linear_refusals(status, kw):
     assert _linear(**kw) == status
@@ -110,8 +112,8 @@ def test_linear_refusals(status, kw):
 def test_workspace_query():
     need = ctypes.c_int64()
     q = dss.lib().dss_tokens_workspace
-    assert q(400, 8, 64, 0, ctypes.byref(need)) == OK and need.value >= 400 * 64 + 400 * 4
-    assert q(1 << 33, 8, 64, 0, ctypes.byref(need)) == OK and need.value >= (1 << 33) * 68
+    assert q(500, 8, 2500, 0, ctypes.byref(need)) == OK and need.value >= 500 * 2500 + 500 * 4
+    assert q(1 << 33, 8, 2500, 0, ctypes.byref(need)) == OK and need.value >= (1 << 33) * 2504
     assert q(0, 8, 64, 0, ctypes.byref(need)) == OK
     for bad in ((-1, 8, 64), (4, 0, 64), (4, 8, 0)):
         assert q(*bad, 0, ctypes.byref(need)) == INVALID

@@ -385,5 +385,6 @@ def test_binding_refusals():
         dss.linear_i8(x, w, ws, out=torch.empty(12, 10, device="cuda")[::2, ::2])
     assert e.value.status == 3
     with pytest.raises(dss.DssError) as e:
-        dss.linear_i8(_x(500, 8), w, ws, workspace=torch.empty(10, dtype=torch.uint8, device="cuda"))
+        dss.linear_i8(_x(500, 2500), _dev(_weights(5, 2500)[0]), ws,
+                      workspace=torch.empty(10, dtype=torch.uint8, device="cuda"))
     assert e.value.status == 2
