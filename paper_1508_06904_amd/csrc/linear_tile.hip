@@ -82,7 +82,7 @@ __global__ __launch_bounds__(1024) void linear_tile_kernel(Layer L, Values V, in
     extern __shared__ __align__(16) int8_t lds[];
     const int K = L.K, pitch = tile_pitch(K);
     float* scales = reinterpret_cast<float*>(lds + tokens * pitch);
-    const int64_t m0 = (int64_t)blockIdx.x * tokens, left = L.M - m0;
+    const int64_t m0 = xcd_order(blockIdx.x, gridDim.x) * tokens, left = L.M - m0;
     if constexpr (ROWS)
         code_rows(static_cast<const T*>(V.x) + m0 * V.token_stride, V.token_stride, left, K, pitch, lds, scales);
     else

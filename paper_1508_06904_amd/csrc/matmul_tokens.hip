@@ -48,13 +48,6 @@ __device__ __attribute__((aligned(16))) const unsigned int g_zero16[4] = {0u, 0u
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-// Workgroups are handed to the 8 XCDs in turn: the id of the tile that makes the
-// tiles of one XCD (and of its L2) neighbours.
-__device__ __forceinline__ int64_t xcd_order(int64_t b, int64_t n) {
-    const int64_t x = b & 7, q = n >> 3, r = n & 7;
-    return x * q + min(x, r) + (b >> 3);
-}
-
 template <typename Tout, int BI, int BJ, int WI, int WJ, bool DMA>
 __global__ __launch_bounds__(WI* WJ * 64) void matmul_tile_kernel(Layer L, int tiles_i, int tiles_j) {
     constexpr int NW = WI * WJ, THREADS = NW * 64;

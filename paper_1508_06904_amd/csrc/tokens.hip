@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kMapWaves * 64) void quantize_map_kernel(const T* _
                                                                       int Kp, float* __restrict__ scales) {
     using Tile = MapTile<T>;
     __shared__ uint32_t tops[kMapWaves * 64];
-    const int64_t m0 = (int64_t)blockIdx.x * Tile::kTokens;
+    const int64_t m0 = xcd_order(blockIdx.x, gridDim.x) * Tile::kTokens;
     const int left = (int)min(M - m0, (int64_t)Tile::kTokens);
     const int span = (int)(blockDim.x >> 6) * 64;      // channels held at once
     Tile tile;

@@ -13,6 +13,13 @@ namespace dss {
 
 constexpr uint32_t kInfBits = 0x7f800000u;
 
+// Workgroups are handed to the 8 XCDs in turn: the id of the tile that makes the
+// tiles of one XCD (and of its L2) neighbours.
+__device__ __forceinline__ int64_t xcd_order(int64_t b, int64_t n) {
+    const int64_t x = b & 7, q = n >> 3, r = n & 7;
+    return x * q + min(x, r) + (b >> 3);
+}
+
 // 16 bytes of a row, as words: their values unpack where they are used.
 template <typename T>
 struct Chunk {
@@ -232,32 +239,66 @@ __device__ __forceinline__ float output_of(int sum, float wscale, float scale, f
     return activate_nan(act, (float)sum * wscale * scale + bias);
 }
 
-// Four adjacent outputs D[i][j .. j+3] of a layer, those from J on left out.
+// Four adjacent outputs to p, those from n on left out.
 template <typename Tout>
-__device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum) {
-    Tout* p = static_cast<Tout*>(L.out) + i * L.ldo + j;
+__device__ __forceinline__ void store_four(Tout* p, int64_t n, const float (&y)[4]) {
     struct Four {
         Tout v[4];
     } r;
-    const int n = (int)min(J - j, (int64_t)4);
-    if (L.map) {
-        const float ws = L.weight_scales[i], b = L.bias ? L.bias[i] : 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) store_elem(&r.v[k], output_of(sum[k], ws, k < n ? L.scales[j + k] : 0.f, b, L.act));
-    } else {
-        const float s = L.scales[i];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            store_elem(&r.v[k], output_of(sum[k], k < n ? L.weight_scales[j + k] : 0.f, s,
-                                          L.bias && k < n ? L.bias[j + k] : 0.f, L.act));
-    }
-    if (n == 4) {
+    for (int k = 0; k < 4; ++k) store_elem(&r.v[k], y[k]);
+    if (n >= 4) {
         __builtin_memcpy(p, &r, sizeof r);
     } else {
 #pragma unroll
         for (int k = 0; k < 3; ++k)
             if (k < n) p[k] = r.v[k];
     }
+}
+
+// The scales and biases of four adjacent outputs, and of one.
+struct Params4 {
+    float scale[4], bias[4];
+};
+__device__ __forceinline__ Params4 load_params4(const Layer& L, int64_t n) {
+    Params4 r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int64_t at = min(n + k, (int64_t)L.N - 1);
+        r.scale[k] = L.weight_scales[at];
+        r.bias[k] = L.bias ? L.bias[at] : 0.f;
+    }
+    return r;
+}
+struct Params1 {
+    float scale, bias;
+};
+__device__ __forceinline__ Params1 load_params1(const Layer& L, int64_t n) {
+    n = min(n, (int64_t)L.N - 1);
+    return {L.weight_scales[n], L.bias ? L.bias[n] : 0.f};
+}
+
+// Four adjacent outputs D[i][j .. j+3] of a layer, those from J on left out: of one token (rows) ...
+template <typename Tout>
+__device__ __forceinline__ void store_row(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum, const Params4& P) {
+    const float s = L.scales[i];
+    float y[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = output_of(sum[k], P.scale[k], s, P.bias[k], L.act);
+    store_four(static_cast<Tout*>(L.out) + i * L.ldo + j, J - j, y);
+}
+// ... or of one output channel (a map).
+template <typename Tout>
+__device__ __forceinline__ void store_map(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum, const Params1& P) {
+    float y[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = output_of(sum[k], P.scale, j + k < J ? L.scales[j + k] : 0.f, P.bias, L.act);
+    store_four(static_cast<Tout*>(L.out) + i * L.ldo + j, J - j, y);
+}
+template <typename Tout>
+__device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum) {
+    if (L.map) store_map<Tout>(L, i, j, J, sum, load_params1(L, i));
+    else store_row<Tout>(L, i, j, J, sum, load_params4(L, j));
 }
 
 // Bytes k .. k+15 of a row of K bytes, zeros past its end; nothing past the end is read.
