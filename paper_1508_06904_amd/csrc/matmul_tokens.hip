@@ -48,7 +48,7 @@ __device__ __attribute__((aligned(16))) const unsigned int g_zero16[4] = {0u, 0u
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-template <typename Tout, int BI, int BJ, int WI, int WJ, bool DMA>
+template <typename Tout, int BI, int BJ, int WI, int WJ, bool DMA, bool MAP>
 __global__ __launch_bounds__(WI* WJ * 64) void matmul_tile_kernel(Layer L, int tiles_i, int tiles_j) {
     constexpr int NW = WI * WJ, THREADS = NW * 64;
     constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
@@ -131,13 +131,19 @@ __global__ __launch_bounds__(WI* WJ * 64) void matmul_tile_kernel(Layer L, int t
         if (s + 1 < steps) put(s + 1);
         __syncthreads();
     }
+    Side1 side_p[TI];
+    Side4 side_q[TJ];
+#pragma unroll
+    for (int a = 0; a < TI; ++a) side_p[a] = side_i<MAP>(L, i0 + (wi * TI + a) * 16 + l16);
+#pragma unroll
+    for (int b = 0; b < TJ; ++b) side_q[b] = side_j<MAP>(L, j0 + (wj * TJ + b) * 16 + q16 * 4);
 #pragma unroll
     for (int a = 0; a < TI; ++a) {
         const int64_t i = i0 + (wi * TI + a) * 16 + l16;
 #pragma unroll
         for (int b = 0; b < TJ; ++b) {
             const int64_t j = j0 + (wj * TJ + b) * 16 + q16 * 4;
-            if (i < S.I && j < S.J) store_outputs<Tout>(L, i, j, S.J, acc[a][b]);
+            if (i < S.I && j < S.J) store_outputs<Tout, MAP>(L, i, j, S.J, acc[a][b], side_p[a], side_q[b]);
         }
     }
 }
@@ -146,7 +152,7 @@ template <typename Tout, int BI, int BJ, int WI, int WJ, bool DMA>
 hipError_t run_tile(const Layer& L, hipStream_t s) {
     const Sides S = sides_of(L);
     const int64_t ti = ceil_div64(S.I, BI), tj = ceil_div64(S.J, BJ);
-    const auto kern = matmul_tile_kernel<Tout, BI, BJ, WI, WJ, DMA>;
+    const auto kern = L.map ? matmul_tile_kernel<Tout, BI, BJ, WI, WJ, DMA, true> : matmul_tile_kernel<Tout, BI, BJ, WI, WJ, DMA, false>;
     constexpr size_t lds = 2 * (BI + BJ) * kStep;
     const hipError_t e = allow_dynamic_lds((const void*)kern, lds);
     if (e != hipSuccess) return e;

@@ -256,49 +256,46 @@ __device__ __forceinline__ void store_four(Tout* p, int64_t n, const float (&y)[
     }
 }
 
-// The scales and biases of four adjacent outputs, and of one.
-struct Params4 {
+// What a lane's outputs need besides their sums: D's side i (one value) and side j
+// (four adjacent ones).  Read before the first output is stored: to the compiler a
+// store may change any of it.
+struct Side1 {
+    float scale, bias;
+};
+struct Side4 {
     float scale[4], bias[4];
 };
-__device__ __forceinline__ Params4 load_params4(const Layer& L, int64_t n) {
-    Params4 r;
+template <bool MAP>
+__device__ __forceinline__ Side1 side_i(const Layer& L, int64_t i) {
+    if constexpr (MAP) {
+        i = min(i, (int64_t)L.N - 1);
+        return {L.weight_scales[i], L.bias ? L.bias[i] : 0.f};
+    } else {
+        return {L.scales[min(i, L.M - 1)], 0.f};
+    }
+}
+template <bool MAP>
+__device__ __forceinline__ Side4 side_j(const Layer& L, int64_t j) {
+    Side4 r;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const int64_t at = min(n + k, (int64_t)L.N - 1);
-        r.scale[k] = L.weight_scales[at];
-        r.bias[k] = L.bias ? L.bias[at] : 0.f;
+        const int64_t at = min(j + k, MAP ? L.M - 1 : (int64_t)L.N - 1);
+        r.scale[k] = MAP ? L.scales[at] : L.weight_scales[at];
+        r.bias[k] = !MAP && L.bias ? L.bias[at] : 0.f;
     }
     return r;
 }
-struct Params1 {
-    float scale, bias;
-};
-__device__ __forceinline__ Params1 load_params1(const Layer& L, int64_t n) {
-    n = min(n, (int64_t)L.N - 1);
-    return {L.weight_scales[n], L.bias ? L.bias[n] : 0.f};
-}
 
-// Four adjacent outputs D[i][j .. j+3] of a layer, those from J on left out: of one token (rows) ...
-template <typename Tout>
-__device__ __forceinline__ void store_row(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum, const Params4& P) {
-    const float s = L.scales[i];
+// Four adjacent outputs D[i][j .. j+3] of a layer, those from J on left out.
+template <typename Tout, bool MAP>
+__device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum, const Side1& P,
+                                              const Side4& Q) {
     float y[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = output_of(sum[k], P.scale[k], s, P.bias[k], L.act);
+    for (int k = 0; k < 4; ++k)
+        y[k] = MAP ? output_of(sum[k], P.scale, Q.scale[k], P.bias, L.act)
+                   : output_of(sum[k], Q.scale[k], P.scale, Q.bias[k], L.act);
     store_four(static_cast<Tout*>(L.out) + i * L.ldo + j, J - j, y);
-}
-// ... or of one output channel (a map).
-template <typename Tout>
-__device__ __forceinline__ void store_map(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum, const Params1& P) {
-    float y[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = output_of(sum[k], P.scale, j + k < J ? L.scales[j + k] : 0.f, P.bias, L.act);
-    store_four(static_cast<Tout*>(L.out) + i * L.ldo + j, J - j, y);
-}
-template <typename Tout>
-__device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum) {
-    if (L.map) store_map<Tout>(L, i, j, J, sum, load_params1(L, i));
-    else store_row<Tout>(L, i, j, J, sum, load_params4(L, j));
 }
 
 // Bytes k .. k+15 of a row of K bytes, zeros past its end; nothing past the end is read.
