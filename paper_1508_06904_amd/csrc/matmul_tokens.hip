@@ -33,7 +33,7 @@ __host__ __device__ __forceinline__ Sides sides_of(const Layer& L) {
 
 // ------------------------------------------------------------------ tiles
 // BI x BJ outputs for WI x WJ waves; kStep bytes of K at a time through two LDS
-// buffers, the next step's bytes on their way while this one's are multiplied.  A
+// buffers.  A
 // row of a buffer is 8 units of 16 bytes; row r keeps unit u at place u ^ (r & 7),
 // so that the 8 rows that a matrix operand's read takes at once lie in different
 // banks.
@@ -48,8 +48,13 @@ __device__ __attribute__((aligned(16))) const unsigned int g_zero16[4] = {0u, 0u
 
 typedef __attribute__((address_space(3))) void lds_void;
 
+// 16 bytes of each lane from global memory to LDS at wave_dst + 16 * lane.
+__device__ __forceinline__ void copy16(const void* src, char* wave_dst) {
+    __builtin_amdgcn_global_load_lds(src, (lds_void*)wave_dst, 16, 0, 0);
+}
+
 template <typename Tout, int BI, int BJ, int WI, int WJ, bool DMA, bool MAP>
-__global__ __launch_bounds__(WI* WJ * 64) void matmul_tile_kernel(Layer L, int tiles_i, int tiles_j) {
+__global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(1))) void matmul_tile_kernel(Layer L, int tiles_i, int tiles_j) {
     constexpr int NW = WI * WJ, THREADS = NW * 64;
     constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
     constexpr int LP = BI * kUnits / THREADS, LQ = BJ * kUnits / THREADS;   // units of each thread and step
@@ -62,7 +67,7 @@ __global__ __launch_bounds__(WI* WJ * 64) void matmul_tile_kernel(Layer L, int t
     const int64_t strip = id / ((int64_t)8 * tiles_j), in_strip = id - strip * 8 * tiles_j;
     const int rows = min(8, tiles_i - (int)strip * 8);
     const int64_t i0 = (strip * 8 + in_strip % rows) * BI, j0 = in_strip / rows * BJ;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / WJ, wj = wave % WJ;
 
     // the thread's units: rows row0 + n * (THREADS / 8), and one place in each of them
@@ -75,62 +80,77 @@ __global__ __launch_bounds__(WI* WJ * 64) void matmul_tile_kernel(Layer L, int t
 
     const int K = L.K, steps = (K + kStep - 1) / kStep;
     i32x4 acc[TI][TJ] = {};
-    i32x4 rp[DMA ? 1 : LP], rq[DMA ? 1 : LQ];
+    i32x4 held[DMA ? 1 : LP + LQ];
 
-    auto fetch = [&](int s) {
+    // Unit n of the thread's LP + LQ units of step s; past the end of K zeros.  DMA: into the step's
+    // buffer.  Otherwise into registers, from where put() takes them to the buffer.
+    const int8_t* zeros = reinterpret_cast<const int8_t*>(g_zero16);
+    auto fetch = [&](int s, int n) {
         const int k = s * kStep + unit * 16;
-        if constexpr (DMA) {
-            char* to = lds + (s & 1) * BUF + wave * 1024;
-            const bool in = k < K;
-#pragma unroll
-            for (int n = 0; n < LP; ++n)
-                __builtin_amdgcn_global_load_lds(in ? (const void*)(src_p[n] + k) : (const void*)g_zero16,
-                                                 (lds_void*)(to + n * THREADS * 16), 16, 0, 0);
-#pragma unroll
-            for (int n = 0; n < LQ; ++n)
-                __builtin_amdgcn_global_load_lds(in ? (const void*)(src_q[n] + k) : (const void*)g_zero16,
-                                                 (lds_void*)(to + BI * kStep + n * THREADS * 16), 16, 0, 0);
-        } else {
-#pragma unroll
-            for (int n = 0; n < LP; ++n) rp[n] = load_unit(src_p[n], k, K);
-#pragma unroll
-            for (int n = 0; n < LQ; ++n) rq[n] = load_unit(src_q[n], k, K);
-        }
+        const int8_t* row = n < LP ? src_p[n < LP ? n : 0] : src_q[n < LP ? 0 : n - LP];
+        if constexpr (DMA) copy16(k < K ? row + k : zeros, lds + (s & 1) * BUF + (n * NW + wave) * 1024);
+        else held[n] = load_unit(row, k, K);
     };
     auto put = [&](int s) {
         if constexpr (!DMA) {
-            char* to = lds + (s & 1) * BUF + tid * 16;
 #pragma unroll
-            for (int n = 0; n < LP; ++n) *reinterpret_cast<i32x4*>(to + n * THREADS * 16) = rp[n];
+            for (int n = 0; n < LP + LQ; ++n)
+                *reinterpret_cast<i32x4*>(lds + (s & 1) * BUF + (n * THREADS + tid) * 16) = held[n];
+        }
+    };
+    // A barrier that waits for the wave's own copies first: they count as loads, for which a barrier
+    // alone does not wait.
+    auto arrived = [&]() {
+        if constexpr (DMA) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+
+    // The matrix operands of half a step (64 of K): TJ of Q, then TI of P.
+    const int l16 = lane & 15, q16 = lane >> 4;
+    using Half = i32x4[TI + TJ];
+    auto read = [&](Half& o, int n, int s, int h) {
+        const int row = n < TJ ? BI + (wj * TJ + n) * 16 : (wi * TI + n - TJ) * 16;
+        o[n] = *reinterpret_cast<const i32x4*>(lds + (s & 1) * BUF + (row + l16) * kStep + ((h * 4 + q16) ^ (l16 & 7)) * 16);
+    };
+    // Multiplies one half's operands, reads another's (half h of step s) and fetches a step's
+    // units, an LDS read and a fetch after every few matrix instructions.  In a burst the fetches would
+    // hold up the wave, and with it its matrix instructions, until all of them are taken.
+    auto half_step = [&](Half& use, Half& next, int s, int h, bool fetches) {
+        constexpr int R = TI + TJ;
 #pragma unroll
-            for (int n = 0; n < LQ; ++n) *reinterpret_cast<i32x4*>(to + BI * kStep + n * THREADS * 16) = rq[n];
+        for (int n = 0; n < R; ++n) {
+            if (fetches)
+#pragma unroll
+                for (int f = (LP + LQ) * n / R; f < (LP + LQ) * (n + 1) / R; ++f) fetch(s + 1, f);
+            read(next, n, s, h);
+#pragma unroll
+            for (int m = TI * TJ * n / R; m < TI * TJ * (n + 1) / R; ++m)
+                acc[m / TJ][m % TJ] = __builtin_amdgcn_mfma_i32_16x16x64_i8(use[m % TJ], use[TJ + m / TJ], acc[m / TJ][m % TJ], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
-    fetch(0);
-    put(0);
-    __syncthreads();
-    const int l16 = lane & 15, q16 = lane >> 4;
-    for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) fetch(s + 1);
-        const char* bp = lds + (s & 1) * BUF + (wi * TI * 16 + l16) * kStep;
-        const char* bq = lds + (s & 1) * BUF + BI * kStep + (wj * TJ * 16 + l16) * kStep;
+    // A step's second half is read while its first is multiplied.  Then nobody needs the step's
+    // buffer any more, and the next step's bytes have had a step's time to arrive: one barrier for
+    // both, after which the buffer takes the step after the next and the next one's first half is read.
+    // (Past the last step zeros are fetched and read, and not used: no branch divides the loop.)
 #pragma unroll
-        for (int h = 0; h < kStep / 64; ++h) {
-            const int place = ((h * 4 + q16) ^ (l16 & 7)) * 16;
-            i32x4 p[TI], q[TJ];
+    for (int s = 0; s < 2; ++s) {
 #pragma unroll
-            for (int t = 0; t < TJ; ++t) q[t] = *reinterpret_cast<const i32x4*>(bq + t * 16 * kStep + place);
-#pragma unroll
-            for (int t = 0; t < TI; ++t) p[t] = *reinterpret_cast<const i32x4*>(bp + t * 16 * kStep + place);
-#pragma unroll
-            for (int a = 0; a < TI; ++a)
-#pragma unroll
-                for (int b = 0; b < TJ; ++b) acc[a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[b], p[a], acc[a][b], 0, 0, 0);
-        }
-        if (s + 1 < steps) put(s + 1);
-        __syncthreads();
+        for (int n = 0; n < LP + LQ; ++n) fetch(s, n);
+        put(s);
     }
+    arrived();
+    Half h0, h1;
+#pragma unroll
+    for (int n = 0; n < TI + TJ; ++n) read(h0, n, 0, 0);
+    for (int s = 0; s < steps; ++s) {
+        half_step(h0, h1, s, 1, false);
+        if (s > 0) put(s + 1);
+        arrived();
+        half_step(h1, h0, s + 1, 0, true);
+    }
+    arrived();                           // no copy may outlive the workgroup
     Side1 side_p[TI];
     Side4 side_q[TJ];
 #pragma unroll
@@ -168,26 +188,27 @@ struct TileChoice {
 };
 constexpr TileChoice kTiles[] = {{256, 256, 1, 1.0}, {128, 128, 2, 0.8}, {64, 64, 4, 0.4}};
 
-int pick_tile(const Sides& S) {
-    int best = 0;
+int pick_tile(const Sides& S, int first) {
+    int best = first;
     double least = 0;
-    for (int t = 0; t < 3; ++t) {
+    for (int t = first; t < 3; ++t) {
         const TileChoice& c = kTiles[t];
         const double tiles = (double)ceil_div64(S.I, c.bi) * ceil_div64(S.J, c.bj);
         const double rounds = std::ceil(tiles / (256.0 * c.resident)) * c.resident;
         const double time = rounds * c.bi * c.bj / c.rate;
-        if (t == 0 || time < least) best = t, least = time;
+        if (t == first || time < least) best = t, least = time;
     }
     return best;
 }
 
 template <typename Tout, bool DMA>
 hipError_t run_product(const Layer& L, hipStream_t s) {
-    switch (pick_tile(sides_of(L))) {
-        case 0: return run_tile<Tout, 256, 256, 2, 4, DMA>(L, s);
-        case 1: return run_tile<Tout, 128, 128, 2, 2, DMA>(L, s);
-        default: return run_tile<Tout, 64, 64, 2, 2, DMA>(L, s);
-    }
+    // (through registers the largest tile's units would not fit beside its sums)
+    const int t = pick_tile(sides_of(L), DMA ? 0 : 1);
+    if constexpr (DMA)
+        if (t == 0) return run_tile<Tout, 256, 256, 2, 4, DMA>(L, s);
+    if (t == 1) return run_tile<Tout, 128, 128, 2, 2, DMA>(L, s);
+    return run_tile<Tout, 64, 64, 2, 2, DMA>(L, s);
 }
 
 hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, hipStream_t s) {
