@@ -120,7 +120,7 @@ __global__ __launch_bounds__(1024) void linear_tile_kernel(Layer L, Values V, in
         for (; k0 < K; k0 += 64) step(k0, load_unit(w, k0 + q16 * 16, K));
         const int64_t I = MAP ? L.N : L.M, J = MAP ? L.M : L.N;
         Side1 p[4];
-        Side4 q[4];
+        SideN<4> q[4];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             p[g] = side_i<MAP>(L, MAP ? n0 + l16 : t0 + g * 16 + l16);
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(1024) void linear_tile_kernel(Layer L, Values V, in
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int64_t i = MAP ? n0 + l16 : t0 + g * 16 + l16, j = MAP ? t0 + g * 16 + q16 * 4 : n0 + q16 * 4;
-            if (i < I && j < J) store_outputs<Tout, MAP>(L, i, j, J, acc[g], p[g], q[g]);
+            if (i < I && j < J) store_outputs<Tout, MAP>(L, i, j, J, &acc[g], p[g], q[g]);
         }
     }
 }

@@ -152,7 +152,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void matmul_few_kernel(Layer L, Val
         const int n0 = tile * R, n_end = min(n0 + R, L.N);
         const int64_t i = MAP ? n0 + l16 : wave * 16 + l16, j = MAP ? wave * 16 + q16 * 4 : n0 + q16 * 4;
         const int64_t I = MAP ? n_end : L.M, J = MAP ? L.M : n_end;
-        if (i < I && j < J) store_outputs<Tout, MAP>(L, i, j, J, sum, side_i<MAP>(L, i), side_j<MAP>(L, j));
+        if (i < I && j < J) store_outputs<Tout, MAP>(L, i, j, J, &sum, side_i<MAP>(L, i), side_j<MAP>(L, j));
     }
 }
 

@@ -33,13 +33,16 @@ __host__ __device__ __forceinline__ Sides sides_of(const Layer& L) {
 
 // ------------------------------------------------------------------ tiles
 // BI x BJ outputs for WI x WJ waves; kStep bytes of K at a time through two LDS
-// buffers.  A
-// row of a buffer is 8 units of 16 bytes; row r keeps unit u at place u ^ (r & 7),
-// so that the 8 rows that a matrix operand's read takes at once lie in different
-// banks.
+// buffers.
 //
-// DMA: global memory to LDS without a stop in registers; rows have to start at
-// 16-byte units, and K ends at one.  Otherwise through registers, from any address.
+// A matrix operand is 16 rows: of P adjacent ones; of Q those that give a lane 4 TJ
+// adjacent outputs over its TJ operands, rows 4 TJ q + 4 n + r for operand n (q, r <
+// 4), so that the outputs leave in 16-byte stores and whole lines.  A row of a buffer
+// is 8 units of 16 bytes; a row that is an operand's row l keeps unit u at place
+// u ^ (l & 7): the 8 rows that the operand's read takes at once lie in different banks.
+//
+// The units go from global memory to LDS without a stop in registers; for that rows
+// start at 16-byte units, and K ends at one (what does not is copied first).
 constexpr int kStep = 128;
 constexpr int kUnits = kStep / 16;
 
@@ -53,8 +56,8 @@ __device__ __forceinline__ void copy16(const void* src, char* wave_dst) {
     __builtin_amdgcn_global_load_lds(src, (lds_void*)wave_dst, 16, 0, 0);
 }
 
-template <typename Tout, int BI, int BJ, int WI, int WJ, bool DMA, bool MAP>
-__global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(1))) void matmul_tile_kernel(Layer L, int tiles_i, int tiles_j) {
+template <typename Tout, int BI, int BJ, int WI, int WJ, bool MAP>
+__global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))) void matmul_tile_kernel(Layer L, int tiles_i, int tiles_j) {
     constexpr int NW = WI * WJ, THREADS = NW * 64;
     constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
     constexpr int LP = BI * kUnits / THREADS, LQ = BJ * kUnits / THREADS;   // units of each thread and step
@@ -68,10 +71,13 @@ __global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(1))
     const int rows = min(8, tiles_i - (int)strip * 8);
     const int64_t i0 = (strip * 8 + in_strip % rows) * BI, j0 = in_strip / rows * BJ;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, q16 = lane >> 4;
     const int wi = wave / WJ, wj = wave % WJ;
 
     // the thread's units: rows row0 + n * (THREADS / 8), and one place in each of them
-    const int row0 = tid >> 3, unit = (tid & 7) ^ (row0 & 7);
+    const int row0 = tid >> 3;
+    const int unit_p = (tid & 7) ^ (row0 & 7), unit_q = (tid & 7) ^ ((row0 & 3) | (row0 / (TJ * 4) & 1) << 2);
+    static_assert(THREADS / 8 % (TJ * 8) == 0, "the places of a thread's units differ");
     const int8_t *src_p[LP], *src_q[LQ];
 #pragma unroll
     for (int n = 0; n < LP; ++n) src_p[n] = S.P + min(i0 + row0 + n * (THREADS / 8), S.I - 1) * S.ps;
@@ -80,37 +86,28 @@ __global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(1))
 
     const int K = L.K, steps = (K + kStep - 1) / kStep;
     i32x4 acc[TI][TJ] = {};
-    i32x4 held[DMA ? 1 : LP + LQ];
 
-    // Unit n of the thread's LP + LQ units of step s; past the end of K zeros.  DMA: into the step's
-    // buffer.  Otherwise into registers, from where put() takes them to the buffer.
+    // Unit n of the thread's LP + LQ units of step s, into the step's buffer; past the end of K zeros.
     const int8_t* zeros = reinterpret_cast<const int8_t*>(g_zero16);
     auto fetch = [&](int s, int n) {
-        const int k = s * kStep + unit * 16;
+        const int k = s * kStep + (n < LP ? unit_p : unit_q) * 16;
         const int8_t* row = n < LP ? src_p[n < LP ? n : 0] : src_q[n < LP ? 0 : n - LP];
-        if constexpr (DMA) copy16(k < K ? row + k : zeros, lds + (s & 1) * BUF + (n * NW + wave) * 1024);
-        else held[n] = load_unit(row, k, K);
-    };
-    auto put = [&](int s) {
-        if constexpr (!DMA) {
-#pragma unroll
-            for (int n = 0; n < LP + LQ; ++n)
-                *reinterpret_cast<i32x4*>(lds + (s & 1) * BUF + (n * THREADS + tid) * 16) = held[n];
-        }
+        copy16(k < K ? row + k : zeros, lds + (s & 1) * BUF + (n * NW + wave) * 1024);
     };
     // A barrier that waits for the wave's own copies first: they count as loads, for which a barrier
     // alone does not wait.
     auto arrived = [&]() {
-        if constexpr (DMA) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     };
 
     // The matrix operands of half a step (64 of K): TJ of Q, then TI of P.
-    const int l16 = lane & 15, q16 = lane >> 4;
     using Half = i32x4[TI + TJ];
+    const int at_p = (wi * TI * 16 + l16) * kStep;
+    const int at_q = (BI + wj * TJ * 16 + (l16 >> 2) * TJ * 4 + (l16 & 3)) * kStep;
     auto read = [&](Half& o, int n, int s, int h) {
-        const int row = n < TJ ? BI + (wj * TJ + n) * 16 : (wi * TI + n - TJ) * 16;
-        o[n] = *reinterpret_cast<const i32x4*>(lds + (s & 1) * BUF + (row + l16) * kStep + ((h * 4 + q16) ^ (l16 & 7)) * 16);
+        const int at = n < TJ ? at_q + n * 4 * kStep : at_p + (n - TJ) * 16 * kStep;
+        o[n] = *reinterpret_cast<const i32x4*>(lds + (s & 1) * BUF + at + ((h * 4 + q16) ^ (l16 & 7)) * 16);
     };
     // Multiplies one half's operands, reads another's (half h of step s) and fetches a step's
     // units, an LDS read and a fetch after every few matrix instructions.  In a burst the fetches would
@@ -138,7 +135,6 @@ __global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(1))
     for (int s = 0; s < 2; ++s) {
 #pragma unroll
         for (int n = 0; n < LP + LQ; ++n) fetch(s, n);
-        put(s);
     }
     arrived();
     Half h0, h1;
@@ -146,33 +142,27 @@ __global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(1))
     for (int n = 0; n < TI + TJ; ++n) read(h0, n, 0, 0);
     for (int s = 0; s < steps; ++s) {
         half_step(h0, h1, s, 1, false);
-        if (s > 0) put(s + 1);
         arrived();
         half_step(h1, h0, s + 1, 0, true);
     }
     arrived();                           // no copy may outlive the workgroup
+    const int64_t j = j0 + wj * TJ * 16 + q16 * TJ * 4;
+    const auto side_q = side_j<MAP, TJ * 4>(L, j);
     Side1 side_p[TI];
-    Side4 side_q[TJ];
 #pragma unroll
     for (int a = 0; a < TI; ++a) side_p[a] = side_i<MAP>(L, i0 + (wi * TI + a) * 16 + l16);
 #pragma unroll
-    for (int b = 0; b < TJ; ++b) side_q[b] = side_j<MAP>(L, j0 + (wj * TJ + b) * 16 + q16 * 4);
-#pragma unroll
     for (int a = 0; a < TI; ++a) {
         const int64_t i = i0 + (wi * TI + a) * 16 + l16;
-#pragma unroll
-        for (int b = 0; b < TJ; ++b) {
-            const int64_t j = j0 + (wj * TJ + b) * 16 + q16 * 4;
-            if (i < S.I && j < S.J) store_outputs<Tout, MAP>(L, i, j, S.J, acc[a][b], side_p[a], side_q[b]);
-        }
+        if (i < S.I && j < S.J) store_outputs<Tout, MAP>(L, i, j, S.J, acc[a], side_p[a], side_q);
     }
 }
 
-template <typename Tout, int BI, int BJ, int WI, int WJ, bool DMA>
+template <typename Tout, int BI, int BJ, int WI, int WJ>
 hipError_t run_tile(const Layer& L, hipStream_t s) {
     const Sides S = sides_of(L);
     const int64_t ti = ceil_div64(S.I, BI), tj = ceil_div64(S.J, BJ);
-    const auto kern = L.map ? matmul_tile_kernel<Tout, BI, BJ, WI, WJ, DMA, true> : matmul_tile_kernel<Tout, BI, BJ, WI, WJ, DMA, false>;
+    const auto kern = L.map ? matmul_tile_kernel<Tout, BI, BJ, WI, WJ, true> : matmul_tile_kernel<Tout, BI, BJ, WI, WJ, false>;
     constexpr size_t lds = 2 * (BI + BJ) * kStep;
     const hipError_t e = allow_dynamic_lds((const void*)kern, lds);
     if (e != hipSuccess) return e;
@@ -180,54 +170,103 @@ hipError_t run_tile(const Layer& L, hipStream_t s) {
     return hipGetLastError();
 }
 
-// The tile: the one whose launch keeps the GPU's 256 units busy with the least time
-// lost to part-filled rounds; wider tiles read less of P and Q for an output.
-struct TileChoice {
-    int bi, bj, resident;                // outputs of a tile, workgroups of a unit at once
-    double rate;                         // of the 256 x 256 tile's, with all units busy
+// The tile whose launch should take the least time.  A unit (of 256) with q tiles of
+// one kind at once, `most` of them at the most, takes first + (q - 1) * more
+// microseconds for a step of K, and `ends` for the tiles' beginnings and outputs; measured.
+struct TileTime {
+    int b, most;
+    double first, more, ends;
 };
-constexpr TileChoice kTiles[] = {{256, 256, 1, 1.0}, {128, 128, 2, 0.8}, {64, 64, 4, 0.4}};
+constexpr TileTime kTiles[] = {{256, 1, 1.95, 0, 6.0}, {128, 2, 0.60, 0.80, 4.0}, {64, 4, 0.45, 0.22, 2.5}};
 
-int pick_tile(const Sides& S, int first) {
-    int best = first;
+int pick_tile(const Sides& S, int K) {
+    const int steps = (K + kStep - 1) / kStep;
+    int best = 0;
     double least = 0;
-    for (int t = first; t < 3; ++t) {
-        const TileChoice& c = kTiles[t];
-        const double tiles = (double)ceil_div64(S.I, c.bi) * ceil_div64(S.J, c.bj);
-        const double rounds = std::ceil(tiles / (256.0 * c.resident)) * c.resident;
-        const double time = rounds * c.bi * c.bj / c.rate;
-        if (t == first || time < least) best = t, least = time;
+    for (int t = 0; t < 3; ++t) {
+        const TileTime& c = kTiles[t];
+        const int64_t tiles = ceil_div64(S.I, c.b) * ceil_div64(S.J, c.b), full = tiles / (256 * c.most);
+        const int64_t left = ceil_div64(tiles - full * 256 * c.most, 256);
+        double time = full * (steps * (c.first + (c.most - 1) * c.more) + c.ends);
+        if (left) time += steps * (c.first + (left - 1) * c.more) + c.ends;
+        if (t == 0 || time < least) best = t, least = time;
     }
     return best;
 }
 
-template <typename Tout, bool DMA>
+template <typename Tout>
 hipError_t run_product(const Layer& L, hipStream_t s) {
-    // (through registers the largest tile's units would not fit beside its sums)
-    const int t = pick_tile(sides_of(L), DMA ? 0 : 1);
-    if constexpr (DMA)
-        if (t == 0) return run_tile<Tout, 256, 256, 2, 4, DMA>(L, s);
-    if (t == 1) return run_tile<Tout, 128, 128, 2, 2, DMA>(L, s);
-    return run_tile<Tout, 64, 64, 2, 2, DMA>(L, s);
+    const int t = pick_tile(sides_of(L), L.K);
+    if (t == 0) return run_tile<Tout, 256, 256, 2, 4>(L, s);
+    if (t == 1) return run_tile<Tout, 128, 128, 2, 2>(L, s);
+    return run_tile<Tout, 64, 64, 2, 2>(L, s);
 }
 
-hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, hipStream_t s) {
+// ------------------------------------------------------------------ operands at other addresses
+// Rows that do not start, or whose K does not end, at 16-byte units, copied with
+// zeros up to the next one; a thread for each unit.  Of two operands at once.
+struct Rows {
+    const int8_t* from;
+    int64_t stride, rows;
+    int8_t* to;
+};
+
+__global__ __launch_bounds__(256) void copy_rows_kernel(Rows A, Rows B, int K, int units) {
+    int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    Rows R = A;
+    if (u >= A.rows * units) {
+        u -= A.rows * units;
+        R = B;
+    }
+    const int64_t row = u / units;
+    const int k = (int)(u - row * units) * 16;
+    if (row < R.rows) *reinterpret_cast<i32x4*>(R.to + u * 16) = load_unit(R.from + row * R.stride, k, K);
+}
+
+bool whole_units(const int8_t* p, int64_t stride, int64_t rows, int K) {
+    return K % 16 == 0 && (uintptr_t)p % 16 == 0 && (stride % 16 == 0 || rows == 1);
+}
+
+// The codes' row length in a workspace: whole 16-byte units.
+int padded_k(int K) { return (K + 15) / 16 * 16; }
+
+int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
+
+// Tokens whose codes a workspace has room for a copy of: as many as 64 MB hold.
+int64_t copied_tokens(int64_t M, int K) {
+    return std::min(M, std::max<int64_t>(256, ((int64_t)1 << 26) / padded_k(K) / 256 * 256));
+}
+
+// The layer on codes; `room` has the weights' copy and the tokens' (unless these are padded already).
+hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, bool padded, char* room, hipStream_t s) {
     if (L.M <= kFewTokens) return launch_matmul_few(L, out_dtype, s);
-    auto whole = [](const int8_t* p, int64_t stride, int64_t rows) {
-        return (uintptr_t)p % 16 == 0 && (stride % 16 == 0 || rows == 1);
-    };
-    const bool dma = L.K % 16 == 0 && whole(L.codes, L.codes_stride, L.M) && whole(L.weight, L.weight_stride, L.N);
+    const int Kp = padded_k(L.K);
+    Rows W = {L.weight, L.weight_stride, L.N, reinterpret_cast<int8_t*>(room)};
+    int8_t* copies = W.to + align256((int64_t)L.N * Kp);
+    const bool copy_w = !whole_units(L.weight, L.weight_stride, L.N, L.K);
+    const bool copy_c = !padded && !whole_units(L.codes, L.codes_stride, L.M, L.K);
     // a launch has fewer than 2^32 threads
-    const int64_t slab = std::max<int64_t>(256, (((int64_t)1 << 34) / L.N) / 256 * 256);
+    int64_t slab = std::max<int64_t>(256, (((int64_t)1 << 34) / L.N) / 256 * 256);
+    if (copy_c) slab = std::min(slab, copied_tokens(L.M, L.K));
     for (int64_t m = 0; m < L.M; m += slab) {
         Layer S = L;
         S.M = std::min(L.M - m, slab);
         S.codes += m * L.codes_stride;
         S.scales += m;
         S.out = static_cast<char*>(L.out) + m * (L.map ? 1 : L.ldo) * (int64_t)dtype_size(out_dtype);
-        hipError_t e;
-        if (out_dtype == DSS_BF16) e = dma ? run_product<uint16_t, true>(S, s) : run_product<uint16_t, false>(S, s);
-        else e = dma ? run_product<float, true>(S, s) : run_product<float, false>(S, s);
+        Rows C = {S.codes, L.codes_stride, copy_c ? S.M : 0, copies};
+        Rows w = W;
+        if (!copy_w || m > 0) w.rows = 0;
+        const int64_t units = (C.rows + w.rows) * (Kp / 16);
+        if (units) {
+            copy_rows_kernel<<<dim3((unsigned)ceil_div64(units, 256)), 256, 0, s>>>(C, w, L.K, Kp / 16);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        if (copy_c) S.codes = copies, S.codes_stride = Kp;
+        if (copy_w) S.weight = W.to, S.weight_stride = Kp;
+        S.K = Kp;
+        const hipError_t e = out_dtype == DSS_BF16 ? run_product<uint16_t>(S, s) : run_product<float>(S, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -235,11 +274,6 @@ hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, hipStream_t s) {
 
 constexpr int kMaxK = 131071;
 constexpr int kMaxN = 1 << 20;
-
-int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
-
-// The codes' row length in a workspace: whole 16-byte units.
-int padded_k(int K) { return (K + 15) / 16 * 16; }
 
 // Checks of what dss_matmul_tokens and dss_linear_tokens share.
 dss_status check_layer(int64_t M, const int8_t* weight, int64_t weight_stride, const float* weight_scales, int32_t N,
@@ -266,8 +300,13 @@ dss_status check_layer(int64_t M, const int8_t* weight, int64_t weight_stride, c
     return DSS_OK;
 }
 
+// The copies of weights and codes (whatever their addresses turn out to be), or the
+// weights' copy and the tokens' codes and scales.
 int64_t workspace_bytes_of(int64_t M, int32_t N, int32_t K, bool from_codes) {
-    return from_codes || codes_itself(M, K) || linear_in_tiles(M, N, K) ? 0 : align256(M * 4) + align256(M * padded_k(K));
+    const int64_t Kp = padded_k(K), weights = M > kFewTokens ? align256(N * Kp) : 0;
+    if (from_codes) return M > kFewTokens ? weights + align256(copied_tokens(M, K) * Kp) : 0;
+    if (codes_itself(M, K) || linear_in_tiles(M, N, K)) return 0;
+    return weights + align256(M * Kp) + align256(M * 4);
 }
 
 dss_status check_room(int64_t need, const void* workspace, int64_t workspace_bytes) {
@@ -319,7 +358,7 @@ extern "C" dss_status dss_matmul_tokens(const int8_t* codes, int64_t codes_strid
     const bool map = is_map(M, N, out_token_stride, out_channel_stride);
     const Layer L = {codes, codes_stride, scales, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out,
                      map ? out_channel_stride : out_token_stride, map};
-    hipError_t e = launch_matmul(L, out_dtype, stream);
+    hipError_t e = launch_matmul(L, out_dtype, false, static_cast<char*>(workspace), stream);
     return e == hipSuccess ? DSS_OK : hip_fail(e, "token product launch");
 } catch (...) {
     return DSS_E_NOMEM;
@@ -349,13 +388,14 @@ extern "C" dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t 
                                           : launch_linear_tiles(L, V, out_dtype, stream);
         return e == hipSuccess ? DSS_OK : hip_fail(e, "token product launch");
     }
-    float* scales = static_cast<float*>(workspace);
-    int8_t* codes = static_cast<int8_t*>(workspace) + align256(M * 4);
     const int Kp = padded_k(K);
+    char* room = static_cast<char*>(workspace);
+    int8_t* codes = reinterpret_cast<int8_t*>(room) + (M > kFewTokens ? align256((int64_t)N * Kp) : 0);
+    float* scales = reinterpret_cast<float*>(codes + align256(M * Kp));
     hipError_t e = launch_quantize_tokens(dtype, x, M, K, token_stride, channel_stride, codes, Kp, Kp, scales, stream);
     if (e != hipSuccess) return hip_fail(e, "quantize launch");
     const Layer L = {codes, Kp, scales, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out, ldo, map};
-    e = launch_matmul(L, out_dtype, stream);
+    e = launch_matmul(L, out_dtype, true, room, stream);
     return e == hipSuccess ? DSS_OK : hip_fail(e, "token product launch");
 } catch (...) {
     return DSS_E_NOMEM;

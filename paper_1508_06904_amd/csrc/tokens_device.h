@@ -239,31 +239,15 @@ __device__ __forceinline__ float output_of(int sum, float wscale, float scale, f
     return activate_nan(act, (float)sum * wscale * scale + bias);
 }
 
-// Four adjacent outputs to p, those from n on left out.
-template <typename Tout>
-__device__ __forceinline__ void store_four(Tout* p, int64_t n, const float (&y)[4]) {
-    struct Four {
-        Tout v[4];
-    } r;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) store_elem(&r.v[k], y[k]);
-    if (n >= 4) {
-        __builtin_memcpy(p, &r, sizeof r);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 3; ++k)
-            if (k < n) p[k] = r.v[k];
-    }
-}
-
 // What a lane's outputs need besides their sums: D's side i (one value) and side j
-// (four adjacent ones).  Read before the first output is stored: to the compiler a
+// (N adjacent ones).  Read before the first output is stored: to the compiler a
 // store may change any of it.
 struct Side1 {
     float scale, bias;
 };
-struct Side4 {
-    float scale[4], bias[4];
+template <int N>
+struct SideN {
+    float scale[N], bias[N];
 };
 template <bool MAP>
 __device__ __forceinline__ Side1 side_i(const Layer& L, int64_t i) {
@@ -274,11 +258,11 @@ __device__ __forceinline__ Side1 side_i(const Layer& L, int64_t i) {
         return {L.scales[min(i, L.M - 1)], 0.f};
     }
 }
-template <bool MAP>
-__device__ __forceinline__ Side4 side_j(const Layer& L, int64_t j) {
-    Side4 r;
+template <bool MAP, int N = 4>
+__device__ __forceinline__ SideN<N> side_j(const Layer& L, int64_t j) {
+    SideN<N> r;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N; ++k) {
         const int64_t at = min(j + k, MAP ? L.M - 1 : (int64_t)L.N - 1);
         r.scale[k] = MAP ? L.scales[at] : L.weight_scales[at];
         r.bias[k] = !MAP && L.bias ? L.bias[at] : 0.f;
@@ -286,16 +270,31 @@ __device__ __forceinline__ Side4 side_j(const Layer& L, int64_t j) {
     return r;
 }
 
-// Four adjacent outputs D[i][j .. j+3] of a layer, those from J on left out.
-template <typename Tout, bool MAP>
-__device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t j, int64_t J, i32x4 sum, const Side1& P,
-                                              const Side4& Q) {
-    float y[4];
+// N adjacent outputs D[i][j .. j+N-1] of a layer, those from J on left out; sum[N / 4].
+template <typename Tout, bool MAP, int N>
+__device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t j, int64_t J, const i32x4* sum,
+                                              const Side1& P, const SideN<N>& Q) {
+    constexpr int C = N * (int)sizeof(Tout) < 16 ? N : 16 / (int)sizeof(Tout);   // outputs of one store
+    Tout* p = static_cast<Tout*>(L.out) + i * L.ldo + j;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        y[k] = MAP ? output_of(sum[k], P.scale, Q.scale[k], P.bias, L.act)
-                   : output_of(sum[k], Q.scale[k], P.scale, Q.bias[k], L.act);
-    store_four(static_cast<Tout*>(L.out) + i * L.ldo + j, J - j, y);
+    for (int c = 0; c < N; c += C) {
+        struct {
+            Tout v[C];
+        } r;
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            const int s = sum[(c + k) / 4][(c + k) % 4];
+            store_elem(&r.v[k], MAP ? output_of(s, P.scale, Q.scale[c + k], P.bias, L.act)
+                                    : output_of(s, Q.scale[c + k], P.scale, Q.bias[c + k], L.act));
+        }
+        if (j + c + C <= J) {
+            __builtin_memcpy(p + c, &r, sizeof r);
+        } else {
+#pragma unroll
+            for (int k = 0; k < C - 1; ++k)
+                if (j + c + k < J) p[c + k] = r.v[k];
+        }
+    }
 }
 
 // Bytes k .. k+15 of a row of K bytes, zeros past its end; nothing past the end is read.
