@@ -159,7 +159,7 @@ hipError_t run_layouts(const Layer& L, const Values& V, hipStream_t s) {
 
 }  // namespace
 
-bool linear_in_tiles(int64_t M, int N, int K) { return M > kFewTokens && K <= kMaxChannels && N <= 256; }
+bool linear_in_tiles(int64_t M, int N, int K) { return !few_tokens(M, N) && K <= kMaxChannels && N <= 256; }
 
 hipError_t launch_linear_tiles(const Layer& L, const Values& V, dss_dtype out_dtype, hipStream_t s) {
     for (int64_t m = 0; m < L.M; m += kSlabTokens) {

@@ -171,13 +171,17 @@ hipError_t run_few(const Layer& L, const Values& V, hipStream_t s) {
 template <typename Code, typename Tout>
 hipError_t run_groups(const Layer& L, const Values& V, hipStream_t s) {
     if constexpr (sizeof(Code) == 1) {
-        if (L.M > 32) return run_few<Code, Tout, 4>(L, V, s);
         if (L.M > 16) return run_few<Code, Tout, 2>(L, V, s);
     }
     return run_few<Code, Tout, 1>(L, V, s);
 }
 
 }  // namespace
+
+// Up to 16 tokens, and up to 32 while the outputs are few: there the tiles' workgroups
+// are too few or wait longer (32 tokens through 9216 x 512: 11.9 us here and 20.9 on
+// tiles, through 4096 x 16384: 26.3 and 19.4).
+bool few_tokens(int64_t M, int N) { return M <= 16 || (M <= 32 && N <= 8192); }
 
 hipError_t launch_matmul_few(const Layer& L, dss_dtype out_dtype, hipStream_t s) {
     return out_dtype == DSS_BF16 ? run_groups<int8_t, uint16_t>(L, Values{}, s) : run_groups<int8_t, float>(L, Values{}, s);

@@ -33,7 +33,8 @@ __host__ __device__ __forceinline__ Sides sides_of(const Layer& L) {
 
 // ------------------------------------------------------------------ tiles
 // BI x BJ outputs for WI x WJ waves; kStep bytes of K at a time through two LDS
-// buffers.
+// buffers.  With KG > 1 so many groups of waves take the steps in turn, each with buffers
+// of its own: where tiles are fewer than units, a unit has more steps under way.
 //
 // A matrix operand is 16 rows: of P adjacent ones; of Q those that give a lane 4 TJ
 // adjacent outputs over its TJ operands, rows 4 TJ q + 4 n + r for operand n (q, r <
@@ -56,8 +57,8 @@ __device__ __forceinline__ void copy16(const void* src, char* wave_dst) {
     __builtin_amdgcn_global_load_lds(src, (lds_void*)wave_dst, 16, 0, 0);
 }
 
-template <typename Tout, int BI, int BJ, int WI, int WJ, bool MAP>
-__global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))) void matmul_tile_kernel(Layer L, int tiles_i, int tiles_j) {
+template <typename Tout, int BI, int BJ, int WI, int WJ, int KG, bool MAP>
+__global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))) void matmul_tile_kernel(Layer L, int tiles_i, int tiles_j) {
     constexpr int NW = WI * WJ, THREADS = NW * 64;
     constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
     constexpr int LP = BI * kUnits / THREADS, LQ = BJ * kUnits / THREADS;   // units of each thread and step
@@ -70,8 +71,10 @@ __global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))
     const int64_t strip = id / ((int64_t)8 * tiles_j), in_strip = id - strip * 8 * tiles_j;
     const int rows = min(8, tiles_i - (int)strip * 8);
     const int64_t i0 = (strip * 8 + in_strip % rows) * BI, j0 = in_strip / rows * BJ;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS), tid = threadIdx.x - group * THREADS;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, q16 = lane >> 4;
+    char* const buffers = lds + group * 2 * BUF;
     const int wi = wave / WJ, wj = wave % WJ;
 
     // the thread's units: rows row0 + n * (THREADS / 8), and one place in each of them
@@ -84,15 +87,15 @@ __global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
     for (int n = 0; n < LQ; ++n) src_q[n] = S.Q + min(j0 + row0 + n * (THREADS / 8), S.J - 1) * S.qs;
 
-    const int K = L.K, steps = (K + kStep - 1) / kStep;
+    const int K = L.K, steps = (K + KG * kStep - 1) / (KG * kStep);
     i32x4 acc[TI][TJ] = {};
 
     // Unit n of the thread's LP + LQ units of step s, into the step's buffer; past the end of K zeros.
     const int8_t* zeros = reinterpret_cast<const int8_t*>(g_zero16);
     auto fetch = [&](int s, int n) {
-        const int k = s * kStep + (n < LP ? unit_p : unit_q) * 16;
+        const int k = (s * KG + group) * kStep + (n < LP ? unit_p : unit_q) * 16;
         const int8_t* row = n < LP ? src_p[n < LP ? n : 0] : src_q[n < LP ? 0 : n - LP];
-        copy16(k < K ? row + k : zeros, lds + (s & 1) * BUF + (n * NW + wave) * 1024);
+        copy16(k < K ? row + k : zeros, buffers + (s & 1) * BUF + (n * NW + wave) * 1024);
     };
     // A barrier that waits for the wave's own copies first: they count as loads, for which a barrier
     // alone does not wait.
@@ -107,7 +110,7 @@ __global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))
     const int at_q = (BI + wj * TJ * 16 + (l16 >> 2) * TJ * 4 + (l16 & 3)) * kStep;
     auto read = [&](Half& o, int n, int s, int h) {
         const int at = n < TJ ? at_q + n * 4 * kStep : at_p + (n - TJ) * 16 * kStep;
-        o[n] = *reinterpret_cast<const i32x4*>(lds + (s & 1) * BUF + at + ((h * 4 + q16) ^ (l16 & 7)) * 16);
+        o[n] = *reinterpret_cast<const i32x4*>(buffers + (s & 1) * BUF + at + ((h * 4 + q16) ^ (l16 & 7)) * 16);
     };
     // Multiplies one half's operands, reads another's (half h of step s) and fetches a step's
     // units, an LDS read and a fetch after every few matrix instructions.  In a burst the fetches would
@@ -146,6 +149,19 @@ __global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))
         half_step(h1, h0, s + 1, 0, true);
     }
     arrived();                           // no copy may outlive the workgroup
+    if constexpr (KG > 1) {
+        // the groups' sums meet in the buffers
+        i32x4* sums = reinterpret_cast<i32x4*>(lds) + tid;
+#pragma unroll
+        for (int n = 0; n < TI * TJ; ++n)
+            if (group > 0) sums[((group - 1) * TI * TJ + n) * THREADS] = acc[n / TJ][n % TJ];
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int g = 0; g < KG - 1; ++g)
+#pragma unroll
+            for (int n = 0; n < TI * TJ; ++n) acc[n / TJ][n % TJ] += sums[(g * TI * TJ + n) * THREADS];
+    }
     const int64_t j = j0 + wj * TJ * 16 + q16 * TJ * 4;
     const auto side_q = side_j<MAP, TJ * 4>(L, j);
     Side1 side_p[TI];
@@ -158,33 +174,36 @@ __global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))
     }
 }
 
-template <typename Tout, int BI, int BJ, int WI, int WJ>
+template <typename Tout, int BI, int BJ, int WI, int WJ, int KG>
 hipError_t run_tile(const Layer& L, hipStream_t s) {
     const Sides S = sides_of(L);
     const int64_t ti = ceil_div64(S.I, BI), tj = ceil_div64(S.J, BJ);
-    const auto kern = L.map ? matmul_tile_kernel<Tout, BI, BJ, WI, WJ, true> : matmul_tile_kernel<Tout, BI, BJ, WI, WJ, false>;
-    constexpr size_t lds = 2 * (BI + BJ) * kStep;
+    const auto kern = L.map ? matmul_tile_kernel<Tout, BI, BJ, WI, WJ, KG, true>
+                            : matmul_tile_kernel<Tout, BI, BJ, WI, WJ, KG, false>;
+    constexpr size_t lds = KG * 2 * (BI + BJ) * kStep;
     const hipError_t e = allow_dynamic_lds((const void*)kern, lds);
     if (e != hipSuccess) return e;
-    kern<<<dim3((unsigned)(ti * tj)), WI * WJ * 64, lds, s>>>(L, (int)ti, (int)tj);
+    kern<<<dim3((unsigned)(ti * tj)), KG * WI * WJ * 64, lds, s>>>(L, (int)ti, (int)tj);
     return hipGetLastError();
 }
 
 // The tile whose launch should take the least time.  A unit (of 256) with q tiles of
 // one kind at once, `most` of them at the most, takes first + (q - 1) * more
-// microseconds for a step of K, and `ends` for the tiles' beginnings and outputs; measured.
+// microseconds for the steps that its groups take at once, and `ends` for the tiles'
+// beginnings and outputs; measured.
 struct TileTime {
-    int b, most;
+    int b, groups, most;
     double first, more, ends;
 };
-constexpr TileTime kTiles[] = {{256, 1, 1.95, 0, 6.0}, {128, 2, 0.60, 0.80, 4.0}, {64, 4, 0.45, 0.22, 2.5}};
+constexpr TileTime kTiles[] = {{256, 1, 1, 1.95, 0, 6.0}, {128, 1, 2, 0.95, 0.20, 4.0}, {64, 1, 4, 0.40, 0.17, 2.5},
+                               {64, 4, 1, 1.05, 0, 3.0}};
 
 int pick_tile(const Sides& S, int K) {
-    const int steps = (K + kStep - 1) / kStep;
     int best = 0;
     double least = 0;
-    for (int t = 0; t < 3; ++t) {
+    for (int t = 0; t < 4; ++t) {
         const TileTime& c = kTiles[t];
+        const int steps = (K + c.groups * kStep - 1) / (c.groups * kStep);
         const int64_t tiles = ceil_div64(S.I, c.b) * ceil_div64(S.J, c.b), full = tiles / (256 * c.most);
         const int64_t left = ceil_div64(tiles - full * 256 * c.most, 256);
         double time = full * (steps * (c.first + (c.most - 1) * c.more) + c.ends);
@@ -197,9 +216,10 @@ int pick_tile(const Sides& S, int K) {
 template <typename Tout>
 hipError_t run_product(const Layer& L, hipStream_t s) {
     const int t = pick_tile(sides_of(L), L.K);
-    if (t == 0) return run_tile<Tout, 256, 256, 2, 4>(L, s);
-    if (t == 1) return run_tile<Tout, 128, 128, 2, 2>(L, s);
-    return run_tile<Tout, 64, 64, 2, 2>(L, s);
+    if (t == 0) return run_tile<Tout, 256, 256, 2, 4, 1>(L, s);
+    if (t == 1) return run_tile<Tout, 128, 128, 2, 2, 1>(L, s);
+    if (t == 2) return run_tile<Tout, 64, 64, 2, 2, 1>(L, s);
+    return run_tile<Tout, 64, 64, 2, 2, 4>(L, s);
 }
 
 // ------------------------------------------------------------------ operands at other addresses
@@ -239,7 +259,7 @@ int64_t copied_tokens(int64_t M, int K) {
 
 // The layer on codes; `room` has the weights' copy and the tokens' (unless these are padded already).
 hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, bool padded, char* room, hipStream_t s) {
-    if (L.M <= kFewTokens) return launch_matmul_few(L, out_dtype, s);
+    if (few_tokens(L.M, L.N)) return launch_matmul_few(L, out_dtype, s);
     const int Kp = padded_k(L.K);
     Rows W = {L.weight, L.weight_stride, L.N, reinterpret_cast<int8_t*>(room)};
     int8_t* copies = W.to + align256((int64_t)L.N * Kp);
@@ -303,8 +323,8 @@ dss_status check_layer(int64_t M, const int8_t* weight, int64_t weight_stride, c
 // The copies of weights and codes (whatever their addresses turn out to be), or the
 // weights' copy and the tokens' codes and scales.
 int64_t workspace_bytes_of(int64_t M, int32_t N, int32_t K, bool from_codes) {
-    const int64_t Kp = padded_k(K), weights = M > kFewTokens ? align256(N * Kp) : 0;
-    if (from_codes) return M > kFewTokens ? weights + align256(copied_tokens(M, K) * Kp) : 0;
+    const int64_t Kp = padded_k(K), weights = few_tokens(M, N) ? 0 : align256(N * Kp);
+    if (from_codes) return few_tokens(M, N) ? 0 : weights + align256(copied_tokens(M, K) * Kp);
     if (codes_itself(M, K) || linear_in_tiles(M, N, K)) return 0;
     return weights + align256(M * Kp) + align256(M * 4);
 }
@@ -390,7 +410,7 @@ extern "C" dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t 
     }
     const int Kp = padded_k(K);
     char* room = static_cast<char*>(workspace);
-    int8_t* codes = reinterpret_cast<int8_t*>(room) + (M > kFewTokens ? align256((int64_t)N * Kp) : 0);
+    int8_t* codes = reinterpret_cast<int8_t*>(room) + (few_tokens(M, N) ? 0 : align256((int64_t)N * Kp));
     float* scales = reinterpret_cast<float*>(codes + align256(M * Kp));
     hipError_t e = launch_quantize_tokens(dtype, x, M, K, token_stride, channel_stride, codes, Kp, Kp, scales, stream);
     if (e != hipSuccess) return hip_fail(e, "quantize launch");
