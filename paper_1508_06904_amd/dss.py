@@ -571,30 +571,35 @@ def _is_dense(t):
 
 def _tensor_list(tensors, what, dev):
     """The C list of CUDA tensors (dss_tensor[n]: address, count, dtype and a zero, as three 64-bit
-    words each) and the tensors as a list."""
+    words each), the tensors as a list, and whether all of them are contiguous."""
     import torch
-    if isinstance(tensors, torch.Tensor):
+    T = torch.Tensor
+    if isinstance(tensors, T):
         raise ValueError("%s must be a list of tensors" % what)
-    codes, tensors, words = _dtype_codes(), list(tensors), []
-    for t in tensors:
-        if not isinstance(t, torch.Tensor):
-            raise ValueError("%s must be a list of tensors" % what)
-        code = codes.get(t.dtype)
-        if code is None:
-            raise ValueError("%s must be float32 or bfloat16 (got %s)" % (what, t.dtype))
-        if t.get_device() != dev:
-            raise ValueError("%s must be on the current CUDA device (got %s)" % (what, t.device))
-        if not (t.is_contiguous() or _is_dense(t)):
-            raise ValueError("%s must be dense in memory, without gaps or repeated elements" % what)
-        words += (t.data_ptr(), t.numel(), code)
-    return array.array("q", words), tensors
+    codes, tensors = _dtype_codes(), list(tensors)
+    n = len(tensors)
+    if not all([isinstance(t, T) for t in tensors]):
+        raise ValueError("%s must be a list of tensors" % what)
+    if n and any(d != dev for d in set(map(T.get_device, tensors))):
+        raise ValueError("%s must be on the current CUDA device, %d" % (what, dev))
+    dtypes = [codes.get(t.dtype, -1) for t in tensors]
+    if -1 in dtypes:
+        raise ValueError("%s must be float32 or bfloat16 (got %s)" % (what, tensors[dtypes.index(-1)].dtype))
+    plain = all(map(T.is_contiguous, tensors))
+    if not plain and not all([t.is_contiguous() or _is_dense(t) for t in tensors]):
+        raise ValueError("%s must be dense in memory, without gaps or repeated elements" % what)
+    words = array.array("q", bytes(24 * n))
+    words[0::3] = array.array("q", map(T.data_ptr, tensors))
+    words[1::3] = array.array("q", map(T.numel, tensors))
+    words[2::3] = array.array("q", dtypes)
+    return words, tensors, plain
 
 
 def grad_norm(grads, norm=None, workspace=None, stream=None):
     """The norm of a gradient over a list of CUDA tensors (float32 and bfloat16, dense in
     memory, any sizes): sqrt of the sum of all squares, as a float32 tensor of no axes."""
     dev, handle = _launch(stream)
-    a, grads = _tensor_list(grads, "grads", dev)
+    a, grads, _ = _tensor_list(grads, "grads", dev)
     norm, wp, wb, keep = _norm_buffers(norm, workspace, dev, stream)
     _check(lib().dss_grad_norm(a.buffer_info()[0], len(grads), norm.data_ptr(), wp, wb, handle), "dss_grad_norm")
     return norm
@@ -607,7 +612,7 @@ def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None
     import torch
     dev, handle = _launch(stream)
     in_place = out is grads
-    a, grads = _tensor_list(grads, "grads", dev)
+    a, grads, plain = _tensor_list(grads, "grads", dev)
     if in_place:
         b, out = a, grads
     else:
@@ -617,11 +622,9 @@ def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None
             else:
                 with torch.cuda.stream(stream):
                     out = [torch.empty_like(g) for g in grads]
-        b, out = _tensor_list(out, "out", dev)
-        # counts and types at once; shapes and strides one by one
-        if b[1::3] != a[1::3] or b[2::3] != a[2::3] or not all([o.shape == g.shape for o, g in zip(out, grads)]) or \
-                not all([o.stride() == g.stride() for o, g in zip(out, grads) if not g.is_contiguous()
-                         or not o.is_contiguous()]):
+        b, out, plain_out = _tensor_list(out, "out", dev)
+        if b[1::3] != a[1::3] or b[2::3] != a[2::3] or [o.shape for o in out] != [g.shape for g in grads] or \
+                not (plain and plain_out) and [o.stride() for o in out] != [g.stride() for g in grads]:
             raise ValueError("out must be of grads' shapes, strides and types")
     norm, wp, wb, keep = _norm_buffers(norm, workspace, dev, stream)
     ptrs = b[0::3]
