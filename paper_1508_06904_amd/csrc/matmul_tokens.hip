@@ -376,8 +376,9 @@ extern "C" dss_status dss_matmul_tokens(const int8_t* codes, int64_t codes_strid
     s = check_room(workspace_bytes_of(M, N, K, true), workspace, workspace_bytes);
     if (s != DSS_OK) return s;
     const bool map = is_map(M, N, out_token_stride, out_channel_stride);
-    const Layer L = {codes, codes_stride, scales, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out,
-                     map ? out_channel_stride : out_token_stride, map};
+    const int64_t ldo = map ? out_channel_stride : out_token_stride;
+    const Layer L = {codes, codes_stride, scales, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out, ldo,
+                     map, outputs_past(M, N, ldo, out, out_dtype)};
     hipError_t e = launch_matmul(L, out_dtype, false, static_cast<char*>(workspace), stream);
     return e == hipSuccess ? DSS_OK : hip_fail(e, "token product launch");
 } catch (...) {
@@ -401,8 +402,9 @@ extern "C" dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t 
     if (s != DSS_OK) return s;
     const bool map = is_map(M, N, out_token_stride, out_channel_stride);
     const int64_t ldo = map ? out_channel_stride : out_token_stride;
+    Layer L = {nullptr, 0, nullptr, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out, ldo, map,
+               outputs_past(M, N, ldo, out, out_dtype)};
     if (codes_itself(M, K) || linear_in_tiles(M, N, K)) {
-        const Layer L = {nullptr, 0, nullptr, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out, ldo, map};
         const Values V = {x, dtype, token_stride, channel_stride};
         hipError_t e = codes_itself(M, K) ? launch_linear_few(L, V, out_dtype, stream)
                                           : launch_linear_tiles(L, V, out_dtype, stream);
@@ -414,7 +416,9 @@ extern "C" dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t 
     float* scales = reinterpret_cast<float*>(codes + align256(M * Kp));
     hipError_t e = launch_quantize_tokens(dtype, x, M, K, token_stride, channel_stride, codes, Kp, Kp, scales, stream);
     if (e != hipSuccess) return hip_fail(e, "quantize launch");
-    const Layer L = {codes, Kp, scales, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out, ldo, map};
+    L.codes = codes;
+    L.codes_stride = Kp;
+    L.scales = scales;
     e = launch_matmul(L, out_dtype, true, room, stream);
     return e == hipSuccess ? DSS_OK : hip_fail(e, "token product launch");
 } catch (...) {

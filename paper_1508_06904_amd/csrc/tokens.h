@@ -29,7 +29,16 @@ struct Layer {
     void* out;
     int64_t ldo;                         // the output's stride that is not 1
     int map;                             // out is [N][M], not [M][N]
+    int past;                            // the outputs go around the caches
 };
+
+// Whether outputs go around the caches: large ones whose rows are whole lines.  200000 x
+// 1024 in bfloat16 from 512 channels: 280 us around them and 340 through them; 512 x 198025 in
+// binary32 from 256, where rows end inside lines: 925 and 387.
+inline bool outputs_past(int64_t M, int64_t N, int64_t ldo, const void* out, dss_dtype dt) {
+    const int64_t es = (int64_t)dtype_size(dt);
+    return M * N * es > ((int64_t)1 << 26) && ldo * es % 128 == 0 && (uintptr_t)out % 128 == 0;
+}
 
 // Tokens that are not codes yet.
 struct Values {

@@ -288,7 +288,13 @@ __device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t
                                     : output_of(s, Q.scale[c + k], P.scale, Q.bias[c + k], L.act));
         }
         if (j + c + C <= J) {
-            __builtin_memcpy(p + c, &r, sizeof r);
+            if constexpr (sizeof(Tout) * C == 16) {
+                using u32x4 = __attribute__((ext_vector_type(4), aligned(sizeof(Tout)))) uint32_t;
+                if (L.past) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), reinterpret_cast<u32x4*>(p + c));
+                else __builtin_memcpy(p + c, &r, sizeof r);
+            } else {
+                __builtin_memcpy(p + c, &r, sizeof r);
+            }
         } else {
 #pragma unroll
             for (int k = 0; k < C - 1; ++k)
