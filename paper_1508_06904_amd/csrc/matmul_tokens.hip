@@ -36,11 +36,12 @@ __host__ __device__ __forceinline__ Sides sides_of(const Layer& L) {
 // buffers.  With KG > 1 so many groups of waves take the steps in turn, each with buffers
 // of its own: where tiles are fewer than units, a unit has more steps under way.
 //
-// A matrix operand is 16 rows: of P adjacent ones; of Q those that give a lane 4 TJ
-// adjacent outputs over its TJ operands, rows 4 TJ q + 4 n + r for operand n (q, r <
-// 4), so that the outputs leave in 16-byte stores and whole lines.  A row of a buffer
-// is 8 units of 16 bytes; a row that is an operand's row l keeps unit u at place
-// u ^ (l & 7): the 8 rows that the operand's read takes at once lie in different banks.
+// A matrix operand is 16 rows: of P adjacent ones; of Q adjacent ones too for
+// binary32 outputs, where a lane's four outputs are a store of 16 bytes and four lanes
+// write 64 adjacent bytes; for bfloat16 outputs two operands share 32 rows, so that a
+// lane has eight adjacent outputs over both and the same holds.  A row of a buffer is 8
+// units of 16 bytes; a row that is an operand's row l keeps unit u at place u ^ (l & 7):
+// the 8 rows that the operand's read takes at once lie in different banks.
 //
 // The units go from global memory to LDS without a stop in registers; for that rows
 // start at 16-byte units, and K ends at one (what does not is copied first).
@@ -61,6 +62,7 @@ template <typename Tout, int BI, int BJ, int WI, int WJ, int KG, bool MAP>
 __global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))) void matmul_tile_kernel(Layer L, int tiles_i, int tiles_j) {
     constexpr int NW = WI * WJ, THREADS = NW * 64;
     constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
+    constexpr int C = 16 / (int)sizeof(Tout);            // outputs of a store, from C / 4 operands of Q
     constexpr int LP = BI * kUnits / THREADS, LQ = BJ * kUnits / THREADS;   // units of each thread and step
     static_assert(LP * THREADS == BI * kUnits && LQ * THREADS == BJ * kUnits && THREADS % 64 == 0, "tile");
     constexpr int BUF = (BI + BJ) * kStep;
@@ -79,8 +81,8 @@ __global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu
 
     // the thread's units: rows row0 + n * (THREADS / 8), and one place in each of them
     const int row0 = tid >> 3;
-    const int unit_p = (tid & 7) ^ (row0 & 7), unit_q = (tid & 7) ^ ((row0 & 3) | (row0 / (TJ * 4) & 1) << 2);
-    static_assert(THREADS / 8 % (TJ * 8) == 0, "the places of a thread's units differ");
+    const int unit_p = (tid & 7) ^ (row0 & 7), unit_q = (tid & 7) ^ ((row0 & 3) | (row0 / C & 1) << 2);
+    static_assert(THREADS / 8 % 32 == 0 && TJ % (C / 4) == 0, "the places of a thread's units, the operands of a store");
     const int8_t *src_p[LP], *src_q[LQ];
 #pragma unroll
     for (int n = 0; n < LP; ++n) src_p[n] = S.P + min(i0 + row0 + n * (THREADS / 8), S.I - 1) * S.ps;
@@ -107,9 +109,9 @@ __global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu
     // The matrix operands of half a step (64 of K): TJ of Q, then TI of P.
     using Half = i32x4[TI + TJ];
     const int at_p = (wi * TI * 16 + l16) * kStep;
-    const int at_q = (BI + wj * TJ * 16 + (l16 >> 2) * TJ * 4 + (l16 & 3)) * kStep;
+    const int at_q = (BI + wj * TJ * 16 + (l16 >> 2) * C + (l16 & 3)) * kStep;
     auto read = [&](Half& o, int n, int s, int h) {
-        const int at = n < TJ ? at_q + n * 4 * kStep : at_p + (n - TJ) * 16 * kStep;
+        const int at = n < TJ ? at_q + (n / (C / 4) * 4 * C + n % (C / 4) * 4) * kStep : at_p + (n - TJ) * 16 * kStep;
         o[n] = *reinterpret_cast<const i32x4*>(buffers + (s & 1) * BUF + at + ((h * 4 + q16) ^ (l16 & 7)) * 16);
     };
     // Multiplies one half's operands, reads another's (half h of step s) and fetches a step's
@@ -162,15 +164,21 @@ __global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
             for (int n = 0; n < TI * TJ; ++n) acc[n / TJ][n % TJ] += sums[(g * TI * TJ + n) * THREADS];
     }
-    const int64_t j = j0 + wj * TJ * 16 + q16 * TJ * 4;
-    const auto side_q = side_j<MAP, TJ * 4>(L, j);
+    constexpr int STORES = TJ * 4 / C;
+    const int64_t j = j0 + wj * TJ * 16 + q16 * C;
+    SideN<C> side_q[STORES];
     Side1 side_p[TI];
+#pragma unroll
+    for (int c = 0; c < STORES; ++c) side_q[c] = side_j<MAP, C>(L, j + c * 4 * C);
 #pragma unroll
     for (int a = 0; a < TI; ++a) side_p[a] = side_i<MAP>(L, i0 + (wi * TI + a) * 16 + l16);
 #pragma unroll
     for (int a = 0; a < TI; ++a) {
         const int64_t i = i0 + (wi * TI + a) * 16 + l16;
-        if (i < S.I && j < S.J) store_outputs<Tout, MAP>(L, i, j, S.J, acc[a], side_p[a], side_q);
+#pragma unroll
+        for (int c = 0; c < STORES; ++c)
+            if (i < S.I && j + c * 4 * C < S.J)
+                store_outputs<Tout, MAP>(L, i, j + c * 4 * C, S.J, &acc[a][c * (C / 4)], side_p[a], side_q[c]);
     }
 }
 

@@ -173,12 +173,24 @@ struct MapTile {
     __device__ __forceinline__ void load(const T* x, int64_t channel_stride, int left, int k, int K) {
         const int t = (threadIdx.x & 15) * V;
         const T* p = x + t + k * channel_stride;
-        if (left >= kTokens) {
+        const int missing = t + V - left;              // tokens of the lane that do not exist
+        if (missing <= 0) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 c[r] = Chunk<T>{};
                 if (k + r < K) __builtin_memcpy(&c[r], p + r * channel_stride, 16);
             }
+        } else if (missing < V && left >= V) {
+            // the last V tokens that exist, moved to their places
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                c[r] = Chunk<T>{};
+                if (k + r < K) __builtin_memcpy(&c[r], p - missing + r * channel_stride, 16);
+            }
+            const int bits = missing * (int)sizeof(T) * 8;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                c[r] = __builtin_bit_cast(Chunk<T>, __builtin_bit_cast(unsigned __int128, c[r]) >> bits);
         } else {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
