@@ -468,9 +468,16 @@ dss_status dss_quantize_tokens(const void* x, dss_dtype dtype, int64_t M, int32_
                                int64_t channel_stride, int8_t* codes, int64_t codes_stride, float* scales,
                                hipStream_t stream);
 
-/* Workspace bytes of dss_matmul_tokens (from_codes nonzero) or dss_linear_tokens
- * for M tokens of K channels and N outputs, whatever the strides (host only). */
-dss_status dss_tokens_workspace(int64_t M, int32_t N, int32_t K, int32_t from_codes, int64_t* workspace_bytes);
+/* What a layer's tokens are. */
+typedef enum dss_token_source {
+    DSS_TOKENS_ROWS = 0,    /* values, the channels adjacent (dss_linear_tokens with channel_stride = 1) */
+    DSS_TOKENS_MAP = 1,     /* values, the tokens adjacent (dss_linear_tokens with another channel_stride) */
+    DSS_TOKENS_CODES = 2    /* codes (dss_matmul_tokens) */
+} dss_token_source;
+
+/* Workspace bytes of a layer on M tokens of K channels with N outputs, whatever the
+ * other strides (host only). */
+dss_status dss_tokens_workspace(int64_t M, int32_t N, int32_t K, dss_token_source source, int64_t* workspace_bytes);
 
 /* The layer on tokens that are already codes.
  *   codes          device, codes[m * codes_stride + k], codes_stride >= K

@@ -1,5 +1,5 @@
-// A fully connected layer on many tokens in one launch: a workgroup codes its tokens
-// into LDS and multiplies them with all of the weights from there.
+// A fully connected layer on the tokens of a map in one launch: a workgroup codes its
+// tokens into LDS and multiplies them with all of the weights from there.
 //
 // The tokens' values are read once, and their codes never travel: in two launches
 // they are written to and read back from memory, a byte each way beside the 4 (or
@@ -17,24 +17,22 @@ namespace dss {
 
 namespace {
 
-constexpr int kMaxChannels = 1024;       // of a token in LDS
-constexpr int kRowTokens = 64;           // tokens of a workgroup, rows
-constexpr int kRowWaves = 8;
+constexpr int kMaxChannels = kMapWaves * 64;       // of a token in registers, and in LDS
 
 // A token's codes in LDS: whole matrix operands of 64, and 16 bytes more, so that tokens start in different banks.
 __host__ __device__ constexpr int tile_pitch(int K) { return (K + 63) / 64 * 64 + 16; }
 
-// Codes and scales of the tokens of a map from x on: `groups` tiles beside each other, `waves` waves for each.
+// Codes and scales of the tokens of a map from x on: tiles beside each other, `waves` waves for each.
 template <typename T>
-__device__ __forceinline__ void code_map(const T* x, int64_t channel_stride, int64_t left, int K, int waves, int pitch,
-                                         int8_t* codes, float* scales) {
+__device__ __forceinline__ void code_map(const T* x, int64_t channel_stride, int K, int waves, int pitch, int8_t* codes,
+                                         float* scales) {
     using Tile = MapTile<T>;
     __shared__ uint32_t tops[kMapWaves * 64];
     const int wave = threadIdx.x >> 6, group = wave / waves, k = (wave - group * waves) * 64 + ((threadIdx.x >> 4) & 3) * 16;
-    const int t0 = group * Tile::kTokens, t = t0 + (threadIdx.x & 15) * Tile::V;
+    const int t = group * Tile::kTokens + (threadIdx.x & 15) * Tile::V;
     Tile tile;
     uint32_t top[4] = {};
-    tile.load(x + t0, channel_stride, (int)max((int64_t)0, min(left - t0, (int64_t)Tile::kTokens)), k, K);
+    tile.load(x + group * Tile::kTokens, channel_stride, k, K);
     tile.raise_into(top);
     Tile::meet(top, tops, group * waves, waves);
 #pragma unroll
@@ -47,57 +45,26 @@ __device__ __forceinline__ void code_map(const T* x, int64_t channel_stride, int
     }
 }
 
-// The same of kRowTokens rows: each wave takes an eighth of them, kTogether at a time.
-template <typename T>
-__device__ __forceinline__ void code_rows(const T* x, int64_t token_stride, int64_t left, int K, int pitch,
-                                          int8_t* codes, float* scales) {
-    constexpr int E = Chunk<T>::E, CH = kMaxChannels / 64 / E, kTogether = 4;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll 1
-    for (int m = wave * (kRowTokens / kRowWaves); m < (wave + 1) * (kRowTokens / kRowWaves); m += kTogether) {
-        Chunk<T> c[kTogether][CH];
-#pragma unroll
-        for (int u = 0; u < kTogether; ++u) load_row(c[u], x + min((int64_t)(m + u), left - 1) * token_stride, lane, 64, K);
-#pragma unroll
-        for (int u = 0; u < kTogether; ++u) {
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < CH; ++i) top = raise(top, c[u][i]);
-            top = top_bits<T>(top);
-#pragma unroll
-            for (int d = 32; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-            const Coder coder(scale_of(top));
-            if (lane == 0) scales[m + u] = coder.scale;
-#pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                const int at = (i * 64 + lane) * E;
-                if (at < pitch - 16) store_codes(codes + (m + u) * pitch + at, c[u][i], coder, E);
-            }
-        }
-    }
-}
-
-template <typename T, typename Tout, bool ROWS, bool MAP>
-__global__ __launch_bounds__(1024) void linear_tile_kernel(Layer L, Values V, int tokens, int waves) {
+// `tokens` tokens for each workgroup; the last one's end with the last token, and
+// it leaves out what the one before it has.
+template <typename T, typename Tout, bool MAP>
+__global__ __launch_bounds__(kMapWaves * 64) void linear_tile_kernel(Layer L, Values V, int tokens, int waves) {
     extern __shared__ __align__(16) int8_t lds[];
     const int K = L.K, pitch = tile_pitch(K);
     float* scales = reinterpret_cast<float*>(lds + tokens * pitch);
-    const int64_t m0 = xcd_order(blockIdx.x, gridDim.x) * tokens, left = L.M - m0;
-    if constexpr (ROWS)
-        code_rows(static_cast<const T*>(V.x) + m0 * V.token_stride, V.token_stride, left, K, pitch, lds, scales);
-    else
-        code_map(static_cast<const T*>(V.x) + m0, V.channel_stride, left, K, waves, pitch, lds, scales);
+    const int64_t tile0 = xcd_order(blockIdx.x, gridDim.x) * tokens, m0 = min(tile0, L.M - tokens);
+    const int first = (int)(tile0 - m0);
+    code_map(static_cast<const T*>(V.x) + m0, V.channel_stride, K, waves, pitch, lds, scales);
     __syncthreads();
 
     // 16 outputs of 64 tokens at a time for a wave
     const int lane = threadIdx.x & 63, l16 = lane & 15, q16 = lane >> 4;
     const int quarters = tokens / 64, items = (L.N + 15) / 16 * quarters;
     L.scales = scales;
-    L.M = min(left, (int64_t)tokens);
+    L.M = tokens;
     L.out = static_cast<Tout*>(L.out) + m0 * (MAP ? 1 : L.ldo);
     for (int item = threadIdx.x >> 6; item < items; item += blockDim.x >> 6) {
         const int n0 = item / quarters * 16, t0 = (item - item / quarters * quarters) * 64;
-        if (t0 >= L.M) continue;
         const int8_t* w = L.weight + (int64_t)min(n0 + l16, L.N - 1) * L.weight_stride;
         const int8_t* t = lds + (t0 + l16) * pitch + q16 * 16;
         i32x4 acc[4] = {};
@@ -129,50 +96,50 @@ __global__ __launch_bounds__(1024) void linear_tile_kernel(Layer L, Values V, in
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int64_t i = MAP ? n0 + l16 : t0 + g * 16 + l16, j = MAP ? t0 + g * 16 + q16 * 4 : n0 + q16 * 4;
-            if (i < I && j < J) store_outputs<Tout, MAP>(L, i, j, J, &acc[g], p[g], q[g]);
+            if (i >= I || j >= J || (!MAP && i < first)) continue;
+            store_outputs<Tout, MAP>(L, i, j, J, &acc[g], p[g], q[g], MAP ? first : 0);
         }
     }
 }
 
-template <typename T, typename Tout, bool ROWS, bool MAP>
+template <typename T, typename Tout>
 hipError_t run_linear(const Layer& L, const Values& V, hipStream_t s) {
-    int tokens = kRowTokens, waves = kRowWaves, groups = 1;
-    if (!ROWS) {
-        waves = (L.K + 63) / 64;
-        groups = std::max(1, 8 / waves);
-        tokens = groups * MapTile<T>::kTokens;
-    }
+    const int waves = (L.K + 63) / 64, groups = std::max(1, 8 / waves), tokens = groups * MapTile<T>::kTokens;
     const size_t lds = (size_t)tokens * (tile_pitch(L.K) + 4);
-    const auto kern = linear_tile_kernel<T, Tout, ROWS, MAP>;
+    const auto kern = L.map ? linear_tile_kernel<T, Tout, true> : linear_tile_kernel<T, Tout, false>;
     const hipError_t e = allow_dynamic_lds((const void*)kern, lds);
     if (e != hipSuccess) return e;
     kern<<<dim3((unsigned)ceil_div64(L.M, tokens)), waves * groups * 64, lds, s>>>(L, V, tokens, waves);
     return hipGetLastError();
 }
 
-template <typename T, typename Tout>
-hipError_t run_layouts(const Layer& L, const Values& V, hipStream_t s) {
-    if (V.channel_stride == 1 || L.K == 1)
-        return L.map ? run_linear<T, Tout, true, true>(L, V, s) : run_linear<T, Tout, true, false>(L, V, s);
-    return L.map ? run_linear<T, Tout, false, true>(L, V, s) : run_linear<T, Tout, false, false>(L, V, s);
-}
+constexpr int64_t kLeastTokens = 4096;
 
 }  // namespace
 
-bool linear_in_tiles(int64_t M, int N, int K) { return !few_tokens(M, N) && K <= kMaxChannels && N <= 256; }
+// Where one launch is the faster one; in microseconds for one launch and for two,
+// 400000 tokens of 256 channels in binary32 to 16, 64 and 128 outputs: 99/135, 124/153,
+// 159/188, and in bfloat16 62/115, 92/123, 151/144; 100000 of 512 channels to 128 and 256: 64/81,
+// 83/93 in binary32, 64/68, 95/84 in bfloat16; 400000 of 128 channels in bfloat16 to 64: 80/65.
+// Rows of values (the channels adjacent) gain less than a tenth and are always coded first.
+bool linear_in_tiles(int64_t M, int N, int K, bool map) {
+    return map && M >= kLeastTokens && K <= kMaxChannels && ((K >= 512 && N <= 128) || (K >= 256 && N <= 64));
+}
 
 hipError_t launch_linear_tiles(const Layer& L, const Values& V, dss_dtype out_dtype, hipStream_t s) {
-    for (int64_t m = 0; m < L.M; m += kSlabTokens) {
+    // slabs of equal size but for the last, none below kLeastTokens
+    const int64_t slabs = ceil_div64(L.M, kSlabTokens), slab = ceil_div64(L.M, slabs);
+    for (int64_t m = 0; m < L.M; m += slab) {
         Layer S = L;
         Values W = V;
-        S.M = std::min(L.M - m, kSlabTokens);
+        S.M = std::min(L.M - m, slab);
         S.out = static_cast<char*>(L.out) + m * (L.map ? 1 : L.ldo) * (int64_t)dtype_size(out_dtype);
-        W.x = static_cast<const char*>(V.x) + m * V.token_stride * (int64_t)dtype_size(V.dtype);
+        W.x = static_cast<const char*>(V.x) + m * (int64_t)dtype_size(V.dtype);
         hipError_t e;
         if (V.dtype == DSS_BF16)
-            e = out_dtype == DSS_BF16 ? run_layouts<uint16_t, uint16_t>(S, W, s) : run_layouts<uint16_t, float>(S, W, s);
+            e = out_dtype == DSS_BF16 ? run_linear<uint16_t, uint16_t>(S, W, s) : run_linear<uint16_t, float>(S, W, s);
         else
-            e = out_dtype == DSS_BF16 ? run_layouts<float, uint16_t>(S, W, s) : run_layouts<float, float>(S, W, s);
+            e = out_dtype == DSS_BF16 ? run_linear<float, uint16_t>(S, W, s) : run_linear<float, float>(S, W, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

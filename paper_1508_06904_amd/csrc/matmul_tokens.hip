@@ -330,10 +330,10 @@ dss_status check_layer(int64_t M, const int8_t* weight, int64_t weight_stride, c
 
 // The copies of weights and codes (whatever their addresses turn out to be), or the
 // weights' copy and the tokens' codes and scales.
-int64_t workspace_bytes_of(int64_t M, int32_t N, int32_t K, bool from_codes) {
+int64_t workspace_bytes_of(int64_t M, int32_t N, int32_t K, dss_token_source source) {
     const int64_t Kp = padded_k(K), weights = few_tokens(M, N) ? 0 : align256(N * Kp);
-    if (from_codes) return few_tokens(M, N) ? 0 : weights + align256(copied_tokens(M, K) * Kp);
-    if (codes_itself(M, K) || linear_in_tiles(M, N, K)) return 0;
+    if (source == DSS_TOKENS_CODES) return few_tokens(M, N) ? 0 : weights + align256(copied_tokens(M, K) * Kp);
+    if (codes_itself(M, K) || linear_in_tiles(M, N, K, source == DSS_TOKENS_MAP)) return 0;
     return weights + align256(M * Kp) + align256(M * 4);
 }
 
@@ -356,13 +356,15 @@ bool is_map(int64_t M, int32_t N, int64_t out_token_stride, int64_t out_channel_
 
 }  // namespace dss
 
-extern "C" dss_status dss_tokens_workspace(int64_t M, int32_t N, int32_t K, int32_t from_codes,
+extern "C" dss_status dss_tokens_workspace(int64_t M, int32_t N, int32_t K, dss_token_source source,
                                            int64_t* workspace_bytes) try {
     using namespace dss;
     if (!workspace_bytes) return fail(DSS_E_INVALID, "NULL output");
     if (M < 0 || M > kMaxTokens || N < 1 || N > kMaxN || K < 1)
         return fail(DSS_E_INVALID, "%lld tokens of %d channels, %d outputs", (long long)M, K, N);
-    *workspace_bytes = workspace_bytes_of(M, N, K, from_codes != 0);
+    if (source != DSS_TOKENS_ROWS && source != DSS_TOKENS_MAP && source != DSS_TOKENS_CODES)
+        return fail(DSS_E_INVALID, "unknown token source %d", (int)source);
+    *workspace_bytes = workspace_bytes_of(M, N, K, source);
     return DSS_OK;
 } catch (...) {
     return DSS_E_NOMEM;
@@ -381,7 +383,7 @@ extern "C" dss_status dss_matmul_tokens(const int8_t* codes, int64_t codes_strid
     if (M == 0) return DSS_OK;
     if (!codes || !scales || (uintptr_t)scales % 4 != 0)
         return fail(DSS_E_INVALID, "codes or scales is NULL or not aligned to its elements");
-    s = check_room(workspace_bytes_of(M, N, K, true), workspace, workspace_bytes);
+    s = check_room(workspace_bytes_of(M, N, K, DSS_TOKENS_CODES), workspace, workspace_bytes);
     if (s != DSS_OK) return s;
     const bool map = is_map(M, N, out_token_stride, out_channel_stride);
     const int64_t ldo = map ? out_channel_stride : out_token_stride;
@@ -406,13 +408,14 @@ extern "C" dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t 
                     out_channel_stride);
     if (s != DSS_OK) return s;
     if (M == 0) return DSS_OK;
-    s = check_room(workspace_bytes_of(M, N, K, false), workspace, workspace_bytes);
+    const bool from_map = channel_stride != 1 && K > 1;
+    s = check_room(workspace_bytes_of(M, N, K, from_map ? DSS_TOKENS_MAP : DSS_TOKENS_ROWS), workspace, workspace_bytes);
     if (s != DSS_OK) return s;
     const bool map = is_map(M, N, out_token_stride, out_channel_stride);
     const int64_t ldo = map ? out_channel_stride : out_token_stride;
     Layer L = {nullptr, 0, nullptr, M, weight, weight_stride, weight_scales, N, K, bias, (int)act, out, ldo, map,
                outputs_past(M, N, ldo, out, out_dtype)};
-    if (codes_itself(M, K) || linear_in_tiles(M, N, K)) {
+    if (codes_itself(M, K) || linear_in_tiles(M, N, K, from_map)) {
         const Values V = {x, dtype, token_stride, channel_stride};
         hipError_t e = codes_itself(M, K) ? launch_linear_few(L, V, out_dtype, stream)
                                           : launch_linear_tiles(L, V, out_dtype, stream);

@@ -54,9 +54,9 @@ hipError_t launch_matmul_few(const Layer& L, dss_dtype out_dtype, hipStream_t s)
 bool codes_itself(int64_t M, int K);
 hipError_t launch_linear_few(const Layer& L, const Values& V, dss_dtype out_dtype, hipStream_t s);
 
-// The layer on many tokens of few channels with few outputs, coded and multiplied
-// in one launch (linear_tile.hip), and whether it runs there.
-bool linear_in_tiles(int64_t M, int N, int K);
+// The layer on many tokens of a map of few channels with few outputs, coded and
+// multiplied in one launch (linear_tile.hip), and whether it runs there.
+bool linear_in_tiles(int64_t M, int N, int K, bool map);
 hipError_t launch_linear_tiles(const Layer& L, const Values& V, dss_dtype out_dtype, hipStream_t s);
 
 // Codes and scales of M > 0 tokens; codes[m][K .. Kp-1] are written as zeros.

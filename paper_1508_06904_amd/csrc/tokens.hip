@@ -77,8 +77,9 @@ __global__ __launch_bounds__(kThreads) void quantize_long_rows_kernel(const T* _
         store_codes(out + at, load_chunk(row + at, (int)(K - at)), coder, (int)(Kp - at));
 }
 
-// Maps: see MapTile.  Of more channels than a workgroup holds the values are read
-// twice, the second time mostly from cache.
+// Maps of at least a tile's tokens: see MapTile.  The last tile ends with the last
+// token and leaves out what the one before it has.  Of more channels than a workgroup
+// holds the values are read twice, the second time mostly from cache.
 template <typename T>
 __global__ __launch_bounds__(kMapWaves * 64) void quantize_map_kernel(const T* __restrict__ x, int64_t M, int K,
                                                                       int64_t channel_stride,
@@ -86,16 +87,14 @@ __global__ __launch_bounds__(kMapWaves * 64) void quantize_map_kernel(const T* _
                                                                       int Kp, float* __restrict__ scales) {
     using Tile = MapTile<T>;
     __shared__ uint32_t tops[kMapWaves * 64];
-    const int64_t m0 = xcd_order(blockIdx.x, gridDim.x) * Tile::kTokens;
-    const int left = (int)min(M - m0, (int64_t)Tile::kTokens);
+    const int64_t tile0 = xcd_order(blockIdx.x, gridDim.x) * Tile::kTokens, m0 = min(tile0, M - Tile::kTokens);
+    const int first = (int)(tile0 - m0);
     const int span = (int)(blockDim.x >> 6) * 64;      // channels held at once
+    const int own_k = (int)(threadIdx.x >> 4) * 16;
     Tile tile;
     uint32_t top[4] = {};
-    const int own_k = (int)(threadIdx.x >> 4) * 16;
-    tile.load(x + m0, channel_stride, left, own_k, K);
-    tile.raise_into(top);
-    for (int k0 = span; k0 < K; k0 += span) {
-        tile.load(x + m0, channel_stride, left, k0 + own_k, K);
+    for (int k0 = 0; k0 < K; k0 += span) {
+        tile.load(x + m0, channel_stride, k0 + own_k, K);
         tile.raise_into(top);
     }
     Tile::meet(top, tops, 0, blockDim.x >> 6);
@@ -104,11 +103,11 @@ __global__ __launch_bounds__(kMapWaves * 64) void quantize_map_kernel(const T* _
     for (int round = rounds - 1; round >= 0; --round) {
         // (the last span is still there)
         const int k = round * span + own_k;
-        if (round != rounds - 1) tile.load(x + m0, channel_stride, left, k, K);
+        if (round != rounds - 1) tile.load(x + m0, channel_stride, k, K);
 #pragma unroll
         for (int j = 0; j < Tile::V; ++j) {
             const Coder coder(scale_of(Tile::bits(top, j)));
-            if (t + j >= left) continue;
+            if (t + j < first) continue;
             if (round == 0 && threadIdx.x < 16) scales[m0 + t + j] = coder.scale;
             uint32_t w[4];
             tile.codes(j, coder, w);
@@ -124,6 +123,21 @@ __global__ __launch_bounds__(kMapWaves * 64) void quantize_map_kernel(const T* _
     }
 }
 
+// Narrower maps: a workgroup for each token, value by value; the tokens' lines meet in cache.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void quantize_narrow_map_kernel(const T* __restrict__ x, int K,
+                                                                       int64_t channel_stride,
+                                                                       int8_t* __restrict__ codes, int64_t codes_stride,
+                                                                       int Kp, float* __restrict__ scales) {
+    const int64_t m = blockIdx.x;
+    uint32_t top = 0;
+    for (int k = threadIdx.x; k < K; k += kThreads) top = max(top, abs_bits(to_f32(x[m + k * channel_stride])));
+    const Coder coder(scale_of(row_max<kThreads>(top)));
+    if (threadIdx.x == 0) scales[m] = coder.scale;
+    for (int k = threadIdx.x; k < Kp; k += kThreads)
+        codes[m * codes_stride + k] = k < K ? coder.one(to_f32(x[m + k * channel_stride])) : 0;
+}
+
 template <typename T, int LPR, int CH>
 void run_rows(const T* x, int64_t M, int K, int64_t ts, int8_t* codes, int64_t cs, int Kp, float* scales, hipStream_t s) {
     quantize_rows_kernel<T, LPR, CH><<<dim3((unsigned)ceil_div64(M, kThreads / LPR)), kThreads, 0, s>>>(x, M, K, ts, codes,
@@ -135,6 +149,10 @@ void run_quantize(const T* x, int64_t M, int K, int64_t ts, int64_t ks, int8_t* 
                   hipStream_t s) {
     constexpr int E = Chunk<T>::E;
     if (ks != 1 && K > 1) {
+        if (M < MapTile<T>::kTokens) {
+            quantize_narrow_map_kernel<T><<<dim3((unsigned)M), kThreads, 0, s>>>(x, K, ks, codes, cs, Kp, scales);
+            return;
+        }
         const int waves = std::min<int>((K + 63) / 64, kMapWaves);
         quantize_map_kernel<T><<<dim3((unsigned)ceil_div64(M, MapTile<T>::kTokens)), waves * 64, 0, s>>>(x, M, K, ks, codes,
                                                                                                       cs, Kp, scales);

@@ -169,36 +169,13 @@ struct MapTile {
     static constexpr int kTokens = 16 * V;
     Chunk<T> c[16];                                    // c[r].value(j): channel r of the lane's group, token j
 
-    // The tile's tokens start at x, `left` of them exist (or none); the lane's channels k .. k+15, those below K.
-    __device__ __forceinline__ void load(const T* x, int64_t channel_stride, int left, int k, int K) {
-        const int t = (threadIdx.x & 15) * V;
-        const T* p = x + t + k * channel_stride;
-        const int missing = t + V - left;              // tokens of the lane that do not exist
-        if (missing <= 0) {
+    // The tile's tokens start at x; the lane's channels k .. k+15, those below K.
+    __device__ __forceinline__ void load(const T* x, int64_t channel_stride, int k, int K) {
+        const T* p = x + (threadIdx.x & 15) * V + k * channel_stride;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                c[r] = Chunk<T>{};
-                if (k + r < K) __builtin_memcpy(&c[r], p + r * channel_stride, 16);
-            }
-        } else if (missing < V && left >= V) {
-            // the last V tokens that exist, moved to their places
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                c[r] = Chunk<T>{};
-                if (k + r < K) __builtin_memcpy(&c[r], p - missing + r * channel_stride, 16);
-            }
-            const int bits = missing * (int)sizeof(T) * 8;
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                c[r] = __builtin_bit_cast(Chunk<T>, __builtin_bit_cast(unsigned __int128, c[r]) >> bits);
-        } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                c[r] = Chunk<T>{};
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (k + r < K && t + j < left) c[r].set(j, p[r * channel_stride + j]);
-            }
+        for (int r = 0; r < 16; ++r) {
+            c[r] = Chunk<T>{};
+            if (k + r < K) __builtin_memcpy(&c[r], p + r * channel_stride, 16);
         }
     }
     __device__ __forceinline__ void raise_into(uint32_t (&top)[4]) const {
@@ -282,10 +259,10 @@ __device__ __forceinline__ SideN<N> side_j(const Layer& L, int64_t j) {
     return r;
 }
 
-// N adjacent outputs D[i][j .. j+N-1] of a layer, those from J on left out; sum[N / 4].
+// N adjacent outputs D[i][j .. j+N-1] of a layer, those before j_first and from J on left out; sum[N / 4].
 template <typename Tout, bool MAP, int N>
 __device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t j, int64_t J, const i32x4* sum,
-                                              const Side1& P, const SideN<N>& Q) {
+                                              const Side1& P, const SideN<N>& Q, int64_t j_first = 0) {
     constexpr int C = N * (int)sizeof(Tout) < 16 ? N : 16 / (int)sizeof(Tout);   // outputs of one store
     Tout* p = static_cast<Tout*>(L.out) + i * L.ldo + j;
 #pragma unroll
@@ -299,7 +276,7 @@ __device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t
             store_elem(&r.v[k], MAP ? output_of(s, P.scale, Q.scale[c + k], P.bias, L.act)
                                     : output_of(s, Q.scale[c + k], P.scale, Q.bias[c + k], L.act));
         }
-        if (j + c + C <= J) {
+        if (j + c >= j_first && j + c + C <= J) {
             if constexpr (sizeof(Tout) * C == 16) {
                 using u32x4 = __attribute__((ext_vector_type(4), aligned(sizeof(Tout)))) uint32_t;
                 if (L.past) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), reinterpret_cast<u32x4*>(p + c));
@@ -309,8 +286,8 @@ __device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < C - 1; ++k)
-                if (j + c + k < J) p[c + k] = r.v[k];
+            for (int k = 0; k < C; ++k)
+                if (j + c + k >= j_first && j + c + k < J) p[c + k] = r.v[k];
         }
     }
 }

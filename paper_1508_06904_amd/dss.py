@@ -736,13 +736,13 @@ def _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, 
         ((s1, s0) if planar else (s0, s1))
 
 
-def _tokens_room(M, N, K, from_codes, workspace, dev, stream):
-    """(address, bytes) of a call's workspace, and what keeps it."""
+def _tokens_room(M, N, K, source, workspace, dev, stream):
+    """(address, bytes) of a call's workspace, and what keeps it.  source: dss_token_source."""
     import torch
     if workspace is not None:
         return _room(workspace, dev) + (workspace,)
     need = ctypes.c_int64()
-    _check(lib().dss_tokens_workspace(M, N, K, from_codes, need), "dss_tokens_workspace")
+    _check(lib().dss_tokens_workspace(M, N, K, source, need), "dss_tokens_workspace")
     if need.value == 0:
         return None, 0, None
     workspace = _empty(need.value, torch.uint8, stream)
@@ -761,7 +761,7 @@ def matmul_i8(codes, scales, weight, weight_scales, bias=None, act="none", out=N
     M, K = codes.shape
     sp = _check_vector(scales, "scales", M, dev)
     out, N, args = _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, dev, stream)
-    room, size, keep = _tokens_room(M, N, K, 1, workspace, dev, stream)
+    room, size, keep = _tokens_room(M, N, K, 2, workspace, dev, stream)
     _check(lib().dss_matmul_tokens(cp, cstride, sp, M, *args, room, size, handle), "dss_matmul_tokens")
     return out
 
@@ -774,6 +774,6 @@ def linear_i8(x, weight, weight_scales, bias=None, act="none", out=None, out_dty
     dt, M, K = _check_tokens(x, dev)
     ts, ks = x.stride()
     out, N, args = _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, dev, stream)
-    room, size, keep = _tokens_room(M, N, K, 0, workspace, dev, stream)
+    room, size, keep = _tokens_room(M, N, K, 1 if ks != 1 and K > 1 else 0, workspace, dev, stream)
     _check(lib().dss_linear_tokens(x.data_ptr(), dt, M, ts, ks, *args, room, size, handle), "dss_linear_tokens")
     return out

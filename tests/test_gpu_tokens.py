@@ -220,6 +220,28 @@ def test_layers_of_tokens(M, N, K, layout, pad, dtype):
     _check_layer(y if planar else y.t(), codes, scales, w, ws, None, "tanh", True)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("planar", [False, True])
+@pytest.mark.parametrize("M,N,K", [(4096, 16, 256), (4097, 64, 300), (5003, 5, 1000), (8191, 128, 700), (6000, 33, 513),
+                                   (4351, 64, 1024)])
+def test_layers_of_maps_in_one_launch(M, N, K, planar, dtype):
+    """Many tokens of a map, few outputs: coded and multiplied in one launch, into a buffer whose
+    other elements stay; a token that is no number among the last ones."""
+    import torch
+    x = _x(M, K, "map", dtype).clone()
+    x[M - 2, K // 2] = float("nan")
+    x = x.t().contiguous().t()
+    w, ws, bias = _weights(N, K)
+    rows, cols = (N, M) if planar else (M, N)
+    buf = torch.full((rows + 2, cols + 5), -77.0, device="cuda")
+    out = buf[1:rows + 1, 2:2 + cols]
+    dss.linear_i8(x, *map(_dev, (w, ws)), bias=_dev(bias), act="relu", out=out, planar=planar)
+    codes, scales = tokens.quantize(_np(x))
+    _check_layer(out.t() if planar else out, codes, scales, w, ws, bias, "relu")
+    out.fill_(-77)
+    assert bool((buf == -77).all())
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 20, 130), (16, 64, 64), (70, 200, 96), (300, 300, 300)])
 def test_extreme_codes_and_sums(M, N, K):
     """All codes at the ends of their range, -128 among them (a caller's own codes may have it)."""
