@@ -147,6 +147,20 @@ def test_other_orders_of_the_axes():
         _check_clipped(o, t, r)
 
 
+def test_lists_of_more_values_than_the_caches_hold():
+    """Over 2^28 values, in bfloat16: the way around the caches, with the oracle's sums in 64 bits on the GPU."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    grads = [torch.randn(n, generator=gen, device="cuda", dtype=torch.bfloat16) for n in ((1 << 28) - 7, 100_003, 5)]
+    want = float(torch.sqrt(sum((g.double() ** 2).sum() for g in grads)))
+    _check_norm(dss.grad_norm(grads), want)
+    norm, out = dss.clip_grads(grads, 1.0)
+    _check_norm(norm, want)
+    for o, g in zip(out, grads):
+        ref = g.double() * (1.0 / (want + 1e-6))
+        assert bool(((o.double() - ref).abs() <= (2.02 * U + 2.0 ** -8) * ref.abs() + 2.0 ** -134).all())
+
+
 def test_same_gradients_same_bits():
     import torch
     grads = _grads([1_000_003, 77, 300_000], seed=9)
