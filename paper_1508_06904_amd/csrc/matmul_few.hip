@@ -178,10 +178,11 @@ hipError_t run_groups(const Layer& L, const Values& V, hipStream_t s) {
 
 }  // namespace
 
-// Up to 16 tokens, and up to 32 while the outputs are few: there the tiles' workgroups
-// are too few or wait longer (32 tokens through 9216 x 512: 11.9 us here and 20.9 on
-// tiles, through 4096 x 16384: 26.3 and 19.4).
-bool few_tokens(int64_t M, int N) { return M <= 16 || (M <= 32 && N <= 8192); }
+// Up to 32 tokens: there the tiles' workgroups wait longer (32 tokens through 9216 x 512:
+// 11.9 us here and 14.8 on tiles, through 4096 x 4096 8.7 and 10.7), but while the weights are
+// large the tiles' whole-line reading of them counts for more (13 tokens through 4096 x 16384:
+// 19.4 us here, 16.5 on tiles), unless they would be copied for it.
+bool few_tokens(int64_t M, int N, int K) { return M <= 32 && (N <= 8192 || K % 16 != 0); }
 
 hipError_t launch_matmul_few(const Layer& L, dss_dtype out_dtype, hipStream_t s) {
     return out_dtype == DSS_BF16 ? run_groups<int8_t, uint16_t>(L, Values{}, s) : run_groups<int8_t, float>(L, Values{}, s);

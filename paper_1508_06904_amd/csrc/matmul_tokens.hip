@@ -267,7 +267,7 @@ int64_t copied_tokens(int64_t M, int K) {
 
 // The layer on codes; `room` has the weights' copy and the tokens' (unless these are padded already).
 hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, bool padded, char* room, hipStream_t s) {
-    if (few_tokens(L.M, L.N)) return launch_matmul_few(L, out_dtype, s);
+    if (few_tokens(L.M, L.N, L.K)) return launch_matmul_few(L, out_dtype, s);
     const int Kp = padded_k(L.K);
     Rows W = {L.weight, L.weight_stride, L.N, reinterpret_cast<int8_t*>(room)};
     int8_t* copies = W.to + align256((int64_t)L.N * Kp);
@@ -331,8 +331,8 @@ dss_status check_layer(int64_t M, const int8_t* weight, int64_t weight_stride, c
 // The copies of weights and codes (whatever their addresses turn out to be), or the
 // weights' copy and the tokens' codes and scales.
 int64_t workspace_bytes_of(int64_t M, int32_t N, int32_t K, dss_token_source source) {
-    const int64_t Kp = padded_k(K), weights = few_tokens(M, N) ? 0 : align256(N * Kp);
-    if (source == DSS_TOKENS_CODES) return few_tokens(M, N) ? 0 : weights + align256(copied_tokens(M, K) * Kp);
+    const int64_t Kp = padded_k(K), weights = few_tokens(M, N, K) ? 0 : align256(N * Kp);
+    if (source == DSS_TOKENS_CODES) return few_tokens(M, N, K) ? 0 : weights + align256(copied_tokens(M, K) * Kp);
     if (codes_itself(M, K) || linear_in_tiles(M, N, K, source == DSS_TOKENS_MAP)) return 0;
     return weights + align256(M * Kp) + align256(M * 4);
 }
@@ -423,7 +423,7 @@ extern "C" dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t 
     }
     const int Kp = padded_k(K);
     char* room = static_cast<char*>(workspace);
-    int8_t* codes = reinterpret_cast<int8_t*>(room) + (few_tokens(M, N) ? 0 : align256((int64_t)N * Kp));
+    int8_t* codes = reinterpret_cast<int8_t*>(room) + (few_tokens(M, N, K) ? 0 : align256((int64_t)N * Kp));
     float* scales = reinterpret_cast<float*>(codes + align256(M * Kp));
     hipError_t e = launch_quantize_tokens(dtype, x, M, K, token_stride, channel_stride, codes, Kp, Kp, scales, stream);
     if (e != hipSuccess) return hip_fail(e, "quantize launch");

@@ -49,7 +49,7 @@ struct Values {
 
 // The layer for few tokens (matmul_few.hip): whether it runs there, and whether the
 // kernel codes M tokens of K channels itself, with no workspace.
-bool few_tokens(int64_t M, int N);
+bool few_tokens(int64_t M, int N, int K);
 hipError_t launch_matmul_few(const Layer& L, dss_dtype out_dtype, hipStream_t s);
 bool codes_itself(int64_t M, int K);
 hipError_t launch_linear_few(const Layer& L, const Values& V, dss_dtype out_dtype, hipStream_t s);
