@@ -31,7 +31,7 @@ constexpr int kMaxGroups = 1024;         // workgroups (and partial sums) of a l
 // the values that are read for the second time: 132 us, not 152, for 100 million in bfloat16.
 constexpr int64_t kCached = (int64_t)1 << 25;
 // Of even more values little would be left in the caches for the second reading: all of
-// them go around.  470 million in binary32: norm 310 us, not 354, clipping 1150, not 1187.
+// them go around.  537 million in binary32: norm 310 us, not 354, clipping 1150, not 1187.
 constexpr int64_t kPassing = (int64_t)1 << 28;
 constexpr int64_t kMinRun = 4096;        // values of the shortest run: four vectors of each thread
 

@@ -232,7 +232,7 @@ hipError_t run_product(const Layer& L, hipStream_t s) {
 
 // ------------------------------------------------------------------ operands at other addresses
 // Rows that do not start, or whose K does not end, at 16-byte units, copied with
-// zeros up to the next one; a thread for each unit.  Of two operands at once.
+// zeros up to the next one; a wave for each 4 KB of a row.  Of two operands at once.
 struct Rows {
     const int8_t* from;
     int64_t stride, rows;
@@ -240,15 +240,25 @@ struct Rows {
 };
 
 __global__ __launch_bounds__(256) void copy_rows_kernel(Rows A, Rows B, int K, int units) {
-    int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     Rows R = A;
-    if (u >= A.rows * units) {
-        u -= A.rows * units;
+    if (row >= A.rows) {
+        row -= A.rows;
         R = B;
     }
-    const int64_t row = u / units;
-    const int k = (int)(u - row * units) * 16;
-    if (row < R.rows) *reinterpret_cast<i32x4*>(R.to + u * 16) = load_unit(R.from + row * R.stride, k, K);
+    if (row >= R.rows) return;
+    const int8_t* from = R.from + row * R.stride;
+    i32x4* to = reinterpret_cast<i32x4*>(R.to + row * units * 16);
+    const int u0 = blockIdx.y * 256 + (threadIdx.x & 63);
+    i32x4 v[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if ((u0 + c * 64) * 16 + 16 <= K) __builtin_memcpy(&v[c], from + (u0 + c * 64) * 16, 16);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const int u = u0 + c * 64;
+        if (u < units) to[u] = u * 16 + 16 <= K ? v[c] : load_unit(from, u * 16, K);
+    }
 }
 
 bool whole_units(const int8_t* p, int64_t stride, int64_t rows, int K) {
@@ -285,9 +295,9 @@ hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, bool padded, char*
         Rows C = {S.codes, L.codes_stride, copy_c ? S.M : 0, copies};
         Rows w = W;
         if (!copy_w || m > 0) w.rows = 0;
-        const int64_t units = (C.rows + w.rows) * (Kp / 16);
-        if (units) {
-            copy_rows_kernel<<<dim3((unsigned)ceil_div64(units, 256)), 256, 0, s>>>(C, w, L.K, Kp / 16);
+        if (C.rows + w.rows) {
+            copy_rows_kernel<<<dim3((unsigned)ceil_div64(C.rows + w.rows, 4), (unsigned)ceil_div64(Kp, 4096)), 256, 0, s>>>(C, w, L.K,
+                                                                                                            Kp / 16);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }

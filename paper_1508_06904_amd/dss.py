@@ -607,8 +607,9 @@ def grad_norm(grads, norm=None, workspace=None, stream=None):
 
 def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
     """Scales a gradient, given as for grad_norm, by min(1, max_norm / (norm + 1e-6)).
-    Returns (norm, list of scaled tensors).  `out` is the list of tensors to write, of the
-    same shapes, strides and types (`out=grads` clips in place); allocated if None."""
+    Returns (norm, list of scaled tensors).  `out` is the list of tensors to write (allocated if
+    None; `out=grads` clips in place): of the same types and numbers of elements, and of the same
+    shapes and strides unless all tensors are contiguous."""
     import torch
     dev, handle = _launch(stream)
     in_place = out is grads
@@ -623,9 +624,10 @@ def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None
                 with torch.cuda.stream(stream):
                     out = [torch.empty_like(g) for g in grads]
         b, out, plain_out = _tensor_list(out, "out", dev)
-        if b[1::3] != a[1::3] or b[2::3] != a[2::3] or [o.shape for o in out] != [g.shape for g in grads] or \
-                not (plain and plain_out) and [o.stride() for o in out] != [g.stride() for g in grads]:
-            raise ValueError("out must be of grads' shapes, strides and types")
+        if b[1::3] != a[1::3] or b[2::3] != a[2::3] or not (plain and plain_out) and \
+                [(o.shape, o.stride()) for o in out] != [(g.shape, g.stride()) for g in grads]:
+            raise ValueError("out must be of grads' types and sizes, and unless all are contiguous of their shapes "
+                             "and strides")
     norm, wp, wb, keep = _norm_buffers(norm, workspace, dev, stream)
     ptrs = b[0::3]
     _check(lib().dss_clip_grads(a.buffer_info()[0], ptrs.buffer_info()[0], len(grads), max_norm, norm.data_ptr(), wp, wb,
