@@ -69,7 +69,8 @@ __device__ void code_few(const Values& V, int M, int K, int pitch, int8_t* codes
 // The codes' row length in LDS: whole slabs and 16 bytes, so that tokens start in different banks.
 __host__ __device__ constexpr int few_pitch(int K) { return (K + kSlab - 1) / kSlab * kSlab + 16; }
 
-template <typename Code, typename Tout, int GT, bool MAP>
+// ODD: weights or codes that start inside words.
+template <typename Code, typename Tout, int GT, bool MAP, bool ODD>
 __global__ __launch_bounds__(kFewWaves * 64) void matmul_few_kernel(Layer L, Values V, int R) {
     constexpr bool kCodes = sizeof(Code) == 1;
     __shared__ i32x4 part[kFewWaves][GT][64];
@@ -81,9 +82,15 @@ __global__ __launch_bounds__(kFewWaves * 64) void matmul_few_kernel(Layer L, Val
     const int K = L.K;
     constexpr int H = kSlab / 64;
     auto weights = [&](int tile) { return L.weight + (int64_t)min(tile * R + min(l16, R - 1), L.N - 1) * L.weight_stride; };
-    auto fetch = [&](const int8_t* row, int k0, i32x4* to) {
+    const int8_t* const w_end = L.weight + (L.N - 1) * L.weight_stride + K;
+    const int8_t* const c_end = L.codes + (L.M - 1) * L.codes_stride + K;
+    auto fetch = [&](const int8_t* row, int k0, i32x4* to, const int8_t* begin, const int8_t* end) {
 #pragma unroll
-        for (int h = 0; h < H; ++h) __builtin_memcpy(&to[h], row + k0 + h * 64 + q16 * 16, 16);
+        for (int h = 0; h < H; ++h) {
+            const int8_t* from = row + k0 + h * 64 + q16 * 16;
+            if constexpr (ODD) to[h] = load_any(from, begin, end);
+            else __builtin_memcpy(&to[h], from, 16);
+        }
     };
     auto multiply = [](i32x4 u, i32x4 v, i32x4 c) {
         return MAP ? __builtin_amdgcn_mfma_i32_16x16x64_i8(v, u, c, 0, 0, 0)
@@ -93,7 +100,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void matmul_few_kernel(Layer L, Val
     // the first weights are on their way while the tokens are coded
     const int8_t* w = weights(blockIdx.x);
     const int k_first = wave * kSlab, k_whole = K / kSlab * kSlab;
-    if (!kCodes && k_first < k_whole) fetch(w, k_first, a);
+    if (!kCodes && k_first < k_whole) fetch(w, k_first, a, L.weight, w_end);
     if constexpr (kCodes) {
 #pragma unroll
         for (int g = 0; g < GT; ++g) t[g] = L.codes + min((int64_t)(g * 16 + l16), L.M - 1) * L.codes_stride;
@@ -113,7 +120,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void matmul_few_kernel(Layer L, Val
 #pragma unroll
             for (int g = 0; g < GT; ++g) {
                 if constexpr (kCodes) {
-                    fetch(t[g], k0, b[g]);
+                    fetch(t[g], k0, b[g], L.codes, c_end);
                 } else {
 #pragma unroll
                     for (int h = 0; h < H; ++h) b[g][h] = *reinterpret_cast<const i32x4*>(t[g] + k0 + h * 64 + q16 * 16);
@@ -121,7 +128,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void matmul_few_kernel(Layer L, Val
             }
         };
         for (int k0 = k_first; k0 < k_whole; k0 += kFewWaves * kSlab) {
-            if (kCodes || k0 != k_first || tile != (int)blockIdx.x) fetch(w, k0, a);
+            if (kCodes || k0 != k_first || tile != (int)blockIdx.x) fetch(w, k0, a, L.weight, w_end);
             fetch_tokens(k0);
 #pragma unroll
             for (int h = 0; h < H; ++h)
@@ -163,8 +170,13 @@ hipError_t run_few(const Layer& L, const Values& V, hipStream_t s) {
     while (R > 2 && ceil_div64(L.N, R) < 256) R /= 2;
     const dim3 grid((unsigned)std::min<int64_t>(ceil_div64(L.N, R), sizeof(Code) == 1 ? 4096 : 256));
     const size_t lds = sizeof(Code) == 1 ? 0 : (size_t)L.M * few_pitch(L.K);
-    if (L.map) matmul_few_kernel<Code, Tout, GT, true><<<grid, kFewWaves * 64, lds, s>>>(L, V, R);
-    else matmul_few_kernel<Code, Tout, GT, false><<<grid, kFewWaves * 64, lds, s>>>(L, V, R);
+    auto words = [](const int8_t* p, int64_t stride, int64_t rows) {
+        return (uintptr_t)p % 4 == 0 && (stride % 4 == 0 || rows == 1);
+    };
+    const bool odd = !words(L.weight, L.weight_stride, L.N) || (sizeof(Code) == 1 && !words(L.codes, L.codes_stride, L.M));
+    const auto kern = L.map ? (odd ? matmul_few_kernel<Code, Tout, GT, true, true> : matmul_few_kernel<Code, Tout, GT, true, false>)
+                            : (odd ? matmul_few_kernel<Code, Tout, GT, false, true> : matmul_few_kernel<Code, Tout, GT, false, false>);
+    kern<<<grid, kFewWaves * 64, lds, s>>>(L, V, R);
     return hipGetLastError();
 }
 

@@ -247,13 +247,13 @@ __global__ __launch_bounds__(256) void copy_rows_kernel(Rows A, Rows B, int K, i
         R = B;
     }
     if (row >= R.rows) return;
-    const int8_t* from = R.from + row * R.stride;
+    const int8_t *from = R.from + row * R.stride, *end = R.from + (R.rows - 1) * R.stride + K;
     i32x4* to = reinterpret_cast<i32x4*>(R.to + row * units * 16);
     const int u0 = blockIdx.y * 256 + (threadIdx.x & 63);
     i32x4 v[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-        if ((u0 + c * 64) * 16 + 16 <= K) __builtin_memcpy(&v[c], from + (u0 + c * 64) * 16, 16);
+        if ((u0 + c * 64) * 16 + 16 <= K) v[c] = load_any(from + (u0 + c * 64) * 16, R.from, end);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
         const int u = u0 + c * 64;

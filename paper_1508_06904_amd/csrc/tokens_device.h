@@ -292,6 +292,26 @@ __device__ __forceinline__ void store_outputs(const Layer& L, int64_t i, int64_t
     }
 }
 
+// 16 bytes from any address, out of five aligned words: a 16-byte load that starts inside a word
+// takes several times as long.  Where one of the words would leave [begin, end) the load is that one.
+__device__ __forceinline__ i32x4 load_any(const int8_t* p, const int8_t* begin, const int8_t* end) {
+    i32x4 v;
+    const int shift = (int)((uintptr_t)p & 3);
+    const int8_t* q = p - shift;
+    if (q < begin || q + 20 > end) {
+        __builtin_memcpy(&v, p, 16);
+        return v;
+    }
+    using words = __attribute__((ext_vector_type(4), aligned(4))) int;
+    const words w = *reinterpret_cast<const words*>(q);
+    const int last = *reinterpret_cast<const int*>(q + 16);
+    v[0] = __builtin_amdgcn_alignbyte(w[1], w[0], shift);
+    v[1] = __builtin_amdgcn_alignbyte(w[2], w[1], shift);
+    v[2] = __builtin_amdgcn_alignbyte(w[3], w[2], shift);
+    v[3] = __builtin_amdgcn_alignbyte(last, w[3], shift);
+    return v;
+}
+
 // Bytes k .. k+15 of a row of K bytes, zeros past its end; nothing past the end is read.
 __device__ __forceinline__ i32x4 load_unit(const int8_t* row, int k, int K) {
     i32x4 v = {};
