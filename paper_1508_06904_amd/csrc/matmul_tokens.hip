@@ -265,8 +265,9 @@ bool whole_units(const int8_t* p, int64_t stride, int64_t rows, int K) {
     return K % 16 == 0 && (uintptr_t)p % 16 == 0 && (stride % 16 == 0 || rows == 1);
 }
 
-// The codes' row length in a workspace: whole 16-byte units.
-int padded_k(int K) { return (K + 15) / 16 * 16; }
+// The codes' row length in a workspace: whole 16-byte units, and of long rows whole lines
+// (1777 x 1003 x 2305: 14.4 us on the tiles then, 15.7 with rows of 2320).
+int padded_k(int K) { return K >= 1024 ? (K + 127) / 128 * 128 : (K + 15) / 16 * 16; }
 
 int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
 
@@ -303,7 +304,7 @@ hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, bool padded, char*
         }
         if (copy_c) S.codes = copies, S.codes_stride = Kp;
         if (copy_w) S.weight = W.to, S.weight_stride = Kp;
-        S.K = Kp;
+        S.K = (L.K + 15) / 16 * 16;      // (rows that are no copies have no more to read)
         const hipError_t e = out_dtype == DSS_BF16 ? run_product<uint16_t>(S, s) : run_product<float>(S, s);
         if (e != hipSuccess) return e;
     }
