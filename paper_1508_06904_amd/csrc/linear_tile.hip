@@ -5,7 +5,9 @@
 // they are written to and read back from memory, a byte each way beside the 4 (or
 // 2) of a value.  In exchange every workgroup reads all weights, from L2; that
 // stays below the codes' traffic while the weights are few (linear_in_tiles).
-// Bound by memory: the values in, the outputs out.
+// Bound by memory: the values in, the outputs out.  1.88 million tokens of 512 channels to 128 in
+// binary32, map in and map out: 1.13 to 1.20 ms, 4.0 to 4.2 TB/s; at a large copy's 5.07 TB/s
+// it would be 0.95.  The difference is the outputs' rows, which end inside lines there.
 #include <algorithm>
 
 #include "dev_common.h"
