@@ -476,7 +476,8 @@ typedef enum dss_token_source {
 } dss_token_source;
 
 /* Workspace bytes of a layer on M tokens of K channels with N outputs, whatever the
- * other strides (host only). */
+ * other strides (host only).  Errors: DSS_E_INVALID (sizes out of range, unknown
+ * source, NULL workspace_bytes), DSS_E_UNSUPPORTED (K > 131071, as the layers). */
 dss_status dss_tokens_workspace(int64_t M, int32_t N, int32_t K, dss_token_source source, int64_t* workspace_bytes);
 
 /* The layer on tokens that are already codes.

@@ -320,6 +320,10 @@ hipError_t launch_matmul(const Layer& L, dss_dtype out_dtype, bool padded, char*
 constexpr int kMaxK = 131071;
 constexpr int kMaxN = 1 << 20;
 
+dss_status refuse_k(int32_t K) {
+    return fail(DSS_E_UNSUPPORTED, "a sum of %d products of 8-bit codes may leave 32 bits (at most %d)", K, kMaxK);
+}
+
 // Checks of what dss_matmul_tokens and dss_linear_tokens share.
 dss_status check_layer(int64_t M, const int8_t* weight, int64_t weight_stride, const float* weight_scales, int32_t N,
                        int32_t K, const float* bias, dss_act act, const void* out, dss_dtype out_dtype,
@@ -329,8 +333,7 @@ dss_status check_layer(int64_t M, const int8_t* weight, int64_t weight_stride, c
         return fail(DSS_E_INVALID, "unknown activation %d", act);
     if (M < 0 || M > kMaxTokens || N < 1 || N > kMaxN || K < 1)
         return fail(DSS_E_INVALID, "%lld tokens of %d channels, %d outputs", (long long)M, K, N);
-    if (K > kMaxK)
-        return fail(DSS_E_UNSUPPORTED, "a sum of %d products of 8-bit codes may leave 32 bits (at most %d)", K, kMaxK);
+    if (K > kMaxK) return refuse_k(K);
     if (weight_stride < K) return fail(DSS_E_INVALID, "weight_stride %lld is less than %d", (long long)weight_stride, K);
     const bool rows = (out_channel_stride == 1 || N == 1) && (out_token_stride >= N || M <= 1);
     const bool map = (out_token_stride == 1 || M <= 1) && (out_channel_stride >= M || N == 1);
@@ -381,6 +384,7 @@ extern "C" dss_status dss_tokens_workspace(int64_t M, int32_t N, int32_t K, dss_
         return fail(DSS_E_INVALID, "%lld tokens of %d channels, %d outputs", (long long)M, K, N);
     if (source != DSS_TOKENS_ROWS && source != DSS_TOKENS_MAP && source != DSS_TOKENS_CODES)
         return fail(DSS_E_INVALID, "unknown token source %d", (int)source);
+    if (K > kMaxK) return refuse_k(K);   // (what follows counts a row's bytes in 32 bits, and a layer's in 64)
     *workspace_bytes = workspace_bytes_of(M, N, K, source);
     return DSS_OK;
 } catch (...) {
