@@ -82,7 +82,9 @@ __global__ __launch_bounds__(kThreads) void quantize_long_rows_kernel(const T* _
 
 // Maps of at least a tile's tokens: see MapTile.  The last tile ends with the last
 // token and leaves out what the one before it has.  Of more channels than a workgroup
-// holds the values are read twice, the second time mostly from cache.
+// holds the values are read twice, the second time mostly from cache.  Channels are
+// counted in unsigned 32 bits: K is below 2^31, and no count passes it by more than a
+// span of channels.
 template <typename T>
 __global__ __launch_bounds__(kMapWaves * 64) void quantize_map_kernel(const T* __restrict__ x, int64_t M, int K,
                                                                       int64_t channel_stride,
@@ -92,21 +94,22 @@ __global__ __launch_bounds__(kMapWaves * 64) void quantize_map_kernel(const T* _
     __shared__ uint32_t tops[kMapWaves * 64];
     const int64_t tile0 = xcd_order(blockIdx.x, gridDim.x) * Tile::kTokens, m0 = min(tile0, M - Tile::kTokens);
     const int first = (int)(tile0 - m0);
-    const int span = (int)(blockDim.x >> 6) * 64;      // channels held at once
-    const int own_k = (int)(threadIdx.x >> 4) * 16;
+    const uint32_t channels = K, channels_out = Kp;
+    const uint32_t span = (blockDim.x >> 6) * 64;      // channels held at once
+    const uint32_t own_k = (threadIdx.x >> 4) * 16;
     Tile tile;
     uint32_t top[4] = {};
-    for (int k0 = 0; k0 < K; k0 += span) {
-        tile.load(x + m0, channel_stride, k0 + own_k, K);
+    for (uint32_t k0 = 0; k0 < channels; k0 += span) {
+        tile.load(x + m0, channel_stride, k0 + own_k, channels);
         tile.raise_into(top);
     }
     Tile::meet(top, tops, 0, blockDim.x >> 6);
     const int t = (threadIdx.x & 15) * Tile::V;
-    const int rounds = (K + span - 1) / span;
+    const int rounds = (int)((channels + span - 1) / span);
     for (int round = rounds - 1; round >= 0; --round) {
         // (the last span is still there)
-        const int k = round * span + own_k;
-        if (round != rounds - 1) tile.load(x + m0, channel_stride, k, K);
+        const uint32_t k = round * span + own_k;
+        if (round != rounds - 1) tile.load(x + m0, channel_stride, k, channels);
 #pragma unroll
         for (int j = 0; j < Tile::V; ++j) {
             const Coder coder(scale_of(Tile::bits(top, j)));
@@ -115,12 +118,12 @@ __global__ __launch_bounds__(kMapWaves * 64) void quantize_map_kernel(const T* _
             uint32_t w[4];
             tile.codes(j, coder, w);
             int8_t* p = codes + (m0 + t + j) * codes_stride + k;
-            if (k + 16 <= Kp) {
+            if (k + 16 <= channels_out) {
                 __builtin_memcpy(p, w, 16);
             } else {
 #pragma unroll
                 for (int b = 0; b < 16; ++b)
-                    if (k + b < Kp) p[b] = (int8_t)(w[b / 4] >> (8 * (b % 4)));
+                    if (k + b < channels_out) p[b] = (int8_t)(w[b / 4] >> (8 * (b % 4)));
             }
         }
     }
@@ -134,10 +137,10 @@ __global__ __launch_bounds__(kThreads) void quantize_narrow_map_kernel(const T* 
                                                                        int Kp, float* __restrict__ scales) {
     const int64_t m = blockIdx.x;
     uint32_t top = 0;
-    for (int k = threadIdx.x; k < K; k += kThreads) top = max(top, abs_bits(to_f32(x[m + k * channel_stride])));
+    for (int64_t k = threadIdx.x; k < K; k += kThreads) top = max(top, abs_bits(to_f32(x[m + k * channel_stride])));
     const Coder coder(scale_of(row_max<kThreads>(top)));
     if (threadIdx.x == 0) scales[m] = coder.scale;
-    for (int k = threadIdx.x; k < Kp; k += kThreads)
+    for (int64_t k = threadIdx.x; k < Kp; k += kThreads)
         codes[m * codes_stride + k] = k < K ? coder.one(to_f32(x[m + k * channel_stride])) : 0;
 }
 
@@ -156,7 +159,7 @@ void run_quantize(const T* x, int64_t M, int K, int64_t ts, int64_t ks, int8_t* 
             quantize_narrow_map_kernel<T><<<dim3((unsigned)M), kThreads, 0, s>>>(x, K, ks, codes, cs, Kp, scales);
             return;
         }
-        const int waves = std::min<int>((K + 63) / 64, kMapWaves);
+        const int waves = (int)std::min<int64_t>(((int64_t)K + 63) / 64, kMapWaves);
         quantize_map_kernel<T><<<dim3((unsigned)ceil_div64(M, MapTile<T>::kTokens)), waves * 64, 0, s>>>(x, M, K, ks, codes,
                                                                                                       cs, Kp, scales);
         return;

@@ -170,7 +170,7 @@ struct MapTile {
     Chunk<T> c[16];                                    // c[r].value(j): channel r of the lane's group, token j
 
     // The tile's tokens start at x; the lane's channels k .. k+15, those below K.
-    __device__ __forceinline__ void load(const T* x, int64_t channel_stride, int k, int K) {
+    __device__ __forceinline__ void load(const T* x, int64_t channel_stride, uint32_t k, uint32_t K) {
         const T* p = x + (threadIdx.x & 15) * V + k * channel_stride;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {

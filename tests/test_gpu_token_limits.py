@@ -1,0 +1,39 @@
+"""8-bit tokens and clipped gradients at the ends of their ranges: the most channels, the smallest factors, and
+the parts of the products that ordinary sizes do not reach."""
+import numpy as np
+import pytest
+
+from oracle import tokens
+from paper_1508_06904_amd import dss
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    dss.lib()
+    yield
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+
+# ---------------------------------------------------------------------------- channels up to 2^31 - 1
+
+@pytest.mark.parametrize("M,K,dtype", [(1, 2 ** 31 - 1, "f32"), (1, 2 ** 31 - 256, "f32"), (2, 2 ** 31 - 1, "bf16"),
+                                       (64, 2 ** 31 - 1, "f32")])
+def test_channels_up_to_the_largest_count(M, K, dtype):
+    """A token's value repeated over all of its channels (a stride of 0): every code is 127 or -127."""
+    import torch
+    if torch.cuda.mem_get_info()[0] < 1.2 * M * K:
+        pytest.skip("the codes do not fit the free memory")
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    values = torch.linspace(-3, 5, M).add(0.125).to("cuda").to(dt)
+    codes = torch.full((M, K), 55, dtype=torch.int8, device="cuda")
+    _, scales = dss.quantize_tokens(values[:, None].expand(M, K), codes=codes)
+    want, wsc = tokens.quantize(values[:, None].float().cpu().numpy())
+    assert np.array_equal(scales.cpu().numpy(), wsc)
+    want = torch.from_numpy(want).to("cuda")
+    for k in range(0, K, 1 << 27):
+        assert bool((codes[:, k:k + (1 << 27)] == want).all()), k
