@@ -24,12 +24,15 @@ constexpr int kMaxChannels = kMapWaves * 64;       // of a token in registers, a
 // A token's codes in LDS: whole matrix operands of 64, and 16 bytes more, so that tokens start in different banks.
 __host__ __device__ constexpr int tile_pitch(int K) { return (K + 63) / 64 * 64 + 16; }
 
+// A workgroup's LDS: its tokens' codes and scales, and 64 words for each wave's largest values.  All of it is
+// in the launch's own size, whose opt-in above 64 KB knows of no other.
+size_t tile_lds(int tokens, int K, int waves) { return (size_t)tokens * (tile_pitch(K) + 4) + waves * 256; }
+
 // Codes and scales of the tokens of a map from x on: tiles beside each other, `waves` waves for each.
 template <typename T>
 __device__ __forceinline__ void code_map(const T* x, int64_t channel_stride, int K, int waves, int pitch, int8_t* codes,
-                                         float* scales) {
+                                         float* scales, uint32_t* tops) {
     using Tile = MapTile<T>;
-    __shared__ uint32_t tops[kMapWaves * 64];
     const int wave = threadIdx.x >> 6, group = wave / waves, k = (wave - group * waves) * 64 + ((threadIdx.x >> 4) & 3) * 16;
     const int t = group * Tile::kTokens + (threadIdx.x & 15) * Tile::V;
     Tile tile;
@@ -56,7 +59,8 @@ __global__ __launch_bounds__(kMapWaves * 64) void linear_tile_kernel(Layer L, Va
     float* scales = reinterpret_cast<float*>(lds + tokens * pitch);
     const int64_t tile0 = xcd_order(blockIdx.x, gridDim.x) * tokens, m0 = min(tile0, L.M - tokens);
     const int first = (int)(tile0 - m0);
-    code_map(static_cast<const T*>(V.x) + m0, V.channel_stride, K, waves, pitch, lds, scales);
+    code_map(static_cast<const T*>(V.x) + m0, V.channel_stride, K, waves, pitch, lds, scales,
+             reinterpret_cast<uint32_t*>(scales + tokens));
     __syncthreads();
 
     // 16 outputs of 64 tokens at a time for a wave
@@ -107,7 +111,7 @@ __global__ __launch_bounds__(kMapWaves * 64) void linear_tile_kernel(Layer L, Va
 template <typename T, typename Tout>
 hipError_t run_linear(const Layer& L, const Values& V, hipStream_t s) {
     const int waves = (L.K + 63) / 64, groups = std::max(1, 8 / waves), tokens = groups * MapTile<T>::kTokens;
-    const size_t lds = (size_t)tokens * (tile_pitch(L.K) + 4);
+    const size_t lds = tile_lds(tokens, L.K, waves * groups);
     const auto kern = L.map ? linear_tile_kernel<T, Tout, true> : linear_tile_kernel<T, Tout, false>;
     const hipError_t e = allow_dynamic_lds((const void*)kern, lds);
     if (e != hipSuccess) return e;

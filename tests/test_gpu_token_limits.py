@@ -37,3 +37,30 @@ def test_channels_up_to_the_largest_count(M, K, dtype):
     want = torch.from_numpy(want).to("cuda")
     for k in range(0, K, 1 << 27):
         assert bool((codes[:, k:k + (1 << 27)] == want).all()), k
+
+
+# ---------------------------------------------------------------------------- products
+
+def _dev(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).to("cuda")
+
+
+def _weights(N, K, seed=0):
+    rng = np.random.default_rng([seed, N, K, 1])
+    return (_dev(rng.integers(-127, 128, (N, K)).astype(np.int8)), _dev((rng.random(N) * 0.02).astype(np.float32)),
+            _dev(rng.standard_normal(N).astype(np.float32)))
+
+
+@pytest.mark.parametrize("planar", [False, True])
+@pytest.mark.parametrize("K,dtype", [(896, "f32"), (897, "f32"), (930, "f32"), (960, "f32"), (961, "f32"), (930, "bf16")])
+def test_layers_of_maps_around_64_kb_of_lds(K, dtype, planar):
+    """Coded and multiplied in one launch, the same bits as in two: binary32 tokens of 897 to 960 channels need
+    just over 64 KB of LDS with the room for the largest values."""
+    import torch
+    M, N = 4200, 40
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    x = torch.randn((K, M), generator=gen, device="cuda").to(torch.float32 if dtype == "f32" else torch.bfloat16).t()
+    w, ws, bias = _weights(N, K)
+    got = dss.linear_i8(x, w, ws, bias=bias, act="relu", planar=planar)
+    assert torch.equal(got, dss.matmul_i8(*dss.quantize_tokens(x), w, ws, bias=bias, act="relu", planar=planar))
