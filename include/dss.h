@@ -431,12 +431,14 @@ dss_status dss_grad_norm(const dss_tensor* grads, int32_t n, float* norm, void* 
 /* The norm, and the gradient scaled down to at most max_norm:
  *   out[t][i] = min(1, max_norm / (norm + 1e-6)) * grads[t].data[i],
  * formed in binary32 and rounded once to the tensor's type.  With an infinite
- * norm the factor is 0 (an infinite element becomes NaN), with a NaN one it is
- * NaN.
+ * element the factor is 0 (that element becomes NaN), with a NaN it is NaN.  A norm
+ * of finite elements that binary32 cannot hold is written as infinite; the factor
+ * is formed from the norm itself.
  *   out        host array of n device pointers, out[t] for grads[t].count elements
  *              of its type; out[t] == grads[t].data clips in place, and no other
  *              overlap is allowed
- *   max_norm   >= 0; may be infinite (nothing is clipped)
+ *   max_norm   >= 0; may be infinite: then the factor is 1, also with infinite
+ *              elements (with a NaN it is NaN as ever)
  * Other arguments and errors as dss_grad_norm. */
 dss_status dss_clip_grads(const dss_tensor* grads, void* const* out, int32_t n, float max_norm, float* norm,
                           void* workspace, int64_t workspace_bytes, hipStream_t stream);

@@ -45,5 +45,6 @@ def clip(grads, max_norm):
     norm = grad_norm(grads)
     with np.errstate(all="ignore"):
         c = np.float64(max_norm) / np.float64(norm + 1e-6)
-        c = 1.0 if c >= 1.0 else c
+        # an infinite bound clips nothing, infinite elements included; a NaN norm stays one
+        c = 1.0 if c >= 1.0 or (np.isinf(max_norm) and not np.isnan(norm)) else c
         return norm, [np.asarray(g, dtype=np.float64) * c for g in grads]

@@ -150,8 +150,10 @@ __global__ __launch_bounds__(kThreads) void norm_total_kernel(const double* part
     if (threadIdx.x == 0) *norm = (float)v;
 }
 
-// min(1, b / (norm + 1e-6)); a NaN stays one, an infinite norm gives 0.
+// min(1, b / (norm + 1e-6)); a NaN norm stays one, an infinite norm gives 0.  An infinite
+// bound clips nothing, an infinite norm's values included.
 __device__ __forceinline__ float coefficient(double norm, float max_norm) {
+    if (isinf(max_norm) && !isnan(norm)) return 1.f;
     const double c = (double)max_norm / (norm + 1e-6);
     return c >= 1.0 ? 1.f : (float)c;
 }

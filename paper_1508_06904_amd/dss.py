@@ -606,7 +606,8 @@ def grad_norm(grads, norm=None, workspace=None, stream=None):
 
 
 def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
-    """Scales a gradient, given as for grad_norm, by min(1, max_norm / (norm + 1e-6)).
+    """Scales a gradient, given as for grad_norm, by min(1, max_norm / (norm + 1e-6)); max_norm may be
+    infinite (nothing is clipped unless the norm is NaN).
     Returns (norm, list of scaled tensors).  `out` is the list of tensors to write (allocated if
     None; `out=grads` clips in place): of the same types and numbers of elements, and of the same
     shapes and strides unless all tensors are contiguous."""

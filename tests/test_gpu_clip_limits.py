@@ -1,0 +1,56 @@
+"""Gradient clipping at the ends of its ranges: bounds and norms that are infinite, factors that binary32 cannot
+hold with all of its bits, lists of every kernel."""
+import numpy as np
+import pytest
+
+from oracle import tokens
+from paper_1508_06904_amd import dss
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+LISTS = {"one launch": [700, 0, 33], "runs": [70_000, 4097, 1], "tables": [300] * 130 + [9000]}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    dss.lib()
+    yield
+    torch.cuda.synchronize()
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy()
+
+
+def _grads(sizes, dtype, scale=1.0, seed=0):
+    import torch
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    rng = np.random.default_rng(seed)
+    return [torch.from_numpy((rng.standard_normal(s) * scale).astype(np.float32)).to("cuda").to(dt) for s in sizes]
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan"), None])
+@pytest.mark.parametrize("name", LISTS)
+def test_an_infinite_bound_clips_nothing(name, bad, dtype, in_place):
+    import torch
+    grads = _grads(LISTS[name], dtype)
+    if bad is not None:
+        grads[-1][-1] = bad
+    before = [g.clone() for g in grads]
+    norm, out = dss.clip_grads(grads, float("inf"), out=grads if in_place else None)
+    want, ref = tokens.clip([_np(g) for g in before], float("inf"))
+    if bad is None:
+        assert abs(float(norm) - want) <= 1.01 * U * want
+    else:
+        assert np.array_equal(np.float64(float(norm)), np.float64(want), equal_nan=True)
+    for o, g, r in zip(out, before, ref):
+        assert np.array_equal(_np(o), r, equal_nan=True)
+        if bad != bad and g.numel():
+            assert bool(torch.isnan(o).all())
+        elif bad == bad:
+            assert torch.equal(o, g)
