@@ -150,17 +150,30 @@ __global__ __launch_bounds__(kThreads) void norm_total_kernel(const double* part
     if (threadIdx.x == 0) *norm = (float)v;
 }
 
+// The factor c * 2^e of a value.  e is 0 except for factors below the normal binary32
+// numbers, whose last bits (or all) c alone would lose: 1e25 clipped to a norm of 1e-25.
+struct Factor {
+    float c;
+    int e;
+    __device__ __forceinline__ float of(float v) const { return ldexpf(v * c, e); }
+    __device__ __forceinline__ bool is_one() const { return c == 1.f && e == 0; }
+};
+
 // min(1, b / (norm + 1e-6)); a NaN norm stays one, an infinite norm gives 0.  An infinite
 // bound clips nothing, an infinite norm's values included.
-__device__ __forceinline__ float coefficient(double norm, float max_norm) {
-    if (isinf(max_norm) && !isnan(norm)) return 1.f;
+__device__ __forceinline__ Factor factor_of(double norm, float max_norm) {
+    if (isinf(max_norm) && !isnan(norm)) return {1.f, 0};
     const double c = (double)max_norm / (norm + 1e-6);
-    return c >= 1.0 ? 1.f : (float)c;
+    if (c >= 1.0) return {1.f, 0};
+    if (!(c > 0 && c < 0x1p-126)) return {(float)c, 0};
+    int e;
+    const double m = frexp(c, &e);
+    return {(float)m, e};
 }
 
 // Values (LOAD) and outputs (STORE) around the caches or through them.
 template <bool LOAD, bool STORE, typename T>
-__device__ __forceinline__ void scale_run(const T* p, T* q, int64_t n, float c) {
+__device__ __forceinline__ void scale_run(const T* p, T* q, int64_t n, const Factor& f) {
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int U = 4;
     int64_t i = (int64_t)threadIdx.x * V;
@@ -171,12 +184,12 @@ __device__ __forceinline__ void scale_run(const T* p, T* q, int64_t n, float c) 
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int k = 0; k < V; ++k) store_elem(&x[u].v[k], to_f32(x[u].v[k]) * c);
+            for (int k = 0; k < V; ++k) store_elem(&x[u].v[k], f.of(to_f32(x[u].v[k])));
             store16<STORE>(q + i + (int64_t)u * kThreads * V, x[u]);
         }
     }
     for (; i < n; i += (int64_t)kThreads * V)
-        for (int k = 0; k < V && i + k < n; ++k) store_elem(&q[i + k], to_f32(p[i + k]) * c);
+        for (int k = 0; k < V && i + k < n; ++k) store_elem(&q[i + k], f.of(to_f32(p[i + k])));
 }
 
 template <int CAP, bool LOAD, bool STORE>
@@ -184,14 +197,14 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(TensorTable<CAP> t, cons
                                                         float max_norm, float* norm) {
     const double total = norm_of(partial, groups);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)total;
-    const float c = coefficient(total, max_norm);
+    const Factor f = factor_of(total, max_norm);
     for (int r = blockIdx.x; r < t.runs; r += gridDim.x) {
         const int k = find_tensor(t, r);
-        if (c == 1.f && t.in[k] == t.out[k]) continue;   // in place, nothing to clip
+        if (f.is_one() && t.in[k] == t.out[k]) continue;   // in place, nothing to clip
         const int64_t at = (int64_t)(r - t.first[k]) << t.run_shift;
         const int64_t n = min(t.count[k] - at, (int64_t)1 << t.run_shift);
-        if (t.dtype[k] == DSS_BF16) scale_run<LOAD, STORE>((const uint16_t*)t.in[k] + at, (uint16_t*)t.out[k] + at, n, c);
-        else scale_run<LOAD, STORE>((const float*)t.in[k] + at, (float*)t.out[k] + at, n, c);
+        if (t.dtype[k] == DSS_BF16) scale_run<LOAD, STORE>((const uint16_t*)t.in[k] + at, (uint16_t*)t.out[k] + at, n, f);
+        else scale_run<LOAD, STORE>((const float*)t.in[k] + at, (float*)t.out[k] + at, n, f);
     }
 }
 
@@ -224,14 +237,14 @@ __device__ __forceinline__ double short_squares(const T* p, int n, double s) {
 }
 
 template <typename T>
-__device__ __forceinline__ void short_scale(const T* p, T* q, int n, float c) {
+__device__ __forceinline__ void short_scale(const T* p, T* q, int n, const Factor& f) {
     const int lane = threadIdx.x & 63;
     float v[kShortRun / 64];
 #pragma unroll
     for (int k = 0; k < kShortRun / 64; ++k) v[k] = k * 64 + lane < n ? to_f32(p[k * 64 + lane]) : 0.f;
 #pragma unroll
     for (int k = 0; k < kShortRun / 64; ++k)
-        if (k * 64 + lane < n) store_elem(&q[k * 64 + lane], v[k] * c);
+        if (k * 64 + lane < n) store_elem(&q[k * 64 + lane], f.of(v[k]));
 }
 
 __global__ __launch_bounds__(kShortWaves * 64) void clip_short_kernel(ShortTable t, float max_norm, int clip,
@@ -264,16 +277,16 @@ __global__ __launch_bounds__(kShortWaves * 64) void clip_short_kernel(ShortTable
     const double total = sqrt(s);
     if (threadIdx.x == 0) *norm = (float)total;
     if (!clip) return;
-    const float c = coefficient(total, max_norm);
+    const Factor f = factor_of(total, max_norm);
 #pragma unroll
     for (int u = 0; u < kShortRuns / kShortWaves; ++u) {
         if (left[u] == 0) continue;
         const int k = who[u];
-        if (c == 1.f && t.in[k] == t.out[k]) continue;
+        if (f.is_one() && t.in[k] == t.out[k]) continue;
         if (t.dtype[k] == DSS_BF16)
-            short_scale((const uint16_t*)t.in[k] + at[u], (uint16_t*)t.out[k] + at[u], left[u], c);
+            short_scale((const uint16_t*)t.in[k] + at[u], (uint16_t*)t.out[k] + at[u], left[u], f);
         else
-            short_scale((const float*)t.in[k] + at[u], (float*)t.out[k] + at[u], left[u], c);
+            short_scale((const float*)t.in[k] + at[u], (float*)t.out[k] + at[u], left[u], f);
     }
 }
 

@@ -54,3 +54,19 @@ def test_an_infinite_bound_clips_nothing(name, bad, dtype, in_place):
             assert bool(torch.isnan(o).all())
         elif bad == bad:
             assert torch.equal(o, g)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale,bound", [(1e5, 1e-35), (1e20, 1e-20), (1e25, 1e-25), (1e37, 1e-37), (1e37, 1e-44), (1e-3, 1e-42),
+                                         (1e30, 1e-7), (1e3, 1e-36)])
+@pytest.mark.parametrize("name", LISTS)
+def test_factors_below_the_normal_numbers(name, scale, bound, dtype):
+    """The factor bound / norm loses its bits in binary32 where the clipped values need not.  Rounding: the factor and
+    the product 2 * 2^-24 of the value; near the smallest numbers the product is rounded once more, to half of
+    the smallest one, and one of them covers that; bfloat16 as in every clipping."""
+    grads = _grads(LISTS[name], dtype, scale)
+    _, out = dss.clip_grads(grads, bound)
+    ref = tokens.clip([_np(g) for g in grads], np.float32(bound))[1]
+    rel = 2.02 * U + (2.0 ** -8 if dtype == "bf16" else 0)
+    for o, r in zip(out, ref):
+        assert np.all(np.abs(_np(o) - r) <= rel * np.abs(r) + (2.0 ** -133 if dtype == "bf16" else 2.0 ** -149))
