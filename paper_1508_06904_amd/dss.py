@@ -569,29 +569,43 @@ def _is_dense(t):
     return True
 
 
-def _tensor_list(tensors, what, dev):
+def _tensor_list(tensors, what, dev, like=None):
     """The C list of CUDA tensors (dss_tensor[n]: address, count, dtype and a zero, as three 64-bit
-    words each), the tensors as a list, and whether all of them are contiguous."""
+    words each), the tensors as a list, and whether all of them are contiguous.  `like` is such a
+    result for other tensors, whose types, shapes and (unless all are contiguous) strides these have
+    to have."""
     import torch
     T = torch.Tensor
     if isinstance(tensors, T):
         raise ValueError("%s must be a list of tensors" % what)
     codes, tensors = _dtype_codes(), list(tensors)
     n = len(tensors)
-    if not all([isinstance(t, T) for t in tensors]):
-        raise ValueError("%s must be a list of tensors" % what)
-    if n and any(d != dev for d in set(map(T.get_device, tensors))):
+    try:
+        devices = set(map(T.get_device, tensors))
+    except TypeError:
+        raise ValueError("%s must be a list of tensors" % what) from None
+    if devices - {dev}:
         raise ValueError("%s must be on the current CUDA device, %d" % (what, dev))
     dtypes = [codes.get(t.dtype, -1) for t in tensors]
     if -1 in dtypes:
         raise ValueError("%s must be float32 or bfloat16 (got %s)" % (what, tensors[dtypes.index(-1)].dtype))
+    dtypes = array.array("q", dtypes)
     plain = all(map(T.is_contiguous, tensors))
     if not plain and not all([t.is_contiguous() or _is_dense(t) for t in tensors]):
         raise ValueError("%s must be dense in memory, without gaps or repeated elements" % what)
+    if like is None:
+        counts = array.array("q", map(T.numel, tensors))
+    else:
+        words, others, others_plain = like
+        if dtypes != words[2::3] or not all(map(T.is_same_size, tensors, others)) or not (plain and others_plain) and \
+                list(map(T.stride, tensors)) != list(map(T.stride, others)):
+            raise ValueError("%s must be of the gradients' number, types and shapes, and unless all are contiguous of "
+                             "their strides" % what)
+        counts = words[1::3]
     words = array.array("q", bytes(24 * n))
     words[0::3] = array.array("q", map(T.data_ptr, tensors))
-    words[1::3] = array.array("q", map(T.numel, tensors))
-    words[2::3] = array.array("q", dtypes)
+    words[1::3] = counts
+    words[2::3] = dtypes
     return words, tensors, plain
 
 
@@ -609,8 +623,8 @@ def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None
     """Scales a gradient, given as for grad_norm, by min(1, max_norm / (norm + 1e-6)); max_norm may be
     infinite (nothing is clipped unless the norm is NaN).
     Returns (norm, list of scaled tensors).  `out` is the list of tensors to write (allocated if
-    None; `out=grads` clips in place): of the same types and numbers of elements, and of the same
-    shapes and strides unless all tensors are contiguous."""
+    None; `out=grads` clips in place): of the same types and shapes, and of the same strides unless
+    all tensors are contiguous."""
     import torch
     dev, handle = _launch(stream)
     in_place = out is grads
@@ -624,11 +638,7 @@ def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None
             else:
                 with torch.cuda.stream(stream):
                     out = [torch.empty_like(g) for g in grads]
-        b, out, plain_out = _tensor_list(out, "out", dev)
-        if b[1::3] != a[1::3] or b[2::3] != a[2::3] or not (plain and plain_out) and \
-                [(o.shape, o.stride()) for o in out] != [(g.shape, g.stride()) for g in grads]:
-            raise ValueError("out must be of grads' types and sizes, and unless all are contiguous of their shapes "
-                             "and strides")
+        b, out, _ = _tensor_list(out, "out", dev, (a, grads, plain))
     norm, wp, wb, keep = _norm_buffers(norm, workspace, dev, stream)
     ptrs = b[0::3]
     _check(lib().dss_clip_grads(a.buffer_info()[0], ptrs.buffer_info()[0], len(grads), max_norm, norm.data_ptr(), wp, wb,

@@ -70,3 +70,25 @@ def test_factors_below_the_normal_numbers(name, scale, bound, dtype):
     rel = 2.02 * U + (2.0 ** -8 if dtype == "bf16" else 0)
     for o, r in zip(out, ref):
         assert np.all(np.abs(_np(o) - r) <= rel * np.abs(r) + (2.0 ** -133 if dtype == "bf16" else 2.0 ** -149))
+
+
+def test_outputs_of_other_shapes_are_refused():
+    """As many elements are not enough: a contiguous output of another shape would be filled in another order."""
+    import torch
+    grads = _grads([(8, 6), 5], "f32")
+    make = lambda *shapes: [torch.full(s, -7.0, device="cuda") for s in shapes]  # noqa: E731
+    for shapes in [((6, 8), (5,)), ((48,), (5,)), ((8, 6), (5, 1)), ((8, 6, 1), (5,)), ((5,), (8, 6)), ((8, 6),)]:
+        out = make(*shapes)
+        with pytest.raises(ValueError):
+            dss.clip_grads(grads, 1.0, out=out)
+        assert all(bool((o == -7).all()) for o in out)
+    # other strides: refused unless all tensors are contiguous
+    with pytest.raises(ValueError):
+        dss.clip_grads([grads[0].t(), grads[1]], 1.0, out=make((6, 8), (5,)))
+    out = make((8, 6), (5,))
+    dss.clip_grads(grads, 1.0, out=out)
+    dss.clip_grads([grads[0].t(), grads[1]], 1.0, out=[out[0].t(), out[1]])
+    with pytest.raises(ValueError):
+        dss.clip_grads([grads[0], 2.0], 1.0)
+    with pytest.raises(ValueError):
+        dss.clip_grads(grads, 1.0, out=[None, None])
