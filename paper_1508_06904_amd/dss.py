@@ -586,10 +586,10 @@ def _tensor_list(tensors, what, dev, like=None):
         raise ValueError("%s must be a list of tensors" % what) from None
     if devices - {dev}:
         raise ValueError("%s must be on the current CUDA device, %d" % (what, dev))
-    dtypes = [codes.get(t.dtype, -1) for t in tensors]
-    if -1 in dtypes:
-        raise ValueError("%s must be float32 or bfloat16 (got %s)" % (what, tensors[dtypes.index(-1)].dtype))
-    dtypes = array.array("q", dtypes)
+    kinds = set(map(T.dtype.__get__, tensors))
+    if not kinds <= codes.keys():
+        raise ValueError("%s must be float32 or bfloat16 (got %s)" % (what, (kinds - codes.keys()).pop()))
+    dtypes = array.array("q", [codes[k] for k in kinds] * n if len(kinds) == 1 else [codes[t.dtype] for t in tensors])
     plain = all(map(T.is_contiguous, tensors))
     if not plain and not all([t.is_contiguous() or _is_dense(t) for t in tensors]):
         raise ValueError("%s must be dense in memory, without gaps or repeated elements" % what)
@@ -624,7 +624,8 @@ def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None
     infinite (nothing is clipped unless the norm is NaN).
     Returns (norm, list of scaled tensors).  `out` is the list of tensors to write (allocated if
     None; `out=grads` clips in place): of the same types and shapes, and of the same strides unless
-    all tensors are contiguous."""
+    all tensors are contiguous.  An output shares no memory with another one (so that no tensor can be
+    clipped in place twice) or with another tensor's gradient."""
     import torch
     dev, handle = _launch(stream)
     in_place = out is grads
@@ -641,6 +642,9 @@ def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None
         b, out, _ = _tensor_list(out, "out", dev, (a, grads, plain))
     norm, wp, wb, keep = _norm_buffers(norm, workspace, dev, stream)
     ptrs = b[0::3]
+    # (an empty tensor's address is 0)
+    if len(set(ptrs)) != len(ptrs) - max(ptrs.count(0) - 1, 0):
+        raise ValueError("out must not have the same tensor twice")
     _check(lib().dss_clip_grads(a.buffer_info()[0], ptrs.buffer_info()[0], len(grads), max_norm, norm.data_ptr(), wp, wb,
                                 handle), "dss_clip_grads")
     return norm, out

@@ -92,3 +92,21 @@ def test_outputs_of_other_shapes_are_refused():
         dss.clip_grads([grads[0], 2.0], 1.0)
     with pytest.raises(ValueError):
         dss.clip_grads(grads, 1.0, out=[None, None])
+
+
+def test_a_tensor_is_written_once():
+    """Two entries of one list that write the same memory would race: scaled once, or twice.  Reading one twice is
+    no matter, nor are any number of empty tensors."""
+    import torch
+    a, b, empty = _grads([5000, 40, 0], "f32")
+    before = a.clone()
+    for grads, out in (([a, a], "in place"), ([a, b, a], "in place"), ([a, a], [b.new_empty(5000)] * 2),
+                       ([a, empty, a, empty], [a, empty, a, empty])):
+        with pytest.raises(ValueError):
+            dss.clip_grads(grads, 0.5, out=grads if out == "in place" else out)
+        assert torch.equal(a, before)
+    norm, out = dss.clip_grads([a, a, empty, empty], 0.5)
+    want, ref = tokens.clip([_np(a), _np(a)], 0.5)
+    assert abs(float(norm) - want) <= 1.01 * U * want and torch.equal(out[0], out[1])
+    assert np.all(np.abs(_np(out[0]) - ref[0]) <= 2.02 * U * np.abs(ref[0]) + 2.0 ** -149)
+    dss.clip_grads([empty, a, empty], 0.5, out=[empty, a, empty])
