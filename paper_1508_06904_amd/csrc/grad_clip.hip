@@ -375,7 +375,7 @@ dss_status run_tables(const dss_tensor* grads, void* const* out, int32_t n, bool
 dss_status grad_common(const dss_tensor* grads, void* const* out, int32_t n, bool clip, float max_norm, float* norm,
                        void* workspace, int64_t workspace_bytes, hipStream_t stream) {
     if (n < 0 || (n > 0 && !grads)) return fail(DSS_E_INVALID, "%d tensors, NULL list or not", n);
-    if (!norm) return fail(DSS_E_INVALID, "NULL norm");
+    if (!norm || (uintptr_t)norm % 4 != 0) return fail(DSS_E_INVALID, "norm is NULL or not aligned to its elements");
     if (clip && n > 0 && !out) return fail(DSS_E_INVALID, "NULL list of outputs");
     if (clip && !(max_norm >= 0.f)) return fail(DSS_E_INVALID, "max_norm %g is negative or not a number", max_norm);
     int64_t total = 0;

@@ -29,3 +29,11 @@ def test_workspace_of_the_largest_layer(source):
     assert dss.lib().dss_tokens_workspace(2 ** 40, 2 ** 20, MAX_K, source, ctypes.byref(need)) == OK
     weights = 2 ** 20 * (MAX_K + 1)
     assert need.value >= weights and need.value >= (2 ** 40 * (MAX_K + 1) if source != 2 else 0)
+
+
+def test_a_norm_between_words_is_refused():
+    VP, at = ctypes.c_void_p, 1 << 20
+    for off in (1, 2, 3):
+        assert dss.lib().dss_grad_norm(None, 0, VP(at + off), VP(at), 8192, None) == INVALID
+        assert dss.lib().dss_clip_grads(None, None, 0, 1.0, VP(at + off), VP(at), 8192, None) == INVALID
+        assert b"norm" in dss.lib().dss_last_error()
