@@ -748,6 +748,8 @@ def _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, 
         out = _empty(shape, out_dtype, stream)
     elif not isinstance(out, torch.Tensor) or out.shape != shape or out.dtype not in codes or out.get_device() != dev:
         raise ValueError("out must be a float32 or bfloat16 tensor of shape %s on the current CUDA device" % (shape,))
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise ValueError("out is %s, not out_dtype %s" % (out.dtype, out_dtype))
     s0, s1 = out.stride()
     return out, N, (wp, wstride, sp, N, K, bp, ACTS[act], out.data_ptr(), codes[out.dtype]) + \
         ((s1, s0) if planar else (s0, s1))
@@ -772,7 +774,8 @@ def matmul_i8(codes, scales, weight, weight_scales, bias=None, act="none", out=N
     with weights in 8 bits (codes [N][K], scales [N]):
       y[m][n] = act(scales[m] * weight_scales[n] * sum_k codes[m][k] * weight[n][k] + bias[n]),
     the sum exact.  act is "none", "relu" or "tanh".  Returns out, [M][N] or with planar=True the
-    dense map [N][M], of out_dtype (float32 unless given); an `out` of any row stride is taken."""
+    dense map [N][M], of out_dtype (float32, or `out`'s, unless given); an `out` of any row stride is
+    taken."""
     dev, handle = _launch(stream)
     cp, cstride = _check_codes(codes, "codes", None, None, dev)
     M, K = codes.shape

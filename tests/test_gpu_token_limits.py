@@ -64,3 +64,20 @@ def test_layers_of_maps_around_64_kb_of_lds(K, dtype, planar):
     w, ws, bias = _weights(N, K)
     got = dss.linear_i8(x, w, ws, bias=bias, act="relu", planar=planar)
     assert torch.equal(got, dss.matmul_i8(*dss.quantize_tokens(x), w, ws, bias=bias, act="relu", planar=planar))
+
+
+@pytest.mark.parametrize("planar", [False, True])
+def test_an_output_of_another_type_than_asked_for_is_refused(planar):
+    import torch
+    M, N, K = 5, 3, 8
+    x = torch.randn((M, K), device="cuda")
+    w, ws, _ = _weights(N, K)
+    q, s = dss.quantize_tokens(x)
+    for have, ask in ((torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float16)):
+        out = torch.empty((N, M) if planar else (M, N), dtype=have, device="cuda")
+        for call in (lambda **kw: dss.linear_i8(x, w, ws, **kw), lambda **kw: dss.matmul_i8(q, s, w, ws, **kw)):
+            with pytest.raises(ValueError):
+                call(out=out, out_dtype=ask, planar=planar)
+            want = call(out_dtype=have, planar=planar)
+            assert torch.equal(call(out=out, out_dtype=have, planar=planar), want)
+            assert torch.equal(call(out=out, planar=planar), want)
