@@ -20,6 +20,7 @@
 
 #include "dev_common.h"
 #include "dss_internal.h"
+#include "tile_choice.h"
 #include "tokens.h"
 #include "tokens_device.h"
 
@@ -51,7 +52,6 @@ __host__ __device__ __forceinline__ Sides sides_of(const Layer& L) {
 //
 // The units go from global memory to LDS without a stop in registers; for that rows
 // start at 16-byte units, and K ends at one (what does not is copied first).
-constexpr int kStep = 128;
 constexpr int kUnits = kStep / 16;
 
 // 16 zero bytes: the source of the units past the end of K.
@@ -201,35 +201,10 @@ hipError_t run_tile(const Layer& L, hipStream_t s) {
     return hipGetLastError();
 }
 
-// The tile whose launch should take the least time.  A unit (of 256) with q tiles of
-// one kind at once, `most` of them at the most, takes first + (q - 1) * more
-// microseconds for the steps that its groups take at once, and `ends` for the tiles'
-// beginnings and outputs; measured.
-struct TileTime {
-    int b, groups, most;
-    double first, more, ends;
-};
-constexpr TileTime kTiles[] = {{256, 1, 1, 1.95, 0, 6.0}, {128, 1, 2, 0.95, 0.20, 4.0}, {64, 1, 4, 0.40, 0.17, 2.5},
-                               {64, 4, 1, 1.05, 0, 3.0}};
-
-int pick_tile(const Sides& S, int K) {
-    int best = 0;
-    double least = 0;
-    for (int t = 0; t < 4; ++t) {
-        const TileTime& c = kTiles[t];
-        const int steps = (K + c.groups * kStep - 1) / (c.groups * kStep);
-        const int64_t tiles = ceil_div64(S.I, c.b) * ceil_div64(S.J, c.b), full = tiles / (256 * c.most);
-        const int64_t left = ceil_div64(tiles - full * 256 * c.most, 256);
-        double time = full * (steps * (c.first + (c.most - 1) * c.more) + c.ends);
-        if (left) time += steps * (c.first + (left - 1) * c.more) + c.ends;
-        if (t == 0 || time < least) best = t, least = time;
-    }
-    return best;
-}
-
 template <typename Tout>
 hipError_t run_product(const Layer& L, hipStream_t s) {
-    const int t = pick_tile(sides_of(L), L.K);
+    const Sides S = sides_of(L);
+    const int t = pick_tile(S.I, S.J, L.K);
     if (t == 0) return run_tile<Tout, 256, 256, 2, 4, 1>(L, s);
     if (t == 1) return run_tile<Tout, 128, 128, 2, 2, 1>(L, s);
     if (t == 2) return run_tile<Tout, 64, 64, 2, 2, 1>(L, s);

@@ -110,3 +110,21 @@ def test_a_tensor_is_written_once():
     assert abs(float(norm) - want) <= 1.01 * U * want and torch.equal(out[0], out[1])
     assert np.all(np.abs(_np(out[0]) - ref[0]) <= 2.02 * U * np.abs(ref[0]) + 2.0 ** -149)
     dss.clip_grads([empty, a, empty], 0.5, out=[empty, a, empty])
+
+
+def test_binary32_lists_beyond_the_caches():
+    """Over 2^28 values: loads and stores around the caches, against sums and products in 64 bits on the GPU."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    grads = [torch.randn(n, generator=gen, device="cuda") for n in ((1 << 28) - 7, 100_003, 5)]
+    want = float(torch.sqrt(sum((g.double() ** 2).sum() for g in grads)))
+    for bound in (1.0, 1e9):
+        norm, out = dss.clip_grads(grads, bound)
+        assert abs(float(norm) - want) <= 1.01 * U * want
+        assert abs(float(dss.grad_norm(grads)) - want) <= 1.01 * U * want
+        for o, g in zip(out, grads):
+            ref = g.double() * min(1.0, bound / (want + 1e-6))
+            assert bool(((o.double() - ref).abs() <= 2.02 * U * ref.abs() + 2.0 ** -149).all())
+    before = [o.clone() for o in dss.clip_grads(grads, 1.0)[1]]
+    dss.clip_grads(grads, 1.0, out=grads)
+    assert all(torch.equal(a, b) for a, b in zip(grads, before))

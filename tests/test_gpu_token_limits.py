@@ -1,10 +1,12 @@
-"""8-bit tokens and clipped gradients at the ends of their ranges: the most channels, the smallest factors, and
-the parts of the products that ordinary sizes do not reach."""
+"""8-bit tokens at the ends of their ranges: the most channels, the most tokens, and the parts of the products that
+ordinary sizes do not reach.  Bounds as in test_gpu_tokens.py."""
 import numpy as np
 import pytest
 
 from oracle import tokens
 from paper_1508_06904_amd import dss
+from tests.test_gpu_tokens import _check_layer
+from tests.test_tile_choice import SHAPES
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +83,108 @@ def test_an_output_of_another_type_than_asked_for_is_refused(planar):
             want = call(out_dtype=have, planar=planar)
             assert torch.equal(call(out=out, out_dtype=have, planar=planar), want)
             assert torch.equal(call(out=out, planar=planar), want)
+
+
+@pytest.mark.parametrize("planar", [False, True])
+@pytest.mark.parametrize("out,act", [("f32", "none"), ("f32", "relu"), ("bf16", "none"), ("bf16", "tanh")])
+@pytest.mark.parametrize("tile,M,N,K", [(t,) + s for t in SHAPES for s in SHAPES[t]])
+def test_every_tile(tile, M, N, K, out, act, planar):
+    """Whole products on each of the four tiles, over several steps, with sides that no tile divides."""
+    import torch
+    rng = np.random.default_rng([M, N, K])
+    codes, scales = rng.integers(-127, 128, (M, K)).astype(np.int8), (rng.random(M) * 0.02 + 1e-3).astype(np.float32)
+    w, ws, bias = (t.cpu().numpy() for t in _weights(N, K))
+    y = dss.matmul_i8(*map(_dev, (codes, scales, w, ws)), bias=_dev(bias), act=act, planar=planar,
+                      out_dtype=torch.float32 if out == "f32" else torch.bfloat16)
+    _check_layer(y.t() if planar else y, codes, scales, w, ws, bias, act, out == "bf16")
+
+
+@pytest.mark.parametrize("M,N,K", [(20, 70_001, 77), (32, 8192, 130), (3, 20_000, 700), (13, 8400, 512), (32, 8193, 128),
+                                   (1, 66_000, 96)])
+def test_few_tokens_of_wide_layers(M, N, K):
+    """More outputs than a launch's workgroups take at once, and either side of the streaming kernel's width."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    x = torch.randn((M, K), generator=gen, device="cuda")
+    w, ws, bias = _weights(N, K)
+    q, s = dss.quantize_tokens(x)
+    for planar in (False, True):
+        y = dss.linear_i8(x, w, ws, bias=bias, planar=planar)
+        assert torch.equal(y, dss.matmul_i8(q, s, w, ws, bias=bias, planar=planar))
+        _check_layer(y.t() if planar else y, *(t.cpu().numpy() for t in (q, s, w, ws, bias)), "none")
+
+
+@pytest.mark.parametrize("planar", [False, True])
+@pytest.mark.parametrize("M,N,K,out", [(40_064, 512, 200, "f32"), (40_064, 1024, 130, "bf16"), (300_032, 64, 256, "f32")])
+def test_large_outputs_of_whole_lines(M, N, K, out, planar):
+    """Outputs of more than 64 MB whose rows are whole 128-byte lines are stored around the caches: the same bits as
+    through them (one line's room more for each row), and nothing beside them."""
+    import torch
+    dt = torch.float32 if out == "f32" else torch.bfloat16
+    rows, cols = (N, M) if planar else (M, N)
+    assert rows * cols * dt.itemsize > 1 << 26 and cols * dt.itemsize % 128 == 0
+    x = torch.randn((K, M) if planar else (M, K), generator=torch.Generator(device="cuda").manual_seed(K), device="cuda")
+    x = x.t() if planar else x
+    w, ws, bias = _weights(N, K)
+    y = torch.full((rows, cols), -77.0, dtype=dt, device="cuda")
+    assert y.data_ptr() % 128 == 0
+    dss.linear_i8(x, w, ws, bias=bias, out=y, planar=planar)
+    odd = torch.full((rows, cols + 1), -77.0, dtype=dt, device="cuda")
+    dss.linear_i8(x, w, ws, bias=bias, out=odd[:, :cols], planar=planar)
+    assert torch.equal(y, odd[:, :cols]) and bool((odd[:, cols] == -77).all())
+    at = torch.randperm(M, generator=torch.Generator().manual_seed(1))[:2000].to("cuda")
+    q, s = tokens.quantize(x[at].cpu().numpy())
+    part = y[:, at].t() if planar else y[at]
+    _check_layer(part, q, s, *(t.cpu().numpy() for t in (w, ws, bias)), "none", out == "bf16")
+
+
+@pytest.mark.parametrize("planar", [False, True])
+def test_copied_codes_in_two_parts(planar):
+    """Rows of codes at odd addresses are copied 64 MB at a time: more of them than that, with copied weights."""
+    import torch
+    M, N, K = 70_001, 50, 1000
+    assert M * 1008 > 1 << 26
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    buf = torch.randint(-127, 128, (M, K + 3), generator=gen, device="cuda", dtype=torch.int8)
+    scales = torch.rand(M, generator=gen, device="cuda") + 0.1
+    w, ws, bias = _weights(N, K)
+    y = dss.matmul_i8(buf[:, 3:], scales, w, ws, bias=bias, planar=planar)
+    y = y.t() if planar else y
+    for m in range(0, M, 10_000):
+        part = slice(m, min(m + 10_000, M))
+        _check_layer(y[part], *(t.cpu().numpy() for t in (buf[part, 3:], scales[part], w, ws, bias)), "none")
+
+
+@pytest.mark.parametrize("planar", [False, True])
+def test_more_tokens_than_a_launch_has(planar):
+    """2^27 tokens and some: the second launch has shifted codes, scales and outputs, and the weights copied for
+    the first (they lie at an odd address)."""
+    import torch
+    M, N, K = (1 << 27) + 1003, 3, 16
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    codes = torch.randint(-127, 128, (M, K), generator=gen, device="cuda", dtype=torch.int8)
+    scales = torch.rand(M, generator=gen, device="cuda") + 0.1
+    w, ws, bias = _weights(N, K)
+    odd = torch.zeros((N, K + 5), dtype=torch.int8, device="cuda")
+    odd[:, 3:3 + K] = w
+    y = dss.matmul_i8(codes, scales, odd[:, 3:3 + K], ws, bias=bias, out_dtype=torch.bfloat16, planar=planar)
+    y = y.t() if planar else y
+    at = torch.cat([torch.randint(0, M, (5000,), generator=torch.Generator().manual_seed(1)),
+                    torch.arange((1 << 27) - 70, M)]).to("cuda")
+    _check_layer(y[at], *(t.cpu().numpy() for t in (codes[at], scales[at], w, ws, bias)), "none", True)
+
+
+@pytest.mark.parametrize("planar", [False, True])
+def test_more_tokens_of_a_map_than_a_launch_codes(planar):
+    """Over 2^21 tokens, coded and multiplied in one launch for each half, and the same bits as coded first."""
+    import torch
+    M, N, K = (1 << 21) + 71, 16, 256
+    x = torch.randn((K, M), generator=torch.Generator(device="cuda").manual_seed(7), device="cuda").t()
+    w, ws, bias = _weights(N, K)
+    y = dss.linear_i8(x, w, ws, bias=bias, planar=planar)
+    assert torch.equal(y, dss.matmul_i8(*dss.quantize_tokens(x), w, ws, bias=bias, planar=planar))
+    y = y.t() if planar else y
+    half = (M + 1) // 2
+    at = torch.cat([torch.arange(0, 70), torch.arange(half - 70, half + 70), torch.arange(M - 70, M)]).to("cuda")
+    q, s = tokens.quantize(x[at].cpu().numpy())
+    _check_layer(y[at], q, s, *(t.cpu().numpy() for t in (w, ws, bias)), "none")
