@@ -452,7 +452,9 @@ dss_status dss_clip_grads(const dss_tensor* grads, void* const* out, int32_t n, 
  * (scale and quotient are the binary32 ones, rint goes to the nearest integer and
  * from a tie to the even one), and a layer is
  *   y[m][n] = act(scale[m] * weight_scale[n] * sum_k code[m][k] * weight[n][k] + bias[n])
- * with the sum exact in 32-bit integers.  A token of zeros (or one so small that
+ * with the sum exact in 32-bit integers and the rest in binary32, (sum * weight_scale[n])
+ * * scale[m] + bias[n] in this order: a weight scale above 2^96, and it alone, may make the first
+ * product infinite where y need not be.  A token of zeros (or one so small that
  * its scale is 0) has scale 0 and codes 0.  A token with an infinity or a NaN has
  * scale NaN and codes 0, so that its outputs are NaN and no other token's are. */
 

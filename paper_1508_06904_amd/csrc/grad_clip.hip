@@ -14,9 +14,9 @@
 // bisection.  Tensors need no more than their elements' alignment: the 16-byte
 // loads and stores of this GPU take any address.
 //
-// Measured: 537 million binary32 values, norm 310 us (6.9 TB/s), norm and clipping 1.12 ms, of which the
+// Measured: 537 million binary32 values, norm 310 us (6.9 TB/s), norm and clipping 1.13 ms, of which the
 // scaling's reading and writing are 0.81 (5.3 TB/s; a large copy runs at 5.07); 134 million bfloat16
-// values 48 and 130 us; 5.2 million binary32 values in ten tensors 14 us on the GPU in two launches.
+// values 48 and 130 us; 5.2 million binary32 values in ten tensors 15 us on the GPU in two launches.
 #include <algorithm>
 #include <cmath>
 
@@ -32,12 +32,22 @@ constexpr int kTable = 112;              // 112 * 32 bytes of tensors: the table
 constexpr int kSmallTable = 16;          // a short list's table, which takes less time to hand over
 constexpr int kMaxGroups = 1024;         // workgroups (and partial sums) of a launch
 // Lists of more values write their clipped values around the caches, whose room goes to
-// the values that are read for the second time: 132 us, not 152, for 134 million in bfloat16.
+// the values that are read for the second time.  The clipping alone gains from that at every
+// size, but an update that reads the clipped values next finds shorter lists' in the caches.
+// Clipping and update, through the caches and around them, us, of 2^24, 2^25, 2^26 values:
+// binary32 70/72, 155/145, 302/285; bfloat16 71/72, 70/73, 155/144.  (In bytes the two types
+// cross at the same place, 64 to 128 MB; a count of values is 6 % off for 2^25 binary32 ones.)
 constexpr int64_t kCached = (int64_t)1 << 25;
 // Of even more values little would be left in the caches for the second reading: all of
-// them go around.  537 million in binary32: norm 310 us, not 354, clipping 1150, not 1187.
+// them go around.  Clipping with the outputs alone around, and with all, us, of 2^26 to 2^29
+// values: binary32 129/134, 300/280, 586/551, 1168/1103; bfloat16 68/69, 132/138, 304/284,
+// 593/558: the count fits bfloat16 up to 2^27, and is two powers late for binary32.  The norm
+// alone gains from 2^25 on: 27/24 us there, 366/322 at 2^29, in binary32.
 constexpr int64_t kPassing = (int64_t)1 << 28;
-constexpr int64_t kMinRun = 4096;        // values of the shortest run: four vectors of each thread
+// Values of the shortest run: in binary32 the four vectors that each thread has under way at
+// once.  In bfloat16 that takes 8192 values, so lists of up to 2^24 values, whose runs are the
+// shortest, are read and written value by value: 2^24 of them take 51 us, 2^25 37.
+constexpr int64_t kMinRun = 4096;
 
 template <int CAP>
 struct TensorTable {
@@ -211,6 +221,11 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(TensorTable<CAP> t, cons
 // ------------------------------------------------------------------ short lists, in one launch
 // One workgroup of 16 waves: the waves take runs of kShortRun values in turn, sum
 // their squares, meet for the total and scale the same runs, now in cache.
+//
+// One launch and two, us, a call among others from Python: 6 tensors of 200 values 12.5/15.8,
+// 16 of 1024 18.2/21.3, 16 of 2048 (the most) 18.1/21.5.  There the launch that is saved
+// counts; on the GPU alone, as in a graph, one launch is faster for the shortest lists only:
+// 4.4/5.9, 8.2/6.5, 13.9/7.4.
 constexpr int kShortTable = 16;
 constexpr int kShortWaves = 16;
 constexpr int kShortRun = 1024;          // 16 values of each lane

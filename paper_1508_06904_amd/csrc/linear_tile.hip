@@ -123,10 +123,20 @@ constexpr int64_t kLeastTokens = 4096;
 
 }  // namespace
 
-// Where one launch is the faster one; in microseconds for one launch and for two,
-// 400000 tokens of 256 channels in binary32 to 16, 64 and 128 outputs: 99/135, 124/153,
-// 159/188, and in bfloat16 62/115, 92/123, 151/144; 100000 of 512 channels to 128 and 256: 64/81,
-// 83/93 in binary32, 64/68, 95/84 in bfloat16; 400000 of 128 channels in bfloat16 to 64: 80/65.
+// Where one launch is the faster one.  In microseconds for one launch and for two (GPU, outputs
+// as a map), channels to outputs:
+//                binary32: 256-64   512-128   256-128   512-256   bfloat16: 256-64   512-128   256-128   512-256
+//   1000 tokens            9/10     11/14     12/10     15/14               14/13    16/16     19/13     24/17
+//   4096                  10/12     11/14     13/12     15/15               15/14    18/17     20/14     25/18
+//   20000                 12/16     21/27     16/18     28/33               16/17    20/23     22/18     30/30
+//   100000                39/49     73/92     51/58     99/103              31/41    61/78     40/50     71/86
+//   400000               124/159   264/331   160/191   332/419              92/117  187/257   108/142   273/353
+// 1024 channels to 128: 43/45, 167/168, 605/609 and 30/36, 133/137, 417/473 for the last three.
+// The rule takes the two leftmost columns and 1024-128 in both types, from 4096 tokens on:
+// there bfloat16 still loses one microsecond, binary32 gains from 256 tokens on.  The wider layers,
+// which gain from 20000 (binary32) and 100000 (bfloat16) tokens on, are left to two launches.
+// Weights at odd addresses are read here at the price of a tenth (100000 tokens, 512-128: 76 us
+// for 69 in binary32, 66 for 57 in bfloat16), which two launches (89, 73) do not win back.
 // Rows of values (the channels adjacent) gain less than a tenth and are always coded first.
 bool linear_in_tiles(int64_t M, int N, int K, bool map) {
     return map && M >= kLeastTokens && K <= kMaxChannels && ((K >= 512 && N <= 128) || (K >= 256 && N <= 64));

@@ -5,9 +5,9 @@
 // memory to matrix operands (any address), and add their sums through LDS.  With few
 // outputs a workgroup takes fewer of them, down to two, so that all 256 units read.
 //
-// One window through 9216 x 512 with the coding: 8.2 us, of which 4.7 MB of weights at 5 TB/s are
-// 0.9: a chain of latencies (the values, their largest, the codes, the sums).  32 tokens through
-// 4096 x 4096: 8.7 us a call, bound by the call.
+// One window through 9216 x 512 with the coding: 8.4 us, of which 4.7 MB of weights at 5 TB/s are
+// 0.9: a chain of latencies (the values, their largest, the codes, up to five slabs of weights
+// that each wave fetches in turn, the sums).  32 tokens through 4096 x 4096: 9.1 us.
 #include <algorithm>
 
 #include "dev_common.h"
@@ -195,16 +195,24 @@ hipError_t run_groups(const Layer& L, const Values& V, hipStream_t s) {
 
 }  // namespace
 
-// Up to 32 tokens: there the tiles' workgroups wait longer (32 tokens through 9216 x 512:
-// 11.9 us here and 14.8 on tiles, through 4096 x 4096 8.7 and 10.7), but while the weights are
-// large the tiles' whole-line reading of them counts for more (13 tokens through 4096 x 16384:
-// 19.4 us here, 16.5 on tiles), unless they would be copied for it.
+// Up to 32 tokens.  Codes in hand, here and on tiles, us on the GPU, of 1, 13 and 32 tokens
+// through 4096 x 4096: 6.7/10.7, 7.0/10.7, 9.1/11.5; 9216 x 8192: 16/29, 22/29, 33/30; 4096 x
+// 16384: 17/21, 20/21, 29/22; 1024 x 32768: 11.0/10.2, 13.2/10.9, 19.0/12.8.  The tiles gain
+// with the outputs (whose tiles fill the units) and with the tokens, and lose where weights
+// would be copied for them; K, and with it the weights' size, does not decide.  A width of
+// 8192 alone is a coarse rule: up to 13 tokens of 4096 x 16384 are faster here, 32 of 9216 x
+// 8192 on tiles.
 bool few_tokens(int64_t M, int N, int K) { return M <= 32 && (N <= 8192 || K % 16 != 0); }
 
 hipError_t launch_matmul_few(const Layer& L, dss_dtype out_dtype, hipStream_t s) {
     return out_dtype == DSS_BF16 ? run_groups<int8_t, uint16_t>(L, Values{}, s) : run_groups<int8_t, float>(L, Values{}, s);
 }
 
+// Tokens of 1, 2 and 4 that the kernel codes itself, and coded by a launch before, us on the GPU:
+// 9216 x 512 8.4/10.7 (one token); 4096 x 4096 9.0/9.8, 9.7/9.9, 10.7/10.0; 4096 x 16384 20.9/24.1,
+// 22.0/24.6, 23.3/24.6; 9216 x 8192 (one) 22.4/21.6; 1024 x 32768 16.9/13.3, 17.2/13.4, 17.7/13.6:
+// the outputs are not in the rule, though layers of many outputs and few channels would be
+// better coded first.
 bool codes_itself(int64_t M, int K) {
     if (M > 16) return false;
     int p = 1;

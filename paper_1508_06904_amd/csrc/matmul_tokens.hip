@@ -10,8 +10,8 @@
 // matrix instruction Q's rows are the result's rows, so that a lane holds four
 // adjacent outputs.
 //
-// Large products are bound by the matrix units: 8192 x 8192 x 8192 to bfloat16 in 448 to 567 us
-// over machines and data (1.9 to 2.5 Pop/s; these units' own rate at the clock they then keep, 1.4
+// Large products are bound by the matrix units: 8192 x 8192 x 8192 to bfloat16 in 413 to 567 us
+// over machines and data (1.9 to 2.7 Pop/s; these units' own rate at the clock they then keep, 1.4
 // to 1.8 GHz, would be 2.9 to 3.8), with the matrix pipes busy for two thirds of the time and no
 // LDS bank conflict.  Small ones are bound by the steps' latency, those of few channels by their outputs'
 // bytes.
@@ -246,8 +246,10 @@ bool whole_units(const int8_t* p, int64_t stride, int64_t rows, int K) {
     return K % 16 == 0 && (uintptr_t)p % 16 == 0 && (stride % 16 == 0 || rows == 1);
 }
 
-// The codes' row length in a workspace: whole 16-byte units, and of long rows whole lines
-// (1777 x 1003 x 2305: 14.4 us on the tiles then, 15.7 with rows of 2320).
+// The codes' row length in a workspace: whole 16-byte units, and of long rows whole lines.
+// Units and lines, us for coding and product of 1777 tokens to 2305 outputs: 41/37 from 2305
+// channels, 56/50 from 4100, 22.3/21.6 from 1040; 300 to 300 from 2305 18.4/17.0.  (Shorter rows
+// gain no less, 24.3/23.1 from 777; only those of 200 are the same.)
 int padded_k(int K) { return K >= 1024 ? (K + 127) / 128 * 128 : (K + 15) / 16 * 16; }
 
 int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }

@@ -3,8 +3,9 @@
 // Bound by memory: every value is read once and its code written once.  Two
 // layouts: rows (a token's channels adjacent) and maps (a channel's tokens
 // adjacent, as the dense evaluation writes them).  Measured, bytes in and out: 1.88 million tokens of
-// 512 channels in binary32 as a map 1.01 ms (4.75 TB/s), as rows 0.95 ms (5.1 TB/s); 8191 rows of
-// 4097 in bfloat16 21 us (4.8 TB/s); a large copy runs at 5.07 TB/s.
+// 512 channels in binary32 as a map 0.98 to 1.00 ms (4.8 to 4.9 TB/s), as rows 0.88 ms (5.5 TB/s),
+// in bfloat16 0.64 (4.5) and 0.51 ms (5.6); 8191 rows of 4097 in bfloat16 21 us (4.8 TB/s); a
+// large copy runs at 5.07 TB/s.
 #include <algorithm>
 
 #include "dev_common.h"
@@ -130,6 +131,7 @@ __global__ __launch_bounds__(kMapWaves * 64) void quantize_map_kernel(const T* _
 }
 
 // Narrower maps: a workgroup for each token, value by value; the tokens' lines meet in cache.
+// 16 to 63 binary32 tokens of 9216 channels take 22 us: a chain of 36 loads, twice.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void quantize_narrow_map_kernel(const T* __restrict__ x, int K,
                                                                        int64_t channel_stride,
