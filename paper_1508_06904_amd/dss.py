@@ -673,6 +673,9 @@ def _room(workspace, dev):
 
 # ---------------------------------------------------------------------------- tokens in 8 bits
 
+_MOST = 2 ** 31 - 1      # channels and outputs: the C calls take them in 32 bits, into which ctypes would cut larger ones
+
+
 def _check_tokens(x, dev):
     """dss_dtype, M, K of a matrix of tokens."""
     import torch
@@ -683,7 +686,10 @@ def _check_tokens(x, dev):
         raise ValueError("x must be float32 or bfloat16 (got %s)" % x.dtype)
     if x.get_device() != dev:
         raise ValueError("x must be on the current CUDA device (got %s)" % x.device)
-    return dt, x.shape[0], x.shape[1]
+    M, K = x.shape
+    if K > _MOST:
+        raise ValueError("x has %d channels, more than %d" % (K, _MOST))
+    return dt, M, K
 
 
 def _check_vector(t, what, n, dev):
@@ -736,6 +742,8 @@ def _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, 
     import torch
     wp, wstride = _check_codes(weight, "weight", None, K, dev)
     N = weight.shape[0]
+    if N > _MOST:
+        raise ValueError("weight has %d outputs, more than %d" % (N, _MOST))
     sp = _check_vector(weight_scales, "weight_scales", N, dev)
     bp = None if bias is None else _check_vector(bias, "bias", N, dev)
     if act not in ACTS:
@@ -779,6 +787,8 @@ def matmul_i8(codes, scales, weight, weight_scales, bias=None, act="none", out=N
     dev, handle = _launch(stream)
     cp, cstride = _check_codes(codes, "codes", None, None, dev)
     M, K = codes.shape
+    if K > _MOST:
+        raise ValueError("codes have %d channels, more than %d" % (K, _MOST))
     sp = _check_vector(scales, "scales", M, dev)
     out, N, args = _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, dev, stream)
     room, size, keep = _tokens_room(M, N, K, 2, workspace, dev, stream)

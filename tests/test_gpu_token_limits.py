@@ -188,3 +188,19 @@ def test_more_tokens_of_a_map_than_a_launch_codes(planar):
     at = torch.cat([torch.arange(0, 70), torch.arange(half - 70, half + 70), torch.arange(M - 70, M)]).to("cuda")
     q, s = tokens.quantize(x[at].cpu().numpy())
     _check_layer(y[at], q, s, *(t.cpu().numpy() for t in (w, ws, bias)), "none")
+
+
+def test_counts_that_the_library_does_not_take_are_refused():
+    """Channels and outputs of 2^32 and some, which 32 bits would cut to those few."""
+    import torch
+    far = 2 ** 32
+    x = torch.ones((1, 1), device="cuda").expand(1, far + 8)
+    with pytest.raises(ValueError):
+        dss.quantize_tokens(x)
+    w, ws, _ = _weights(3, 8)
+    for call in (lambda: dss.linear_i8(x, w, ws), lambda: dss.linear_i8(x[:, :2 ** 31], w, ws),
+                 lambda: dss.linear_i8(x[:, :1], torch.empty((far + 3, 1), dtype=torch.int8, device="cuda"), ws),
+                 lambda: dss.matmul_i8(torch.empty((1, far + 8), dtype=torch.int8, device="cuda"), ws[:1], w, ws),
+                 lambda: dss.matmul_i8(w[:1, :1], ws[:1], torch.empty((far + 3, 1), dtype=torch.int8, device="cuda"), ws)):
+        with pytest.raises(ValueError):
+            call()
