@@ -546,7 +546,11 @@ def _launch(stream):
             raise ValueError("the tensors must be on a CUDA device, and there is none")
         torch.cuda.init()
     dev = torch._C._cuda_getDevice()
-    return dev, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if stream is None:
+        return dev, torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device.index != dev:
+        raise ValueError("stream must be one of the current CUDA device, %d (got %s)" % (dev, stream.device))
+    return dev, stream.cuda_stream
 
 
 def _empty(shape, dtype, stream):

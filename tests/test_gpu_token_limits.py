@@ -204,3 +204,27 @@ def test_counts_that_the_library_does_not_take_are_refused():
                  lambda: dss.matmul_i8(w[:1, :1], ws[:1], torch.empty((far + 3, 1), dtype=torch.int8, device="cuda"), ws)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_a_stream_of_another_device_is_refused():
+    """The tensors are checked to be on the current device; the kernels have to run there."""
+    import types
+
+    import torch
+    here = torch.cuda.current_device()
+    other = types.SimpleNamespace(device=torch.device("cuda", here + 1), cuda_stream=0)
+    x = torch.randn((5, 8), device="cuda")
+    w, ws, _ = _weights(3, 8)
+    q, s = dss.quantize_tokens(x)
+    for call in (lambda **kw: dss.quantize_tokens(x, codes=q, scales=s, **kw), lambda **kw: dss.linear_i8(x, w, ws, out=y, **kw),
+                 lambda **kw: dss.matmul_i8(q, s, w, ws, out=y, **kw),
+                 lambda **kw: dss.grad_norm([x], norm=norm, workspace=room, **kw),
+                 lambda **kw: dss.clip_grads([x], 0.5, out=[z], norm=norm, workspace=room, **kw)):
+        y, z, norm = torch.empty((5, 3), device="cuda"), torch.empty_like(x), torch.empty((), device="cuda")
+        room = torch.empty(8192, dtype=torch.uint8, device="cuda")
+        with pytest.raises(ValueError):
+            call(stream=other)
+        for stream in (torch.cuda.Stream(), torch.cuda.current_stream(), torch.cuda.default_stream()):
+            stream.wait_stream(torch.cuda.current_stream())
+            call(stream=stream)
+            torch.cuda.current_stream().wait_stream(stream)
