@@ -573,11 +573,16 @@ def _is_dense(t):
     return True
 
 
+def _same_order(a, b):
+    """Whether two dense tensors of one shape have their elements in the same order in memory."""
+    return a.is_contiguous() and b.is_contiguous() or \
+        all(x == y for x, y, n in zip(a.stride(), b.stride(), a.shape) if n != 1)
+
+
 def _tensor_list(tensors, what, dev, like=None):
     """The C list of CUDA tensors (dss_tensor[n]: address, count, dtype and a zero, as three 64-bit
     words each), the tensors as a list, and whether all of them are contiguous.  `like` is such a
-    result for other tensors, whose types, shapes and (unless all are contiguous) strides these have
-    to have."""
+    result for other tensors, whose types, shapes and orders of elements these have to have."""
     import torch
     T = torch.Tensor
     if isinstance(tensors, T):
@@ -602,9 +607,8 @@ def _tensor_list(tensors, what, dev, like=None):
     else:
         words, others, others_plain = like
         if dtypes != words[2::3] or not all(map(T.is_same_size, tensors, others)) or not (plain and others_plain) and \
-                list(map(T.stride, tensors)) != list(map(T.stride, others)):
-            raise ValueError("%s must be of the gradients' number, types and shapes, and unless all are contiguous of "
-                             "their strides" % what)
+                not all(map(_same_order, tensors, others)):
+            raise ValueError("%s must be of the gradients' number, types, shapes and strides" % what)
         counts = words[1::3]
     words = array.array("q", bytes(24 * n))
     words[0::3] = array.array("q", map(T.data_ptr, tensors))
@@ -627,8 +631,8 @@ def clip_grads(grads, max_norm, out=None, norm=None, workspace=None, stream=None
     """Scales a gradient, given as for grad_norm, by min(1, max_norm / (norm + 1e-6)); max_norm may be
     infinite (nothing is clipped unless the norm is NaN).
     Returns (norm, list of scaled tensors).  `out` is the list of tensors to write (allocated if
-    None; `out=grads` clips in place): of the same types and shapes, and of the same strides unless
-    all tensors are contiguous.  An output shares no memory with another one (so that no tensor can be
+    None; `out=grads` clips in place): of the same types, shapes and strides (of axes longer than 1).
+    An output shares no memory with another one (so that no tensor can be
     clipped in place twice) or with another tensor's gradient."""
     import torch
     dev, handle = _launch(stream)

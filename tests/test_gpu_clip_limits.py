@@ -128,3 +128,21 @@ def test_binary32_lists_beyond_the_caches():
     before = [o.clone() for o in dss.clip_grads(grads, 1.0)[1]]
     dss.clip_grads(grads, 1.0, out=grads)
     assert all(torch.equal(a, b) for a, b in zip(grads, before))
+
+
+def test_strides_that_do_not_matter():
+    """Beside a tensor in another order of its axes: one of a single row out of a wider buffer, and empty ones, whose
+    outputs have other strides for the same order of elements."""
+    import torch
+    wide = torch.randn((4, 100), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    grads = [wide[:, :6].contiguous().t(), wide.as_strided((1, 5), (100, 1)), wide[:, :0], wide[:0, 3:7]]
+    want, ref = tokens.clip([_np(g) for g in grads], 0.5)
+    outs = [torch.empty((4, 6), device="cuda").t()] + [torch.empty(g.shape, device="cuda") for g in grads[1:]]
+    for out in (None, outs):
+        norm, got = dss.clip_grads(grads, 0.5, out=out)
+        assert abs(float(norm) - want) <= 1.01 * U * want
+        for o, g, r in zip(got, grads, ref):
+            assert o.shape == g.shape and np.all(np.abs(_np(o) - r) <= 2.02 * U * np.abs(r) + 2.0 ** -149)
+    outs[0] = torch.empty((6, 4), device="cuda")
+    with pytest.raises(ValueError):
+        dss.clip_grads(grads, 0.5, out=outs)
