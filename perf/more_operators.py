@@ -1,0 +1,392 @@
+"""The operators of a network that learns from a larger one and answers in 4 bits: tokens (window positions, or
+rows of features) in microscaled 4-bit floating point, the fully connected layers on them, and the distillation
+from a teacher's top logits with its gradient.
+
+  listed()              the named cases
+  draw(rng)             one more case of the same ranges
+  prepare(case, seed)   what a program has in hand before the call, on the GPU
+  run(state)            one call; in plain torch operations where `own` is false
+  work(case)            bytes and operations that the call cannot do without
+  exact(case, seed)     the same outputs from the definitions in 64 bits
+
+A token x[m][0..K-1] is coded in blocks b of 32 adjacent channels (the last one may be shorter):
+    X[m][b] = 2^e,  e = floor(log2(max_{k in b} |x[m][k]|)) - 2, at least -127 (and there for a block of zeros),
+    q[m][k] = the value of {0, 0.5, 1, 1.5, 2, 3, 4, 6} nearest to |x[m][k]| / X[m][b], with x's sign;
+a tie goes to the value whose code (its place in the list) is even, and what lies above 6 becomes 6. The product of
+such tokens with weights of the same kind, v[n][k] in blocks of scales W[n][b], is
+    y[m][n] = act(sum_b X[m][b] W[n][b] sum_{k in b} q[m][k] v[n][k] + bias[n]).
+Distillation takes of each position m the student's logits z[0..C-1] and a list of the teacher's largest logits
+t[0..k-1] with their classes i[0..k-1] (below 0: an empty place), and with a temperature T, a position's weight w and a
+common scale s gives
+    p = softmax(t / T) over the list,   r = softmax(z / T) over all classes,
+    loss = s w T^2 sum_j p_j (log p_j - log r_{i_j}),
+    grad_c = dloss / dz_c = s w T (r_c - sum_{j: i_j = c} p_j);
+both are 0 where w is 0 or the list is empty, whatever the logits are.
+
+A case names an operator ("op") and its sizes:
+  op "quantize"       M tokens of K channels to codes, and back to the values that these stand for: "rows"
+                      (channels adjacent, "pad" elements between the tokens) or "map" (a dense map [K][M])
+  op "linear"         the same tokens, coded and multiplied by N rows of weights in one call
+  op "product"        tokens that are already codes and scales
+  op "distill"        M positions of C classes, "top" logits of the teacher for each, "rows" or "map" as above;
+                      "grad" with the gradient or the loss alone, "masked" with weights that leave positions out
+"""
+import math
+
+import torch
+
+own = False
+
+
+# ---------------------------------------------------------------------------- cases
+
+def listed():
+    return [
+        # every window of an HD frame: the 512 maps of the last hidden layer, coded window by window
+        _tokens("quantize_map_hd", "quantize", 1013 * 1853, 512, layout="map"),
+        # rows of an odd width out of a wider buffer, in bfloat16
+        _tokens("quantize_rows_odd", "quantize", 8191, 4097, dtype="bf16", pad=3),
+        # a single window through the first fully connected layer (256 maps of 6 x 6): answering one at a time
+        _tokens("linear_one_window", "linear", 1, 9216, 512, act="relu"),
+        # a few tokens of a server's step through a wide layer
+        _tokens("linear_few_tokens", "linear", 13, 4096, 16384, dtype="bf16", out="bf16"),
+        # a fully connected layer on every window of an HD frame, map in and map out
+        _tokens("linear_map_hd", "linear", 1013 * 1853, 512, 128, layout="map", act="relu"),
+        # a large product of codes: the matrix units' own limit
+        _tokens("product_large", "product", 8192, 8192, 8192, out="bf16"),
+        # a medium product of which no tile divides a side
+        _tokens("product_odd", "product", 1777, 2305, 1003, act="tanh"),
+        # a single window's few classes: launches and their latencies count
+        _distill("distill_one_window", 1, 4, 2),
+        # a training step's gradient over every window of an HD frame
+        _distill("distill_map_hd", 1013 * 1853, 64, 8, layout="map", temperature=2.0),
+        # the windows of a 512 x 512 frame with many classes, in bfloat16; a tenth of them are not to be learnt
+        _distill("distill_map_wide", 445 * 445, 1000, 16, layout="map", dtype="bf16", temperature=4.0, masked=True),
+        # a training step on rows of very many classes
+        _distill("distill_rows", 4096, 32768, 64, dtype="bf16"),
+        # the loss alone, as an evaluation has it, on the longest rows
+        _distill("distill_long_loss", 513, 131071, 128, grad=False, masked=True),
+    ]
+
+
+def _tokens(name, op, M, K, N=0, layout="rows", dtype="f32", out="f32", act="none", pad=0):
+    c = {"op": op, "M": M, "K": K, "N": N, "layout": layout, "dtype": dtype, "out": out, "act": act, "pad": pad}
+    if name:
+        c["name"] = name
+    return c
+
+
+def _distill(name, M, C, top, layout="rows", dtype="f32", temperature=1.0, grad=True, masked=False):
+    c = {"op": "distill", "M": M, "C": C, "top": top, "layout": layout, "dtype": dtype, "temperature": temperature,
+         "grad": grad, "masked": masked}
+    if name:
+        c["name"] = name
+    return c
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _width(rng, lo, hi):
+    """A width: as it comes, or a multiple of 64 as most layers have."""
+    k = _log_int(rng, lo, hi)
+    return max(64, k // 64 * 64) if k >= 64 and rng.random() < 0.5 else k
+
+
+def draw(rng):
+    op = rng.choice(["quantize", "linear", "linear", "product", "product", "distill", "distill", "distill"])
+    dtype = rng.choice(["f32", "bf16"])
+    layout = rng.choice(["rows", "map"])
+    if op == "distill":
+        C = rng.choice([_width(rng, 2, 64), _width(rng, 2, 2048), _width(rng, 1024, 131072)])
+        most = min(1 << 21, (1 << 27) // C)
+        return _distill(None, rng.choice([_log_int(rng, 1, most), _log_int(rng, min(128, most), most)]), C,
+                        _log_int(rng, 1, min(C, 128)), layout=layout, dtype=dtype,
+                        temperature=rng.choice([1.0, 1.0, 2.0, 3.5]), grad=rng.random() < 0.75,
+                        masked=rng.random() < 0.5)
+    if op == "quantize":
+        K = _width(rng, 16, 16384)
+        return _tokens(None, op, _log_int(rng, 1, min(1 << 20, (1 << 28) // K)), K, layout=layout, dtype=dtype,
+                       pad=rng.choice([0, 0, 1, 64]) if layout == "rows" else 0)
+    K, N = _width(rng, 16, 9216), _width(rng, 2, 16384)
+    most = min(1 << 20, (1 << 28) // K, (1 << 28) // N, (1 << 38) // (K * N))
+    M = rng.choice([_log_int(rng, 1, 16), _log_int(rng, 1, most), _log_int(rng, min(128, most), most)])
+    return _tokens(None, op, M, K, N, layout=layout, dtype=dtype if op == "linear" else "f32",
+                   out=rng.choice(["f32", "bf16"]), act=rng.choice(["none", "relu", "tanh"]),
+                   pad=rng.choice([0, 0, 1, 64]) if layout == "rows" else 0)
+
+
+_TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+# ---------------------------------------------------------------------------- inputs
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    if case["op"] == "distill":
+        return _prepare_distill(case, gen)
+    dt = _TYPES[case["dtype"]]
+    M, K, N = case["M"], case["K"], case["N"]
+    if case["layout"] == "map":
+        # maps after a ReLU: [K][M], the tokens adjacent
+        x = torch.randn((K, M), generator=gen, device="cuda").clamp_(min=0).to(dt).t()
+    else:
+        # hidden states: the tokens' sizes differ
+        x = torch.randn((M, K + case["pad"]), generator=gen, device="cuda")
+        x = (x * torch.exp(torch.randn((M, 1), generator=gen, device="cuda"))).to(dt)[:, :K]
+    state = {"case": case, "x": x}
+    if case["op"] == "quantize":
+        return state
+    w = torch.randn((N, K), generator=gen, device="cuda") * math.sqrt(2.0 / K)
+    w *= torch.exp(0.3 * torch.randn((N, 1), generator=gen, device="cuda"))
+    state["bias"] = 0.1 * torch.randn((N,), generator=gen, device="cuda")
+    state["weight"] = _pack(w)
+    if case["op"] == "product":
+        state["x"] = _pack(x)
+    return state
+
+
+def _pack(x):
+    """(codes, scales) as a program keeps them: codes uint8 [M][16 B], the even channel of two in the low half of
+    their byte and zeros from K on; scales uint8 [B][M], e + 127."""
+    q, e = _elements(x)
+    a = q.abs()
+    code = torch.where(a < 2, 2 * a, torch.where(a < 4, a + 2, a / 2 + 4)).to(torch.uint8)
+    code = (code + 8 * (q < 0).to(torch.uint8)).reshape(q.shape[0], -1)
+    return code[:, ::2] + 16 * code[:, 1::2], (e + 127).to(torch.uint8).t().contiguous()
+
+
+def _prepare_distill(case, gen):
+    M, C, k = case["M"], case["C"], case["top"]
+    is_map = case["layout"] == "map"
+
+    def rand(fn, n):  # [M][n], a map's with the positions adjacent
+        return fn((n, M), generator=gen, device="cuda").t() if is_map else fn((M, n), generator=gen, device="cuda")
+
+    # distinct classes in no order of their own, the teacher's logits from the largest down
+    ids = torch.arange(k, device="cuda") * (C // k) + torch.randint(0, C, (M, 1), generator=gen, device="cuda")
+    ids = (ids % C).to(torch.int32)
+    top = 6.0 - torch.cumsum(0.1 + rand(torch.rand, k), dim=1)
+    # a student that has begun to agree with it
+    z = 1.5 * rand(torch.randn, C)
+    z.scatter_add_(1, ids.long(), 0.6 * top)
+    z = z.to(_TYPES[case["dtype"]])
+    # lists that end early
+    ids = torch.where((torch.arange(k, device="cuda") >= 1) & (rand(torch.rand, k) < 0.05), -1, ids)
+    layout = (lambda t: t.t().contiguous().t()) if is_map else (lambda t: t.contiguous())
+    state = {"case": case, "z": z, "top": layout(top), "ids": layout(ids), "scale": 1.0 / M, "weights": None}
+    if case["masked"]:
+        w = torch.rand((M,), generator=gen, device="cuda")
+        state["weights"] = torch.where(w < 0.1, 0.0, 0.5 + w)
+    return state
+
+
+# ---------------------------------------------------------------------------- plain forms
+
+_ELEMENTS = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def _power(e):
+    """2^e of whole numbers from -127 to 127, from its bits."""
+    return torch.where(e > -127, (e + 127) << 23, 1 << 22).to(torch.int32).view(torch.float32)
+
+
+def _elements(x):
+    """x's rows as q, [M][B][32], and e, [M][B]."""
+    x = x.float()
+    M, K = x.shape
+    if K % 32:
+        x = torch.nn.functional.pad(x, (0, 32 - K % 32))
+    x = x.reshape(M, -1, 32)
+    top = x.abs().amax(dim=2)
+    e = torch.where(top > 0, (torch.frexp(top)[1] - 3).clamp(min=-127), -127)
+    q = x.abs() * _power(-e)[:, :, None]
+    step = torch.where(q < 2, 0.5, torch.where(q < 4, 1.0, 2.0))
+    q = torch.clamp(torch.round(q / step) * step, max=6.0)
+    return torch.where(x < 0, -q, q), e
+
+
+def _coded_values(x):
+    """What the codes of x's rows stand for."""
+    q, e = _elements(x)
+    return (q * _power(e)[:, :, None]).reshape(x.shape[0], -1)[:, :x.shape[1]]
+
+
+def _held_values(codes, scales, K):
+    """What codes and scales stand for."""
+    code = torch.stack([codes & 15, codes >> 4], dim=2).reshape(codes.shape[0], -1, 32)
+    table = torch.tensor(_ELEMENTS + tuple(-v for v in _ELEMENTS), device=codes.device)
+    e = scales.t().to(torch.int32) - 127
+    return (table[code.int()] * _power(e)[:, :, None]).reshape(codes.shape[0], -1)[:, :K]
+
+
+def _layer(x, state):
+    """A layer's outputs from the values that its tokens' codes stand for."""
+    case = state["case"]
+    w = _held_values(*state["weight"], case["K"])
+    if case["layout"] == "map":  # a map comes out as one: [N][M]
+        y = torch.matmul(w, x.t()) + state["bias"][:, None]
+    else:
+        y = torch.matmul(x, w.t()) + state["bias"][None]
+    y = torch.relu(y) if case["act"] == "relu" else torch.tanh(y) if case["act"] == "tanh" else y
+    return y.to(_TYPES[case["out"]])
+
+
+def _plain_distill(state):
+    case, ids = state["case"], state["ids"].long()
+    T = case["temperature"]
+    z = state["z"].float() / T
+    z = z - z.amax(dim=1, keepdim=True)
+    e = torch.exp(z)
+    total = e.sum(dim=1, keepdim=True)
+    used = ids >= 0
+    t = torch.where(used, state["top"].float() / T, -math.inf)
+    t = t - t.amax(dim=1, keepdim=True)
+    pe = torch.exp(t)
+    ptotal = pe.sum(dim=1, keepdim=True)
+    p = pe / ptotal
+    at = ids.clamp(min=0)
+    terms = p * ((t - torch.log(ptotal)) - (torch.gather(z, 1, at) - torch.log(total)))
+    live = used.any(dim=1)
+    w = torch.full_like(total[:, 0], state["scale"])
+    if state["weights"] is not None:
+        w = w * state["weights"]
+        live = live & (state["weights"] != 0)
+    out = {"losses": torch.where(live, w * T * T * torch.where(p > 0, terms, 0).sum(dim=1), 0)}
+    if case["grad"]:
+        g = (e / total).scatter_add_(1, at, torch.where(used, -p, 0))
+        out["grad"] = torch.where(live[:, None], g * (w * T)[:, None], 0).to(state["z"].dtype)
+    return out
+
+
+def _plain(state):
+    case = state["case"]
+    if case["op"] == "distill":
+        return _plain_distill(state)
+    if case["op"] == "quantize":
+        return _coded_values(state["x"]).to(_TYPES[case["dtype"]])
+    return _layer(_coded_values(state["x"]) if case["op"] == "linear" else _held_values(*state["x"], case["K"]), state)
+
+
+def run(state):
+    if not own:
+        return _plain(state)
+    from paper_1508_06904_amd import dss
+    case = state["case"]
+    if case["op"] == "distill":
+        losses, grad = dss.distill(state["z"], state["top"], state["ids"], temperature=case["temperature"],
+                                   scale=state["scale"], weights=state["weights"], with_grad=case["grad"])
+        return {"losses": losses, "grad": grad} if case["grad"] else {"losses": losses}
+    if case["op"] == "quantize":
+        codes, scales = dss.quantize_mx4(state["x"])
+        is_map = case["layout"] == "map"
+        values = dss.dequantize_mx4(codes, scales, case["K"], out_dtype=_TYPES[case["dtype"]], planar=is_map)
+        return values.t() if is_map else values
+    weight, weight_scales = state["weight"]
+    more = {"bias": state["bias"], "act": case["act"], "out_dtype": _TYPES[case["out"]],
+            "planar": case["layout"] == "map"}
+    if case["op"] == "linear":
+        return dss.linear_mx4(state["x"], weight, weight_scales, **more)
+    return dss.matmul_mx4(*state["x"], weight, weight_scales, **more)
+
+
+# ---------------------------------------------------------------------------- work
+
+def work(case):
+    """Every input read once, every output written once. Four operations for each coded value (its size, the largest of
+    a block, the scaling and the rounding); a multiply and an add for each product; of each logit the largest, the
+    difference, the power and the sum, with the gradient a product more; some ten for each of the teacher's logits."""
+    if case["op"] == "distill":
+        M, C, k = case["M"], case["C"], case["top"]
+        es = 2 if case["dtype"] == "bf16" else 4
+        bytes_ = M * C * es * (2 if case["grad"] else 1) + M * k * 8 + M * (8 if case["masked"] else 4)
+        return {"bytes": float(bytes_), "flops": (5.0 if case["grad"] else 4.0) * M * C + 10.0 * M * k}
+    M, K, N = case["M"], case["K"], case["N"]
+    es, B = 2 if case["dtype"] == "bf16" else 4, -(-K // 32)
+    if case["op"] == "quantize":
+        return {"bytes": 2.0 * M * K * es, "flops": 4.0 * M * K}
+    bytes_ = M * 17 * B if case["op"] == "product" else M * K * es
+    bytes_ += N * 17 * B + N * 4 + M * N * (2 if case["out"] == "bf16" else 4)
+    return {"bytes": float(bytes_), "flops": 2.0 * M * N * K}
+
+
+# ---------------------------------------------------------------------------- 64 bits
+
+# The values between which a coded one goes up, by their place; "even" places take a tie.
+_BORDERS = (0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0)
+
+
+def _exact_values(x):
+    """What the codes of some rows stand for, in doubles, by counting the borders that |x| / X passes."""
+    x = x.double()
+    M, K = x.shape
+    B = -(-K // 32)
+    wide = torch.zeros((M, B * 32), dtype=torch.float64, device=x.device)
+    wide[:, :K] = x
+    blocks = wide.view(M, B, 32)
+    top = blocks.abs().max(dim=2, keepdim=True).values
+    e = torch.floor(torch.log2(top)).clamp(min=-200.0)
+    e = torch.where(torch.exp2(e + 1) <= top, e + 1, torch.where(torch.exp2(e) > top, e - 1, e))
+    scale = torch.exp2((e - 2).clamp(min=-127.0))
+    q = blocks.abs() / scale
+    place = torch.zeros(q.shape, dtype=torch.uint8, device=x.device)
+    for n, border in enumerate(_BORDERS):
+        place += (q >= border) if n % 2 else (q > border)
+    elements = torch.tensor(_ELEMENTS, dtype=torch.float64, device=x.device)
+    return (elements[place.long()] * scale * torch.sign(blocks)).view(M, B * 32)[:, :K]
+
+
+def exact(case, seed):
+    """From the definitions, in double, of the tokens or positions some at a time."""
+    state = prepare(case, seed)
+    if case["op"] == "distill":
+        return _exact_distill(state)
+    M, K, N = case["M"], case["K"], case["N"]
+    step = max(1, (1 << 25) // max(K, N))
+    y = torch.empty((M, K if case["op"] == "quantize" else N), dtype=torch.float64, device="cuda")
+
+    def held(coded, m, n):
+        codes, scales = coded[0][m:n], coded[1][:, m:n].t().double()
+        halves = torch.stack((codes % 16, codes // 16), dim=-1).flatten(1).long()
+        size = torch.tensor(_ELEMENTS, dtype=torch.float64, device="cuda")[halves % 8]
+        values = torch.where(halves >= 8, -size, size)
+        return (values * torch.exp2(scales - 127.0).repeat_interleave(32, dim=1))[:, :K].contiguous()
+
+    if case["op"] != "quantize":
+        w = held(state["weight"], 0, N).t().contiguous()
+    for m in range(0, M, step):
+        x = held(state["x"], m, m + step) if case["op"] == "product" else _exact_values(state["x"][m:m + step])
+        if case["op"] == "quantize":
+            y[m:m + step] = x
+            continue
+        z = torch.mm(x.contiguous(), w) + state["bias"].double()
+        y[m:m + step] = z.clamp(min=0.0) if case["act"] == "relu" else z.tanh() if case["act"] == "tanh" else z
+    return y.t().contiguous() if case["layout"] == "map" and case["op"] != "quantize" else y
+
+
+def _exact_distill(state):
+    case = state["case"]
+    M, C, T = case["M"], case["C"], case["temperature"]
+    losses = torch.zeros((M,), dtype=torch.float64, device="cuda")
+    grad = torch.zeros((M, C), dtype=torch.float64, device="cuda") if case["grad"] else None
+    step = max(1, (1 << 26) // C)
+    for m in range(0, M, step):
+        ids, z = state["ids"][m:m + step].long(), state["z"][m:m + step].double() / T
+        used = ids >= 0
+        t = (state["top"][m:m + step].double() / T).masked_fill(~used, -math.inf)
+        log_p, log_r = t - torch.logsumexp(t, dim=1, keepdim=True), z - torch.logsumexp(z, dim=1, keepdim=True)
+        p = log_p.exp().masked_fill(~used, 0.0)
+        w = torch.full((z.shape[0],), state["scale"], dtype=torch.float64, device="cuda")
+        if state["weights"] is not None:
+            w = w * state["weights"][m:m + step].double()
+        diff = (log_p - log_r.gather(1, ids.clamp(min=0))).masked_fill(~used, 0.0)
+        losses[m:m + step] = w * T * T * (p * diff).sum(dim=1)
+        if grad is not None:
+            # the lists' classes one place after the other
+            g = log_r.exp()
+            rows = torch.arange(g.shape[0], device="cuda")
+            for j in range(ids.shape[1]):
+                g[rows, ids[:, j].clamp(min=0)] -= p[:, j]
+            grad[m:m + step] = g * (w * T)[:, None]
+    return {"losses": losses, "grad": grad} if case["grad"] else {"losses": losses}
