@@ -515,6 +515,120 @@ dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t M, int64_t 
                              int64_t out_token_stride, int64_t out_channel_stride, void* workspace,
                              int64_t workspace_bytes, hipStream_t stream);
 
+/* ---------------------------------------------------------------- tokens in 4 bits */
+
+/* Fully connected layers on tokens and weights in microscaled 4-bit floating point: every block
+ * of 32 adjacent channels b = 0 .. B-1 (B = ceil(K / 32), the last block may be shorter)
+ * has a power of two for a scale and its elements are 4-bit codes (OCP Microscaling Formats v1.0, MXFP4):
+ *   scale = 2^e,  e = floor(log2(max |x|)) - 2, at least -127 (and -127 for a block of zeros),
+ *   code  = the number of the nearest value to |x| / scale in {0, 0.5, 1, 1.5, 2, 3, 4, 6}, counted
+ *           from 0, ties to the even number, above 6 the last one; plus 8 where x is negative.
+ * A block with an infinity or a NaN has the scale NaN and codes 0: its token's
+ * outputs are NaN, and no other token's are.  A layer is
+ *   y[m][n] = act(sum_b scale[m][b] weight_scale[n][b] sum_{k in b} value[m][k] weight_value[n][k] + bias[n])
+ * with the sum in binary32.  Its order depends on the sizes alone: the same call gives the same bits, M
+ * tokens in one call and in several may differ in a last place.
+ *
+ * Rows of B blocks, of tokens or of weights:
+ *   codes   codes[m * codes_stride + k / 2], the even channel in the lower half of its byte.
+ *           16-byte aligned, codes_stride >= 16 B, a multiple of 16 (one row alone: any).  Whole
+ *           blocks are read: channels from K on have to be zeros in one of a product's two sides (the calls here
+ *           write them so)
+ *   scales  scales[b * scales_stride + m], the byte e + 127, 255 for NaN; scales_stride >= M.  Block by
+ *           block, so that the scales of adjacent tokens are adjacent, as the matrix units take
+ *           them */
+
+/* Codes and scales of M tokens of K channels, x[m * token_stride + k * channel_stride], as for
+ * dss_quantize_tokens.  Weights are coded by the same call.  Inputs and outputs must not overlap.
+ * M = 0 does nothing.  Errors: DSS_E_INVALID (NULL or misaligned pointers, M < 0, K < 1, strides
+ * out of range), DSS_E_UNSUPPORTED (dtype, no stride of 1), DSS_E_HIP. */
+dss_status dss_quantize_blocks(const void* x, dss_dtype dtype, int64_t M, int32_t K, int64_t token_stride,
+                            int64_t channel_stride, uint8_t* codes, int64_t codes_stride, uint8_t* scales,
+                            int64_t scales_stride, hipStream_t stream);
+
+/* The values that codes and scales stand for, exactly:
+ *   out  device, binary32 or bfloat16, out[m * out_token_stride + k * out_channel_stride] for k < K; strides as
+ *        dss_matmul_tokens' outputs
+ * Errors as dss_quantize_blocks. */
+dss_status dss_dequantize_blocks(const uint8_t* codes, int64_t codes_stride, const uint8_t* scales, int64_t scales_stride,
+                              int64_t M, int32_t K, void* out, dss_dtype out_dtype, int64_t out_token_stride,
+                              int64_t out_channel_stride, hipStream_t stream);
+
+/* The layer on tokens that are already codes, both sides of `blocks` blocks.
+ *   bias, act, out  as for dss_matmul_tokens
+ * Inputs and outputs must not overlap.  M = 0 does nothing.  Errors: DSS_E_INVALID (NULL or
+ * misaligned pointers, sizes or strides out of range, unknown act), DSS_E_UNSUPPORTED (out_dtype,
+ * no stride of 1), DSS_E_HIP. */
+dss_status dss_matmul_blocks(const uint8_t* codes, int64_t codes_stride, const uint8_t* scales, int64_t scales_stride,
+                          int64_t M, const uint8_t* weight, int64_t weight_stride, const uint8_t* weight_scales,
+                          int64_t weight_scales_stride, int32_t N, int32_t blocks, const float* bias, dss_act act,
+                          void* out, dss_dtype out_dtype, int64_t out_token_stride, int64_t out_channel_stride,
+                          hipStream_t stream);
+
+/* Workspace bytes of dss_linear_blocks on M tokens of K channels with N outputs, whatever the other
+ * strides (host only; 0 for DSS_TOKENS_CODES: dss_matmul_blocks has no workspace).  Errors:
+ * DSS_E_INVALID (sizes out of range, unknown source, NULL workspace_bytes). */
+dss_status dss_blocks_workspace(int64_t M, int32_t N, int32_t K, dss_token_source source, int64_t* workspace_bytes);
+
+/* The layer on tokens as they are: codes them as dss_quantize_blocks does (the same codes) and multiplies, in one
+ * call.
+ *   workspace  device scratch of dss_blocks_workspace bytes (256-byte aligned); may be NULL where
+ *              these are 0
+ * Other arguments and errors as dss_quantize_blocks's and dss_matmul_blocks's, and DSS_E_SHAPE
+ * (workspace too small). */
+dss_status dss_linear_blocks(const void* x, dss_dtype dtype, int64_t M, int64_t token_stride, int64_t channel_stride,
+                          const uint8_t* weight, int64_t weight_stride, const uint8_t* weight_scales,
+                          int64_t weight_scales_stride, int32_t N, int32_t K, const float* bias, dss_act act, void* out,
+                          dss_dtype out_dtype, int64_t out_token_stride, int64_t out_channel_stride, void* workspace,
+                          int64_t workspace_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------- distillation */
+
+/* A teacher's largest logits for every position, and their classes; any strides >= 0. */
+typedef struct dss_top_logits {
+    const void* logits;     /* device, logits[m * token_stride + j * place_stride], j < count */
+    const void* ids;        /* device, ids[m * id_token_stride + j * id_place_stride]: a class, or a
+                               number below 0 for an empty place */
+    int64_t token_stride, place_stride;
+    int64_t id_token_stride, id_place_stride;
+    int32_t count;          /* 1 .. 1024 */
+    int32_t dtype;          /* dss_dtype of the logits */
+    int32_t id_bytes;       /* 4 or 8: signed integers */
+    int32_t reserved;
+} dss_top_logits;
+
+/* Bytes of the workspace of dss_distill_tokens, for any call. */
+#define DSS_DISTILL_WORKSPACE_BYTES 65536
+
+/* The loss of a network's logits z against a teacher's top logits t, and its gradient, for M positions
+ * (window positions of a dense map, or rows) of C classes:
+ *   p = softmax(t / T) over a position's list,   r = softmax(z / T) over all classes,
+ *   losses[m]  = scale * w[m] * T^2 * sum_j p_j * (log p_j - log r_{id_j}),
+ *   grad[m][c] = scale * w[m] * T * (r_c - sum_{j: id_j = c} p_j),
+ * in binary32, the gradient rounded once to its type (an exponential below 2^-126 of its row's largest may
+ * count as 0).  A list of one place at T = 1 is the
+ * cross entropy with a label.  A class may be in a list more than once.
+ *   logits         device, binary32 or bfloat16, logits[m * token_stride + c * channel_stride], strides as
+ *                  dss_quantize_tokens' (rows, or dss_eval_dense's map)
+ *   top            host; read during the call only
+ *   token_weights  device, binary32 [M], or NULL for ones
+ *   temperature    T, 2^-60 .. 2^60;   scale  finite
+ *   losses         device, binary32 [M]
+ *   grad           device, the logits' type, in the logits' orientation with strides of its own (the one
+ *                  that is not 1 at least the length it steps over), or NULL for the losses alone.
+ *                  The logits themselves, with their strides, may be the gradient; no other overlap is allowed
+ *   workspace      device scratch of DSS_DISTILL_WORKSPACE_BYTES (256-byte aligned)
+ * A position of weight 0, or without a place whose logit is above -infinity, has loss 0 and gradient 0,
+ * whatever its logits.  At any other one infinities and NaN follow the formulas (a
+ * place of logit -infinity adds 0), and a class of C or more makes loss and gradient NaN.
+ * M = 0 does nothing.  Errors: DSS_E_INVALID (NULL or misaligned pointers, sizes or strides out of
+ * range, a temperature that is not above 0, no finite numbers), DSS_E_UNSUPPORTED (dtypes, id_bytes,
+ * temperatures beyond the range, no stride of 1), DSS_E_SHAPE (workspace too small), DSS_E_HIP. */
+dss_status dss_distill_tokens(const void* logits, dss_dtype dtype, int64_t M, int32_t C, int64_t token_stride,
+                              int64_t channel_stride, const dss_top_logits* top, const float* token_weights,
+                              float temperature, float scale, float* losses, void* grad, int64_t grad_token_stride,
+                              int64_t grad_channel_stride, void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
 /* ---------------------------------------------------------------- telemetry */
 
 /* Per-launch record of an evaluation on a plan with timing enabled. */

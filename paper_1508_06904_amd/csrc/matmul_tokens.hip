@@ -312,16 +312,10 @@ dss_status check_layer(int64_t M, const int8_t* weight, int64_t weight_stride, c
         return fail(DSS_E_INVALID, "%lld tokens of %d channels, %d outputs", (long long)M, K, N);
     if (K > kMaxK) return refuse_k(K);
     if (weight_stride < K) return fail(DSS_E_INVALID, "weight_stride %lld is less than %d", (long long)weight_stride, K);
-    const bool rows = (out_channel_stride == 1 || N == 1) && (out_token_stride >= N || M <= 1);
-    const bool map = (out_token_stride == 1 || M <= 1) && (out_channel_stride >= M || N == 1);
-    if (!rows && !map)
-        return fail(out_channel_stride == 1 || out_token_stride == 1 ? DSS_E_INVALID : DSS_E_UNSUPPORTED,
-                    "output strides %lld (tokens) and %lld (channels)", (long long)out_token_stride,
-                    (long long)out_channel_stride);
+    dss_status s = check_outputs(M, N, out, out_dtype, out_token_stride, out_channel_stride);
+    if (s != DSS_OK) return s;
     if (!weight || !weight_scales || (uintptr_t)weight_scales % 4 != 0 || (uintptr_t)bias % 4 != 0)
         return fail(DSS_E_INVALID, "weight or weight_scales is NULL, or the scales or the bias are not aligned");
-    if (M > 0 && (!out || (uintptr_t)out % dtype_size(out_dtype) != 0))
-        return fail(DSS_E_INVALID, "out is NULL or not aligned to its elements");
     return DSS_OK;
 }
 
@@ -334,6 +328,8 @@ int64_t workspace_bytes_of(int64_t M, int32_t N, int32_t K, dss_token_source sou
     return weights + align256(M * Kp) + align256(M * 4);
 }
 
+}  // namespace
+
 dss_status check_room(int64_t need, const void* workspace, int64_t workspace_bytes) {
     if (need == 0) return DSS_OK;
     if (!workspace || ((uintptr_t)workspace & 255u) != 0)
@@ -344,12 +340,23 @@ dss_status check_room(int64_t need, const void* workspace, int64_t workspace_byt
     return DSS_OK;
 }
 
+dss_status check_outputs(int64_t M, int32_t N, const void* out, dss_dtype out_dtype, int64_t out_token_stride,
+                         int64_t out_channel_stride) {
+    const bool rows = (out_channel_stride == 1 || N == 1) && (out_token_stride >= N || M <= 1);
+    const bool map = (out_token_stride == 1 || M <= 1) && (out_channel_stride >= M || N == 1);
+    if (!rows && !map)
+        return fail(out_channel_stride == 1 || out_token_stride == 1 ? DSS_E_INVALID : DSS_E_UNSUPPORTED,
+                    "output strides %lld (tokens) and %lld (channels)", (long long)out_token_stride,
+                    (long long)out_channel_stride);
+    if (M > 0 && (!out || (uintptr_t)out % dtype_size(out_dtype) != 0))
+        return fail(DSS_E_INVALID, "out is NULL or not aligned to its elements");
+    return DSS_OK;
+}
+
 // The output's orientation: as rows where both would do.
 bool is_map(int64_t M, int32_t N, int64_t out_token_stride, int64_t out_channel_stride) {
     return !((out_channel_stride == 1 || N == 1) && (out_token_stride >= N || M <= 1));
 }
-
-}  // namespace
 
 }  // namespace dss
 

@@ -1,0 +1,45 @@
+// Internal declarations of the tokens in microscaled 4-bit floating point: their coding (mx4.hip)
+// and their products with weights of the same kind (matmul_mx4.hip, few_mx4.hip).
+#pragma once
+
+#include "tokens.h"
+
+namespace dss {
+
+constexpr int kBlock = 32;               // channels that share a scale: 16 bytes of codes
+
+inline int64_t blocks_of(int64_t K) { return (K + kBlock - 1) / kBlock; }
+
+// Rows in 4 bits: codes[r * stride + 16 b ..], scales[b * scales_stride + r].
+struct Mx4Rows {
+    const uint8_t* codes;
+    int64_t stride;
+    const uint8_t* scales;
+    int64_t scales_stride;
+    int64_t rows;
+};
+
+// A fully connected layer (the tokens unused where the kernel codes them itself).
+struct Mx4Layer {
+    Mx4Rows tokens, weight;
+    int B;                               // blocks of a row
+    const float* bias;
+    int act;
+    void* out;
+    int64_t ldo;                         // the output's stride that is not 1
+    int map;                             // out is [N][M], not [M][N]
+    int past;                            // the outputs go around the caches
+};
+
+// The checks of rows of B blocks, codes and scales.
+dss_status check_mx4_rows(const Mx4Rows& R, int64_t B, const char* what);
+
+// Codes and scales of M > 0 tokens.
+hipError_t launch_quantize_mx4(dss_dtype dt, const void* x, int64_t M, int K, int64_t token_stride, int64_t channel_stride,
+                               uint8_t* codes, int64_t codes_stride, uint8_t* scales, int64_t scales_stride, hipStream_t s);
+
+// The layer where one side has at most kFewRows rows.
+constexpr int kFewRows = 32;
+hipError_t launch_few_mx4(const Mx4Layer& L, dss_dtype out_dtype, hipStream_t s);
+
+}  // namespace dss

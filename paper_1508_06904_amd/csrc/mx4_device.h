@@ -1,0 +1,67 @@
+// Device helpers of the 4-bit tokens: a block's scale, its codes, and a layer's outputs.
+#pragma once
+
+#include "mx4.h"
+#include "tokens_device.h"
+
+namespace dss {
+
+using f32x4 = __attribute__((ext_vector_type(4))) float;
+
+// The scale byte of a block from its largest |x|'s bits: the exponent less 2, so that the largest
+// value comes to lie in [4, 8); 255 (NaN) if that is no finite number.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+    return top >= kInfBits ? 255u : (uint32_t)max((int)(top >> 23) - 2, 0);
+}
+
+// 2^(byte - 127) as the conversions take it: they read the exponent's bits alone, those of 2^-127 (0) too.
+__device__ __forceinline__ float scale_operand(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Eight codes of adjacent channels: v_cvt_scalef32_pk_fp4_f32 divides by the scale and rounds to the
+// nearest code, ties to the even one, and to 6 from above it; signs are kept.
+__device__ __forceinline__ uint32_t eight_codes(const float (&v)[8], float scale) {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
+}
+
+// c + the product of 16 rows of 128 codes each with 16 others. A lane has 32 adjacent codes of row
+// (lane & 15), block (lane >> 4), and their scale in the lowest byte; row r of the first operand and row
+// l of the second meet in lane (l, r >> 2), register r & 3.
+__device__ __forceinline__ f32x4 multiply_mx4(i32x4 a, uint32_t a_scale, i32x4 b, uint32_t b_scale, f32x4 c) {
+    using i32x8 = __attribute__((ext_vector_type(8))) int;
+    const i32x8 a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
+    const i32x8 b8 = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, 0, (int)a_scale, 0, (int)b_scale);
+}
+
+// N adjacent outputs from p on, which has place j of J; those past the end are left out.
+template <typename Tout, int N>
+__device__ __forceinline__ void store_values(Tout* p, const float (&v)[N], int64_t j, int64_t J, int past) {
+    constexpr int C = N * (int)sizeof(Tout) < 16 ? N : 16 / (int)sizeof(Tout);   // outputs of one store
+#pragma unroll
+    for (int c = 0; c < N; c += C) {
+        struct {
+            Tout v[C];
+        } r;
+#pragma unroll
+        for (int k = 0; k < C; ++k) store_elem(&r.v[k], v[c + k]);
+        if (j + c + C <= J) {
+            if constexpr (sizeof(Tout) * C == 16) {
+                using u32x4 = __attribute__((ext_vector_type(4), aligned(sizeof(Tout)))) uint32_t;
+                if (past) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), reinterpret_cast<u32x4*>(p + c));
+                else __builtin_memcpy(p + c, &r, sizeof r);
+            } else {
+                __builtin_memcpy(p + c, &r, sizeof r);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < C; ++k)
+                if (j + c + k < J) p[c + k] = r.v[k];
+        }
+    }
+}
+
+}  // namespace dss

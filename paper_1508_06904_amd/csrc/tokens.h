@@ -14,6 +14,12 @@ constexpr int64_t kSlabTokens = (int64_t)1 << 21;
 dss_status check_tokens(const void* x, dss_dtype dtype, int64_t M, int32_t K, int64_t token_stride,
                         int64_t channel_stride);
 
+// The checks of a layer's outputs and of its workspace, and whether the output is a map (as rows where both would do).
+dss_status check_outputs(int64_t M, int32_t N, const void* out, dss_dtype out_dtype, int64_t out_token_stride,
+                         int64_t out_channel_stride);
+dss_status check_room(int64_t need, const void* workspace, int64_t workspace_bytes);
+bool is_map(int64_t M, int32_t N, int64_t out_token_stride, int64_t out_channel_stride);
+
 // A fully connected layer on codes (codes and scales unused where the kernel codes the tokens itself).
 struct Layer {
     const int8_t* codes;

@@ -61,6 +61,12 @@ class LayerGeometry(ctypes.Structure):
         return {n: getattr(self, n) for n, _ in self._fields_ if n != "reserved"}
 
 
+class TopLogits(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("ids", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int64) for n in ("token_stride", "place_stride", "id_token_stride", "id_place_stride")] + \
+               [(n, ctypes.c_int32) for n in ("count", "dtype", "id_bytes", "reserved")]
+
+
 class LaunchRecord(ctypes.Structure):
     _fields_ = [("kernel", ctypes.c_char_p), ("chain_layer", ctypes.c_int32), ("tile_mode", ctypes.c_int32),
                 ("ms", ctypes.c_double), ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
@@ -72,6 +78,7 @@ class Tensor(ctypes.Structure):
 
 
 GRAD_NORM_WORKSPACE_BYTES = 8192
+DISTILL_WORKSPACE_BYTES = 65536
 
 EXPORTS = ("dss_chain_geometry", "dss_chain_layer_geometry", "dss_plan_create", "dss_plan_destroy",
            "dss_plan_geometry", "dss_plan_layer_geometry", "dss_eval_dense", "dss_eval_mixed", "dss_eval_slide",
@@ -79,7 +86,8 @@ EXPORTS = ("dss_chain_geometry", "dss_chain_layer_geometry", "dss_plan_create", 
            "dss_plan_dilate_geometry", "dss_eval_dilate", "dss_chain_backward_geometry",
            "dss_plan_backward_geometry", "dss_backward_dense", "dss_eval_dense_noalloc", "dss_frag", "dss_defrag",
            "dss_grad_norm", "dss_clip_grads", "dss_quantize_tokens", "dss_tokens_workspace", "dss_matmul_tokens",
-           "dss_linear_tokens", "dss_plan_set_timing", "dss_plan_timings", "dss_status_string", "dss_last_error", "dss_version")
+           "dss_linear_tokens", "dss_quantize_blocks", "dss_dequantize_blocks", "dss_blocks_workspace", "dss_matmul_blocks",
+           "dss_linear_blocks", "dss_distill_tokens", "dss_plan_set_timing", "dss_plan_timings", "dss_status_string", "dss_last_error", "dss_version")
 
 _lib = None
 
@@ -138,6 +146,14 @@ def lib():
         L.dss_matmul_tokens.argtypes = [VP, I64, VP, I64, VP, I64, VP, I32, I32, VP, I32, VP, I32, I64, I64, VP, I64, VP]
         L.dss_linear_tokens.argtypes = [VP, I32, I64, I64, I64, VP, I64, VP, I32, I32, VP, I32, VP, I32, I64, I64, VP,
                                         I64, VP]
+        L.dss_quantize_blocks.argtypes = [VP, I32, I64, I32, I64, I64, VP, I64, VP, I64, VP]
+        L.dss_dequantize_blocks.argtypes = [VP, I64, VP, I64, I64, I32, VP, I32, I64, I64, VP]
+        L.dss_blocks_workspace.argtypes = [I64, I32, I32, I32, P(I64)]
+        L.dss_matmul_blocks.argtypes = [VP, I64, VP, I64, I64, VP, I64, VP, I64, I32, I32, VP, I32, VP, I32, I64, I64, VP]
+        L.dss_linear_blocks.argtypes = [VP, I32, I64, I64, I64, VP, I64, VP, I64, I32, I32, VP, I32, VP, I32, I64, I64, VP, I64,
+                                     VP]
+        L.dss_distill_tokens.argtypes = [VP, I32, I64, I32, I64, I64, P(TopLogits), VP, ctypes.c_float, ctypes.c_float, VP,
+                                         VP, I64, I64, VP, I64, VP]
         L.dss_plan_set_timing.argtypes = [VP, I32]
         L.dss_plan_timings.argtypes = [VP, P(LaunchRecord), I32, P(I32)]
         L.dss_status_string.argtypes = [I32]
@@ -153,7 +169,8 @@ def lib():
                      "dss_plan_dilate_geometry", "dss_eval_dilate", "dss_chain_backward_geometry",
                      "dss_plan_backward_geometry", "dss_backward_dense", "dss_eval_dense_noalloc", "dss_grad_norm",
                      "dss_clip_grads", "dss_quantize_tokens", "dss_tokens_workspace", "dss_matmul_tokens",
-                     "dss_linear_tokens"):
+                     "dss_linear_tokens", "dss_quantize_blocks", "dss_dequantize_blocks", "dss_blocks_workspace",
+                     "dss_matmul_blocks", "dss_linear_blocks", "dss_distill_tokens"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -747,12 +764,18 @@ def quantize_tokens(x, codes=None, scales=None, stream=None):
 
 def _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, dev, stream):
     """Checks a layer's weights and output: (out, N, the C arguments from the weight to the output's strides)."""
-    import torch
     wp, wstride = _check_codes(weight, "weight", None, K, dev)
     N = weight.shape[0]
     if N > _MOST:
         raise ValueError("weight has %d outputs, more than %d" % (N, _MOST))
     sp = _check_vector(weight_scales, "weight_scales", N, dev)
+    out, tail = _output_args(M, N, bias, act, out, out_dtype, planar, dev, stream)
+    return out, N, (wp, wstride, sp, N, K) + tail
+
+
+def _output_args(M, N, bias, act, out, out_dtype, planar, dev, stream):
+    """Checks a layer's bias and output: (out, the C arguments from the bias to the output's strides)."""
+    import torch
     bp = None if bias is None else _check_vector(bias, "bias", N, dev)
     if act not in ACTS:
         raise ValueError("unknown activation %r" % (act,))
@@ -767,8 +790,7 @@ def _layer_args(M, K, weight, weight_scales, bias, act, out, out_dtype, planar, 
     elif out_dtype is not None and out.dtype != out_dtype:
         raise ValueError("out is %s, not out_dtype %s" % (out.dtype, out_dtype))
     s0, s1 = out.stride()
-    return out, N, (wp, wstride, sp, N, K, bp, ACTS[act], out.data_ptr(), codes[out.dtype]) + \
-        ((s1, s0) if planar else (s0, s1))
+    return out, (bp, ACTS[act], out.data_ptr(), codes[out.dtype]) + ((s1, s0) if planar else (s0, s1))
 
 
 def _tokens_room(M, N, K, source, workspace, dev, stream):
@@ -815,3 +837,159 @@ def linear_i8(x, weight, weight_scales, bias=None, act="none", out=None, out_dty
     room, size, keep = _tokens_room(M, N, K, 1 if ks != 1 and K > 1 else 0, workspace, dev, stream)
     _check(lib().dss_linear_tokens(x.data_ptr(), dt, M, ts, ks, *args, room, size, handle), "dss_linear_tokens")
     return out
+
+
+# ---------------------------------------------------------------------------- tokens in 4 bits
+
+_BLOCK = 32              # channels that share a scale: 16 bytes of codes
+
+
+def _check_mx4(codes, scales, what, blocks, dev):
+    """(codes' address and row stride, scales' address and block stride), rows, blocks of rows in 4 bits."""
+    import torch
+    T = torch.Tensor
+    if not isinstance(codes, T) or codes.dtype != torch.uint8 or codes.dim() != 2 or codes.get_device() != dev or \
+            not isinstance(scales, T) or scales.dtype != torch.uint8 or scales.dim() != 2 or scales.get_device() != dev:
+        raise ValueError("%s must be two uint8 matrices, codes and scales, on the current CUDA device" % what)
+    (m, k), (b, ms) = codes.shape, scales.shape
+    if m != ms or k != 16 * b or blocks is not None and b != blocks:
+        raise ValueError("%s must be codes [rows][16 blocks] and scales [blocks][rows]%s (got [%d][%d] and [%d][%d])" %
+                         (what, "" if blocks is None else " of %d blocks" % blocks, m, k, b, ms))
+    (rs, cs), (bs, ss) = codes.stride(), scales.stride()
+    if k and cs != 1 or m > 1 and (rs < k or rs % 16) or codes.data_ptr() % 16:
+        raise ValueError("%s: the codes must have adjacent bytes, rows that do not overlap and a multiple of 16 bytes for "
+                         "their address and row stride" % what)
+    if m > 1 and ss != 1 or b > 1 and bs < m:
+        raise ValueError("%s: the scales of adjacent rows must be adjacent, and blocks not overlap" % what)
+    return (codes.data_ptr(), rs if m > 1 else max(rs, k), scales.data_ptr(), bs if b > 1 else max(bs, m)), m, b
+
+
+def quantize_mx4(x, codes=None, scales=None, stream=None):
+    """Microscaled 4-bit floating point codes of the tokens (rows) of x, given as for quantize_tokens: in each block of
+    32 channels a power of two for a scale, 2^(floor(log2(max|x|)) - 2), and codes of the nearest of
+    +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} to x / scale.  Returns (codes uint8 [M][16 B], scales uint8 [B][M]), B = ceil(K / 32):
+    two codes a byte, the even channel in its lower half, and the scales' exponents + 127, block by block.  A
+    weight matrix [N][K] is coded the same way."""
+    import torch
+    dev, handle = _launch(stream)
+    dt, M, K = _check_tokens(x, dev)
+    B = -(-K // _BLOCK)
+    if codes is None:
+        codes = _empty((M, 16 * B), torch.uint8, stream)
+    if scales is None:
+        scales = _empty((B, M), torch.uint8, stream)
+    rows, m, _ = _check_mx4(codes, scales, "tokens", B, dev)
+    if m != M:
+        raise ValueError("codes and scales are of %d tokens, x has %d" % (m, M))
+    ts, ks = x.stride()
+    _check(lib().dss_quantize_blocks(x.data_ptr(), dt, M, K, ts, ks, *rows, handle), "dss_quantize_blocks")
+    return codes, scales
+
+
+def dequantize_mx4(codes, scales, channels=None, out=None, out_dtype=None, planar=False, stream=None):
+    """The values of quantize_mx4's codes and scales: [M][channels] (all of the blocks' unless given), or with planar=True
+    the dense map [channels][M], exactly, of out_dtype (float32, or `out`'s, unless given)."""
+    dev, handle = _launch(stream)
+    rows, M, B = _check_mx4(codes, scales, "tokens", None, dev)
+    K = _BLOCK * B if channels is None else channels
+    if -(-K // _BLOCK) != B or K > _MOST:
+        raise ValueError("%d channels do not have %d blocks" % (K, B))
+    out, (_, _, *tail) = _output_args(M, K, None, "none", out, out_dtype, planar, dev, stream)
+    _check(lib().dss_dequantize_blocks(*rows, M, K, *tail, handle), "dss_dequantize_blocks")
+    return out
+
+
+def _weight_mx4(weight, weight_scales, blocks, dev):
+    rows, N, _ = _check_mx4(weight, weight_scales, "weight", blocks, dev)
+    if N > _MOST:
+        raise ValueError("weight has %d outputs, more than %d" % (N, _MOST))
+    return rows, N
+
+
+def matmul_mx4(codes, scales, weight, weight_scales, bias=None, act="none", out=None, out_dtype=None, planar=False,
+               stream=None):
+    """A fully connected layer on tokens in 4 bits (quantize_mx4's codes and scales) with weights in 4 bits (the same
+    of a matrix [N][K]):  y[m][n] = act(sum_k x[m][k] w[n][k] + bias[n])  of the values that the codes stand for, summed in
+    binary32.  act, out, out_dtype, planar and what is returned are as matmul_i8's."""
+    dev, handle = _launch(stream)
+    rows, M, B = _check_mx4(codes, scales, "tokens", None, dev)
+    if B > _MOST // _BLOCK + 1:
+        raise ValueError("tokens have %d blocks, more than %d" % (B, _MOST // _BLOCK + 1))
+    w, N = _weight_mx4(weight, weight_scales, B, dev)
+    out, tail = _output_args(M, N, bias, act, out, out_dtype, planar, dev, stream)
+    _check(lib().dss_matmul_blocks(*rows, M, *w, N, B, *tail, handle), "dss_matmul_blocks")
+    return out
+
+
+def linear_mx4(x, weight, weight_scales, bias=None, act="none", out=None, out_dtype=None, planar=False, workspace=None,
+               stream=None):
+    """matmul_mx4 on float32 or bfloat16 tokens x [M][K], given as for quantize_tokens: codes them as quantize_mx4 does
+    and multiplies in one call."""
+    import torch
+    dev, handle = _launch(stream)
+    dt, M, K = _check_tokens(x, dev)
+    ts, ks = x.stride()
+    w, N = _weight_mx4(weight, weight_scales, -(-K // _BLOCK), dev)
+    out, tail = _output_args(M, N, bias, act, out, out_dtype, planar, dev, stream)
+    if workspace is not None:
+        room, size = _room(workspace, dev)
+    else:
+        need = ctypes.c_int64()
+        _check(lib().dss_blocks_workspace(M, N, K, 1 if ks != 1 and K > 1 else 0, need), "dss_blocks_workspace")
+        size = need.value
+        if size:
+            workspace = _empty(size, torch.uint8, stream)
+        room = workspace.data_ptr() if size else None
+    _check(lib().dss_linear_blocks(x.data_ptr(), dt, M, ts, ks, *w, N, K, *tail, room, size, handle), "dss_linear_blocks")
+    return out
+
+
+# ---------------------------------------------------------------------------- distillation
+
+def distill(logits, top_logits, top_ids, temperature=1.0, scale=1.0, weights=None, with_grad=True, losses=None, grad=None,
+            workspace=None, stream=None):
+    """The loss of a network's logits [M][C] against a teacher's top logits, and its gradient.  logits is a float32 or
+    bfloat16 CUDA matrix given as for quantize_tokens (rows, or `eval_dense(...).flatten(1).t()`), top_logits
+    (float32 or bfloat16) and top_ids (int32 or int64) are [M][k], k at most 1024, of any strides; an id below 0 is an
+    empty place.  With p = softmax(top_logits / T) over a position's places and r = softmax(logits / T),
+      losses[m] = scale * weights[m] * T^2 * sum_j p_j (log p_j - log r[id_j]),
+      grad[m][c] = scale * weights[m] * T * (r_c - sum of p_j with id_j = c);
+    a position of weight 0 or with an empty list has 0 for both.  Returns (losses float32 [M], grad [M][C] of the logits'
+    type and order in memory); with with_grad=False grad is None and nothing is computed for it.  `grad=logits` writes
+    the gradient over the logits."""
+    import torch
+    dev, handle = _launch(stream)
+    dt, M, C = _check_tokens(logits, dev)
+    ts, cs = logits.stride()
+    for t, what, kinds in ((top_logits, "top_logits", _dtype_codes()), (top_ids, "top_ids", (torch.int32, torch.int64))):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.shape[0] != M or t.get_device() != dev or t.dtype not in kinds:
+            raise ValueError("%s must be a %s matrix of %d rows on the current CUDA device" %
+                             (what, "float32 or bfloat16" if what == "top_logits" else "int32 or int64", M))
+    k = top_logits.shape[1]
+    if top_ids.shape[1] != k or not 1 <= k <= 1024:
+        raise ValueError("top_logits and top_ids have %d and %d places (1 to 1024, the same)" % (k, top_ids.shape[1]))
+    wp = None if weights is None else _check_vector(weights, "weights", M, dev)
+    if losses is None:
+        losses = _empty(M, torch.float32, stream)
+    lp = _check_vector(losses, "losses", M, dev)
+    gp, gts, gcs = None, 0, 0
+    if not with_grad:
+        if grad is not None:
+            raise ValueError("grad is given, with_grad is False")
+    else:
+        if grad is None:
+            is_map = cs != 1 and C > 1
+            grad = _empty((C, M) if is_map else (M, C), logits.dtype, stream)
+            grad = grad.t() if is_map else grad
+        elif not isinstance(grad, torch.Tensor) or grad.shape != logits.shape or grad.dtype != logits.dtype or \
+                grad.get_device() != dev:
+            raise ValueError("grad must be of the logits' shape and type on the current CUDA device")
+        gp, (gts, gcs) = grad.data_ptr(), grad.stride()
+    if workspace is None:
+        workspace = _empty(DISTILL_WORKSPACE_BYTES, torch.uint8, stream)
+    room, size = _room(workspace, dev)
+    top = TopLogits(top_logits.data_ptr(), top_ids.data_ptr(), *top_logits.stride(), *top_ids.stride(), k,
+                    _dtype_codes()[top_logits.dtype], top_ids.element_size(), 0)
+    _check(lib().dss_distill_tokens(logits.data_ptr(), dt, M, C, ts, cs, top, wp, temperature, scale, lp, gp, gts, gcs, room,
+                                    size, handle), "dss_distill_tokens")
+    return losses, grad
