@@ -7,6 +7,7 @@
 #include "dss_internal.h"
 #include "mx4.h"
 #include "mx4_device.h"
+#include "tile_choice.h"
 
 namespace dss {
 
@@ -14,16 +15,284 @@ namespace {
 
 int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
 
+// ------------------------------------------------------------------ tiles
+// D[i][j] = sum_k P[i][k] Q[j][k] with the output's adjacent axis as j: for rows P are the tokens and Q the
+// weights, for dense maps the other way round.  In the matrix instruction Q's rows are the result's
+// rows, so that a lane holds four adjacent outputs.
+//
+// BI x BJ outputs for WI x WJ waves; kStep bytes of K (256 channels) at a time through two LDS buffers.  With KG > 1
+// so many groups of waves take the steps in turn, each with buffers of its own: where tiles are
+// fewer than units, a unit has more steps under way.
+//
+// A matrix operand is 16 rows.  Of P they are TI apart: row l of operand a is l TI + a, so that a lane's
+// scales for its TI operands are adjacent bytes and come with one load.  Of Q they are adjacent for binary32 outputs, where a
+// lane's four outputs are a store of 16 bytes and four lanes write 64 adjacent bytes; for
+// bfloat16 outputs two operands share 32 rows, so that a lane has eight adjacent outputs over
+// both and the same holds; its scales come byte by byte.  A row of a buffer is 8 units of 16 bytes, a block's codes each; a
+// row that is an operand's row l keeps unit u at place u ^ (l & 7): the 8 rows that the operand's
+// read takes at once lie in different banks.
+constexpr int kUnits = kStep / 16;
+
+// 16 zero bytes: the source of the blocks past the end of K.
+__device__ __attribute__((aligned(16))) const unsigned int g_zero16[4] = {0u, 0u, 0u, 0u};
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// 16 bytes of each lane from global memory to LDS at wave_dst + 16 * lane.
+__device__ __forceinline__ void copy16(const void* src, char* wave_dst) {
+    __builtin_amdgcn_global_load_lds(src, (lds_void*)wave_dst, 16, 0, 0);
+}
+
+// N adjacent scales, in the low bytes.
+template <int N>
+struct Scales {
+    uint32_t w[(N + 3) / 4];
+};
+template <int N>
+__device__ __forceinline__ Scales<N> load_scales(const uint8_t* p, int shift) {
+    Scales<N> r = {};
+    if constexpr (N == 8) {
+        uint64_t v;
+        __builtin_memcpy(&v, p, 8);
+        v >>= shift;
+        r.w[0] = (uint32_t)v;
+        r.w[1] = (uint32_t)(v >> 32);
+    } else {
+        __builtin_memcpy(r.w, p, N);
+        r.w[0] >>= shift;
+    }
+    return r;
+}
+
+template <int BYTE_A>
+__device__ __forceinline__ f32x4 multiply_byte(i32x4 q, uint32_t q_scale, i32x4 p, uint32_t p_scale, f32x4 c) {
+    using i32x8 = __attribute__((ext_vector_type(8))) int;
+    const i32x8 q8 = __builtin_shufflevector(q, q, 0, 1, 2, 3, -1, -1, -1, -1);
+    const i32x8 p8 = __builtin_shufflevector(p, p, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(q8, p8, c, 4, 4, 0, (int)q_scale, BYTE_A, (int)p_scale);
+}
+// With the scale in byte a of p_scale (constant once the loops are unrolled).
+__device__ __forceinline__ f32x4 multiply_at(int a, i32x4 q, uint32_t q_scale, i32x4 p, uint32_t p_scale, f32x4 c) {
+    switch (a & 3) {
+        case 0: return multiply_byte<0>(q, q_scale, p, p_scale, c);
+        case 1: return multiply_byte<1>(q, q_scale, p, p_scale, c);
+        case 2: return multiply_byte<2>(q, q_scale, p, p_scale, c);
+        default: return multiply_byte<3>(q, q_scale, p, p_scale, c);
+    }
+}
+
+struct Sides {
+    Mx4Rows P, Q;
+};
+__host__ __device__ __forceinline__ Sides sides_of(const Mx4Layer& L) {
+    if (L.map) return {L.weight, L.tokens};
+    return {L.tokens, L.weight};
+}
+
+template <typename Tout, int BI, int BJ, int WI, int WJ, int KG, bool MAP>
+__global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))) void matmul_mx4_kernel(Mx4Layer L, int tiles_i, int tiles_j) {
+    constexpr int NW = WI * WJ, THREADS = NW * 64;
+    constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
+    constexpr int C = 16 / (int)sizeof(Tout);            // outputs of a store, from C / 4 operands of Q
+    constexpr int LP = BI * kUnits / THREADS, LQ = BJ * kUnits / THREADS;   // units of each thread and step
+    static_assert(LP * THREADS == BI * kUnits && LQ * THREADS == BJ * kUnits && THREADS % 64 == 0, "tile");
+    static_assert(TI <= 8 && THREADS / 8 % (8 * TI) == 0 && THREADS / 8 % 32 == 0 && TJ % (C / 4) == 0,
+                  "the places of a thread's units, the operands of a store");
+    constexpr int BUF = (BI + BJ) * kStep;
+    extern __shared__ __align__(16) char lds[];
+    const Sides S = sides_of(L);
+    const int64_t I = S.P.rows, J = S.Q.rows;
+    // tiles in strips of 8 along i: a strip's tiles share their rows of Q in cache
+    const int64_t id = xcd_order(blockIdx.x, (int64_t)tiles_i * tiles_j);
+    const int64_t strip = id / ((int64_t)8 * tiles_j), in_strip = id - strip * 8 * tiles_j;
+    const int rows = min(8, tiles_i - (int)strip * 8);
+    const int64_t i0 = (strip * 8 + in_strip % rows) * BI, j0 = in_strip / rows * BJ;
+    const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS), tid = threadIdx.x - group * THREADS;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, q16 = lane >> 4;
+    char* const buffers = lds + group * 2 * BUF;
+    const int wi = wave / WJ, wj = wave % WJ;
+
+    // the thread's units: rows row0 + n * (THREADS / 8), and one place in each of them.  Their
+    // offsets from the tile's first rows fit 32 bits (kMostStride).
+    const int row0 = tid >> 3;
+    const int unit_p = (tid & 7) ^ (row0 / TI & 7), unit_q = (tid & 7) ^ ((row0 & 3) | (row0 / C & 1) << 2);
+    const uint8_t *const base_p = S.P.codes + i0 * S.P.stride, *const base_q = S.Q.codes + j0 * S.Q.stride;
+    uint32_t src_p[LP], src_q[LQ];
+#pragma unroll
+    for (int n = 0; n < LP; ++n) src_p[n] = (uint32_t)min((int64_t)row0 + n * (THREADS / 8), I - 1 - i0) * (uint32_t)S.P.stride;
+#pragma unroll
+    for (int n = 0; n < LQ; ++n) src_q[n] = (uint32_t)min((int64_t)row0 + n * (THREADS / 8), J - 1 - j0) * (uint32_t)S.Q.stride;
+
+    const int B = L.B, steps = (B + KG * kUnits - 1) / (KG * kUnits);
+    f32x4 acc[TI][TJ] = {};
+
+    // Unit n of the thread's LP + LQ units of step s, into the step's buffer; past the end of K zeros.
+    const uint8_t* zeros = reinterpret_cast<const uint8_t*>(g_zero16);
+    auto fetch = [&](int s, int n) {
+        const int b = (s * KG + group) * kUnits + (n < LP ? unit_p : unit_q);
+        const uint8_t* row = n < LP ? base_p + src_p[n < LP ? n : 0] : base_q + src_q[n < LP ? 0 : n - LP];
+        copy16(b < B ? row + (int64_t)b * 16 : zeros, buffers + (s & 1) * BUF + (n * NW + wave) * 1024);
+    };
+    // A barrier that waits for the wave's own copies first: they count as loads, for which a barrier
+    // alone does not wait.
+    auto arrived = [&]() {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+
+    // The scales of half a step (4 blocks): the lane's block is b.  Past the end of K, where the codes are zeros, the
+    // last block's (if that is NaN, so are the outputs already).  The last rows' loads end with them.
+    const int64_t i_lane = i0 + wi * TI * 16 + l16 * TI, i_at = min(i_lane, I - TI);
+    const int shift_p = 8 * (int)min(i_lane - i_at, (int64_t)TI - 1);
+    uint32_t off_q[TJ];
+#pragma unroll
+    for (int n = 0; n < TJ; ++n)
+        off_q[n] = (uint32_t)min(j0 + wj * TJ * 16 + (l16 >> 2) * C + (l16 & 3) + n / (C / 4) * 4 * C + n % (C / 4) * 4, J - 1);
+    struct Half {
+        i32x4 o[TI + TJ];
+        Scales<TI> p;
+        uint32_t q[TJ];
+    };
+    auto scales = [&](Half& o, int s, int h) {
+        const int64_t b = min((s * KG + group) * kUnits + h * 4 + q16, B - 1);
+        o.p = load_scales<TI>(S.P.scales + b * S.P.scales_stride + i_at, shift_p);
+        const uint8_t* q = S.Q.scales + b * S.Q.scales_stride;
+#pragma unroll
+        for (int n = 0; n < TJ; ++n) o.q[n] = q[off_q[n]];
+    };
+
+    // The matrix operands of half a step: TJ of Q, then TI of P.
+    const int at_p = (wi * TI * 16 + l16 * TI) * kStep;
+    const int at_q = (BI + wj * TJ * 16 + (l16 >> 2) * C + (l16 & 3)) * kStep;
+    auto read = [&](Half& o, int n, int s, int h) {
+        const int at = n < TJ ? at_q + (n / (C / 4) * 4 * C + n % (C / 4) * 4) * kStep : at_p + (n - TJ) * kStep;
+        o.o[n] = *reinterpret_cast<const i32x4*>(buffers + (s & 1) * BUF + at + ((h * 4 + q16) ^ (l16 & 7)) * 16);
+    };
+    // Multiplies one half's operands, reads another's (half h of step s) and fetches a step's
+    // units, an LDS read and a fetch after every few matrix instructions.  In a burst the fetches would
+    // hold up the wave, and with it its matrix instructions, until all of them are taken.
+    auto half_step = [&](Half& use, Half& next, int s, int h, bool fetches) {
+        constexpr int R = TI + TJ;
+        scales(next, s, h);
+#pragma unroll
+        for (int n = 0; n < R; ++n) {
+            if (fetches)
+#pragma unroll
+                for (int f = (LP + LQ) * n / R; f < (LP + LQ) * (n + 1) / R; ++f) fetch(s + 1, f);
+            read(next, n, s, h);
+#pragma unroll
+            for (int m = TI * TJ * n / R; m < TI * TJ * (n + 1) / R; ++m)
+                acc[m / TJ][m % TJ] = multiply_at(m / TJ, use.o[m % TJ], use.q[m % TJ], use.o[TJ + m / TJ], use.p.w[m / TJ / 4], acc[m / TJ][m % TJ]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    // A step's second half is read while its first is multiplied.  Then nobody needs the step's
+    // buffer any more, and the next step's bytes have had a step's time to arrive: one barrier for
+    // both, after which the buffer takes the step after the next and the next one's first half is read.
+    // (Past the last step zeros are fetched and read, and not used: no branch divides the loop.)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int n = 0; n < LP + LQ; ++n) fetch(s, n);
+    }
+    Half h0, h1;
+    scales(h0, 0, 0);
+    arrived();
+#pragma unroll
+    for (int n = 0; n < TI + TJ; ++n) read(h0, n, 0, 0);
+    for (int s = 0; s < steps; ++s) {
+        half_step(h0, h1, s, 1, false);
+        arrived();
+        half_step(h1, h0, s + 1, 0, true);
+    }
+    arrived();                           // no copy may outlive the workgroup
+    if constexpr (KG > 1) {
+        // the groups' sums meet in the buffers, and are added in the groups' order
+        f32x4* sums = reinterpret_cast<f32x4*>(lds) + tid;
+#pragma unroll
+        for (int n = 0; n < TI * TJ; ++n)
+            if (group > 0) sums[((group - 1) * TI * TJ + n) * THREADS] = acc[n / TJ][n % TJ];
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int g = 0; g < KG - 1; ++g)
+#pragma unroll
+            for (int n = 0; n < TI * TJ; ++n) acc[n / TJ][n % TJ] += sums[(g * TI * TJ + n) * THREADS];
+    }
+    constexpr int STORES = TJ * 4 / C;
+    const int64_t j = j0 + wj * TJ * 16 + q16 * C;
+    float bias_j[STORES][C] = {};
+    if (!MAP && L.bias) {
+#pragma unroll
+        for (int c = 0; c < STORES; ++c)
+#pragma unroll
+            for (int k = 0; k < C; ++k) bias_j[c][k] = L.bias[min(j + c * 4 * C + k, J - 1)];
+    }
+    float bias_i[TI] = {};
+    if (MAP && L.bias) {
+#pragma unroll
+        for (int a = 0; a < TI; ++a) bias_i[a] = L.bias[min(i_lane + a, I - 1)];
+    }
+#pragma unroll
+    for (int a = 0; a < TI; ++a) {
+        const int64_t i = i_lane + a;
+#pragma unroll
+        for (int c = 0; c < STORES; ++c) {
+            if (i >= I || j + c * 4 * C >= J) continue;
+            float v[C];
+#pragma unroll
+            for (int k = 0; k < C; ++k)
+                v[k] = activate_nan(L.act, acc[a][c * (C / 4) + k / 4][k % 4] + (MAP ? bias_i[a] : bias_j[c][k]));
+            store_values(static_cast<Tout*>(L.out) + i * L.ldo + j + c * 4 * C, v, j + c * 4 * C, J, L.past);
+        }
+    }
+}
+
+template <typename Tout, int BI, int BJ, int WI, int WJ, int KG>
+hipError_t run_tile(const Mx4Layer& L, hipStream_t s) {
+    const Sides S = sides_of(L);
+    const int64_t ti = ceil_div64(S.P.rows, BI), tj = ceil_div64(S.Q.rows, BJ);
+    const auto kern = L.map ? matmul_mx4_kernel<Tout, BI, BJ, WI, WJ, KG, true>
+                            : matmul_mx4_kernel<Tout, BI, BJ, WI, WJ, KG, false>;
+    constexpr size_t lds = KG * 2 * (BI + BJ) * kStep;
+    const hipError_t e = allow_dynamic_lds((const void*)kern, lds);
+    if (e != hipSuccess) return e;
+    kern<<<dim3((unsigned)(ti * tj)), KG * WI * WJ * 64, lds, s>>>(L, (int)ti, (int)tj);
+    return hipGetLastError();
+}
+
+template <typename Tout>
+hipError_t run_product(const Mx4Layer& L, hipStream_t s) {
+    const Sides S = sides_of(L);
+    const int t = pick_tile(S.P.rows, S.Q.rows, L.B * 16);
+    if (t == 0) return run_tile<Tout, 256, 256, 2, 4, 1>(L, s);
+    if (t == 1) return run_tile<Tout, 128, 128, 2, 2, 1>(L, s);
+    if (t == 2) return run_tile<Tout, 64, 64, 2, 2, 1>(L, s);
+    return run_tile<Tout, 64, 64, 2, 2, 4>(L, s);
+}
+
+// The largest row stride of a tile's operands: 256 rows of them stay in 32 bits.
+constexpr int64_t kMostStride = (int64_t)1 << 23;
+
 // The layer on codes.
 hipError_t launch_matmul(const Mx4Layer& L, dss_dtype out_dtype, hipStream_t s) {
-    if (L.tokens.rows <= kFewRows || L.weight.rows <= kFewRows) return launch_few_mx4(L, out_dtype, s);
-    for (int64_t m = 0; m < L.tokens.rows; m += kFewRows) {
+    const bool few = L.tokens.rows <= kFewRows || L.weight.rows <= kFewRows;
+    if (few) return launch_few_mx4(L, out_dtype, s);
+    // rows too long for the tiles are taken kFewRows at a time; a launch of tiles has fewer than 2^32
+    // threads: at most 2^21 tiles of 64 x 64 and 1024 threads
+    const bool tiles = std::max(L.tokens.stride, L.weight.stride) <= kMostStride;
+    const int64_t slab = tiles ? std::max<int64_t>(256, (((int64_t)1 << 27) / ceil_div64(L.weight.rows, 64)) / 256 * 256) : kFewRows;
+    for (int64_t m = 0; m < L.tokens.rows; m += slab) {
         Mx4Layer S = L;
-        S.tokens.rows = std::min<int64_t>(kFewRows, L.tokens.rows - m);
+        S.tokens.rows = std::min(slab, L.tokens.rows - m);
         S.tokens.codes += m * L.tokens.stride;
         S.tokens.scales += m;
         S.out = static_cast<char*>(L.out) + m * (L.map ? 1 : L.ldo) * (int64_t)dtype_size(out_dtype);
-        const hipError_t e = launch_few_mx4(S, out_dtype, s);
+        const bool tile = tiles && S.tokens.rows > kFewRows;
+        const hipError_t e = !tile ? launch_few_mx4(S, out_dtype, s)
+                             : out_dtype == DSS_BF16 ? run_product<uint16_t>(S, s) : run_product<float>(S, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
