@@ -15,15 +15,140 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// A thread for each block of a token, any strides; blocks of adjacent tokens are adjacent threads'.
+// ------------------------------------------------------------------ rows
+// A workgroup has kRowTokens tokens of kRowBlocks blocks, four lanes for a block: a wave reads 512 adjacent channels of a
+// token at a time. The scales turn round in LDS, so that those of adjacent tokens leave together.
+constexpr int kRowTokens = 32, kRowBlocks = 16;
+
+// Eight adjacent channels of a lane.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void quantize_mx4_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t ts,
-                                                                int64_t ks, uint8_t* __restrict__ codes,
-                                                                int64_t codes_stride, uint8_t* __restrict__ scales,
-                                                                int64_t scales_stride) {
+struct Eight {
+    Chunk<T> c[8 / Chunk<T>::E];
+
+    // From p on, those from n on as zeros (n may be negative).
+    __device__ __forceinline__ void load(const T* p, int64_t n) {
+#pragma unroll
+        for (int i = 0; i < 8 / Chunk<T>::E; ++i)
+            c[i] = load_chunk(p + i * Chunk<T>::E, (int)max(min(n - i * Chunk<T>::E, (int64_t)8), (int64_t)0));
+    }
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t t = 0;
+#pragma unroll
+        for (int i = 0; i < 8 / Chunk<T>::E; ++i) t = raise(t, c[i]);
+        return top_bits<T>(t);
+    }
+    __device__ __forceinline__ uint32_t codes(uint32_t byte) const {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c[k / Chunk<T>::E].value(k % Chunk<T>::E);
+        return byte == 255u ? 0u : eight_codes(v, scale_operand(byte));
+    }
+};
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void quantize_mx4_rows_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t ts,
+                                                                     uint8_t* __restrict__ codes, int64_t codes_stride,
+                                                                     uint8_t* __restrict__ scales, int64_t scales_stride) {
+    __shared__ uint8_t bytes[kRowBlocks][kRowTokens];
+    const int64_t m0 = (int64_t)blockIdx.x * kRowTokens, b0 = (int64_t)blockIdx.y * kRowBlocks;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t b = b0 + (lane >> 2), k = b0 * kBlock + lane * 8;
+    constexpr int PER = kRowTokens / (kThreads / 64);      // tokens of a wave
+    Eight<T> v[PER];
+#pragma unroll
+    for (int n = 0; n < PER; ++n)
+        if (m0 + wave * PER + n < M) v[n].load(x + (m0 + wave * PER + n) * ts + k, K - k);
+#pragma unroll
+    for (int n = 0; n < PER; ++n) {
+        uint32_t top = v[n].top();
+        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+        const uint32_t byte = scale_byte(top);
+        const int64_t m = m0 + wave * PER + n;
+        if (m < M && b * kBlock < K) *reinterpret_cast<uint32_t*>(codes + m * codes_stride + k / 2) = v[n].codes(byte);
+        if ((lane & 3) == 0) bytes[lane >> 2][wave * PER + n] = (uint8_t)byte;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = threadIdx.x; n < kRowBlocks * kRowTokens; n += kThreads) {
+        const int64_t m = m0 + n % kRowTokens, at = b0 + n / kRowTokens;
+        if (m < M && at * kBlock < K) scales[at * scales_stride + m] = bytes[n / kRowTokens][n % kRowTokens];
+    }
+}
+
+// ------------------------------------------------------------------ maps
+// 16 lanes have 16 bytes each of one channel, 256 adjacent bytes; a lane has the 32 channels of a block of its
+// tokens, so that a block's codes leave it as 16 bytes and its tokens' scales as one word, and nothing passes between
+// lanes. The last tile ends with the last token, and computes what the one before it has over again.
+template <typename T>
+struct MapBlock {
+    static constexpr int V = 16 / (int)sizeof(T);      // tokens of a lane
+    static constexpr int kTokens = 16 * V;
+    Chunk<T> c[kBlock];                                // c[k].value(j): channel k of the block, token j
+
+    __device__ __forceinline__ void load(const T* p, int64_t ks, int n) {
+#pragma unroll
+        for (int k = 0; k < kBlock; ++k) {
+            c[k] = Chunk<T>{};
+            if (k < n) __builtin_memcpy(&c[k], p + k * ks, 16);
+        }
+    }
+    __device__ __forceinline__ void scale_bytes(uint32_t (&byte)[V]) const {
+        uint32_t top[4] = {};
+#pragma unroll
+        for (int k = 0; k < kBlock; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top[j] = raise<T>(top[j], c[k].w[j]);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            byte[j] = scale_byte(V == 4 ? top[j] : j & 1 ? top[j / 2] & 0xffff0000u : top[j / 2] << 16);
+    }
+    // The 32 codes of token j.
+    __device__ __forceinline__ i32x4 codes(int j, uint32_t byte) const {
+        const float scale = scale_operand(byte);
+        i32x4 w;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = c[8 * q + k].value(j);
+            w[q] = (int)(byte == 255u ? 0u : eight_codes(v, scale));
+        }
+        return w;
+    }
+};
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void quantize_mx4_map_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t ks,
+                                                                    uint8_t* __restrict__ codes, int64_t codes_stride,
+                                                                    uint8_t* __restrict__ scales, int64_t scales_stride) {
+    using Block = MapBlock<T>;
+    const int64_t m = min(xcd_order(blockIdx.x, gridDim.x) * Block::kTokens, M - Block::kTokens) + (threadIdx.x & 15) * Block::V;
+    const int64_t b = (int64_t)blockIdx.y * (kThreads / 16) + (threadIdx.x >> 4);
+    if (b * kBlock >= K) return;
+    Block v;
+    v.load(x + m + b * kBlock * ks, ks, (int)min((int64_t)kBlock, K - b * kBlock));
+    uint32_t byte[Block::V];
+    v.scale_bytes(byte);
+#pragma unroll
+    for (int j = 0; j < Block::V; ++j)
+        *reinterpret_cast<i32x4*>(codes + (m + j) * codes_stride + b * 16) = v.codes(j, byte[j]);
+    struct {
+        uint8_t b[Block::V];
+    } all;
+#pragma unroll
+    for (int j = 0; j < Block::V; ++j) all.b[j] = (uint8_t)byte[j];
+    __builtin_memcpy(scales + b * scales_stride + m, &all, sizeof all);
+}
+
+// Narrower maps: a thread for each block of a token.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void quantize_mx4_narrow_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t ks,
+                                                                       uint8_t* __restrict__ codes, int64_t codes_stride,
+                                                                       uint8_t* __restrict__ scales, int64_t scales_stride) {
     const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, b = id / M, m = id - b * M, k0 = b * kBlock;
     if (k0 >= K) return;
-    const T* p = x + m * ts + k0 * ks;
+    const T* p = x + m + k0 * ks;
     const int n = (int)min((int64_t)kBlock, K - k0);
     float v[kBlock];
     uint32_t top = 0;
@@ -43,54 +168,137 @@ __global__ __launch_bounds__(kThreads) void quantize_mx4_kernel(const T* __restr
     scales[b * scales_stride + m] = (uint8_t)byte;
 }
 
-// The values of a block, any strides.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void dequantize_mx4_kernel(Mx4Rows R, int64_t K, T* __restrict__ out, int64_t ts,
-                                                                  int64_t ks) {
+// ------------------------------------------------------------------ values
+__device__ __forceinline__ float value_of(uint32_t word, int k, float scale, bool nan) {
     using f32x2 = __attribute__((ext_vector_type(2))) float;
-    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, b = id / R.rows, m = id - b * R.rows, k0 = b * kBlock;
-    if (k0 >= K) return;
-    const i32x4 w = *reinterpret_cast<const i32x4*>(R.codes + m * R.stride + b * 16);
-    const uint32_t byte = R.scales[b * R.scales_stride + m];
-    const float scale = scale_operand(byte);
-    const int n = (int)min((int64_t)kBlock, K - k0);
-    T* p = out + m * ts + k0 * ks;
-    auto put = [&](int k, f32x2 v) {
-        if (byte == 255u) v[0] = v[1] = __uint_as_float(0x7fc00000u);
-        if (k < n) store_elem(p + k * ks, v[0]);
-        if (k + 1 < n) store_elem(p + (k + 1) * ks, v[1]);
-    };
+    f32x2 v;
+    switch (k / 2) {
+        case 0: v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 0); break;
+        case 1: v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 1); break;
+        case 2: v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 2); break;
+        default: v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 3); break;
+    }
+    return nan ? __uint_as_float(0x7fc00000u) : v[k & 1];
+}
+
+// Rows: four lanes for a block, eight adjacent values each.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void dequantize_mx4_rows_kernel(Mx4Rows R, int64_t K, T* __restrict__ out, int64_t ts) {
+    const int64_t m0 = (int64_t)blockIdx.x * kRowTokens + (threadIdx.x >> 6) * (kRowTokens / (kThreads / 64));
+    const int lane = threadIdx.x & 63;
+    const int64_t b = (int64_t)blockIdx.y * kRowBlocks + (lane >> 2), k = (int64_t)blockIdx.y * kRowBlocks * kBlock + lane * 8;
+    if (b * kBlock >= K) return;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        put(8 * j, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)w[j], scale, 0));
-        put(8 * j + 2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)w[j], scale, 1));
-        put(8 * j + 4, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)w[j], scale, 2));
-        put(8 * j + 6, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)w[j], scale, 3));
+    for (int n = 0; n < kRowTokens / (kThreads / 64); ++n) {
+        const int64_t m = m0 + n;
+        if (m >= R.rows) return;
+        const uint32_t word = *reinterpret_cast<const uint32_t*>(R.codes + m * R.stride + k / 2);
+        const uint32_t byte = R.scales[b * R.scales_stride + m];
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = value_of(word, i, scale_operand(byte), byte == 255u);
+        store_values(out + m * ts + k, v, k, K, 0);
     }
 }
 
-// Tokens of a launch: fewer than 2^32 threads.
-int64_t slab_tokens(int64_t B) { return ((int64_t)1 << 31) / B; }    // (B <= 2^26)
+// Maps: as for their coding, a block of 4 or 8 adjacent tokens for a lane; the last tokens one by one.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void dequantize_mx4_map_kernel(Mx4Rows R, int64_t K, T* __restrict__ out, int64_t ks) {
+    constexpr int V = 16 / (int)sizeof(T);
+    const int64_t m = (xcd_order(blockIdx.x, gridDim.x) * 16 + (threadIdx.x & 15)) * V;
+    const int64_t b = (int64_t)blockIdx.y * (kThreads / 16) + (threadIdx.x >> 4);
+    if (b * kBlock >= K || m >= R.rows) return;
+    i32x4 w[V];
+    uint32_t byte[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int64_t at = min(m + j, R.rows - 1);
+        w[j] = *reinterpret_cast<const i32x4*>(R.codes + at * R.stride + b * 16);
+        byte[j] = R.scales[b * R.scales_stride + at];
+    }
+    const int n = (int)min((int64_t)kBlock, K - b * kBlock);
+    T* p = out + m + b * kBlock * ks;
+#pragma unroll
+    for (int k = 0; k < kBlock; ++k) {
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = value_of((uint32_t)w[j][k / 8], k % 8, scale_operand(byte[j]), byte[j] == 255u);
+        if (k < n) store_values(p + k * ks, v, m, R.rows, 0);
+    }
+}
+
+// A launch has fewer than 2^32 threads, and 65535 workgroups along y, so large calls take several: `tokens` at a
+// time, and so many blocks.
+constexpr int64_t kGridY = 65535;
+int64_t slab_tokens(int64_t B, int64_t blocks_y) {
+    const int64_t y = std::min(ceil_div64(B, blocks_y), kGridY);
+    return std::max<int64_t>(64, ((int64_t)1 << 23) / y) * 32;
+}
+
+template <typename T>
+hipError_t run_quantize(const T* x, int64_t M, int64_t K, int64_t ts, int64_t ks, uint8_t* codes, int64_t cs, uint8_t* scales,
+                        int64_t ss, hipStream_t s) {
+    const bool map = ks != 1 && K > 1, narrow = map && M < MapBlock<T>::kTokens;
+    const int64_t B = blocks_of(K);
+    if (narrow) {
+        const int64_t slab_b = (int64_t)1 << 24;        // (of fewer than 128 tokens)
+        for (int64_t b = 0; b < B; b += slab_b) {
+            const int64_t k = b * kBlock, channels = std::min(K - k, slab_b * kBlock);
+            const dim3 grid((unsigned)ceil_div64(M * blocks_of(channels), kThreads));
+            quantize_mx4_narrow_kernel<T><<<grid, kThreads, 0, s>>>(x + k * ks, M, channels, ks, codes + b * 16, cs, scales + b * ss, ss);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
+    const int64_t per_y = map ? kThreads / 16 : kRowBlocks, slab_b = kGridY * per_y, slab = slab_tokens(B, per_y);
+    for (int64_t b = 0; b < B; b += slab_b) {
+        const int64_t n_b = std::min(B - b, slab_b), k = b * kBlock;
+        for (int64_t m = 0; m < M; m += slab) {
+            int64_t n = std::min(M - m, slab), m0 = m;
+            if (map && n < MapBlock<T>::kTokens) m0 = M - MapBlock<T>::kTokens, n = MapBlock<T>::kTokens;
+            const T* p = x + m0 * (map ? 1 : ts) + k * (map ? ks : 1);
+            uint8_t *c = codes + m0 * cs + b * 16, *sc = scales + b * ss + m0;
+            const dim3 grid((unsigned)ceil_div64(n, map ? MapBlock<T>::kTokens : kRowTokens), (unsigned)ceil_div64(n_b, per_y));
+            const int64_t channels = std::min(K - k, slab_b * kBlock);
+            if (map) quantize_mx4_map_kernel<T><<<grid, kThreads, 0, s>>>(p, n, channels, ks, c, cs, sc, ss);
+            else quantize_mx4_rows_kernel<T><<<grid, kThreads, 0, s>>>(p, n, channels, ts, c, cs, sc, ss);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
+}
+
+template <typename T>
+hipError_t run_dequantize(const Mx4Rows& R, int64_t K, T* out, int64_t ts, int64_t ks, bool map, hipStream_t s) {
+    constexpr int kTokens = 16 * (16 / (int)sizeof(T));
+    const int64_t B = blocks_of(K), per_y = map ? kThreads / 16 : kRowBlocks, slab_b = kGridY * per_y;
+    const int64_t slab = slab_tokens(B, per_y);
+    for (int64_t b = 0; b < B; b += slab_b) {
+        const int64_t n_b = std::min(B - b, slab_b), k = b * kBlock, channels = std::min(K - k, slab_b * kBlock);
+        for (int64_t m = 0; m < R.rows; m += slab) {
+            const Mx4Rows P = {R.codes + m * R.stride + b * 16, R.stride, R.scales + b * R.scales_stride + m, R.scales_stride,
+                               std::min(R.rows - m, slab)};
+            const dim3 grid((unsigned)ceil_div64(P.rows, map ? kTokens : kRowTokens), (unsigned)ceil_div64(n_b, per_y));
+            T* p = out + m * (map ? 1 : ts) + k * (map ? ks : 1);
+            if (map) dequantize_mx4_map_kernel<T><<<grid, kThreads, 0, s>>>(P, channels, p, ks);
+            else dequantize_mx4_rows_kernel<T><<<grid, kThreads, 0, s>>>(P, channels, p, ts);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+    }
+    return hipSuccess;
+}
 
 }  // namespace
 
 hipError_t launch_quantize_mx4(dss_dtype dt, const void* x, int64_t M, int K, int64_t token_stride, int64_t channel_stride,
                                uint8_t* codes, int64_t codes_stride, uint8_t* scales, int64_t scales_stride, hipStream_t s) {
-    const int64_t B = blocks_of(K), slab = slab_tokens(B);
-    for (int64_t m = 0; m < M; m += slab) {
-        const int64_t n = std::min(M - m, slab), at = m * token_stride;
-        const dim3 grid((unsigned)ceil_div64(n * B, kThreads));
-        uint8_t* c = codes + m * codes_stride;
-        if (dt == DSS_BF16)
-            quantize_mx4_kernel<uint16_t><<<grid, kThreads, 0, s>>>((const uint16_t*)x + at, n, K, token_stride, channel_stride, c,
-                                                                    codes_stride, scales + m, scales_stride);
-        else
-            quantize_mx4_kernel<float><<<grid, kThreads, 0, s>>>((const float*)x + at, n, K, token_stride, channel_stride, c,
-                                                                 codes_stride, scales + m, scales_stride);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    return dt == DSS_BF16 ? run_quantize((const uint16_t*)x, M, K, token_stride, channel_stride, codes, codes_stride, scales,
+                                         scales_stride, s)
+                          : run_quantize((const float*)x, M, K, token_stride, channel_stride, codes, codes_stride, scales,
+                                         scales_stride, s);
 }
 
 dss_status check_mx4_rows(const Mx4Rows& R, int64_t B, const char* what) {
@@ -126,24 +334,16 @@ extern "C" dss_status dss_dequantize_blocks(const uint8_t* codes, int64_t codes_
     using namespace dss;
     if (out_dtype != DSS_F32 && out_dtype != DSS_BF16) return fail(DSS_E_UNSUPPORTED, "unknown dtype %d", out_dtype);
     if (M < 0 || M > kMaxTokens || K < 1) return fail(DSS_E_INVALID, "%lld tokens of %d channels", (long long)M, K);
-    const int64_t B = blocks_of(K), slab = slab_tokens(B);
-    dss_status s = check_mx4_rows({codes, codes_stride, scales, scales_stride, M}, B, "tokens");
+    const Mx4Rows R = {codes, codes_stride, scales, scales_stride, M};
+    dss_status s = check_mx4_rows(R, blocks_of(K), "tokens");
     if (s != DSS_OK) return s;
     s = check_outputs(M, K, out, out_dtype, out_token_stride, out_channel_stride);
-    if (s != DSS_OK) return s;
-    for (int64_t m = 0; m < M; m += slab) {
-        const Mx4Rows R = {codes + m * codes_stride, codes_stride, scales + m, scales_stride, std::min(M - m, slab)};
-        const dim3 grid((unsigned)ceil_div64(R.rows * B, kThreads));
-        if (out_dtype == DSS_BF16)
-            dequantize_mx4_kernel<uint16_t><<<grid, kThreads, 0, stream>>>(R, K, (uint16_t*)out + m * out_token_stride, out_token_stride,
-                                                                           out_channel_stride);
-        else
-            dequantize_mx4_kernel<float><<<grid, kThreads, 0, stream>>>(R, K, (float*)out + m * out_token_stride, out_token_stride,
-                                                                        out_channel_stride);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return hip_fail(e, "dequantize launch");
-    }
-    return DSS_OK;
+    if (s != DSS_OK || M == 0) return s;
+    const bool map = is_map(M, K, out_token_stride, out_channel_stride);
+    hipError_t e = out_dtype == DSS_BF16
+                       ? run_dequantize(R, K, (uint16_t*)out, out_token_stride, out_channel_stride, map, stream)
+                       : run_dequantize(R, K, (float*)out, out_token_stride, out_channel_stride, map, stream);
+    return e == hipSuccess ? DSS_OK : hip_fail(e, "dequantize launch");
 } catch (...) {
     return DSS_E_NOMEM;
 }
