@@ -2,162 +2,369 @@
 // over all classes,
 //   loss = s w T^2 sum_j p_j (log p_j - log r_{i_j}),   dloss / dz_c = s w T (r_c - sum_{j: i_j = c} p_j).
 //
-// Bound by memory: the logits are read and the gradient is written once.
-//
-// All exponents are taken to base 2 of differences to the largest logit, so that nothing
-// overflows; logarithms of p and r come from those differences and the sums' logarithms.
+// Bound by memory: the logits are read and the gradient is written once.  This file has the entry point
+// and the rows (a position's classes adjacent), distill_map.hip the maps.
 #include <algorithm>
 #include <cmath>
 
 #include "dev_common.h"
+#include "distill.h"
 #include "dss_internal.h"
-#include "tokens.h"
-#include "tokens_device.h"
 
 namespace dss {
 
 namespace {
 
-constexpr int kMostTop = 1024;
 constexpr int kThreads = 256;
-constexpr float kLn2 = 0.69314718055994531f;
 constexpr double kLog2e = 1.4426950408889634;
 
-// What a call asks for.
-struct Distill {
-    const void* z;
-    int64_t M, C, ts, cs;                // cs: the channels' stride
-    const void* top;
-    int top_bf16;
-    int64_t top_ts, top_ps;
-    const void* ids;
-    int ids_64;
-    int64_t ids_ts, ids_ps;
-    int k;
-    const float* weights;
-    float to_log2;                       // log2(e) / T
-    float scale, T;
-    float* losses;
-    void* grad;                          // NULL: the losses alone
-    int64_t gts, gcs;
-};
-
-__device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
-
-// The class of place j: -1 for an empty place, C for one that there is not.
-__device__ __forceinline__ int64_t class_of(const Distill& D, int64_t m, int j) {
-    const int64_t at = m * D.ids_ts + j * D.ids_ps;
-    const int64_t id = D.ids_64 ? static_cast<const int64_t*>(D.ids)[at] : (int64_t)static_cast<const int32_t*>(D.ids)[at];
-    return id < 0 ? -1 : min(id, D.C);
-}
-__device__ __forceinline__ float teacher_of(const Distill& D, int64_t m, int j) {
-    const int64_t at = m * D.top_ts + j * D.top_ps;
-    return D.top_bf16 ? to_f32(static_cast<const uint16_t*>(D.top)[at]) : static_cast<const float*>(D.top)[at];
-}
-
-// Over a workgroup's threads.  `room` has a place for each wave; two calls in a row need a barrier between.
-struct Max {
-    static __device__ __forceinline__ float of(float a, float b) { return fmaxf(a, b); }
-};
-struct Sum {
-    static __device__ __forceinline__ float of(float a, float b) { return a + b; }
-};
-template <typename Op>
-__device__ __forceinline__ float over_threads(float v, float* room) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v = Op::of(v, __shfl_xor(v, d));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = room[0];
-    for (int w = 1; w < (int)blockDim.x / 64; ++w) v = Op::of(v, room[w]);
-    return v;
-}
-
-// A workgroup for each position.
+// ------------------------------------------------------------------ any strides
+// A workgroup for each position, which reads its logits three times: maps with long lists, or of few positions.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void distill_kernel(Distill D) {
-    __shared__ float room[kThreads / 64];
+    __shared__ float room[kThreads / 64 * 2];
     __shared__ float p[kMostTop];
-    __shared__ int64_t ids[kMostTop];
+    __shared__ int ids[kMostTop];
     const int64_t m = blockIdx.x;
     const T* z = static_cast<const T*>(D.z) + m * D.ts;
     T* grad = static_cast<T*>(D.grad) + m * D.gts;
     const float weight = D.weights ? D.weights[m] : 1.f;
     constexpr int J = kMostTop / kThreads;
-    float t[J], zj[J];
-    int64_t id[J];
-    float t_max = -INFINITY;
-    int state = 0;                       // 1: a place that counts (a NaN does), 2: a class that there is not
+    Place a[J];
+    float lists[2] = {-INFINITY, 0.f};
 #pragma unroll
     for (int n = 0; n < J; ++n) {
         const int j = n * kThreads + threadIdx.x;
-        id[n] = j < D.k ? class_of(D, m, j) : -1;
-        t[n] = id[n] >= 0 ? teacher_of(D, m, j) : -INFINITY;
-        zj[n] = id[n] >= 0 && id[n] < D.C ? to_f32(z[id[n] * D.cs]) : 0.f;
-        state |= (t[n] != -INFINITY ? 1 : 0) | (id[n] >= D.C ? 3 : 0);
-        t_max = fmaxf(t_max, t[n]);
+        a[n] = j < D.k ? place_of(D, m, j, z) : Place{-1, -INFINITY, 0.f};
+        lists[0] = fmaxf(lists[0], a[n].t);
+        lists[1] = fmaxf(lists[1], a[n].state(D));
     }
-    t_max = over_threads<Max>(t_max, room);
-    const bool wrong = __syncthreads_or(state & 2);
-    if (!__syncthreads_or(state & 1) || weight == 0.f) {         // not to be learnt
+    over_lanes<Max, kThreads>(lists, room);
+    const float t_max = lists[0];
+    if (weight == 0.f || lists[1] == 0.f) {                      // not to be learnt
         if (threadIdx.x == 0) D.losses[m] = 0.f;
         if (D.grad)
             for (int64_t c = threadIdx.x; c < D.C; c += kThreads) store_elem(grad + c * D.gcs, 0.f);
         return;
     }
-    const float nan = wrong ? __uint_as_float(0x7fc00000u) : 0.f;
-    float sum_p = 0.f;
+    const float nan = lists[1] == 3.f ? quiet_nan() : 0.f;
+    float z_max[1] = {-INFINITY};
+    for (int64_t c = threadIdx.x; c < D.C; c += kThreads) z_max[0] = fmaxf(z_max[0], to_f32(z[c * D.cs]));
+    over_lanes<Max, kThreads>(z_max, room);
+    float sums[2] = {0.f, 0.f};
 #pragma unroll
-    for (int n = 0; n < J; ++n) sum_p += t[n] == -INFINITY ? 0.f : exp2_of((t[n] - t_max) * D.to_log2);
-    sum_p = over_threads<Sum>(sum_p, room) + nan;
-    float z_max = -INFINITY;
-    for (int64_t c = threadIdx.x; c < D.C; c += kThreads) z_max = fmaxf(z_max, to_f32(z[c * D.cs]));
-    z_max = over_threads<Max>(z_max, room);
-    float sum_r = 0.f;
-    for (int64_t c = threadIdx.x; c < D.C; c += kThreads) sum_r += exp2_of((to_f32(z[c * D.cs]) - z_max) * D.to_log2);
-    sum_r = over_threads<Sum>(sum_r, room);
-    // log r - log p = (z - z_max - t + t_max) / T + log(sum_p / sum_r)
-    const float log_sums = logf(sum_p) - logf(sum_r), per_T = D.to_log2 * kLn2;
-    float loss = 0.f;
+    for (int n = 0; n < J; ++n) sums[0] += weight_of(D, a[n].t, t_max);
+    for (int64_t c = threadIdx.x; c < D.C; c += kThreads) sums[1] += exp2_of((to_f32(z[c * D.cs]) - z_max[0]) * D.to_log2);
+    over_lanes<Sum, kThreads>(sums, room);
+    const float sum_p = sums[0] + nan, sum_r = sums[1] + nan, log_sums = logf(sum_p) - logf(sum_r);
+    float loss[1] = {0.f};
 #pragma unroll
     for (int n = 0; n < J; ++n) {
         const int j = n * kThreads + threadIdx.x;
         if (j >= D.k) continue;
-        const float pj = (t[n] == -INFINITY ? 0.f : exp2_of((t[n] - t_max) * D.to_log2)) / sum_p;
-        if (!(pj <= 0.f)) loss += pj * (((t[n] - t_max) - (zj[n] - z_max)) * per_T - log_sums);
-        p[j] = pj;
-        ids[j] = id[n];
+        p[j] = weight_of(D, a[n].t, t_max) / sum_p;
+        ids[j] = a[n].id;
+        loss[0] += loss_of(D, p[j], a[n].t, t_max, a[n].z, z_max[0], log_sums);
     }
-    loss = over_threads<Sum>(loss, room);    // (with barriers: p and ids are there)
+    over_lanes<Sum, kThreads>(loss, room);   // (with barriers: p and ids are there)
     const float sw = D.scale * weight;
-    if (threadIdx.x == 0) D.losses[m] = sw * D.T * (D.T * loss);
+    if (threadIdx.x == 0) D.losses[m] = sw * D.T * (D.T * loss[0]);
     if (!D.grad) return;
-    const float g = sw * D.T, per_sum = 1.f / sum_r + nan;
+    const float g = sw * D.T, per_sum = 1.f / sum_r;
     for (int64_t c = threadIdx.x; c < D.C; c += kThreads)
-        store_elem(grad + c * D.gcs, g * (exp2_of((to_f32(z[c * D.cs]) - z_max) * D.to_log2) * per_sum));
+        store_elem(grad + c * D.gcs, g * (exp2_of((to_f32(z[c * D.cs]) - z_max[0]) * D.to_log2) * per_sum));
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < J; ++n) {
         const int j = n * kThreads + threadIdx.x;
-        if (j >= D.k || id[n] < 0 || id[n] >= D.C) continue;
+        if (j >= D.k || a[n].id < 0 || a[n].id >= (int)D.C) continue;
         float of_class = 0.f;            // (a class may be there more than once)
-        for (int i = 0; i < D.k; ++i) of_class += ids[i] == id[n] ? p[i] : 0.f;
-        store_elem(grad + id[n] * D.gcs, g * (exp2_of((zj[n] - z_max) * D.to_log2) * per_sum - of_class));
+        for (int i = 0; i < D.k; ++i) of_class += ids[i] == a[n].id ? p[i] : 0.f;
+        store_elem(grad + a[n].id * D.gcs, g * (exp2_of((a[n].z - z_max[0]) * D.to_log2) * per_sum - of_class));
     }
 }
 
-hipError_t launch_distill(const Distill& D, dss_dtype dt, hipStream_t s) {
+// ------------------------------------------------------------------ rows
+// A position's list in LDS: the teacher's logits (then p), the student's, and the classes.
+struct List {
+    float *t, *z;
+    int* id;
+
+    static __host__ __device__ size_t bytes(int k) { return (size_t)k * 12; }
+    __device__ __forceinline__ List(char* lds, int k) : t((float*)lds), z(t + k), id((int*)(z + k)) {}
+    // The sum of p over the places of a class, in the places' order.
+    __device__ __forceinline__ float of_class(int c, int k) const {
+        float s = 0.f;
+        for (int i = 0; i < k; ++i) s += id[i] == c ? t[i] : 0.f;
+        return s;
+    }
+};
+
+// LPR threads hold a position's logits, CH chunks each, in registers: they are read once.
+template <typename T, int LPR, int CH>
+__global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_kernel(Distill D) {
+    constexpr int E = Chunk<T>::E, ROWS = LPR < kThreads ? kThreads / LPR : 1;
+    __shared__ float room[LPR > 64 ? LPR / 64 * 3 : 1];
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x % LPR, row = threadIdx.x / LPR, k = D.k;
+    const int64_t m_own = (int64_t)blockIdx.x * ROWS + row, m = min(m_own, D.M - 1);
+    const T* z = static_cast<const T*>(D.z) + m * D.ts;
+    const float weight = D.weights ? D.weights[m] : 1.f;
+    const List list(lds + row * List::bytes(k), k);
+    Chunk<T> c[CH];
+    const int C = weight == 0.f ? 0 : (int)D.C, last = C / E;    // the chunk that C ends in, if it ends in one
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        c[i] = no_logits<T>();
+        if (i * LPR + lane < last) __builtin_memcpy(&c[i], z + (i * LPR + lane) * E, 16);
+    }
+    if (C % E != 0 && last % LPR == lane) {
+        const Chunk<T> end = load_logits(z + last * E, C % E);
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+            if (i == last / LPR) c[i] = end;
+    }
+    float tops[3] = {-INFINITY, 0.f, -INFINITY};       // of the list, its state, of the logits
+    for (int j = lane; j < k; j += LPR) {
+        const Place a = place_of(D, m, j, z);
+        list.t[j] = a.t;
+        list.z[j] = a.z;
+        list.id[j] = a.id;
+        tops[0] = fmaxf(tops[0], a.t);
+        tops[1] = fmaxf(tops[1], a.state(D));
+    }
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        tops[2] = top_of(tops[2], c[i]);
+        forget(c[i]);
+    }
+    over_lanes<Max, LPR>(tops, room);
+    const float t_max = tops[0], z_max = tops[2];
+    const bool live = weight != 0.f && tops[1] != 0.f;
+    const float nan = tops[1] == 3.f ? quiet_nan() : 0.f;
+    float sums[2] = {0.f, 0.f};
+    for (int j = lane; j < k; j += LPR) sums[0] += weight_of(D, list.t[j], t_max);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        float part = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float v = exp2_of((c[i].value(e) - z_max) * D.to_log2);
+            if constexpr (E == 4) c[i].w[e] = __float_as_uint(v);     // (bfloat16 has no room for it)
+            part += v;
+        }
+        sums[1] += part;
+        forget(c[i]);
+    }
+    over_lanes<Sum, LPR>(sums, room);
+    const float sum_p = sums[0] + nan, sum_r = sums[1] + nan, log_sums = logf(sum_p) - logf(sum_r);
+    float loss[1] = {0.f};
+    for (int j = lane; j < k; j += LPR) {
+        const float t = list.t[j], p = weight_of(D, t, t_max) / sum_p;
+        loss[0] += loss_of(D, p, t, t_max, list.z[j], z_max, log_sums);
+        list.t[j] = p;
+    }
+    over_lanes<Sum, LPR>(loss, room);
+    const float sw = D.scale * weight;
+    if (lane == 0 && m_own < D.M) D.losses[m] = live ? sw * D.T * (D.T * loss[0]) : 0.f;
+    if (!D.grad) return;
+    const float g = sw * D.T, per_sum = 1.f / sum_r;
+    T* grad = static_cast<T*>(D.grad) + m * D.gts;
+    if (m_own < D.M) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int at = (i * LPR + lane) * E;
+            if (at >= (int)D.C) continue;
+            float v[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                v[e] = E == 4 ? c[i].value(e) : exp2_of((c[i].value(e) - z_max) * D.to_log2);
+                v[e] = live ? g * (v[e] * per_sum) : 0.f;
+            }
+            store_gradients(grad + at, v, D.C - at);
+        }
+    }
+    __syncthreads();                     // the classes of the list are stored over
+    if (m_own >= D.M || !live) return;
+    for (int j = lane; j < k; j += LPR) {
+        const int id = list.id[j];
+        if (id >= 0 && id < (int)D.C)
+            store_elem(grad + id, g * (exp2_of((list.z[j] - z_max) * D.to_log2) * per_sum - list.of_class(id, k)));
+    }
+}
+
+// Rows longer than the registers hold, or too few for the units: `parts` workgroups share a position's classes.  First
+// each takes its part's largest logit and sum.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void distill_parts_kernel(Distill D, int64_t per_part, Part* parts) {
+    constexpr int E = Chunk<T>::E, U = 8;
+    __shared__ float room[kThreads / 64];
+    const int64_t m = blockIdx.y, c0 = blockIdx.x * per_part, c1 = min(c0 + per_part, D.C);
+    if (D.weights && D.weights[m] == 0.f) return;
+    const T* z = static_cast<const T*>(D.z) + m * D.ts;
+    Part own = {-INFINITY, 0.f};
+    for (int64_t at = c0 + threadIdx.x * E; at < c1; at += U * kThreads * E) {
+        Chunk<T> c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) c[u] = load_logits(z + at + u * kThreads * E, c1 - at - u * kThreads * E);
+        float top = own.top;
+#pragma unroll
+        for (int u = 0; u < U; ++u) top = top_of(top, c[u]);
+        const float to = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum += exp2_of((c[u].value(e) - to) * D.to_log2);
+        own.sum = own.sum * exp2_of((own.top - to) * D.to_log2) + sum;
+        own.top = top;
+    }
+    float top[1] = {own.top};
+    over_lanes<Max, kThreads>(top, room);
+    float sum[1] = {joined(D, {top[0], 0.f}, own).sum};
+    over_lanes<Sum, kThreads>(sum, room);
+    if (threadIdx.x == 0) parts[m * gridDim.x + blockIdx.x] = {top[0], sum[0]};
+}
+
+// Then the loss (workgroups 0 of a position) and the gradient of their parts.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill D, int64_t per_part, const Part* parts, int n_parts,
+                                                                  int with_loss) {
+    constexpr int E = Chunk<T>::E, U = 4;
+    __shared__ float room[kThreads / 64 * 3];
+    extern __shared__ __align__(16) char lds[];
+    const int64_t m = blockIdx.y, c0 = blockIdx.x * per_part, c1 = min(c0 + per_part, D.C);
+    const int k = D.k;
+    const T* z = static_cast<const T*>(D.z) + m * D.ts;
+    T* grad = static_cast<T*>(D.grad) + m * D.gts;
+    const float weight = D.weights ? D.weights[m] : 1.f;
+    const List list(lds, k);
+    float tops[3] = {-INFINITY, 0.f, -INFINITY};
+    for (int j = threadIdx.x; j < k; j += kThreads) {
+        // (the student's logits of other parts may be their gradients already, if these are written over them)
+        const int id = class_of(D, m, j);
+        const bool own = id >= c0 && id < c1;
+        list.id[j] = id;
+        list.t[j] = id >= 0 ? teacher_of(D, m, j) : -INFINITY;
+        list.z[j] = id >= 0 && id < (int)D.C && (own || (with_loss && blockIdx.x == 0)) ? to_f32(z[id]) : 0.f;
+        tops[0] = fmaxf(tops[0], list.t[j]);
+        tops[1] = fmaxf(tops[1], Place{id, list.t[j], 0.f}.state(D));
+    }
+    Part own = {-INFINITY, 0.f};
+    if (weight != 0.f)
+        for (int p = threadIdx.x; p < n_parts; p += kThreads) own = joined(D, own, parts[m * n_parts + p]);
+    tops[2] = own.top;
+    over_lanes<Max, kThreads>(tops, room);
+    const float t_max = tops[0], z_max = tops[2];
+    const bool live = weight != 0.f && tops[1] != 0.f;
+    const float nan = tops[1] == 3.f ? quiet_nan() : 0.f;
+    float sums[2] = {0.f, joined(D, {z_max, 0.f}, own).sum};
+    for (int j = threadIdx.x; j < k; j += kThreads) sums[0] += weight_of(D, list.t[j], t_max);
+    over_lanes<Sum, kThreads>(sums, room);
+    // (a row of -infinities has the sum 0 here, and no softmax)
+    const float sum_p = sums[0] + nan, sum_r = z_max == -INFINITY ? quiet_nan() : sums[1] + nan;
+    const float log_sums = logf(sum_p) - logf(sum_r);
+    float loss[1] = {0.f};
+    for (int j = threadIdx.x; j < k; j += kThreads) {
+        const float t = list.t[j], p = weight_of(D, t, t_max) / sum_p;
+        loss[0] += loss_of(D, p, t, t_max, list.z[j], z_max, log_sums);
+        list.t[j] = p;
+    }
+    over_lanes<Sum, kThreads>(loss, room);
+    const float sw = D.scale * weight;
+    if (threadIdx.x == 0 && blockIdx.x == 0 && with_loss) D.losses[m] = live ? sw * D.T * (D.T * loss[0]) : 0.f;
+    if (!D.grad) return;
+    const float g = sw * D.T, per_sum = 1.f / sum_r;
+    for (int64_t at = c0 + threadIdx.x * E; at < c1; at += U * kThreads * E) {
+        Chunk<T> c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) c[u] = load_logits(z + at + u * kThreads * E, live ? c1 - at - u * kThreads * E : 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = live ? g * (exp2_of((c[u].value(e) - z_max) * D.to_log2) * per_sum) : 0.f;
+            const int64_t from = at + u * kThreads * E;
+            if (from < c1) store_gradients(grad + from, v, c1 - from);
+        }
+    }
+    __syncthreads();                     // the classes of the list are stored over
+    if (!live) return;
+    for (int j = threadIdx.x; j < k; j += kThreads) {
+        const int id = list.id[j];
+        if (id >= c0 && id < c1)
+            store_elem(grad + id, g * (exp2_of((list.z[j] - z_max) * D.to_log2) * per_sum - list.of_class(id, k)));
+    }
+}
+
+template <typename T, int LPR, int CH>
+hipError_t run_rows(const Distill& D, hipStream_t s) {
+    constexpr int ROWS = LPR < kThreads ? kThreads / LPR : 1;
+    distill_rows_kernel<T, LPR, CH><<<dim3((unsigned)ceil_div64(D.M, ROWS)), ROWS * LPR, ROWS * List::bytes(D.k), s>>>(D);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_parts(const Distill& D, Part* parts, hipStream_t s) {
+    // enough workgroups for the units, of at least some thousand classes each
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(1024 / D.M, D.C / 4096));
+    const int64_t per_part = ceil_div64(ceil_div64(D.C, most), 64) * 64, n = ceil_div64(D.C, per_part);
+    distill_parts_kernel<T><<<dim3((unsigned)n, (unsigned)D.M), kThreads, 0, s>>>(D, per_part, parts);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const bool over = D.grad == D.z;     // the losses need all of the logits first
+    Distill L = D;
+    if (over) L.grad = nullptr;
+    if (over || !D.grad) {
+        distill_finish_kernel<T><<<dim3(1, (unsigned)D.M), kThreads, List::bytes(D.k), s>>>(L, D.C, parts, (int)n, 1);
+        e = hipGetLastError();
+        if (e != hipSuccess || !D.grad) return e;
+    }
+    distill_finish_kernel<T><<<dim3((unsigned)n, (unsigned)D.M), kThreads, List::bytes(D.k), s>>>(D, per_part, parts, (int)n, !over);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_distill(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
+    constexpr int E = Chunk<T>::E;
+    const bool long_rows = D.C > 1024 * 16 * E || (!D.grad && D.C > 256 * 16 * E);
+    if (long_rows || (D.M < 128 && D.C >= 16384)) {
+        // (a launch has 65535 workgroups along y)
+        const int64_t slab = 4096;
+        for (int64_t m = 0; m < D.M; m += slab) {
+            const hipError_t e = run_parts<T>(positions(D, dt, m, std::min(D.M - m, slab)), parts, s);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
     for (int64_t m = 0; m < D.M; m += kSlabTokens) {
-        Distill S = D;
-        S.M = std::min(D.M - m, kSlabTokens);
-        const int64_t es = (int64_t)dtype_size(dt);
-        S.z = static_cast<const char*>(D.z) + m * D.ts * es;
-        S.top = static_cast<const char*>(D.top) + m * D.top_ts * (D.top_bf16 ? 2 : 4);
-        S.ids = static_cast<const char*>(D.ids) + m * D.ids_ts * (D.ids_64 ? 8 : 4);
-        if (D.weights) S.weights = D.weights + m;
-        S.losses = D.losses + m;
-        if (D.grad) S.grad = static_cast<char*>(D.grad) + m * D.gts * es;
+        const Distill S = positions(D, dt, m, std::min(D.M - m, kSlabTokens));
+        // as few threads for a row as hold it, and the lists of their workgroup's rows in 48 KB of LDS
+        const int64_t rows = (int64_t)(48 * 1024 / List::bytes(D.k));
+        hipError_t e;
+        if (D.C <= 4 * 4 * E && rows >= 64) e = run_rows<T, 4, 4>(S, s);
+        else if (D.C <= 16 * 4 * E && rows >= 16) e = run_rows<T, 16, 4>(S, s);
+        else if (D.C <= 64 * 4 * E && rows >= 4) e = run_rows<T, 64, 4>(S, s);
+        else if (D.C <= 256 * 4 * E) e = run_rows<T, 256, 4>(S, s);
+        else if (D.C <= 256 * 16 * E) e = run_rows<T, 256, 16>(S, s);
+        else e = run_rows<T, 1024, 16>(S, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_distill(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
+    if (D.cs == 1 || D.C == 1)
+        return dt == DSS_BF16 ? run_distill<uint16_t>(D, dt, parts, s) : run_distill<float>(D, dt, parts, s);
+    return launch_distill_map(D, dt, parts, s);
+}
+
+}  // namespace
+
+// A workgroup for each position.
+hipError_t launch_distill_any(const Distill& D, dss_dtype dt, hipStream_t s) {
+    for (int64_t m = 0; m < D.M; m += kSlabTokens) {
+        const Distill S = positions(D, dt, m, std::min(D.M - m, kSlabTokens));
         const dim3 grid((unsigned)S.M);
         if (dt == DSS_BF16) distill_kernel<uint16_t><<<grid, kThreads, 0, s>>>(S);
         else distill_kernel<float><<<grid, kThreads, 0, s>>>(S);
@@ -167,7 +374,18 @@ hipError_t launch_distill(const Distill& D, dss_dtype dt, hipStream_t s) {
     return hipSuccess;
 }
 
-}  // namespace
+Distill positions(const Distill& D, dss_dtype dt, int64_t m, int64_t n) {
+    Distill S = D;
+    const int64_t es = (int64_t)dtype_size(dt);
+    S.M = n;
+    S.z = static_cast<const char*>(D.z) + m * D.ts * es;
+    S.top = static_cast<const char*>(D.top) + m * D.top_ts * (D.top_bf16 ? 2 : 4);
+    S.ids = static_cast<const char*>(D.ids) + m * D.ids_ts * (D.ids_64 ? 8 : 4);
+    if (D.weights) S.weights = D.weights + m;
+    S.losses = D.losses + m;
+    if (D.grad) S.grad = static_cast<char*>(D.grad) + m * D.gts * es;
+    return S;
+}
 
 }  // namespace dss
 
@@ -199,6 +417,8 @@ extern "C" dss_status dss_distill_tokens(const void* logits, dss_dtype dtype, in
             return fail(DSS_E_INVALID, "gradient strides %lld (tokens) and %lld (channels) for logits of %lld and %lld",
                         (long long)grad_token_stride, (long long)grad_channel_stride, (long long)token_stride,
                         (long long)channel_stride);
+        if (grad == logits && ((grad_token_stride != token_stride && M > 1) || (grad_channel_stride != channel_stride && C > 1)))
+            return fail(DSS_E_INVALID, "a gradient over the logits with other strides");
         if ((uintptr_t)grad % dtype_size(dtype) != 0) return fail(DSS_E_INVALID, "grad is not aligned to its elements");
     }
     if (M == 0) return DSS_OK;
@@ -213,7 +433,7 @@ extern "C" dss_status dss_distill_tokens(const void* logits, dss_dtype dtype, in
                        top->place_stride, top->ids, top->id_bytes == 8, top->id_token_stride, top->id_place_stride,
                        top->count, token_weights, (float)to_log2, scale, temperature, losses, grad, grad_token_stride,
                        grad_channel_stride};
-    hipError_t e = launch_distill(D, dtype, stream);
+    hipError_t e = launch_distill(D, dtype, static_cast<Part*>(workspace), stream);
     return e == hipSuccess ? DSS_OK : hip_fail(e, "distillation launch");
 } catch (...) {
     return DSS_E_NOMEM;

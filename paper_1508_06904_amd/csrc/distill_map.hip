@@ -1,0 +1,482 @@
+// Distillation from a teacher's top logits on maps: a class's positions are adjacent (distill.hip has the formulas).
+//
+// Bound by memory as the rows: the logits are read and the gradient is written once where a tile's logits fit LDS or
+// registers (up to 1024 classes); of more classes they are read twice.
+#include <algorithm>
+
+#include "dev_common.h"
+#include "distill.h"
+#include "dss_internal.h"
+
+namespace dss {
+
+namespace {
+
+// ------------------------------------------------------------------ few classes
+// A lane for each position, its logits in a column of LDS that no other lane touches: lists are gathered and gradients
+// of listed classes put together there, with no barrier.  Of a class that is in the list (its bit in `listed`) the column has the
+// gradient in the end, of any other one the logit.
+constexpr int kColumns = 128;            // classes at most
+
+template <typename T>
+__global__ void distill_columns_kernel(Distill D) {
+    extern __shared__ float columns[];
+    const int C = (int)D.C, lane = threadIdx.x & 63, k = D.k;
+    float* const col = columns + (threadIdx.x >> 6) * C * 64 + lane;
+    const int64_t own = xcd_order(blockIdx.x, gridDim.x) * blockDim.x + threadIdx.x, m = min(own, D.M - 1);
+    const T* z = static_cast<const T*>(D.z) + m;
+    constexpr int U = 16;
+    float z_max = -INFINITY;
+    for (int c0 = 0; c0 < C; c0 += U) {
+        float v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = to_f32(z[min(c0 + u, C - 1) * D.cs]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (c0 + u < C) {
+                col[(c0 + u) * 64] = v[u];
+                z_max = fmaxf(z_max, v[u]);
+            }
+    }
+    const float weight = D.weights ? D.weights[m] : 1.f;
+    float t_max = -INFINITY, state = 0.f;
+    for (int j = 0; j < k; ++j) {
+        const int id = class_of(D, m, j);
+        const float t = id >= 0 ? teacher_of(D, m, j) : -INFINITY;
+        t_max = fmaxf(t_max, t);
+        state = fmaxf(state, Place{id, t, 0.f}.state(D));
+    }
+    const bool live = weight != 0.f && state != 0.f;
+    const float nan = state == 3.f ? quiet_nan() : 0.f;
+    float sum_r = nan, sum_p = nan;
+    for (int c0 = 0; c0 < C; c0 += U) {
+        float part = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (c0 + u < C) part += exp2_of((col[(c0 + u) * 64] - z_max) * D.to_log2);
+        sum_r += part;
+    }
+    for (int j = 0; j < k; ++j)
+        if (class_of(D, m, j) >= 0) sum_p += weight_of(D, teacher_of(D, m, j), t_max);
+    const float log_sums = logf(sum_p) - logf(sum_r), per_sum = 1.f / sum_r;
+    float loss = 0.f;
+    for (int j = 0; j < k; ++j) {
+        const int id = class_of(D, m, j);
+        if (id < 0 || id >= C) continue;
+        const float t = teacher_of(D, m, j);
+        loss += loss_of(D, weight_of(D, t, t_max) / sum_p, t, t_max, col[id * 64], z_max, log_sums);
+    }
+    const float sw = D.scale * weight, g = sw * D.T;
+    if (own < D.M) D.losses[m] = live ? sw * D.T * (D.T * (loss + nan)) : 0.f;
+    if (!D.grad) return;
+    uint32_t listed[kColumns / 32] = {};
+    for (int j = 0; j < k; ++j) {
+        const int id = class_of(D, m, j);
+        if (id < 0 || id >= C) continue;
+        const float p = weight_of(D, teacher_of(D, m, j), t_max) / sum_p;
+        float v = col[id * 64];
+        bool before = false;
+#pragma unroll
+        for (int w = 0; w < kColumns / 32; ++w) {
+            const uint32_t bit = id / 32 == w ? 1u << (id % 32) : 0u;
+            before |= (listed[w] & bit) != 0;
+            listed[w] |= bit;
+        }
+        if (!before) v = exp2_of((v - z_max) * D.to_log2) * per_sum;
+        col[id * 64] = v - p;
+    }
+    T* grad = static_cast<T*>(D.grad) + m;
+#pragma unroll
+    for (int w = 0; w < kColumns / 32; ++w) {
+#pragma unroll 8
+        for (int c = w * 32; c < min(w * 32 + 32, C); ++c) {
+            float v = col[c * 64];
+            if (!(listed[w] >> (c % 32) & 1)) v = exp2_of((v - z_max) * D.to_log2) * per_sum;
+            if (own < D.M) store_elem(grad + c * D.gcs, live ? g * v : 0.f);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ tiles
+// A workgroup has the 16 V positions of 16 lanes with 16 bytes each; a lane has 16 adjacent classes of its V positions, so a
+// wave has 64 classes.
+template <typename T>
+struct Tile {
+    static constexpr int V = Chunk<T>::E, kTokens = 16 * V;
+    Chunk<T> c[16];
+
+    // The lane's classes c0 .. c0+15, those below C, of the V positions from p on; -infinity elsewhere.
+    __device__ __forceinline__ void load(const T* p, int64_t cs, int c0, int C) {
+        p += c0 * cs;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            c[r] = no_logits<T>();
+            if (c0 + r < C) __builtin_memcpy(&c[r], p, 16);
+            p += cs;
+        }
+    }
+    // The same of the first n positions from p on.
+    __device__ __forceinline__ void load(const T* p, int64_t cs, int64_t c0, int64_t C, int64_t n) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) c[r] = load_logits(p + (c0 + r) * cs, c0 + r < C ? n : 0);
+    }
+    __device__ __forceinline__ void raise_into(float (&top)[V]) const {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+            for (int v = 0; v < V; ++v) top[v] = fmaxf(top[v], c[r].value(v));
+    }
+};
+
+// Each position's value over the lanes that have it; room has V * 16 places for each wave.
+template <typename Op, int V>
+__device__ __forceinline__ void over_tile(float (&v)[V], float* room) {
+    const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        v[j] = Op::of(v[j], __shfl_xor(v[j], 16));
+        v[j] = Op::of(v[j], __shfl_xor(v[j], 32));
+    }
+    __syncthreads();
+    if (lane < 16)
+#pragma unroll
+        for (int j = 0; j < V; ++j) room[((threadIdx.x >> 6) * 16 + lane) * V + j] = v[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = room[(lane & 15) * V + j];
+    for (int w = 1; w < waves; ++w)
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = Op::of(v[j], room[(w * 16 + (lane & 15)) * V + j]);
+}
+
+// What a position's gradient is made of, and its list: classes and the student's logits there (of classes c0 .. c1-1
+// and, with a loss to form, all). In LDS, the positions of a tile adjacent.
+template <typename T>
+struct Lists {
+    static constexpr int N = Tile<T>::kTokens;
+    static constexpr int kZMax = 0, kPerSum = N, kTMax = 2 * N, kSumP = 3 * N, kG = 4 * N, kLive = 5 * N, kIds = 6 * N;
+    float* at;
+    int k;
+
+    static __host__ __device__ size_t bytes(int k) { return (size_t)N * (6 + 2 * k) * 4; }
+    __device__ __forceinline__ int& id(int n) const { return reinterpret_cast<int*>(at)[kIds + n]; }
+    __device__ __forceinline__ float& z(int n) const { return at[kIds + k * N + n]; }
+
+    __device__ __forceinline__ void fill(const Distill& D, int64_t m0, const T* logits, int64_t c0, int64_t c1) const {
+        for (int n = threadIdx.x; n < D.k * N; n += blockDim.x) {
+            const int64_t m = min(m0 + n % N, D.M - 1);
+            const int c = class_of(D, m, n / N);
+            id(n) = c;
+            z(n) = c >= c0 && c < c1 ? to_f32(logits[m + c * D.cs]) : 0.f;
+        }
+    }
+    // Of position n: its stats, and its loss if that is to be written.  sum_r is NaN or above 0.
+    __device__ __forceinline__ void finish(const Distill& D, int64_t m0, int n, float top, float sum_r, bool with_loss) const {
+        const int64_t m = m0 + n;
+        if (m >= D.M) return;
+        const float weight = D.weights ? D.weights[m] : 1.f;
+        float tm = -INFINITY, state = 0.f;
+        for (int j = 0; j < D.k; ++j) {
+            const int c = id(j * N + n);
+            const float t = c >= 0 ? teacher_of(D, m, j) : -INFINITY;
+            tm = fmaxf(tm, t);
+            state = fmaxf(state, Place{c, t, 0.f}.state(D));
+        }
+        const float nan = state == 3.f ? quiet_nan() : 0.f;
+        float sum_p = nan;
+        for (int j = 0; j < D.k; ++j)
+            if (id(j * N + n) >= 0) sum_p += weight_of(D, teacher_of(D, m, j), tm);
+        sum_r += nan;
+        const float sw = D.scale * weight;
+        const bool learn = weight != 0.f && state != 0.f;
+        at[kZMax + n] = top;
+        at[kPerSum + n] = 1.f / sum_r;
+        at[kTMax + n] = tm;
+        at[kSumP + n] = sum_p;
+        at[kG + n] = sw * D.T;
+        at[kLive + n] = learn ? 1.f : 0.f;
+        if (!with_loss) return;
+        const float log_sums = logf(sum_p) - logf(sum_r);
+        float loss = nan;
+        for (int j = 0; j < D.k; ++j) {
+            if (id(j * N + n) < 0) continue;
+            const float t = teacher_of(D, m, j);
+            loss += loss_of(D, weight_of(D, t, tm) / sum_p, t, tm, z(j * N + n), top, log_sums);
+        }
+        D.losses[m] = learn ? sw * D.T * (D.T * loss) : 0.f;
+    }
+    // The gradients of the listed classes c0 .. c1-1, after all others are written, of positions `first` on.
+    __device__ __forceinline__ void listed(const Distill& D, int64_t m0, T* grad, int64_t c0, int64_t c1, int first = 0) const {
+        for (int n = threadIdx.x; n < D.k * N; n += blockDim.x) {
+            const int own = n % N, c = id(n);
+            const int64_t m = m0 + own;
+            if (own < first || m >= D.M || c < c0 || c >= c1 || at[kLive + own] == 0.f) continue;
+            float of_class = 0.f;        // (a class may be there more than once)
+            for (int i = 0; i < D.k; ++i)
+                if (id(i * N + own) == c) of_class += weight_of(D, teacher_of(D, m, i), at[kTMax + own]) / at[kSumP + own];
+            const float r = exp2_of((z(n) - at[kZMax + own]) * D.to_log2) * at[kPerSum + own];
+            store_elem(grad + m + c * D.gcs, at[kG + own] * (r - of_class));
+        }
+    }
+};
+
+// Up to 1024 classes: the tile's logits stay in registers.  Whole tiles only: the last one ends with the last
+// position and writes those from `first` on, which the one before it does not have.  (What it reads of the others
+// may be their gradients already, if these are written over the logits; positions do not mix.)
+template <typename T>
+__global__ __launch_bounds__(1024) void distill_tile_kernel(Distill D) {
+    constexpr int V = Tile<T>::V, N = Tile<T>::kTokens;
+    extern __shared__ __align__(16) char lds[];
+    const Lists<T> lists = {reinterpret_cast<float*>(lds), D.k};
+    float* room = reinterpret_cast<float*>(lds + Lists<T>::bytes(D.k));
+    const int64_t tile0 = xcd_order(blockIdx.x, gridDim.x) * N, m0 = min(tile0, D.M - N);
+    const int first = (int)(tile0 - m0);
+    const int l16 = threadIdx.x & 15;
+    const int64_t m = m0 + l16 * V;
+    const T* z = static_cast<const T*>(D.z);
+    const int C = (int)D.C;
+    int c0 = (threadIdx.x >> 4) * 16;
+    Tile<T> tile;
+    tile.load(z + m, D.cs, c0, C);
+    lists.fill(D, m0, z, 0, D.C);
+    float top[V], sum[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) top[v] = -INFINITY, sum[v] = 0.f;
+    tile.raise_into(top);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) forget(tile.c[r]);
+    over_tile<Max>(top, room);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float e = exp2_of((tile.c[r].value(v) - top[v]) * D.to_log2);
+            if constexpr (V == 4) tile.c[r].w[v] = __float_as_uint(e);       // (bfloat16 has no room for it)
+            sum[v] += e;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) forget(tile.c[r]);
+    over_tile<Sum>(sum, room);           // (with barriers: the lists are there)
+    if (threadIdx.x < 16)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            lists.at[Lists<T>::kZMax + l16 * V + v] = top[v];
+            lists.at[Lists<T>::kPerSum + l16 * V + v] = sum[v];
+        }
+    __syncthreads();
+    for (int n = first + threadIdx.x; n < N; n += blockDim.x) lists.finish(D, m0, n, lists.at[Lists<T>::kZMax + n], lists.at[Lists<T>::kPerSum + n], true);
+    if (!D.grad) return;
+    __syncthreads();
+    T* grad = static_cast<T*>(D.grad);
+    float per[V];
+    uint32_t live = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        per[v] = lists.at[Lists<T>::kG + l16 * V + v] * lists.at[Lists<T>::kPerSum + l16 * V + v];
+        live |= (lists.at[Lists<T>::kLive + l16 * V + v] != 0.f ? 1u : 0u) << v;
+    }
+    asm volatile("" : "+v"(c0));         // (nothing of the loads' addresses is kept)
+    T* p = grad + m + c0 * D.gcs;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        if (c0 + r < C) {
+            float v[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                v[j] = V == 4 ? tile.c[r].value(j) : exp2_of((tile.c[r].value(j) - top[j]) * D.to_log2);
+                v[j] = live >> j & 1 ? v[j] * per[j] : 0.f;
+            }
+            if (l16 * V >= first) {
+                store_gradients(p, v, V);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (l16 * V + j >= first) store_elem(p + j, v[j]);
+            }
+        }
+        p += D.gcs;
+        asm volatile("" : "+v"(p));      // (one address at a time: there are no registers for 16)
+    }
+    __syncthreads();                     // the classes of the lists are stored over
+    lists.listed(D, m0, grad, 0, D.C, first);
+}
+
+// More classes, or too few positions for the units: `parts` workgroups share a tile's classes.  First each takes its
+// part's largest logits and sums.
+constexpr int kPartThreads = 256, kPartSpan = kPartThreads / 16 * 16;
+
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void distill_map_parts_kernel(Distill D, int64_t per_part, Part* parts) {
+    constexpr int V = Tile<T>::V;
+    __shared__ float room[kPartThreads / 64 * 16 * V];
+    const int64_t m = (int64_t)blockIdx.x * Tile<T>::kTokens + (threadIdx.x & 15) * V;
+    const int64_t c1 = min((blockIdx.y + 1) * per_part, D.C);
+    const T* z = static_cast<const T*>(D.z);
+    float top[V], sum[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) top[v] = -INFINITY, sum[v] = 0.f;
+    for (int64_t c0 = blockIdx.y * per_part; c0 < c1; c0 += kPartSpan) {
+        Tile<T> tile;
+        tile.load(z + m, D.cs, c0 + (threadIdx.x >> 4) * 16, c1, D.M - m);
+        float next[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) next[v] = top[v];
+        tile.raise_into(next);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) forget(tile.c[r]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float to = next[v] == -INFINITY ? 0.f : next[v];
+            float s = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s += exp2_of((tile.c[r].value(v) - to) * D.to_log2);
+            sum[v] = sum[v] * exp2_of((top[v] - to) * D.to_log2) + s;
+            top[v] = next[v];
+        }
+    }
+    float all[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) all[v] = top[v];
+    over_tile<Max>(all, room);
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum[v] = joined(D, {all[v], 0.f}, {top[v], sum[v]}).sum;
+    over_tile<Sum>(sum, room);
+    if (threadIdx.x < 16)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (m + v < D.M) parts[(m + v) * gridDim.y + blockIdx.y] = {all[v], sum[v]};
+}
+
+// Then the losses (workgroups 0 of a tile) and the gradient of their parts.
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void distill_map_finish_kernel(Distill D, int64_t per_part, const Part* parts, int n_parts,
+                                                                          int with_loss) {
+    constexpr int V = Tile<T>::V, N = Tile<T>::kTokens;
+    extern __shared__ __align__(16) char lds[];
+    const Lists<T> lists = {reinterpret_cast<float*>(lds), D.k};
+    const int64_t m0 = (int64_t)blockIdx.x * N, m = m0 + (threadIdx.x & 15) * V;
+    const int64_t c_from = blockIdx.y * per_part, c1 = min(c_from + per_part, D.C);
+    const int l16 = threadIdx.x & 15;
+    const bool losses = with_loss && blockIdx.y == 0;
+    const T* z = static_cast<const T*>(D.z);
+    // (the student's logits of other parts may be their gradients already, if these are written over them)
+    lists.fill(D, m0, z, losses ? 0 : c_from, losses ? D.C : c1);
+    __syncthreads();
+    for (int n = threadIdx.x; n < N; n += kPartThreads) {
+        if (m0 + n >= D.M) continue;
+        Part all = {-INFINITY, 0.f};
+        for (int p = 0; p < n_parts; ++p) all = joined(D, all, parts[(m0 + n) * n_parts + p]);
+        // (a position of -infinities has the sum 0 here, and no softmax)
+        lists.finish(D, m0, n, all.top, all.top == -INFINITY ? quiet_nan() : all.sum, losses);
+    }
+    if (!D.grad) return;
+    __syncthreads();
+    T* grad = static_cast<T*>(D.grad);
+    if (m < D.M) {
+        float per[V], top[V];
+        uint32_t live = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float* own = lists.at + l16 * V + v;
+            live |= (m + v < D.M && own[Lists<T>::kLive] != 0.f ? 1u : 0u) << v;
+            per[v] = own[Lists<T>::kG] * own[Lists<T>::kPerSum], top[v] = own[Lists<T>::kZMax];
+        }
+        for (int64_t c0 = c_from + (threadIdx.x >> 4) * 16; c0 < c1; c0 += kPartSpan) {
+            Tile<T> tile;
+            tile.load(z + m, D.cs, c0, c1, D.M - m);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                if (c0 + r >= c1) continue;
+                float v[V];
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    v[j] = live >> j & 1 ? exp2_of((tile.c[r].value(j) - top[j]) * D.to_log2) * per[j] : 0.f;
+                store_gradients(grad + m + (c0 + r) * D.gcs, v, D.M - m);
+            }
+        }
+    }
+    __syncthreads();                     // the classes of the lists are stored over
+    lists.listed(D, m0, grad, c_from, c1);
+}
+
+template <typename T>
+hipError_t run_columns(const Distill& D, dss_dtype dt, hipStream_t s) {
+    // two workgroups' columns fit a unit's LDS
+    const int waves = D.C <= 64 ? 4 : 2;
+    for (int64_t m = 0; m < D.M; m += (int64_t)1 << 30) {
+        const Distill S = positions(D, dt, m, std::min(D.M - m, (int64_t)1 << 30));
+        distill_columns_kernel<T><<<dim3((unsigned)ceil_div64(S.M, waves * 64)), waves * 64, (size_t)D.C * waves * 256, s>>>(S);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename T>
+hipError_t run_tiles(const Distill& D, dss_dtype dt, hipStream_t s) {
+    constexpr int N = Tile<T>::kTokens;
+    const int waves = (int)ceil_div64(D.C, 64);
+    const size_t lds = Lists<T>::bytes(D.k) + (size_t)waves * N * 4;
+    const hipError_t e = allow_dynamic_lds((const void*)distill_tile_kernel<T>, lds);
+    if (e != hipSuccess) return e;
+    for (int64_t m = 0; m < D.M;) {
+        // (what is left after this launch has a whole tile's positions)
+        const int64_t n = D.M - m <= kSlabTokens ? D.M - m : kSlabTokens - N;
+        const Distill S = positions(D, dt, m, n);
+        distill_tile_kernel<T><<<dim3((unsigned)ceil_div64(n, N)), waves * 64, lds, s>>>(S);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        m += n;
+    }
+    return hipSuccess;
+}
+
+template <typename T>
+hipError_t run_map_parts(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
+    constexpr int N = Tile<T>::kTokens;
+    const size_t lds = Lists<T>::bytes(D.k);
+    const hipError_t allowed = allow_dynamic_lds((const void*)distill_map_finish_kernel<T>, lds);
+    if (allowed != hipSuccess) return allowed;
+    constexpr int64_t slab = 65536;
+    for (int64_t m = 0; m < D.M; m += slab) {
+        const Distill S = positions(D, dt, m, std::min(D.M - m, slab));
+        // enough workgroups for the units, of at least a span of classes each
+        const int64_t tiles = ceil_div64(S.M, N);
+        const int64_t most = std::max<int64_t>(1, std::min({ceil_div64(1024, tiles), ceil_div64(D.C, kPartSpan), (int64_t)kMostParts / S.M}));
+        const int64_t per_part = ceil_div64(ceil_div64(D.C, most), kPartSpan) * kPartSpan, n = ceil_div64(D.C, per_part);
+        const dim3 grid((unsigned)tiles, (unsigned)n);
+        distill_map_parts_kernel<T><<<grid, kPartThreads, 0, s>>>(S, per_part, parts);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        const bool over = D.grad == D.z;     // the losses need all of the logits first
+        Distill L = S;
+        if (over) L.grad = nullptr;
+        if (over || !D.grad) {
+            distill_map_finish_kernel<T><<<dim3((unsigned)tiles, 1), kPartThreads, lds, s>>>(L, D.C, parts, (int)n, 1);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        if (D.grad) distill_map_finish_kernel<T><<<grid, kPartThreads, lds, s>>>(S, per_part, parts, (int)n, !over);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename T>
+hipError_t run_map(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
+    if (D.C <= kColumns) return run_columns<T>(D, dt, s);
+    // (lists of up to 128 places: 128 KB for 128 positions)
+    if (D.k > 128) return launch_distill_any(D, dt, s);
+    return D.C <= 1024 && D.M >= Tile<T>::kTokens ? run_tiles<T>(D, dt, s) : run_map_parts<T>(D, dt, parts, s);
+}
+
+}  // namespace
+
+hipError_t launch_distill_map(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
+    return dt == DSS_BF16 ? run_map<uint16_t>(D, dt, parts, s) : run_map<float>(D, dt, parts, s);
+}
+
+}  // namespace dss
