@@ -18,19 +18,44 @@ namespace {
 // gradient in the end, of any other one the logit.
 constexpr int kColumns = 128;            // classes at most
 
+// kPlaces places of a list, loaded together: what a pass over a list costs is its loads' latency.  Lists of no more stay
+// in registers.
+constexpr int kPlaces = 8;
+struct Places {
+    int id[kPlaces];
+    float t[kPlaces];
+
+    __device__ __forceinline__ void load(const Distill& D, int64_t m, int j0) {
+#pragma unroll
+        for (int j = 0; j < kPlaces; ++j) {
+            id[j] = class_of(D, m, min(j0 + j, D.k - 1));
+            t[j] = teacher_of(D, m, min(j0 + j, D.k - 1));
+        }
+#pragma unroll
+        for (int j = 0; j < kPlaces; ++j) {
+            if (j0 + j >= D.k) id[j] = -1;
+            if (id[j] < 0) t[j] = -INFINITY;
+        }
+    }
+};
+
 template <typename T>
-__global__ void distill_columns_kernel(Distill D) {
+__global__ __launch_bounds__(64) void distill_columns_kernel(Distill D) {
     extern __shared__ float columns[];
-    const int C = (int)D.C, lane = threadIdx.x & 63, k = D.k;
-    float* const col = columns + (threadIdx.x >> 6) * C * 64 + lane;
-    const int64_t own = xcd_order(blockIdx.x, gridDim.x) * blockDim.x + threadIdx.x, m = min(own, D.M - 1);
+    const int C = (int)D.C, lane = threadIdx.x, k = D.k;
+    float* const col = columns + lane;
+    const int64_t own = xcd_order(blockIdx.x, gridDim.x) * 64 + lane, m = min(own, D.M - 1);
     const T* z = static_cast<const T*>(D.z) + m;
-    constexpr int U = 16;
+    Places a;
+    a.load(D, m, 0);
+    const float weight = D.weights ? D.weights[m] : 1.f;
+    constexpr int U = 32;
     float z_max = -INFINITY;
     for (int c0 = 0; c0 < C; c0 += U) {
         float v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = to_f32(z[min(c0 + u, C - 1) * D.cs]);
+        for (int u = 0; u < U; ++u)
+            if (c0 + u < C) v[u] = to_f32(z[(c0 + u) * D.cs]);
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (c0 + u < C) {
@@ -38,42 +63,42 @@ __global__ void distill_columns_kernel(Distill D) {
                 z_max = fmaxf(z_max, v[u]);
             }
     }
-    const float weight = D.weights ? D.weights[m] : 1.f;
+    // f of the list's places, batch by batch
+    auto over_places = [&](auto f) {
+        for (int j0 = 0; j0 < k; j0 += kPlaces) {
+            if (k > kPlaces) a.load(D, m, j0);
+#pragma unroll
+            for (int j = 0; j < kPlaces; ++j) f(a.id[j], a.t[j]);
+        }
+    };
     float t_max = -INFINITY, state = 0.f;
-    for (int j = 0; j < k; ++j) {
-        const int id = class_of(D, m, j);
-        const float t = id >= 0 ? teacher_of(D, m, j) : -INFINITY;
+    over_places([&](int id, float t) {
         t_max = fmaxf(t_max, t);
         state = fmaxf(state, Place{id, t, 0.f}.state(D));
-    }
+    });
     const bool live = weight != 0.f && state != 0.f;
     const float nan = state == 3.f ? quiet_nan() : 0.f;
     float sum_r = nan, sum_p = nan;
-    for (int c0 = 0; c0 < C; c0 += U) {
+    over_places([&](int id, float t) { sum_p += weight_of(D, t, t_max); });
+    for (int c0 = 0; c0 < C; c0 += 16) {
         float part = 0.f;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < 16; ++u)
             if (c0 + u < C) part += exp2_of((col[(c0 + u) * 64] - z_max) * D.to_log2);
         sum_r += part;
     }
-    for (int j = 0; j < k; ++j)
-        if (class_of(D, m, j) >= 0) sum_p += weight_of(D, teacher_of(D, m, j), t_max);
-    const float log_sums = logf(sum_p) - logf(sum_r), per_sum = 1.f / sum_r;
-    float loss = 0.f;
-    for (int j = 0; j < k; ++j) {
-        const int id = class_of(D, m, j);
-        if (id < 0 || id >= C) continue;
-        const float t = teacher_of(D, m, j);
-        loss += loss_of(D, weight_of(D, t, t_max) / sum_p, t, t_max, col[id * 64], z_max, log_sums);
-    }
+    const float log_sums = logf(sum_p) - logf(sum_r), per_sum = 1.f / sum_r, per_p = 1.f / sum_p;
+    float loss = nan;
+    over_places([&](int id, float t) {
+        if (id >= 0 && id < C) loss += loss_of(D, weight_of(D, t, t_max) * per_p, t, t_max, col[id * 64], z_max, log_sums);
+    });
     const float sw = D.scale * weight, g = sw * D.T;
-    if (own < D.M) D.losses[m] = live ? sw * D.T * (D.T * (loss + nan)) : 0.f;
+    if (own < D.M) D.losses[m] = live ? sw * D.T * (D.T * loss) : 0.f;
     if (!D.grad) return;
     uint32_t listed[kColumns / 32] = {};
-    for (int j = 0; j < k; ++j) {
-        const int id = class_of(D, m, j);
-        if (id < 0 || id >= C) continue;
-        const float p = weight_of(D, teacher_of(D, m, j), t_max) / sum_p;
+    over_places([&](int id, float t) {
+        if (id < 0 || id >= C) return;
+        const float p = weight_of(D, t, t_max) * per_p;
         float v = col[id * 64];
         bool before = false;
 #pragma unroll
@@ -84,15 +109,17 @@ __global__ void distill_columns_kernel(Distill D) {
         }
         if (!before) v = exp2_of((v - z_max) * D.to_log2) * per_sum;
         col[id * 64] = v - p;
-    }
+    });
+    if (own >= D.M) return;
     T* grad = static_cast<T*>(D.grad) + m;
 #pragma unroll
     for (int w = 0; w < kColumns / 32; ++w) {
-#pragma unroll 8
+        if (w * 32 >= C) break;
+#pragma unroll 16
         for (int c = w * 32; c < min(w * 32 + 32, C); ++c) {
             float v = col[c * 64];
             if (!(listed[w] >> (c % 32) & 1)) v = exp2_of((v - z_max) * D.to_log2) * per_sum;
-            if (own < D.M) store_elem(grad + c * D.gcs, live ? g * v : 0.f);
+            store_elem(grad + c * D.gcs, live ? g * v : 0.f);
         }
     }
 }
@@ -149,24 +176,35 @@ __device__ __forceinline__ void over_tile(float (&v)[V], float* room) {
         for (int j = 0; j < V; ++j) v[j] = Op::of(v[j], room[(w * 16 + (lane & 15)) * V + j]);
 }
 
-// What a position's gradient is made of, and its list: classes and the student's logits there (of classes c0 .. c1-1
-// and, with a loss to form, all). In LDS, the positions of a tile adjacent.
+// What a position's gradient is made of, and its list: classes, the student's logits there (of classes c0 .. c1-1
+// and, with a loss to form, all) and the teacher's, unless these stay in memory for want of room. In LDS, the
+// positions of a tile adjacent.
 template <typename T>
 struct Lists {
     static constexpr int N = Tile<T>::kTokens;
-    static constexpr int kZMax = 0, kPerSum = N, kTMax = 2 * N, kSumP = 3 * N, kG = 4 * N, kLive = 5 * N, kIds = 6 * N;
+    static constexpr int kZMax = 0, kPerSum = N, kTMax = 2 * N, kPerP = 3 * N, kG = 4 * N, kLive = 5 * N, kIds = 6 * N;
     float* at;
     int k;
 
-    static __host__ __device__ size_t bytes(int k) { return (size_t)N * (6 + 2 * k) * 4; }
+    static __host__ __device__ bool holds_t(int k) { return k * N <= 8192; }
+    static __host__ __device__ size_t bytes(int k) { return (size_t)N * (6 + (holds_t(k) ? 3 : 2) * k) * 4; }
     __device__ __forceinline__ int& id(int n) const { return reinterpret_cast<int*>(at)[kIds + n]; }
     __device__ __forceinline__ float& z(int n) const { return at[kIds + k * N + n]; }
+    // Of place j, position n: -infinity for an empty place.
+    __device__ __forceinline__ float t(const Distill& D, int64_t m0, int j, int n) const {
+        if (holds_t(k)) return at[kIds + (2 * k + j) * N + n];
+        return id(j * N + n) >= 0 ? teacher_of(D, m0 + n, j) : -INFINITY;
+    }
 
     __device__ __forceinline__ void fill(const Distill& D, int64_t m0, const T* logits, int64_t c0, int64_t c1) const {
         for (int n = threadIdx.x; n < D.k * N; n += blockDim.x) {
             const int64_t m = min(m0 + n % N, D.M - 1);
             const int c = class_of(D, m, n / N);
             id(n) = c;
+            if (holds_t(k)) {
+                const float t = teacher_of(D, m, n / N);
+                at[kIds + 2 * k * N + n] = c >= 0 ? t : -INFINITY;
+            }
             z(n) = c >= c0 && c < c1 ? to_f32(logits[m + c * D.cs]) : 0.f;
         }
     }
@@ -177,31 +215,28 @@ struct Lists {
         const float weight = D.weights ? D.weights[m] : 1.f;
         float tm = -INFINITY, state = 0.f;
         for (int j = 0; j < D.k; ++j) {
-            const int c = id(j * N + n);
-            const float t = c >= 0 ? teacher_of(D, m, j) : -INFINITY;
-            tm = fmaxf(tm, t);
-            state = fmaxf(state, Place{c, t, 0.f}.state(D));
+            const float a = t(D, m0, j, n);
+            tm = fmaxf(tm, a);
+            state = fmaxf(state, Place{id(j * N + n), a, 0.f}.state(D));
         }
         const float nan = state == 3.f ? quiet_nan() : 0.f;
         float sum_p = nan;
-        for (int j = 0; j < D.k; ++j)
-            if (id(j * N + n) >= 0) sum_p += weight_of(D, teacher_of(D, m, j), tm);
+        for (int j = 0; j < D.k; ++j) sum_p += weight_of(D, t(D, m0, j, n), tm);
         sum_r += nan;
         const float sw = D.scale * weight;
         const bool learn = weight != 0.f && state != 0.f;
         at[kZMax + n] = top;
         at[kPerSum + n] = 1.f / sum_r;
         at[kTMax + n] = tm;
-        at[kSumP + n] = sum_p;
+        at[kPerP + n] = 1.f / sum_p;
         at[kG + n] = sw * D.T;
         at[kLive + n] = learn ? 1.f : 0.f;
         if (!with_loss) return;
-        const float log_sums = logf(sum_p) - logf(sum_r);
+        const float log_sums = logf(sum_p) - logf(sum_r), per_p = 1.f / sum_p;
         float loss = nan;
         for (int j = 0; j < D.k; ++j) {
-            if (id(j * N + n) < 0) continue;
-            const float t = teacher_of(D, m, j);
-            loss += loss_of(D, weight_of(D, t, tm) / sum_p, t, tm, z(j * N + n), top, log_sums);
+            const float a = t(D, m0, j, n);
+            loss += loss_of(D, weight_of(D, a, tm) * per_p, a, tm, z(j * N + n), top, log_sums);
         }
         D.losses[m] = learn ? sw * D.T * (D.T * loss) : 0.f;
     }
@@ -213,7 +248,7 @@ struct Lists {
             if (own < first || m >= D.M || c < c0 || c >= c1 || at[kLive + own] == 0.f) continue;
             float of_class = 0.f;        // (a class may be there more than once)
             for (int i = 0; i < D.k; ++i)
-                if (id(i * N + own) == c) of_class += weight_of(D, teacher_of(D, m, i), at[kTMax + own]) / at[kSumP + own];
+                if (id(i * N + own) == c) of_class += weight_of(D, t(D, m0, i, own), at[kTMax + own]) * at[kPerP + own];
             const float r = exp2_of((z(n) - at[kZMax + own]) * D.to_log2) * at[kPerSum + own];
             store_elem(grad + m + c * D.gcs, at[kG + own] * (r - of_class));
         }
@@ -403,11 +438,10 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_finish_kernel(Distil
 
 template <typename T>
 hipError_t run_columns(const Distill& D, dss_dtype dt, hipStream_t s) {
-    // two workgroups' columns fit a unit's LDS
-    const int waves = D.C <= 64 ? 4 : 2;
+    // (a launch has fewer than 2^32 threads)
     for (int64_t m = 0; m < D.M; m += (int64_t)1 << 30) {
         const Distill S = positions(D, dt, m, std::min(D.M - m, (int64_t)1 << 30));
-        distill_columns_kernel<T><<<dim3((unsigned)ceil_div64(S.M, waves * 64)), waves * 64, (size_t)D.C * waves * 256, s>>>(S);
+        distill_columns_kernel<T><<<dim3((unsigned)ceil_div64(S.M, 64)), 64, (size_t)D.C * 256, s>>>(S);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
