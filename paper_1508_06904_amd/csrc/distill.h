@@ -122,55 +122,64 @@ __device__ __forceinline__ void over_lanes(float (&v)[N], float* room) {
     }
 }
 
-// E logits of which none is there.
-template <typename T>
-__device__ __forceinline__ Chunk<T> no_logits() {
-    Chunk<T> r;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) r.w[w] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
-    return r;
-}
-// E logits from p on, -infinity for those from n on.
-template <typename T>
-__device__ __forceinline__ Chunk<T> load_logits(const T* p, int64_t n) {
-    Chunk<T> r = no_logits<T>();
-    if (n >= Chunk<T>::E) {
-        __builtin_memcpy(&r, p, 16);
-    } else {
-#pragma unroll
-        for (int e = 0; e < Chunk<T>::E; ++e)
-            if (e < n) {
-                if constexpr (sizeof(T) == 4) r.w[e] = __builtin_bit_cast(uint32_t, p[e]);
-                else r.w[e / 2] = e & 1 ? (r.w[e / 2] & 0xffffu) | (uint32_t)p[e] << 16 : (r.w[e / 2] & 0xffff0000u) | p[e];
-            }
+// 4 W bytes of adjacent logits, as words: their values unpack where they are used.
+template <typename T, int W = 4>
+struct Logits {
+    static constexpr int E = 4 * W / (int)sizeof(T);
+    uint32_t w[W];
+
+    __device__ __forceinline__ float value(int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        else return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
     }
-    return r;
-}
-// The same words, of which the compiler knows no more: bfloat16 unpacked for one pass is not kept for
-// the next one, for which there are no registers.
-template <typename T>
-__device__ __forceinline__ void forget(Chunk<T>& c) {
-    if constexpr (sizeof(T) == 2) asm volatile("" : "+v"(c.w[0]), "+v"(c.w[1]), "+v"(c.w[2]), "+v"(c.w[3]));
-}
-template <typename T>
-__device__ __forceinline__ float top_of(float top, const Chunk<T>& c) {
+    // None: -infinity.
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int e = 0; e < Chunk<T>::E; ++e) top = fmaxf(top, c.value(e));
-    return top;
-}
+        for (int i = 0; i < W; ++i) w[i] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    }
+    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(w, p, 4 * W); }
+    // Those from p on, -infinity for those from n on.
+    __device__ __forceinline__ void load(const T* p, int64_t n) {
+        clear();
+        if (n >= E) {
+            load(p);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e < n) {
+                    if constexpr (sizeof(T) == 4) w[e] = __builtin_bit_cast(uint32_t, p[e]);
+                    else w[e / 2] = e & 1 ? (w[e / 2] & 0xffffu) | (uint32_t)p[e] << 16 : (w[e / 2] & 0xffff0000u) | p[e];
+                }
+        }
+    }
+    __device__ __forceinline__ float top(float of) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e) of = fmaxf(of, value(e));
+        return of;
+    }
+    // The same words, of which the compiler knows no more: bfloat16 unpacked for one pass is not kept
+    // for the next one, for which there are no registers.
+    __device__ __forceinline__ void forget() {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) asm volatile("" : "+v"(w[i]));
+        }
+    }
+};
+
 // E gradients from p on, the first n of them.
-template <typename T>
-__device__ __forceinline__ void store_gradients(T* p, const float (&v)[Chunk<T>::E], int64_t n) {
+template <typename T, int E>
+__device__ __forceinline__ void store_gradients(T* p, const float (&v)[E], int64_t n) {
     struct {
-        T v[Chunk<T>::E];
+        T v[E];
     } r;
 #pragma unroll
-    for (int e = 0; e < Chunk<T>::E; ++e) store_elem(&r.v[e], v[e]);
-    if (n >= Chunk<T>::E) {
-        __builtin_memcpy(p, &r, 16);
+    for (int e = 0; e < E; ++e) store_elem(&r.v[e], v[e]);
+    if (n >= E) {
+        __builtin_memcpy(p, &r, sizeof r);
     } else {
 #pragma unroll
-        for (int e = 0; e < Chunk<T>::E; ++e)
+        for (int e = 0; e < E; ++e)
             if (e < n) p[e] = r.v[e];
     }
 }

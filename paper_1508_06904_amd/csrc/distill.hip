@@ -103,7 +103,7 @@ struct List {
 // LPR threads hold a position's logits, CH chunks each, in registers: they are read once.
 template <typename T, int LPR, int CH>
 __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_kernel(Distill D) {
-    constexpr int E = Chunk<T>::E, ROWS = LPR < kThreads ? kThreads / LPR : 1;
+    constexpr int E = Logits<T>::E, ROWS = LPR < kThreads ? kThreads / LPR : 1;
     __shared__ float room[LPR > 64 ? LPR / 64 * 3 : 1];
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x % LPR, row = threadIdx.x / LPR, k = D.k;
@@ -111,15 +111,16 @@ __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_
     const T* z = static_cast<const T*>(D.z) + m * D.ts;
     const float weight = D.weights ? D.weights[m] : 1.f;
     const List list(lds + row * List::bytes(k), k);
-    Chunk<T> c[CH];
+    Logits<T> c[CH];
     const int C = weight == 0.f ? 0 : (int)D.C, last = C / E;    // the chunk that C ends in, if it ends in one
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        c[i] = no_logits<T>();
-        if (i * LPR + lane < last) __builtin_memcpy(&c[i], z + (i * LPR + lane) * E, 16);
+        c[i].clear();
+        if (i * LPR + lane < last) c[i].load(z + (i * LPR + lane) * E);
     }
     if (C % E != 0 && last % LPR == lane) {
-        const Chunk<T> end = load_logits(z + last * E, C % E);
+        Logits<T> end;
+        end.load(z + last * E, C % E);
 #pragma unroll
         for (int i = 0; i < CH; ++i)
             if (i == last / LPR) c[i] = end;
@@ -135,8 +136,8 @@ __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_
     }
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        tops[2] = top_of(tops[2], c[i]);
-        forget(c[i]);
+        tops[2] = c[i].top(tops[2]);
+        c[i].forget();
     }
     over_lanes<Max, LPR>(tops, room);
     const float t_max = tops[0], z_max = tops[2];
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_
             part += v;
         }
         sums[1] += part;
-        forget(c[i]);
+        c[i].forget();
     }
     over_lanes<Sum, LPR>(sums, room);
     const float sum_p = sums[0] + nan, sum_r = sums[1] + nan, log_sums = logf(sum_p) - logf(sum_r);
@@ -197,19 +198,19 @@ __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_
 // each takes its part's largest logit and sum.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void distill_parts_kernel(Distill D, int64_t per_part, Part* parts) {
-    constexpr int E = Chunk<T>::E, U = 8;
+    constexpr int E = Logits<T>::E, U = 8;
     __shared__ float room[kThreads / 64];
     const int64_t m = blockIdx.y, c0 = blockIdx.x * per_part, c1 = min(c0 + per_part, D.C);
     if (D.weights && D.weights[m] == 0.f) return;
     const T* z = static_cast<const T*>(D.z) + m * D.ts;
     Part own = {-INFINITY, 0.f};
     for (int64_t at = c0 + threadIdx.x * E; at < c1; at += U * kThreads * E) {
-        Chunk<T> c[U];
+        Logits<T> c[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) c[u] = load_logits(z + at + u * kThreads * E, c1 - at - u * kThreads * E);
+        for (int u = 0; u < U; ++u) c[u].load(z + at + u * kThreads * E, c1 - at - u * kThreads * E);
         float top = own.top;
 #pragma unroll
-        for (int u = 0; u < U; ++u) top = top_of(top, c[u]);
+        for (int u = 0; u < U; ++u) top = c[u].top(top);
         const float to = top == -INFINITY ? 0.f : top;
         float sum = 0.f;
 #pragma unroll
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void distill_parts_kernel(Distill D, int6
 template <typename T>
 __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill D, int64_t per_part, const Part* parts, int n_parts,
                                                                   int with_loss) {
-    constexpr int E = Chunk<T>::E, U = 4;
+    constexpr int E = Logits<T>::E, U = 4;
     __shared__ float room[kThreads / 64 * 3];
     extern __shared__ __align__(16) char lds[];
     const int64_t m = blockIdx.y, c0 = blockIdx.x * per_part, c1 = min(c0 + per_part, D.C);
@@ -276,9 +277,9 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill D, int
     if (!D.grad) return;
     const float g = sw * D.T, per_sum = 1.f / sum_r;
     for (int64_t at = c0 + threadIdx.x * E; at < c1; at += U * kThreads * E) {
-        Chunk<T> c[U];
+        Logits<T> c[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) c[u] = load_logits(z + at + u * kThreads * E, live ? c1 - at - u * kThreads * E : 0);
+        for (int u = 0; u < U; ++u) c[u].load(z + at + u * kThreads * E, live ? c1 - at - u * kThreads * E : 0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float v[E];
@@ -326,7 +327,7 @@ hipError_t run_parts(const Distill& D, Part* parts, hipStream_t s) {
 
 template <typename T>
 hipError_t run_distill(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
-    constexpr int E = Chunk<T>::E;
+    constexpr int E = Logits<T>::E;
     const bool long_rows = D.C > 1024 * 16 * E || (!D.grad && D.C > 256 * 16 * E);
     if (long_rows || (D.M < 128 && D.C >= 16384)) {
         // (a launch has 65535 workgroups along y)

@@ -125,27 +125,27 @@ __global__ __launch_bounds__(64) void distill_columns_kernel(Distill D) {
 }
 
 // ------------------------------------------------------------------ tiles
-// A workgroup has the 16 V positions of 16 lanes with 16 bytes each; a lane has 16 adjacent classes of its V positions, so a
+// A workgroup has the 16 V positions of 16 lanes with W words each; a lane has 16 adjacent classes of its V positions, so a
 // wave has 64 classes.
-template <typename T>
+template <typename T, int W>
 struct Tile {
-    static constexpr int V = Chunk<T>::E, kTokens = 16 * V;
-    Chunk<T> c[16];
+    static constexpr int V = Logits<T, W>::E, kTokens = 16 * V;
+    Logits<T, W> c[16];
 
     // The lane's classes c0 .. c0+15, those below C, of the V positions from p on; -infinity elsewhere.
     __device__ __forceinline__ void load(const T* p, int64_t cs, int c0, int C) {
         p += c0 * cs;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            c[r] = no_logits<T>();
-            if (c0 + r < C) __builtin_memcpy(&c[r], p, 16);
+            c[r].clear();
+            if (c0 + r < C) c[r].load(p);
             p += cs;
         }
     }
     // The same of the first n positions from p on.
     __device__ __forceinline__ void load(const T* p, int64_t cs, int64_t c0, int64_t C, int64_t n) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) c[r] = load_logits(p + (c0 + r) * cs, c0 + r < C ? n : 0);
+        for (int r = 0; r < 16; ++r) c[r].load(p + (c0 + r) * cs, c0 + r < C ? n : 0);
     }
     __device__ __forceinline__ void raise_into(float (&top)[V]) const {
 #pragma unroll
@@ -176,81 +176,93 @@ __device__ __forceinline__ void over_tile(float (&v)[V], float* room) {
         for (int j = 0; j < V; ++j) v[j] = Op::of(v[j], room[(w * 16 + (lane & 15)) * V + j]);
 }
 
-// What a position's gradient is made of, and its list: classes, the student's logits there (of classes c0 .. c1-1
-// and, with a loss to form, all) and the teacher's, unless these stay in memory for want of room. In LDS, the
-// positions of a tile adjacent.
-template <typename T>
+// The lists of a tile's N positions in LDS (adjacent there): classes, the teacher's logits (-infinity at empty places) and
+// the student's; and of each position what its loss and gradient are made of.
+template <typename T, int N>
 struct Lists {
-    static constexpr int N = Tile<T>::kTokens;
-    static constexpr int kZMax = 0, kPerSum = N, kTMax = 2 * N, kPerP = 3 * N, kG = 4 * N, kLive = 5 * N, kIds = 6 * N;
+    static constexpr int kTMax = 0, kPerP = N, kRef = 2 * N, kParts = 3 * N, kMass = 4 * N, kState = 5 * N, kZMax = 6 * N,
+                         kPerSum = 7 * N, kPlace0 = 8 * N;
     float* at;
     int k;
 
+    // (the teacher's logits stay in memory where there is no room for them)
     static __host__ __device__ bool holds_t(int k) { return k * N <= 8192; }
-    static __host__ __device__ size_t bytes(int k) { return (size_t)N * (6 + (holds_t(k) ? 3 : 2) * k) * 4; }
-    __device__ __forceinline__ int& id(int n) const { return reinterpret_cast<int*>(at)[kIds + n]; }
-    __device__ __forceinline__ float& z(int n) const { return at[kIds + k * N + n]; }
-    // Of place j, position n: -infinity for an empty place.
+    static __host__ __device__ size_t bytes(int k) { return (size_t)N * (8 + (holds_t(k) ? 3 : 2) * k) * 4; }
+    __device__ __forceinline__ int& id(int n) const { return reinterpret_cast<int*>(at)[kPlace0 + n]; }
+    __device__ __forceinline__ float& z(int n) const { return at[kPlace0 + k * N + n]; }
     __device__ __forceinline__ float t(const Distill& D, int64_t m0, int j, int n) const {
-        if (holds_t(k)) return at[kIds + (2 * k + j) * N + n];
+        if (holds_t(k)) return at[kPlace0 + (2 * k + j) * N + n];
         return id(j * N + n) >= 0 ? teacher_of(D, m0 + n, j) : -INFINITY;
     }
 
-    __device__ __forceinline__ void fill(const Distill& D, int64_t m0, const T* logits, int64_t c0, int64_t c1) const {
-        for (int n = threadIdx.x; n < D.k * N; n += blockDim.x) {
-            const int64_t m = min(m0 + n % N, D.M - 1);
-            const int c = class_of(D, m, n / N);
-            id(n) = c;
-            if (holds_t(k)) {
-                const float t = teacher_of(D, m, n / N);
-                at[kIds + 2 * k * N + n] = c >= 0 ? t : -INFINITY;
-            }
-            z(n) = c >= c0 && c < c1 ? to_f32(logits[m + c * D.cs]) : 0.f;
-        }
+    // Place n / N of position n % N; the student's logits of classes c0 .. c1-1 alone.
+    __device__ __forceinline__ Place read(const Distill& D, int64_t m0, const T* logits, int n, int64_t c0, int64_t c1) const {
+        const int64_t m = min(m0 + n % N, D.M - 1);
+        Place a;
+        a.id = class_of(D, m, n / N);
+        a.t = holds_t(k) ? teacher_of(D, m, n / N) : 0.f;
+        a.z = a.id >= c0 && a.id < c1 ? to_f32(logits[m + a.id * D.cs]) : 0.f;
+        return a;
     }
-    // Of position n: its stats, and its loss if that is to be written.  sum_r is NaN or above 0.
-    __device__ __forceinline__ void finish(const Distill& D, int64_t m0, int n, float top, float sum_r, bool with_loss) const {
-        const int64_t m = m0 + n;
-        if (m >= D.M) return;
-        const float weight = D.weights ? D.weights[m] : 1.f;
-        float tm = -INFINITY, state = 0.f;
-        for (int j = 0; j < D.k; ++j) {
-            const float a = t(D, m0, j, n);
-            tm = fmaxf(tm, a);
-            state = fmaxf(state, Place{id(j * N + n), a, 0.f}.state(D));
+    __device__ __forceinline__ void put(int n, const Place& a) const {
+        id(n) = a.id;
+        z(n) = a.z;
+        if (holds_t(k)) at[kPlace0 + 2 * k * N + n] = a.id >= 0 ? a.t : -INFINITY;
+    }
+    // Of position n, from its list alone: with p of the list, z' the largest of its student's logits and d_j = (t_j - t_max) / T
+    // - (z_j - z') / T, the sums of p_j d_j and of p_j.  Its loss is then sum p_j d_j - sum p_j ((z' - z_max) / T + log(sum_p / sum_r)).
+    __device__ __forceinline__ void sum_up(const Distill& D, int64_t m0, int n) const {
+        float t_max = -INFINITY, state = 0.f, sum_p = 0.f, ref = -3.4028235e38f, parts = 0.f, mass = 0.f;
+        if (m0 + n < D.M) {
+#pragma unroll 4
+            for (int j = 0; j < k; ++j) {
+                const float a = t(D, m0, j, n);
+                t_max = fmaxf(t_max, a);
+                state = fmaxf(state, Place{id(j * N + n), a, 0.f}.state(D));
+            }
+#pragma unroll 4
+            for (int j = 0; j < k; ++j) {
+                const float p = weight_of(D, t(D, m0, j, n), t_max);
+                sum_p += p;
+                if (p > 0.f) ref = fmaxf(ref, z(j * N + n));
+            }
+            if (state == 3.f) sum_p = quiet_nan();
+            const float per_p = 1.f / sum_p;
+#pragma unroll 4
+            for (int j = 0; j < k; ++j) {
+                const float a = t(D, m0, j, n), p = weight_of(D, a, t_max) * per_p;
+                parts += p <= 0.f ? 0.f : p * (((a - t_max) - (z(j * N + n) - ref)) * (D.to_log2 * kLn2));
+                mass += p;
+            }
+            if (D.weights && D.weights[m0 + n] == 0.f) state = 0.f;
         }
-        const float nan = state == 3.f ? quiet_nan() : 0.f;
-        float sum_p = nan;
-        for (int j = 0; j < D.k; ++j) sum_p += weight_of(D, t(D, m0, j, n), tm);
-        sum_r += nan;
-        const float sw = D.scale * weight;
-        const bool learn = weight != 0.f && state != 0.f;
-        at[kZMax + n] = top;
-        at[kPerSum + n] = 1.f / sum_r;
-        at[kTMax + n] = tm;
+        at[kTMax + n] = t_max;
         at[kPerP + n] = 1.f / sum_p;
-        at[kG + n] = sw * D.T;
-        at[kLive + n] = learn ? 1.f : 0.f;
-        if (!with_loss) return;
-        const float log_sums = logf(sum_p) - logf(sum_r), per_p = 1.f / sum_p;
-        float loss = nan;
-        for (int j = 0; j < D.k; ++j) {
-            const float a = t(D, m0, j, n);
-            loss += loss_of(D, weight_of(D, a, tm) * per_p, a, tm, z(j * N + n), top, log_sums);
-        }
-        D.losses[m] = learn ? sw * D.T * (D.T * loss) : 0.f;
+        at[kRef + n] = ref;
+        at[kParts + n] = parts;
+        at[kMass + n] = mass;
+        at[kState + n] = state;          // 0: nothing is to be learnt
+    }
+    // Of position n, from its list and its logits' largest and sum: whether there is anything to learn, and the gradient's factor.
+    __device__ __forceinline__ float factor(const Distill& D, int64_t m, int n) const {
+        return D.scale * (D.weights ? D.weights[min(m, D.M - 1)] : 1.f) * D.T;
+    }
+    __device__ __forceinline__ void put_loss(const Distill& D, int64_t m0, int n, float top, float sum) const {
+        const float state = at[kState + n], sum_r = state == 3.f ? quiet_nan() : sum;
+        const float away = (at[kRef + n] - top) * (D.to_log2 * kLn2) - logf(at[kPerP + n]) - logf(sum_r);
+        D.losses[m0 + n] = state == 0.f ? 0.f : factor(D, m0 + n, n) * (D.T * (at[kParts + n] - at[kMass + n] * away));
     }
     // The gradients of the listed classes c0 .. c1-1, after all others are written, of positions `first` on.
     __device__ __forceinline__ void listed(const Distill& D, int64_t m0, T* grad, int64_t c0, int64_t c1, int first = 0) const {
-        for (int n = threadIdx.x; n < D.k * N; n += blockDim.x) {
+        for (int n = threadIdx.x; n < k * N; n += blockDim.x) {
             const int own = n % N, c = id(n);
             const int64_t m = m0 + own;
-            if (own < first || m >= D.M || c < c0 || c >= c1 || at[kLive + own] == 0.f) continue;
+            if (own < first || m >= D.M || c < c0 || c >= c1 || at[kState + own] == 0.f) continue;
             float of_class = 0.f;        // (a class may be there more than once)
-            for (int i = 0; i < D.k; ++i)
+            for (int i = 0; i < k; ++i)
                 if (id(i * N + own) == c) of_class += weight_of(D, t(D, m0, i, own), at[kTMax + own]) * at[kPerP + own];
             const float r = exp2_of((z(n) - at[kZMax + own]) * D.to_log2) * at[kPerSum + own];
-            store_elem(grad + m + c * D.gcs, at[kG + own] * (r - of_class));
+            store_elem(grad + m + c * D.gcs, factor(D, m, own) * (r - of_class));
         }
     }
 };
@@ -258,69 +270,70 @@ struct Lists {
 // Up to 1024 classes: the tile's logits stay in registers.  Whole tiles only: the last one ends with the last
 // position and writes those from `first` on, which the one before it does not have.  (What it reads of the others
 // may be their gradients already, if these are written over the logits; positions do not mix.)
-template <typename T>
-__global__ __launch_bounds__(1024) void distill_tile_kernel(Distill D) {
-    constexpr int V = Tile<T>::V, N = Tile<T>::kTokens;
+template <typename T, int W>
+__global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(16 / W))) void distill_tile_kernel(Distill D) {
+    constexpr int V = Tile<T, W>::V, N = Tile<T, W>::kTokens;
+    using List = Lists<T, N>;
     extern __shared__ __align__(16) char lds[];
-    const Lists<T> lists = {reinterpret_cast<float*>(lds), D.k};
-    float* room = reinterpret_cast<float*>(lds + Lists<T>::bytes(D.k));
+    const List lists = {reinterpret_cast<float*>(lds), D.k};
+    float* room = reinterpret_cast<float*>(lds + List::bytes(D.k));
     const int64_t tile0 = xcd_order(blockIdx.x, gridDim.x) * N, m0 = min(tile0, D.M - N);
-    const int first = (int)(tile0 - m0);
-    const int l16 = threadIdx.x & 15;
-    const int64_t m = m0 + l16 * V;
+    const int first = (int)(tile0 - m0), l16 = threadIdx.x & 15, C = (int)D.C, places = D.k * N;
     const T* z = static_cast<const T*>(D.z);
-    const int C = (int)D.C;
     int c0 = (threadIdx.x >> 4) * 16;
-    Tile<T> tile;
-    tile.load(z + m, D.cs, c0, C);
-    lists.fill(D, m0, z, 0, D.C);
+    // (the lists first: there are no registers for them beside the tile, but another workgroup's work)
+    for (int n = threadIdx.x; n < places; n += blockDim.x) lists.put(n, lists.read(D, m0, z, n, 0, C));
+    __syncthreads();
+    for (int n = threadIdx.x; n < N; n += blockDim.x) lists.sum_up(D, m0, n);
+    __builtin_amdgcn_sched_barrier(0);
+    Tile<T, W> tile;
+    tile.load(z + m0 + l16 * V, D.cs, c0, C);
     float top[V], sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) top[v] = -INFINITY, sum[v] = 0.f;
     tile.raise_into(top);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) forget(tile.c[r]);
+    for (int r = 0; r < 16; ++r) tile.c[r].forget();
     over_tile<Max>(top, room);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float e = exp2_of((tile.c[r].value(v) - top[v]) * D.to_log2);
-            if constexpr (V == 4) tile.c[r].w[v] = __float_as_uint(e);       // (bfloat16 has no room for it)
+            if constexpr (sizeof(T) == 4) tile.c[r].w[v] = __float_as_uint(e);       // (bfloat16 has no room for it)
             sum[v] += e;
         }
         __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) forget(tile.c[r]);
-    over_tile<Sum>(sum, room);           // (with barriers: the lists are there)
-    if (threadIdx.x < 16)
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            lists.at[Lists<T>::kZMax + l16 * V + v] = top[v];
-            lists.at[Lists<T>::kPerSum + l16 * V + v] = sum[v];
-        }
-    __syncthreads();
-    for (int n = first + threadIdx.x; n < N; n += blockDim.x) lists.finish(D, m0, n, lists.at[Lists<T>::kZMax + n], lists.at[Lists<T>::kPerSum + n], true);
-    if (!D.grad) return;
-    __syncthreads();
-    T* grad = static_cast<T*>(D.grad);
+    for (int r = 0; r < 16; ++r) tile.c[r].forget();
+    over_tile<Sum>(sum, room);
     float per[V];
     uint32_t live = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        per[v] = lists.at[Lists<T>::kG + l16 * V + v] * lists.at[Lists<T>::kPerSum + l16 * V + v];
-        live |= (lists.at[Lists<T>::kLive + l16 * V + v] != 0.f ? 1u : 0u) << v;
+        const int n = l16 * V + v;
+        const float state = lists.at[List::kState + n];
+        const float per_sum = state == 3.f ? quiet_nan() : 1.f / sum[v];
+        live |= (state != 0.f ? 1u : 0u) << v;
+        per[v] = lists.factor(D, m0 + n, n) * per_sum;
+        if (threadIdx.x < 16) {
+            lists.at[List::kZMax + n] = top[v];
+            lists.at[List::kPerSum + n] = per_sum;
+            if (n >= first) lists.put_loss(D, m0, n, top[v], sum[v]);
+        }
     }
+    if (!D.grad) return;
+    T* grad = static_cast<T*>(D.grad);
     asm volatile("" : "+v"(c0));         // (nothing of the loads' addresses is kept)
-    T* p = grad + m + c0 * D.gcs;
+    T* p = grad + m0 + l16 * V + c0 * D.gcs;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         if (c0 + r < C) {
             float v[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                v[j] = V == 4 ? tile.c[r].value(j) : exp2_of((tile.c[r].value(j) - top[j]) * D.to_log2);
+                v[j] = sizeof(T) == 4 ? tile.c[r].value(j) : exp2_of((tile.c[r].value(j) - top[j]) * D.to_log2);
                 v[j] = live >> j & 1 ? v[j] * per[j] : 0.f;
             }
             if (l16 * V >= first) {
@@ -344,23 +357,23 @@ constexpr int kPartThreads = 256, kPartSpan = kPartThreads / 16 * 16;
 
 template <typename T>
 __global__ __launch_bounds__(kPartThreads) void distill_map_parts_kernel(Distill D, int64_t per_part, Part* parts) {
-    constexpr int V = Tile<T>::V;
+    constexpr int V = Tile<T, 4>::V;
     __shared__ float room[kPartThreads / 64 * 16 * V];
-    const int64_t m = (int64_t)blockIdx.x * Tile<T>::kTokens + (threadIdx.x & 15) * V;
+    const int64_t m = (int64_t)blockIdx.x * Tile<T, 4>::kTokens + (threadIdx.x & 15) * V;
     const int64_t c1 = min((blockIdx.y + 1) * per_part, D.C);
     const T* z = static_cast<const T*>(D.z);
     float top[V], sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) top[v] = -INFINITY, sum[v] = 0.f;
     for (int64_t c0 = blockIdx.y * per_part; c0 < c1; c0 += kPartSpan) {
-        Tile<T> tile;
+        Tile<T, 4> tile;
         tile.load(z + m, D.cs, c0 + (threadIdx.x >> 4) * 16, c1, D.M - m);
         float next[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) next[v] = top[v];
         tile.raise_into(next);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) forget(tile.c[r]);
+        for (int r = 0; r < 16; ++r) tile.c[r].forget();
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float to = next[v] == -INFINITY ? 0.f : next[v];
@@ -388,23 +401,29 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_parts_kernel(Distill
 template <typename T>
 __global__ __launch_bounds__(kPartThreads) void distill_map_finish_kernel(Distill D, int64_t per_part, const Part* parts, int n_parts,
                                                                           int with_loss) {
-    constexpr int V = Tile<T>::V, N = Tile<T>::kTokens;
+    constexpr int V = Tile<T, 4>::V, N = Tile<T, 4>::kTokens;
     extern __shared__ __align__(16) char lds[];
-    const Lists<T> lists = {reinterpret_cast<float*>(lds), D.k};
+    using List = Lists<T, N>;
+    const List lists = {reinterpret_cast<float*>(lds), D.k};
     const int64_t m0 = (int64_t)blockIdx.x * N, m = m0 + (threadIdx.x & 15) * V;
     const int64_t c_from = blockIdx.y * per_part, c1 = min(c_from + per_part, D.C);
     const int l16 = threadIdx.x & 15;
     const bool losses = with_loss && blockIdx.y == 0;
     const T* z = static_cast<const T*>(D.z);
     // (the student's logits of other parts may be their gradients already, if these are written over them)
-    lists.fill(D, m0, z, losses ? 0 : c_from, losses ? D.C : c1);
+    for (int n = threadIdx.x; n < D.k * N; n += kPartThreads)
+        lists.put(n, lists.read(D, m0, z, n, losses ? 0 : c_from, losses ? D.C : c1));
     __syncthreads();
     for (int n = threadIdx.x; n < N; n += kPartThreads) {
+        lists.sum_up(D, m0, n);
         if (m0 + n >= D.M) continue;
         Part all = {-INFINITY, 0.f};
         for (int p = 0; p < n_parts; ++p) all = joined(D, all, parts[(m0 + n) * n_parts + p]);
         // (a position of -infinities has the sum 0 here, and no softmax)
-        lists.finish(D, m0, n, all.top, all.top == -INFINITY ? quiet_nan() : all.sum, losses);
+        const float sum = all.top == -INFINITY ? quiet_nan() : all.sum;
+        lists.at[List::kZMax + n] = all.top;
+        lists.at[List::kPerSum + n] = lists.at[List::kState + n] == 3.f ? quiet_nan() : 1.f / sum;
+        if (losses) lists.put_loss(D, m0, n, all.top, sum);
     }
     if (!D.grad) return;
     __syncthreads();
@@ -414,12 +433,12 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_finish_kernel(Distil
         uint32_t live = 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const float* own = lists.at + l16 * V + v;
-            live |= (m + v < D.M && own[Lists<T>::kLive] != 0.f ? 1u : 0u) << v;
-            per[v] = own[Lists<T>::kG] * own[Lists<T>::kPerSum], top[v] = own[Lists<T>::kZMax];
+            const int n = l16 * V + v;
+            live |= (m + v < D.M && lists.at[List::kState + n] != 0.f ? 1u : 0u) << v;
+            per[v] = lists.factor(D, m0 + n, n) * lists.at[List::kPerSum + n], top[v] = lists.at[List::kZMax + n];
         }
         for (int64_t c0 = c_from + (threadIdx.x >> 4) * 16; c0 < c1; c0 += kPartSpan) {
-            Tile<T> tile;
+            Tile<T, 4> tile;
             tile.load(z + m, D.cs, c0, c1, D.M - m);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -448,18 +467,18 @@ hipError_t run_columns(const Distill& D, dss_dtype dt, hipStream_t s) {
     return hipSuccess;
 }
 
-template <typename T>
+template <typename T, int W>
 hipError_t run_tiles(const Distill& D, dss_dtype dt, hipStream_t s) {
-    constexpr int N = Tile<T>::kTokens;
+    constexpr int N = Tile<T, W>::kTokens;
     const int waves = (int)ceil_div64(D.C, 64);
-    const size_t lds = Lists<T>::bytes(D.k) + (size_t)waves * N * 4;
-    const hipError_t e = allow_dynamic_lds((const void*)distill_tile_kernel<T>, lds);
+    const size_t lds = Lists<T, N>::bytes(D.k) + (size_t)waves * N * 4;
+    const hipError_t e = allow_dynamic_lds((const void*)distill_tile_kernel<T, W>, lds);
     if (e != hipSuccess) return e;
     for (int64_t m = 0; m < D.M;) {
         // (what is left after this launch has a whole tile's positions)
         const int64_t n = D.M - m <= kSlabTokens ? D.M - m : kSlabTokens - N;
         const Distill S = positions(D, dt, m, n);
-        distill_tile_kernel<T><<<dim3((unsigned)ceil_div64(n, N)), waves * 64, lds, s>>>(S);
+        distill_tile_kernel<T, W><<<dim3((unsigned)ceil_div64(n, N)), waves * 64, lds, s>>>(S);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         m += n;
@@ -469,8 +488,8 @@ hipError_t run_tiles(const Distill& D, dss_dtype dt, hipStream_t s) {
 
 template <typename T>
 hipError_t run_map_parts(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
-    constexpr int N = Tile<T>::kTokens;
-    const size_t lds = Lists<T>::bytes(D.k);
+    constexpr int N = Tile<T, 4>::kTokens;
+    const size_t lds = Lists<T, N>::bytes(D.k);
     const hipError_t allowed = allow_dynamic_lds((const void*)distill_map_finish_kernel<T>, lds);
     if (allowed != hipSuccess) return allowed;
     constexpr int64_t slab = 65536;
@@ -504,7 +523,7 @@ hipError_t run_map(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
     if (D.C <= kColumns) return run_columns<T>(D, dt, s);
     // (lists of up to 128 places: 128 KB for 128 positions)
     if (D.k > 128) return launch_distill_any(D, dt, s);
-    return D.C <= 1024 && D.M >= Tile<T>::kTokens ? run_tiles<T>(D, dt, s) : run_map_parts<T>(D, dt, parts, s);
+    return D.C <= 1024 && D.M >= Tile<T, 2>::kTokens ? run_tiles<T, 2>(D, dt, s) : run_map_parts<T>(D, dt, parts, s);
 }
 
 }  // namespace
