@@ -20,7 +20,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCES = ["chain.cpp", "api.cpp", "device_attrs.cpp", "kernels_data.hip", "conv_direct.hip", "conv_mfma.hip", "backward.hip",
            "chain_fused.hip", "noalloc.hip", "grad_clip.hip", "tokens.hip", "matmul_tokens.hip",
            "matmul_few.hip", "linear_tile.hip", "mx4.hip", "few_mx4.hip", "matmul_mx4.hip", "distill.hip",
-           "distill_map.hip"]
+           "distill_map.hip", "linear_mx4.hip"]
 
 # -packed-fp32-ops: no v_pk_*_f32 code generation (device code only; the host
 # pass warns that it does not know the feature, which is harmless).

@@ -58,7 +58,7 @@ __global__ __launch_bounds__(kWaves * 64) void matmul_few_mx4_kernel(Mx4Layer L,
             for (int g = 0; g < GT; ++g) {
                 const i32x4 v = *reinterpret_cast<const i32x4*>(codes_f[g] + b * 16);
                 const uint32_t y = scale_f[g][b * D.F.scales_stride];
-                acc[g] = ADJ ? multiply_mx4(a[h], x[h], v, y, acc[g]) : multiply_mx4(v, y, a[h], x[h], acc[g]);
+                acc[g] = ADJ ? multiply_byte<0>(a[h], x[h], v, y, acc[g]) : multiply_byte<0>(v, y, a[h], x[h], acc[g]);
             }
         }
     }

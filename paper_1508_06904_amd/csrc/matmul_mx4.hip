@@ -64,23 +64,6 @@ __device__ __forceinline__ Scales<N> load_scales(const uint8_t* p, int shift) {
     return r;
 }
 
-template <int BYTE_A>
-__device__ __forceinline__ f32x4 multiply_byte(i32x4 q, uint32_t q_scale, i32x4 p, uint32_t p_scale, f32x4 c) {
-    using i32x8 = __attribute__((ext_vector_type(8))) int;
-    const i32x8 q8 = __builtin_shufflevector(q, q, 0, 1, 2, 3, -1, -1, -1, -1);
-    const i32x8 p8 = __builtin_shufflevector(p, p, 0, 1, 2, 3, -1, -1, -1, -1);
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(q8, p8, c, 4, 4, 0, (int)q_scale, BYTE_A, (int)p_scale);
-}
-// With the scale in byte a of p_scale (constant once the loops are unrolled).
-__device__ __forceinline__ f32x4 multiply_at(int a, i32x4 q, uint32_t q_scale, i32x4 p, uint32_t p_scale, f32x4 c) {
-    switch (a & 3) {
-        case 0: return multiply_byte<0>(q, q_scale, p, p_scale, c);
-        case 1: return multiply_byte<1>(q, q_scale, p, p_scale, c);
-        case 2: return multiply_byte<2>(q, q_scale, p, p_scale, c);
-        default: return multiply_byte<3>(q, q_scale, p, p_scale, c);
-    }
-}
-
 struct Sides {
     Mx4Rows P, Q;
 };
@@ -339,7 +322,8 @@ extern "C" dss_status dss_blocks_workspace(int64_t M, int32_t N, int32_t K, dss_
         return fail(DSS_E_INVALID, "unknown token source %d", (int)source);
     if (source != DSS_TOKENS_CODES && M > ((int64_t)1 << 62) / (blocks_of(K) * 17))
         return fail(DSS_E_INVALID, "the codes of %lld tokens of %d channels", (long long)M, K);
-    *workspace_bytes = source == DSS_TOKENS_CODES ? 0 : workspace_bytes_of(M, blocks_of(K));
+    const bool none = source == DSS_TOKENS_CODES || linear_mx4_at_once(M, N, K, source == DSS_TOKENS_MAP);
+    *workspace_bytes = none ? 0 : workspace_bytes_of(M, blocks_of(K));
     return DSS_OK;
 } catch (...) {
     return DSS_E_NOMEM;
@@ -376,11 +360,17 @@ extern "C" dss_status dss_linear_blocks(const void* x, dss_dtype dtype, int64_t 
     const Mx4Rows W = {weight, weight_stride, weight_scales, weight_scales_stride, N};
     s = check_layer(M, W, B, bias, act, out, out_dtype, out_token_stride, out_channel_stride);
     if (s != DSS_OK || M == 0) return s;
+    const bool from_map = channel_stride != 1 && K > 1;
     int64_t need = 0;
-    s = dss_blocks_workspace(M, N, K, channel_stride != 1 && K > 1 ? DSS_TOKENS_MAP : DSS_TOKENS_ROWS, &need);
+    s = dss_blocks_workspace(M, N, K, from_map ? DSS_TOKENS_MAP : DSS_TOKENS_ROWS, &need);
     if (s != DSS_OK) return s;
     s = check_room(need, workspace, workspace_bytes);
     if (s != DSS_OK) return s;
+    if (linear_mx4_at_once(M, N, K, from_map)) {
+        const Mx4Layer L = layer_of({nullptr, 0, nullptr, 0, M}, W, B, bias, act, out, out_dtype, out_token_stride, out_channel_stride);
+        hipError_t e = launch_linear_mx4(L, {x, dtype, K, token_stride, channel_stride}, out_dtype, stream);
+        return e == hipSuccess ? DSS_OK : hip_fail(e, "token product launch");
+    }
     uint8_t* codes = static_cast<uint8_t*>(workspace);
     uint8_t* scales = codes + align256(M * B * 16);
     hipError_t e = launch_quantize_mx4(dtype, x, M, K, token_stride, channel_stride, codes, B * 16, scales, M, stream);

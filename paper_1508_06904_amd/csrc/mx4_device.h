@@ -27,14 +27,69 @@ __device__ __forceinline__ uint32_t eight_codes(const float (&v)[8], float scale
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
 }
 
+// A block of 32 channels of V adjacent tokens of a map (W words of each channel), which a lane has in registers.
+template <typename T, int W = 4>
+struct MapBlock {
+    static constexpr int V = 4 * W / (int)sizeof(T);
+    static constexpr int kTokens = 16 * V;             // of a wave, of whose lanes 16 have adjacent tokens
+    uint32_t w[kBlock][W];
+
+    // Channel k of the block, token j.
+    __device__ __forceinline__ float value(int k, int j) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[k][j]);
+        else return __uint_as_float(j & 1 ? w[k][j / 2] & 0xffff0000u : w[k][j / 2] << 16);
+    }
+    __device__ __forceinline__ void load(const T* p, int64_t ks, int n) {
+#pragma unroll
+        for (int k = 0; k < kBlock; ++k) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[k][i] = 0;
+            if (k < n) __builtin_memcpy(w[k], p + k * ks, 4 * W);
+        }
+    }
+    __device__ __forceinline__ void scale_bytes(uint32_t (&byte)[V]) const {
+        uint32_t top[W] = {};
+#pragma unroll
+        for (int k = 0; k < kBlock; ++k)
+#pragma unroll
+            for (int i = 0; i < W; ++i) top[i] = raise<T>(top[i], w[k][i]);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            byte[j] = scale_byte(sizeof(T) == 4 ? top[j] : j & 1 ? top[j / 2] & 0xffff0000u : top[j / 2] << 16);
+    }
+    // The 32 codes of token j.
+    __device__ __forceinline__ i32x4 codes(int j, uint32_t byte) const {
+        const float scale = scale_operand(byte);
+        i32x4 r;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = value(8 * q + k, j);
+            r[q] = (int)(byte == 255u ? 0u : eight_codes(v, scale));
+        }
+        return r;
+    }
+};
+
 // c + the product of 16 rows of 128 codes each with 16 others. A lane has 32 adjacent codes of row
-// (lane & 15), block (lane >> 4), and their scale in the lowest byte; row r of the first operand and row
+// (lane & 15), block (lane >> 4), and their scale in the lowest byte of a_scale and in BYTE of b_scale; row r of the first operand and row
 // l of the second meet in lane (l, r >> 2), register r & 3.
-__device__ __forceinline__ f32x4 multiply_mx4(i32x4 a, uint32_t a_scale, i32x4 b, uint32_t b_scale, f32x4 c) {
+template <int BYTE>
+__device__ __forceinline__ f32x4 multiply_byte(i32x4 a, uint32_t a_scale, i32x4 b, uint32_t b_scale, f32x4 c) {
     using i32x8 = __attribute__((ext_vector_type(8))) int;
     const i32x8 a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
     const i32x8 b8 = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, 0, (int)a_scale, 0, (int)b_scale);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, 0, (int)a_scale, BYTE, (int)b_scale);
+}
+// (A byte that is constant once the loops are unrolled.)
+__device__ __forceinline__ f32x4 multiply_at(int byte, i32x4 a, uint32_t a_scale, i32x4 b, uint32_t b_scale, f32x4 c) {
+    switch (byte & 3) {
+        case 0: return multiply_byte<0>(a, a_scale, b, b_scale, c);
+        case 1: return multiply_byte<1>(a, a_scale, b, b_scale, c);
+        case 2: return multiply_byte<2>(a, a_scale, b, b_scale, c);
+        default: return multiply_byte<3>(a, a_scale, b, b_scale, c);
+    }
 }
 
 // N adjacent outputs from p on, which has place j of J; those past the end are left out.
