@@ -2,8 +2,9 @@
 // with a layer's weights, or many tokens with the weights of few outputs.
 //
 // Bound by the bytes of the other side, which are read once, straight from memory to matrix operands.
-// A wave takes R of its rows and a part of K in turns of kSlab blocks; the parts' sums are added
-// through LDS in the order of K.
+// A wave takes R of its rows at a time and a part of K in turns of kSlab blocks, two of them on their way; the parts'
+// sums are added through LDS in the order of K.  The few rows' codes are in LDS for all of a workgroup's waves; few tokens
+// that are values yet are coded there.
 #include <algorithm>
 
 #include "dev_common.h"
@@ -16,6 +17,7 @@ namespace dss {
 namespace {
 
 constexpr int kSlab = 16;                // blocks: four matrix instructions
+constexpr int kSteps = kSlab / 4;
 constexpr int kWaves = 8;
 
 // The streamed rows s, the few rows f, and D[s][f]: ADJ says whether s is the output's adjacent axis.
@@ -24,12 +26,171 @@ struct FewSides {
     int bias_on_s;
 };
 
+// The few rows' codes and scales in LDS: 16 bytes more for a row than it has, so that rows start in different banks.
+struct Held {
+    int B;
+    __host__ __device__ int pitch() const { return B * 16 + 16; }
+    __host__ __device__ int scale_pitch() const { return (B + 3) / 4 * 4 + 4; }
+    __host__ __device__ int64_t bytes(int64_t rows) const { return rows * (pitch() + scale_pitch()); }
+};
+
+// Codes what is in memory as values, M <= 16 tokens of K channels, into LDS.
+template <typename T>
+__device__ __forceinline__ void hold_values(const Mx4Values& X, int M, int B, uint8_t* codes, int pitch, uint8_t* scales, int scale_pitch) {
+    const int64_t K = X.channels;
+    if (X.channel_stride == 1) {
+        // four lanes for a block, with the loads of U of them under way
+        constexpr int U = 4;
+        const int quarters = M * B * 4, lane4 = threadIdx.x & 3;
+        for (int n0 = threadIdx.x; n0 < (quarters + 63) / 64 * 64; n0 += U * kWaves * 64) {
+            Eight<T> v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int n = (n0 + u * kWaves * 64) / 4, m = n / B, b = n - m * B;
+                const int64_t k = b * kBlock + lane4 * 8;
+                if (n < M * B) v[u].load(static_cast<const T*>(X.x) + m * X.token_stride + k, K - k);
+                else v[u].clear();
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int n = (n0 + u * kWaves * 64) / 4, m = n / B, b = n - m * B;
+                const uint32_t byte = v[u].scale_byte_of_four();
+                if (n >= M * B) continue;
+                *reinterpret_cast<uint32_t*>(codes + m * pitch + b * 16 + lane4 * 4) = v[u].codes(byte);
+                if (lane4 == 0) scales[m * scale_pitch + b] = (uint8_t)byte;
+            }
+        }
+    } else {
+        for (int n = threadIdx.x; n < M * B; n += kWaves * 64) {
+            const int b = n / M, m = n - b * M;
+            uint32_t byte;
+            const i32x4 w = block_codes(static_cast<const T*>(X.x) + m + b * kBlock * X.channel_stride, X.channel_stride,
+                                        (int)min((int64_t)kBlock, K - b * kBlock), byte);
+            *reinterpret_cast<i32x4*>(codes + m * pitch + b * 16) = w;
+            scales[m * scale_pitch + b] = (uint8_t)byte;
+        }
+    }
+}
+
+// X: uint8_t where the few rows are codes in memory, else their values' type.
+template <typename X, typename Tout, int GT, bool ADJ>
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))) void matmul_few_mx4_kernel(Mx4Layer L, FewSides D, Mx4Values V, int R, int parts) {
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, q16 = lane >> 4;
+    const int part = wave % parts, side = wave / parts, sides = kWaves / parts;
+    const int B = L.B, rows_f = (int)D.F.rows;
+    const Held held = {B};
+    f32x4* const sums = reinterpret_cast<f32x4*>(lds);                   // [kWaves][GT][64]
+    uint8_t* const codes = lds + kWaves * GT * 64 * 16;
+    uint8_t* const scales = codes + rows_f * held.pitch();
+    const int64_t tiles = (D.S.rows + R - 1) / R, turns = (tiles - (int64_t)blockIdx.x * sides + (int64_t)gridDim.x * sides - 1) / ((int64_t)gridDim.x * sides);
+    const int slabs = (B + kSlab - 1) / kSlab, own = (slabs - part + parts - 1) / parts;     // of them the wave's
+
+    // A slab of a tile's rows: past the end of K the last block with zeros for its codes (its scales count already).
+    struct Slab {
+        i32x4 a[kSteps];
+        uint32_t x[kSteps];
+    };
+    auto tile_of = [&](int64_t turn) { return ((int64_t)blockIdx.x + turn * gridDim.x) * sides + side; };
+    auto fetch = [&](Slab& to, int64_t turn, int n) {
+        const int64_t s = min(min(tile_of(turn), tiles - 1) * R + min(l16, R - 1), D.S.rows - 1);
+        const uint8_t *c = D.S.codes + s * D.S.stride, *x = D.S.scales + s;
+#pragma unroll
+        for (int h = 0; h < kSteps; ++h) {
+            const int at = (part + n * parts) * kSlab + h * 4 + q16, b = min(at, B - 1);
+            to.a[h] = *reinterpret_cast<const i32x4*>(c + (int64_t)b * 16);
+            if (b != at) to.a[h] = i32x4{};
+            to.x[h] = x[b * D.S.scales_stride];
+        }
+    };
+    Slab next[2];
+    // the first slabs are on their way while the few rows are put into LDS
+    int64_t turn1 = 0;                   // the turn and place of the slab to fetch next
+    int at1 = 0;
+    auto ahead = [&](Slab& to) {
+        fetch(to, turn1, at1);
+        if (++at1 >= own) at1 = 0, ++turn1;
+    };
+    if (own > 0) {
+        ahead(next[0]);
+        ahead(next[1]);
+    }
+    if constexpr (sizeof(X) == 1) {
+        for (int n = threadIdx.x; n < rows_f * B; n += kWaves * 64) {
+            const int f = n / B, b = n - f * B;
+            *reinterpret_cast<i32x4*>(codes + f * held.pitch() + b * 16) = *reinterpret_cast<const i32x4*>(D.F.codes + f * D.F.stride + b * 16);
+        }
+        for (int n = threadIdx.x; n < rows_f * B; n += kWaves * 64) {
+            const int b = n / rows_f, f = n - b * rows_f;
+            scales[f * held.scale_pitch() + b] = D.F.scales[b * D.F.scales_stride + f];
+        }
+    } else {
+        hold_values<X>(V, rows_f, B, codes, held.pitch(), scales, held.scale_pitch());
+    }
+    __syncthreads();
+    int buffer = 0;
+    for (int64_t turn = 0; turn < turns; ++turn) {
+        f32x4 acc[GT] = {};
+        auto multiply = [&](const Slab& use, int n) {
+#pragma unroll
+            for (int h = 0; h < kSteps; ++h) {
+                const int b = min((part + n * parts) * kSlab + h * 4 + q16, B - 1);
+#pragma unroll
+                for (int g = 0; g < GT; ++g) {
+                    const int f = min(g * 16 + l16, rows_f - 1);
+                    const i32x4 v = *reinterpret_cast<const i32x4*>(codes + f * held.pitch() + b * 16);
+                    const uint32_t y = scales[f * held.scale_pitch() + b];
+                    acc[g] = ADJ ? multiply_byte<0>(use.a[h], use.x[h], v, y, acc[g]) : multiply_byte<0>(v, y, use.a[h], use.x[h], acc[g]);
+                }
+            }
+        };
+        for (int n = 0; n < own; ++n) {
+            // (the slabs are named, so that they stay in registers)
+            if (buffer == 0) {
+                const Slab use = next[0];
+                ahead(next[0]);
+                multiply(use, n);
+            } else {
+                const Slab use = next[1];
+                ahead(next[1]);
+                multiply(use, n);
+            }
+            buffer ^= 1;
+        }
+        const int64_t s0 = tile_of(turn) * R, s_end = min(s0 + R, D.S.rows);
+        if (parts > 1) {
+            if (turn) __syncthreads();   // the sums of the last turn have been read
+#pragma unroll
+            for (int g = 0; g < GT; ++g) sums[(wave * GT + g) * 64 + lane] = acc[g];
+            __syncthreads();
+        }
+#pragma unroll
+        for (int g = 0; g < GT; ++g) {
+            if (g % parts != part) continue;
+            f32x4 sum = acc[g];
+            if (parts > 1) {
+                sum = sums[((wave - part) * GT + g) * 64 + lane];
+                for (int p = 1; p < parts; ++p) sum += sums[((wave - part + p) * GT + g) * 64 + lane];
+            }
+            const int64_t i = ADJ ? g * 16 + l16 : s0 + l16, j = ADJ ? s0 + q16 * 4 : g * 16 + q16 * 4;
+            const int64_t I = ADJ ? rows_f : s_end, J = ADJ ? s_end : rows_f;
+            if (i >= I || j >= J) continue;
+            const bool bias_on_j = ADJ == (D.bias_on_s != 0);
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                v[k] = activate_nan(L.act, sum[k] + (L.bias ? L.bias[bias_on_j ? min(j + k, J - 1) : i] : 0.f));
+            store_values(static_cast<Tout*>(L.out) + i * L.ldo + j, v, j, J, 0);
+        }
+    }
+}
+
+// Rows of which LDS does not hold one (over 200 thousand channels): the few rows are read from memory too.
 template <typename Tout, int GT, bool ADJ>
-__global__ __launch_bounds__(kWaves * 64) void matmul_few_mx4_kernel(Mx4Layer L, FewSides D, int R, int parts) {
+__global__ __launch_bounds__(kWaves * 64) void matmul_long_mx4_kernel(Mx4Layer L, FewSides D, int R) {
     __shared__ f32x4 sums[kWaves][GT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, q16 = lane >> 4;
-    const int part = wave % parts;
-    const int64_t s0 = ((int64_t)blockIdx.x * (kWaves / parts) + wave / parts) * R;
+    const int64_t s0 = (int64_t)blockIdx.x * R;
     const int64_t s = min(s0 + min(l16, R - 1), D.S.rows - 1);
     const uint8_t *codes_s = D.S.codes + s * D.S.stride, *scale_s = D.S.scales + s;
     const uint8_t *codes_f[GT], *scale_f[GT];
@@ -40,11 +201,11 @@ __global__ __launch_bounds__(kWaves * 64) void matmul_few_mx4_kernel(Mx4Layer L,
         scale_f[g] = D.F.scales + f;
     }
     f32x4 acc[GT] = {};
-    for (int64_t b0 = (int64_t)part * kSlab; b0 < L.B; b0 += (int64_t)parts * kSlab) {
-        i32x4 a[kSlab / 4];
-        uint32_t x[kSlab / 4];
+    for (int64_t b0 = (int64_t)wave * kSlab; b0 < L.B; b0 += kWaves * kSlab) {
+        i32x4 a[kSteps];
+        uint32_t x[kSteps];
 #pragma unroll
-        for (int h = 0; h < kSlab / 4; ++h) {
+        for (int h = 0; h < kSteps; ++h) {
             // past the end of K: the last block with zeros for one side's codes (its scales count already)
             const int64_t b = min(b0 + h * 4 + q16, (int64_t)L.B - 1);
             a[h] = *reinterpret_cast<const i32x4*>(codes_s + b * 16);
@@ -52,7 +213,7 @@ __global__ __launch_bounds__(kWaves * 64) void matmul_few_mx4_kernel(Mx4Layer L,
             x[h] = scale_s[b * D.S.scales_stride];
         }
 #pragma unroll
-        for (int h = 0; h < kSlab / 4; ++h) {
+        for (int h = 0; h < kSteps; ++h) {
             const int64_t b = min(b0 + h * 4 + q16, (int64_t)L.B - 1);
 #pragma unroll
             for (int g = 0; g < GT; ++g) {
@@ -65,13 +226,15 @@ __global__ __launch_bounds__(kWaves * 64) void matmul_few_mx4_kernel(Mx4Layer L,
 #pragma unroll
     for (int g = 0; g < GT; ++g) sums[wave][g][lane] = acc[g];
     __syncthreads();
-    for (int g = part; g < GT; g += parts) {
-        f32x4 sum = sums[wave - part][g][lane];
-        for (int p = 1; p < parts; ++p) sum += sums[wave - part + p][g][lane];
+    if (wave >= GT) return;
+    {
+        const int g = wave;
+        f32x4 sum = sums[0][g][lane];
+        for (int p = 1; p < kWaves; ++p) sum += sums[p][g][lane];
         const int64_t s_end = min(s0 + R, D.S.rows);
         const int64_t i = ADJ ? g * 16 + l16 : s0 + l16, j = ADJ ? s0 + q16 * 4 : g * 16 + q16 * 4;
         const int64_t I = ADJ ? D.F.rows : s_end, J = ADJ ? s_end : D.F.rows;
-        if (i >= I || j >= J) continue;
+        if (i >= I || j >= J) return;
         const bool bias_on_j = ADJ == (D.bias_on_s != 0);
         float v[4];
 #pragma unroll
@@ -81,30 +244,55 @@ __global__ __launch_bounds__(kWaves * 64) void matmul_few_mx4_kernel(Mx4Layer L,
     }
 }
 
-template <typename Tout, int GT>
-hipError_t run_few(const Mx4Layer& L, const FewSides& D, bool adj, hipStream_t s) {
-    // as many waves share K as have a slab of it; few rows are spread over all units
+// LDS of a launch with G groups of 16 few rows.
+int64_t lds_of(int B, int64_t rows, int G) { return (int64_t)kWaves * G * 64 * 16 + Held{B}.bytes(rows); }
+constexpr int64_t kMostLds = 160 * 1024;
+
+template <typename X, typename Tout, int GT>
+hipError_t run_few(const Mx4Layer& L, const FewSides& D, const Mx4Values& V, bool adj, hipStream_t s) {
+    // few rows are spread over all units, and K is shared while there are fewer waves than units have room for
     int parts = 1, R = 16;
-    while (parts < kWaves && parts * kSlab < L.B) parts *= 2;
-    while (R > 2 && ceil_div64(D.S.rows, R * (kWaves / parts)) < 256) R /= 2;
-    const int64_t groups = ceil_div64(D.S.rows, R * (kWaves / parts));
-    const auto kern = adj ? matmul_few_mx4_kernel<Tout, GT, true> : matmul_few_mx4_kernel<Tout, GT, false>;
+    while (R > 2 && ceil_div64(D.S.rows, R) < 256) R /= 2;
+    while (parts < kWaves && parts * kSlab < L.B && ceil_div64(D.S.rows, R) * parts < 2048) parts *= 2;
+    const int64_t groups = ceil_div64(ceil_div64(D.S.rows, R), kWaves / parts);
+    const auto kern = adj ? matmul_few_mx4_kernel<X, Tout, GT, true> : matmul_few_mx4_kernel<X, Tout, GT, false>;
+    const int64_t lds = lds_of(L.B, D.F.rows, GT);
+    const hipError_t e = allow_dynamic_lds((const void*)kern, (size_t)lds);
+    if (e != hipSuccess) return e;
+    const int64_t resident = 256 * std::max<int64_t>(1, std::min<int64_t>(2, kMostLds / lds));
+    kern<<<dim3((unsigned)std::min(groups, resident)), kWaves * 64, (size_t)lds, s>>>(L, D, V, R, parts);
+    return hipGetLastError();
+}
+
+template <typename Tout, int GT>
+hipError_t run_long(const Mx4Layer& L, const FewSides& D, bool adj, hipStream_t s) {
+    int R = 16;
+    while (R > 2 && ceil_div64(D.S.rows, R) < 256) R /= 2;
+    const auto kern = adj ? matmul_long_mx4_kernel<Tout, GT, true> : matmul_long_mx4_kernel<Tout, GT, false>;
     // a launch has fewer than 2^32 threads
-    const int64_t most = (int64_t)1 << 22, rows = most * R * (kWaves / parts);
-    for (int64_t at = 0; at < groups; at += most) {
+    const int64_t rows = (int64_t)R << 22;
+    for (int64_t at = 0; at < D.S.rows; at += rows) {
         Mx4Layer P = L;
         FewSides E = D;
-        const int64_t s0 = at / most * rows;
-        E.S.codes += s0 * D.S.stride;
-        E.S.scales += s0;
-        E.S.rows = std::min(rows, D.S.rows - s0);
-        P.out = static_cast<Tout*>(L.out) + s0 * (adj ? 1 : L.ldo);
-        if (L.bias && D.bias_on_s) P.bias += s0;
-        kern<<<dim3((unsigned)std::min(most, groups - at)), kWaves * 64, 0, s>>>(P, E, R, parts);
+        E.S.codes += at * D.S.stride;
+        E.S.scales += at;
+        E.S.rows = std::min(rows, D.S.rows - at);
+        P.out = static_cast<Tout*>(L.out) + at * (adj ? 1 : L.ldo);
+        if (L.bias && D.bias_on_s) P.bias += at;
+        kern<<<dim3((unsigned)ceil_div64(E.S.rows, R)), kWaves * 64, 0, s>>>(P, E, R);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+template <typename X>
+hipError_t run_types(const Mx4Layer& L, const FewSides& D, const Mx4Values& V, dss_dtype out_dtype, bool adj, hipStream_t s) {
+    if constexpr (sizeof(X) == 1) {
+        if (D.F.rows > 16)
+            return out_dtype == DSS_BF16 ? run_few<X, uint16_t, 2>(L, D, V, adj, s) : run_few<X, float, 2>(L, D, V, adj, s);
+    }
+    return out_dtype == DSS_BF16 ? run_few<X, uint16_t, 1>(L, D, V, adj, s) : run_few<X, float, 1>(L, D, V, adj, s);
 }
 
 }  // namespace
@@ -113,8 +301,34 @@ hipError_t launch_few_mx4(const Mx4Layer& L, dss_dtype out_dtype, hipStream_t s)
     const bool tokens = L.tokens.rows <= kFewRows;       // else the outputs are few
     const FewSides D = tokens ? FewSides{L.weight, L.tokens, 1} : FewSides{L.tokens, L.weight, 0};
     const bool adj = tokens != (L.map != 0);
-    if (D.F.rows > 16) return out_dtype == DSS_BF16 ? run_few<uint16_t, 2>(L, D, adj, s) : run_few<float, 2>(L, D, adj, s);
-    return out_dtype == DSS_BF16 ? run_few<uint16_t, 1>(L, D, adj, s) : run_few<float, 1>(L, D, adj, s);
+    // as many of the few rows at a time as LDS holds
+    const int64_t most = (kMostLds - kWaves * 2 * 64 * 16) / Held{L.B}.bytes(1);
+    if (most == 0) {
+        if (D.F.rows > 16) return out_dtype == DSS_BF16 ? run_long<uint16_t, 2>(L, D, adj, s) : run_long<float, 2>(L, D, adj, s);
+        return out_dtype == DSS_BF16 ? run_long<uint16_t, 1>(L, D, adj, s) : run_long<float, 1>(L, D, adj, s);
+    }
+    for (int64_t f = 0; f < D.F.rows; f += most) {
+        Mx4Layer P = L;
+        FewSides E = D;
+        E.F.rows = std::min(most, D.F.rows - f);
+        E.F.codes += f * D.F.stride;
+        E.F.scales += f;
+        P.out = static_cast<char*>(L.out) + f * (adj ? L.ldo : 1) * (int64_t)dtype_size(out_dtype);
+        if (L.bias && !D.bias_on_s) P.bias += f;
+        const hipError_t e = run_types<uint8_t>(P, E, Mx4Values{}, out_dtype, adj, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+bool few_codes_itself(int64_t M, int64_t N, int64_t K) {
+    return M <= 16 && M * K <= 65536;
+}
+
+hipError_t launch_linear_few_mx4(const Mx4Layer& L, const Mx4Values& X, dss_dtype out_dtype, hipStream_t s) {
+    const FewSides D = {L.weight, L.tokens, 1};
+    return X.dtype == DSS_BF16 ? run_types<uint16_t>(L, D, X, out_dtype, L.map == 0, s)
+                               : run_types<float>(L, D, X, out_dtype, L.map == 0, s);
 }
 
 }  // namespace dss

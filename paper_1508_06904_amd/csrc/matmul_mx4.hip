@@ -322,7 +322,7 @@ extern "C" dss_status dss_blocks_workspace(int64_t M, int32_t N, int32_t K, dss_
         return fail(DSS_E_INVALID, "unknown token source %d", (int)source);
     if (source != DSS_TOKENS_CODES && M > ((int64_t)1 << 62) / (blocks_of(K) * 17))
         return fail(DSS_E_INVALID, "the codes of %lld tokens of %d channels", (long long)M, K);
-    const bool none = source == DSS_TOKENS_CODES || linear_mx4_at_once(M, N, K, source == DSS_TOKENS_MAP);
+    const bool none = source == DSS_TOKENS_CODES || few_codes_itself(M, N, K) || linear_mx4_at_once(M, N, K, source == DSS_TOKENS_MAP);
     *workspace_bytes = none ? 0 : workspace_bytes_of(M, blocks_of(K));
     return DSS_OK;
 } catch (...) {
@@ -366,9 +366,11 @@ extern "C" dss_status dss_linear_blocks(const void* x, dss_dtype dtype, int64_t 
     if (s != DSS_OK) return s;
     s = check_room(need, workspace, workspace_bytes);
     if (s != DSS_OK) return s;
-    if (linear_mx4_at_once(M, N, K, from_map)) {
+    const bool few = few_codes_itself(M, N, K);
+    if (few || linear_mx4_at_once(M, N, K, from_map)) {
         const Mx4Layer L = layer_of({nullptr, 0, nullptr, 0, M}, W, B, bias, act, out, out_dtype, out_token_stride, out_channel_stride);
-        hipError_t e = launch_linear_mx4(L, {x, dtype, K, token_stride, channel_stride}, out_dtype, stream);
+        const Mx4Values X = {x, dtype, K, token_stride, channel_stride};
+        hipError_t e = few ? launch_linear_few_mx4(L, X, out_dtype, stream) : launch_linear_mx4(L, X, out_dtype, stream);
         return e == hipSuccess ? DSS_OK : hip_fail(e, "token product launch");
     }
     uint8_t* codes = static_cast<uint8_t*>(workspace);

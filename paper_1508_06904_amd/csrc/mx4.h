@@ -45,12 +45,15 @@ struct Mx4Values {
 hipError_t launch_quantize_mx4(dss_dtype dt, const void* x, int64_t M, int K, int64_t token_stride, int64_t channel_stride,
                                uint8_t* codes, int64_t codes_stride, uint8_t* scales, int64_t scales_stride, hipStream_t s);
 
-// The layer where one side has at most kFewRows rows.
-constexpr int kFewRows = 32;
-hipError_t launch_few_mx4(const Mx4Layer& L, dss_dtype out_dtype, hipStream_t s);
-
 // The layer on the tokens of a map, coded and multiplied in one launch (linear_mx4.hip), and whether it runs there.
 bool linear_mx4_at_once(int64_t M, int64_t N, int64_t K, bool map);
 hipError_t launch_linear_mx4(const Mx4Layer& L, const Mx4Values& X, dss_dtype out_dtype, hipStream_t s);
+
+// The layer where one side has at most kFewRows rows (few_mx4.hip); and on so few tokens that the kernel codes them itself,
+// and whether it does.
+constexpr int kFewRows = 32;
+hipError_t launch_few_mx4(const Mx4Layer& L, dss_dtype out_dtype, hipStream_t s);
+bool few_codes_itself(int64_t M, int64_t N, int64_t K);
+hipError_t launch_linear_few_mx4(const Mx4Layer& L, const Mx4Values& X, dss_dtype out_dtype, hipStream_t s);
 
 }  // namespace dss

@@ -20,31 +20,6 @@ constexpr int kThreads = 256;
 // token at a time. The scales turn round in LDS, so that those of adjacent tokens leave together.
 constexpr int kRowTokens = 32, kRowBlocks = 16;
 
-// Eight adjacent channels of a lane.
-template <typename T>
-struct Eight {
-    Chunk<T> c[8 / Chunk<T>::E];
-
-    // From p on, those from n on as zeros (n may be negative).
-    __device__ __forceinline__ void load(const T* p, int64_t n) {
-#pragma unroll
-        for (int i = 0; i < 8 / Chunk<T>::E; ++i)
-            c[i] = load_chunk(p + i * Chunk<T>::E, (int)max(min(n - i * Chunk<T>::E, (int64_t)8), (int64_t)0));
-    }
-    __device__ __forceinline__ uint32_t top() const {
-        uint32_t t = 0;
-#pragma unroll
-        for (int i = 0; i < 8 / Chunk<T>::E; ++i) t = raise(t, c[i]);
-        return top_bits<T>(t);
-    }
-    __device__ __forceinline__ uint32_t codes(uint32_t byte) const {
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = c[k / Chunk<T>::E].value(k % Chunk<T>::E);
-        return byte == 255u ? 0u : eight_codes(v, scale_operand(byte));
-    }
-};
-
 template <typename T>
 __global__ __launch_bounds__(kThreads) void quantize_mx4_rows_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t ts,
                                                                      uint8_t* __restrict__ codes, int64_t codes_stride,
@@ -60,10 +35,7 @@ __global__ __launch_bounds__(kThreads) void quantize_mx4_rows_kernel(const T* __
         if (m0 + wave * PER + n < M) v[n].load(x + (m0 + wave * PER + n) * ts + k, K - k);
 #pragma unroll
     for (int n = 0; n < PER; ++n) {
-        uint32_t top = v[n].top();
-        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-        const uint32_t byte = scale_byte(top);
+        const uint32_t byte = v[n].scale_byte_of_four();
         const int64_t m = m0 + wave * PER + n;
         if (m < M && b * kBlock < K) *reinterpret_cast<uint32_t*>(codes + m * codes_stride + k / 2) = v[n].codes(byte);
         if ((lane & 3) == 0) bytes[lane >> 2][wave * PER + n] = (uint8_t)byte;
@@ -110,23 +82,8 @@ __global__ __launch_bounds__(kThreads) void quantize_mx4_narrow_kernel(const T* 
                                                                        uint8_t* __restrict__ scales, int64_t scales_stride) {
     const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, b = id / M, m = id - b * M, k0 = b * kBlock;
     if (k0 >= K) return;
-    const T* p = x + m + k0 * ks;
-    const int n = (int)min((int64_t)kBlock, K - k0);
-    float v[kBlock];
-    uint32_t top = 0;
-#pragma unroll
-    for (int k = 0; k < kBlock; ++k) {
-        v[k] = k < n ? to_f32(p[k * ks]) : 0.f;
-        top = max(top, abs_bits(v[k]));
-    }
-    const uint32_t byte = scale_byte(top);
-    i32x4 w;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float e[8] = {v[8 * j], v[8 * j + 1], v[8 * j + 2], v[8 * j + 3], v[8 * j + 4], v[8 * j + 5], v[8 * j + 6], v[8 * j + 7]};
-        w[j] = byte == 255u ? 0 : (int)eight_codes(e, scale_operand(byte));
-    }
-    *reinterpret_cast<i32x4*>(codes + m * codes_stride + b * 16) = w;
+    uint32_t byte;
+    *reinterpret_cast<i32x4*>(codes + m * codes_stride + b * 16) = block_codes(x + m + k0 * ks, ks, (int)min((int64_t)kBlock, K - k0), byte);
     scales[b * scales_stride + m] = (uint8_t)byte;
 }
 

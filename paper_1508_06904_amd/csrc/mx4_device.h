@@ -27,6 +27,59 @@ __device__ __forceinline__ uint32_t eight_codes(const float (&v)[8], float scale
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
 }
 
+// Eight adjacent channels of a row, a quarter of a block: four adjacent lanes have a block.
+template <typename T>
+struct Eight {
+    Chunk<T> c[8 / Chunk<T>::E];
+
+    // From p on, those from n on as zeros (n may be negative).
+    __device__ __forceinline__ void load(const T* p, int64_t n) {
+#pragma unroll
+        for (int i = 0; i < 8 / Chunk<T>::E; ++i)
+            c[i] = load_chunk(p + i * Chunk<T>::E, (int)max(min(n - i * Chunk<T>::E, (int64_t)8), (int64_t)0));
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 8 / Chunk<T>::E; ++i) c[i] = Chunk<T>{};
+    }
+    // The scale of the four lanes' block.
+    __device__ __forceinline__ uint32_t scale_byte_of_four() const {
+        uint32_t t = 0;
+#pragma unroll
+        for (int i = 0; i < 8 / Chunk<T>::E; ++i) t = raise(t, c[i]);
+        t = top_bits<T>(t);
+        t = max(t, (uint32_t)__shfl_xor((int)t, 1));
+        t = max(t, (uint32_t)__shfl_xor((int)t, 2));
+        return scale_byte(t);
+    }
+    __device__ __forceinline__ uint32_t codes(uint32_t byte) const {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c[k / Chunk<T>::E].value(k % Chunk<T>::E);
+        return byte == 255u ? 0u : eight_codes(v, scale_operand(byte));
+    }
+};
+
+// A block of n channels from p on, `stride` apart: its codes, and its scale in `byte`.
+template <typename T>
+__device__ __forceinline__ i32x4 block_codes(const T* p, int64_t stride, int n, uint32_t& byte) {
+    float v[kBlock];
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < kBlock; ++k) {
+        v[k] = k < n ? to_f32(p[k * stride]) : 0.f;
+        top = max(top, abs_bits(v[k]));
+    }
+    byte = scale_byte(top);
+    i32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float e[8] = {v[8 * j], v[8 * j + 1], v[8 * j + 2], v[8 * j + 3], v[8 * j + 4], v[8 * j + 5], v[8 * j + 6], v[8 * j + 7]};
+        w[j] = byte == 255u ? 0 : (int)eight_codes(e, scale_operand(byte));
+    }
+    return w;
+}
+
 // A block of 32 channels of V adjacent tokens of a map (W words of each channel), which a lane has in registers.
 template <typename T, int W = 4>
 struct MapBlock {
