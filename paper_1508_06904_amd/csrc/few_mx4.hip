@@ -72,18 +72,36 @@ __device__ __forceinline__ void hold_values(const Mx4Values& X, int M, int B, ui
     }
 }
 
+constexpr int kSums = kWaves * 64 * 16;  // bytes of the parts' sums
+
+// A lane's outputs of rows s0 .. s_end-1: ADJ: four adjacent ones of few row l16; else of row s0 + l16.
+template <typename Tout, bool ADJ>
+__device__ __forceinline__ void store_few(const Mx4Layer& L, const FewSides& D, f32x4 sum, int64_t s0, int64_t s_end) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q16 = lane >> 4;
+    const int64_t i = ADJ ? l16 : s0 + l16, j = ADJ ? s0 + q16 * 4 : q16 * 4;
+    const int64_t I = ADJ ? D.F.rows : s_end, J = ADJ ? s_end : D.F.rows;
+    if (i >= I || j >= J) return;
+    const bool bias_on_j = ADJ == (D.bias_on_s != 0);
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = activate_nan(L.act, sum[k] + (L.bias ? L.bias[bias_on_j ? min(j + k, J - 1) : i] : 0.f));
+    store_values(static_cast<Tout*>(L.out) + i * L.ldo + j, v, j, J, 0);
+}
+
 // X: uint8_t where the few rows are codes in memory, else their values' type.
-template <typename X, typename Tout, int GT, bool ADJ>
+template <typename X, typename Tout, bool ADJ>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))) void matmul_few_mx4_kernel(Mx4Layer L, FewSides D, Mx4Values V, int R, int parts) {
     extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, q16 = lane >> 4;
     const int part = wave % parts, side = wave / parts, sides = kWaves / parts;
-    const int B = L.B, rows_f = (int)D.F.rows;
+    const int B = L.B, rows_f = (int)D.F.rows, own_f = min(l16, rows_f - 1);
     const Held held = {B};
-    f32x4* const sums = reinterpret_cast<f32x4*>(lds);                   // [kWaves][GT][64]
-    uint8_t* const codes = lds + kWaves * GT * 64 * 16;
+    f32x4* const sums = reinterpret_cast<f32x4*>(lds);                   // [kWaves][64]
+    uint8_t* const codes = lds + kSums;
     uint8_t* const scales = codes + rows_f * held.pitch();
-    const int64_t tiles = (D.S.rows + R - 1) / R, turns = (tiles - (int64_t)blockIdx.x * sides + (int64_t)gridDim.x * sides - 1) / ((int64_t)gridDim.x * sides);
+    // (neighbours on one XCD: a line of scales belongs to 128 rows)
+    const int64_t first = xcd_order(blockIdx.x, gridDim.x), all = (int64_t)gridDim.x * sides;
+    const int64_t tiles = (D.S.rows + R - 1) / R, turns = (tiles - first * sides + all - 1) / all;
     const int slabs = (B + kSlab - 1) / kSlab, own = (slabs - part + parts - 1) / parts;     // of them the wave's
 
     // A slab of a tile's rows: past the end of K the last block with zeros for its codes (its scales count already).
@@ -91,7 +109,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))
         i32x4 a[kSteps];
         uint32_t x[kSteps];
     };
-    auto tile_of = [&](int64_t turn) { return ((int64_t)blockIdx.x + turn * gridDim.x) * sides + side; };
+    auto tile_of = [&](int64_t turn) { return first * sides + turn * all + side; };
     auto fetch = [&](Slab& to, int64_t turn, int n) {
         const int64_t s = min(min(tile_of(turn), tiles - 1) * R + min(l16, R - 1), D.S.rows - 1);
         const uint8_t *c = D.S.codes + s * D.S.stride, *x = D.S.scales + s;
@@ -130,18 +148,14 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))
     __syncthreads();
     int buffer = 0;
     for (int64_t turn = 0; turn < turns; ++turn) {
-        f32x4 acc[GT] = {};
+        f32x4 acc = {};
         auto multiply = [&](const Slab& use, int n) {
 #pragma unroll
             for (int h = 0; h < kSteps; ++h) {
                 const int b = min((part + n * parts) * kSlab + h * 4 + q16, B - 1);
-#pragma unroll
-                for (int g = 0; g < GT; ++g) {
-                    const int f = min(g * 16 + l16, rows_f - 1);
-                    const i32x4 v = *reinterpret_cast<const i32x4*>(codes + f * held.pitch() + b * 16);
-                    const uint32_t y = scales[f * held.scale_pitch() + b];
-                    acc[g] = ADJ ? multiply_byte<0>(use.a[h], use.x[h], v, y, acc[g]) : multiply_byte<0>(v, y, use.a[h], use.x[h], acc[g]);
-                }
+                const i32x4 v = *reinterpret_cast<const i32x4*>(codes + own_f * held.pitch() + b * 16);
+                const uint32_t y = scales[own_f * held.scale_pitch() + b];
+                acc = ADJ ? multiply_byte<0>(use.a[h], use.x[h], v, y, acc) : multiply_byte<0>(v, y, use.a[h], use.x[h], acc);
             }
         };
         for (int n = 0; n < own; ++n) {
@@ -157,50 +171,29 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))
             }
             buffer ^= 1;
         }
-        const int64_t s0 = tile_of(turn) * R, s_end = min(s0 + R, D.S.rows);
+        const int64_t s0 = tile_of(turn) * R;
         if (parts > 1) {
             if (turn) __syncthreads();   // the sums of the last turn have been read
-#pragma unroll
-            for (int g = 0; g < GT; ++g) sums[(wave * GT + g) * 64 + lane] = acc[g];
+            sums[wave * 64 + lane] = acc;
             __syncthreads();
+            if (part > 0) continue;
+            for (int p = 1; p < parts; ++p) acc += sums[(wave + p) * 64 + lane];
         }
-#pragma unroll
-        for (int g = 0; g < GT; ++g) {
-            if (g % parts != part) continue;
-            f32x4 sum = acc[g];
-            if (parts > 1) {
-                sum = sums[((wave - part) * GT + g) * 64 + lane];
-                for (int p = 1; p < parts; ++p) sum += sums[((wave - part + p) * GT + g) * 64 + lane];
-            }
-            const int64_t i = ADJ ? g * 16 + l16 : s0 + l16, j = ADJ ? s0 + q16 * 4 : g * 16 + q16 * 4;
-            const int64_t I = ADJ ? rows_f : s_end, J = ADJ ? s_end : rows_f;
-            if (i >= I || j >= J) continue;
-            const bool bias_on_j = ADJ == (D.bias_on_s != 0);
-            float v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                v[k] = activate_nan(L.act, sum[k] + (L.bias ? L.bias[bias_on_j ? min(j + k, J - 1) : i] : 0.f));
-            store_values(static_cast<Tout*>(L.out) + i * L.ldo + j, v, j, J, 0);
-        }
+        store_few<Tout, ADJ>(L, D, acc, s0, min(s0 + R, D.S.rows));
     }
 }
 
 // Rows of which LDS does not hold one (over 200 thousand channels): the few rows are read from memory too.
-template <typename Tout, int GT, bool ADJ>
+template <typename Tout, bool ADJ>
 __global__ __launch_bounds__(kWaves * 64) void matmul_long_mx4_kernel(Mx4Layer L, FewSides D, int R) {
-    __shared__ f32x4 sums[kWaves][GT][64];
+    __shared__ f32x4 sums[kWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, q16 = lane >> 4;
     const int64_t s0 = (int64_t)blockIdx.x * R;
     const int64_t s = min(s0 + min(l16, R - 1), D.S.rows - 1);
     const uint8_t *codes_s = D.S.codes + s * D.S.stride, *scale_s = D.S.scales + s;
-    const uint8_t *codes_f[GT], *scale_f[GT];
-#pragma unroll
-    for (int g = 0; g < GT; ++g) {
-        const int64_t f = min((int64_t)(g * 16 + l16), D.F.rows - 1);
-        codes_f[g] = D.F.codes + f * D.F.stride;
-        scale_f[g] = D.F.scales + f;
-    }
-    f32x4 acc[GT] = {};
+    const int64_t f = min((int64_t)l16, D.F.rows - 1);
+    const uint8_t *codes_f = D.F.codes + f * D.F.stride, *scale_f = D.F.scales + f;
+    f32x4 acc = {};
     for (int64_t b0 = (int64_t)wave * kSlab; b0 < L.B; b0 += kWaves * kSlab) {
         i32x4 a[kSteps];
         uint32_t x[kSteps];
@@ -215,48 +208,30 @@ __global__ __launch_bounds__(kWaves * 64) void matmul_long_mx4_kernel(Mx4Layer L
 #pragma unroll
         for (int h = 0; h < kSteps; ++h) {
             const int64_t b = min(b0 + h * 4 + q16, (int64_t)L.B - 1);
-#pragma unroll
-            for (int g = 0; g < GT; ++g) {
-                const i32x4 v = *reinterpret_cast<const i32x4*>(codes_f[g] + b * 16);
-                const uint32_t y = scale_f[g][b * D.F.scales_stride];
-                acc[g] = ADJ ? multiply_byte<0>(a[h], x[h], v, y, acc[g]) : multiply_byte<0>(v, y, a[h], x[h], acc[g]);
-            }
+            const i32x4 v = *reinterpret_cast<const i32x4*>(codes_f + b * 16);
+            const uint32_t y = scale_f[b * D.F.scales_stride];
+            acc = ADJ ? multiply_byte<0>(a[h], x[h], v, y, acc) : multiply_byte<0>(v, y, a[h], x[h], acc);
         }
     }
-#pragma unroll
-    for (int g = 0; g < GT; ++g) sums[wave][g][lane] = acc[g];
+    sums[wave][lane] = acc;
     __syncthreads();
-    if (wave >= GT) return;
-    {
-        const int g = wave;
-        f32x4 sum = sums[0][g][lane];
-        for (int p = 1; p < kWaves; ++p) sum += sums[p][g][lane];
-        const int64_t s_end = min(s0 + R, D.S.rows);
-        const int64_t i = ADJ ? g * 16 + l16 : s0 + l16, j = ADJ ? s0 + q16 * 4 : g * 16 + q16 * 4;
-        const int64_t I = ADJ ? D.F.rows : s_end, J = ADJ ? s_end : D.F.rows;
-        if (i >= I || j >= J) return;
-        const bool bias_on_j = ADJ == (D.bias_on_s != 0);
-        float v[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            v[k] = activate_nan(L.act, sum[k] + (L.bias ? L.bias[bias_on_j ? min(j + k, J - 1) : i] : 0.f));
-        store_values(static_cast<Tout*>(L.out) + i * L.ldo + j, v, j, J, 0);
-    }
+    if (wave > 0) return;
+    for (int p = 1; p < kWaves; ++p) acc += sums[p][lane];
+    store_few<Tout, ADJ>(L, D, acc, s0, min(s0 + R, D.S.rows));
 }
 
-// LDS of a launch with G groups of 16 few rows.
-int64_t lds_of(int B, int64_t rows, int G) { return (int64_t)kWaves * G * 64 * 16 + Held{B}.bytes(rows); }
+int64_t lds_of(int B, int64_t rows) { return kSums + Held{B}.bytes(rows); }
 constexpr int64_t kMostLds = 160 * 1024;
 
-template <typename X, typename Tout, int GT>
+template <typename X, typename Tout>
 hipError_t run_few(const Mx4Layer& L, const FewSides& D, const Mx4Values& V, bool adj, hipStream_t s) {
     // few rows are spread over all units, and K is shared while there are fewer waves than units have room for
     int parts = 1, R = 16;
     while (R > 2 && ceil_div64(D.S.rows, R) < 256) R /= 2;
     while (parts < kWaves && parts * kSlab < L.B && ceil_div64(D.S.rows, R) * parts < 2048) parts *= 2;
     const int64_t groups = ceil_div64(ceil_div64(D.S.rows, R), kWaves / parts);
-    const auto kern = adj ? matmul_few_mx4_kernel<X, Tout, GT, true> : matmul_few_mx4_kernel<X, Tout, GT, false>;
-    const int64_t lds = lds_of(L.B, D.F.rows, GT);
+    const auto kern = adj ? matmul_few_mx4_kernel<X, Tout, true> : matmul_few_mx4_kernel<X, Tout, false>;
+    const int64_t lds = lds_of(L.B, D.F.rows);
     const hipError_t e = allow_dynamic_lds((const void*)kern, (size_t)lds);
     if (e != hipSuccess) return e;
     const int64_t resident = 256 * std::max<int64_t>(1, std::min<int64_t>(2, kMostLds / lds));
@@ -264,11 +239,11 @@ hipError_t run_few(const Mx4Layer& L, const FewSides& D, const Mx4Values& V, boo
     return hipGetLastError();
 }
 
-template <typename Tout, int GT>
+template <typename Tout>
 hipError_t run_long(const Mx4Layer& L, const FewSides& D, bool adj, hipStream_t s) {
     int R = 16;
     while (R > 2 && ceil_div64(D.S.rows, R) < 256) R /= 2;
-    const auto kern = adj ? matmul_long_mx4_kernel<Tout, GT, true> : matmul_long_mx4_kernel<Tout, GT, false>;
+    const auto kern = adj ? matmul_long_mx4_kernel<Tout, true> : matmul_long_mx4_kernel<Tout, false>;
     // a launch has fewer than 2^32 threads
     const int64_t rows = (int64_t)R << 22;
     for (int64_t at = 0; at < D.S.rows; at += rows) {
@@ -288,11 +263,7 @@ hipError_t run_long(const Mx4Layer& L, const FewSides& D, bool adj, hipStream_t 
 
 template <typename X>
 hipError_t run_types(const Mx4Layer& L, const FewSides& D, const Mx4Values& V, dss_dtype out_dtype, bool adj, hipStream_t s) {
-    if constexpr (sizeof(X) == 1) {
-        if (D.F.rows > 16)
-            return out_dtype == DSS_BF16 ? run_few<X, uint16_t, 2>(L, D, V, adj, s) : run_few<X, float, 2>(L, D, V, adj, s);
-    }
-    return out_dtype == DSS_BF16 ? run_few<X, uint16_t, 1>(L, D, V, adj, s) : run_few<X, float, 1>(L, D, V, adj, s);
+    return out_dtype == DSS_BF16 ? run_few<X, uint16_t>(L, D, V, adj, s) : run_few<X, float>(L, D, V, adj, s);
 }
 
 }  // namespace
@@ -302,11 +273,8 @@ hipError_t launch_few_mx4(const Mx4Layer& L, dss_dtype out_dtype, hipStream_t s)
     const FewSides D = tokens ? FewSides{L.weight, L.tokens, 1} : FewSides{L.tokens, L.weight, 0};
     const bool adj = tokens != (L.map != 0);
     // as many of the few rows at a time as LDS holds
-    const int64_t most = (kMostLds - kWaves * 2 * 64 * 16) / Held{L.B}.bytes(1);
-    if (most == 0) {
-        if (D.F.rows > 16) return out_dtype == DSS_BF16 ? run_long<uint16_t, 2>(L, D, adj, s) : run_long<float, 2>(L, D, adj, s);
-        return out_dtype == DSS_BF16 ? run_long<uint16_t, 1>(L, D, adj, s) : run_long<float, 1>(L, D, adj, s);
-    }
+    const int64_t most = (kMostLds - kSums) / Held{L.B}.bytes(1);
+    if (most == 0) return out_dtype == DSS_BF16 ? run_long<uint16_t>(L, D, adj, s) : run_long<float>(L, D, adj, s);
     for (int64_t f = 0; f < D.F.rows; f += most) {
         Mx4Layer P = L;
         FewSides E = D;

@@ -51,7 +51,7 @@ hipError_t launch_linear_mx4(const Mx4Layer& L, const Mx4Values& X, dss_dtype ou
 
 // The layer where one side has at most kFewRows rows (few_mx4.hip); and on so few tokens that the kernel codes them itself,
 // and whether it does.
-constexpr int kFewRows = 32;
+constexpr int kFewRows = 16;
 hipError_t launch_few_mx4(const Mx4Layer& L, dss_dtype out_dtype, hipStream_t s);
 bool few_codes_itself(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear_few_mx4(const Mx4Layer& L, const Mx4Values& X, dss_dtype out_dtype, hipStream_t s);
