@@ -2,6 +2,7 @@
 //   y[m][n] = act(sum_b X[b][m] W[b][n] sum_{k in b} q[m][k] v[n][k] + bias[n]),
 // on v_mfma_scale_f32_16x16x128_f8f6f4, whose binary32 sums take the blocks' scales with them.
 #include <algorithm>
+#include <type_traits>
 
 #include "dev_common.h"
 #include "dss_internal.h"
@@ -20,9 +21,7 @@ int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
 // weights, for dense maps the other way round.  In the matrix instruction Q's rows are the result's
 // rows, so that a lane holds four adjacent outputs.
 //
-// BI x BJ outputs for WI x WJ waves; kStep bytes of K (256 channels) at a time through two LDS buffers.  With KG > 1
-// so many groups of waves take the steps in turn, each with buffers of its own: where tiles are
-// fewer than units, a unit has more steps under way.
+// BI x BJ outputs for WI x WJ waves; kStep bytes of K (256 channels) at a time through two LDS buffers.
 //
 // A matrix operand is 16 rows.  Of P they are TI apart: row l of operand a is l TI + a, so that a lane's
 // scales for its TI operands are adjacent bytes and come with one load.  Of Q they are adjacent for binary32 outputs, where a
@@ -72,8 +71,40 @@ __host__ __device__ __forceinline__ Sides sides_of(const Mx4Layer& L) {
     return {L.tokens, L.weight};
 }
 
-template <typename Tout, int BI, int BJ, int WI, int WJ, int KG, bool MAP>
-__global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))) void matmul_mx4_kernel(Mx4Layer L, int tiles_i, int tiles_j) {
+// A lane's outputs of a tile: of rows i .. i+TI-1, C adjacent ones from j on, and every 4 C further.
+template <typename Tout, int TI, int TJ, bool MAP>
+__device__ __forceinline__ void store_tile(const Mx4Layer& L, const f32x4 (&acc)[TI][TJ], int64_t i_lane, int64_t I, int64_t j, int64_t J) {
+    constexpr int C = 16 / (int)sizeof(Tout);
+    constexpr int STORES = TJ * 4 / C;
+    float bias_j[STORES][C] = {};
+    if (!MAP && L.bias) {
+#pragma unroll
+        for (int c = 0; c < STORES; ++c)
+#pragma unroll
+            for (int k = 0; k < C; ++k) bias_j[c][k] = L.bias[min(j + c * 4 * C + k, J - 1)];
+    }
+    float bias_i[TI] = {};
+    if (MAP && L.bias) {
+#pragma unroll
+        for (int a = 0; a < TI; ++a) bias_i[a] = L.bias[min(i_lane + a, I - 1)];
+    }
+#pragma unroll
+    for (int a = 0; a < TI; ++a) {
+        const int64_t i = i_lane + a;
+#pragma unroll
+        for (int c = 0; c < STORES; ++c) {
+            if (i >= I || j + c * 4 * C >= J) continue;
+            float v[C];
+#pragma unroll
+            for (int k = 0; k < C; ++k)
+                v[k] = activate_nan(L.act, acc[a][c * (C / 4) + k / 4][k % 4] + (MAP ? bias_i[a] : bias_j[c][k]));
+            store_values(static_cast<Tout*>(L.out) + i * L.ldo + j + c * 4 * C, v, j + c * 4 * C, J, L.past);
+        }
+    }
+}
+
+template <typename Tout, int BI, int BJ, int WI, int WJ, bool MAP>
+__global__ __launch_bounds__(WI* WJ * 64) __attribute__((amdgpu_waves_per_eu(2))) void matmul_mx4_kernel(Mx4Layer L, int tiles_i, int tiles_j) {
     constexpr int NW = WI * WJ, THREADS = NW * 64;
     constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
     constexpr int C = 16 / (int)sizeof(Tout);            // outputs of a store, from C / 4 operands of Q
@@ -90,10 +121,8 @@ __global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu
     const int64_t strip = id / ((int64_t)8 * tiles_j), in_strip = id - strip * 8 * tiles_j;
     const int rows = min(8, tiles_i - (int)strip * 8);
     const int64_t i0 = (strip * 8 + in_strip % rows) * BI, j0 = in_strip / rows * BJ;
-    const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS), tid = threadIdx.x - group * THREADS;
-    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, q16 = lane >> 4;
-    char* const buffers = lds + group * 2 * BUF;
     const int wi = wave / WJ, wj = wave % WJ;
 
     // the thread's units: rows row0 + n * (THREADS / 8), and one place in each of them.  Their
@@ -107,15 +136,15 @@ __global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
     for (int n = 0; n < LQ; ++n) src_q[n] = (uint32_t)min((int64_t)row0 + n * (THREADS / 8), J - 1 - j0) * (uint32_t)S.Q.stride;
 
-    const int B = L.B, steps = (B + KG * kUnits - 1) / (KG * kUnits);
+    const int B = L.B, steps = (B + kUnits - 1) / kUnits;
     f32x4 acc[TI][TJ] = {};
 
     // Unit n of the thread's LP + LQ units of step s, into the step's buffer; past the end of K zeros.
     const uint8_t* zeros = reinterpret_cast<const uint8_t*>(g_zero16);
     auto fetch = [&](int s, int n) {
-        const int b = (s * KG + group) * kUnits + (n < LP ? unit_p : unit_q);
+        const int b = s * kUnits + (n < LP ? unit_p : unit_q);
         const uint8_t* row = n < LP ? base_p + src_p[n < LP ? n : 0] : base_q + src_q[n < LP ? 0 : n - LP];
-        copy16(b < B ? row + (int64_t)b * 16 : zeros, buffers + (s & 1) * BUF + (n * NW + wave) * 1024);
+        copy16(b < B ? row + (int64_t)b * 16 : zeros, lds + (s & 1) * BUF + (n * NW + wave) * 1024);
     };
     // A barrier that waits for the wave's own copies first: they count as loads, for which a barrier
     // alone does not wait.
@@ -138,7 +167,7 @@ __global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu
         uint32_t q[TJ];
     };
     auto scales = [&](Half& o, int s, int h) {
-        const int64_t b = min((s * KG + group) * kUnits + h * 4 + q16, B - 1);
+        const int64_t b = min(s * kUnits + h * 4 + q16, B - 1);
         o.p = load_scales<TI>(S.P.scales + b * S.P.scales_stride + i_at, shift_p);
         const uint8_t* q = S.Q.scales + b * S.Q.scales_stride;
 #pragma unroll
@@ -150,7 +179,7 @@ __global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu
     const int at_q = (BI + wj * TJ * 16 + (l16 >> 2) * C + (l16 & 3)) * kStep;
     auto read = [&](Half& o, int n, int s, int h) {
         const int at = n < TJ ? at_q + (n / (C / 4) * 4 * C + n % (C / 4) * 4) * kStep : at_p + (n - TJ) * kStep;
-        o.o[n] = *reinterpret_cast<const i32x4*>(buffers + (s & 1) * BUF + at + ((h * 4 + q16) ^ (l16 & 7)) * 16);
+        o.o[n] = *reinterpret_cast<const i32x4*>(lds + (s & 1) * BUF + at + ((h * 4 + q16) ^ (l16 & 7)) * 16);
     };
     // Multiplies one half's operands, reads another's (half h of step s) and fetches a step's
     // units, an LDS read and a fetch after every few matrix instructions.  In a burst the fetches would
@@ -191,69 +220,164 @@ __global__ __launch_bounds__(KG* WI* WJ * 64) __attribute__((amdgpu_waves_per_eu
         half_step(h1, h0, s + 1, 0, true);
     }
     arrived();                           // no copy may outlive the workgroup
-    if constexpr (KG > 1) {
-        // the groups' sums meet in the buffers, and are added in the groups' order
-        f32x4* sums = reinterpret_cast<f32x4*>(lds) + tid;
-#pragma unroll
-        for (int n = 0; n < TI * TJ; ++n)
-            if (group > 0) sums[((group - 1) * TI * TJ + n) * THREADS] = acc[n / TJ][n % TJ];
-        __syncthreads();
-        if (group > 0) return;
-#pragma unroll
-        for (int g = 0; g < KG - 1; ++g)
-#pragma unroll
-            for (int n = 0; n < TI * TJ; ++n) acc[n / TJ][n % TJ] += sums[(g * TI * TJ + n) * THREADS];
-    }
-    constexpr int STORES = TJ * 4 / C;
-    const int64_t j = j0 + wj * TJ * 16 + q16 * C;
-    float bias_j[STORES][C] = {};
-    if (!MAP && L.bias) {
-#pragma unroll
-        for (int c = 0; c < STORES; ++c)
-#pragma unroll
-            for (int k = 0; k < C; ++k) bias_j[c][k] = L.bias[min(j + c * 4 * C + k, J - 1)];
-    }
-    float bias_i[TI] = {};
-    if (MAP && L.bias) {
-#pragma unroll
-        for (int a = 0; a < TI; ++a) bias_i[a] = L.bias[min(i_lane + a, I - 1)];
-    }
-#pragma unroll
-    for (int a = 0; a < TI; ++a) {
-        const int64_t i = i_lane + a;
-#pragma unroll
-        for (int c = 0; c < STORES; ++c) {
-            if (i >= I || j + c * 4 * C >= J) continue;
-            float v[C];
-#pragma unroll
-            for (int k = 0; k < C; ++k)
-                v[k] = activate_nan(L.act, acc[a][c * (C / 4) + k / 4][k % 4] + (MAP ? bias_i[a] : bias_j[c][k]));
-            store_values(static_cast<Tout*>(L.out) + i * L.ldo + j + c * 4 * C, v, j + c * 4 * C, J, L.past);
-        }
-    }
+    store_tile<Tout, TI, TJ, MAP>(L, acc, i_lane, I, j0 + wj * TJ * 16 + q16 * C, J);
 }
 
-template <typename Tout, int BI, int BJ, int WI, int WJ, int KG>
+// ------------------------------------------------------------------ small tiles
+// Where a step's matrix instructions take less time than its bytes need to arrive: NB buffers, so that NB - 1 steps are
+// on their way, and all scales of the tile's rows in LDS beforehand (a load into registers between the copies would have
+// to wait for those before it).  (BI + BJ) B bytes of LDS for them.
+template <typename Tout, int BI, int BJ, int NB, bool MAP>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void matmul_mx4_deep_kernel(Mx4Layer L, int tiles_i, int tiles_j) {
+    constexpr int WI = 2, WJ = 2, NW = 4, THREADS = 256;
+    constexpr int TI = BI / WI / 16, TJ = BJ / WJ / 16;
+    constexpr int C = 16 / (int)sizeof(Tout);
+    constexpr int LP = BI * kUnits / THREADS, LQ = BJ * kUnits / THREADS;
+    constexpr int BUF = (BI + BJ) * kStep;
+    static_assert(32 % (8 * TI) == 0 && TJ % (C / 4) == 0, "the places of a thread's units, the operands of a store");
+    extern __shared__ __align__(16) char lds[];
+    const Sides S = sides_of(L);
+    const int64_t I = S.P.rows, J = S.Q.rows;
+    const int64_t id = xcd_order(blockIdx.x, (int64_t)tiles_i * tiles_j);
+    const int64_t strip = id / ((int64_t)8 * tiles_j), in_strip = id - strip * 8 * tiles_j;
+    const int strip_rows = min(8, tiles_i - (int)strip * 8);
+    const int64_t i0 = (strip * 8 + in_strip % strip_rows) * BI, j0 = in_strip / strip_rows * BJ;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, q16 = lane >> 4, wi = wave / WJ, wj = wave % WJ;
+    const int B = L.B, steps = (B + kUnits - 1) / kUnits;
+    uint8_t* const scales = reinterpret_cast<uint8_t*>(lds) + NB * BUF;      // [B][BI + BJ]
+
+    // Four adjacent rows' scales of a block at a time, U of them under way; past a side's end any.
+    constexpr int U = 8, FOURS = (BI + BJ) / 4;
+    auto load_four = [&](int n) {
+        const int b = min(n / FOURS, B - 1), r = n % FOURS * 4;
+        const bool p = r < BI;
+        const int64_t at = p ? i0 + r : j0 + r - BI, rows = p ? I : J;
+        const uint8_t* from = p ? S.P.scales + b * S.P.scales_stride : S.Q.scales + b * S.Q.scales_stride;
+        const int64_t start = min(at, rows - 4);         // (the rows before `at` are shifted out)
+        uint32_t w;
+        __builtin_memcpy(&w, from + start, 4);
+        return w >> 8 * (int)min(at - start, (int64_t)3);
+    };
+    auto put_fours = [&](int n0, const uint32_t (&w)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (n0 + u * THREADS < B * FOURS) reinterpret_cast<uint32_t*>(scales)[n0 + u * THREADS] = w[u];
+    };
+    uint32_t fours[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) fours[u] = load_four(tid + u * THREADS);
+
+    const int row0 = tid >> 3;
+    const int unit_p = (tid & 7) ^ (row0 / TI & 7), unit_q = (tid & 7) ^ ((row0 & 3) | (row0 / C & 1) << 2);
+    const uint8_t *const base_p = S.P.codes + i0 * S.P.stride, *const base_q = S.Q.codes + j0 * S.Q.stride;
+    uint32_t src_p[LP], src_q[LQ];
+#pragma unroll
+    for (int n = 0; n < LP; ++n) src_p[n] = (uint32_t)min((int64_t)row0 + n * 32, I - 1 - i0) * (uint32_t)S.P.stride;
+#pragma unroll
+    for (int n = 0; n < LQ; ++n) src_q[n] = (uint32_t)min((int64_t)row0 + n * 32, J - 1 - j0) * (uint32_t)S.Q.stride;
+    const uint8_t* zeros = reinterpret_cast<const uint8_t*>(g_zero16);
+    auto fetch = [&](int s, char* buffer) {
+#pragma unroll
+        for (int n = 0; n < LP + LQ; ++n) {
+            const int b = s * kUnits + (n < LP ? unit_p : unit_q);
+            const uint8_t* row = n < LP ? base_p + src_p[n < LP ? n : 0] : base_q + src_q[n < LP ? 0 : n - LP];
+            copy16(b < B ? row + (int64_t)b * 16 : zeros, buffer + (n * NW + wave) * 1024);
+        }
+    };
+    const int at_p = (wi * TI * 16 + l16 * TI) * kStep;
+    const int at_q = (BI + wj * TJ * 16 + (l16 >> 2) * C + (l16 & 3)) * kStep;
+    const uint8_t* const scales_p = scales + wi * TI * 16 + l16 * TI;
+    const uint8_t* const scales_q = scales + BI + wj * TJ * 16 + (l16 >> 2) * C;
+    const int shift_q = 8 * (l16 & 3);
+    // (words, not bytes: a byte might be one that a copy writes, and its read would wait for all of them)
+    using Word = std::conditional_t<TI == 2, uint16_t, uint32_t>;
+    static_assert(TI == (int)sizeof(Word));
+
+    f32x4 acc[TI][TJ] = {};
+    char* next = lds;                    // the buffer that the next fetch takes
+    auto turn = [&](char* b) { return b + BUF == lds + NB * BUF ? lds : b + BUF; };
+#pragma unroll
+    for (int s = 0; s < NB - 1; ++s) {
+        fetch(s, next);
+        next = turn(next);
+    }
+    put_fours(tid, fours);
+    for (int n0 = tid + U * THREADS; n0 < B * FOURS; n0 += U * THREADS) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) fours[u] = load_four(n0 + u * THREADS);
+        put_fours(n0, fours);
+    }
+    char* use = lds;
+    for (int s = 0; s < steps; ++s) {
+        // step s has arrived, for all waves, and nobody reads the buffer of step s - 1 any more
+        // (a barrier of the language would wait for all copies)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NB - 2) * (LP + LQ)) : "memory");
+        fetch(s + NB - 1, next);         // (past the last step zeros, which are not used)
+        next = turn(next);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            i32x4 p[TI], q[TJ];
+            const int unit = ((h * 4 + q16) ^ (l16 & 7)) * 16, b = min(s * kUnits + h * 4 + q16, B - 1);
+#pragma unroll
+            for (int n = 0; n < TJ; ++n) q[n] = *reinterpret_cast<const i32x4*>(use + at_q + (n / (C / 4) * 4 * C + n % (C / 4) * 4) * kStep + unit);
+#pragma unroll
+            for (int n = 0; n < TI; ++n) p[n] = *reinterpret_cast<const i32x4*>(use + at_p + n * kStep + unit);
+            const uint32_t x = *reinterpret_cast<const Word*>(scales_p + b * (BI + BJ));
+#pragma unroll
+            for (int n = 0; n < TJ; ++n) {
+                const uint32_t y = *reinterpret_cast<const uint32_t*>(scales_q + b * (BI + BJ) + n / (C / 4) * 4 * C + n % (C / 4) * 4) >> shift_q;
+#pragma unroll
+                for (int a = 0; a < TI; ++a) acc[a][n] = multiply_at(a, q[n], y, p[a], x, acc[a][n]);
+            }
+        }
+        use = turn(use);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // no copy may outlive the workgroup
+    store_tile<Tout, TI, TJ, MAP>(L, acc, i0 + wi * TI * 16 + l16 * TI, I, j0 + wj * TJ * 16 + q16 * C, J);
+}
+
+template <typename Tout, int BI, int BJ, int WI, int WJ>
 hipError_t run_tile(const Mx4Layer& L, hipStream_t s) {
     const Sides S = sides_of(L);
     const int64_t ti = ceil_div64(S.P.rows, BI), tj = ceil_div64(S.Q.rows, BJ);
-    const auto kern = L.map ? matmul_mx4_kernel<Tout, BI, BJ, WI, WJ, KG, true>
-                            : matmul_mx4_kernel<Tout, BI, BJ, WI, WJ, KG, false>;
-    constexpr size_t lds = KG * 2 * (BI + BJ) * kStep;
+    const auto kern = L.map ? matmul_mx4_kernel<Tout, BI, BJ, WI, WJ, true>
+                            : matmul_mx4_kernel<Tout, BI, BJ, WI, WJ, false>;
+    constexpr size_t lds = 2 * (BI + BJ) * kStep;
     const hipError_t e = allow_dynamic_lds((const void*)kern, lds);
     if (e != hipSuccess) return e;
-    kern<<<dim3((unsigned)(ti * tj)), KG * WI * WJ * 64, lds, s>>>(L, (int)ti, (int)tj);
+    kern<<<dim3((unsigned)(ti * tj)), WI * WJ * 64, lds, s>>>(L, (int)ti, (int)tj);
     return hipGetLastError();
 }
+
+size_t deep_lds(int BI, int BJ, int NB, int B) { return (size_t)(BI + BJ) * (NB * kStep + B); }
+
+template <typename Tout, int BI, int BJ, int NB>
+hipError_t run_deep(const Mx4Layer& L, hipStream_t s) {
+    const Sides S = sides_of(L);
+    const int64_t ti = ceil_div64(S.P.rows, BI), tj = ceil_div64(S.Q.rows, BJ);
+    const auto kern = L.map ? matmul_mx4_deep_kernel<Tout, BI, BJ, NB, true> : matmul_mx4_deep_kernel<Tout, BI, BJ, NB, false>;
+    const size_t lds = deep_lds(BI, BJ, NB, L.B);
+    const hipError_t e = allow_dynamic_lds((const void*)kern, lds);
+    if (e != hipSuccess) return e;
+    kern<<<dim3((unsigned)(ti * tj)), 256, lds, s>>>(L, (int)ti, (int)tj);
+    return hipGetLastError();
+}
+
+// Measured as kTiles are; steps of kStep bytes of K.  Microseconds on 256, 128 and 64: 8192 x 8192 x 8192 346, 465, 853;
+// 4096 x 4096 x 4096 47, 56, 83; 2048 x 4096 x 4096 39, 30, 45; 512 x 4096 x 4096 37, 24, 12.7; 1777 x 1003 x 2305 32, 19,
+// 11.2; 300 x 300 x 2304 23, 12, 7.0; 100000 x 512 x 256 44, 43, 54; 128 x 8192 x 9216 70, 46, 19.
+constexpr TileTime kMx4Tiles[] = {{256, 1, 1, 2.4, 0, 7.0}, {128, 1, 2, 1.2, 0.4, 4.5}, {64, 1, 3, 0.42, 0.13, 3.0}};
 
 template <typename Tout>
 hipError_t run_product(const Mx4Layer& L, hipStream_t s) {
     const Sides S = sides_of(L);
-    const int t = pick_tile(S.P.rows, S.Q.rows, L.B * 16);
-    if (t == 0) return run_tile<Tout, 256, 256, 2, 4, 1>(L, s);
-    if (t == 1) return run_tile<Tout, 128, 128, 2, 2, 1>(L, s);
-    if (t == 2) return run_tile<Tout, 64, 64, 2, 2, 1>(L, s);
-    return run_tile<Tout, 64, 64, 2, 2, 4>(L, s);
+    // (the small tiles hold their scales in LDS, of up to 28672 channels)
+    const bool small = deep_lds(64, 64, 3, L.B) <= 160 * 1024;
+    const int t = pick_tile(kMx4Tiles, small ? 3 : 2, S.P.rows, S.Q.rows, L.B * 16);
+    if (t == 0) return run_tile<Tout, 256, 256, 2, 4>(L, s);
+    if (t == 1) return run_tile<Tout, 128, 128, 2, 2>(L, s);
+    return run_deep<Tout, 64, 64, 3>(L, s);
 }
 
 // The largest row stride of a tile's operands: 256 rows of them stay in 32 bits.
@@ -264,7 +388,7 @@ hipError_t launch_matmul(const Mx4Layer& L, dss_dtype out_dtype, hipStream_t s) 
     const bool few = L.tokens.rows <= kFewRows || L.weight.rows <= kFewRows;
     if (few) return launch_few_mx4(L, out_dtype, s);
     // rows too long for the tiles are taken kFewRows at a time; a launch of tiles has fewer than 2^32
-    // threads: at most 2^21 tiles of 64 x 64 and 1024 threads
+    // threads: at most 2^21 tiles of 64 x 64
     const bool tiles = std::max(L.tokens.stride, L.weight.stride) <= kMostStride;
     const int64_t slab = tiles ? std::max<int64_t>(256, (((int64_t)1 << 27) / ceil_div64(L.weight.rows, 64)) / 256 * 256) : kFewRows;
     for (int64_t m = 0; m < L.tokens.rows; m += slab) {

@@ -1,4 +1,4 @@
-// Which tile a product of 8-bit codes runs on (matmul_tokens.hip).  Plain C++.
+// Which tile a product of codes runs on (matmul_tokens.hip, matmul_mx4.hip).  Plain C++.
 #pragma once
 
 #include <cstdint>
@@ -18,12 +18,12 @@ struct TileTime {
 constexpr TileTime kTiles[] = {{256, 1, 1, 1.95, 0, 6.0}, {128, 1, 2, 0.95, 0.20, 4.0}, {64, 1, 4, 0.40, 0.17, 2.5},
                                {64, 4, 1, 1.05, 0, 3.0}};
 
-// The index in kTiles for I x J outputs of K products each.
-inline int pick_tile(int64_t I, int64_t J, int K) {
+// The index in `tiles_of` for I x J outputs of K bytes of products each.
+inline int pick_tile(const TileTime* tiles_of, int n, int64_t I, int64_t J, int K) {
     int best = 0;
     double least = 0;
-    for (int t = 0; t < 4; ++t) {
-        const TileTime& c = kTiles[t];
+    for (int t = 0; t < n; ++t) {
+        const TileTime& c = tiles_of[t];
         const int steps = (K + c.groups * kStep - 1) / (c.groups * kStep);
         const int64_t tiles = ((I + c.b - 1) / c.b) * ((J + c.b - 1) / c.b), full = tiles / (256 * c.most);
         const int64_t left = (tiles - full * 256 * c.most + 255) / 256;
@@ -33,5 +33,8 @@ inline int pick_tile(int64_t I, int64_t J, int K) {
     }
     return best;
 }
+
+// The index in kTiles for I x J outputs of K products each.
+inline int pick_tile(int64_t I, int64_t J, int K) { return pick_tile(kTiles, 4, I, J, K); }
 
 }  // namespace dss
