@@ -598,7 +598,7 @@ typedef struct dss_top_logits {
 } dss_top_logits;
 
 /* Bytes of the workspace of dss_distill_tokens, for any call. */
-#define DSS_DISTILL_WORKSPACE_BYTES (1 << 20)
+#define DSS_DISTILL_WORKSPACE_BYTES (1 << 22)
 
 /* The loss of a network's logits z against a teacher's top logits t, and its gradient, for M positions
  * (window positions of a dense map, or rows) of C classes:

@@ -187,12 +187,15 @@ struct Lists {
 
     // (the teacher's logits stay in memory where there is no room for them)
     static __host__ __device__ bool holds_t(int k) { return k * N <= 8192; }
-    static __host__ __device__ size_t bytes(int k) { return (size_t)N * (8 + (holds_t(k) ? 3 : 2) * k) * 4; }
-    __device__ __forceinline__ int& id(int n) const { return reinterpret_cast<int*>(at)[kPlace0 + n]; }
-    __device__ __forceinline__ float& z(int n) const { return at[kPlace0 + k * N + n]; }
+    // (an odd number of places, so that positions start in different banks)
+    static __host__ __device__ int pitch(int k) { return k | 1; }
+    static __host__ __device__ size_t bytes(int k) { return (size_t)N * (8 + (holds_t(k) ? 3 : 2) * pitch(k)) * 4; }
+    // Place j of position n.
+    __device__ __forceinline__ int& id(int j, int n) const { return reinterpret_cast<int*>(at)[kPlace0 + n * pitch(k) + j]; }
+    __device__ __forceinline__ float& z(int j, int n) const { return at[kPlace0 + (N + n) * pitch(k) + j]; }
     __device__ __forceinline__ float t(const Distill& D, int64_t m0, int j, int n) const {
-        if (holds_t(k)) return at[kPlace0 + (2 * k + j) * N + n];
-        return id(j * N + n) >= 0 ? teacher_of(D, m0 + n, j) : -INFINITY;
+        if (holds_t(k)) return at[kPlace0 + (2 * N + n) * pitch(k) + j];
+        return id(j, n) >= 0 ? teacher_of(D, m0 + n, j) : -INFINITY;
     }
 
     // Place n / N of position n % N; the student's logits of classes c0 .. c1-1 alone.
@@ -205,43 +208,50 @@ struct Lists {
         return a;
     }
     __device__ __forceinline__ void put(int n, const Place& a) const {
-        id(n) = a.id;
-        z(n) = a.z;
-        if (holds_t(k)) at[kPlace0 + 2 * k * N + n] = a.id >= 0 ? a.t : -INFINITY;
+        id(n / N, n % N) = a.id;
+        z(n / N, n % N) = a.z;
+        if (holds_t(k)) at[kPlace0 + (2 * N + n % N) * pitch(k) + n / N] = a.id >= 0 ? a.t : -INFINITY;
     }
-    // Of position n, from its list alone: with p of the list, z' the largest of its student's logits and d_j = (t_j - t_max) / T
-    // - (z_j - z') / T, the sums of p_j d_j and of p_j.  Its loss is then sum p_j d_j - sum p_j ((z' - z_max) / T + log(sum_p / sum_r)).
-    __device__ __forceinline__ void sum_up(const Distill& D, int64_t m0, int n) const {
-        float t_max = -INFINITY, state = 0.f, sum_p = 0.f, ref = -3.4028235e38f, parts = 0.f, mass = 0.f;
-        if (m0 + n < D.M) {
-#pragma unroll 4
-            for (int j = 0; j < k; ++j) {
+    // Of each position, from its list alone, 16 lanes for one: with p of the list, z' the largest of its student's logits and
+    // d_j = (t_j - t_max) / T - (z_j - z') / T, the sums of p_j d_j and of p_j.  Its loss is then
+    // sum p_j d_j - sum p_j ((z' - z_max) / T + log(sum_p / sum_r)).
+    __device__ __forceinline__ void sum_up(const Distill& D, int64_t m0) const {
+        const int lane = threadIdx.x & 15;
+        for (int n = threadIdx.x >> 4; n < N; n += blockDim.x >> 4) {
+            float tops[2] = {-INFINITY, 0.f};              // t_max, the list's state
+            const bool there = m0 + n < D.M;
+            for (int j = lane; j < k && there; j += 16) {
                 const float a = t(D, m0, j, n);
-                t_max = fmaxf(t_max, a);
-                state = fmaxf(state, Place{id(j * N + n), a, 0.f}.state(D));
+                tops[0] = fmaxf(tops[0], a);
+                tops[1] = fmaxf(tops[1], Place{id(j, n), a, 0.f}.state(D));
             }
-#pragma unroll 4
-            for (int j = 0; j < k; ++j) {
+            over_lanes<Max, 16>(tops, nullptr);
+            const float t_max = tops[0];
+            float sum[1] = {0.f}, ref[1] = {-3.4028235e38f};
+            for (int j = lane; j < k && there; j += 16) {
                 const float p = weight_of(D, t(D, m0, j, n), t_max);
-                sum_p += p;
-                if (p > 0.f) ref = fmaxf(ref, z(j * N + n));
+                sum[0] += p;
+                if (p > 0.f) ref[0] = fmaxf(ref[0], z(j, n));
             }
-            if (state == 3.f) sum_p = quiet_nan();
-            const float per_p = 1.f / sum_p;
-#pragma unroll 4
-            for (int j = 0; j < k; ++j) {
+            over_lanes<Sum, 16>(sum, nullptr);
+            over_lanes<Max, 16>(ref, nullptr);
+            const float per_p = tops[1] == 3.f ? quiet_nan() : 1.f / sum[0];
+            float sums[2] = {0.f, 0.f};                    // of p d, of p
+            for (int j = lane; j < k && there; j += 16) {
                 const float a = t(D, m0, j, n), p = weight_of(D, a, t_max) * per_p;
-                parts += p <= 0.f ? 0.f : p * (((a - t_max) - (z(j * N + n) - ref)) * (D.to_log2 * kLn2));
-                mass += p;
+                sums[0] += p <= 0.f ? 0.f : p * (((a - t_max) - (z(j, n) - ref[0])) * (D.to_log2 * kLn2));
+                sums[1] += p;
             }
-            if (D.weights && D.weights[m0 + n] == 0.f) state = 0.f;
+            over_lanes<Sum, 16>(sums, nullptr);
+            if (lane != 0) continue;
+            at[kTMax + n] = t_max;
+            at[kPerP + n] = per_p;
+            at[kRef + n] = ref[0];
+            at[kParts + n] = sums[0];
+            at[kMass + n] = sums[1];
+            // 0: nothing is to be learnt
+            at[kState + n] = there && D.weights && D.weights[m0 + n] == 0.f ? 0.f : tops[1];
         }
-        at[kTMax + n] = t_max;
-        at[kPerP + n] = 1.f / sum_p;
-        at[kRef + n] = ref;
-        at[kParts + n] = parts;
-        at[kMass + n] = mass;
-        at[kState + n] = state;          // 0: nothing is to be learnt
     }
     // Of position n, from its list and its logits' largest and sum: whether there is anything to learn, and the gradient's factor.
     __device__ __forceinline__ float factor(const Distill& D, int64_t m, int n) const {
@@ -255,13 +265,13 @@ struct Lists {
     // The gradients of the listed classes c0 .. c1-1, after all others are written, of positions `first` on.
     __device__ __forceinline__ void listed(const Distill& D, int64_t m0, T* grad, int64_t c0, int64_t c1, int first = 0) const {
         for (int n = threadIdx.x; n < k * N; n += blockDim.x) {
-            const int own = n % N, c = id(n);
+            const int own = n % N, c = id(n / N, own);
             const int64_t m = m0 + own;
             if (own < first || m >= D.M || c < c0 || c >= c1 || at[kState + own] == 0.f) continue;
             float of_class = 0.f;        // (a class may be there more than once)
             for (int i = 0; i < k; ++i)
-                if (id(i * N + own) == c) of_class += weight_of(D, t(D, m0, i, own), at[kTMax + own]) * at[kPerP + own];
-            const float r = exp2_of((z(n) - at[kZMax + own]) * D.to_log2) * at[kPerSum + own];
+                if (id(i, own) == c) of_class += weight_of(D, t(D, m0, i, own), at[kTMax + own]) * at[kPerP + own];
+            const float r = exp2_of((z(n / N, own) - at[kZMax + own]) * D.to_log2) * at[kPerSum + own];
             store_elem(grad + m + c * D.gcs, factor(D, m, own) * (r - of_class));
         }
     }
@@ -284,7 +294,7 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(16 / W))) 
     // (the lists first: there are no registers for them beside the tile, but another workgroup's work)
     for (int n = threadIdx.x; n < places; n += blockDim.x) lists.put(n, lists.read(D, m0, z, n, 0, C));
     __syncthreads();
-    for (int n = threadIdx.x; n < N; n += blockDim.x) lists.sum_up(D, m0, n);
+    lists.sum_up(D, m0);
     __builtin_amdgcn_sched_barrier(0);
     Tile<T, W> tile;
     tile.load(z + m0 + l16 * V, D.cs, c0, C);
@@ -397,45 +407,89 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_parts_kernel(Distill
             if (m + v < D.M) parts[(m + v) * gridDim.y + blockIdx.y] = {all[v], sum[v]};
 }
 
-// Then the losses (workgroups 0 of a tile) and the gradient of their parts.
+// What the gradients of a slab's positions are made of, one array after the other.
+constexpr int64_t kSlabPositions = 32768;
+struct Stats {
+    float* at;
+    __device__ __forceinline__ float& z_max(int64_t m) const { return at[m]; }
+    __device__ __forceinline__ float& per_sum(int64_t m) const { return at[kSlabPositions + m]; }
+    __device__ __forceinline__ float& t_max(int64_t m) const { return at[2 * kSlabPositions + m]; }
+    __device__ __forceinline__ float& per_p(int64_t m) const { return at[3 * kSlabPositions + m]; }
+    __device__ __forceinline__ float& factor(int64_t m) const { return at[4 * kSlabPositions + m]; }
+    // 0: nothing is to be learnt, 1: every class is in the list once, 2: one is there more than once.
+    __device__ __forceinline__ float& kind(int64_t m) const { return at[5 * kSlabPositions + m]; }
+};
+constexpr int kStats = 6;
+
+// Then the parts are joined and the lists summed up, 16 lanes for a position: the losses, and the positions' stats.
+constexpr int kJoined = kPartThreads / 16;
+
 template <typename T>
-__global__ __launch_bounds__(kPartThreads) void distill_map_finish_kernel(Distill D, int64_t per_part, const Part* parts, int n_parts,
-                                                                          int with_loss) {
-    constexpr int V = Tile<T, 4>::V, N = Tile<T, 4>::kTokens;
+__global__ __launch_bounds__(kPartThreads) void distill_map_join_kernel(Distill D, const Part* parts, int n_parts, Stats stats) {
+    using List = Lists<T, kJoined>;
     extern __shared__ __align__(16) char lds[];
-    using List = Lists<T, N>;
     const List lists = {reinterpret_cast<float*>(lds), D.k};
+    const int64_t m0 = (int64_t)blockIdx.x * kJoined, m = m0 + (threadIdx.x >> 4);
+    const int lane = threadIdx.x & 15, n = threadIdx.x >> 4, k = D.k;
+    for (int i = threadIdx.x; i < k * kJoined; i += kPartThreads) lists.put(i, lists.read(D, m0, static_cast<const T*>(D.z), i, 0, D.C));
+    __syncthreads();
+    lists.sum_up(D, m0);
+    Part own = {-INFINITY, 0.f};
+    for (int p = lane; p < n_parts && m < D.M; p += 16) own = joined(D, own, parts[m * n_parts + p]);
+    float top[1] = {own.top};
+    over_lanes<Max, 16>(top, nullptr);
+    float sum[1] = {joined(D, {top[0], 0.f}, own).sum}, twice[1] = {0.f};
+    over_lanes<Sum, 16>(sum, nullptr);
+    for (int j = lane; j < k; j += 16) {
+        const int c = lists.id(j, n);
+        for (int i = 0; i < j && c >= 0; ++i) twice[0] = lists.id(i, n) == c ? 1.f : twice[0];
+    }
+    over_lanes<Max, 16>(twice, nullptr);
+    __syncthreads();
+    if (lane != 0 || m >= D.M) return;
+    // (a position of -infinities has the sum 0 here, and no softmax)
+    const float sum_r = top[0] == -INFINITY ? quiet_nan() : sum[0], state = lists.at[List::kState + n];
+    stats.z_max(m) = top[0];
+    stats.per_sum(m) = state == 3.f ? quiet_nan() : 1.f / sum_r;
+    stats.t_max(m) = lists.at[List::kTMax + n];
+    stats.per_p(m) = lists.at[List::kPerP + n];
+    stats.factor(m) = lists.factor(D, m, n);
+    stats.kind(m) = state == 0.f ? 0.f : 1.f + twice[0];
+    lists.put_loss(D, m0, n, top[0], sum_r);
+}
+
+// Then the gradient, a part of a tile's classes for a workgroup.  Where it is written over the logits, those of the
+// listed classes are put aside first (in LDS).
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void distill_map_gradient_kernel(Distill D, int64_t per_part, Stats stats) {
+    constexpr int V = Tile<T, 4>::V, N = Tile<T, 4>::kTokens;
+    extern __shared__ float kept[];
     const int64_t m0 = (int64_t)blockIdx.x * N, m = m0 + (threadIdx.x & 15) * V;
     const int64_t c_from = blockIdx.y * per_part, c1 = min(c_from + per_part, D.C);
-    const int l16 = threadIdx.x & 15;
-    const bool losses = with_loss && blockIdx.y == 0;
     const T* z = static_cast<const T*>(D.z);
-    // (the student's logits of other parts may be their gradients already, if these are written over them)
-    for (int n = threadIdx.x; n < D.k * N; n += kPartThreads)
-        lists.put(n, lists.read(D, m0, z, n, losses ? 0 : c_from, losses ? D.C : c1));
-    __syncthreads();
-    for (int n = threadIdx.x; n < N; n += kPartThreads) {
-        lists.sum_up(D, m0, n);
-        if (m0 + n >= D.M) continue;
-        Part all = {-INFINITY, 0.f};
-        for (int p = 0; p < n_parts; ++p) all = joined(D, all, parts[(m0 + n) * n_parts + p]);
-        // (a position of -infinities has the sum 0 here, and no softmax)
-        const float sum = all.top == -INFINITY ? quiet_nan() : all.sum;
-        lists.at[List::kZMax + n] = all.top;
-        lists.at[List::kPerSum + n] = lists.at[List::kState + n] == 3.f ? quiet_nan() : 1.f / sum;
-        if (losses) lists.put_loss(D, m0, n, all.top, sum);
-    }
-    if (!D.grad) return;
-    __syncthreads();
     T* grad = static_cast<T*>(D.grad);
+    const bool over = D.grad == D.z;
+    // f(place, position, class, n) of the listed classes of this part
+    auto over_listed = [&](auto f) {
+        for (int n = threadIdx.x; n < D.k * N; n += kPartThreads) {
+            const int64_t p = m0 + n % N;
+            if (p >= D.M) continue;
+            const int c = class_of(D, p, n / N);
+            if (c >= c_from && c < c1) f(n / N, p, c, n);
+        }
+    };
+    if (over) {
+        over_listed([&](int, int64_t p, int c, int n) { kept[n] = to_f32(z[p + c * D.cs]); });
+        __syncthreads();
+    }
     if (m < D.M) {
         float per[V], top[V];
         uint32_t live = 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int n = l16 * V + v;
-            live |= (m + v < D.M && lists.at[List::kState + n] != 0.f ? 1u : 0u) << v;
-            per[v] = lists.factor(D, m0 + n, n) * lists.at[List::kPerSum + n], top[v] = lists.at[List::kZMax + n];
+            const int64_t p = min(m + v, D.M - 1);
+            live |= (stats.kind(p) != 0.f ? 1u : 0u) << v;
+            per[v] = stats.factor(p) * stats.per_sum(p), top[v] = stats.z_max(p);
         }
         for (int64_t c0 = c_from + (threadIdx.x >> 4) * 16; c0 < c1; c0 += kPartSpan) {
             Tile<T, 4> tile;
@@ -451,8 +505,20 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_finish_kernel(Distil
             }
         }
     }
-    __syncthreads();                     // the classes of the lists are stored over
-    lists.listed(D, m0, grad, c_from, c1);
+    __syncthreads();                     // the classes of the list are stored over
+    over_listed([&](int j, int64_t p, int c, int n) {
+        const float kind = stats.kind(p);
+        if (kind == 0.f) return;
+        auto share = [&](int i) { return weight_of(D, teacher_of(D, p, i), stats.t_max(p)) * stats.per_p(p); };
+        float of_class = share(j);
+        if (kind == 2.f) {
+            of_class = 0.f;
+            for (int i = 0; i < D.k; ++i)
+                if (class_of(D, p, i) == c) of_class += share(i);
+        }
+        const float own = over ? kept[n] : to_f32(z[p + c * D.cs]);
+        store_elem(grad + p + c * D.gcs, stats.factor(p) * (exp2_of((own - stats.z_max(p)) * D.to_log2) * stats.per_sum(p) - of_class));
+    });
 }
 
 template <typename T>
@@ -489,29 +555,24 @@ hipError_t run_tiles(const Distill& D, dss_dtype dt, hipStream_t s) {
 template <typename T>
 hipError_t run_map_parts(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
     constexpr int N = Tile<T, 4>::kTokens;
-    const size_t lds = Lists<T, N>::bytes(D.k);
-    const hipError_t allowed = allow_dynamic_lds((const void*)distill_map_finish_kernel<T>, lds);
-    if (allowed != hipSuccess) return allowed;
-    constexpr int64_t slab = 65536;
-    for (int64_t m = 0; m < D.M; m += slab) {
-        const Distill S = positions(D, dt, m, std::min(D.M - m, slab));
+    const size_t kept = D.grad == D.z ? (size_t)D.k * N * 4 : 0, lists = Lists<T, kJoined>::bytes(D.k);
+    const Stats stats = {reinterpret_cast<float*>(parts)};
+    parts += kStats * kSlabPositions * 4 / (int)sizeof(Part);
+    constexpr int64_t room = kMostParts - kStats * kSlabPositions * 4 / (int)sizeof(Part);
+    for (int64_t m = 0; m < D.M; m += kSlabPositions) {
+        const Distill S = positions(D, dt, m, std::min(D.M - m, kSlabPositions));
         // enough workgroups for the units, of at least a span of classes each
         const int64_t tiles = ceil_div64(S.M, N);
-        const int64_t most = std::max<int64_t>(1, std::min({ceil_div64(1024, tiles), ceil_div64(D.C, kPartSpan), (int64_t)kMostParts / S.M}));
+        const int64_t most = std::max<int64_t>(1, std::min({ceil_div64(1024, tiles), ceil_div64(D.C, kPartSpan), room / S.M}));
         const int64_t per_part = ceil_div64(ceil_div64(D.C, most), kPartSpan) * kPartSpan, n = ceil_div64(D.C, per_part);
         const dim3 grid((unsigned)tiles, (unsigned)n);
         distill_map_parts_kernel<T><<<grid, kPartThreads, 0, s>>>(S, per_part, parts);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        const bool over = D.grad == D.z;     // the losses need all of the logits first
-        Distill L = S;
-        if (over) L.grad = nullptr;
-        if (over || !D.grad) {
-            distill_map_finish_kernel<T><<<dim3((unsigned)tiles, 1), kPartThreads, lds, s>>>(L, D.C, parts, (int)n, 1);
-            e = hipGetLastError();
-            if (e != hipSuccess) return e;
-        }
-        if (D.grad) distill_map_finish_kernel<T><<<grid, kPartThreads, lds, s>>>(S, per_part, parts, (int)n, !over);
+        distill_map_join_kernel<T><<<dim3((unsigned)ceil_div64(S.M, kJoined)), kPartThreads, lists, s>>>(S, parts, (int)n, stats);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (D.grad) distill_map_gradient_kernel<T><<<grid, kPartThreads, kept, s>>>(S, per_part, stats);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -78,7 +78,7 @@ class Tensor(ctypes.Structure):
 
 
 GRAD_NORM_WORKSPACE_BYTES = 8192
-DISTILL_WORKSPACE_BYTES = 1 << 20
+DISTILL_WORKSPACE_BYTES = 1 << 22
 
 EXPORTS = ("dss_chain_geometry", "dss_chain_layer_geometry", "dss_plan_create", "dss_plan_destroy",
            "dss_plan_geometry", "dss_plan_layer_geometry", "dss_eval_dense", "dss_eval_mixed", "dss_eval_slide",
