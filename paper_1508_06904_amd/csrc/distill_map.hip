@@ -3,6 +3,7 @@
 // Bound by memory as the rows: the logits are read and the gradient is written once where a tile's logits fit LDS or
 // registers (up to 1024 classes); of more classes they are read twice.
 #include <algorithm>
+#include <type_traits>
 
 #include "dev_common.h"
 #include "distill.h"
@@ -176,41 +177,39 @@ __device__ __forceinline__ void over_tile(float (&v)[V], float* room) {
         for (int j = 0; j < V; ++j) v[j] = Op::of(v[j], room[(w * 16 + (lane & 15)) * V + j]);
 }
 
-// The lists of a tile's N positions in LDS (adjacent there): classes, the teacher's logits (-infinity at empty places) and
-// the student's; and of each position what its loss and gradient are made of.
+// The lists of a tile's N positions in LDS: classes, the teacher's logits (-infinity at empty places; later their parts of
+// the gradient) and the student's; and of each position what its loss is made of.
 template <typename T, int N>
 struct Lists {
-    static constexpr int kTMax = 0, kPerP = N, kRef = 2 * N, kParts = 3 * N, kMass = 4 * N, kState = 5 * N, kZMax = 6 * N,
-                         kPerSum = 7 * N, kPlace0 = 8 * N;
+    static constexpr int kTMax = 0, kPerP = N, kRef = 2 * N, kParts = 3 * N, kMass = 4 * N, kState = 5 * N, kPlace0 = 6 * N;
     float* at;
     int k;
 
-    // (the teacher's logits stay in memory where there is no room for them)
-    static __host__ __device__ bool holds_t(int k) { return k * N <= 8192; }
     // (an odd number of places, so that positions start in different banks)
     static __host__ __device__ int pitch(int k) { return k | 1; }
-    static __host__ __device__ size_t bytes(int k) { return (size_t)N * (8 + (holds_t(k) ? 3 : 2) * pitch(k)) * 4; }
+    // Before the student's logits, and with them.
+    static __host__ __device__ size_t bytes_of_t(int k) { return (size_t)N * (6 + 2 * pitch(k)) * 4; }
+    static __host__ __device__ size_t bytes(int k) { return (size_t)N * (6 + 3 * pitch(k)) * 4; }
     // Place j of position n.
     __device__ __forceinline__ int& id(int j, int n) const { return reinterpret_cast<int*>(at)[kPlace0 + n * pitch(k) + j]; }
-    __device__ __forceinline__ float& z(int j, int n) const { return at[kPlace0 + (N + n) * pitch(k) + j]; }
-    __device__ __forceinline__ float t(const Distill& D, int64_t m0, int j, int n) const {
-        if (holds_t(k)) return at[kPlace0 + (2 * N + n) * pitch(k) + j];
-        return id(j, n) >= 0 ? teacher_of(D, m0 + n, j) : -INFINITY;
-    }
+    __device__ __forceinline__ float& t(int j, int n) const { return at[kPlace0 + (N + n) * pitch(k) + j]; }
+    __device__ __forceinline__ float& z(int j, int n) const { return at[kPlace0 + (2 * N + n) * pitch(k) + j]; }
 
-    // Place n / N of position n % N; the student's logits of classes c0 .. c1-1 alone.
-    __device__ __forceinline__ Place read(const Distill& D, int64_t m0, const T* logits, int n, int64_t c0, int64_t c1) const {
-        const int64_t m = min(m0 + n % N, D.M - 1);
-        Place a;
-        a.id = class_of(D, m, n / N);
-        a.t = holds_t(k) ? teacher_of(D, m, n / N) : 0.f;
-        a.z = a.id >= c0 && a.id < c1 ? to_f32(logits[m + a.id * D.cs]) : 0.f;
-        return a;
+    // f(place, position) of all places, a thread for each.
+    template <typename F>
+    __device__ __forceinline__ void over_places(F f) const {
+        for (int i = threadIdx.x; i < k * N; i += blockDim.x) f(i / N, i % N);
     }
-    __device__ __forceinline__ void put(int n, const Place& a) const {
-        id(n / N, n % N) = a.id;
-        z(n / N, n % N) = a.z;
-        if (holds_t(k)) at[kPlace0 + (2 * N + n % N) * pitch(k) + n / N] = a.id >= 0 ? a.t : -INFINITY;
+    __device__ __forceinline__ void read(const Distill& D, int64_t m0, const T* logits) const {
+#pragma unroll 4
+        for (int i = threadIdx.x; i < k * N; i += blockDim.x) {
+            const int64_t m = min(m0 + i % N, D.M - 1);
+            const int c = class_of(D, m, i / N);
+            const float a = teacher_of(D, m, i / N);
+            id(i / N, i % N) = c;
+            t(i / N, i % N) = c >= 0 ? a : -INFINITY;
+            if (logits) z(i / N, i % N) = c >= 0 && c < (int)D.C ? to_f32(logits[m + c * D.cs]) : 0.f;
+        }
     }
     // Of each position, from its list alone, 16 lanes for one: with p of the list, z' the largest of its student's logits and
     // d_j = (t_j - t_max) / T - (z_j - z') / T, the sums of p_j d_j and of p_j.  Its loss is then
@@ -221,7 +220,7 @@ struct Lists {
             float tops[2] = {-INFINITY, 0.f};              // t_max, the list's state
             const bool there = m0 + n < D.M;
             for (int j = lane; j < k && there; j += 16) {
-                const float a = t(D, m0, j, n);
+                const float a = t(j, n);
                 tops[0] = fmaxf(tops[0], a);
                 tops[1] = fmaxf(tops[1], Place{id(j, n), a, 0.f}.state(D));
             }
@@ -229,7 +228,7 @@ struct Lists {
             const float t_max = tops[0];
             float sum[1] = {0.f}, ref[1] = {-3.4028235e38f};
             for (int j = lane; j < k && there; j += 16) {
-                const float p = weight_of(D, t(D, m0, j, n), t_max);
+                const float p = weight_of(D, t(j, n), t_max);
                 sum[0] += p;
                 if (p > 0.f) ref[0] = fmaxf(ref[0], z(j, n));
             }
@@ -238,7 +237,7 @@ struct Lists {
             const float per_p = tops[1] == 3.f ? quiet_nan() : 1.f / sum[0];
             float sums[2] = {0.f, 0.f};                    // of p d, of p
             for (int j = lane; j < k && there; j += 16) {
-                const float a = t(D, m0, j, n), p = weight_of(D, a, t_max) * per_p;
+                const float a = t(j, n), p = weight_of(D, a, t_max) * per_p;
                 sums[0] += p <= 0.f ? 0.f : p * (((a - t_max) - (z(j, n) - ref[0])) * (D.to_log2 * kLn2));
                 sums[1] += p;
             }
@@ -262,20 +261,71 @@ struct Lists {
         const float away = (at[kRef + n] - top) * (D.to_log2 * kLn2) - logf(at[kPerP + n]) - logf(sum_r);
         D.losses[m0 + n] = state == 0.f ? 0.f : factor(D, m0 + n, n) * (D.T * (at[kParts + n] - at[kMass + n] * away));
     }
-    // The gradients of the listed classes c0 .. c1-1, after all others are written, of positions `first` on.
-    __device__ __forceinline__ void listed(const Distill& D, int64_t m0, T* grad, int64_t c0, int64_t c1, int first = 0) const {
-        for (int n = threadIdx.x; n < k * N; n += blockDim.x) {
-            const int own = n % N, c = id(n / N, own);
-            const int64_t m = m0 + own;
-            if (own < first || m >= D.M || c < c0 || c >= c1 || at[kState + own] == 0.f) continue;
-            float of_class = 0.f;        // (a class may be there more than once)
-            for (int i = 0; i < k; ++i)
-                if (id(i, own) == c) of_class += weight_of(D, t(D, m0, i, own), at[kTMax + own]) * at[kPerP + own];
-            const float r = exp2_of((z(n / N, own) - at[kZMax + own]) * D.to_log2) * at[kPerSum + own];
-            store_elem(grad + m + c * D.gcs, factor(D, m, own) * (r - of_class));
-        }
+    // Whether the class of place j is in position n's list at another place too.
+    __device__ __forceinline__ bool again(int j, int n) const {
+        const int c = id(j, n);
+        bool other = false;
+#pragma unroll 8
+        for (int i = 0; i < k; ++i) other |= id(i, n) == c && i != j;
+        return other && c >= 0;
+    }
+    // The teacher's logits become what they take off the gradient of their class, p_of(logit, position), and of a class that is
+    // there more than once (twice(place, position)) all of it at its first place, whose other places are emptied.
+    template <typename F, typename G>
+    __device__ __forceinline__ void share_out(F p_of, G twice) const {
+        over_places([&](int j, int n) { t(j, n) = p_of(t(j, n), n); });
+        __syncthreads();
+        uint64_t later = 0;              // a bit for each of the thread's places, of which there are at most 64
+        int turn = 0;
+        over_places([&](int j, int n) {
+            if (twice(j, n)) {
+                const int c = id(j, n);
+                float p = t(j, n);
+                bool first = true;
+                for (int i = 0; i < k && first; ++i) {
+                    if (i == j || id(i, n) != c) continue;
+                    if (i < j) first = false;
+                    else p += t(i, n);
+                }
+                if (first) t(j, n) = p;  // (nobody else reads a first place)
+                else later |= 1ull << turn;
+            }
+            ++turn;
+        });
+        __syncthreads();
+        turn = 0;
+        over_places([&](int j, int n) {
+            if (later >> turn++ & 1) id(j, n) = -1;
+        });
     }
 };
+
+// Which place of its position's list a class has (counted from 1; 0: none), a byte for each class of a tile and
+// position.  Gradients are then written once: stored over, a listed class's line would come back from memory and go there again.
+template <int N>
+struct Marks {
+    uint8_t* at;
+
+    static __host__ __device__ int bytes(int classes) { return (classes + 15) / 16 * 16 * N; }
+    // (16 classes are a lane's: the same one of its neighbours' lies in other banks)
+    __device__ __forceinline__ uint8_t* of(int c, int n) const { return at + (c ^ ((c >> 4) & 3)) * N + n; }
+    __device__ __forceinline__ void clear(int classes) const {
+        for (int i = threadIdx.x; i < bytes(classes) / 4; i += blockDim.x) reinterpret_cast<uint32_t*>(at)[i] = 0;
+    }
+};
+
+// Takes off V adjacent positions' gradients of a class what its places take.
+template <typename List, int N, int V>
+__device__ __forceinline__ void take_off(float (&v)[V], const List& lists, const Marks<N>& marks, int c, int n) {
+    using Word = std::conditional_t<V == 2, uint16_t, uint32_t>;
+    const uint32_t places = *reinterpret_cast<const Word*>(marks.of(c, n));
+    if (places == 0) return;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int place = places >> (8 * j) & 255;
+        if (place) v[j] -= lists.t(place - 1, n + j);
+    }
+}
 
 // Up to 1024 classes: the tile's logits stay in registers.  Whole tiles only: the last one ends with the last
 // position and writes those from `first` on, which the one before it does not have.  (What it reads of the others
@@ -286,15 +336,28 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(16 / W))) 
     using List = Lists<T, N>;
     extern __shared__ __align__(16) char lds[];
     const List lists = {reinterpret_cast<float*>(lds), D.k};
-    float* room = reinterpret_cast<float*>(lds + List::bytes(D.k));
     const int64_t tile0 = xcd_order(blockIdx.x, gridDim.x) * N, m0 = min(tile0, D.M - N);
-    const int first = (int)(tile0 - m0), l16 = threadIdx.x & 15, C = (int)D.C, places = D.k * N;
+    const int first = (int)(tile0 - m0), l16 = threadIdx.x & 15, C = (int)D.C;
+    float* const room = reinterpret_cast<float*>(lds + List::bytes_of_t(D.k));
+    // (the marks take the place of the student's logits)
+    const Marks<N> marks = {reinterpret_cast<uint8_t*>(room + (blockDim.x >> 6) * N)};
     const T* z = static_cast<const T*>(D.z);
     int c0 = (threadIdx.x >> 4) * 16;
     // (the lists first: there are no registers for them beside the tile, but another workgroup's work)
-    for (int n = threadIdx.x; n < places; n += blockDim.x) lists.put(n, lists.read(D, m0, z, n, 0, C));
+    lists.read(D, m0, z);
     __syncthreads();
     lists.sum_up(D, m0);
+    __syncthreads();
+    if (D.grad) {
+        marks.clear(C);
+        lists.share_out([&](float t, int n) {
+            return lists.factor(D, m0 + n, n) * (weight_of(D, t, lists.at[List::kTMax + n]) * lists.at[List::kPerP + n]);
+        }, [&](int j, int n) { return lists.again(j, n); });
+        lists.over_places([&](int j, int n) {
+            const int c = lists.id(j, n);
+            if (c >= 0 && c < C && lists.at[List::kState + n] != 0.f) *marks.of(c, n) = (uint8_t)(j + 1);
+        });
+    }
     __builtin_amdgcn_sched_barrier(0);
     Tile<T, W> tile;
     tile.load(z + m0 + l16 * V, D.cs, c0, C);
@@ -327,11 +390,7 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(16 / W))) 
         const float per_sum = state == 3.f ? quiet_nan() : 1.f / sum[v];
         live |= (state != 0.f ? 1u : 0u) << v;
         per[v] = lists.factor(D, m0 + n, n) * per_sum;
-        if (threadIdx.x < 16) {
-            lists.at[List::kZMax + n] = top[v];
-            lists.at[List::kPerSum + n] = per_sum;
-            if (n >= first) lists.put_loss(D, m0, n, top[v], sum[v]);
-        }
+        if (threadIdx.x < 16 && n >= first) lists.put_loss(D, m0, n, top[v], sum[v]);
     }
     if (!D.grad) return;
     T* grad = static_cast<T*>(D.grad);
@@ -346,6 +405,7 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(16 / W))) 
                 v[j] = sizeof(T) == 4 ? tile.c[r].value(j) : exp2_of((tile.c[r].value(j) - top[j]) * D.to_log2);
                 v[j] = live >> j & 1 ? v[j] * per[j] : 0.f;
             }
+            take_off(v, lists, marks, c0 + r, l16 * V);
             if (l16 * V >= first) {
                 store_gradients(p, v, V);
             } else {
@@ -357,8 +417,6 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(16 / W))) 
         p += D.gcs;
         asm volatile("" : "+v"(p));      // (one address at a time: there are no registers for 16)
     }
-    __syncthreads();                     // the classes of the lists are stored over
-    lists.listed(D, m0, grad, 0, D.C, first);
 }
 
 // More classes, or too few positions for the units: `parts` workgroups share a tile's classes.  First each takes its
@@ -430,20 +488,19 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_join_kernel(Distill 
     extern __shared__ __align__(16) char lds[];
     const List lists = {reinterpret_cast<float*>(lds), D.k};
     const int64_t m0 = (int64_t)blockIdx.x * kJoined, m = m0 + (threadIdx.x >> 4);
-    const int lane = threadIdx.x & 15, n = threadIdx.x >> 4, k = D.k;
-    for (int i = threadIdx.x; i < k * kJoined; i += kPartThreads) lists.put(i, lists.read(D, m0, static_cast<const T*>(D.z), i, 0, D.C));
+    const int lane = threadIdx.x & 15, n = threadIdx.x >> 4;
+    lists.read(D, m0, static_cast<const T*>(D.z));
     __syncthreads();
     lists.sum_up(D, m0);
     Part own = {-INFINITY, 0.f};
-    for (int p = lane; p < n_parts && m < D.M; p += 16) own = joined(D, own, parts[m * n_parts + p]);
+#pragma unroll 8
+    for (int p = lane; p < n_parts; p += 16) own = joined(D, own, parts[min(m, D.M - 1) * n_parts + p]);
     float top[1] = {own.top};
     over_lanes<Max, 16>(top, nullptr);
     float sum[1] = {joined(D, {top[0], 0.f}, own).sum}, twice[1] = {0.f};
     over_lanes<Sum, 16>(sum, nullptr);
-    for (int j = lane; j < k; j += 16) {
-        const int c = lists.id(j, n);
-        for (int i = 0; i < j && c >= 0; ++i) twice[0] = lists.id(i, n) == c ? 1.f : twice[0];
-    }
+    for (int j = lane; j < D.k; j += 16)
+        if (lists.again(j, n)) twice[0] = 1.f;
     over_lanes<Max, 16>(twice, nullptr);
     __syncthreads();
     if (lane != 0 || m >= D.M) return;
@@ -458,67 +515,61 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_join_kernel(Distill 
     lists.put_loss(D, m0, n, top[0], sum_r);
 }
 
-// Then the gradient, a part of a tile's classes for a workgroup.  Where it is written over the logits, those of the
-// listed classes are put aside first (in LDS).
+// Then the gradient, a part of a tile's classes for a workgroup, a span of them at a time.
 template <typename T>
 __global__ __launch_bounds__(kPartThreads) void distill_map_gradient_kernel(Distill D, int64_t per_part, Stats stats) {
-    constexpr int V = Tile<T, 4>::V, N = Tile<T, 4>::kTokens;
-    extern __shared__ float kept[];
+    constexpr int W = (int)sizeof(T), V = Tile<T, W>::V, N = Tile<T, W>::kTokens;
+    using List = Lists<T, N>;
+    extern __shared__ __align__(16) char lds[];
+    const List lists = {reinterpret_cast<float*>(lds), D.k};
+    const Marks<N> marks = {reinterpret_cast<uint8_t*>(lds + List::bytes_of_t(D.k))};
     const int64_t m0 = (int64_t)blockIdx.x * N, m = m0 + (threadIdx.x & 15) * V;
     const int64_t c_from = blockIdx.y * per_part, c1 = min(c_from + per_part, D.C);
     const T* z = static_cast<const T*>(D.z);
     T* grad = static_cast<T*>(D.grad);
-    const bool over = D.grad == D.z;
-    // f(place, position, class, n) of the listed classes of this part
-    auto over_listed = [&](auto f) {
-        for (int n = threadIdx.x; n < D.k * N; n += kPartThreads) {
-            const int64_t p = m0 + n % N;
-            if (p >= D.M) continue;
-            const int c = class_of(D, p, n / N);
-            if (c >= c_from && c < c1) f(n / N, p, c, n);
-        }
+    lists.read(D, m0, nullptr);
+    marks.clear(kPartSpan);
+    __syncthreads();
+    lists.share_out([&](float t, int n) {
+        const int64_t p = min(m0 + n, D.M - 1);
+        return stats.factor(p) * (weight_of(D, t, stats.t_max(p)) * stats.per_p(p));
+    }, [&](int, int n) { return stats.kind(min(m0 + n, D.M - 1)) == 2.f; });
+    // the marks of the span's listed classes, or none again
+    auto mark = [&](int64_t c0, bool set) {
+        lists.over_places([&](int j, int n) {
+            const int64_t c = lists.id(j, n);
+            if (c >= c0 && c < min(c0 + kPartSpan, D.C)) *marks.of((int)(c - c0), n) = (uint8_t)(set ? j + 1 : 0);
+        });
     };
-    if (over) {
-        over_listed([&](int, int64_t p, int c, int n) { kept[n] = to_f32(z[p + c * D.cs]); });
+    float per[V], top[V];
+    uint32_t live = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int64_t p = min(m + v, D.M - 1);
+        live |= (stats.kind(p) != 0.f ? 1u : 0u) << v;
+        per[v] = stats.factor(p) * stats.per_sum(p), top[v] = stats.z_max(p);
+    }
+    const int own = (threadIdx.x >> 4) * 16;
+    for (int64_t span = c_from; span < c1; span += kPartSpan) {
+        const int64_t c0 = span + own;
+        Tile<T, W> tile;
+        tile.load(z + m, D.cs, c0, c1, D.M - m);
+        mark(span, true);
         __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            if (c0 + r >= c1 || m >= D.M) continue;
+            float v[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = exp2_of((tile.c[r].value(j) - top[j]) * D.to_log2) * per[j];
+            take_off(v, lists, marks, own + r, (threadIdx.x & 15) * V);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = live >> j & 1 ? v[j] : 0.f;
+            store_gradients(grad + m + (c0 + r) * D.gcs, v, D.M - m);
+        }
+        __syncthreads();
+        mark(span, false);
     }
-    if (m < D.M) {
-        float per[V], top[V];
-        uint32_t live = 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int64_t p = min(m + v, D.M - 1);
-            live |= (stats.kind(p) != 0.f ? 1u : 0u) << v;
-            per[v] = stats.factor(p) * stats.per_sum(p), top[v] = stats.z_max(p);
-        }
-        for (int64_t c0 = c_from + (threadIdx.x >> 4) * 16; c0 < c1; c0 += kPartSpan) {
-            Tile<T, 4> tile;
-            tile.load(z + m, D.cs, c0, c1, D.M - m);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                if (c0 + r >= c1) continue;
-                float v[V];
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    v[j] = live >> j & 1 ? exp2_of((tile.c[r].value(j) - top[j]) * D.to_log2) * per[j] : 0.f;
-                store_gradients(grad + m + (c0 + r) * D.gcs, v, D.M - m);
-            }
-        }
-    }
-    __syncthreads();                     // the classes of the list are stored over
-    over_listed([&](int j, int64_t p, int c, int n) {
-        const float kind = stats.kind(p);
-        if (kind == 0.f) return;
-        auto share = [&](int i) { return weight_of(D, teacher_of(D, p, i), stats.t_max(p)) * stats.per_p(p); };
-        float of_class = share(j);
-        if (kind == 2.f) {
-            of_class = 0.f;
-            for (int i = 0; i < D.k; ++i)
-                if (class_of(D, p, i) == c) of_class += share(i);
-        }
-        const float own = over ? kept[n] : to_f32(z[p + c * D.cs]);
-        store_elem(grad + p + c * D.gcs, stats.factor(p) * (exp2_of((own - stats.z_max(p)) * D.to_log2) * stats.per_sum(p) - of_class));
-    });
 }
 
 template <typename T>
@@ -537,7 +588,7 @@ template <typename T, int W>
 hipError_t run_tiles(const Distill& D, dss_dtype dt, hipStream_t s) {
     constexpr int N = Tile<T, W>::kTokens;
     const int waves = (int)ceil_div64(D.C, 64);
-    const size_t lds = Lists<T, N>::bytes(D.k) + (size_t)waves * N * 4;
+    const size_t lds = std::max(Lists<T, N>::bytes_of_t(D.k) + (size_t)waves * N * 4 + Marks<N>::bytes((int)D.C), Lists<T, N>::bytes(D.k));
     const hipError_t e = allow_dynamic_lds((const void*)distill_tile_kernel<T, W>, lds);
     if (e != hipSuccess) return e;
     for (int64_t m = 0; m < D.M;) {
@@ -554,8 +605,11 @@ hipError_t run_tiles(const Distill& D, dss_dtype dt, hipStream_t s) {
 
 template <typename T>
 hipError_t run_map_parts(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
-    constexpr int N = Tile<T, 4>::kTokens;
-    const size_t kept = D.grad == D.z ? (size_t)D.k * N * 4 : 0, lists = Lists<T, kJoined>::bytes(D.k);
+    // (the parts' tiles and the gradients', which are half as wide of bfloat16)
+    constexpr int N = Tile<T, 4>::kTokens, G = Tile<T, (int)sizeof(T)>::kTokens;
+    const size_t lists = Lists<T, kJoined>::bytes(D.k), gradient = Lists<T, G>::bytes_of_t(D.k) + Marks<G>::bytes(kPartSpan);
+    const hipError_t allowed = allow_dynamic_lds((const void*)distill_map_gradient_kernel<T>, gradient);
+    if (allowed != hipSuccess) return allowed;
     const Stats stats = {reinterpret_cast<float*>(parts)};
     parts += kStats * kSlabPositions * 4 / (int)sizeof(Part);
     constexpr int64_t room = kMostParts - kStats * kSlabPositions * 4 / (int)sizeof(Part);
@@ -572,7 +626,8 @@ hipError_t run_map_parts(const Distill& D, dss_dtype dt, Part* parts, hipStream_
         distill_map_join_kernel<T><<<dim3((unsigned)ceil_div64(S.M, kJoined)), kPartThreads, lists, s>>>(S, parts, (int)n, stats);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
-        if (D.grad) distill_map_gradient_kernel<T><<<grid, kPartThreads, kept, s>>>(S, per_part, stats);
+        if (D.grad)
+            distill_map_gradient_kernel<T><<<dim3((unsigned)ceil_div64(S.M, G), (unsigned)n), kPartThreads, gradient, s>>>(S, per_part, stats);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -582,7 +637,7 @@ hipError_t run_map_parts(const Distill& D, dss_dtype dt, Part* parts, hipStream_
 template <typename T>
 hipError_t run_map(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
     if (D.C <= kColumns) return run_columns<T>(D, dt, s);
-    // (lists of up to 128 places: 128 KB for 128 positions)
+    // (lists of up to 128 places: 64 positions' take 98 KB)
     if (D.k > 128) return launch_distill_any(D, dt, s);
     return D.C <= 1024 && D.M >= Tile<T, 2>::kTokens ? run_tiles<T, 2>(D, dt, s) : run_map_parts<T>(D, dt, parts, s);
 }
