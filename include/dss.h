@@ -597,8 +597,13 @@ typedef struct dss_top_logits {
     int32_t reserved;
 } dss_top_logits;
 
-/* Bytes of the workspace of dss_distill_tokens, for any call. */
+/* The most that dss_distill_workspace gives. */
 #define DSS_DISTILL_WORKSPACE_BYTES (1 << 22)
+
+/* Workspace bytes of dss_distill_tokens on positions of C classes (host only): `map` is nonzero where the
+ * positions are adjacent (a channel stride other than 1).  0 for rows of fewer than 16384 classes and maps of at
+ * most 128.  Errors: DSS_E_INVALID (C < 1, NULL workspace_bytes). */
+dss_status dss_distill_workspace(int32_t C, int32_t map, int64_t* workspace_bytes);
 
 /* The loss of a network's logits z against a teacher's top logits t, and its gradient, for M positions
  * (window positions of a dense map, or rows) of C classes:
@@ -617,7 +622,7 @@ typedef struct dss_top_logits {
  *   grad           device, the logits' type, in the logits' orientation with strides of its own (the one
  *                  that is not 1 at least the length it steps over), or NULL for the losses alone.
  *                  The logits themselves, with their strides, may be the gradient; no other overlap is allowed
- *   workspace      device scratch of DSS_DISTILL_WORKSPACE_BYTES (256-byte aligned)
+ *   workspace      device scratch of dss_distill_workspace bytes (256-byte aligned); may be NULL where these are 0
  * A position of weight 0, or without a place whose logit is above -infinity, has loss 0 and gradient 0,
  * whatever its logits.  At any other one infinities and NaN follow the formulas (a
  * place of logit -infinity adds 0), and a class of C or more makes loss and gradient NaN.

@@ -42,6 +42,7 @@ Distill positions(const Distill& D, dss_dtype dt, int64_t m, int64_t n);
 
 // Logits whose positions are adjacent.  `parts` has room for kMostParts.
 constexpr int kMostParts = DSS_DISTILL_WORKSPACE_BYTES / (int)sizeof(Part);
+constexpr int kColumns = 128;            // classes of a map that need no parts
 hipError_t launch_distill_map(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s);
 
 // A workgroup for each position, any strides: maps of few positions or with long lists.

@@ -194,6 +194,8 @@ __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_
     }
 }
 
+constexpr int kSharedClasses = 16384;    // of the shortest rows that several workgroups share
+
 // Rows longer than the registers hold, or too few for the units: `parts` workgroups share a position's classes.  First
 // each takes its part's largest logit and sum.
 template <typename T>
@@ -328,8 +330,9 @@ hipError_t run_parts(const Distill& D, Part* parts, hipStream_t s) {
 template <typename T>
 hipError_t run_distill(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
     constexpr int E = Logits<T>::E;
+    // (a call without workspace comes to neither: rows of fewer than kSharedClasses)
     const bool long_rows = D.C > 1024 * 16 * E || (!D.grad && D.C > 256 * 16 * E);
-    if (long_rows || (D.M < 128 && D.C >= 16384)) {
+    if (long_rows || (D.M < 128 && D.C >= kSharedClasses)) {
         // (a launch has 65535 workgroups along y)
         const int64_t slab = 4096;
         for (int64_t m = 0; m < D.M; m += slab) {
@@ -390,6 +393,22 @@ Distill positions(const Distill& D, dss_dtype dt, int64_t m, int64_t n) {
 
 }  // namespace dss
 
+namespace dss {
+static int64_t distill_workspace(int32_t C, bool map) {
+    return C >= (map ? kColumns + 1 : kSharedClasses) ? DSS_DISTILL_WORKSPACE_BYTES : 0;
+}
+}  // namespace dss
+
+extern "C" dss_status dss_distill_workspace(int32_t C, int32_t map, int64_t* workspace_bytes) try {
+    using namespace dss;
+    if (!workspace_bytes) return fail(DSS_E_INVALID, "NULL output");
+    if (C < 1) return fail(DSS_E_INVALID, "%d classes", C);
+    *workspace_bytes = distill_workspace(C, map != 0);
+    return DSS_OK;
+} catch (...) {
+    return DSS_E_NOMEM;
+}
+
 extern "C" dss_status dss_distill_tokens(const void* logits, dss_dtype dtype, int64_t M, int32_t C, int64_t token_stride,
                                          int64_t channel_stride, const dss_top_logits* top, const float* token_weights,
                                          float temperature, float scale, float* losses, void* grad,
@@ -428,7 +447,7 @@ extern "C" dss_status dss_distill_tokens(const void* logits, dss_dtype dtype, in
         return fail(DSS_E_INVALID, "the teacher's logits or classes are NULL or not aligned to their elements");
     if (!losses || (uintptr_t)losses % 4 != 0 || (uintptr_t)token_weights % 4 != 0)
         return fail(DSS_E_INVALID, "losses is NULL, or the losses or the weights are not aligned");
-    s = check_room(DSS_DISTILL_WORKSPACE_BYTES, workspace, workspace_bytes);
+    s = check_room(distill_workspace(C, map), workspace, workspace_bytes);
     if (s != DSS_OK) return s;
     const Distill D = {logits, M, C, token_stride, channel_stride, top->logits, top->dtype == DSS_BF16, top->token_stride,
                        top->place_stride, top->ids, top->id_bytes == 8, top->id_token_stride, top->id_place_stride,

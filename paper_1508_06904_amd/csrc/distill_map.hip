@@ -17,8 +17,6 @@ namespace {
 // A lane for each position, its logits in a column of LDS that no other lane touches: lists are gathered and gradients
 // of listed classes put together there, with no barrier.  Of a class that is in the list (its bit in `listed`) the column has the
 // gradient in the end, of any other one the logit.
-constexpr int kColumns = 128;            // classes at most
-
 // kPlaces places of a list, loaded together: what a pass over a list costs is its loads' latency.  Lists of no more stay
 // in registers.
 constexpr int kPlaces = 8;
@@ -208,7 +206,7 @@ struct Lists {
             const float a = teacher_of(D, m, i / N);
             id(i / N, i % N) = c;
             t(i / N, i % N) = c >= 0 ? a : -INFINITY;
-            if (logits) z(i / N, i % N) = c >= 0 && c < (int)D.C ? to_f32(logits[m + c * D.cs]) : 0.f;
+            z(i / N, i % N) = c >= 0 && c < (int)D.C ? to_f32(logits[m + c * D.cs]) : 0.f;
         }
     }
     // Of each position, from its list alone, 16 lanes for one: with p of the list, z' the largest of its student's logits and
@@ -527,20 +525,47 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_gradient_kernel(Dist
     const int64_t c_from = blockIdx.y * per_part, c1 = min(c_from + per_part, D.C);
     const T* z = static_cast<const T*>(D.z);
     T* grad = static_cast<T*>(D.grad);
-    lists.read(D, m0, nullptr);
     marks.clear(kPartSpan);
-    __syncthreads();
-    lists.share_out([&](float t, int n) {
-        const int64_t p = min(m0 + n, D.M - 1);
-        return stats.factor(p) * (weight_of(D, t, stats.t_max(p)) * stats.per_p(p));
-    }, [&](int, int n) { return stats.kind(min(m0 + n, D.M - 1)) == 2.f; });
+    // The part's listed classes, and what their places take off: of the thread's places a bit for each that there is.
+    constexpr int U = 8;                 // classes under way
+    uint64_t mine = 0;
+    for (int turn = 0; turn * kPartThreads < D.k * N; turn += U) {
+        int c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = (turn + u) * kPartThreads + threadIdx.x;
+            c[u] = class_of(D, min(m0 + i % N, D.M - 1), min(i / N, D.k - 1));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = (turn + u) * kPartThreads + threadIdx.x, j = i / N, n = i % N;
+            if (i >= D.k * N || m0 + n >= D.M || c[u] < c_from || c[u] >= c1) continue;
+            const int64_t p = m0 + n;
+            const float kind = stats.kind(p);
+            auto share = [&](int place) { return weight_of(D, teacher_of(D, p, place), stats.t_max(p)) * stats.per_p(p); };
+            float of_class = share(j);
+            bool first = kind != 0.f;
+            if (kind == 2.f)             // (a class that is there more than once: all of it at its first place)
+                for (int o = 0; o < D.k && first; ++o) {
+                    if (o == j || class_of(D, p, o) != c[u]) continue;
+                    if (o < j) first = false;
+                    else of_class += share(o);
+                }
+            if (!first) continue;
+            lists.id(j, n) = c[u];
+            lists.t(j, n) = stats.factor(p) * of_class;
+            mine |= 1ull << (turn + u);
+        }
+    }
     // the marks of the span's listed classes, or none again
     auto mark = [&](int64_t c0, bool set) {
-        lists.over_places([&](int j, int n) {
-            const int64_t c = lists.id(j, n);
-            if (c >= c0 && c < min(c0 + kPartSpan, D.C)) *marks.of((int)(c - c0), n) = (uint8_t)(set ? j + 1 : 0);
-        });
+        for (uint64_t left = mine; left; left &= left - 1) {
+            const int i = (int)(__ffsll((long long)left) - 1) * kPartThreads + threadIdx.x;
+            const int64_t c = lists.id(i / N, i % N) - c0;
+            if (c >= 0 && c < kPartSpan) *marks.of((int)c, i % N) = (uint8_t)(set ? i / N + 1 : 0);
+        }
     };
+    __syncthreads();                     // the marks are clear
     float per[V], top[V];
     uint32_t live = 0;
 #pragma unroll

@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -78,7 +79,6 @@ class Tensor(ctypes.Structure):
 
 
 GRAD_NORM_WORKSPACE_BYTES = 8192
-DISTILL_WORKSPACE_BYTES = 1 << 22
 
 EXPORTS = ("dss_chain_geometry", "dss_chain_layer_geometry", "dss_plan_create", "dss_plan_destroy",
            "dss_plan_geometry", "dss_plan_layer_geometry", "dss_eval_dense", "dss_eval_mixed", "dss_eval_slide",
@@ -87,7 +87,7 @@ EXPORTS = ("dss_chain_geometry", "dss_chain_layer_geometry", "dss_plan_create", 
            "dss_plan_backward_geometry", "dss_backward_dense", "dss_eval_dense_noalloc", "dss_frag", "dss_defrag",
            "dss_grad_norm", "dss_clip_grads", "dss_quantize_tokens", "dss_tokens_workspace", "dss_matmul_tokens",
            "dss_linear_tokens", "dss_quantize_blocks", "dss_dequantize_blocks", "dss_blocks_workspace", "dss_matmul_blocks",
-           "dss_linear_blocks", "dss_distill_tokens", "dss_plan_set_timing", "dss_plan_timings", "dss_status_string", "dss_last_error", "dss_version")
+           "dss_linear_blocks", "dss_distill_workspace", "dss_distill_tokens", "dss_plan_set_timing", "dss_plan_timings", "dss_status_string", "dss_last_error", "dss_version")
 
 _lib = None
 
@@ -152,6 +152,7 @@ def lib():
         L.dss_matmul_blocks.argtypes = [VP, I64, VP, I64, I64, VP, I64, VP, I64, I32, I32, VP, I32, VP, I32, I64, I64, VP]
         L.dss_linear_blocks.argtypes = [VP, I32, I64, I64, I64, VP, I64, VP, I64, I32, I32, VP, I32, VP, I32, I64, I64, VP, I64,
                                      VP]
+        L.dss_distill_workspace.argtypes = [I32, I32, P(I64)]
         L.dss_distill_tokens.argtypes = [VP, I32, I64, I32, I64, I64, P(TopLogits), VP, ctypes.c_float, ctypes.c_float, VP,
                                          VP, I64, I64, VP, I64, VP]
         L.dss_plan_set_timing.argtypes = [VP, I32]
@@ -170,7 +171,7 @@ def lib():
                      "dss_plan_backward_geometry", "dss_backward_dense", "dss_eval_dense_noalloc", "dss_grad_norm",
                      "dss_clip_grads", "dss_quantize_tokens", "dss_tokens_workspace", "dss_matmul_tokens",
                      "dss_linear_tokens", "dss_quantize_blocks", "dss_dequantize_blocks", "dss_blocks_workspace",
-                     "dss_matmul_blocks", "dss_linear_blocks", "dss_distill_tokens"):
+                     "dss_matmul_blocks", "dss_linear_blocks", "dss_distill_workspace", "dss_distill_tokens"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -946,6 +947,14 @@ def linear_mx4(x, weight, weight_scales, bias=None, act="none", out=None, out_dt
 
 # ---------------------------------------------------------------------------- distillation
 
+@functools.lru_cache(maxsize=64)
+def distill_workspace(classes, planar=False):
+    """Workspace bytes of distill on positions of so many classes: rows, or with planar=True a map's."""
+    need = ctypes.c_int64()
+    _check(lib().dss_distill_workspace(classes, planar, need), "dss_distill_workspace")
+    return need.value
+
+
 def distill(logits, top_logits, top_ids, temperature=1.0, scale=1.0, weights=None, with_grad=True, losses=None, grad=None,
             workspace=None, stream=None):
     """The loss of a network's logits [M][C] against a teacher's top logits, and its gradient.  logits is a float32 or
@@ -985,9 +994,13 @@ def distill(logits, top_logits, top_ids, temperature=1.0, scale=1.0, weights=Non
                 grad.get_device() != dev:
             raise ValueError("grad must be of the logits' shape and type on the current CUDA device")
         gp, (gts, gcs) = grad.data_ptr(), grad.stride()
-    if workspace is None:
-        workspace = _empty(DISTILL_WORKSPACE_BYTES, torch.uint8, stream)
-    room, size = _room(workspace, dev)
+    if workspace is not None:
+        room, size = _room(workspace, dev)
+    else:
+        size = distill_workspace(C, cs != 1 and C > 1)
+        if size:
+            workspace = _empty(size, torch.uint8, stream)
+        room = workspace.data_ptr() if size else None
     top = TopLogits(top_logits.data_ptr(), top_ids.data_ptr(), *top_logits.stride(), *top_ids.stride(), k,
                     _dtype_codes()[top_logits.dtype], top_ids.element_size(), 0)
     _check(lib().dss_distill_tokens(logits.data_ptr(), dt, M, C, ts, cs, top, wp, temperature, scale, lp, gp, gts, gcs, room,

@@ -12,13 +12,17 @@ VP = ctypes.c_void_p
 
 
 def _distill(z=PTR, dt=0, M=4, C=10, ts=10, cs=1, top=True, weights=PTR, T=1.0, scale=1.0, losses=PTR, grad=PTR, gts=10, gcs=1,
-             room=PTR, bytes=dss.DISTILL_WORKSPACE_BYTES, **lists):
+             room=PTR, bytes=1 << 22, **lists):
     fields = dict(logits=PTR, ids=PTR, token_stride=3, place_stride=1, id_token_stride=3, id_place_stride=1, count=3, dtype=0,
                   id_bytes=4, reserved=0)
     fields.update(lists)
     t = dss.TopLogits(**fields)
     return dss.lib().dss_distill_tokens(VP(z), dt, M, C, ts, cs, ctypes.byref(t) if top else None, VP(weights), T, scale,
                                         VP(losses), VP(grad), gts, gcs, VP(room), bytes, None)
+
+
+LONG = dict(C=16384, ts=16384, gts=16384)              # sizes that need a workspace
+WIDE = dict(C=129, ts=1, cs=4, gts=1, gcs=4)
 
 
 @pytest.mark.parametrize("status,kw", [
@@ -33,12 +37,23 @@ def _distill(z=PTR, dt=0, M=4, C=10, ts=10, cs=1, top=True, weights=PTR, T=1.0, 
     (INVALID, dict(scale=float("nan"))), (INVALID, dict(losses=None)), (INVALID, dict(losses=PTR + 2)),
     (INVALID, dict(weights=PTR + 1)), (INVALID, dict(grad=PTR + 2)), (INVALID, dict(gts=9)), (INVALID, dict(gts=1, gcs=4)),
     (INVALID, dict(gts=20, gcs=2)), (INVALID, dict(ts=1, cs=4, gts=10, gcs=1)), (INVALID, dict(ts=1, cs=4, gts=1, gcs=3)),
-    (INVALID, dict(room=None)), (INVALID, dict(room=PTR + 8)), (SHAPE, dict(bytes=100)),
+    (INVALID, dict(LONG, room=None)), (INVALID, dict(LONG, room=PTR + 8)), (SHAPE, dict(LONG, bytes=100)),
+    (INVALID, dict(WIDE, room=None)), (SHAPE, dict(WIDE, bytes=100)), (INVALID, dict(grad=PTR, z=PTR, ts=20, gts=10)),
     (OK, dict(M=0, z=None, losses=None, grad=None, room=None)), (OK, dict(M=0, ts=1, cs=4, gts=1, gcs=4)),
 ], ids=str)
 def test_refusals(status, kw):
     assert _distill(**kw) == status
     assert status == OK or dss.lib().dss_last_error()
+
+
+def test_workspace_query():
+    need = ctypes.c_int64()
+    q = dss.lib().dss_distill_workspace
+    for C, planar, none in ((1, 0, True), (16383, 0, True), (16384, 0, False), (128, 1, True), (129, 1, False),
+                            (2 ** 31 - 1, 0, False), (2 ** 31 - 1, 1, False)):
+        assert q(C, planar, ctypes.byref(need)) == OK and (need.value == 0) == none and 0 <= need.value <= 1 << 22
+        assert dss.distill_workspace(C, bool(planar)) == need.value
+    assert q(0, 0, ctypes.byref(need)) == INVALID and q(4, 0, None) == INVALID
 
 
 def test_binding_refuses_what_is_no_cuda_tensor():

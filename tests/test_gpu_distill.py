@@ -266,7 +266,7 @@ def test_graph_replays(M, C, k, layout):
     """Two captured calls that share a workspace, replayed in turn with new inputs."""
     import torch
     z, top, ids = _inputs(M, C, k, layout)
-    room = torch.empty(dss.DISTILL_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    room = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
     outs = [(torch.empty(M, device="cuda"), torch.empty_like(z)) for _ in range(2)]
     graphs = []
     for n, (losses, grad) in enumerate(outs):
@@ -312,7 +312,7 @@ def test_binding_refusals():
                          (lambda: dss.distill(z, top, ids, grad=torch.empty((10, 6), device="cuda").t()), 1),
                          (lambda: dss.distill(z[:1].expand(6, 10), top, ids, grad=z[:1].expand(6, 10)), 1),
                          (lambda: dss.distill(z[::2, ::2], top[::2], ids[::2]), 3),
-                         (lambda: dss.distill(z, top, ids, workspace=torch.empty(100, dtype=torch.uint8, device="cuda")), 2)):
+                         (lambda: dss.distill(*_inputs(2, 20000, 3), workspace=torch.empty(100, dtype=torch.uint8, device="cuda")), 2)):
         with pytest.raises(dss.DssError) as e:
             call()
         assert e.value.status == status
