@@ -171,17 +171,23 @@ struct Logits {
 // E gradients from p on, the first n of them.
 template <typename T, int E>
 __device__ __forceinline__ void store_gradients(T* p, const float (&v)[E], int64_t n) {
-    struct {
-        T v[E];
-    } r;
-#pragma unroll
-    for (int e = 0; e < E; ++e) store_elem(&r.v[e], v[e]);
     if (n >= E) {
-        __builtin_memcpy(p, &r, sizeof r);
+        uint32_t w[E * sizeof(T) / 4];
+#pragma unroll
+        for (int i = 0; i < (int)(E * sizeof(T) / 4); ++i) {
+            if constexpr (sizeof(T) == 4) {
+                w[i] = __float_as_uint(v[i]);
+            } else {                     // (two at a time: one instruction)
+                using f32x2 = __attribute__((ext_vector_type(2))) float;
+                using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
+                w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{v[2 * i], v[2 * i + 1]}), bf16x2));
+            }
+        }
+        __builtin_memcpy(p, w, sizeof w);
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (e < n) p[e] = r.v[e];
+            if (e < n) store_elem(p + e, v[e]);
     }
 }
 

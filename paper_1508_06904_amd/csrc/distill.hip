@@ -151,7 +151,7 @@ __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float v = exp2_of((c[i].value(e) - z_max) * D.to_log2);
-            if constexpr (E == 4) c[i].w[e] = __float_as_uint(v);     // (bfloat16 has no room for it)
+            if constexpr (sizeof(T) == 4) c[i].w[e] = __float_as_uint(v);     // (bfloat16 has no room for it)
             part += v;
         }
         sums[1] += part;
@@ -169,19 +169,17 @@ __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_
     const float sw = D.scale * weight;
     if (lane == 0 && m_own < D.M) D.losses[m] = live ? sw * D.T * (D.T * loss[0]) : 0.f;
     if (!D.grad) return;
-    const float g = sw * D.T, per_sum = 1.f / sum_r;
+    const float g = sw * D.T, per_sum = 1.f / sum_r, per = g * per_sum;
     T* grad = static_cast<T*>(D.grad) + m * D.gts;
     if (m_own < D.M) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int at = (i * LPR + lane) * E;
             if (at >= (int)D.C) continue;
-            float v[E];
+            float v[E] = {};
+            if (live)
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                v[e] = E == 4 ? c[i].value(e) : exp2_of((c[i].value(e) - z_max) * D.to_log2);
-                v[e] = live ? g * (v[e] * per_sum) : 0.f;
-            }
+                for (int e = 0; e < E; ++e) v[e] = (sizeof(T) == 4 ? c[i].value(e) : exp2_of((c[i].value(e) - z_max) * D.to_log2)) * per;
             store_gradients(grad + at, v, D.C - at);
         }
     }
@@ -277,7 +275,7 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill D, int
     const float sw = D.scale * weight;
     if (threadIdx.x == 0 && blockIdx.x == 0 && with_loss) D.losses[m] = live ? sw * D.T * (D.T * loss[0]) : 0.f;
     if (!D.grad) return;
-    const float g = sw * D.T, per_sum = 1.f / sum_r;
+    const float g = sw * D.T, per_sum = 1.f / sum_r, per = g * per_sum;
     for (int64_t at = c0 + threadIdx.x * E; at < c1; at += U * kThreads * E) {
         Logits<T> c[U];
 #pragma unroll
@@ -286,7 +284,7 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill D, int
         for (int u = 0; u < U; ++u) {
             float v[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[e] = live ? g * (exp2_of((c[u].value(e) - z_max) * D.to_log2) * per_sum) : 0.f;
+            for (int e = 0; e < E; ++e) v[e] = live ? exp2_of((c[u].value(e) - z_max) * D.to_log2) * per : 0.f;
             const int64_t from = at + u * kThreads * E;
             if (from < c1) store_gradients(grad + from, v, c1 - from);
         }
