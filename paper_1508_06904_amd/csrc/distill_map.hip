@@ -14,9 +14,9 @@ namespace dss {
 namespace {
 
 // ------------------------------------------------------------------ few classes
-// A lane for each position, its logits in a column of LDS that no other lane touches: lists are gathered and gradients
-// of listed classes put together there, with no barrier.  Of a class that is in the list (its bit in `listed`) the column has the
-// gradient in the end, of any other one the logit.
+// A lane for each position, its logits in a column of LDS that no other lane touches: lists are gathered, and what they take
+// off the listed classes is taken off, there, with no barrier.  The column has the logits, then their exponentials, less
+// what the list takes off them.
 // kPlaces places of a list, loaded together: what a pass over a list costs is its loads' latency.  Lists of no more stay
 // in registers.
 constexpr int kPlaces = 8;
@@ -38,30 +38,36 @@ struct Places {
     }
 };
 
+// f(number, class) for all classes: 32, 8 and one at a time, so that what a class waits for is under way for others too.
+template <typename F>
+__device__ __forceinline__ void over_classes(int C, F f) {
+    int c = 0;
+    for (; c + 32 <= C; c += 32) f(std::integral_constant<int, 32>{}, c);
+    for (; c + 8 <= C; c += 8) f(std::integral_constant<int, 8>{}, c);
+    for (; c < C; ++c) f(std::integral_constant<int, 1>{}, c);
+}
+
 template <typename T>
 __global__ __launch_bounds__(64) void distill_columns_kernel(Distill D) {
     extern __shared__ float columns[];
     const int C = (int)D.C, lane = threadIdx.x, k = D.k;
     float* const col = columns + lane;
     const int64_t own = xcd_order(blockIdx.x, gridDim.x) * 64 + lane, m = min(own, D.M - 1);
-    const T* z = static_cast<const T*>(D.z) + m;
     Places a;
     a.load(D, m, 0);
     const float weight = D.weights ? D.weights[m] : 1.f;
-    constexpr int U = 32;
     float z_max = -INFINITY;
-    for (int c0 = 0; c0 < C; c0 += U) {
-        float v[U];
+    const T* z = static_cast<const T*>(D.z) + m;
+    over_classes(C, [&](auto n, int c) {
+        float v[n];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (c0 + u < C) v[u] = to_f32(z[(c0 + u) * D.cs]);
+        for (int u = 0; u < n; ++u, z += D.cs) v[u] = to_f32(*z);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (c0 + u < C) {
-                col[(c0 + u) * 64] = v[u];
-                z_max = fmaxf(z_max, v[u]);
-            }
-    }
+        for (int u = 0; u < n; ++u) {
+            col[(c + u) * 64] = v[u];
+            z_max = fmaxf(z_max, v[u]);
+        }
+    });
     // f of the list's places, batch by batch
     auto over_places = [&](auto f) {
         for (int j0 = 0; j0 < k; j0 += kPlaces) {
@@ -79,48 +85,44 @@ __global__ __launch_bounds__(64) void distill_columns_kernel(Distill D) {
     const float nan = state == 3.f ? quiet_nan() : 0.f;
     float sum_r = nan, sum_p = nan;
     over_places([&](int id, float t) { sum_p += weight_of(D, t, t_max); });
-    for (int c0 = 0; c0 < C; c0 += 16) {
-        float part = 0.f;
-#pragma unroll
-        for (int u = 0; u < 16; ++u)
-            if (c0 + u < C) part += exp2_of((col[(c0 + u) * 64] - z_max) * D.to_log2);
-        sum_r += part;
-    }
-    const float log_sums = logf(sum_p) - logf(sum_r), per_sum = 1.f / sum_r, per_p = 1.f / sum_p;
-    float loss = nan;
-    over_places([&](int id, float t) {
-        if (id >= 0 && id < C) loss += loss_of(D, weight_of(D, t, t_max) * per_p, t, t_max, col[id * 64], z_max, log_sums);
-    });
-    const float sw = D.scale * weight, g = sw * D.T;
-    if (own < D.M) D.losses[m] = live ? sw * D.T * (D.T * loss) : 0.f;
-    if (!D.grad) return;
-    uint32_t listed[kColumns / 32] = {};
+    // the loss but for its last term, sum p log(sum_p / sum_r)
+    const float per_p = 1.f / sum_p;
+    float loss = nan, mass = 0.f;
     over_places([&](int id, float t) {
         if (id < 0 || id >= C) return;
         const float p = weight_of(D, t, t_max) * per_p;
-        float v = col[id * 64];
-        bool before = false;
+        loss += loss_of(D, p, t, t_max, col[id * 64], z_max, 0.f);
+        mass += p;
+    });
+    over_classes(C, [&](auto n, int c) {
+        float v[n], part = 0.f;
 #pragma unroll
-        for (int w = 0; w < kColumns / 32; ++w) {
-            const uint32_t bit = id / 32 == w ? 1u << (id % 32) : 0u;
-            before |= (listed[w] & bit) != 0;
-            listed[w] |= bit;
+        for (int u = 0; u < n; ++u) v[u] = col[(c + u) * 64];
+#pragma unroll
+        for (int u = 0; u < n; ++u) {
+            v[u] = exp2_of((v[u] - z_max) * D.to_log2);
+            part += v[u];
+            col[(c + u) * 64] = v[u];
         }
-        if (!before) v = exp2_of((v - z_max) * D.to_log2) * per_sum;
-        col[id * 64] = v - p;
+        sum_r += part;
+    });
+    loss -= mass * (logf(sum_p) - logf(sum_r));
+    const float g = D.scale * weight * D.T;
+    if (own < D.M) D.losses[m] = live ? g * (D.T * loss) : 0.f;
+    if (!D.grad) return;
+    over_places([&](int id, float t) {
+        if (id >= 0 && id < C) col[id * 64] -= weight_of(D, t, t_max) * per_p * sum_r;
     });
     if (own >= D.M) return;
+    const float per = g / sum_r;
     T* grad = static_cast<T*>(D.grad) + m;
+    over_classes(C, [&](auto n, int c) {
+        float v[n];
 #pragma unroll
-    for (int w = 0; w < kColumns / 32; ++w) {
-        if (w * 32 >= C) break;
-#pragma unroll 16
-        for (int c = w * 32; c < min(w * 32 + 32, C); ++c) {
-            float v = col[c * 64];
-            if (!(listed[w] >> (c % 32) & 1)) v = exp2_of((v - z_max) * D.to_log2) * per_sum;
-            store_elem(grad + c * D.gcs, live ? g * v : 0.f);
-        }
-    }
+        for (int u = 0; u < n; ++u) v[u] = col[(c + u) * 64];
+#pragma unroll
+        for (int u = 0; u < n; ++u, grad += D.gcs) store_elem(grad, live ? v[u] * per : 0.f);
+    });
 }
 
 // ------------------------------------------------------------------ tiles
