@@ -84,7 +84,8 @@ __device__ __forceinline__ void store_few(const Mx4Layer& L, const FewSides& D, 
     const bool bias_on_j = ADJ == (D.bias_on_s != 0);
     float v[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = activate_nan(L.act, sum[k] + (L.bias ? L.bias[bias_on_j ? min(j + k, J - 1) : i] : 0.f));
+    for (int k = 0; k < 4; ++k) v[k] = sum[k] + (L.bias ? L.bias[bias_on_j ? min(j + k, J - 1) : i] : 0.f);
+    activate_all(L.act, v);
     store_values(static_cast<Tout*>(L.out) + i * L.ldo + j, v, j, J, 0);
 }
 

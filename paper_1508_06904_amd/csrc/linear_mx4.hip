@@ -6,7 +6,8 @@
 // a lane gets V adjacent tokens of four channels, which are a map's stores of 16 bytes, 256 adjacent bytes for 16 lanes.
 // The weights are in LDS.
 //
-// Bound by memory: the values in, the outputs out.
+// Bound by memory: the values in, the outputs out.  1.88 million tokens of 512 channels to 128 in binary32, map in and map out:
+// 1.10 ms (4.3 TB/s), and 1.03 where the map's rows are whole lines; at a large copy's 4.85 TB/s it would be 0.99.
 #include <algorithm>
 
 #include "dev_common.h"
@@ -26,8 +27,9 @@ using Block = MapBlock<T, (int)sizeof(T)>;
 
 // A weight row's codes in LDS: 16 bytes more than it has, so that rows start in different banks.
 __host__ __device__ constexpr int pitch_of(int B) { return B * 16 + 16; }
-// The weights' rows are a multiple of 16 there, their scales block by block.
-size_t weights_lds(int64_t N, int B) { return (size_t)ceil_div64(N, 16) * 16 * (pitch_of(B) + B); }
+// The weights' rows are a multiple of 16 there, their scales block by block; and the bias (loaded beside the outputs' stores it
+// would wait for them).
+size_t weights_lds(int64_t N, int B) { return (size_t)ceil_div64(N, 16) * 16 * (pitch_of(B) + B + 4); }
 
 // S steps of 128 channels.
 template <typename T, typename Tout, int S, bool MAP>
@@ -35,7 +37,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     constexpr int V = Block<T>::V;
     extern __shared__ __align__(16) uint8_t lds[];
     const int B = L.B, N = (int)L.weight.rows, N16 = (N + 15) / 16 * 16, pitch = pitch_of(B);
-    uint8_t* const scales = lds + N16 * pitch;
+    float* const biases = reinterpret_cast<float*>(lds + N16 * pitch);
+    uint8_t* const scales = reinterpret_cast<uint8_t*>(biases + N16);
     const int lane = threadIdx.x & 63, l16 = lane & 15, q16 = lane >> 4;
     const int64_t M = L.tokens.rows, K = X.channels, ks = X.channel_stride;
     // (the last tile ends with the last token, and computes what the ones before it have over again)
@@ -50,10 +53,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
     };
     // the first values are on their way while the weights are put into LDS
     load(0);
-    for (int n = threadIdx.x; n < N16 * B; n += kThreads) {
-        const int row = n / B, b = n - row * B, from = min(row, N - 1);
-        *reinterpret_cast<i32x4*>(lds + row * pitch + b * 16) = *reinterpret_cast<const i32x4*>(L.weight.codes + from * L.weight.stride + b * 16);
-        scales[b * N16 + row] = L.weight.scales[b * L.weight.scales_stride + from];
+    for (int n = threadIdx.x; n < N16; n += kThreads) biases[n] = L.bias ? L.bias[min(n, N - 1)] : 0.f;
+    constexpr int U = 8;                 // of them under way
+    for (int n0 = threadIdx.x; n0 < N16 * B; n0 += U * kThreads) {
+        i32x4 w[U];
+        uint8_t x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int n = min(n0 + u * kThreads, N16 * B - 1), from = min(n / B, N - 1);
+            w[u] = *reinterpret_cast<const i32x4*>(L.weight.codes + from * L.weight.stride + (n % B) * 16);
+            // (in the order in which they lie)
+            x[u] = L.weight.scales[n / N16 * L.weight.scales_stride + min(n % N16, N - 1)];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int n = n0 + u * kThreads;
+            if (n >= N16 * B) continue;
+            *reinterpret_cast<i32x4*>(lds + n / B * pitch + (n % B) * 16) = w[u];
+            scales[n] = x[u];
+        }
     }
 #pragma unroll
     for (int s = 0; s < S; ++s) {
@@ -80,28 +98,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2))) v
             for (int j = 0; j < V; ++j) acc[j] = multiply_at(j, w, w_scale, codes[s][j], bytes[s], acc[j]);
         }
         const int n = n0 + q16 * 4;
-        float bias[4] = {};
-        if (L.bias)
+        const f32x4 bias = *reinterpret_cast<const f32x4*>(biases + n);
+        float out[4 * V];                // [channel][token] of a map, [token][channel] of rows
 #pragma unroll
-            for (int r = 0; r < 4; ++r) bias[r] = L.bias[min(n + r, N - 1)];
-        if constexpr (MAP) {
+        for (int j = 0; j < V; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (n + r >= N) continue;
-                float out[V];
+            for (int r = 0; r < 4; ++r) out[MAP ? r * V + j : j * 4 + r] = acc[j][r] + bias[r];
+        activate_all(L.act, out);
+        constexpr int LINES = MAP ? 4 : V, PER = MAP ? V : 4;
 #pragma unroll
-                for (int j = 0; j < V; ++j) out[j] = activate_nan(L.act, acc[j][r] + bias[r]);
-                store_values(static_cast<Tout*>(L.out) + (n + r) * L.ldo + m, out, 0, V, L.past);
+        for (int l = 0; l < LINES; ++l) {
+            float line[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) line[i] = out[l * PER + i];
+            if constexpr (MAP) {
+                if (n + l < N) store_values(static_cast<Tout*>(L.out) + (n + l) * L.ldo + m, line, 0, V, L.past);
+            } else {
+                if (n < N) store_values(static_cast<Tout*>(L.out) + (m + l) * L.ldo + n, line, n, N, L.past);
             }
-        } else {
-            if (n < N)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float out[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) out[r] = activate_nan(L.act, acc[j][r] + bias[r]);
-                    store_values(static_cast<Tout*>(L.out) + (m + j) * L.ldo + n, out, n, N, L.past);
-                }
         }
     }
 }
@@ -121,16 +135,27 @@ hipError_t run_steps(const Mx4Layer& L, const Mx4Values& X, hipStream_t s) {
     return L.B <= 8 ? run_linear<T, Tout, 2>(L, X, s) : run_linear<T, Tout, 4>(L, X, s);
 }
 
-constexpr int64_t kLeastTokens = 4096;
+constexpr int64_t kLeastTokens = 256;
 
 }  // namespace
 
+// Where one launch is the faster one.  In microseconds for one launch and for two (GPU, outputs a binary32 map), channels to
+// outputs:
+//                binary32: 64-256    256-16    256-64   256-256   512-128   bfloat16: 64-256    256-64   256-256   512-128
+//   1000 tokens            14/8       7/8       9/8      15/8      17/9               14/10     9/9      15/9      16/10
+//   20000                  17/15      9/12     11/13     19/17     21/19              17/16    11/12     18/16     20/16
+//   100000                 27/36     25/36     29/39     52/55     58/73              25/35    23/30     42/46     43/54
+//   400000                135/150    95/125   117/146   201/249   238/295            129/136   74/99    168/211   156/212
+// The rule takes all of them from 32768 tokens on; few outputs of few channels, where the two are about as fast on the GPU,
+// for the launch and the workspace that a call then does without, from 256 on.  1.88 million bfloat16 tokens of 64
+// channels to 256 outputs lose (697/645): they are the only ones measured.
 bool linear_mx4_at_once(int64_t M, int64_t N, int64_t K, bool map) {
-    return map && M >= kLeastTokens && K <= 512 && weights_lds(N, (int)blocks_of(K)) <= 72 * 1024;
+    const bool fits = map && K <= 512 && weights_lds(N, (int)blocks_of(K)) <= 72 * 1024;
+    return fits && (M >= 32768 || (M >= kLeastTokens && N <= 64 && K <= 256));
 }
 
 hipError_t launch_linear_mx4(const Mx4Layer& L, const Mx4Values& X, dss_dtype out_dtype, hipStream_t s) {
-    // slabs of equal size but for the last, none below kLeastTokens
+    // (slabs of equal size but for the last, none below a tile)
     const int64_t slab = ceil_div64(L.tokens.rows, ceil_div64(L.tokens.rows, (int64_t)1 << 29));
     for (int64_t m = 0; m < L.tokens.rows; m += slab) {
         Mx4Layer P = L;

@@ -97,7 +97,8 @@ __device__ __forceinline__ void store_tile(const Mx4Layer& L, const f32x4 (&acc)
             float v[C];
 #pragma unroll
             for (int k = 0; k < C; ++k)
-                v[k] = activate_nan(L.act, acc[a][c * (C / 4) + k / 4][k % 4] + (MAP ? bias_i[a] : bias_j[c][k]));
+                v[k] = acc[a][c * (C / 4) + k / 4][k % 4] + (MAP ? bias_i[a] : bias_j[c][k]);
+            activate_all(L.act, v);
             store_values(static_cast<Tout*>(L.out) + i * L.ldo + j + c * 4 * C, v, j + c * 4 * C, J, L.past);
         }
     }
