@@ -365,17 +365,10 @@ hipError_t run_deep(const Mx4Layer& L, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Measured as kTiles are; steps of kStep bytes of K.  Microseconds on 256, 128 and 64: 8192 x 8192 x 8192 346, 465, 853;
-// 4096 x 4096 x 4096 47, 56, 83; 2048 x 4096 x 4096 39, 30, 45; 512 x 4096 x 4096 37, 24, 12.7; 1777 x 1003 x 2305 32, 19,
-// 11.2; 300 x 300 x 2304 23, 12, 7.0; 100000 x 512 x 256 44, 43, 54; 128 x 8192 x 9216 70, 46, 19.
-constexpr TileTime kMx4Tiles[] = {{256, 1, 1, 2.4, 0, 7.0}, {128, 1, 2, 1.2, 0.4, 4.5}, {64, 1, 3, 0.42, 0.13, 3.0}};
-
 template <typename Tout>
 hipError_t run_product(const Mx4Layer& L, hipStream_t s) {
     const Sides S = sides_of(L);
-    // (the small tiles hold their scales in LDS, of up to 28672 channels)
-    const bool small = deep_lds(64, 64, 3, L.B) <= 160 * 1024;
-    const int t = pick_tile(kMx4Tiles, small ? 3 : 2, S.P.rows, S.Q.rows, L.B * 16);
+    const int t = pick_mx4_tile(S.P.rows, S.Q.rows, L.B);
     if (t == 0) return run_tile<Tout, 256, 256, 2, 4>(L, s);
     if (t == 1) return run_tile<Tout, 128, 128, 2, 2>(L, s);
     return run_deep<Tout, 64, 64, 3>(L, s);
