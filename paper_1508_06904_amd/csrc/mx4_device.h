@@ -169,13 +169,9 @@ __device__ __forceinline__ void store_values(Tout* p, const float (&v)[N], int64
 #pragma unroll
         for (int k = 0; k < C; ++k) store_elem(&r.v[k], v[c + k]);
         if (j + c + C <= J) {
-            if constexpr (sizeof(Tout) * C == 16) {
-                using u32x4 = __attribute__((ext_vector_type(4), aligned(sizeof(Tout)))) uint32_t;
-                if (past) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, r), reinterpret_cast<u32x4*>(p + c));
-                else __builtin_memcpy(p + c, &r, sizeof r);
-            } else {
-                __builtin_memcpy(p + c, &r, sizeof r);
-            }
+            using Words = __attribute__((ext_vector_type(C * sizeof(Tout) / 4), aligned(sizeof(Tout)))) uint32_t;
+            if (past) __builtin_nontemporal_store(__builtin_bit_cast(Words, r), reinterpret_cast<Words*>(p + c));
+            else __builtin_memcpy(p + c, &r, sizeof r);
         } else {
 #pragma unroll
             for (int k = 0; k < C; ++k)
