@@ -3,6 +3,7 @@
 //
 // Bound by memory: every value is read once, its half byte and a 32nd of a scale's byte written once.
 #include <algorithm>
+#include <type_traits>
 
 #include "dev_common.h"
 #include "dss_internal.h"
@@ -16,35 +17,40 @@ namespace {
 constexpr int kThreads = 256;
 
 // ------------------------------------------------------------------ rows
-// A workgroup has kRowTokens tokens of kRowBlocks blocks, four lanes for a block: a wave reads 512 adjacent channels of a
-// token at a time. The scales turn round in LDS, so that those of adjacent tokens leave together.
-constexpr int kRowTokens = 32, kRowBlocks = 16;
+// A workgroup has BLOCKS blocks of its tokens, four lanes for a block: a wave reads 512 adjacent channels of a
+// token at a time, or 128 of four tokens that have no more. The scales turn round in LDS, so that those of adjacent tokens
+// leave together.
+constexpr int kRowBlocks = 512;          // of a workgroup, of all its tokens
+constexpr int kFewBlocks = 4;            // of a token, at most, where a workgroup has four times the tokens
 
-template <typename T>
+template <typename T, int BLOCKS>
 __global__ __launch_bounds__(kThreads) void quantize_mx4_rows_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t ts,
                                                                      uint8_t* __restrict__ codes, int64_t codes_stride,
                                                                      uint8_t* __restrict__ scales, int64_t scales_stride) {
-    __shared__ uint8_t bytes[kRowBlocks][kRowTokens];
-    const int64_t m0 = (int64_t)blockIdx.x * kRowTokens, b0 = (int64_t)blockIdx.y * kRowBlocks;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t b = b0 + (lane >> 2), k = b0 * kBlock + lane * 8;
-    constexpr int PER = kRowTokens / (kThreads / 64);      // tokens of a wave
+    constexpr int TOKENS = kRowBlocks / BLOCKS, PER = kRowBlocks * 4 / kThreads;
+    __shared__ uint8_t bytes[BLOCKS][TOKENS];
+    const int64_t m0 = (int64_t)blockIdx.x * TOKENS, b0 = (int64_t)blockIdx.y * BLOCKS;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = lane % (BLOCKS * 4), block = quarter >> 2;
+    const int64_t b = b0 + block, k = b0 * kBlock + quarter * 8;
+    constexpr int AT_ONCE = 16 / BLOCKS;                   // tokens of a wave's load
+    const int own = wave * PER * AT_ONCE + (AT_ONCE > 1 ? lane / (BLOCKS * 4) : 0);
+    const int64_t m_own = m0 + own;
     Eight<T> v[PER];
 #pragma unroll
     for (int n = 0; n < PER; ++n)
-        if (m0 + wave * PER + n < M) v[n].load(x + (m0 + wave * PER + n) * ts + k, K - k);
+        if (m_own + n * AT_ONCE < M) v[n].load(x + (m_own + n * AT_ONCE) * ts + k, K - k);
 #pragma unroll
     for (int n = 0; n < PER; ++n) {
         const uint32_t byte = v[n].scale_byte_of_four();
-        const int64_t m = m0 + wave * PER + n;
+        const int64_t m = m_own + n * AT_ONCE;
         if (m < M && b * kBlock < K) *reinterpret_cast<uint32_t*>(codes + m * codes_stride + k / 2) = v[n].codes(byte);
-        if ((lane & 3) == 0) bytes[lane >> 2][wave * PER + n] = (uint8_t)byte;
+        if ((quarter & 3) == 0) bytes[block][own + n * AT_ONCE] = (uint8_t)byte;
     }
     __syncthreads();
 #pragma unroll
-    for (int n = threadIdx.x; n < kRowBlocks * kRowTokens; n += kThreads) {
-        const int64_t m = m0 + n % kRowTokens, at = b0 + n / kRowTokens;
-        if (m < M && at * kBlock < K) scales[at * scales_stride + m] = bytes[n / kRowTokens][n % kRowTokens];
+    for (int n = threadIdx.x; n < kRowBlocks; n += kThreads) {
+        const int64_t m = m0 + n % TOKENS, at = b0 + n / TOKENS;
+        if (m < M && at * kBlock < K) scales[at * scales_stride + m] = bytes[n / TOKENS][n % TOKENS];
     }
 }
 
@@ -100,36 +106,57 @@ __device__ __forceinline__ float value_of(uint32_t word, int k, float scale, boo
     return nan ? __uint_as_float(0x7fc00000u) : v[k & 1];
 }
 
-// Rows: four lanes for a block, eight adjacent values each.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void dequantize_mx4_rows_kernel(Mx4Rows R, int64_t K, T* __restrict__ out, int64_t ts) {
-    const int64_t m0 = (int64_t)blockIdx.x * kRowTokens + (threadIdx.x >> 6) * (kRowTokens / (kThreads / 64));
-    const int lane = threadIdx.x & 63;
-    const int64_t b = (int64_t)blockIdx.y * kRowBlocks + (lane >> 2), k = (int64_t)blockIdx.y * kRowBlocks * kBlock + lane * 8;
-    if (b * kBlock >= K) return;
+// Rows: 16 bytes of values for a lane, so that a wave writes 1 KB at a time, around the caches where rows are whole lines.
+// The scales of a workgroup's tokens and blocks come through LDS: of a block they are adjacent, of a token they are not.
+// 1.88 million tokens of 512 channels to binary32: 743 us; with 32 bytes for a lane, which are two stores of half the lines, and scales
+// from memory 1815.  (A fill of the values takes 560.)
+template <typename T, int BLOCKS>
+__global__ __launch_bounds__(kThreads) void dequantize_mx4_rows_kernel(Mx4Rows R, int64_t K, T* __restrict__ out, int64_t ts, int past) {
+    constexpr int V = 16 / (int)sizeof(T), TOKENS = kRowBlocks / BLOCKS, PER = kRowBlocks * (kBlock / V) / kThreads;
+    using Word = std::conditional_t<V == 4, uint16_t, uint32_t>;         // V codes
+    __shared__ uint8_t bytes[BLOCKS][TOKENS];
+    const int64_t m0 = (int64_t)blockIdx.x * TOKENS, b0 = (int64_t)blockIdx.y * BLOCKS;
 #pragma unroll
-    for (int n = 0; n < kRowTokens / (kThreads / 64); ++n) {
-        const int64_t m = m0 + n;
-        if (m >= R.rows) return;
-        const uint32_t word = *reinterpret_cast<const uint32_t*>(R.codes + m * R.stride + k / 2);
-        const uint32_t byte = R.scales[b * R.scales_stride + m];
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = value_of(word, i, scale_operand(byte), byte == 255u);
-        store_values(out + m * ts + k, v, k, K, 0);
+    for (int n = threadIdx.x; n < kRowBlocks; n += kThreads) {
+        const int64_t m = m0 + n % TOKENS, at = b0 + n / TOKENS;
+        bytes[n / TOKENS][n % TOKENS] = m < R.rows && at * kBlock < K ? R.scales[at * R.scales_stride + m] : (uint8_t)0;
     }
+    // A lane's pieces of V values: TURNS of a token that has ROW, or one of each AT_ONCE tokens.
+    constexpr int ROW = BLOCKS * kBlock / V, TURNS = ROW > 64 ? ROW / 64 : 1, AT_ONCE = ROW > 64 ? 1 : 64 / ROW, N = PER / TURNS;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int own = wave * N * AT_ONCE + (AT_ONCE > 1 ? lane / ROW : 0), place = AT_ONCE > 1 ? lane % ROW : lane;
+    Word w[N][TURNS];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int t = 0; t < TURNS; ++t) {
+            const int64_t m = m0 + own + n * AT_ONCE, k = b0 * kBlock + (t * 64 + place) * V;
+            w[n][t] = m < R.rows && k < K ? *reinterpret_cast<const Word*>(R.codes + m * R.stride + k / 2) : (Word)0;
+        }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int t = 0; t < TURNS; ++t) {
+            const int64_t m = m0 + own + n * AT_ONCE, k = b0 * kBlock + (t * 64 + place) * V;
+            if (m >= R.rows || k >= K) continue;
+            const uint32_t byte = bytes[(t * 64 + place) * V / kBlock][own + n * AT_ONCE];
+            float v[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = value_of(w[n][t], i, scale_operand(byte), byte == 255u);
+            store_values(out + m * ts + k, v, k, K, past);
+        }
 }
 
-// Maps: a block of 4 or 8 adjacent tokens for a lane, and a wave's tokens are adjacent, so that it writes 1 KB of a channel
-// at a time.  1.88 million tokens of 512 channels to binary32: 1242 us; 256 bytes at a time 1515, 4 KB (four waves side by
-// side) 1380.
-constexpr int kMapBlocks = 4, kMapTokens = 64;        // of a workgroup: blocks, lanes side by side
+// Maps whose rows are whole lines of 128 bytes: a block of 4 or 8 adjacent tokens for a lane, and a wave's tokens are adjacent, so
+// that it writes 1 KB of a channel at a time, around the caches.
+constexpr int kMapWaves = 4;             // of a workgroup, adjacent blocks of the same tokens
 
 template <typename T>
-__global__ __launch_bounds__(kMapBlocks * kMapTokens) void dequantize_mx4_map_kernel(Mx4Rows R, int64_t K, T* __restrict__ out, int64_t ks) {
+__global__ __launch_bounds__(kMapWaves * 64) void dequantize_mx4_whole_kernel(Mx4Rows R, int64_t K, T* __restrict__ out, int64_t ks) {
     constexpr int V = 16 / (int)sizeof(T);
-    const int64_t m = (xcd_order(blockIdx.x, gridDim.x) * kMapTokens + threadIdx.x % kMapTokens) * V;
-    const int64_t b = (int64_t)blockIdx.y * kMapBlocks + threadIdx.x / kMapTokens;
+    const int64_t m = (xcd_order(blockIdx.x, gridDim.x) * 64 + (threadIdx.x & 63)) * V;
+    const int64_t b = (int64_t)blockIdx.y * kMapWaves + (threadIdx.x >> 6);
     if (b * kBlock >= K || m >= R.rows) return;
     i32x4 w[V];
     uint32_t byte[V];
@@ -146,7 +173,59 @@ __global__ __launch_bounds__(kMapBlocks * kMapTokens) void dequantize_mx4_map_ke
         float v[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = value_of((uint32_t)w[j][k / 8], k % 8, scale_operand(byte[j]), byte[j] == 255u);
-        if (k < n) store_values(p + k * ks, v, m, R.rows, 0);
+        if (k < n) store_values(p + k * ks, v, m, R.rows, 1);
+    }
+}
+
+// Other maps: a channel's lines start at any token. A wave writes whole ones all the same, 256 tokens of a channel at a time: it
+// has a line's tokens more, a block of each in LDS, from where a lane takes those of the channel's lines.  With its tokens in registers
+// and the lines as they come 1.88 million tokens of 512 channels took 1194 us for 870 (bfloat16 642 for 591); where
+// rows are whole lines the detour through LDS costs (884 for 870, but 518 for 599 of bfloat16, and 10.4 for 14.0 of 20000 tokens).
+template <typename T>
+struct MapLines {
+    // (8 of bfloat16 for a lane would read 32 bytes of LDS 32 bytes apart, twice over the same banks: 829 us for 518)
+    static constexpr int V = 4, kTokens = 64 * V, kLine = 128 / (int)sizeof(T), kAll = kTokens + kLine;
+    uint32_t words[4][kAll];             // of eight codes each
+    uint32_t scales[kAll];
+};
+
+template <typename T>
+__global__ __launch_bounds__(kMapWaves * 64) void dequantize_mx4_map_kernel(Mx4Rows R, int64_t K, T* __restrict__ out, int64_t ks) {
+    using Lines = MapLines<T>;
+    constexpr int V = Lines::V;
+    __shared__ Lines lines[kMapWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int64_t m0 = xcd_order(blockIdx.x, gridDim.x) * Lines::kTokens, b = (int64_t)blockIdx.y * kMapWaves + wave;
+    const bool there = b * kBlock < K;
+    Lines& own = lines[wave];
+    if (there) {
+#pragma unroll
+        for (int t = lane; t < Lines::kAll; t += 64) {
+            const int64_t m = min(m0 + t, R.rows - 1);
+            const i32x4 w = *reinterpret_cast<const i32x4*>(R.codes + m * R.stride + b * 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) own.words[i][t] = (uint32_t)w[i];
+            own.scales[t] = (uint32_t)R.scales[b * R.scales_stride + m] << 23;
+        }
+    }
+    __syncthreads();
+    if (!there) return;
+    const int n = (int)min((int64_t)kBlock, K - b * kBlock);
+    T* p = out + m0 + b * kBlock * ks;
+#pragma unroll 8
+    for (int k = 0; k < kBlock; ++k, p += ks) {
+        if (k >= n) break;
+        const int shift = (int)(-(uintptr_t)p % 128 / sizeof(T)), at = shift + lane * V;
+        auto value = [&](uint32_t word, uint32_t scale) { return value_of(word, k % 8, __uint_as_float(scale), scale == 255u << 23); };
+        uint32_t w[V], x[V];
+        __builtin_memcpy(w, &own.words[k / 8][at], sizeof w);
+        __builtin_memcpy(x, &own.scales[at], sizeof x);
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = value(w[j], x[j]);
+        store_values(p + at, v, m0 + at, R.rows, 1);
+        // the first tokens' part of a line
+        if (m0 == 0 && lane < min((int64_t)shift, R.rows)) store_elem(p + lane, value(own.words[k / 8][lane], own.scales[lane]));
     }
 }
 
@@ -174,7 +253,7 @@ hipError_t run_quantize(const T* x, int64_t M, int64_t K, int64_t ts, int64_t ks
         }
         return hipSuccess;
     }
-    const int64_t per_y = map ? kThreads / 16 : kRowBlocks, slab_b = kGridY * per_y, slab = slab_tokens(B, per_y);
+    const int64_t row_blocks = B <= kFewBlocks ? kFewBlocks : 16, per_y = map ? kThreads / 16 : row_blocks, slab_b = kGridY * per_y, slab = slab_tokens(B, per_y);
     for (int64_t b = 0; b < B; b += slab_b) {
         const int64_t n_b = std::min(B - b, slab_b), k = b * kBlock;
         for (int64_t m = 0; m < M; m += slab) {
@@ -182,10 +261,11 @@ hipError_t run_quantize(const T* x, int64_t M, int64_t K, int64_t ts, int64_t ks
             if (map && n < MapBlock<T>::kTokens) m0 = M - MapBlock<T>::kTokens, n = MapBlock<T>::kTokens;
             const T* p = x + m0 * (map ? 1 : ts) + k * (map ? ks : 1);
             uint8_t *c = codes + m0 * cs + b * 16, *sc = scales + b * ss + m0;
-            const dim3 grid((unsigned)ceil_div64(n, map ? MapBlock<T>::kTokens : kRowTokens), (unsigned)ceil_div64(n_b, per_y));
+            const dim3 grid((unsigned)ceil_div64(n, map ? MapBlock<T>::kTokens : kRowBlocks / row_blocks), (unsigned)ceil_div64(n_b, per_y));
             const int64_t channels = std::min(K - k, slab_b * kBlock);
             if (map) quantize_mx4_map_kernel<T><<<grid, kThreads, 0, s>>>(p, n, channels, ks, c, cs, sc, ss);
-            else quantize_mx4_rows_kernel<T><<<grid, kThreads, 0, s>>>(p, n, channels, ts, c, cs, sc, ss);
+            else if (row_blocks == 16) quantize_mx4_rows_kernel<T, 16><<<grid, kThreads, 0, s>>>(p, n, channels, ts, c, cs, sc, ss);
+            else quantize_mx4_rows_kernel<T, kFewBlocks><<<grid, kThreads, 0, s>>>(p, n, channels, ts, c, cs, sc, ss);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
@@ -195,18 +275,21 @@ hipError_t run_quantize(const T* x, int64_t M, int64_t K, int64_t ts, int64_t ks
 
 template <typename T>
 hipError_t run_dequantize(const Mx4Rows& R, int64_t K, T* out, int64_t ts, int64_t ks, bool map, hipStream_t s) {
-    constexpr int kTokens = kMapTokens * (16 / (int)sizeof(T));
-    const int64_t B = blocks_of(K), per_y = map ? kMapBlocks : kRowBlocks, slab_b = kGridY * per_y;
-    const int64_t slab = slab_tokens(B, per_y);  // (tiles of at least 256 tokens: fewer threads than rows have)
+    const int64_t B = blocks_of(K), row_blocks = B <= kFewBlocks ? kFewBlocks : 16, per_y = map ? kMapWaves : row_blocks, slab_b = kGridY * per_y;
+    const bool whole = (map ? ks : ts) * (int64_t)sizeof(T) % 128 == 0 && (uintptr_t)out % 128 == 0;
+    const int64_t tokens = !map ? kRowBlocks / row_blocks : whole ? 64 * (16 / (int)sizeof(T)) : MapLines<T>::kTokens;
+    const int64_t slab = slab_tokens(B, per_y);  // (tiles of maps have 256 tokens: fewer threads than rows)
     for (int64_t b = 0; b < B; b += slab_b) {
         const int64_t n_b = std::min(B - b, slab_b), k = b * kBlock, channels = std::min(K - k, slab_b * kBlock);
         for (int64_t m = 0; m < R.rows; m += slab) {
             const Mx4Rows P = {R.codes + m * R.stride + b * 16, R.stride, R.scales + b * R.scales_stride + m, R.scales_stride,
                                std::min(R.rows - m, slab)};
-            const dim3 grid((unsigned)ceil_div64(P.rows, map ? kTokens : kRowTokens), (unsigned)ceil_div64(n_b, per_y));
+            const dim3 grid((unsigned)ceil_div64(P.rows, tokens), (unsigned)ceil_div64(n_b, per_y));
             T* p = out + m * (map ? 1 : ts) + k * (map ? ks : 1);
-            if (map) dequantize_mx4_map_kernel<T><<<grid, kMapBlocks * kMapTokens, 0, s>>>(P, channels, p, ks);
-            else dequantize_mx4_rows_kernel<T><<<grid, kThreads, 0, s>>>(P, channels, p, ts);
+            if (!map && row_blocks == 16) dequantize_mx4_rows_kernel<T, 16><<<grid, kThreads, 0, s>>>(P, channels, p, ts, whole);
+            else if (!map) dequantize_mx4_rows_kernel<T, kFewBlocks><<<grid, kThreads, 0, s>>>(P, channels, p, ts, whole);
+            else if (whole) dequantize_mx4_whole_kernel<T><<<grid, kMapWaves * 64, 0, s>>>(P, channels, p, ks);
+            else dequantize_mx4_map_kernel<T><<<grid, kMapWaves * 64, 0, s>>>(P, channels, p, ks);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }

@@ -249,3 +249,49 @@ def test_a_call_on_a_stream_that_is_not_the_current_one_owns_its_memory():
         torch.empty(4096 * 400, dtype=torch.uint8, device="cuda").fill_(255)   # (as large as the workspace)
     torch.cuda.current_stream().wait_stream(side)
     assert all(torch.equal(want, y) for y in got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K", [(1, 40), (2, 33), (40, 32), (65, 31), (255, 100), (256, 64), (257, 129), (700, 70), (1025, 32)])
+def test_maps_whose_lines_start_anywhere(M, K, dtype):
+    """Values to maps of every place within a line, for their first element and from channel to channel, and nothing beside
+    them."""
+    import torch
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    codes, scales = _coded(M, K, 21)
+    want = _dev(mx4.values(codes, scales, K).astype(np.float32)).to(dt).t()
+    q, s = _dev(codes), _dev(scales)
+    line = 128 // dt.itemsize
+    for pad in (0, 1, line // 2, line - 1, line - M % line):
+        for first in sorted({0, 1, line // 2 + 1, line - 1, line}):
+            buf = torch.full((first + K * (M + pad) + line,), -77.0, dtype=dt, device="cuda")
+            out = buf.as_strided((K, M), (M + pad, 1), first)
+            dss.dequantize_mx4(q, s, K, out=out, planar=True)
+            assert torch.equal(out, want), (pad, first)
+            out.fill_(-77)
+            assert bool((buf == -77).all()), (pad, first)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K", [1, 7, 31, 32, 33, 64, 96, 100, 127, 128, 129, 160])
+def test_rows_of_few_blocks(K, dtype):
+    """Around the count of blocks up to which a wave has several tokens: codes and values, and nothing beside them."""
+    import torch
+    for M in (1, 3, 127, 128, 129, 300):
+        x = _x(M, K, "rows", dtype, seed=K)
+        B = -(-K // 32)
+        cbuf = torch.full((M + 2, 16 * B + 32), 55, dtype=torch.uint8, device="cuda")
+        sbuf = torch.full((B + 2, M + 3), 55, dtype=torch.uint8, device="cuda")
+        q, s = cbuf[1:M + 1, 16:16 + 16 * B], sbuf[1:B + 1, 1:M + 1]
+        dss.quantize_mx4(x, q, s)
+        want, wsc = mx4.quantize(_np(x))
+        assert np.array_equal(q.cpu().numpy(), want) and np.array_equal(s.cpu().numpy(), wsc)
+        for pad in (0, 3, 128 // x.dtype.itemsize - K % 64):
+            buf = torch.full((M + 2, K + max(pad, 0) + 1), -77.0, dtype=x.dtype, device="cuda")
+            out = buf[1:M + 1, :K]
+            dss.dequantize_mx4(q, s, K, out=out)
+            assert np.array_equal(_np(out), mx4.values(want, wsc, K)), (M, pad)
+            out.fill_(-77)
+            assert bool((buf == -77).all())
+        q.fill_(55), s.fill_(55)
+        assert bool((cbuf == 55).all()) and bool((sbuf == 55).all())
