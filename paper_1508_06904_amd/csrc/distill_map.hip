@@ -594,8 +594,10 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_gradient_kernel(Dist
             for (int j = 0; j < V; ++j) v[j] = live >> j & 1 ? v[j] : 0.f;
             store_gradients(grad + m + (c0 + r) * D.gcs, v, D.M - m);
         }
+        if (span + kPartSpan >= c1) break;
         __syncthreads();
         mark(span, false);
+        __syncthreads();                 // (a class of the next span may have the same mark)
     }
 }
 
