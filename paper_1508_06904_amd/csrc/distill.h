@@ -32,6 +32,10 @@ struct Distill {
     int64_t gts, gcs;
 };
 
+// Bytes of logits beyond which a pass over them had better leave the caches to others; and beyond which the next pass
+// would not find them there either.
+constexpr int64_t kLarge = (int64_t)1 << 26, kNeverCached = (int64_t)1 << 28;
+
 // The largest logit of a part of a position's classes, and the sum of exponentials of differences to it.
 struct Part {
     float top, sum;
@@ -45,7 +49,7 @@ constexpr int kMostParts = DSS_DISTILL_WORKSPACE_BYTES / (int)sizeof(Part);
 constexpr int kColumns = 128;            // classes of a map that need no parts
 hipError_t launch_distill_map(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s);
 
-// A workgroup for each position, any strides: maps of few positions or with long lists.
+// A workgroup for each position, any strides: maps with long lists.
 hipError_t launch_distill_any(const Distill& D, dss_dtype dt, hipStream_t s);
 
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
@@ -138,12 +142,21 @@ struct Logits {
 #pragma unroll
         for (int i = 0; i < W; ++i) w[i] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
     }
-    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(w, p, 4 * W); }
+    // PAST: around the caches.
+    template <bool PAST = false>
+    __device__ __forceinline__ void load(const T* p) {
+        using Words = __attribute__((ext_vector_type(W), aligned(sizeof(T)))) uint32_t;
+        const Words* const q = reinterpret_cast<const Words*>(p);
+        const Words v = PAST ? __builtin_nontemporal_load(q) : *q;
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = v[i];
+    }
     // Those from p on, -infinity for those from n on.
+    template <bool PAST = false>
     __device__ __forceinline__ void load(const T* p, int64_t n) {
         clear();
         if (n >= E) {
-            load(p);
+            load<PAST>(p);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e)
@@ -169,10 +182,11 @@ struct Logits {
 };
 
 // E gradients from p on, the first n of them.
-template <typename T, int E>
+template <bool PAST, typename T, int E>
 __device__ __forceinline__ void store_gradients(T* p, const float (&v)[E], int64_t n) {
     if (n >= E) {
-        uint32_t w[E * sizeof(T) / 4];
+        using Words = __attribute__((ext_vector_type(E * sizeof(T) / 4), aligned(sizeof(T)))) uint32_t;
+        Words w;
 #pragma unroll
         for (int i = 0; i < (int)(E * sizeof(T) / 4); ++i) {
             if constexpr (sizeof(T) == 4) {
@@ -183,7 +197,8 @@ __device__ __forceinline__ void store_gradients(T* p, const float (&v)[E], int64
                 w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{v[2 * i], v[2 * i + 1]}), bf16x2));
             }
         }
-        __builtin_memcpy(p, w, sizeof w);
+        if constexpr (PAST) __builtin_nontemporal_store(w, reinterpret_cast<Words*>(p));
+        else *reinterpret_cast<Words*>(p) = w;
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)

@@ -19,7 +19,7 @@ constexpr int kThreads = 256;
 constexpr double kLog2e = 1.4426950408889634;
 
 // ------------------------------------------------------------------ any strides
-// A workgroup for each position, which reads its logits three times: maps with long lists, or of few positions.
+// A workgroup for each position, which reads its logits three times: maps of more than 128 classes with lists of more than 128 places.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void distill_kernel(Distill D) {
     __shared__ float room[kThreads / 64 * 2];
@@ -101,7 +101,7 @@ struct List {
 };
 
 // LPR threads hold a position's logits, CH chunks each, in registers: they are read once.
-template <typename T, int LPR, int CH>
+template <typename T, int LPR, int CH, bool PAST>
 __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_kernel(Distill D) {
     constexpr int E = Logits<T>::E, ROWS = LPR < kThreads ? kThreads / LPR : 1;
     __shared__ float room[LPR > 64 ? LPR / 64 * 3 : 1];
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         c[i].clear();
-        if (i * LPR + lane < last) c[i].load(z + (i * LPR + lane) * E);
+        if (i * LPR + lane < last) c[i].template load<PAST>(z + (i * LPR + lane) * E);
     }
     if (C % E != 0 && last % LPR == lane) {
         Logits<T> end;
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_
             if (live)
 #pragma unroll
                 for (int e = 0; e < E; ++e) v[e] = (sizeof(T) == 4 ? c[i].value(e) : exp2_of((c[i].value(e) - z_max) * D.to_log2)) * per;
-            store_gradients(grad + at, v, D.C - at);
+            store_gradients<PAST>(grad + at, v, D.C - at);
         }
     }
     __syncthreads();                     // the classes of the list are stored over
@@ -196,7 +196,7 @@ constexpr int kSharedClasses = 16384;    // of the shortest rows that several wo
 
 // Rows longer than the registers hold, or too few for the units: `parts` workgroups share a position's classes.  First
 // each takes its part's largest logit and sum.
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(kThreads) void distill_parts_kernel(Distill D, int64_t per_part, Part* parts) {
     constexpr int E = Logits<T>::E, U = 8;
     __shared__ float room[kThreads / 64];
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(kThreads) void distill_parts_kernel(Distill D, int6
     for (int64_t at = c0 + threadIdx.x * E; at < c1; at += U * kThreads * E) {
         Logits<T> c[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) c[u].load(z + at + u * kThreads * E, c1 - at - u * kThreads * E);
+        for (int u = 0; u < U; ++u) c[u].template load<PAST>(z + at + u * kThreads * E, c1 - at - u * kThreads * E);
         float top = own.top;
 #pragma unroll
         for (int u = 0; u < U; ++u) top = c[u].top(top);
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kThreads) void distill_parts_kernel(Distill D, int6
 }
 
 // Then the loss (workgroups 0 of a position) and the gradient of their parts.
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill D, int64_t per_part, const Part* parts, int n_parts,
                                                                   int with_loss) {
     constexpr int E = Logits<T>::E, U = 4;
@@ -279,14 +279,14 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill D, int
     for (int64_t at = c0 + threadIdx.x * E; at < c1; at += U * kThreads * E) {
         Logits<T> c[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) c[u].load(z + at + u * kThreads * E, live ? c1 - at - u * kThreads * E : 0);
+        for (int u = 0; u < U; ++u) c[u].template load<PAST>(z + at + u * kThreads * E, live ? c1 - at - u * kThreads * E : 0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float v[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) v[e] = live ? exp2_of((c[u].value(e) - z_max) * D.to_log2) * per : 0.f;
             const int64_t from = at + u * kThreads * E;
-            if (from < c1) store_gradients(grad + from, v, c1 - from);
+            if (from < c1) store_gradients<PAST>(grad + from, v, c1 - from);
         }
     }
     __syncthreads();                     // the classes of the list are stored over
@@ -301,7 +301,11 @@ __global__ __launch_bounds__(kThreads) void distill_finish_kernel(Distill D, int
 template <typename T, int LPR, int CH>
 hipError_t run_rows(const Distill& D, hipStream_t s) {
     constexpr int ROWS = LPR < kThreads ? kThreads / LPR : 1;
-    distill_rows_kernel<T, LPR, CH><<<dim3((unsigned)ceil_div64(D.M, ROWS)), ROWS * LPR, ROWS * List::bytes(D.k), s>>>(D);
+    // Long rows go around the caches: 4096 of 32768 bfloat16 classes 119 us through them, 105 around.  (Shorter rows' loads share
+    // lines: 1 million of 40 classes 91 us, 113 around.)
+    const bool past = LPR >= kThreads && D.M * D.C * (int64_t)sizeof(T) > kLarge;
+    const auto kern = past ? distill_rows_kernel<T, LPR, CH, (LPR >= kThreads)> : distill_rows_kernel<T, LPR, CH, false>;
+    kern<<<dim3((unsigned)ceil_div64(D.M, ROWS)), ROWS * LPR, ROWS * List::bytes(D.k), s>>>(D);
     return hipGetLastError();
 }
 
@@ -310,18 +314,21 @@ hipError_t run_parts(const Distill& D, Part* parts, hipStream_t s) {
     // enough workgroups for the units, of at least some thousand classes each
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(1024 / D.M, D.C / 4096));
     const int64_t per_part = ceil_div64(ceil_div64(D.C, most), 64) * 64, n = ceil_div64(D.C, per_part);
-    distill_parts_kernel<T><<<dim3((unsigned)n, (unsigned)D.M), kThreads, 0, s>>>(D, per_part, parts);
+    const int64_t bytes = D.M * D.C * (int64_t)sizeof(T);
+    const auto first = bytes > (D.grad ? kNeverCached : kLarge) ? distill_parts_kernel<T, true> : distill_parts_kernel<T, false>;
+    const auto finish = bytes > kLarge ? distill_finish_kernel<T, true> : distill_finish_kernel<T, false>;
+    first<<<dim3((unsigned)n, (unsigned)D.M), kThreads, 0, s>>>(D, per_part, parts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const bool over = D.grad == D.z;     // the losses need all of the logits first
     Distill L = D;
     if (over) L.grad = nullptr;
     if (over || !D.grad) {
-        distill_finish_kernel<T><<<dim3(1, (unsigned)D.M), kThreads, List::bytes(D.k), s>>>(L, D.C, parts, (int)n, 1);
+        finish<<<dim3(1, (unsigned)D.M), kThreads, List::bytes(D.k), s>>>(L, D.C, parts, (int)n, 1);
         e = hipGetLastError();
         if (e != hipSuccess || !D.grad) return e;
     }
-    distill_finish_kernel<T><<<dim3((unsigned)n, (unsigned)D.M), kThreads, List::bytes(D.k), s>>>(D, per_part, parts, (int)n, !over);
+    finish<<<dim3((unsigned)n, (unsigned)D.M), kThreads, List::bytes(D.k), s>>>(D, per_part, parts, (int)n, !over);
     return hipGetLastError();
 }
 
@@ -341,14 +348,18 @@ hipError_t run_distill(const Distill& D, dss_dtype dt, Part* parts, hipStream_t 
     }
     for (int64_t m = 0; m < D.M; m += kSlabTokens) {
         const Distill S = positions(D, dt, m, std::min(D.M - m, kSlabTokens));
-        // as few threads for a row as hold it, and the lists of their workgroup's rows in 48 KB of LDS
+        // As few threads and registers for a row as hold it, and the lists of their workgroup's rows in 48 KB of LDS: what is
+        // left empty is rows that are not on their way.  4096 rows of 40000 bfloat16 classes 148 us on 512 threads, 290 on
+        // 1024; 20000 rows of 10000 156 us in 8 chunks, 187 in 16.
         const int64_t rows = (int64_t)(48 * 1024 / List::bytes(D.k));
         hipError_t e;
         if (D.C <= 4 * 4 * E && rows >= 64) e = run_rows<T, 4, 4>(S, s);
         else if (D.C <= 16 * 4 * E && rows >= 16) e = run_rows<T, 16, 4>(S, s);
         else if (D.C <= 64 * 4 * E && rows >= 4) e = run_rows<T, 64, 4>(S, s);
         else if (D.C <= 256 * 4 * E) e = run_rows<T, 256, 4>(S, s);
+        else if (D.C <= 256 * 8 * E) e = run_rows<T, 256, 8>(S, s);
         else if (D.C <= 256 * 16 * E) e = run_rows<T, 256, 16>(S, s);
+        else if (D.C <= 512 * 16 * E) e = run_rows<T, 512, 16>(S, s);
         else e = run_rows<T, 1024, 16>(S, s);
         if (e != hipSuccess) return e;
     }

@@ -47,7 +47,7 @@ __device__ __forceinline__ void over_classes(int C, F f) {
     for (; c < C; ++c) f(std::integral_constant<int, 1>{}, c);
 }
 
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(64) void distill_columns_kernel(Distill D) {
     extern __shared__ float columns[];
     const int C = (int)D.C, lane = threadIdx.x, k = D.k;
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(64) void distill_columns_kernel(Distill D) {
     over_classes(C, [&](auto n, int c) {
         float v[n];
 #pragma unroll
-        for (int u = 0; u < n; ++u, z += D.cs) v[u] = to_f32(*z);
+        for (int u = 0; u < n; ++u, z += D.cs) v[u] = to_f32(PAST ? __builtin_nontemporal_load(z) : *z);
 #pragma unroll
         for (int u = 0; u < n; ++u) {
             col[(c + u) * 64] = v[u];
@@ -121,7 +121,12 @@ __global__ __launch_bounds__(64) void distill_columns_kernel(Distill D) {
 #pragma unroll
         for (int u = 0; u < n; ++u) v[u] = col[(c + u) * 64];
 #pragma unroll
-        for (int u = 0; u < n; ++u, grad += D.gcs) store_elem(grad, live ? v[u] * per : 0.f);
+        for (int u = 0; u < n; ++u, grad += D.gcs) {
+            T r;
+            store_elem(&r, live ? v[u] * per : 0.f);
+            if constexpr (PAST) __builtin_nontemporal_store(r, grad);
+            else *grad = r;
+        }
     });
 }
 
@@ -144,9 +149,10 @@ struct Tile {
         }
     }
     // The same of the first n positions from p on.
+    template <bool PAST = false>
     __device__ __forceinline__ void load(const T* p, int64_t cs, int64_t c0, int64_t C, int64_t n) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) c[r].load(p + (c0 + r) * cs, c0 + r < C ? n : 0);
+        for (int r = 0; r < 16; ++r) c[r].template load<PAST>(p + (c0 + r) * cs, c0 + r < C ? n : 0);
     }
     __device__ __forceinline__ void raise_into(float (&top)[V]) const {
 #pragma unroll
@@ -330,7 +336,7 @@ __device__ __forceinline__ void take_off(float (&v)[V], const List& lists, const
 // Up to 1024 classes: the tile's logits stay in registers.  Whole tiles only: the last one ends with the last
 // position and writes those from `first` on, which the one before it does not have.  (What it reads of the others
 // may be their gradients already, if these are written over the logits; positions do not mix.)
-template <typename T, int W>
+template <typename T, int W, bool PAST>
 __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(16 / W))) void distill_tile_kernel(Distill D) {
     constexpr int V = Tile<T, W>::V, N = Tile<T, W>::kTokens;
     using List = Lists<T, N>;
@@ -407,7 +413,7 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(16 / W))) 
             }
             take_off(v, lists, marks, c0 + r, l16 * V);
             if (l16 * V >= first) {
-                store_gradients(p, v, V);
+                store_gradients<PAST>(p, v, V);
             } else {
 #pragma unroll
                 for (int j = 0; j < V; ++j)
@@ -423,7 +429,7 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(16 / W))) 
 // part's largest logits and sums.
 constexpr int kPartThreads = 256, kPartSpan = kPartThreads / 16 * 16;
 
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(kPartThreads) void distill_map_parts_kernel(Distill D, int64_t per_part, Part* parts) {
     constexpr int V = Tile<T, 4>::V;
     __shared__ float room[kPartThreads / 64 * 16 * V];
@@ -435,7 +441,7 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_parts_kernel(Distill
     for (int v = 0; v < V; ++v) top[v] = -INFINITY, sum[v] = 0.f;
     for (int64_t c0 = blockIdx.y * per_part; c0 < c1; c0 += kPartSpan) {
         Tile<T, 4> tile;
-        tile.load(z + m, D.cs, c0 + (threadIdx.x >> 4) * 16, c1, D.M - m);
+        tile.template load<PAST>(z + m, D.cs, c0 + (threadIdx.x >> 4) * 16, c1, D.M - m);
         float next[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) next[v] = top[v];
@@ -516,7 +522,7 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_join_kernel(Distill 
 }
 
 // Then the gradient, a part of a tile's classes for a workgroup, a span of them at a time.
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(kPartThreads) void distill_map_gradient_kernel(Distill D, int64_t per_part, Stats stats) {
     constexpr int W = (int)sizeof(T), V = Tile<T, W>::V, N = Tile<T, W>::kTokens;
     using List = Lists<T, N>;
@@ -592,7 +598,7 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_gradient_kernel(Dist
             take_off(v, lists, marks, own + r, (threadIdx.x & 15) * V);
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] = live >> j & 1 ? v[j] : 0.f;
-            store_gradients(grad + m + (c0 + r) * D.gcs, v, D.M - m);
+            store_gradients<PAST>(grad + m + (c0 + r) * D.gcs, v, D.M - m);
         }
         if (span + kPartSpan >= c1) break;
         __syncthreads();
@@ -601,12 +607,18 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_gradient_kernel(Dist
     }
 }
 
+// Whether the gradient goes around the caches: large, and of whole lines, which 16 lanes' stores fill.  198016 positions of 1000
+// bfloat16 classes 235 us, through the caches 263; where lines are shared with other tiles' stores (198025) 404 and 308.
+bool gradient_past(const Distill& D, dss_dtype dt) { return D.grad && outputs_past(D.M, D.C, D.gcs, D.grad, dt); }
+
 template <typename T>
 hipError_t run_columns(const Distill& D, dss_dtype dt, hipStream_t s) {
+    const bool past = (!D.grad || gradient_past(D, dt)) && outputs_past(D.M, D.C, D.cs, D.z, dt);
+    const auto kern = past ? distill_columns_kernel<T, true> : distill_columns_kernel<T, false>;
     // (a launch has fewer than 2^32 threads)
     for (int64_t m = 0; m < D.M; m += (int64_t)1 << 30) {
         const Distill S = positions(D, dt, m, std::min(D.M - m, (int64_t)1 << 30));
-        distill_columns_kernel<T><<<dim3((unsigned)ceil_div64(S.M, 64)), 64, (size_t)D.C * 256, s>>>(S);
+        kern<<<dim3((unsigned)ceil_div64(S.M, 64)), 64, (size_t)D.C * 256, s>>>(S);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -618,13 +630,14 @@ hipError_t run_tiles(const Distill& D, dss_dtype dt, hipStream_t s) {
     constexpr int N = Tile<T, W>::kTokens;
     const int waves = (int)ceil_div64(D.C, 64);
     const size_t lds = std::max(Lists<T, N>::bytes_of_t(D.k) + (size_t)waves * N * 4 + Marks<N>::bytes((int)D.C), Lists<T, N>::bytes(D.k));
-    const hipError_t e = allow_dynamic_lds((const void*)distill_tile_kernel<T, W>, lds);
+    const auto kern = gradient_past(D, dt) ? distill_tile_kernel<T, W, true> : distill_tile_kernel<T, W, false>;
+    const hipError_t e = allow_dynamic_lds((const void*)kern, lds);
     if (e != hipSuccess) return e;
     for (int64_t m = 0; m < D.M;) {
         // (what is left after this launch has a whole tile's positions)
         const int64_t n = D.M - m <= kSlabTokens ? D.M - m : kSlabTokens - N;
         const Distill S = positions(D, dt, m, n);
-        distill_tile_kernel<T, W><<<dim3((unsigned)ceil_div64(n, N)), waves * 64, lds, s>>>(S);
+        kern<<<dim3((unsigned)ceil_div64(n, N)), waves * 64, lds, s>>>(S);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         m += n;
@@ -637,11 +650,14 @@ hipError_t run_map_parts(const Distill& D, dss_dtype dt, Part* parts, hipStream_
     // (the parts' tiles and the gradients', which are half as wide of bfloat16)
     constexpr int N = Tile<T, 4>::kTokens, G = Tile<T, (int)sizeof(T)>::kTokens;
     const size_t lists = Lists<T, kJoined>::bytes(D.k), gradient = Lists<T, G>::bytes_of_t(D.k) + Marks<G>::bytes(kPartSpan);
-    const hipError_t allowed = allow_dynamic_lds((const void*)distill_map_gradient_kernel<T>, gradient);
+    const auto last = gradient_past(D, dt) ? distill_map_gradient_kernel<T, true> : distill_map_gradient_kernel<T, false>;
+    const hipError_t allowed = allow_dynamic_lds((const void*)last, gradient);
     if (allowed != hipSuccess) return allowed;
     const Stats stats = {reinterpret_cast<float*>(parts)};
     parts += kStats * kSlabPositions * 4 / (int)sizeof(Part);
     constexpr int64_t room = kMostParts - kStats * kSlabPositions * 4 / (int)sizeof(Part);
+    const auto first = D.M * D.C * (int64_t)sizeof(T) > (D.grad ? kNeverCached : kLarge) ? distill_map_parts_kernel<T, true>
+                                                                                         : distill_map_parts_kernel<T, false>;
     for (int64_t m = 0; m < D.M; m += kSlabPositions) {
         const Distill S = positions(D, dt, m, std::min(D.M - m, kSlabPositions));
         // enough workgroups for the units, of at least a span of classes each
@@ -649,14 +665,14 @@ hipError_t run_map_parts(const Distill& D, dss_dtype dt, Part* parts, hipStream_
         const int64_t most = std::max<int64_t>(1, std::min({ceil_div64(1024, tiles), ceil_div64(D.C, kPartSpan), room / S.M}));
         const int64_t per_part = ceil_div64(ceil_div64(D.C, most), kPartSpan) * kPartSpan, n = ceil_div64(D.C, per_part);
         const dim3 grid((unsigned)tiles, (unsigned)n);
-        distill_map_parts_kernel<T><<<grid, kPartThreads, 0, s>>>(S, per_part, parts);
+        first<<<grid, kPartThreads, 0, s>>>(S, per_part, parts);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         distill_map_join_kernel<T><<<dim3((unsigned)ceil_div64(S.M, kJoined)), kPartThreads, lists, s>>>(S, parts, (int)n, stats);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (D.grad)
-            distill_map_gradient_kernel<T><<<dim3((unsigned)ceil_div64(S.M, G), (unsigned)n), kPartThreads, gradient, s>>>(S, per_part, stats);
+            last<<<dim3((unsigned)ceil_div64(S.M, G), (unsigned)n), kPartThreads, gradient, s>>>(S, per_part, stats);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -78,7 +78,8 @@ def test_long_lists_of_one_class(M, C, k, layout):
 
 
 @pytest.mark.parametrize("layout", ["rows", "map"])
-@pytest.mark.parametrize("M,C,k", [(70, 64, 8), (70, 500, 8), (70, 2000, 8), (9, 40000, 8), (130, 600, 130)])
+@pytest.mark.parametrize("M,C,k", [(70, 64, 8), (70, 500, 8), (70, 2000, 8), (9, 40000, 8), (130, 600, 130),
+                                   (16384, 1100, 8), (32768, 1300, 40)])
 def test_the_same_call_gives_the_same_bits(M, C, k, layout):
     import torch
     z, top, ids = _inputs(M, C, k, layout, repeat=True)
@@ -114,3 +115,36 @@ def test_largest_and_smallest_temperatures():
                 scale = 2.0 ** -40 if T > 1e10 else 1.0
                 losses, grad = dss.distill(zs, ts, ids, temperature=T, scale=scale)
                 _check(losses, grad, zs, ts, ids, T=T, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,C,layout", [(9000, 4100, "rows"), (4400, 9000, "rows"), (1200, 33000, "rows"), (700, 70_001, "rows"),
+                                        (600, 140_000, "rows"), (1 << 20, 40, "map"), (1 << 18, 200, "map"), (32768, 1100, "map"),
+                                        (70_016, 1030, "map"), ((1 << 20) + 3, 40, "map")])
+def test_calls_around_the_caches(M, C, layout, dtype):
+    """Calls too large for the caches, over their logits too, write nothing else; where one workgroup has all of a position they
+    give the bits of calls that fit the caches."""
+    import torch
+    z, top, ids = _large(M, C, 4, layout, dtype)
+    assert M * C * z.element_size() > 1 << 26
+    losses, grad = dss.distill(z, top, ids, temperature=0.5)
+    few = (1 << 26) // (C * z.element_size()) // 64 * 64
+    alone = C < 1024 if layout == "map" else C < 65536
+    for at in (0, M // 128 * 64, M - few):
+        part = slice(at, at + few)
+        if alone:
+            some, grads = dss.distill(z[part], top[part], ids[part], temperature=0.5)
+            assert torch.equal(some, losses[part]) and torch.equal(grads, grad[part])
+        part = slice(at, at + min(few, 64))
+        _check(losses[part], grad[part], z[part], top[part], ids[part], T=0.5)
+    only, _ = dss.distill(z, top, ids, temperature=0.5, with_grad=False)
+    _check(only[part], None, z[part], top[part], ids[part], T=0.5)
+    rows, cols = (C, M) if layout == "map" else (M, C)
+    buf = torch.full((rows + 2, cols + 64), -77.0, dtype=z.dtype, device="cuda")
+    over = buf[1:rows + 1, 64:]
+    over.copy_(z.t() if layout == "map" else z)
+    over = over.t() if layout == "map" else over
+    again, _ = dss.distill(over, top, ids, temperature=0.5, grad=over)
+    assert torch.equal(again, losses) and torch.equal(over, grad)
+    over.fill_(-77)
+    assert bool((buf == -77).all())
