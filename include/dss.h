@@ -526,8 +526,8 @@ dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t M, int64_t 
  * A block with an infinity or a NaN has the scale NaN and codes 0: its token's
  * outputs are NaN, and no other token's are.  A layer is
  *   y[m][n] = act(sum_b scale[m][b] weight_scale[n][b] sum_{k in b} value[m][k] weight_value[n][k] + bias[n])
- * with the sum in binary32.  Its order depends on the sizes alone: the same call gives the same bits, M
- * tokens in one call and in several may differ in a last place.
+ * with the sum in binary32.  Its order depends on the sizes, types and strides alone: the same call gives the
+ * same bits, M tokens in one call and in several may differ in a last place.
  *
  * Rows of B blocks, of tokens or of weights:
  *   codes   codes[m * codes_stride + k / 2], the even channel in the lower half of its byte.
@@ -601,7 +601,7 @@ typedef struct dss_top_logits {
 #define DSS_DISTILL_WORKSPACE_BYTES (1 << 22)
 
 /* Workspace bytes of dss_distill_tokens on positions of C classes (host only): `map` is nonzero where the
- * positions are adjacent (a channel stride other than 1).  0 for rows of fewer than 16384 classes and maps of at
+ * positions are adjacent (a channel stride other than 1).  0 for rows of at most 32768 classes and maps of at
  * most 128.  Errors: DSS_E_INVALID (C < 1, NULL workspace_bytes). */
 dss_status dss_distill_workspace(int32_t C, int32_t map, int64_t* workspace_bytes);
 

@@ -192,9 +192,9 @@ __global__ __launch_bounds__(LPR < kThreads ? kThreads : LPR) void distill_rows_
     }
 }
 
-constexpr int kSharedClasses = 16384;    // of the shortest rows that several workgroups share
+constexpr int kOwnClasses = 32768;       // of rows that never have several workgroups
 
-// Rows longer than the registers hold, or too few for the units: `parts` workgroups share a position's classes.  First
+// Rows longer than the registers hold, or too long for one workgroup of few: `parts` workgroups share a position's classes.  First
 // each takes its part's largest logit and sum.
 template <typename T, bool PAST>
 __global__ __launch_bounds__(kThreads) void distill_parts_kernel(Distill D, int64_t per_part, Part* parts) {
@@ -335,9 +335,16 @@ hipError_t run_parts(const Distill& D, Part* parts, hipStream_t s) {
 template <typename T>
 hipError_t run_distill(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
     constexpr int E = Logits<T>::E;
-    // (a call without workspace comes to neither: rows of fewer than kSharedClasses)
-    const bool long_rows = D.C > 1024 * 16 * E || (!D.grad && D.C > 256 * 16 * E);
-    if (long_rows || (D.M < 128 && D.C >= kSharedClasses)) {
+    // Several workgroups for a row beyond what one holds in registers; for the losses alone from half of that, and where few
+    // rows leave units empty.  In microseconds for one workgroup and for several, with the gradient:
+    //                 32768 binary32 classes   60000 bfloat16    120000 bfloat16
+    //   8 rows               9 / 12               13 / 12            20 / 12
+    //   60 rows              9 / 13               14 / 17            22 / 18
+    //   120 rows            11 / 17               16 / 18            24 / 23
+    // and the losses alone of 4000 rows: 81 / 91, 85 / 91 and 243 / 159.
+    const int64_t one = 512 * 16 * E, most = D.grad ? (D.M < 128 ? 65536 : 2 * one) : one;
+    static_assert(512 * 16 * E >= kOwnClasses);
+    if (D.C > most) {
         // (a launch has 65535 workgroups along y)
         const int64_t slab = 4096;
         for (int64_t m = 0; m < D.M; m += slab) {
@@ -404,7 +411,7 @@ Distill positions(const Distill& D, dss_dtype dt, int64_t m, int64_t n) {
 
 namespace dss {
 static int64_t distill_workspace(int32_t C, bool map) {
-    return C >= (map ? kColumns + 1 : kSharedClasses) ? DSS_DISTILL_WORKSPACE_BYTES : 0;
+    return C > (map ? kColumns : kOwnClasses) ? DSS_DISTILL_WORKSPACE_BYTES : 0;
 }
 }  // namespace dss
 

@@ -21,7 +21,7 @@ def _distill(z=PTR, dt=0, M=4, C=10, ts=10, cs=1, top=True, weights=PTR, T=1.0, 
                                         VP(losses), VP(grad), gts, gcs, VP(room), bytes, None)
 
 
-LONG = dict(C=16384, ts=16384, gts=16384)              # sizes that need a workspace
+LONG = dict(C=32769, ts=32769, gts=32769)              # sizes that need a workspace
 WIDE = dict(C=129, ts=1, cs=4, gts=1, gcs=4)
 
 
@@ -49,7 +49,7 @@ def test_refusals(status, kw):
 def test_workspace_query():
     need = ctypes.c_int64()
     q = dss.lib().dss_distill_workspace
-    for C, planar, none in ((1, 0, True), (16383, 0, True), (16384, 0, False), (128, 1, True), (129, 1, False),
+    for C, planar, none in ((1, 0, True), (32768, 0, True), (32769, 0, False), (128, 1, True), (129, 1, False),
                             (2 ** 31 - 1, 0, False), (2 ** 31 - 1, 1, False)):
         assert q(C, planar, ctypes.byref(need)) == OK and (need.value == 0) == none and 0 <= need.value <= 1 << 22
         assert dss.distill_workspace(C, bool(planar)) == need.value

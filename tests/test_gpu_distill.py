@@ -178,7 +178,7 @@ def test_the_gradient_over_the_logits(M, C, k, dtype, layout):
 
 
 @pytest.mark.parametrize("layout", ["rows", "map"])
-@pytest.mark.parametrize("M,C,k", [(1, 5, 2), (67, 64, 8), (130, 500, 9), (5, 30000, 20)])
+@pytest.mark.parametrize("M,C,k", [(1, 5, 2), (67, 64, 8), (130, 500, 9), (5, 30000, 20), (5, 140000, 20)])
 def test_gradients_and_lists_in_wider_buffers(M, C, k, layout):
     """Strides of every operand; beside the gradient nothing is written."""
     import torch
@@ -251,7 +251,7 @@ def test_no_positions():
 def test_other_stream():
     import torch
     side = torch.cuda.Stream()
-    for M, C in ((100, 40), (3, 50000)):
+    for M, C in ((100, 40), (3, 50000), (3, 140000)):
         z, top, ids = _inputs(M, C, 7)
         ref = dss.distill(z, top, ids)
         side.wait_stream(torch.cuda.current_stream())
@@ -312,7 +312,7 @@ def test_binding_refusals():
                          (lambda: dss.distill(z, top, ids, grad=torch.empty((10, 6), device="cuda").t()), 1),
                          (lambda: dss.distill(z[:1].expand(6, 10), top, ids, grad=z[:1].expand(6, 10)), 1),
                          (lambda: dss.distill(z[::2, ::2], top[::2], ids[::2]), 3),
-                         (lambda: dss.distill(*_inputs(2, 20000, 3), workspace=torch.empty(100, dtype=torch.uint8, device="cuda")), 2)):
+                         (lambda: dss.distill(*_inputs(2, 40000, 3), workspace=torch.empty(100, dtype=torch.uint8, device="cuda")), 2)):
         with pytest.raises(dss.DssError) as e:
             call()
         assert e.value.status == status

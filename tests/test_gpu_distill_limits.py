@@ -57,7 +57,7 @@ def test_calls_of_several_launches(M, C, k, layout, dtype):
 @pytest.mark.parametrize("M,C,k", [(70, c, k) for c in (63, 64, 65, 127, 128, 129, 255, 256, 257, 512, 513, 1023, 1024, 1025)
                                    for k in (1, 8, 9)] +
                          [(5, c, 20) for c in (2048, 2049, 4096, 4097, 8192, 8193, 16383, 16384, 16385, 32768, 32769, 65536,
-                                               65537)] + [(130, 16384, 3), (127, 16384, 3), (200, 300, 128), (200, 300, 129),
+                                               65537, 131072, 131073)] + [(130, 65537, 3), (127, 65537, 3), (130, 16384, 3), (200, 300, 128), (200, 300, 129),
                                                           (31, 200, 4), (32, 200, 4), (63, 200, 4), (64, 200, 4)])
 def test_kernels_borders(M, C, k, layout, dtype):
     z, top, ids = _inputs(M, C, min(k, C), layout, dtype, repeat=k > 100)
@@ -78,7 +78,7 @@ def test_long_lists_of_one_class(M, C, k, layout):
 
 
 @pytest.mark.parametrize("layout", ["rows", "map"])
-@pytest.mark.parametrize("M,C,k", [(70, 64, 8), (70, 500, 8), (70, 2000, 8), (9, 40000, 8), (130, 600, 130),
+@pytest.mark.parametrize("M,C,k", [(70, 64, 8), (70, 500, 8), (70, 2000, 8), (9, 40000, 8), (9, 70000, 8), (130, 600, 130),
                                    (16384, 1100, 8), (32768, 1300, 40)])
 def test_the_same_call_gives_the_same_bits(M, C, k, layout):
     import torch
@@ -92,7 +92,7 @@ def test_the_same_call_gives_the_same_bits(M, C, k, layout):
 def test_two_streams_with_workspaces_of_their_own():
     import torch
     sides = [torch.cuda.Stream() for _ in range(2)]
-    cases = [_inputs(40, 30000, 9, "rows", seed=1), _inputs(50, 3000, 9, "map", seed=2)]
+    cases = [_inputs(40, 70000, 9, "rows", seed=1), _inputs(50, 3000, 9, "map", seed=2)]
     want = [dss.distill(*c) for c in cases]
     torch.cuda.synchronize()
     got = [[], []]
