@@ -23,12 +23,13 @@ constexpr double kLog2e = 1.4426950408889634;
 
 // ------------------------------------------------------------------ any strides
 // A workgroup for each position, which reads its logits three times: maps of more than 128 classes with lists of more than 128 places.
+// (Neighbours, which share lines, on one XCD: 20000 positions of 1000 classes 397 us for 932.)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void distill_kernel(Distill D) {
     __shared__ float room[kThreads / 64 * 2];
     __shared__ float p[kMostTop];
     __shared__ int ids[kMostTop];
-    const int64_t m = blockIdx.x;
+    const int64_t m = xcd_order(blockIdx.x, gridDim.x);
     const T* z = static_cast<const T*>(D.z) + m * D.ts;
     T* grad = static_cast<T*>(D.grad) + m * D.gts;
     const float weight = D.weights ? D.weights[m] : 1.f;

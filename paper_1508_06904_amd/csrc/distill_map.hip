@@ -4,7 +4,7 @@
 // registers (up to 1024 classes); of more classes they are read twice.
 //
 // 1.88 million positions of 64 binary32 classes: 298 us, 3.6 TB/s with the lists, where no channel's positions are whole lines, and 243
-// where they are; 198025 of 1000 bfloat16 classes 304 us (2.7 TB/s), 198016 235 (3.5); 20480 of 5000 binary32 classes 266 us.
+// where they are; 198025 of 1000 bfloat16 classes 304 us (2.7 TB/s), 198016 235 (3.5); 20480 of 5000 binary32 classes 277 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -323,6 +323,16 @@ struct Marks {
     }
 };
 
+// What the places of a part's listed classes take off their gradients.
+template <int N>
+struct Shares {
+    float* at;
+    int k;
+
+    static __host__ __device__ size_t bytes(int k) { return (size_t)N * (k | 1) * 4; }
+    __device__ __forceinline__ float& t(int j, int n) const { return at[n * (k | 1) + j]; }
+};
+
 // Takes off V adjacent positions' gradients of a class what its places take.
 template <typename List, int N, int V>
 __device__ __forceinline__ void take_off(float (&v)[V], const List& lists, const Marks<N>& marks, int c, int n) {
@@ -432,17 +442,25 @@ __global__ __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(16 / W))) 
 // part's largest logits and sums.
 constexpr int kPartThreads = 256, kPartSpan = kPartThreads / 16 * 16;
 
+// The workgroup's tile and part: neighbouring tiles of a part, which may share lines, on one XCD (20481 positions of 5000 binary32
+// classes 330 us for 378; where they do not share any 277 for 267).
+__device__ __forceinline__ int2 tile_and_part() {
+    const int id = (int)xcd_order(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
+    return {id % (int)gridDim.x, id / (int)gridDim.x};
+}
+
 template <typename T, bool PAST>
 __global__ __launch_bounds__(kPartThreads) void distill_map_parts_kernel(Distill D, int64_t per_part, Part* parts) {
     constexpr int V = Tile<T, 4>::V;
     __shared__ float room[kPartThreads / 64 * 16 * V];
-    const int64_t m = (int64_t)blockIdx.x * Tile<T, 4>::kTokens + (threadIdx.x & 15) * V;
-    const int64_t c1 = min((blockIdx.y + 1) * per_part, D.C);
+    const int2 own = tile_and_part();
+    const int64_t m = (int64_t)own.x * Tile<T, 4>::kTokens + (threadIdx.x & 15) * V;
+    const int64_t c1 = min((own.y + 1) * per_part, D.C);
     const T* z = static_cast<const T*>(D.z);
     float top[V], sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) top[v] = -INFINITY, sum[v] = 0.f;
-    for (int64_t c0 = blockIdx.y * per_part; c0 < c1; c0 += kPartSpan) {
+    for (int64_t c0 = own.y * per_part; c0 < c1; c0 += kPartSpan) {
         Tile<T, 4> tile;
         tile.template load<PAST>(z + m, D.cs, c0 + (threadIdx.x >> 4) * 16, c1, D.M - m);
         float next[V];
@@ -471,7 +489,7 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_parts_kernel(Distill
     if (threadIdx.x < 16)
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (m + v < D.M) parts[(m + v) * gridDim.y + blockIdx.y] = {all[v], sum[v]};
+            if (m + v < D.M) parts[(m + v) * gridDim.y + own.y] = {all[v], sum[v]};
 }
 
 // What the gradients of a slab's positions are made of, one array after the other.
@@ -528,12 +546,12 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_join_kernel(Distill 
 template <typename T, bool PAST>
 __global__ __launch_bounds__(kPartThreads) void distill_map_gradient_kernel(Distill D, int64_t per_part, Stats stats) {
     constexpr int W = (int)sizeof(T), V = Tile<T, W>::V, N = Tile<T, W>::kTokens;
-    using List = Lists<T, N>;
     extern __shared__ __align__(16) char lds[];
-    const List lists = {reinterpret_cast<float*>(lds), D.k};
-    const Marks<N> marks = {reinterpret_cast<uint8_t*>(lds + List::bytes_of_t(D.k))};
-    const int64_t m0 = (int64_t)blockIdx.x * N, m = m0 + (threadIdx.x & 15) * V;
-    const int64_t c_from = blockIdx.y * per_part, c1 = min(c_from + per_part, D.C);
+    const Shares<N> shares = {reinterpret_cast<float*>(lds), D.k};
+    const Marks<N> marks = {reinterpret_cast<uint8_t*>(lds + Shares<N>::bytes(D.k))};
+    const int2 place = tile_and_part();
+    const int64_t m0 = (int64_t)place.x * N, m = m0 + (threadIdx.x & 15) * V;
+    const int64_t c_from = place.y * per_part, c1 = min(c_from + per_part, D.C);
     const T* z = static_cast<const T*>(D.z);
     T* grad = static_cast<T*>(D.grad);
     marks.clear(kPartSpan);
@@ -563,8 +581,7 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_gradient_kernel(Dist
                     else of_class += share(o);
                 }
             if (!first) continue;
-            lists.id(j, n) = c[u];
-            lists.t(j, n) = stats.factor(p) * of_class;
+            shares.t(j, n) = stats.factor(p) * of_class;
             mine |= 1ull << (turn + u);
         }
     }
@@ -572,7 +589,7 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_gradient_kernel(Dist
     auto mark = [&](int64_t c0, bool set) {
         for (uint64_t left = mine; left; left &= left - 1) {
             const int i = (int)(__ffsll((long long)left) - 1) * kPartThreads + threadIdx.x;
-            const int64_t c = lists.id(i / N, i % N) - c0;
+            const int64_t c = class_of(D, m0 + i % N, i / N) - c0;
             if (c >= 0 && c < kPartSpan) *marks.of((int)c, i % N) = (uint8_t)(set ? i / N + 1 : 0);
         }
     };
@@ -598,7 +615,7 @@ __global__ __launch_bounds__(kPartThreads) void distill_map_gradient_kernel(Dist
             float v[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] = exp2_of((tile.c[r].value(j) - top[j]) * D.to_log2) * per[j];
-            take_off(v, lists, marks, own + r, (threadIdx.x & 15) * V);
+            take_off(v, shares, marks, own + r, (threadIdx.x & 15) * V);
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] = live >> j & 1 ? v[j] : 0.f;
             store_gradients<PAST>(grad + m + (c0 + r) * D.gcs, v, D.M - m);
@@ -652,7 +669,7 @@ template <typename T>
 hipError_t run_map_parts(const Distill& D, dss_dtype dt, Part* parts, hipStream_t s) {
     // (the parts' tiles and the gradients', which are half as wide of bfloat16)
     constexpr int N = Tile<T, 4>::kTokens, G = Tile<T, (int)sizeof(T)>::kTokens;
-    const size_t lists = Lists<T, kJoined>::bytes(D.k), gradient = Lists<T, G>::bytes_of_t(D.k) + Marks<G>::bytes(kPartSpan);
+    const size_t lists = Lists<T, kJoined>::bytes(D.k), gradient = Shares<G>::bytes(D.k) + Marks<G>::bytes(kPartSpan);
     const auto last = gradient_past(D, dt) ? distill_map_gradient_kernel<T, true> : distill_map_gradient_kernel<T, false>;
     const hipError_t allowed = allow_dynamic_lds((const void*)last, gradient);
     if (allowed != hipSuccess) return allowed;
