@@ -922,6 +922,14 @@ def matmul_mx4(codes, scales, weight, weight_scales, bias=None, act="none", out=
     return out
 
 
+@functools.lru_cache(maxsize=256)
+def _blocks_workspace(tokens, outputs, channels, source):
+    """Workspace bytes of linear_mx4.  source: dss_token_source."""
+    need = ctypes.c_int64()
+    _check(lib().dss_blocks_workspace(tokens, outputs, channels, source, need), "dss_blocks_workspace")
+    return need.value
+
+
 def linear_mx4(x, weight, weight_scales, bias=None, act="none", out=None, out_dtype=None, planar=False, workspace=None,
                stream=None):
     """matmul_mx4 on float32 or bfloat16 tokens x [M][K], given as for quantize_tokens: codes them as quantize_mx4 does
@@ -935,9 +943,7 @@ def linear_mx4(x, weight, weight_scales, bias=None, act="none", out=None, out_dt
     if workspace is not None:
         room, size = _room(workspace, dev)
     else:
-        need = ctypes.c_int64()
-        _check(lib().dss_blocks_workspace(M, N, K, 1 if ks != 1 and K > 1 else 0, need), "dss_blocks_workspace")
-        size = need.value
+        size = _blocks_workspace(M, N, K, 1 if ks != 1 and K > 1 else 0)
         if size:
             workspace = _empty(size, torch.uint8, stream)
         room = workspace.data_ptr() if size else None
