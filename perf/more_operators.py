@@ -288,8 +288,7 @@ def run(state):
             "planar": case["layout"] == "map"}
     if case["op"] == "linear":
         return dss.linear_mx4(state["x"], weight, weight_scales, **more)
-    codes, scales = state["x"]  # (a map's tokens' codes may lie across: their bytes have to be adjacent)
-    return dss.matmul_mx4(codes.contiguous(), scales, weight, weight_scales, **more)
+    return dss.matmul_mx4(*state["x"], weight, weight_scales, **more)
 
 
 # ---------------------------------------------------------------------------- work
