@@ -907,12 +907,25 @@ def _weight_mx4(weight, weight_scales, blocks, dev):
     return rows, N
 
 
+def _rows_of_codes(codes, dev, stream):
+    """codes [M][16 B], with their bytes adjacent: a copy, on the call's stream, where they are not."""
+    import torch
+    if not isinstance(codes, torch.Tensor) or codes.dtype != torch.uint8 or codes.dim() != 2 or codes.get_device() != dev or \
+            codes.stride(1) == 1 or not codes.numel():
+        return codes
+    rows = _empty(codes.shape, torch.uint8, stream)
+    with torch.cuda.stream(stream):                     # (None: the current one)
+        return rows.copy_(codes)
+
+
 def matmul_mx4(codes, scales, weight, weight_scales, bias=None, act="none", out=None, out_dtype=None, planar=False,
                stream=None):
     """A fully connected layer on tokens in 4 bits (quantize_mx4's codes and scales) with weights in 4 bits (the same
     of a matrix [N][K]):  y[m][n] = act(sum_k x[m][k] w[n][k] + bias[n])  of the values that the codes stand for, summed in
-    binary32.  act, out, out_dtype, planar and what is returned are as matmul_i8's."""
+    binary32.  Tokens' codes whose bytes are not adjacent (packed by elementwise operations on a map they lie across) are
+    copied into rows first.  act, out, out_dtype, planar and what is returned are as matmul_i8's."""
     dev, handle = _launch(stream)
+    codes = _rows_of_codes(codes, dev, stream)
     rows, M, B = _check_mx4(codes, scales, "tokens", None, dev)
     if B > _MOST // _BLOCK + 1:
         raise ValueError("tokens have %d blocks, more than %d" % (B, _MOST // _BLOCK + 1))
