@@ -42,7 +42,8 @@ struct Held {
 template <typename T>
 __device__ __forceinline__ void hold_values(const Mx4Values& X, int M, int B, uint8_t* codes, int pitch, uint8_t* scales, int scale_pitch) {
     const int64_t K = X.channels;
-    if (X.channel_stride == 1) {
+    // (one channel alone has any stride, and its tokens theirs; else those of a map are adjacent)
+    if (X.channel_stride == 1 || K == 1) {
         // four lanes for a block, with the loads of U of them under way
         constexpr int U = 4;
         const int quarters = M * B * 4, lane4 = threadIdx.x & 3;

@@ -4,7 +4,7 @@ import pytest
 
 from oracle import mx4
 from paper_1508_06904_amd import dss
-from tests.test_gpu_mx4 import _check_layer, _coded, _dev
+from tests.test_gpu_mx4 import _check_layer, _coded, _dev, _np
 
 pytestmark = pytest.mark.gpu
 
@@ -77,3 +77,28 @@ def test_other_codes_are_refused_as_before():
             dss.matmul_mx4(c, s, w, ws)
     with pytest.raises(ValueError):
         dss.matmul_mx4(codes, scales, w.t().contiguous().t(), ws)
+
+
+# ---------------------------------------------------------------------------- one channel
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [1, 2, 3, 7, 15, 16, 17, 40, 300])
+def test_layers_of_one_channel_at_any_strides(M, dtype):
+    """With one channel any two strides are allowed: every second window of a map, one token for all, tokens far apart."""
+    import torch
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    buf = torch.from_numpy(np.random.default_rng(M).standard_normal(9 * M + 20).astype(np.float32)).to("cuda").to(dt)
+    weight = _coded(33, 1, 4)
+    w, ws = map(_dev, weight)
+    w8, ws8 = dss.quantize_tokens(_dev(mx4.values(*weight, 1).astype(np.float32)))
+    every_second = buf[:2 * M][None][:, ::2].t()
+    assert M == 1 or every_second.stride()[0] == 2
+    for x in (every_second, buf.as_strided((M, 1), (0, 7)), buf.as_strided((M, 1), (9, 3)), buf.as_strided((M, 1), (3, 0)),
+              buf.as_strided((M, 1), (5, 1)), buf.as_strided((M, 1), (1, 4))):
+        for planar in (False, True):
+            y = dss.linear_mx4(x, w, ws, planar=planar)
+            _check_layer(y.t() if planar else y, mx4.values(*mx4.quantize(_np(x)), 1), mx4.values(*weight, 1))
+            two = dss.matmul_mx4(*dss.quantize_mx4(x), w, ws, planar=planar)
+            assert torch.equal(y, two)
+            y = dss.linear_i8(x, w8, ws8, planar=planar)
+            assert torch.equal(y, dss.linear_i8(x.contiguous(), w8, ws8, planar=planar))
