@@ -624,8 +624,8 @@ dss_status dss_distill_workspace(int32_t C, int32_t map, int64_t* workspace_byte
  *                  The logits themselves, with their strides, may be the gradient; no other overlap is allowed
  *   workspace      device scratch of dss_distill_workspace bytes (256-byte aligned); may be NULL where these are 0
  * A position of weight 0, or without a place whose logit is above -infinity, has loss 0 and gradient 0,
- * whatever its logits.  At any other one infinities and NaN follow the formulas (a
- * place of logit -infinity adds 0), and a class of C or more makes loss and gradient NaN.
+ * whatever its logits.  At any other one infinities and NaN follow the formulas: a place of
+ * logit -infinity adds 0, whatever its class, and any other one of a class of C or more makes loss and gradient NaN.
  * M = 0 does nothing.  Errors: DSS_E_INVALID (NULL or misaligned pointers, sizes or strides out of
  * range, a temperature that is not above 0, no finite numbers), DSS_E_UNSUPPORTED (dtypes, id_bytes,
  * temperatures beyond the range, no stride of 1), DSS_E_SHAPE (workspace too small), DSS_E_HIP. */

@@ -22,9 +22,10 @@ def distill(z, top, ids, T=1.0, scale=1.0, weights=None):
     with np.errstate(all="ignore"):
         for m in range(M):
             w = 1.0 if weights is None else float(weights[m])
-            used = np.asarray(ids[m]) >= 0
+            # a place of logit -infinity adds 0, whatever its class
+            used = (np.asarray(ids[m]) >= 0) & (np.asarray(top[m], dtype=np.float64) != -np.inf)
             t, i = np.asarray(top[m], dtype=np.float64)[used] / T, np.asarray(ids[m])[used]
-            if w == 0 or not np.any((t > -np.inf) | np.isnan(t) | (i >= C)):
+            if w == 0 or not used.any():
                 continue
             if np.any(i >= C):
                 losses[m], grad[m] = np.nan, np.nan

@@ -71,8 +71,9 @@ struct Place {
     int id;
     float t, z;
 
-    // 3: a class that there is not, 1: a place that counts (a NaN does), 0: one that does not.
-    __device__ __forceinline__ float state(const Distill& D) const { return id >= (int)D.C ? 3.f : t != -INFINITY ? 1.f : 0.f; }
+    // 0: a place that does not count (of logit -infinity, whatever its class), 3: of a class that there is not, 1: any
+    // other one (a NaN counts).
+    __device__ __forceinline__ float state(const Distill& D) const { return t == -INFINITY ? 0.f : id >= (int)D.C ? 3.f : 1.f; }
 };
 template <typename T>
 __device__ __forceinline__ Place place_of(const Distill& D, int64_t m, int j, const T* z) {
