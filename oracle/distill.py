@@ -57,9 +57,10 @@ def error_bound(z, top, ids, T=1.0, scale=1.0, weights=None):
 
     def share(v):
         d = np.abs(v - np.max(v)) / T
-        p = np.exp(_log_softmax(v / T))
+        log_p = _log_softmax(v / T)
+        p = np.exp(log_p)
         of_sum = min(v.size, 1024) + v.size / 256 + 16 + np.sum(p * (3 * d + 2))
-        return p, d, u * of_sum, u * (3 * d + 2 + 2)
+        return p, log_p, d, u * of_sum, u * (3 * d + 2 + 2)
 
     for m in range(M):
         w = abs(scale) * (1.0 if weights is None else abs(float(weights[m])))
@@ -68,9 +69,9 @@ def error_bound(z, top, ids, T=1.0, scale=1.0, weights=None):
         if w == 0 or not np.any(t > -np.inf):
             continue
         t, i = t[t > -np.inf], i[t > -np.inf]
-        p, dt, sum_p, one_p = share(t)
-        r, dz, sum_r, one_r = share(z[m])
-        size = np.abs(np.log(p) - np.log(r[i]))
+        p, log_p, dt, sum_p, one_p = share(t)
+        r, log_r, dz, sum_r, one_r = share(z[m])
+        size = np.abs(log_p - log_r[i])      # (r itself may be 0 in 64 bits)
         logs = abs(np.log(np.sum(np.exp(-dt)))) + abs(np.log(np.sum(np.exp(-dz))))
         off = 4 * u * (dt + dz[i]) + sum_p + sum_r + 2 * u * logs + 2 * u * size
         losses[m] = w * T * T * np.sum(p * (size * (sum_p + one_p + (t.size + 8) * u) + off) + small * size)

@@ -52,3 +52,20 @@ def test_a_place_of_minus_infinity_adds_nothing_whatever_its_class(M, C, k, dtyp
     want, wgrad = oracle.distill(_np(some), _np(top), ids.cpu().numpy(), 1.5)
     assert np.array_equal(np.isnan(want), _np(torch.isnan(losses)) != 0)
     assert np.array_equal(np.isnan(wgrad), _np(torch.isnan(grad)) != 0)
+
+
+# ---------------------------------------------------------------------------- classes far below the largest logit
+
+@pytest.mark.parametrize("layout", ["rows", "map"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,C,k", [(70, 40, 6), (70, 300, 6), (70, 300, 130), (70, 3000, 6), (3, 20000, 6), (3, 70001, 6), (3, 140000, 6)])
+@pytest.mark.parametrize("spread", [100.0, 1000.0, 1e30])
+def test_losses_of_classes_far_below(M, C, k, dtype, layout, spread):
+    z, top, ids = _inputs(M, C, k, layout, dtype, spread=spread)
+    for T in (1.0, 4.0):
+        losses, grad = dss.distill(z, top, ids, temperature=T)
+        want, _ = oracle.distill(_np(z), _np(top), ids.cpu().numpy(), T)
+        bound, gbound = oracle.error_bound(_np(z), _np(top), ids.cpu().numpy(), T)
+        assert np.isfinite(want).all() and np.isfinite(bound).all() and np.isfinite(gbound).all()
+        assert (bound <= 1e-3 * (1 + np.abs(want))).all()
+        _check(losses, grad, z, top, ids, T=T)
