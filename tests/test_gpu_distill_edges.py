@@ -5,9 +5,11 @@ import pytest
 
 from oracle import distill as oracle
 from paper_1508_06904_amd import dss
-from tests.test_gpu_distill import _check, _inputs, _np
+from tests.test_gpu_distill import _check, _dev, _inputs, _np
 
 pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -18,6 +20,50 @@ def _gpu():
     yield
     torch.cuda.synchronize()
     torch.cuda.empty_cache()
+
+
+# ---------------------------------------------------------------------------- sums of few classes and of many places
+# Maps of up to 128 classes. Their sums have one term of 1 (of each 32) and others a little under u = 2^-24, half a last place
+# below 1's next number: one after the other, each of them would be rounded away.
+
+S = -16.643                              # exp(S) = 0.993 u
+
+
+@pytest.mark.parametrize("C", [32, 64, 96, 128])
+def test_the_classes_sum_keeps_small_terms(C):
+    """r's sum is C / 32 (1 + 31 exp(S)).  Adding 32 terms by halves and C / 32 such sums one after the other rounds 5 + C / 32 - 1
+    times, each by at most u of the sum; the logarithm is within 2 u of its value; exp(S) is off by less than 60 u of
+    itself. The loss, log sum, has no other rounding (p = 1, the difference is 0): 5 + 3 + 2 log 4 + 1 < 12 u. The gradient of
+    an unlisted class of logit 0 is 1 / sum, a division and a product more: 5 + 3 + 2 + 1 < 12 u of it."""
+    z = np.full((70, C), S, dtype=np.float32)
+    z[:, ::32] = 0
+    top, ids = np.zeros((70, 1), dtype=np.float32), np.zeros((70, 1), dtype=np.int64)
+    losses, grad = dss.distill(_dev(z.T.copy()).t(), _dev(top), _dev(ids))
+    want, wgrad = oracle.distill(z, top, ids)
+    assert np.abs(_np(losses) - want).max() <= 12 * U, np.abs(_np(losses) - want).max() / U
+    if C > 32:
+        off = np.abs(_np(grad)[:, 32] / wgrad[:, 32] - 1)
+        assert off.max() <= 12 * U, off.max() / U
+
+
+@pytest.mark.parametrize("k", [30, 100, 128, 600, 1024])
+def test_a_lists_sum_keeps_small_terms(k):
+    """Two classes of equal logits, the first listed with weight 1 and the other one k - 1 times with exp(S): with e = (k - 1) exp(S),
+    the loss is log 2 - log(1 + e) + e S / (1 + e). Places are added 8 by halves, 8 such sums one after the other, and then these:
+    d = 3 + min(7, k / 8) + k / 64 roundings, each by at most u of the sum, in sum_p and in the sum of p, whose rounding counts log 2 times;
+    p rounds 3 times more, and the two logarithms by 2 u of log 2 and of e. Beside (d + 0.7 (d + 3) + 2 + 3) u there are
+    only terms of e u. Without them the loss would be off by e, more than that."""
+    top = np.full((70, k), S, dtype=np.float32)
+    top[:, 0] = 0
+    ids = np.ones((70, k), dtype=np.int64)
+    ids[:, 0] = 0
+    z = np.zeros((70, 2), dtype=np.float32)
+    losses, _ = dss.distill(_dev(z.T.copy()).t(), _dev(top), _dev(ids))
+    want, _ = oracle.distill(z, top, ids)
+    d = 3 + min(7, k // 8) + k // 64
+    bound = (d + 0.7 * (d + 3) + 5) * U
+    assert (k - 1) * np.exp(S) > bound
+    assert np.abs(_np(losses) - want).max() <= bound, (np.abs(_np(losses) - want).max() / U, bound / U)
 
 
 # ---------------------------------------------------------------------------- places of logit -infinity
