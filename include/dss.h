@@ -526,8 +526,9 @@ dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t M, int64_t 
  * A block with an infinity or a NaN has the scale NaN and codes 0: its token's
  * outputs are NaN, and no other token's are.  A layer is
  *   y[m][n] = act(sum_b scale[m][b] weight_scale[n][b] sum_{k in b} value[m][k] weight_value[n][k] + bias[n])
- * with the sum in binary32.  Its order depends on the sizes, types and strides alone: the same call gives the
- * same bits, M tokens in one call and in several may differ in a last place.
+ * with the sum in binary32: sums below 2^-126 keep binary32's subnormal places, and one that leaves its range, on
+ * the way to its end too, is infinite (NaN where parts of both signs are).  Its order depends on the sizes, types and
+ * strides alone: the same call gives the same bits, M tokens in one call and in several may differ in a last place.
  *
  * Rows of B blocks, of tokens or of weights:
  *   codes   codes[m * codes_stride + k / 2], the even channel in the lower half of its byte.
