@@ -115,3 +115,26 @@ def test_losses_of_classes_far_below(M, C, k, dtype, layout, spread):
         assert np.isfinite(want).all() and np.isfinite(bound).all() and np.isfinite(gbound).all()
         assert (bound <= 1e-3 * (1 + np.abs(want))).all()
         _check(losses, grad, z, top, ids, T=T)
+
+
+# ---------------------------------------------------------------------------- the gradient over the logits
+
+@pytest.mark.parametrize("layout", ["rows", "map"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,C,k", [(65, 7, 3), (67, 64, 8), (130, 500, 9), (40, 300, 130), (130, 2500, 9), (5, 30000, 20), (3, 140001, 20)])
+def test_beside_logits_that_their_gradient_is_written_over_nothing_changes(M, C, k, dtype, layout):
+    import torch
+    z, top, ids = _inputs(M, C, k, layout, dtype)
+    want, wgrad = dss.distill(z, top, ids, temperature=1.5)
+    rows, cols = (C, M) if layout == "map" else (M, C)
+    wide = torch.full((rows + 2, cols + 5), -77.0, dtype=z.dtype, device="cuda")
+    inner = wide[1:rows + 1, 3:3 + cols]
+    over = inner.t() if layout == "map" else inner
+    over.copy_(z)
+    losses, grad = dss.distill(over, top, ids, temperature=1.5, grad=over)
+    assert grad is over
+    _check(losses, grad, z, top, ids, T=1.5)
+    bound, gbound = oracle.error_bound(_np(z), _np(top), ids.cpu().numpy(), 1.5)
+    assert (np.abs(_np(losses) - _np(want)) <= 2 * bound).all()
+    inner.fill_(-77)
+    assert bool((wide == -77).all())
