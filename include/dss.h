@@ -522,7 +522,7 @@ dss_status dss_linear_tokens(const void* x, dss_dtype dtype, int64_t M, int64_t 
  * has a power of two for a scale and its elements are 4-bit codes (OCP Microscaling Formats v1.0, MXFP4):
  *   scale = 2^e,  e = floor(log2(max |x|)) - 2, at least -127 (and -127 for a block of zeros),
  *   code  = the number of the nearest value to |x| / scale in {0, 0.5, 1, 1.5, 2, 3, 4, 6}, counted
- *           from 0, ties to the even number, above 6 the last one; plus 8 where x is negative.
+ *           from 0, ties to the even number, above 6 the last one; plus 8 where x's sign bit is set (-0 too).
  * A block with an infinity or a NaN has the scale NaN and codes 0: its token's
  * outputs are NaN, and no other token's are.  A layer is
  *   y[m][n] = act(sum_b scale[m][b] weight_scale[n][b] sum_{k in b} value[m][k] weight_value[n][k] + bias[n])

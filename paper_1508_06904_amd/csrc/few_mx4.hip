@@ -6,8 +6,8 @@
 // sums are added through LDS in the order of K.  The few rows' codes are in LDS for all of a workgroup's waves; few tokens
 // that are values yet are coded there.
 //
-// One token of 9216 channels to 512 outputs: 6.7 us, of which an empty launch is 2; 13 of 4096 to 16384 as codes 12.5 us (36 MB,
-// 2.9 TB/s), as values 17.4, since each workgroup codes them.  Half as many waves for each row (so that all 512 resident
+// One token of 9216 channels to 512 outputs: 6.4 us in a captured graph, of which an empty launch is 2, and 7.8 between other
+// calls; 13 of 4096 to 16384 as codes 12.5 us (36 MB, 2.9 TB/s), as values 16.3 to 17.6, since each workgroup codes them.  Half as many waves for each row (so that all 512 resident
 // workgroups have some) took 14.2 and 21.9 us; the few rows loaded 8 at a time, not as they come, 12.5 and 17.5.
 #include <algorithm>
 
@@ -298,8 +298,10 @@ hipError_t launch_few_mx4(const Mx4Layer& L, dss_dtype out_dtype, hipStream_t s)
 }
 
 // Up to 65536 values: at 16 x 4096 to 4096 outputs the GPU takes 14.4 us for 13.2 in two launches, but the call 10 for 15 where its
-// launches are what bounds it; with twice as many values the GPU is what does.
-bool few_codes_itself(int64_t M, int64_t N, int64_t K) {
+// launches are what bounds it; with twice as many values the GPU is what does. Where calls cost nothing, in a captured graph,
+// one launch is the faster one for 9216 channels of one token to 512 outputs (6.4 us for 8.9) and the slower one for wide layers
+// (13.2 for 11.9 at 16 x 4096 to 4096, 16.3 for 15.7 at 13 x 4096 to 16384), for the workspace that it does without.
+bool few_codes_itself(int64_t M, int64_t K) {
     return M <= 16 && M * K <= 65536;
 }
 

@@ -149,8 +149,8 @@ constexpr int64_t kLeastTokens = 256;
 //   100000                 27/36     25/36     29/39     52/55     58/73              25/35    23/30     42/46     43/54
 //   400000                135/150    95/125   117/146   201/249   238/295            129/136   74/99    168/211   156/212
 // The rule takes all of them from 32768 tokens on; few outputs of few channels, where the two are about as fast on the GPU,
-// for the launch and the workspace that a call then does without, from 256 on.  1.88 million bfloat16 tokens of 64
-// channels to 256 outputs lose (697/645): they are the only ones measured.
+// for the launch and the workspace that a call then does without, from 256 on.  Two of those measured lose: 1.88 million bfloat16
+// tokens of 64 channels to 256 outputs (697/645) and 1000 binary32 tokens of 256 channels to 64 (9/8; in a captured graph 8.6/7.7).
 bool linear_mx4_at_once(int64_t M, int64_t N, int64_t K, bool map) {
     const bool fits = map && K <= 512 && weights_lds(N, (int)blocks_of(K)) <= 72 * 1024;
     return fits && (M >= 32768 || (M >= kLeastTokens && N <= 64 && K <= 256));

@@ -2,8 +2,9 @@
 //   y[m][n] = act(sum_b X[b][m] W[b][n] sum_{k in b} q[m][k] v[n][k] + bias[n]),
 // on v_mfma_scale_f32_16x16x128_f8f6f4, whose binary32 sums take the blocks' scales with them.
 //
-// Bound by the matrix units where all sides are large: 8192 x 8192 x 8192 to bfloat16 297 - 303 us, 3.65 PFLOP/s (a library's product of
-// the same format 340 us); by latency where they are not: 1777 x 2305 x 1003 11 - 14 us.
+// Bound by the matrix units where all sides are large: 8192 x 8192 x 8192 to bfloat16 297 to 303 us in long runs of calls, 3.65
+// PFLOP/s (a library's product of the same format 340 us), and 320 to 350 in the first hundred after a pause; by latency where
+// they are not: 1777 x 2305 x 1003 11 to 14 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -448,7 +449,7 @@ extern "C" dss_status dss_blocks_workspace(int64_t M, int32_t N, int32_t K, dss_
         return fail(DSS_E_INVALID, "unknown token source %d", (int)source);
     if (source != DSS_TOKENS_CODES && M > ((int64_t)1 << 62) / (blocks_of(K) * 17))
         return fail(DSS_E_INVALID, "the codes of %lld tokens of %d channels", (long long)M, K);
-    const bool none = source == DSS_TOKENS_CODES || few_codes_itself(M, N, K) || linear_mx4_at_once(M, N, K, source == DSS_TOKENS_MAP);
+    const bool none = source == DSS_TOKENS_CODES || few_codes_itself(M, K) || linear_mx4_at_once(M, N, K, source == DSS_TOKENS_MAP);
     *workspace_bytes = none ? 0 : workspace_bytes_of(M, blocks_of(K));
     return DSS_OK;
 } catch (...) {
@@ -492,7 +493,7 @@ extern "C" dss_status dss_linear_blocks(const void* x, dss_dtype dtype, int64_t 
     if (s != DSS_OK) return s;
     s = check_room(need, workspace, workspace_bytes);
     if (s != DSS_OK) return s;
-    const bool few = few_codes_itself(M, N, K);
+    const bool few = few_codes_itself(M, K);
     if (few || linear_mx4_at_once(M, N, K, from_map)) {
         const Mx4Layer L = layer_of({nullptr, 0, nullptr, 0, M}, W, B, bias, act, out, out_dtype, out_token_stride, out_channel_stride);
         const Mx4Values X = {x, dtype, K, token_stride, channel_stride};

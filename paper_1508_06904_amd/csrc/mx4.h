@@ -54,7 +54,7 @@ hipError_t launch_linear_mx4(const Mx4Layer& L, const Mx4Values& X, dss_dtype ou
 // us for 10.9, 32 x 9216 to 8192 17 for 31 (but 17 x 9216 to 512 14.9 for 10.1).
 constexpr int kFewRows = 16;
 hipError_t launch_few_mx4(const Mx4Layer& L, dss_dtype out_dtype, hipStream_t s);
-bool few_codes_itself(int64_t M, int64_t N, int64_t K);
+bool few_codes_itself(int64_t M, int64_t K);
 hipError_t launch_linear_few_mx4(const Mx4Layer& L, const Mx4Values& X, dss_dtype out_dtype, hipStream_t s);
 
 }  // namespace dss

@@ -38,7 +38,8 @@ inline int pick_tile(const TileTime* tiles_of, int n, int64_t I, int64_t J, int 
 inline int pick_tile(int64_t I, int64_t J, int K) { return pick_tile(kTiles, 4, I, J, K); }
 
 // The tiles of the 4-bit products, whose step of kStep bytes has twice the channels, and the index of the one for I x J
-// outputs of B blocks.  Microseconds on 256, 128 and 64: 8192 x 8192 x 8192 346, 465, 853;
+// outputs of B blocks.  Microseconds on 256, 128 and 64, a few calls after a pause (the first one 300 in long runs):
+// 8192 x 8192 x 8192 346, 465, 853;
 // 4096 x 4096 x 4096 47, 56, 83; 2048 x 4096 x 4096 39, 30, 45; 512 x 4096 x 4096 37, 24, 12.7; 1777 x 1003 x 2305 32, 19,
 // 11.2; 300 x 300 x 2304 23, 12, 7.0; 100000 x 512 x 256 44, 43, 54; 128 x 8192 x 9216 70, 46, 19.
 constexpr TileTime kMx4Tiles[] = {{256, 1, 1, 2.4, 0, 7.0}, {128, 1, 2, 1.2, 0.4, 4.5}, {64, 1, 3, 0.42, 0.13, 3.0}};
